@@ -432,6 +432,128 @@ dkv_status_t dkv_candidate_order_noalloc(const void* K_bank, const float* base, 
                                          int32_t N, int32_t d, int32_t dtype, const dkv_params_t* params,
                                          float* scores_out, int32_t* perm_out, void* stream);
 
+/* ------------------------------------------------------------------------------------
+ * Paged cache of the window's keys and values.
+ *
+ * The window that attention reads beside the bank (Sec. 4.1, App. D: one sink frame and
+ * the most recent frames) moves on with every block.  A cache keeps its keys and values
+ * in pages of page_len positions, so that the pages of positions that have left the
+ * window are given to new ones and nothing is moved.  Three calls:
+ *
+ *   dkv_cache_write    the newest tokens' keys and values into their pages, as they are
+ *                      or quantised on the way in
+ *   dkv_cache_read     a range of positions back as dense rows: the block that leaves the
+ *                      window on its way to dkv_bank_admit, or the K_w, V_w of
+ *                      dkv_bank_attend
+ *   dkv_cache_attend   softmax attention of the newest tokens over their sequence's cached
+ *                      keys, causal by blocks, with a sliding window and sinks
+ *
+ * Sequences.  A call covers n_seq sequences of different lengths.  Sequence b holds
+ * seq_len[b] positions, those of the call's own tokens included; its n_b newest tokens are
+ * rows row_start[b] .. row_start[b + 1] - 1 of the packed tensors, at the positions
+ * seq_len[b] - n_b .. seq_len[b] - 1.  Position j is slot j % page_len of page
+ * block_table[b][j / page_len].  Sequences may share pages that a call only reads; the
+ * slots that one write call fills must be different.  Table entries of positions that a
+ * call does not touch are not read.  The arrays are read on the device during the call's
+ * work, so a captured call follows what they hold when it is replayed.
+ *
+ * A row_start that decreases or passes the call's rows, a length above max_pages * page_len,
+ * a page outside [0, n_pages) in a touched place, or more than max_rows tokens in one
+ * sequence set the sticky error word (DKV_ERR_DEVICE, see dkv_cache_sync); the call
+ * stays inside its buffers, and what it does for the sequences at fault is unspecified.
+ *
+ * Packed tensors are [heads][rows][d] bf16 with any strides (in elements) between heads and
+ * rows that are multiples of 8; d is contiguous and the address 16-byte aligned.
+ *
+ * A handle keeps no state between calls but the error word.  Calls on it may run at once
+ * on several streams, in graphs too, each attend with scratch of its own; a write and the
+ * calls that touch the same pages are ordered by the caller.  Every call runs on the device
+ * that was current when the handle was created, whichever is current when it is made.    */
+typedef struct dkv_cache_s* dkv_cache_t;
+
+/* DKV_CACHE_BF16: keys and values as they are.  DKV_CACHE_E4M3: 8-bit codes (sign, 4
+ * exponent and 3 mantissa bits) and for each (position, head) row of d values one scale, a
+ * power of two 2^e stored as the byte e + 127: e is the smallest integer >= -110 with
+ * max |x| <= 448 2^e, 0 for a row of zeros, and code = x 2^-e to nearest, ties to even (a
+ * code that would stand for 2^128, more than bf16 holds, is the one below).  A row that
+ * holds a NaN or an infinity gets the byte 255 and reads back as NaN in all d places.  code 2^e
+ * is exact in bf16, so reading back and attending see the same numbers.                  */
+typedef enum { DKV_CACHE_BF16 = 0, DKV_CACHE_E4M3 = 1 } dkv_cache_format_t;
+
+typedef struct {
+  void* k;             /* device [n_pages][H][page_len][d] bf16, or one byte codes; 128-byte aligned */
+  void* v;             /* the same for the values                                          */
+  uint8_t* k_scale;    /* device [n_pages][H][page_len] scale bytes, 16-byte aligned (e4m3;  */
+  uint8_t* v_scale;    /*   ignored for bf16)                                              */
+  int32_t* status;     /* device [2], private to the handle: the error word                */
+} dkv_cache_buffers_t;
+
+typedef struct {
+  const int32_t* block_table;   /* device [n_seq][max_pages]                               */
+  const int32_t* seq_len;       /* device [n_seq]                                          */
+  const int32_t* row_start;     /* device [n_seq + 1]                                      */
+  int32_t n_seq;                /* 1 .. 4096                                               */
+  int32_t max_pages;            /* >= 1, max_pages * page_len <= 2^30                      */
+} dkv_cache_seqs_t;
+
+/* What a token at position p of a sequence of L positions sees.  With
+ * end(p) = min(L, (p / block + 1) block), or L when block = 0, position j is visible when
+ *   j < end(p)  and  (window = 0  or  j >= end(p) - window  or  j < sinks).
+ * block = 1 is causal attention; block = 4680 the block-causal attention of 3-frame blocks
+ * (a token sees its whole block); block = 0 has no causal mask.                            */
+typedef struct {
+  float scale;         /* of q.k; <= 0 selects 1 / sqrt(d)                                 */
+  int32_t window;      /* >= 0; 0: no limit                                                */
+  int32_t sinks;       /* >= 0; no effect without a window                                 */
+  int32_t block;       /* >= 0                                                             */
+  int32_t max_rows;    /* most tokens of any one sequence in the call, >= 1; the choice of
+                          kernel goes by it (1 when every sequence brings one token)       */
+} dkv_cache_attend_t;
+
+/* Creates a handle over caller-owned pages.  Clears the error word (synchronously) and
+ * touches nothing else.  Limits: 1 <= H <= 4096, d in {64, 128}, page_len in {16, 32, 64,
+ * 128, 256}, 1 <= n_pages <= 2^30.                                                        */
+dkv_status_t dkv_cache_create(dkv_cache_t* out, int32_t H, int32_t d, int32_t page_len, int32_t n_pages,
+                              int32_t format, const dkv_cache_buffers_t* buffers);
+
+/* Releases the handle (the pages are untouched).  Safe on NULL. */
+void dkv_cache_destroy(dkv_cache_t cache);
+
+/* K, V: device [H][rows][d] bf16, the newest tokens of every sequence; 1 <= rows <= 1<<20.
+ * Rows from row_start[n_seq] on and tokens at negative positions are ignored.             */
+dkv_status_t dkv_cache_write(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const void* K, const void* V,
+                             int32_t rows, int64_t k_head_stride, int64_t k_row_stride, int64_t v_head_stride,
+                             int64_t v_row_stride, void* stream);
+
+/* Row row_start[b] + i of K, V (device [H][rows][d] bf16) := position first[b] + i of
+ * sequence b; positions outside [0, seq_len[b]) give zeros.  first: device int32 [n_seq].
+ * Rows from row_start[n_seq] on are left as they were.                                    */
+dkv_status_t dkv_cache_read(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const int32_t* first, void* K, void* V,
+                            int32_t rows, int64_t k_head_stride, int64_t k_row_stride, int64_t v_head_stride,
+                            int64_t v_row_stride, void* stream);
+
+/* Scratch bytes of an attend call with these arguments (0: invalid arguments). */
+size_t dkv_cache_attend_scratch_size(dkv_cache_t cache, int32_t n_seq, int32_t H_q, int32_t rows, int32_t max_rows);
+
+/* O[h][i] = sum_j softmax_j(scale Q[h][i] . K[j]) V[j] over the positions j that token i of
+ * its sequence sees (dkv_cache_attend_t) in key head h / (H_q / H).
+ *   Q, O : device [H_q][rows][d] bf16; H_q a multiple of H, at most 128 times it; 1 <= rows <= 1<<20.
+ *   scratch : device, 256-byte aligned, >= dkv_cache_attend_scratch_size(); in use until the
+ *             call's work has completed.
+ * A token that sees no position (a negative position of its own, an empty sequence) gets
+ * zeros.  Rows from row_start[n_seq] on are left as they were.  What lies in places that a
+ * token does not see, NaN and infinities too, does not reach its output.  Scores, sums and
+ * outputs are held in fp32; the weights are rounded to bf16 before they meet the values.
+ * The order of the sums follows from the sizes and arrays of the call and from the device.  */
+dkv_status_t dkv_cache_attend(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const void* Q, int32_t H_q,
+                              int32_t rows, int64_t q_head_stride, int64_t q_row_stride, void* O,
+                              int64_t o_head_stride, int64_t o_row_stride, const dkv_cache_attend_t* how,
+                              void* scratch, size_t scratch_bytes, void* stream);
+
+/* Waits for the stream of the handle's last call, then reports and clears the error word
+ * (as dkv_bank_sync).                                                                     */
+dkv_status_t dkv_cache_sync(dkv_cache_t cache);
+
 #ifdef __cplusplus
 }
 #endif

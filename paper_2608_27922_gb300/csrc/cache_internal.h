@@ -1,0 +1,126 @@
+// The paged cache (include/dkv.h): what its host API and kernels share.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "dkv_device.cuh"
+#include "dkv_internal.h"
+
+namespace dkv {
+namespace cache {
+
+// Pages, [n_pages][H][page_len][d] codes (bf16 or e4m3) and [n_pages][H][page_len] scale bytes.
+struct Pool {
+  void* k;
+  void* v;
+  uint8_t* ks;
+  uint8_t* vs;
+  int32_t* status;   // sticky error word, first failing site
+  int H, d, page_len, page_log2, n_pages;
+  int e4m3;
+};
+
+// The sequences of a call (device arrays).
+struct Seqs {
+  const int32_t* table;
+  const int32_t* len;
+  const int32_t* row_start;
+  int n, max_pages;
+  int rows;   // packed rows of the call's tensors
+};
+
+// Packed tensors [heads][rows][d].
+struct Packed {
+  void* p;
+  int64_t head, row;   // strides in elements
+};
+
+struct Mask {
+  float sl2;   // scale * log2(e)
+  int window, sinks, block;
+};
+
+enum : int { SITE_ROWS = 1, SITE_LEN = 2, SITE_PAGE = 3, SITE_CHUNK = 4, SITE_WAIT = 400 };
+
+#ifdef __CUDACC__
+// (The index arithmetic below also compiles for the host, where a test walks its bounds.)
+__host__ __device__ __forceinline__ void fail(int32_t* status, int32_t code, int32_t site) {
+#ifdef __CUDA_ARCH__
+  if (atomicCAS(status, 0, code) == 0) atomicExch(status + 1, site);
+#else
+  if (status[0] == 0) {
+    status[0] = code;
+    status[1] = site;
+  }
+#endif
+}
+
+__host__ __device__ __forceinline__ int clamp(int x, int lo, int hi) { return x < lo ? lo : x > hi ? hi : x; }
+
+// One sequence as the call may use it: its rows inside the tensors, its length inside the table.
+struct Seq {
+  int r0, n, len;
+};
+
+__host__ __device__ __forceinline__ Seq seq_at(const Pool& c, const Seqs& s, int b) {
+  Seq q;
+  const int a = s.row_start[b], z = s.row_start[b + 1], len = s.len[b];
+  const int64_t cap = (int64_t)s.max_pages << c.page_log2;
+  q.r0 = clamp(a, 0, s.rows);
+  q.n = clamp(z, q.r0, s.rows) - q.r0;
+  q.len = clamp(len, 0, (int)cap);
+  if (a < 0 || z < a || z > s.rows) fail(c.status, DEV_INCONSISTENT, SITE_ROWS);
+  if (len < 0 || len > cap) fail(c.status, DEV_INCONSISTENT, SITE_LEN);
+  return q;
+}
+
+// The sequence of a packed row (row < row_start[n]): the last b with row_start[b] <= row.
+__host__ __device__ __forceinline__ int seq_of_row(const Seqs& s, int row) {
+  int lo = 0, hi = s.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (s.row_start[mid] <= row) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Row of position pos (0 <= pos < table's positions) of sequence b and head h in the pool, -1
+// where the table names no page of it.
+__host__ __device__ __forceinline__ int64_t pool_row(const Pool& c, const Seqs& s, int b, int h, int pos) {
+  const int page = s.table[(int64_t)b * s.max_pages + (pos >> c.page_log2)];
+  if ((unsigned)page >= (unsigned)c.n_pages) {
+    fail(c.status, DEV_INCONSISTENT, SITE_PAGE);
+    return -1;
+  }
+  return (((int64_t)page * c.H + h) << c.page_log2) + (pos & (c.page_len - 1));
+}
+
+// 2^(byte - 127); the byte 255 is NaN.  Bytes are at least 17 (e >= -110) in rows that the cache wrote.
+__device__ __forceinline__ float scale_of(uint32_t byte) {
+  return byte == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(byte << 23);
+}
+
+// end(p) of include/dkv.h.
+__host__ __device__ __forceinline__ int visible_end(const Mask& m, int p, int len) {
+  if (m.block == 0) return len;
+  const int64_t e = ((int64_t)(p / m.block) + 1) * m.block;
+  return e < len ? (int)e : len;
+}
+// First position of the window that ends there (the sinks before it are visible too).
+__host__ __device__ __forceinline__ int window_first(const Mask& m, int end) {
+  return m.window == 0 || m.window > end ? 0 : end - m.window;
+}
+#endif
+
+cudaError_t launch_write(const Pool& c, const Seqs& s, const Packed& k, const Packed& v, cudaStream_t st);
+cudaError_t launch_read(const Pool& c, const Seqs& s, const int32_t* first, const Packed& k, const Packed& v,
+                        cudaStream_t st);
+size_t attend_scratch(const Pool& c, int n_seq, int Hq, int rows, int max_rows);
+cudaError_t launch_attend(const Pool& c, const Seqs& s, const Packed& q, const Packed& o, int Hq, int max_rows,
+                          const Mask& m, void* scratch, cudaStream_t st);
+
+}  // namespace cache
+}  // namespace dkv

@@ -61,9 +61,25 @@ class dkv_intermediates_t(ctypes.Structure):
                 ("M_max", ctypes.c_int64)]
 
 
+class dkv_cache_buffers_t(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class dkv_cache_seqs_t(ctypes.Structure):
+    _fields_ = [("block_table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("row_start", ctypes.c_void_p),
+                ("n_seq", ctypes.c_int32), ("max_pages", ctypes.c_int32)]
+
+
+class dkv_cache_attend_t(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("block", ctypes.c_int32), ("max_rows", ctypes.c_int32)]
+
+
 # (name, restype, argtypes) of every exported symbol declared in include/dkv.h
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
+_L = ctypes.c_int64
 SIGNATURES = [
     ("dkv_status_str", ctypes.c_char_p, [_I]),
     ("dkv_version", _I, []),
@@ -94,6 +110,14 @@ SIGNATURES = [
     ("dkv_selftest_wait_timeout", _I, [_I, ctypes.POINTER(ctypes.c_int64)]),
     ("dkv_sequential_scratch_size", ctypes.c_size_t, [_I, _I, _I, _I]),
     ("dkv_bank_update_sequential", _I, [_P, _P, _P, _I, ctypes.c_int64, _P, ctypes.c_size_t, _P]),
+    ("dkv_cache_create", _I, [ctypes.POINTER(_P), _I, _I, _I, _I, _I, ctypes.POINTER(dkv_cache_buffers_t)]),
+    ("dkv_cache_destroy", None, [_P]),
+    ("dkv_cache_write", _I, [_P, ctypes.POINTER(dkv_cache_seqs_t), _P, _P, _I, _L, _L, _L, _L, _P]),
+    ("dkv_cache_read", _I, [_P, ctypes.POINTER(dkv_cache_seqs_t), _P, _P, _P, _I, _L, _L, _L, _L, _P]),
+    ("dkv_cache_attend_scratch_size", ctypes.c_size_t, [_P, _I, _I, _I, _I]),
+    ("dkv_cache_attend", _I, [_P, ctypes.POINTER(dkv_cache_seqs_t), _P, _I, _I, _L, _L, _P, _L, _L,
+                              ctypes.POINTER(dkv_cache_attend_t), _P, ctypes.c_size_t, _P]),
+    ("dkv_cache_sync", _I, [_P]),
 ]
 
 DKV_NOALLOC_MAX_N = 16384
@@ -479,3 +503,166 @@ class BankLayer:
 
     def kernel_times(self):
         return dkv_bank_kernel_times(self.handle)
+
+
+# ----------------------------------------------------------------- paged cache of the window
+DKV_CACHE_BF16, DKV_CACHE_E4M3 = 0, 1
+_CACHE_FORMAT = {"bf16": DKV_CACHE_BF16, "e4m3": DKV_CACHE_E4M3}
+
+
+class CacheSeqs:
+    """The sequences of a cache call (device int32 tensors, see include/dkv.h): block_table
+    [n_seq][max_pages], seq_len [n_seq], row_start [n_seq + 1].  The tensors are kept and read when
+    the calls' work runs; a program updates them in place between calls."""
+
+    def __init__(self, block_table: torch.Tensor, seq_len: torch.Tensor, row_start: torch.Tensor):
+        n = seq_len.numel()
+        for t, shape, name in ((block_table, (n, block_table.shape[-1]), "block_table"), (seq_len, (n,), "seq_len"),
+                               (row_start, (n + 1,), "row_start")):
+            if (t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous()
+                    or t.device != seq_len.device or not t.is_cuda):
+                raise ValueError(f"{name}: expected contiguous {torch.int32} {shape} on one CUDA device, "
+                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        self.block_table, self.seq_len, self.row_start = block_table, seq_len, row_start
+        self.n_seq, self.device = n, seq_len.device
+        self._c = dkv_cache_seqs_t(block_table.data_ptr(), seq_len.data_ptr(), row_start.data_ptr(), n,
+                                   block_table.shape[-1])
+        self._ref = ctypes.byref(self._c)
+
+
+class PagedCache:
+    """Keys and values of H heads in pages of page_len positions, bf16 or quantised to e4m3
+    ("bf16" / "e4m3"): allocates the pages with torch, or takes them (k, v and, for e4m3, k_scale,
+    v_scale), and drives the C ABI.  Packed tensors are [heads][rows][d] bf16 with any strides that
+    are multiples of 8 between heads and rows.  All methods enqueue on the current (or given)
+    stream; a call on another stream than the one its tensors were made on is ordered by the caller."""
+
+    def __init__(self, H: int, d: int, page_len: int, n_pages: int, fmt: str = "bf16", device="cuda",
+                 k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None,
+                 k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None):
+        if fmt not in _CACHE_FORMAT:
+            raise ValueError(f"fmt: expected one of {sorted(_CACHE_FORMAT)}, got {fmt!r}")
+        dev = k.device if k is not None else torch.device(device)
+        if dev.type == "cuda" and dev.index is None:
+            dev = torch.device("cuda", torch.cuda.current_device())
+        self.H, self.d, self.page_len, self.n_pages, self.fmt, self.device = H, d, page_len, n_pages, fmt, dev
+        e4m3 = fmt == "e4m3"
+
+        def pages(t, dtype, shape, name):
+            if t is None:
+                return torch.zeros(shape, dtype=torch.uint8 if dtype.itemsize == 1 else dtype, device=dev).view(dtype)
+            if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != dev:
+                raise ValueError(f"{name}: expected contiguous {dtype} {shape} on {dev}, "
+                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+            return t
+        shape = (n_pages, H, page_len, d)
+        self.k = pages(k, torch.float8_e4m3fn if e4m3 else torch.bfloat16, shape, "k")
+        self.v = pages(v, torch.float8_e4m3fn if e4m3 else torch.bfloat16, shape, "v")
+        self.k_scale = pages(k_scale, torch.uint8, shape[:3], "k_scale") if e4m3 else None
+        self.v_scale = pages(v_scale, torch.uint8, shape[:3], "v_scale") if e4m3 else None
+        self._status = torch.zeros(2, dtype=torch.int32, device=dev)
+        bufs = dkv_cache_buffers_t(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr() if e4m3 else None,
+                                   self.v_scale.data_ptr() if e4m3 else None, self._status.data_ptr())
+        h = ctypes.c_void_p()
+        with torch.cuda.device(dev):
+            _check(lib().dkv_cache_create(ctypes.byref(h), H, d, page_len, n_pages, _CACHE_FORMAT[fmt],
+                                          ctypes.byref(bufs)), "dkv_cache_create")
+        self.handle = h.value
+        self._scratch_size: Dict[Tuple[int, int, int, int], int] = {}
+        self._how: Dict[tuple, dkv_cache_attend_t] = {}
+
+    def close(self):
+        if getattr(self, "handle", None):
+            lib().dkv_cache_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _packed(self, t: torch.Tensor, heads: int, rows: int, name: str):
+        """Strides of a packed tensor between heads and rows."""
+        s = t.stride()
+        if t.dtype != torch.bfloat16 or t.shape != (heads, rows, self.d) or t.device != self.device or s[2] != 1:
+            raise ValueError(f"{name}: expected {torch.bfloat16} {(heads, rows, self.d)} with contiguous rows on "
+                             f"{self.device}, got {t.dtype} {tuple(t.shape)}, strides {s}, on {t.device}")
+        return s
+
+    def _on(self, stream):
+        """The stream of a call, and a context in which torch allocates for it."""
+        if stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream, None
+        if not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=self.device)
+        return stream.cuda_stream, torch.cuda.stream(stream)
+
+    def _new(self, ctx, *shape, dtype=torch.bfloat16):
+        if ctx is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with ctx:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def _seqs(self, seqs: CacheSeqs):
+        if seqs.device != self.device:
+            raise ValueError(f"seqs: expected tensors on {self.device}, got {seqs.device}")
+        return seqs._ref
+
+    def write(self, K: torch.Tensor, V: torch.Tensor, seqs: CacheSeqs, stream=None) -> None:
+        """The sequences' newest tokens K, V [H][rows][d] into their pages (quantised if fmt is e4m3)."""
+        rows = K.shape[1]
+        k, v = self._packed(K, self.H, rows, "K"), self._packed(V, self.H, rows, "V")
+        s, _ = self._on(stream)
+        _check(lib().dkv_cache_write(self.handle, self._seqs(seqs), K.data_ptr(), V.data_ptr(), rows, k[0], k[1], v[0],
+                                     v[1], s), "dkv_cache_write")
+
+    def read(self, seqs: CacheSeqs, first: torch.Tensor, rows: int, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
+             stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Positions first[b], first[b] + 1, .. of every sequence as rows row_start[b] .. of K, V
+        [H][rows][d]; positions that a sequence does not hold are zeros."""
+        if (first.dtype != torch.int32 or tuple(first.shape) != (seqs.n_seq,) or not first.is_contiguous()
+                or first.device != self.device):
+            raise ValueError(f"first: expected contiguous {torch.int32} {(seqs.n_seq,)} on {self.device}")
+        s, ctx = self._on(stream)
+        K, V = out if out is not None else (self._new(ctx, self.H, rows, self.d), self._new(ctx, self.H, rows, self.d))
+        k, v = self._packed(K, self.H, rows, "K"), self._packed(V, self.H, rows, "V")
+        _check(lib().dkv_cache_read(self.handle, self._seqs(seqs), first.data_ptr(), K.data_ptr(), V.data_ptr(), rows,
+                                    k[0], k[1], v[0], v[1], s), "dkv_cache_read")
+        return K, V
+
+    def attend(self, Q: torch.Tensor, seqs: CacheSeqs, window: int = 0, sinks: int = 0, block: int = 1,
+               scale: Optional[float] = None, max_rows: Optional[int] = None, out: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+        """Attention of the sequences' newest tokens Q [H_q][rows][d] over their cached keys (the
+        mask of dkv_cache_attend_t).  max_rows: the most tokens of any one sequence, 1 when every
+        sequence brings one (default: all rows)."""
+        Hq, rows = Q.shape[0], Q.shape[1]
+        q = self._packed(Q, Hq, rows, "Q")
+        most = rows if max_rows is None else min(int(max_rows), rows)
+        key = (seqs.n_seq, Hq, rows, most)
+        size = self._scratch_size.get(key)
+        if size is None:
+            if len(self._scratch_size) > 4096:
+                self._scratch_size.clear()
+            size = self._scratch_size[key] = int(lib().dkv_cache_attend_scratch_size(self.handle, *key))
+        how = (scale, window, sinks, block, most)
+        h = self._how.get(how)
+        if h is None:
+            if scale is not None and not scale > 0.0:
+                raise ValueError("scale: expected a positive number")
+            if len(self._how) > 4096:
+                self._how.clear()
+            h = self._how[how] = dkv_cache_attend_t(0.0 if scale is None else scale, window, sinks, block, most)
+        s, ctx = self._on(stream)
+        if out is None:
+            out = self._new(ctx, Hq, rows, self.d)
+        o = self._packed(out, Hq, rows, "out")
+        scratch = self._new(ctx, size, dtype=torch.uint8)
+        _check(lib().dkv_cache_attend(self.handle, self._seqs(seqs), Q.data_ptr(), Hq, rows, q[0], q[1],
+                                      out.data_ptr(), o[0], o[1], ctypes.byref(h), scratch.data_ptr(), size, s),
+               "dkv_cache_attend")
+        return out
+
+    def sync(self) -> None:
+        _check(lib().dkv_cache_sync(self.handle), "dkv_cache_sync")
