@@ -11,6 +11,7 @@ using namespace dkv;
 
 struct dkv_cache_s {
   cache::Pool pool{};
+  cache::Maps maps{};
   int device = 0;
   std::atomic<cudaStream_t> last{nullptr};   // (calls may come from several threads)
 };
@@ -92,6 +93,7 @@ dkv_status_t dkv_cache_create(dkv_cache_t* out, int32_t H, int32_t d, int32_t pa
   if (taken(cudaGetDevice(&dev)) != cudaSuccess) return DKV_ERR_CUDA;
   if (taken(cudaGetDeviceProperties(&prop, dev)) != cudaSuccess) return DKV_ERR_CUDA;
   if (prop.major != 10 || prop.minor != 3) return DKV_ERR_UNSUPPORTED;   // built for sm_103a only
+  if (cache::attend_tc_set_smem_limits() != cudaSuccess) return DKV_ERR_CUDA;
   if (taken(cudaMemset(buf->status, 0, 2 * sizeof(int32_t))) != cudaSuccess) return DKV_ERR_CUDA;
   dkv_cache_s* c = new (std::nothrow) dkv_cache_s();
   if (!c) return DKV_ERR_ARG;
@@ -100,6 +102,10 @@ dkv_status_t dkv_cache_create(dkv_cache_t* out, int32_t H, int32_t d, int32_t pa
   c->pool = cache::Pool{buf->k, buf->v, e4m3 ? buf->k_scale : nullptr, e4m3 ? buf->v_scale : nullptr, buf->status,
                         H, d, page_len, log2, n_pages, e4m3 ? 1 : 0};
   c->device = dev;
+  if (!cache::make_maps(c->pool, &c->maps)) {
+    delete c;
+    return DKV_ERR_CUDA;
+  }
   *out = c;
   return DKV_OK;
 }
@@ -166,7 +172,7 @@ dkv_status_t dkv_cache_attend(dkv_cache_t c, const dkv_cache_seqs_t* seqs, const
   OnDevice on(c->device);
   if (!on.ok) return DKV_ERR_CUDA;
   c->last = (cudaStream_t)stream;
-  return status_of(cache::launch_attend(c->pool, s, q, o, H_q, max_rows, m, scratch, (cudaStream_t)stream));
+  return status_of(cache::launch_attend(c->pool, c->maps, s, q, o, H_q, max_rows, m, scratch, (cudaStream_t)stream));
 }
 
 dkv_status_t dkv_cache_sync(dkv_cache_t c) {

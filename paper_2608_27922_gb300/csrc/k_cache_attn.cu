@@ -79,10 +79,11 @@ __global__ void __launch_bounds__(WARPS * 32) cache_attend_simple(Pool c, Seqs s
 
 }  // namespace
 
-size_t attend_scratch(const Pool&, int, int, int, int) { return 256; }
+size_t attend_scratch(const Pool& c, int, int, int, int) { return attend_tc_scratch(c); }
 
-cudaError_t launch_attend(const Pool& c, const Seqs& s, const Packed& q, const Packed& o, int Hq, int max_rows,
-                          const Mask& m, void*, cudaStream_t st) {
+cudaError_t launch_attend(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
+                          int max_rows, const Mask& m, void* scratch, cudaStream_t st) {
+  if (max_rows * (Hq / c.H) > 16) return launch_attend_tc(c, maps, s, q, o, Hq, max_rows, m, scratch, st);
   const dim3 grid((s.rows + WARPS - 1) / WARPS, Hq);
   auto* f = c.d == 128 ? (c.e4m3 ? cache_attend_simple<128, true> : cache_attend_simple<128, false>)
                        : (c.e4m3 ? cache_attend_simple<64, true> : cache_attend_simple<64, false>);

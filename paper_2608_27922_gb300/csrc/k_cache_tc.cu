@@ -1,0 +1,917 @@
+// Attention of chunks of tokens over the paged cache on the tensor cores (include/dkv.h: dkv_cache_attend).
+//
+// A unit is two tiles of 128 query rows of one sequence and one key head.  With G query heads on a
+// key head a tile holds TQ = 128 / G tokens, row = token * G + head, so that all of a group's
+// queries meet a key tile in one product.  The unit's visible keys, in tiles of 128 positions (the sinks'
+// tiles, then the window's), stream past both query tiles:
+//   S_g = Q_g K^T            tcgen05.mma into TMEM, one softmax warpgroup a tile, thread = query row
+//   P_g = exp2(S_g scale log2(e) - m_g)   packed bf16 over S_g in TMEM; what a row does not see is 0
+//   O_g += P_g V             tcgen05.mma with A = P_g from TMEM
+// with the running maximum raised only when a tile's exceeds it by more than 2^8 (O_g is then
+// rescaled in TMEM).  Bound by the tensor pipe (4 d flops a row and key) and close to it by the exponentials.
+//
+// Pages come in by TMA, one box a page and 64-column panel, in the layout that the products read.
+// A quantised cache's codes land beside that layout and four warps turn them into bf16 in place
+// of the copy: code bits shifted into bf16's fields are the value times 2^-120, one product with
+// 2^120 times the row's scale makes it exact (bf16 holds every code times its scale).
+//
+// Persistent: one CTA an SM walks items (whole units; the last ones, where they do not fill the SMs, cut
+// into equal parts of their key tiles, joined by cache_merge).  The producer warp runs one item
+// ahead and every barrier runs on from item to item, so that an item's first products are
+// issued while the previous one's outputs are still being stored.
+//
+// Values in places that a row does not see meet its weight 0, and 0 times a NaN or an infinity
+// is NaN.  So in a tile that some row does not see whole, the softmax warps first clear what is
+// not finite in V's tile; rows that do see such a value get it back at the end (wild_masks).
+#include "attn_math.cuh"
+#include "cache_internal.h"
+#include "tc_ptx.cuh"
+
+#include <algorithm>
+
+namespace dkv {
+
+bool make_map_4d(CUtensorMap* m, const void* base, int elem_bytes, const int64_t (&dim)[4], const int64_t (&stride)[3],
+                 const int (&box)[4], bool swizzle);
+
+namespace cache {
+
+namespace {
+
+using namespace tc;
+
+constexpr int BQ = 128, BK = 128;        // query rows of a tile, keys of a tile
+constexpr int PANEL = 128 * 128;         // bytes of a 64-column panel of 128 rows
+constexpr uint32_t TMEM_COLS = 512;      // S_0 [0,128), O_0 [128,256), S_1 [256,384), O_1 [384,512)
+constexpr float RESCALE_LOG2 = 8.0f;
+constexpr int MAX_CTAS = 152;            // persistent CTAs (the SMs of the GPU): sizes the scratch
+constexpr int MAX_PARTS = 3 * MAX_CTAS;  // parts of cut units
+constexpr int MAX_CUT = 32;              // parts of one unit
+constexpr int MIN_PART = 4;              // key tiles of a part, at least
+// What an item costs beside its key tiles, and the joining of parts, in key tiles (1.1 us each at
+// two query tiles of 128 dimensions)
+constexpr int ITEM_TILES = 2, JOIN_TILES = 6;
+
+template <int D, bool E4M3>
+struct Lay {
+  static constexpr int NP = D / 64;                    // panels of a row
+  static constexpr int TB = NP * PANEL;                // bytes of a 128-row tile
+  static constexpr int NK = 2, NV = E4M3 ? 2 : 3;
+  static constexpr int Q = 0;                          // [2 groups]
+  static constexpr int K = 2 * TB;                     // [NK]
+  static constexpr int V = K + NK * TB;                // [NV]
+  static constexpr int CODES = V + NV * TB;            // [2] tiles of codes, [128][D]
+  static constexpr int SCALES = CODES + (E4M3 ? 2 * 128 * D : 0);   // [2][128]
+  static constexpr int CTRL = SCALES + (E4M3 ? 256 : 0);
+  static constexpr size_t BYTES = CTRL + 512;          // base 1024-aligned (checked)
+  static constexpr int SOFT0 = E4M3 ? 4 : 2;           // first softmax warp
+  static constexpr int CONV0 = SOFT0 + 8;              // first converting warp
+  static constexpr int THREADS = E4M3 ? 512 : 320;
+  static constexpr int READERS = 1 + 8 + (E4M3 ? 4 : 0);   // warps that follow the producer's items
+  static_assert(BYTES <= 227 * 1024, "shared memory per CTA");
+};
+
+struct Job {
+  Pool c;
+  Seqs s;
+  Mask m;
+  Packed o;
+  int G, TQ, max_rows;
+  int cut;            // units may be cut
+  int4* plan;         // {whole units, cut units, parts of each, -}, for cache_merge
+  float* parts;       // [MAX_PARTS][(D + 1) * 256]
+};
+
+// One item: a unit's key tiles [i0, i1) of its list.
+struct Item {
+  int state;          // 1: an item, 0: no more
+  int b, h, r0;       // sequence, key head, packed row of the first token
+  int n, p0, len;     // tokens, position of the first, length of the sequence
+  int ns, w0;         // the list: tiles 0 .. ns - 1, then w0, w0 + 1, ..
+  int i0, i1, part;   // part: slot of the partial result, -1: a whole unit
+};
+
+// What the tokens of one query tile see.
+struct Span {
+  int n;              // tokens with a position, 0: none
+  int whole;          // all of its tokens have one
+  int e0, e1, l0, l1; // end and window's first position of the first and the last token
+  int sk;             // sinks that the last token sees
+};
+
+__device__ __forceinline__ Span span_of(const Mask& m, int tokens, int p0, int len, int g, int TQ) {
+  Span s{};
+  const int at = g * TQ, n = min(tokens - at, TQ), pf = p0 + at, pl = pf + n - 1;
+  if (n <= 0 || pl < 0) return s;
+  s.n = n;
+  s.whole = pf >= 0;
+  s.e0 = visible_end(m, max(pf, 0), len);
+  s.e1 = visible_end(m, pl, len);
+  s.l0 = window_first(m, s.e0);
+  s.l1 = window_first(m, s.e1);
+  s.sk = m.window ? min(m.sinks, s.e1) : 0;
+  return s;
+}
+
+// Some row sees some key of the tile / every row every key.
+__device__ __forceinline__ bool active(const Span& s, int kt) {
+  const int k0 = kt * BK;
+  return s.n > 0 && k0 < s.e1 && (k0 + BK > s.l0 || k0 < s.sk);
+}
+__device__ __forceinline__ bool all_seen(const Mask& m, const Span& s, int kt) {
+  const int k0 = kt * BK;
+  return s.whole && k0 + BK <= s.e0 && (k0 >= s.l1 || (m.window && k0 + BK <= m.sinks));
+}
+__device__ __forceinline__ int tile_of(const Item& it, int i) { return i < it.ns ? i : it.w0 + (i - it.ns); }
+
+// The list of a unit's key tiles: ns, w0 and how many in all; lo and end of what its rows see beside the sinks.
+struct List {
+  int ns, w0, n, lo, end, sk;
+};
+__device__ __forceinline__ List list_of(const Mask& m, int tokens, int p0, int len, int TQ) {
+  const Span a = span_of(m, tokens, p0, len, 0, TQ), z = span_of(m, tokens, p0, len, 1, TQ);
+  List l{};
+  if (a.n == 0 && z.n == 0) return l;
+  l.lo = a.n ? a.l0 : z.l0;
+  l.end = z.n ? z.e1 : a.e1;
+  l.sk = z.n ? z.sk : a.sk;
+  l.ns = (l.sk + BK - 1) / BK;
+  l.w0 = max(l.ns, l.lo / BK);
+  l.n = l.ns + max(0, (l.end + BK - 1) / BK - l.w0);
+  return l;
+}
+
+// ------------------------------------------------------------------ the walk over items
+// Units, sequence by sequence, key head by key head, last tokens first (they see most); U whole
+// ones, then R cut into S parts each (part s of all of them before part s + 1: the parts that read
+// the same keys run side by side).
+struct Plan {
+  int U, R, S;
+};
+
+__device__ __forceinline__ int units_of(const Job& j, const Seq& q) { return (q.n + 2 * j.TQ - 1) / (2 * j.TQ); }
+
+// All lanes of one warp.
+__device__ Plan make_plan(const Job& j, int ctas) {
+  const int lane = threadIdx.x & 31;
+  int units = 0, longest = 0;
+  for (int b = lane; b < j.s.n; b += 32) {
+    const Seq q = seq_at(j.c, j.s, b);
+    if (q.n > j.max_rows) fail(j.c.status, DEV_INCONSISTENT, SITE_CHUNK);
+    const int nu = units_of(j, q);
+    units += nu * j.c.H;
+    if (nu > 0) {
+      const int t0 = (nu - 1) * 2 * j.TQ;
+      longest = max(longest, list_of(j.m, q.n - t0, q.len - q.n + t0, q.len, j.TQ).n);
+    }
+  }
+  units = __reduce_add_sync(0xffffffffu, units);
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  Plan p{units / ctas * ctas, units % ctas, 1};
+  if (p.R > 0 && j.cut) {
+    // lane: S = lane + 1 parts; the units that do not fill the CTAs take ceil(R S / ctas) rounds of longest / S tiles
+    const int S = lane + 1;
+    const bool fits = S == 1 || (longest >= S * MIN_PART && p.R * S <= MAX_PARTS);
+    const int rounds = (p.R * S + ctas - 1) / ctas;
+    const int est = rounds * ((longest + S - 1) / S + ITEM_TILES) + (S > 1 ? JOIN_TILES : 0);
+    const unsigned best = __reduce_min_sync(0xffffffffu, fits ? ((unsigned)min(est, 1 << 24) << 6) | S : 0xffffffffu);
+    p.S = best & 63;
+  }
+  return p;
+}
+
+// Unit u -> its sequence and place; all lanes of one warp.
+struct Unit {
+  int b, h, t;
+  Seq q;
+};
+__device__ Unit find_unit(const Job& j, int u) {
+  const int lane = threadIdx.x & 31;
+  for (int b0 = 0;; b0 += 32) {
+    const int b = b0 + lane;
+    Seq q{};
+    if (b < j.s.n) q = seq_at(j.c, j.s, b);
+    const int nu = units_of(j, q);
+    int incl = nu * j.c.H;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += v;
+    }
+    const unsigned past = __ballot_sync(0xffffffffu, b < j.s.n && incl > u);
+    if (past || b0 + 32 >= j.s.n) {
+      const int k = past ? __ffs(past) - 1 : 31;   // (u is below the sum of all)
+      const int before = __shfl_sync(0xffffffffu, incl - nu * j.c.H, k);
+      Unit r;
+      r.b = min(b0 + k, j.s.n - 1);
+      r.q.r0 = __shfl_sync(0xffffffffu, q.r0, k);
+      r.q.n = __shfl_sync(0xffffffffu, q.n, k);
+      r.q.len = __shfl_sync(0xffffffffu, q.len, k);
+      const int n = max(1, units_of(j, r.q)), rem = u - before;
+      r.h = min(rem / n, j.c.H - 1);
+      r.t = max(0, n - 1 - rem % n);
+      return r;
+    }
+    u -= __shfl_sync(0xffffffffu, incl, 31);
+  }
+}
+
+__device__ Item make_item(const Job& j, const Plan& p, int it) {
+  const bool whole = it < p.U;
+  const int k = it - p.U;
+  const int part = whole ? 0 : k / p.R, S = whole ? 1 : p.S;
+  const Unit u = find_unit(j, whole ? it : p.U + k % p.R);
+  const int t0 = u.t * 2 * j.TQ;
+  Item x;
+  x.state = 1;
+  x.b = u.b;
+  x.h = u.h;
+  x.r0 = u.q.r0 + t0;
+  x.n = min(u.q.n - t0, 2 * j.TQ);
+  x.p0 = u.q.len - u.q.n + t0;
+  x.len = u.q.len;
+  const List l = list_of(j.m, x.n, x.p0, x.len, j.TQ);
+  x.ns = l.ns;
+  x.w0 = l.w0;
+  x.i0 = (int)((int64_t)l.n * part / S);
+  x.i1 = (int)((int64_t)l.n * (part + 1) / S);
+  x.part = S > 1 ? k : -1;
+  return x;
+}
+
+// ------------------------------------------------------------------ values that are not finite
+// Clears what is not finite in one bf16 row (128-byte swizzled panels); whether there was any.
+template <int D>
+__device__ __forceinline__ bool clear_row(uint8_t* tile, int row) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) {
+    uint4* p = reinterpret_cast<uint4*>(tile + (c >> 3) * PANEL + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+    const uint4 x = *p;
+    // an exponent field of ones plus one carries into the (cleared) sign
+    any |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) |
+           ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
+  }
+  if ((any & 0x80008000u) == 0) return false;
+  for (int c = 0; c < D / 2; ++c) {
+    uint32_t* p = reinterpret_cast<uint32_t*>(tile + (c >> 5) * PANEL + row * 128 + ((((c >> 2) & 7) ^ (row & 7)) << 4)) + (c & 3);
+    const uint32_t x = *p, bad = ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    if (bad) *p = x & ~(((bad >> 15) & 0x00010001u) * 0xffffu);
+  }
+  return true;
+}
+
+// The columns [c0, c0 + 32) in which row (position range [lo, end) and sinks) meets a NaN, +inf, -inf in the tiles
+// of this item that clear_row may have been at.
+struct Wild {
+  uint32_t nan, pos, neg;
+};
+template <int D, bool E4M3>
+__device__ __noinline__ Wild wild_masks(const Job& j, const Item& it, int end, int lo, int c0) {
+  Wild w{0, 0, 0};
+  const Span a = span_of(j.m, it.n, it.p0, it.len, 0, j.TQ), z = span_of(j.m, it.n, it.p0, it.len, 1, j.TQ);
+  for (int i = it.i0; i < it.i1; ++i) {
+    const int kt = tile_of(it, i);
+    if ((!active(a, kt) || all_seen(j.m, a, kt)) && (!active(z, kt) || all_seen(j.m, z, kt))) continue;
+    for (int p = kt * BK; p < min(end, kt * BK + BK); ++p) {
+      if (p < lo && !(j.m.window && p < j.m.sinks)) continue;
+      const int64_t at = pool_row(j.c, j.s, it.b, it.h, p);
+      if (at < 0) continue;
+      if (E4M3) {
+        if (j.c.vs[at] == 255) w.nan = 0xffffffffu;
+        continue;
+      }
+      const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(j.c.v) + at * D + c0;
+      for (int k = 0; k < 32; ++k) {
+        const float x = __bfloat162float(v[k]);
+        if (isnan(x)) w.nan |= 1u << k;
+        if (x == INFINITY) w.pos |= 1u << k;
+        if (x == -INFINITY) w.neg |= 1u << k;
+      }
+    }
+  }
+  return w;
+}
+
+// Bits k < x.
+__device__ __forceinline__ uint32_t below(int x) { return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; }
+
+// Scores of what the row does not see become -inf (columns k0 .. k0 + 31 of the positions).
+__device__ __forceinline__ void mask_row(float (&v)[32], int k0, int end, int lo, int sk) {
+  const uint32_t see = below(end - k0) & (~below(lo - k0) | below(sk - k0));
+#pragma unroll
+  for (int k = 0; k < 32; ++k)
+    if (!((see >> k) & 1u)) v[k] = -INFINITY;
+}
+
+// ------------------------------------------------------------------ codes into bf16
+// Two bf16 from two codes in the high bytes of the halves of x: the code's bits in bf16's fields
+// are its value times 2^-120 (subnormal codes included).
+__device__ __forceinline__ uint32_t widen(uint32_t x, __nv_bfloat162 f) {
+  const uint32_t y = (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u);
+  const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&y), f);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ __nv_bfloat162 pair_of(uint32_t exponent_field) {
+  const uint32_t b = exponent_field << 7, w = b | (b << 16);
+  return *reinterpret_cast<const __nv_bfloat162*>(&w);
+}
+
+// A [128][D] tile of codes and its rows' scales into a swizzled bf16 tile (128 threads).
+template <int D>
+__device__ __forceinline__ void widen_tile(const uint8_t* codes, const uint8_t* scales, uint8_t* tile, int t) {
+  constexpr int LANES = D / 16, ROWS = 128 / LANES;
+  const int c = t % LANES;
+  const __nv_bfloat16 nan = __ushort_as_bfloat16((unsigned short)0x7fff);
+#pragma unroll
+  for (int pass = 0; pass < LANES; ++pass) {
+    const int row = pass * ROWS + t / LANES;
+    const uint4 x = *reinterpret_cast<const uint4*>(codes + row * D + c * 16);
+    const uint32_t s = scales[row];
+    // 2^120 2^(s - 127) in one factor where it is a bf16 number, else in two; 255: NaN
+    const bool two = s > 134u && s != 255u;
+    const __nv_bfloat162 f = s == 255u ? __nv_bfloat162(nan, nan) : pair_of(two ? 247u : s + 120u);
+    uint32_t y[8];
+    const uint32_t* w = &x.x;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      y[2 * k] = widen(__byte_perm(w[k], 0, 0x1404), f);
+      y[2 * k + 1] = widen(__byte_perm(w[k], 0, 0x3424), f);
+    }
+    if (__any_sync(0xffffffffu, two)) {
+      const __nv_bfloat162 f2 = pair_of(two ? s : 127u);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const __nv_bfloat162 v = __hmul2(*reinterpret_cast<__nv_bfloat162*>(&y[k]), f2);
+        y[k] = *reinterpret_cast<const uint32_t*>(&v);
+      }
+    }
+    // 16-byte chunks 2c and 2c + 1 of the row; the upper panel's threads write theirs the other way
+    // round, so that a store's eight threads of a row meet eight different banks
+    uint8_t* base = tile + (c >> 2) * PANEL + row * 128;
+    const int ch = 2 * (c & 3), flip = (c >> 2) & 1, x7 = row & 7;
+    const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
+    *reinterpret_cast<uint4*>(base + (((ch + flip) ^ x7) << 4)) = flip ? b : a;
+    *reinterpret_cast<uint4*>(base + (((ch + 1 - flip) ^ x7) << 4)) = flip ? a : b;
+  }
+}
+
+// ------------------------------------------------------------------ the kernel
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
+    cache_attend_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+                    const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Job j) {
+  using L = Lay<D, E4M3>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  if ((smem_u32(smem) & 1023u) != 0u) {   // 128-byte-swizzled tiles need 1024-byte alignment
+    if (threadIdx.x == 0) fail(j.c.status, DEV_INCONSISTENT, 9903);
+    return;
+  }
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::CTRL);
+  uint64_t* q_full = bars + 0;
+  uint64_t* q_empty = bars + 1;     // all score products of the item complete
+  uint64_t* k_full = bars + 2;      // [2]
+  uint64_t* k_empty = bars + 4;     // [2]
+  uint64_t* v_full = bars + 6;      // [3]
+  uint64_t* v_empty = bars + 9;     // [3]
+  uint64_t* c_full = bars + 12;     // [2] tiles of codes
+  uint64_t* c_empty = bars + 14;    // [2]
+  uint64_t* s_full = bars + 16;     // [2] by group
+  uint64_t* p_full = bars + 18;     // [2]
+  uint64_t* o_full = bars + 20;     // [2]
+  uint64_t* it_full = bars + 22;    // [2] items
+  uint64_t* it_empty = bars + 24;   // [2]
+  uint64_t* done = bars + 26;
+  Item* items = reinterpret_cast<Item*>(bars + 28);                        // [2]
+  volatile int* wild = reinterpret_cast<volatile int*>(items + 2);         // [2] number of the last item with values cleared
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(items + 2) + 2;
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
+  static_assert(28 * 8 + 2 * sizeof(Item) + 16 <= 512, "control block");
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  if (threadIdx.x == 64) {
+    mbar_init(q_full, 1);
+    mbar_init(q_empty, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(k_full + i, E4M3 ? 4 : 1);
+      mbar_init(k_empty + i, 1);
+      mbar_init(c_full + i, 1);
+      mbar_init(c_empty + i, 4);
+      mbar_init(s_full + i, 1);
+      mbar_init(p_full + i, 4);
+      mbar_init(o_full + i, 1);
+      mbar_init(it_full + i, 1);
+      mbar_init(it_empty + i, L::READERS);
+      wild[i] = 0;
+    }
+    for (int i = 0; i < 3; ++i) {
+      mbar_init(v_full + i, E4M3 ? 4 : 1);
+      mbar_init(v_empty + i, 1);
+    }
+    mbar_init(done, 1);
+    *abort_flag = 0;
+    fence_barrier_init();
+  }
+  if (warp == 1) tmem_alloc(tmem_holder, TMEM_COLS);
+  pdl_trigger();   // cache_merge's blocks start as SMs free up, and wait there
+  fence_before_sync();
+  __syncthreads();
+  fence_after_sync();
+  const uint32_t tmem = *tmem_holder;
+
+  auto give_up = [&](int site) {
+    *abort_flag = 1;
+    fail(j.c.status, DEV_TIMEOUT, SITE_WAIT + site);
+  };
+  // Reader warps: the next item (state 0: none, or the CTA has given up).
+  auto next_item = [&](uint32_t n) -> Item {
+    Item x;
+    x.state = 0;
+    if (mbar_wait_warp(it_full + (n & 1), (n >> 1) & 1, abort_flag)) {
+      x = items[n & 1];
+      __syncwarp();
+      if (lane == 0) mbar_arrive(it_empty + (n & 1));
+    }
+    return x;
+  };
+
+  if (warp < L::SOFT0) {
+    if (E4M3) regs_lower<72>();
+    if (warp == 0) {
+      // ---------------- producer: items; Q, then the tiles of K and V, K one ahead
+      const Plan plan = make_plan(j, gridDim.x);
+      if (blockIdx.x == 0 && lane == 0) *j.plan = make_int4(plan.U, plan.R, plan.S, 0);
+      const int total = plan.U + plan.R * plan.S;
+      const int rows = min(j.c.page_len, BK), np = BK / rows;   // rows and boxes of a tile
+      uint32_t tc = 0, nq = 0, ni = 0, cc = 0;
+      bool ok = true;
+      for (int it = blockIdx.x;; it += gridDim.x, ++ni) {
+        Item x;
+        x.state = 0;
+        List l{};
+        if (it < total) {
+          x = make_item(j, plan, it);
+          l = list_of(j.m, x.n, x.p0, x.len, j.TQ);
+        }
+        if (ni >= 2) ok = mbar_wait_warp(it_empty + (ni & 1), ((ni >> 1) & 1) ^ 1, abort_flag);
+        if (!ok) break;
+        if (lane == 0) {
+          items[ni & 1] = x;
+          mbar_arrive(it_full + (ni & 1));
+        }
+        __syncwarp();
+        if (x.state == 0) break;
+        const int n = x.i1 - x.i0;
+        if (n <= 0) continue;
+        if (nq > 0 && !(ok = mbar_wait_warp(q_empty, (nq - 1) & 1, abort_flag))) break;
+        ++nq;
+        if (lane == 0) {
+          const int groups = x.n > j.TQ ? 2 : 1, bytes = j.TQ * j.G * 128;
+          mbar_arrive_expect_tx(q_full, groups * L::NP * bytes);
+          for (int g = 0; g < groups; ++g)
+            for (int p = 0; p < L::NP; ++p)
+              tma_load_4d(smem + L::Q + g * L::TB + p * PANEL, &tmQ, q_full, p * 64, 0, x.r0 + g * j.TQ, x.h);
+        }
+        __syncwarp();
+        // one tile of K or V: a lane a box
+        auto load = [&](bool is_k, int i) -> bool {
+          const int kt = tile_of(x, i);
+          const uint32_t t = tc + (uint32_t)(i - x.i0);
+          const int box = E4M3 ? lane : lane / L::NP, panel = E4M3 ? 0 : lane % L::NP;
+          // the box's page; nobody's (zeros) where no row of the unit sees into it
+          const int k0 = kt * BK + box * rows;
+          int page = j.c.n_pages;
+          if (box < np && k0 < l.end && (k0 + rows > l.lo || k0 < l.sk)) {
+            page = __ldg(j.s.table + (int64_t)x.b * j.s.max_pages + (k0 >> j.c.page_log2));
+            if ((unsigned)page >= (unsigned)j.c.n_pages) {
+              fail(j.c.status, DEV_INCONSISTENT, SITE_PAGE);
+              page = j.c.n_pages;
+            }
+          }
+          const int slot = k0 & (j.c.page_len - 1);
+          if (E4M3) {
+            const uint32_t c = cc++;
+            uint64_t* bar = c_full + (c & 1);
+            if (c >= 2 && !mbar_wait_warp(c_empty + (c & 1), ((c >> 1) & 1) ^ 1, abort_flag)) return false;
+            const unsigned named = __ballot_sync(0xffffffffu, page < j.c.n_pages);
+            if (lane == 0) mbar_arrive_expect_tx(bar, BK * D + __popc(named) * rows);
+            __syncwarp();
+            if (box < np) {
+              tma_load_4d(smem + L::CODES + (c & 1) * 128 * D + box * rows * D, is_k ? &tmK : &tmV, bar, 0, slot, x.h, page);
+              if (page < j.c.n_pages)
+                bulk_load(smem + L::SCALES + (c & 1) * 128 + box * rows,
+                          (is_k ? j.c.ks : j.c.vs) + (((int64_t)page * j.c.H + x.h) << j.c.page_log2) + slot, rows, bar);
+            }
+          } else {
+            const uint32_t nb = is_k ? L::NK : L::NV, sl = t % nb;
+            uint64_t* bar = (is_k ? k_full : v_full) + sl;
+            if (t >= nb && !mbar_wait_warp((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
+            if (lane == 0) mbar_arrive_expect_tx(bar, L::TB);
+            __syncwarp();
+            if (box < np)
+              tma_load_4d(smem + (is_k ? L::K : L::V) + sl * L::TB + panel * PANEL + box * rows * 128, is_k ? &tmK : &tmV,
+                          bar, panel * 64, slot, x.h, page);
+          }
+          __syncwarp();
+          return true;
+        };
+        ok = load(true, x.i0);
+        for (int i = x.i0; ok && i < x.i1; ++i) {
+          if (i + 1 < x.i1) ok = load(true, i + 1);
+          ok = ok && load(false, i);
+        }
+        tc += n;
+        if (!ok) break;
+      }
+      if (!ok) {
+        if (lane == 0) give_up(0);
+        // copies may be in flight that nobody waits for any more: far longer than one takes
+        const uint64_t t0 = globaltimer_ns();
+        while (globaltimer_ns() - t0 < 50000ull) {
+        }
+      }
+    } else if (warp == 1) {
+      // ---------------- MMA issuer (the whole warp, one elected lane issues)
+      constexpr uint32_t id_s = idesc_bf16(BQ, BK), id_o = idesc_bf16(BQ, D, /*b_mn_major=*/true);
+      const uint64_t qd0 = desc_sw128(smem_u32(smem + L::Q)), kd0 = desc_sw128(smem_u32(smem + L::K));
+      const uint64_t vd0 = desc_sw128_mn(smem_u32(smem + L::V), PANEL, 1024);
+      uint32_t tc = 0, nq = 0, np[2] = {0, 0};
+      bool ok = true;
+      auto issue_s = [&](int g, uint32_t t) {
+        const uint64_t qd = desc_add(qd0, g * L::TB), kd = desc_add(kd0, (t % L::NK) * L::TB);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * PANEL + (kk & 3) * 32;
+            mma_bf16(tmem + g * 256, desc_add(qd, off), desc_add(kd, off), id_s, kk > 0);
+          }
+          mma_commit(s_full + g);
+        }
+        __syncwarp();
+      };
+      auto issue_pv = [&](int g, uint32_t t, bool first) {
+        const uint64_t vd = desc_add(vd0, (t % L::NV) * L::TB);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)
+            mma_bf16_ts(tmem + g * 256 + 128, tmem + g * 256 + kk * 8, desc_add(vd, kk * 2048), id_o,
+                        first && kk == 0 ? 0u : 1u);
+        }
+        __syncwarp();
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (elect_one()) mma_commit(bar);
+        __syncwarp();
+      };
+      for (uint32_t ni = 0; ok; ++ni) {
+        const Item x = next_item(ni);
+        if (x.state == 0) break;
+        const int n = x.i1 - x.i0;
+        if (n <= 0) continue;
+        const Span sp[2] = {span_of(j.m, x.n, x.p0, x.len, 0, j.TQ), span_of(j.m, x.n, x.p0, x.len, 1, j.TQ)};
+        int left[2] = {0, 0};   // active tiles to come
+        bool first[2] = {true, true};
+        for (int i = x.i0; i < x.i1; ++i) {
+          left[0] += active(sp[0], tile_of(x, i));
+          left[1] += active(sp[1], tile_of(x, i));
+        }
+        ok = mbar_wait_warp(q_full, nq & 1, abort_flag) &&
+             mbar_wait_warp(k_full + tc % L::NK, (tc / L::NK) & 1, abort_flag);
+        ++nq;
+        if (!ok) break;
+        fence_after_sync();
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          if (active(sp[g], tile_of(x, x.i0))) issue_s(g, tc);
+        commit(k_empty + tc % L::NK);
+        if (n == 1) commit(q_empty);
+        for (int i = x.i0; i < x.i1; ++i) {
+          const uint32_t t = tc + (uint32_t)(i - x.i0);
+          const bool next = i + 1 < x.i1;
+          ok = (!next || mbar_wait_warp(k_full + (t + 1) % L::NK, ((t + 1) / L::NK) & 1, abort_flag)) &&
+               mbar_wait_warp(v_full + t % L::NV, (t / L::NV) & 1, abort_flag);
+          if (!ok) break;
+          const int kt = tile_of(x, i), kn = tile_of(x, i + 1);
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            if (active(sp[g], kt)) {
+              if (!(ok = mbar_wait_warp(p_full + g, np[g] & 1, abort_flag))) break;
+              ++np[g];
+              fence_after_sync();
+              issue_pv(g, t, first[g]);
+              first[g] = false;
+              if (--left[g] == 0) commit(o_full + g);
+            }
+            if (next && active(sp[g], kn)) {
+              fence_after_sync();
+              issue_s(g, t + 1);
+            }
+          }
+          if (!ok) break;
+          if (next) commit(k_empty + (t + 1) % L::NK);
+          if (i + 2 == x.i1) commit(q_empty);
+          commit(v_empty + t % L::NV);
+        }
+        tc += n;
+      }
+      if (!ok && lane == 0) give_up(1);
+      // every product complete before TMEM is freed
+      commit(done);
+      volatile int no_abort = 0;
+      mbar_wait(done, 0, &no_abort);
+    }
+  } else if (warp < L::CONV0) {
+    if (E4M3) regs_raise<184>();
+    // ---------------- softmax group g over query tile g, thread = query row = TMEM lane
+    const int g = (warp - L::SOFT0) >> 2, qd = warp & 3, r = qd * 32 + lane;
+    const uint32_t lane_off = (uint32_t)(qd * 32) << 16;
+    const uint32_t sc = tmem + lane_off + g * 256, oc = sc + 128;
+    const int tok = r / j.G, hq = r - tok * j.G;
+    uint32_t ns = 0, no = 0, tc = 0;
+    bool ok = true;
+    for (uint32_t ni = 0; ok; ++ni) {
+      // (the item stays in its slot until its outputs are stored: fewer registers)
+      if (!mbar_wait_warp(it_full + (ni & 1), (ni >> 1) & 1, abort_flag)) break;
+      const Item& x = items[ni & 1];
+      if (x.state == 0) break;
+      const Span sp = span_of(j.m, x.n, x.p0, x.len, g, j.TQ);
+      const int p = x.p0 + g * j.TQ + tok;                // the row's position
+      const int end = p >= 0 ? visible_end(j.m, p, x.len) : 0, lo = window_first(j.m, end);
+      const int sk = j.m.window ? j.m.sinks : 0;
+      float mrun = -INFINITY, l = 0.f;
+      bool some = false;
+      for (int i = x.i0; i < x.i1; ++i) {
+        const int kt = tile_of(x, i);
+        if (!active(sp, kt)) continue;
+        const bool partial = !all_seen(j.m, sp, kt);
+        if (partial) {
+          const uint32_t t = tc + (uint32_t)(i - x.i0);
+          if (!(ok = mbar_wait_warp(v_full + t % L::NV, (t / L::NV) & 1, abort_flag))) break;
+          if (clear_row<D>(smem + L::V + (t % L::NV) * L::TB, r)) wild[ni & 1] = (int)ni + 1;
+          fence_async_smem();
+        }
+        if (!(ok = mbar_wait_warp(s_full + g, ns & 1, abort_flag))) break;
+        ++ns;
+        fence_after_sync();
+        float s0[32], s1[32], s2[32], s3[32];
+        tmem_ld32(sc, s0);
+        tmem_ld32(sc + 32, s1);
+        tmem_ld32(sc + 64, s2);
+        tmem_ld32(sc + 96, s3);
+        tmem_wait_ld();
+        if (partial) {
+          const int k0 = kt * BK;
+          mask_row(s0, k0, end, lo, sk);
+          mask_row(s1, k0 + 32, end, lo, sk);
+          mask_row(s2, k0 + 64, end, lo, sk);
+          mask_row(s3, k0 + 96, end, lo, sk);
+        }
+        float tmax;
+        {
+          float t[8];
+#pragma unroll
+          for (int k = 0; k < 8; ++k) t[k] = -INFINITY;
+          max_acc(t, s0); max_acc(t, s1); max_acc(t, s2); max_acc(t, s3);
+          tmax = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
+        }
+        tmax *= j.m.sl2;
+        // S_g of this tile complete implies O_g of the one before complete (issued earlier by one thread)
+        const bool raise = tmax > mrun + RESCALE_LOG2 || (mrun == -INFINITY && tmax > -INFINITY);
+        const float mprev = mrun;
+        if (raise) {
+          l *= some ? ex2(mrun - tmax) : 0.f;
+          mrun = tmax;
+        }
+        const float nm = mrun == -INFINITY ? 0.f : -mrun;   // (a row that has seen nothing yet: all weights 0)
+        float2 lab = make_float2(0.f, 0.f);
+        {
+          uint32_t pk[32];
+          exp_pack(s0, s1, j.m.sl2, nm, lab, pk);
+          tmem_st32(sc, pk);
+          exp_pack(s2, s3, j.m.sl2, nm, lab, pk);
+          tmem_st32(sc + 32, pk);
+        }
+        if (__any_sync(0xffffffffu, raise && some)) {
+          const float alpha = raise ? ex2(mprev - mrun) : 1.0f;
+#pragma unroll
+          for (int c = 0; c < D / 32; ++c) {
+            float v[32];
+            tmem_ld32(oc + c * 32, v);
+            tmem_wait_ld();
+            uint32_t w32[32];
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const float2 y = __fmul2_rn(make_float2(v[2 * k], v[2 * k + 1]), make_float2(alpha, alpha));
+              w32[2 * k] = __float_as_uint(y.x);
+              w32[2 * k + 1] = __float_as_uint(y.y);
+            }
+            tmem_st32(oc + c * 32, w32);
+          }
+        }
+        some = true;
+        l += lab.x + lab.y;
+        tmem_wait_st();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + g);
+      }
+      tc += (uint32_t)max(0, x.i1 - x.i0);
+      if (ok && some) {
+        ok = mbar_wait_warp(o_full + g, no & 1, abort_flag);
+        ++no;
+      }
+      if (!ok) break;
+      fence_after_sync();
+      // ---- outputs
+      const int token = g * j.TQ + tok;
+      const bool mine = tok < j.TQ && token < x.n;
+      const bool whole = x.part < 0;
+      const bool fix = wild[ni & 1] == (int)ni + 1;
+      const float inv = l == 0.f ? 0.f : 1.0f / l;         // (a NaN stays one)
+      float* part = whole ? nullptr : j.parts + (int64_t)x.part * (256 * (D + 1));
+      if (!whole) part[256 * D + g * BQ + r] = l == 0.f ? -INFINITY : mrun + log2f(l);
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        float v[32];
+        if (some) {   // warp-uniform
+          tmem_ld32(oc + c * 32, v);
+          tmem_wait_ld();
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = some ? v[k] * inv : 0.f;
+        if (fix) {
+          const Wild w = wild_masks<D, E4M3>(j, x, mine ? end : 0, lo, c * 32);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            if ((w.pos >> k) & 1u) v[k] += INFINITY;
+            if ((w.neg >> k) & 1u) v[k] -= INFINITY;
+            if ((w.nan >> k) & 1u) v[k] = __int_as_float(0x7fffffff);
+          }
+        }
+        if (!whole) {
+          float4* dst = reinterpret_cast<float4*>(part) + (c * 8) * 256 + g * BQ + r;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) dst[k * 256] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        } else if (mine) {
+          uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(x.h * j.G + hq) * j.o.head +
+                                                (int64_t)(x.r0 + token) * j.o.row + c * 32);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            dst[k] = make_uint4(pack_bf16(v[8 * k], v[8 * k + 1]), pack_bf16(v[8 * k + 2], v[8 * k + 3]),
+                                pack_bf16(v[8 * k + 4], v[8 * k + 5]), pack_bf16(v[8 * k + 6], v[8 * k + 7]));
+        }
+      }
+      fence_before_sync();   // O_g read before the next item's products overwrite it (they wait for its weights)
+      __syncwarp();
+      if (lane == 0) mbar_arrive(it_empty + (ni & 1));
+    }
+    if (!ok && lane == 0) give_up(2);
+  } else {
+    if (E4M3) regs_lower<72>();
+    // ---------------- codes into bf16, in the order of the copies: K(0), K(1), V(0), K(2), V(1), ..
+    const int t128 = threadIdx.x - L::CONV0 * 32;
+    uint32_t tc = 0, cc = 0;
+    bool ok = true;
+    auto turn = [&](bool is_k, uint32_t t) -> bool {
+      const uint32_t c = cc++;
+      const uint32_t nb = is_k ? L::NK : L::NV, sl = t % nb;
+      if (!mbar_wait_warp(c_full + (c & 1), (c >> 1) & 1, abort_flag)) return false;
+      if (t >= nb && !mbar_wait_warp((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
+      widen_tile<D>(smem + L::CODES + (c & 1) * 128 * D, smem + L::SCALES + (c & 1) * 128,
+                    smem + (is_k ? L::K : L::V) + sl * L::TB, t128);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) {
+        mbar_arrive((is_k ? k_full : v_full) + sl);
+        mbar_arrive(c_empty + (c & 1));
+      }
+      return true;
+    };
+    for (uint32_t ni = 0; ok; ++ni) {
+      const Item x = next_item(ni);
+      if (x.state == 0) break;
+      const int n = x.i1 - x.i0;
+      if (n <= 0) continue;
+      ok = turn(true, tc);
+      for (int i = 0; ok && i < n; ++i) {
+        if (i + 1 < n) ok = turn(true, tc + i + 1);
+        ok = ok && turn(false, tc + i);
+      }
+      tc += n;
+    }
+    if (!ok && lane == 0) give_up(3);
+  }
+  fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after_sync();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+}
+
+// Joins the parts of cut units: O = sum_s 2^(lse_s - max) O_s / sum_s 2^(lse_s - max), parts in
+// order.  Block (unit, 32 rows), thread = (row, D / 8 columns).
+constexpr int MG_ROWS = 32;
+
+template <int D>
+__global__ void __launch_bounds__(256) cache_merge(const __grid_constant__ Job j) {
+  pdl_wait();
+  const int4 p = *j.plan;
+  if (p.z < 2 || (int)blockIdx.x >= p.y) return;
+  __shared__ float lse[MAX_CUT][MG_ROWS];
+  __shared__ Unit su;
+  if (threadIdx.x < 32) {
+    const Unit u = find_unit(j, p.x + blockIdx.x);
+    if (threadIdx.x == 0) su = u;
+  }
+  const int S = min(p.z, MAX_CUT), R = p.y, row0 = blockIdx.y * MG_ROWS;
+  auto part = [&](int s) { return j.parts + (int64_t)(s * R + (int)blockIdx.x) * (256 * (D + 1)); };
+  for (int e = threadIdx.x; e < S * MG_ROWS; e += 256) lse[e / MG_ROWS][e % MG_ROWS] = part(e / MG_ROWS)[256 * D + row0 + e % MG_ROWS];
+  __syncthreads();
+  const Unit u = su;
+  const int rl = threadIdx.x % MG_ROWS, row = row0 + rl, q = threadIdx.x / MG_ROWS;   // 8 column groups
+  const int g = row / BQ, r = row % BQ, tok = r / j.G, token = g * j.TQ + tok;
+  if (tok >= j.TQ || u.t * 2 * j.TQ + token >= u.q.n) return;
+  float mx = -INFINITY, den = 0.f;
+  for (int s = 0; s < S; ++s) mx = fmaxf(mx, lse[s][rl]);
+  float o[D / 8];
+#pragma unroll
+  for (int k = 0; k < D / 8; ++k) o[k] = 0.f;
+  for (int s = 0; s < S; ++s) {
+    const float z = lse[s][rl];
+    if (z == -INFINITY) continue;                          // the part saw nothing of this row's
+    const float w = exp2f(z - mx);
+    den += w;
+    const float4* src = reinterpret_cast<const float4*>(part(s)) + row;
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) {
+      const float4 x = src[(q * (D / 32) + k) * 256];
+      o[4 * k] = fmaf(w, x.x, o[4 * k]);
+      o[4 * k + 1] = fmaf(w, x.y, o[4 * k + 1]);
+      o[4 * k + 2] = fmaf(w, x.z, o[4 * k + 2]);
+      o[4 * k + 3] = fmaf(w, x.w, o[4 * k + 3]);
+    }
+  }
+  const float inv = den == 0.f ? 0.f : 1.0f / den;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(static_cast<__nv_bfloat16*>(j.o.p) +
+                                              (int64_t)(u.h * j.G + r - tok * j.G) * j.o.head +
+                                              (int64_t)(u.q.r0 + u.t * 2 * j.TQ + token) * j.o.row + q * (D / 8));
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) dst[k] = pack_bf16(o[2 * k] * inv, o[2 * k + 1] * inv);
+}
+
+template <int D, bool E4M3>
+cudaError_t launch_d(const Maps& maps, const Job& job, const CUtensorMap& mq, int ctas, cudaStream_t st) {
+  using L = Lay<D, E4M3>;
+  cudaError_t e = launch_kernel(cache_attend_tc<D, E4M3>, dim3(ctas), L::THREADS, L::BYTES, 1, false, st, mq, maps.k,
+                                maps.v, job);
+  if (e == cudaSuccess && job.cut)
+    e = launch_kernel(cache_merge<D>, dim3(ctas, 256 / MG_ROWS), 256, 0, 1, true, st, job);
+  return e;
+}
+
+template <int D, bool E4M3>
+cudaError_t set_limit() {
+  return taken(cudaFuncSetAttribute(cache_attend_tc<D, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    (int)Lay<D, E4M3>::BYTES));
+}
+
+}  // namespace
+
+cudaError_t attend_tc_set_smem_limits() {
+  cudaError_t e = set_limit<128, false>();
+  if (e == cudaSuccess) e = set_limit<128, true>();
+  if (e == cudaSuccess) e = set_limit<64, false>();
+  if (e == cudaSuccess) e = set_limit<64, true>();
+  return e;
+}
+
+bool make_maps(const Pool& c, Maps* m) {
+  const int es = c.e4m3 ? 1 : 2;
+  const int64_t dim[4] = {c.d, c.page_len, c.H, c.n_pages};
+  const int64_t stride[3] = {(int64_t)c.d * es, (int64_t)c.page_len * c.d * es, (int64_t)c.H * c.page_len * c.d * es};
+  const int box[4] = {c.e4m3 ? c.d : 64, std::min(c.page_len, BK), 1, 1};
+  return make_map_4d(&m->k, c.k, es, dim, stride, box, !c.e4m3) && make_map_4d(&m->v, c.v, es, dim, stride, box, !c.e4m3);
+}
+
+size_t attend_tc_scratch(const Pool& c) { return 256 + sizeof(float) * (size_t)MAX_PARTS * 256 * (c.d + 1); }
+
+cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
+                             int max_rows, const Mask& m, void* scratch, cudaStream_t st) {
+  const int G = Hq / c.H, TQ = BQ / G, n_sm = std::min(sm_count(), MAX_CTAS);
+  if (n_sm <= 0) return cudaErrorInvalidDevice;
+  CUtensorMap mq;
+  const int64_t dim[4] = {c.d, G, s.rows, c.H};
+  const int64_t head = q.head ? q.head : c.d, row = q.row ? q.row : c.d;   // (one head or row: any stride)
+  const int64_t stride[3] = {head * 2, row * 2, G * head * 2};
+  const int box[4] = {64, G, TQ, 1};
+  if (!make_map_4d(&mq, q.p, 2, dim, stride, box, true)) return cudaErrorInvalidValue;
+  Job job{c, s, m, o, G, TQ, max_rows, 1, static_cast<int4*>(scratch),
+          reinterpret_cast<float*>(static_cast<char*>(scratch) + 256)};
+  if (c.d == 128)
+    return c.e4m3 ? launch_d<128, true>(maps, job, mq, n_sm, st) : launch_d<128, false>(maps, job, mq, n_sm, st);
+  return c.e4m3 ? launch_d<64, true>(maps, job, mq, n_sm, st) : launch_d<64, false>(maps, job, mq, n_sm, st);
+}
+
+}  // namespace cache
+}  // namespace dkv

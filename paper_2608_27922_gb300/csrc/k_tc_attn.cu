@@ -25,6 +25,7 @@
 // 68-cycle MMA.  Same products in the same order, measured at 2,070 MHz: 12 heads x 4,680
 // queries x 14,040 keys 283 -> 249 us in short bursts (85% of 1.9 PFLOP/s; back to back 296 ->
 // 265, at the power limit), 160 heads of mixed budgets 3,417 -> 3,124 us.  (The pair passes, bound by their epilogues, did not gain: unchanged.)
+#include "attn_math.cuh"
 #include "attn_schedule.h"
 #include "dkv_internal.h"
 #include "tc_ptx.cuh"
@@ -53,54 +54,6 @@ constexpr int OFF_X = 7 * TB;           // float [2 groups][2 (m, l)][BQ]
 constexpr int OFF_BAR = OFF_X + 2 * 2 * BQ * 4;
 constexpr size_t SMEM_BYTES = OFF_BAR + 256;   // base 1024-aligned (checked)
 constexpr float RESCALE_LOG2 = 8.0f;
-
-__device__ __forceinline__ float ex2(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
-
-// max(a, b, c) in one instruction (three-input form, sm_100 and later).
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float y;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(y) : "f"(a), "f"(b), "f"(c));
-  return y;
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-  return *reinterpret_cast<uint32_t*>(&v);
-}
-
-// Row maximum accumulation over 32 scores (t: eight partial maxima).
-__device__ __forceinline__ void max_acc(float (&t)[8], const float (&v)[32]) {
-#pragma unroll
-  for (int k = 0; k < 16; ++k) t[k & 7] = max3(t[k & 7], v[2 * k], v[2 * k + 1]);
-}
-
-// Scores of the columns at or past `lim` (keys past the end of the range) become -inf:
-// they do not raise the maximum and their exponentials are exactly 0.
-__device__ __forceinline__ void mask_tail(float (&v)[32], int lim) {
-#pragma unroll
-  for (int k = 0; k < 32; ++k)
-    if (k >= lim) v[k] = -INFINITY;
-}
-
-// P = 2^(s sl2 - m) over 64 scores (a: the first 32, b: the next 32) as 32 packed bf16
-// pairs; lab accumulates the even and the odd columns.
-__device__ __forceinline__ void exp_pack(const float (&a)[32], const float (&b)[32], float sl2, float nm,
-                                         float2& lab, uint32_t (&pk)[32]) {
-  const float2 sl2x2 = make_float2(sl2, sl2), nmx2 = make_float2(nm, nm);
-#pragma unroll
-  for (int k = 0; k < 32; ++k) {
-    const float s0 = k < 16 ? a[2 * k] : b[2 * k - 32];
-    const float s1 = k < 16 ? a[2 * k + 1] : b[2 * k - 31];
-    const float2 x = __ffma2_rn(make_float2(s0, s1), sl2x2, nmx2);
-    const float2 pp = make_float2(ex2(x.x), ex2(x.y));
-    lab = __fadd2_rn(lab, pp);
-    pk[k] = pack_bf16(pp.x, pp.y);
-  }
-}
 
 struct AttnJob {
   Bank b;

@@ -1440,6 +1440,25 @@ bool make_map_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t heads
   return encode(m, base, 128, rows, heads, 64, box_rows, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
+// Any 4-D tensor of 1- or 2-byte elements (strides in bytes, of dimensions 1 to 3): boxes of box[0] x box[1] x
+// box[2] x box[3] elements, 128-byte swizzle or none; out-of-range places read as zeros.
+bool make_map_4d(CUtensorMap* m, const void* base, int elem_bytes, const int64_t (&dim)[4], const int64_t (&stride)[3],
+                 const int (&box)[4], bool swizzle) {
+  EncodeTiledFn fn = encode_fn();
+  if (!fn) return false;
+  cuuint64_t dims[4], strides[3];
+  cuuint32_t boxes[4], es[4] = {1, 1, 1, 1};
+  for (int i = 0; i < 4; ++i) {
+    dims[i] = (cuuint64_t)dim[i];
+    boxes[i] = (cuuint32_t)box[i];
+    if (i < 3) strides[i] = (cuuint64_t)stride[i];
+  }
+  return fn(m, elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4,
+            const_cast<void*>(base), dims, strides, boxes, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 // bf16 [heads][rows][32] extension rows: boxes of 16 columns x box_rows rows, 32-byte swizzle.
 bool make_map_ext(CUtensorMap* m, const void* base, int64_t rows, int64_t heads, int box_rows) {
   return encode(m, base, 32, rows, heads, 16, box_rows, CU_TENSOR_MAP_SWIZZLE_32B);
