@@ -11,7 +11,7 @@
 // rescaled in TMEM).  Bound by the tensor pipe (4 d flops a row and key) and close to it by the exponentials.
 //
 // Pages come in by TMA, one box a page and 64-column panel, in the layout that the products read.
-// A quantised cache's codes land beside that layout and four warps turn them into bf16 in place
+// A quantised cache's codes land beside that layout and eight warps turn them into bf16 in place
 // of the copy: code bits shifted into bf16's fields are the value times 2^-120, one product with
 // 2^120 times the row's scale makes it exact (bf16 holds every code times its scale).
 //
@@ -28,6 +28,7 @@
 #include "tc_ptx.cuh"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace dkv {
 
@@ -64,10 +65,15 @@ struct Lay {
   static constexpr int SCALES = CODES + (E4M3 ? 2 * 128 * D : 0);   // [2][128]
   static constexpr int CTRL = SCALES + (E4M3 ? 256 : 0);
   static constexpr size_t BYTES = CTRL + 512;          // base 1024-aligned (checked)
-  static constexpr int SOFT0 = E4M3 ? 4 : 2;           // first softmax warp
+  static constexpr int SOFT0 = 4;                      // first softmax warp (warps 2 and 3 idle)
   static constexpr int CONV0 = SOFT0 + 8;              // first converting warp
-  static constexpr int THREADS = E4M3 ? 512 : 320;
-  static constexpr int READERS = 1 + 8 + (E4M3 ? 4 : 0);   // warps that follow the producer's items
+  static constexpr int CONV = E4M3 ? 8 : 0;            // converting warps
+  static constexpr int THREADS = (12 + CONV) * 32;
+  // registers a thread of the first four warps, of the softmax warps and of the converting ones; the
+  // launch gives every thread 96 (640 threads) or 168 (384)
+  static constexpr int REGS_IO = 80, REGS_SOFT = E4M3 ? 144 : 208, REGS_CONV = 56;
+  static_assert(REGS_IO + 2 * REGS_SOFT + (E4M3 ? 2 * REGS_CONV : 0) <= (E4M3 ? 5 * 96 : 3 * 168), "register split");
+  static constexpr int READERS = 1 + 8 + CONV;   // warps that follow the producer's items
   static_assert(BYTES <= 227 * 1024, "shared memory per CTA");
 };
 
@@ -91,12 +97,14 @@ struct Item {
   int i0, i1, part;   // part: slot of the partial result, -1: a whole unit
 };
 
-// What the tokens of one query tile see.
+// What the tokens of one query tile see, in key tiles: tile kt has a key that some row sees if
+// kt < any_end and (kt >= any_lo or kt < any_sk), and every row sees all of it if
+// kt < all_end and (kt >= all_lo or kt < all_sk).
 struct Span {
-  int n;              // tokens with a position, 0: none
-  int whole;          // all of its tokens have one
-  int e0, e1, l0, l1; // end and window's first position of the first and the last token
-  int sk;             // sinks that the last token sees
+  int n;                          // tokens with a position among them, 0: none
+  int any_end, any_lo, any_sk;
+  int all_end, all_lo, all_sk;
+  int lo, end, sk;                // in positions: the first token's window, the last one's end and sinks
 };
 
 __device__ __forceinline__ Span span_of(const Mask& m, int tokens, int p0, int len, int g, int TQ) {
@@ -104,23 +112,24 @@ __device__ __forceinline__ Span span_of(const Mask& m, int tokens, int p0, int l
   const int at = g * TQ, n = min(tokens - at, TQ), pf = p0 + at, pl = pf + n - 1;
   if (n <= 0 || pl < 0) return s;
   s.n = n;
-  s.whole = pf >= 0;
-  s.e0 = visible_end(m, max(pf, 0), len);
-  s.e1 = visible_end(m, pl, len);
-  s.l0 = window_first(m, s.e0);
-  s.l1 = window_first(m, s.e1);
-  s.sk = m.window ? min(m.sinks, s.e1) : 0;
+  const int e0 = visible_end(m, max(pf, 0), len), l1 = window_first(m, visible_end(m, pl, len));
+  s.end = visible_end(m, pl, len);
+  s.lo = window_first(m, e0);
+  s.sk = m.window ? min(m.sinks, s.end) : 0;
+  s.any_end = (s.end + BK - 1) / BK;
+  s.any_lo = s.lo / BK;
+  s.any_sk = (s.sk + BK - 1) / BK;
+  s.all_end = pf >= 0 ? e0 / BK : 0;
+  s.all_lo = (l1 + BK - 1) / BK;
+  s.all_sk = m.window ? m.sinks / BK : 0;
   return s;
 }
 
-// Some row sees some key of the tile / every row every key.
 __device__ __forceinline__ bool active(const Span& s, int kt) {
-  const int k0 = kt * BK;
-  return s.n > 0 && k0 < s.e1 && (k0 + BK > s.l0 || k0 < s.sk);
+  return kt < s.any_end && (kt >= s.any_lo || kt < s.any_sk);
 }
-__device__ __forceinline__ bool all_seen(const Mask& m, const Span& s, int kt) {
-  const int k0 = kt * BK;
-  return s.whole && k0 + BK <= s.e0 && (k0 >= s.l1 || (m.window && k0 + BK <= m.sinks));
+__device__ __forceinline__ bool all_seen(const Span& s, int kt) {
+  return kt < s.all_end && (kt >= s.all_lo || kt < s.all_sk);
 }
 __device__ __forceinline__ int tile_of(const Item& it, int i) { return i < it.ns ? i : it.w0 + (i - it.ns); }
 
@@ -132,8 +141,8 @@ __device__ __forceinline__ List list_of(const Mask& m, int tokens, int p0, int l
   const Span a = span_of(m, tokens, p0, len, 0, TQ), z = span_of(m, tokens, p0, len, 1, TQ);
   List l{};
   if (a.n == 0 && z.n == 0) return l;
-  l.lo = a.n ? a.l0 : z.l0;
-  l.end = z.n ? z.e1 : a.e1;
+  l.lo = a.n ? a.lo : z.lo;
+  l.end = z.n ? z.end : a.end;
   l.sk = z.n ? z.sk : a.sk;
   l.ns = (l.sk + BK - 1) / BK;
   l.w0 = max(l.ns, l.lo / BK);
@@ -272,7 +281,7 @@ __device__ __noinline__ Wild wild_masks(const Job& j, const Item& it, int end, i
   const Span a = span_of(j.m, it.n, it.p0, it.len, 0, j.TQ), z = span_of(j.m, it.n, it.p0, it.len, 1, j.TQ);
   for (int i = it.i0; i < it.i1; ++i) {
     const int kt = tile_of(it, i);
-    if ((!active(a, kt) || all_seen(j.m, a, kt)) && (!active(z, kt) || all_seen(j.m, z, kt))) continue;
+    if ((!active(a, kt) || all_seen(a, kt)) && (!active(z, kt) || all_seen(z, kt))) continue;
     for (int p = kt * BK; p < min(end, kt * BK + BK); ++p) {
       if (p < lo && !(j.m.window && p < j.m.sinks)) continue;
       const int64_t at = pool_row(j.c, j.s, it.b, it.h, p);
@@ -305,54 +314,64 @@ __device__ __forceinline__ void mask_row(float (&v)[32], int k0, int end, int lo
 }
 
 // ------------------------------------------------------------------ codes into bf16
-// Two bf16 from two codes in the high bytes of the halves of x: the code's bits in bf16's fields
-// are its value times 2^-120 (subnormal codes included).
-__device__ __forceinline__ uint32_t widen(uint32_t x, __nv_bfloat162 f) {
-  const uint32_t y = (x & 0x80008000u) | ((x >> 4) & 0x07f007f0u);
-  const __nv_bfloat162 v = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&y), f);
-  return *reinterpret_cast<const uint32_t*>(&v);
+// Four bf16 (two pairs) from four codes: a code's bits in bf16's fields (sign; three zero bits and the first
+// of the exponent above; the rest below) are its value times 2^-120, subnormal codes included; f
+// holds 2^120 times the scale.
+__device__ __forceinline__ uint2 widen(uint32_t w, __nv_bfloat162 f) {
+  const uint32_t hi = (w & 0x80808080u) | ((w >> 4) & 0x07070707u), lo = (w << 4) & 0xf0f0f0f0u;
+  const uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);
+  const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), f);
+  const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), f);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
 }
-__device__ __forceinline__ __nv_bfloat162 pair_of(uint32_t exponent_field) {
-  const uint32_t b = exponent_field << 7, w = b | (b << 16);
-  return *reinterpret_cast<const __nv_bfloat162*>(&w);
+__device__ __forceinline__ __nv_bfloat162 bf2(uint32_t bits) { return *reinterpret_cast<const __nv_bfloat162*>(&bits); }
+__device__ __forceinline__ uint32_t times(uint32_t x, __nv_bfloat162 f) {
+  const __nv_bfloat162 y = __hmul2(bf2(x), f);
+  return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// A [128][D] tile of codes and its rows' scales into a swizzled bf16 tile (128 threads).
-template <int D>
+// A [128][D] tile of codes and its rows' scales into a swizzled bf16 tile (W warps).  Eight
+// neighbouring threads take 64 columns of two rows, chosen so that neither the 16-byte loads (128-byte
+// swizzled codes at D = 128, plain ones at 64) nor the 16-byte stores of a quarter warp share a bank: rows r
+// and r ^ 5 at D = 128, two adjacent ones at 64.
+template <int D, int W>
 __device__ __forceinline__ void widen_tile(const uint8_t* codes, const uint8_t* scales, uint8_t* tile, int t) {
-  constexpr int LANES = D / 16, ROWS = 128 / LANES;
-  const int c = t % LANES;
-  const __nv_bfloat16 nan = __ushort_as_bfloat16((unsigned short)0x7fff);
+  constexpr int PANELS = D / 64, UNITS = 16 * PANELS / W;   // units of (8 rows, 64 columns): a warp's
+  static_assert(W % PANELS == 0, "a warp stays in its panel");
+  constexpr int ROWS = W / PANELS * 8;                // rows from one of them to the next
+  const int warp = t >> 5, quarter = (t & 31) >> 3, half = (t >> 2) & 1, c = t & 3;
+  const int r8 = D == 128 ? (half ? quarter ^ 5 : quarter) : 2 * quarter + half;
+  const int row = (warp / PANELS) * 8 + r8, panel = warp % PANELS;
+  codes += row * D + (D == 128 ? (((panel * 4 + c) ^ r8) << 4) : c * 16);
+  uint8_t* lo = tile + panel * PANEL + row * 128 + (((2 * c) ^ r8) << 4);
+  uint8_t* hi = tile + panel * PANEL + row * 128 + (((2 * c + 1) ^ r8) << 4);
+  uint32_t s[UNITS], big = 0;
 #pragma unroll
-  for (int pass = 0; pass < LANES; ++pass) {
-    const int row = pass * ROWS + t / LANES;
-    const uint4 x = *reinterpret_cast<const uint4*>(codes + row * D + c * 16);
-    const uint32_t s = scales[row];
-    // 2^120 2^(s - 127) in one factor where it is a bf16 number, else in two; 255: NaN
-    const bool two = s > 134u && s != 255u;
-    const __nv_bfloat162 f = s == 255u ? __nv_bfloat162(nan, nan) : pair_of(two ? 247u : s + 120u);
-    uint32_t y[8];
-    const uint32_t* w = &x.x;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      y[2 * k] = widen(__byte_perm(w[k], 0, 0x1404), f);
-      y[2 * k + 1] = widen(__byte_perm(w[k], 0, 0x3424), f);
+  for (int k = 0; k < UNITS; ++k) {
+    s[k] = scales[row + k * ROWS];
+    big = max(big, s[k]);
+  }
+  // one factor where 2^120 times the scale is a bf16 number; else two, the scale by itself (255: NaN)
+  if (__any_sync(0xffffffffu, big > 134u)) {
+#pragma unroll 1
+    for (int k = 0; k < UNITS; ++k) {
+      const uint32_t sk = scales[row + k * ROWS];
+      const uint4 x = *reinterpret_cast<const uint4*>(codes + k * ROWS * D);
+      const __nv_bfloat162 f = bf2((sk > 134u ? 247u : sk + 120u) * 0x00800080u);
+      const __nv_bfloat162 f2 = bf2(sk == 255u ? 0x7fff7fffu : (sk > 134u ? sk : 127u) * 0x00800080u);
+      const uint2 y0 = widen(x.x, f), y1 = widen(x.y, f), y2 = widen(x.z, f), y3 = widen(x.w, f);
+      *reinterpret_cast<uint4*>(lo + k * ROWS * 128) = make_uint4(times(y0.x, f2), times(y0.y, f2), times(y1.x, f2), times(y1.y, f2));
+      *reinterpret_cast<uint4*>(hi + k * ROWS * 128) = make_uint4(times(y2.x, f2), times(y2.y, f2), times(y3.x, f2), times(y3.y, f2));
     }
-    if (__any_sync(0xffffffffu, two)) {
-      const __nv_bfloat162 f2 = pair_of(two ? s : 127u);
+  } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        const __nv_bfloat162 v = __hmul2(*reinterpret_cast<__nv_bfloat162*>(&y[k]), f2);
-        y[k] = *reinterpret_cast<const uint32_t*>(&v);
-      }
+    for (int k = 0; k < UNITS; ++k) {
+      const uint4 x = *reinterpret_cast<const uint4*>(codes + k * ROWS * D);
+      const __nv_bfloat162 f = bf2((s[k] + 120u) * 0x00800080u);
+      const uint2 y0 = widen(x.x, f), y1 = widen(x.y, f), y2 = widen(x.z, f), y3 = widen(x.w, f);
+      *reinterpret_cast<uint4*>(lo + k * ROWS * 128) = make_uint4(y0.x, y0.y, y1.x, y1.y);
+      *reinterpret_cast<uint4*>(hi + k * ROWS * 128) = make_uint4(y2.x, y2.y, y3.x, y3.y);
     }
-    // 16-byte chunks 2c and 2c + 1 of the row; the upper panel's threads write theirs the other way
-    // round, so that a store's eight threads of a row meet eight different banks
-    uint8_t* base = tile + (c >> 2) * PANEL + row * 128;
-    const int ch = 2 * (c & 3), flip = (c >> 2) & 1, x7 = row & 7;
-    const uint4 a = make_uint4(y[0], y[1], y[2], y[3]), b = make_uint4(y[4], y[5], y[6], y[7]);
-    *reinterpret_cast<uint4*>(base + (((ch + flip) ^ x7) << 4)) = flip ? b : a;
-    *reinterpret_cast<uint4*>(base + (((ch + 1 - flip) ^ x7) << 4)) = flip ? a : b;
   }
 }
 
@@ -393,10 +412,10 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     for (int i = 0; i < 2; ++i) {
-      mbar_init(k_full + i, E4M3 ? 4 : 1);
+      mbar_init(k_full + i, E4M3 ? L::CONV : 1);
       mbar_init(k_empty + i, 1);
       mbar_init(c_full + i, 1);
-      mbar_init(c_empty + i, 4);
+      mbar_init(c_empty + i, E4M3 ? L::CONV : 1);
       mbar_init(s_full + i, 1);
       mbar_init(p_full + i, 4);
       mbar_init(o_full + i, 1);
@@ -405,7 +424,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       wild[i] = 0;
     }
     for (int i = 0; i < 3; ++i) {
-      mbar_init(v_full + i, E4M3 ? 4 : 1);
+      mbar_init(v_full + i, E4M3 ? L::CONV : 1);
       mbar_init(v_empty + i, 1);
     }
     mbar_init(done, 1);
@@ -436,9 +455,9 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
   };
 
   if (warp < L::SOFT0) {
-    if (E4M3) regs_lower<72>();
+    regs_lower<L::REGS_IO>();
     if (warp == 0) {
-      // ---------------- producer: items; Q, then the tiles of K and V, K one ahead
+      // ---------------- producer: items; Q, then K(0), V(0), K(1), ..
       const Plan plan = make_plan(j, gridDim.x);
       if (blockIdx.x == 0 && lane == 0) *j.plan = make_int4(plan.U, plan.R, plan.S, 0);
       const int total = plan.U + plan.R * plan.S;
@@ -517,8 +536,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         };
         ok = load(true, x.i0);
         for (int i = x.i0; ok && i < x.i1; ++i) {
-          if (i + 1 < x.i1) ok = load(true, i + 1);
-          ok = ok && load(false, i);
+          ok = load(false, i);
+          if (ok && i + 1 < x.i1) ok = load(true, i + 1);
         }
         tc += n;
         if (!ok) break;
@@ -535,10 +554,16 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       constexpr uint32_t id_s = idesc_bf16(BQ, BK), id_o = idesc_bf16(BQ, D, /*b_mn_major=*/true);
       const uint64_t qd0 = desc_sw128(smem_u32(smem + L::Q)), kd0 = desc_sw128(smem_u32(smem + L::K));
       const uint64_t vd0 = desc_sw128_mn(smem_u32(smem + L::V), PANEL, 1024);
-      uint32_t tc = 0, nq = 0, np[2] = {0, 0};
+      uint32_t nq = 0, ks = 0, kph = 0, vs = 0, vph = 0, pph[2] = {0, 0};   // slots and phases
       bool ok = true;
-      auto issue_s = [&](int g, uint32_t t) {
-        const uint64_t qd = desc_add(qd0, g * L::TB), kd = desc_add(kd0, (t % L::NK) * L::TB);
+      auto step = [](uint32_t& slot, uint32_t& phase, uint32_t n) {
+        if (++slot == n) {
+          slot = 0;
+          phase ^= 1;
+        }
+      };
+      auto issue_s = [&](int g, uint32_t slot) {
+        const uint64_t qd = desc_add(qd0, g * L::TB), kd = desc_add(kd0, slot * L::TB);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk) {
@@ -549,8 +574,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         }
         __syncwarp();
       };
-      auto issue_pv = [&](int g, uint32_t t, bool first) {
-        const uint64_t vd = desc_add(vd0, (t % L::NV) * L::TB);
+      auto issue_pv = [&](int g, uint32_t slot, bool first) {
+        const uint64_t vd = desc_add(vd0, slot * L::TB);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < 8; ++kk)
@@ -563,56 +588,74 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         if (elect_one()) mma_commit(bar);
         __syncwarp();
       };
+      // (lane 0's copy of the item for all: loop bounds, slots and descriptors stay warp-uniform, where the
+      // tensor instructions take them from)
+      auto uni = [](int v) { return __shfl_sync(0xffffffffu, v, 0); };
       for (uint32_t ni = 0; ok; ++ni) {
-        const Item x = next_item(ni);
-        if (x.state == 0) break;
+        Item x = next_item(ni);
+        if (uni(x.state) == 0) break;
+        x.i0 = uni(x.i0);
+        x.i1 = uni(x.i1);
+        x.ns = uni(x.ns);
+        x.w0 = uni(x.w0);
         const int n = x.i1 - x.i0;
         if (n <= 0) continue;
-        const Span sp[2] = {span_of(j.m, x.n, x.p0, x.len, 0, j.TQ), span_of(j.m, x.n, x.p0, x.len, 1, j.TQ)};
-        int left[2] = {0, 0};   // active tiles to come
-        bool first[2] = {true, true};
-        for (int i = x.i0; i < x.i1; ++i) {
-          left[0] += active(sp[0], tile_of(x, i));
-          left[1] += active(sp[1], tile_of(x, i));
+        Span sp[2];
+        int last[2];            // list index of the group's last active tile
+        bool fresh[2] = {true, true};
+#pragma unroll
+        for (int g = 0; g < 2; ++g) {
+          sp[g] = span_of(j.m, uni(x.n), uni(x.p0), uni(x.len), g, j.TQ);
+          const int kt = sp[g].any_end - 1;
+          last[g] = kt < x.ns ? kt : x.ns + (kt - x.w0);
         }
         ok = mbar_wait_warp(q_full, nq & 1, abort_flag) &&
-             mbar_wait_warp(k_full + tc % L::NK, (tc / L::NK) & 1, abort_flag);
+             mbar_wait_warp(k_full + ks, kph, abort_flag);
         ++nq;
         if (!ok) break;
         fence_after_sync();
-#pragma unroll
-        for (int g = 0; g < 2; ++g)
-          if (active(sp[g], tile_of(x, x.i0))) issue_s(g, tc);
-        commit(k_empty + tc % L::NK);
+        int kt = tile_of(x, x.i0);
+        bool act[2] = {active(sp[0], kt), active(sp[1], kt)};
+        if (act[0]) issue_s(0, ks);
+        if (act[1]) issue_s(1, ks);
+        commit(k_empty + ks);
         if (n == 1) commit(q_empty);
+        step(ks, kph, L::NK);
         for (int i = x.i0; i < x.i1; ++i) {
-          const uint32_t t = tc + (uint32_t)(i - x.i0);
           const bool next = i + 1 < x.i1;
-          ok = (!next || mbar_wait_warp(k_full + (t + 1) % L::NK, ((t + 1) / L::NK) & 1, abort_flag)) &&
-               mbar_wait_warp(v_full + t % L::NV, (t / L::NV) & 1, abort_flag);
-          if (!ok) break;
-          const int kt = tile_of(x, i), kn = tile_of(x, i + 1);
+          kt = tile_of(x, i + 1);
+          const bool actn[2] = {next && active(sp[0], kt), next && active(sp[1], kt)};
+          if (!(ok = mbar_wait_warp(v_full + vs, vph, abort_flag))) break;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
-            if (active(sp[g], kt)) {
-              if (!(ok = mbar_wait_warp(p_full + g, np[g] & 1, abort_flag))) break;
-              ++np[g];
+            if (act[g]) {
+              if (!(ok = mbar_wait_warp(p_full + g, pph[g], abort_flag))) break;
+              pph[g] ^= 1;
               fence_after_sync();
-              issue_pv(g, t, first[g]);
-              first[g] = false;
-              if (--left[g] == 0) commit(o_full + g);
+              issue_pv(g, vs, fresh[g]);
+              fresh[g] = false;
+              if (i == last[g]) commit(o_full + g);
             }
-            if (next && active(sp[g], kn)) {
+            if (g == 0 && next) {
+              if (!(ok = mbar_wait_warp(k_full + ks, kph, abort_flag))) break;
               fence_after_sync();
-              issue_s(g, t + 1);
             }
+            if (actn[g]) issue_s(g, ks);
+            act[g] = actn[g];
           }
           if (!ok) break;
-          if (next) commit(k_empty + (t + 1) % L::NK);
-          if (i + 2 == x.i1) commit(q_empty);
-          commit(v_empty + t % L::NV);
+          commit(v_empty + vs);
+          if (next) {
+            commit(k_empty + ks);
+            if (i + 2 == x.i1) commit(q_empty);
+            step(ks, kph, L::NK);
+          }
+          step(vs, vph, L::NV);
         }
-        tc += n;
+        if (!ok) break;
+#pragma unroll
+        for (int g = 0; g < 2; ++g)   // a part that ends before the group's last tile
+          if (!fresh[g] && last[g] >= x.i1) commit(o_full + g);
       }
       if (!ok && lane == 0) give_up(1);
       // every product complete before TMEM is freed
@@ -621,7 +664,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       mbar_wait(done, 0, &no_abort);
     }
   } else if (warp < L::CONV0) {
-    if (E4M3) regs_raise<184>();
+    regs_raise<L::REGS_SOFT>();
     // ---------------- softmax group g over query tile g, thread = query row = TMEM lane
     const int g = (warp - L::SOFT0) >> 2, qd = warp & 3, r = qd * 32 + lane;
     const uint32_t lane_off = (uint32_t)(qd * 32) << 16;
@@ -643,7 +686,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       for (int i = x.i0; i < x.i1; ++i) {
         const int kt = tile_of(x, i);
         if (!active(sp, kt)) continue;
-        const bool partial = !all_seen(j.m, sp, kt);
+        const bool partial = !all_seen(sp, kt);
         if (partial) {
           const uint32_t t = tc + (uint32_t)(i - x.i0);
           if (!(ok = mbar_wait_warp(v_full + t % L::NV, (t / L::NV) & 1, abort_flag))) break;
@@ -653,25 +696,30 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         if (!(ok = mbar_wait_warp(s_full + g, ns & 1, abort_flag))) break;
         ++ns;
         fence_after_sync();
-        float s0[32], s1[32], s2[32], s3[32];
-        tmem_ld32(sc, s0);
-        tmem_ld32(sc + 32, s1);
-        tmem_ld32(sc + 64, s2);
-        tmem_ld32(sc + 96, s3);
-        tmem_wait_ld();
-        if (partial) {
-          const int k0 = kt * BK;
-          mask_row(s0, k0, end, lo, sk);
-          mask_row(s1, k0 + 32, end, lo, sk);
-          mask_row(s2, k0 + 64, end, lo, sk);
-          mask_row(s3, k0 + 96, end, lo, sk);
-        }
+        // the row's 128 scores, 64 at a time and read twice (maximum, weights): fewer registers and
+        // half the instructions than the whole row at once, which the instruction caches repay
+        const int k0 = kt * BK;
+        auto scores = [&](int half, float (&a)[32], float (&b)[32]) {
+          tmem_ld32(sc + half * 64, a);
+          tmem_ld32(sc + half * 64 + 32, b);
+          tmem_wait_ld();
+          if (partial) {
+            mask_row(a, k0 + half * 64, end, lo, sk);
+            mask_row(b, k0 + half * 64 + 32, end, lo, sk);
+          }
+        };
         float tmax;
         {
           float t[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) t[k] = -INFINITY;
-          max_acc(t, s0); max_acc(t, s1); max_acc(t, s2); max_acc(t, s3);
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            float a[32], b[32];
+            scores(half, a, b);
+            max_acc(t, a);
+            max_acc(t, b);
+          }
           tmax = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
         }
         tmax *= j.m.sl2;
@@ -684,16 +732,17 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         }
         const float nm = mrun == -INFINITY ? 0.f : -mrun;   // (a row that has seen nothing yet: all weights 0)
         float2 lab = make_float2(0.f, 0.f);
-        {
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          float a[32], b[32];
           uint32_t pk[32];
-          exp_pack(s0, s1, j.m.sl2, nm, lab, pk);
-          tmem_st32(sc, pk);
-          exp_pack(s2, s3, j.m.sl2, nm, lab, pk);
-          tmem_st32(sc + 32, pk);
+          scores(half, a, b);
+          exp_pack(a, b, j.m.sl2, nm, lab, pk);
+          tmem_st32(sc + half * 32, pk);
         }
         if (__any_sync(0xffffffffu, raise && some)) {
           const float alpha = raise ? ex2(mprev - mrun) : 1.0f;
-#pragma unroll
+#pragma unroll 1
           for (int c = 0; c < D / 32; ++c) {
             float v[32];
             tmem_ld32(oc + c * 32, v);
@@ -730,7 +779,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       const float inv = l == 0.f ? 0.f : 1.0f / l;         // (a NaN stays one)
       float* part = whole ? nullptr : j.parts + (int64_t)x.part * (256 * (D + 1));
       if (!whole) part[256 * D + g * BQ + r] = l == 0.f ? -INFINITY : mrun + log2f(l);
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         float v[32];
         if (some) {   // warp-uniform
@@ -766,10 +815,11 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       if (lane == 0) mbar_arrive(it_empty + (ni & 1));
     }
     if (!ok && lane == 0) give_up(2);
-  } else {
-    if (E4M3) regs_lower<72>();
-    // ---------------- codes into bf16, in the order of the copies: K(0), K(1), V(0), K(2), V(1), ..
-    const int t128 = threadIdx.x - L::CONV0 * 32;
+  } else if constexpr (E4M3) {
+    regs_lower<L::REGS_CONV>();
+    // ---------------- codes into bf16, in the order of the copies: K(0), V(0), K(1), V(1), .. (V(i) is wanted
+    // half a step before K(i + 1))
+    const int tid = threadIdx.x - L::CONV0 * 32;
     uint32_t tc = 0, cc = 0;
     bool ok = true;
     auto turn = [&](bool is_k, uint32_t t) -> bool {
@@ -777,8 +827,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       const uint32_t nb = is_k ? L::NK : L::NV, sl = t % nb;
       if (!mbar_wait_warp(c_full + (c & 1), (c >> 1) & 1, abort_flag)) return false;
       if (t >= nb && !mbar_wait_warp((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
-      widen_tile<D>(smem + L::CODES + (c & 1) * 128 * D, smem + L::SCALES + (c & 1) * 128,
-                    smem + (is_k ? L::K : L::V) + sl * L::TB, t128);
+      widen_tile<D, L::CONV>(smem + L::CODES + (c & 1) * 128 * D, smem + L::SCALES + (c & 1) * 128,
+                    smem + (is_k ? L::K : L::V) + sl * L::TB, tid);
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
@@ -794,8 +844,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       if (n <= 0) continue;
       ok = turn(true, tc);
       for (int i = 0; ok && i < n; ++i) {
-        if (i + 1 < n) ok = turn(true, tc + i + 1);
-        ok = ok && turn(false, tc + i);
+        ok = turn(false, tc + i);
+        if (ok && i + 1 < n) ok = turn(true, tc + i + 1);
       }
       tc += n;
     }
@@ -891,7 +941,8 @@ bool make_maps(const Pool& c, Maps* m) {
   const int64_t dim[4] = {c.d, c.page_len, c.H, c.n_pages};
   const int64_t stride[3] = {(int64_t)c.d * es, (int64_t)c.page_len * c.d * es, (int64_t)c.H * c.page_len * c.d * es};
   const int box[4] = {c.e4m3 ? c.d : 64, std::min(c.page_len, BK), 1, 1};
-  return make_map_4d(&m->k, c.k, es, dim, stride, box, !c.e4m3) && make_map_4d(&m->v, c.v, es, dim, stride, box, !c.e4m3);
+  const bool swizzle = !c.e4m3 || c.d == 128;   // (see widen_tile)
+  return make_map_4d(&m->k, c.k, es, dim, stride, box, swizzle) && make_map_4d(&m->v, c.v, es, dim, stride, box, swizzle);
 }
 
 size_t attend_tc_scratch(const Pool& c) { return 256 + sizeof(float) * (size_t)MAX_PARTS * 256 * (c.d + 1); }
