@@ -49,6 +49,15 @@ struct OnDevice {
 
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
+// Which attention kernel: the one for few rows where a sequence's tokens and the heads that share a key head make
+// no more than ROWS_MOST.
+constexpr int ROWS_MOST = 16;
+bool few_rows(const cache::Pool& c, int Hq, int max_rows) { return (int64_t)max_rows * (Hq / c.H) <= ROWS_MOST; }
+
+size_t scratch_of(const cache::Pool& c, int Hq, int max_rows) {
+  return few_rows(c, Hq, max_rows) ? cache::attend_rows_scratch(c, Hq / c.H, max_rows) : cache::attend_tc_scratch(c);
+}
+
 dkv_status_t status_of(cudaError_t e) { return e == cudaSuccess ? DKV_OK : DKV_ERR_CUDA; }
 
 dkv_status_t check_seqs(const cache::Pool& c, const dkv_cache_seqs_t* s, int32_t rows, cache::Seqs* out) {
@@ -93,7 +102,8 @@ dkv_status_t dkv_cache_create(dkv_cache_t* out, int32_t H, int32_t d, int32_t pa
   if (taken(cudaGetDevice(&dev)) != cudaSuccess) return DKV_ERR_CUDA;
   if (taken(cudaGetDeviceProperties(&prop, dev)) != cudaSuccess) return DKV_ERR_CUDA;
   if (prop.major != 10 || prop.minor != 3) return DKV_ERR_UNSUPPORTED;   // built for sm_103a only
-  if (cache::attend_tc_set_smem_limits() != cudaSuccess) return DKV_ERR_CUDA;
+  if (cache::attend_tc_set_smem_limits() != cudaSuccess || cache::attend_rows_set_smem_limits() != cudaSuccess)
+    return DKV_ERR_CUDA;
   if (taken(cudaMemset(buf->status, 0, 2 * sizeof(int32_t))) != cudaSuccess) return DKV_ERR_CUDA;
   dkv_cache_s* c = new (std::nothrow) dkv_cache_s();
   if (!c) return DKV_ERR_ARG;
@@ -102,7 +112,7 @@ dkv_status_t dkv_cache_create(dkv_cache_t* out, int32_t H, int32_t d, int32_t pa
   c->pool = cache::Pool{buf->k, buf->v, e4m3 ? buf->k_scale : nullptr, e4m3 ? buf->v_scale : nullptr, buf->status,
                         H, d, page_len, log2, n_pages, e4m3 ? 1 : 0};
   c->device = dev;
-  if (!cache::make_maps(c->pool, &c->maps)) {
+  if (!cache::make_tc_maps(c->pool, &c->maps) || !cache::make_rows_maps(c->pool, &c->maps)) {
     delete c;
     return DKV_ERR_CUDA;
   }
@@ -147,7 +157,7 @@ dkv_status_t dkv_cache_read(dkv_cache_t c, const dkv_cache_seqs_t* seqs, const i
 size_t dkv_cache_attend_scratch_size(dkv_cache_t c, int32_t n_seq, int32_t H_q, int32_t rows, int32_t max_rows) {
   if (!c || n_seq < 1 || n_seq > kMaxSeqs || rows < 1 || rows > kMaxRows || max_rows < 1) return 0;
   if (H_q < c->pool.H || H_q % c->pool.H || H_q / c->pool.H > kMaxGroup) return 0;
-  return cache::attend_scratch(c->pool, n_seq, H_q, rows, max_rows);
+  return scratch_of(c->pool, H_q, max_rows < rows ? max_rows : rows);
 }
 
 dkv_status_t dkv_cache_attend(dkv_cache_t c, const dkv_cache_seqs_t* seqs, const void* Q, int32_t H_q, int32_t rows,
@@ -166,13 +176,14 @@ dkv_status_t dkv_cache_attend(dkv_cache_t c, const dkv_cache_seqs_t* seqs, const
   if (st == DKV_OK) st = check_packed(O, H_q, rows, o_head, o_row, true, &o);
   if (st != DKV_OK) return st;
   const int max_rows = how->max_rows < rows ? how->max_rows : rows;
-  if (scratch_bytes < cache::attend_scratch(c->pool, s.n, H_q, rows, max_rows)) return DKV_ERR_NOMEM;
+  if (scratch_bytes < scratch_of(c->pool, H_q, max_rows)) return DKV_ERR_NOMEM;
   const float scale = how->scale > 0.f ? how->scale : 1.0f / std::sqrt((float)c->pool.d);
   const cache::Mask m{scale * 1.4426950408889634f, how->window, how->sinks, how->block};
   OnDevice on(c->device);
   if (!on.ok) return DKV_ERR_CUDA;
   c->last = (cudaStream_t)stream;
-  return status_of(cache::launch_attend(c->pool, c->maps, s, q, o, H_q, max_rows, m, scratch, (cudaStream_t)stream));
+  auto* launch = few_rows(c->pool, H_q, max_rows) ? cache::launch_attend_rows : cache::launch_attend_tc;
+  return status_of(launch(c->pool, c->maps, s, q, o, H_q, max_rows, m, scratch, (cudaStream_t)stream));
 }
 
 dkv_status_t dkv_cache_sync(dkv_cache_t c) {

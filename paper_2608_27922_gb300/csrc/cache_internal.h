@@ -115,23 +115,27 @@ __host__ __device__ __forceinline__ int window_first(const Mask& m, int end) {
 }
 #endif
 
-// Boxes of the pages as the tensor-core kernel loads them, made once for a handle.
+// Boxes of the pages as the two attention kernels load them, made once for a handle.
 struct Maps {
-  CUtensorMap k, v;
+  CUtensorMap k, v;     // chunks of tokens: 128 positions a tile
+  CUtensorMap rk, rv;   // few rows: a stage
 };
-bool make_maps(const Pool& c, Maps* m);
 
 cudaError_t launch_write(const Pool& c, const Seqs& s, const Packed& k, const Packed& v, cudaStream_t st);
 cudaError_t launch_read(const Pool& c, const Seqs& s, const int32_t* first, const Packed& k, const Packed& v,
                         cudaStream_t st);
-size_t attend_scratch(const Pool& c, int n_seq, int Hq, int rows, int max_rows);
-cudaError_t launch_attend(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
-                          int max_rows, const Mask& m, void* scratch, cudaStream_t st);
 // chunks of tokens, on the tensor cores
-cudaError_t attend_tc_set_smem_limits();   // on the current device
+bool make_tc_maps(const Pool& c, Maps* m);
+cudaError_t attend_tc_set_smem_limits();     // on the current device
 size_t attend_tc_scratch(const Pool& c);
 cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
                              int max_rows, const Mask& m, void* scratch, cudaStream_t st);
+// few query rows a sequence and key head
+bool make_rows_maps(const Pool& c, Maps* m);
+cudaError_t attend_rows_set_smem_limits();   // on the current device
+size_t attend_rows_scratch(const Pool& c, int G, int max_rows);
+cudaError_t launch_attend_rows(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
+                               int max_rows, const Mask& m, void* scratch, cudaStream_t st);
 
 }  // namespace cache
 }  // namespace dkv

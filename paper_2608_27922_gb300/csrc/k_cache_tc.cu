@@ -33,7 +33,7 @@
 namespace dkv {
 
 bool make_map_4d(CUtensorMap* m, const void* base, int elem_bytes, const int64_t (&dim)[4], const int64_t (&stride)[3],
-                 const int (&box)[4], bool swizzle);
+                 const int (&box)[4], int swizzle);
 
 namespace cache {
 
@@ -936,12 +936,12 @@ cudaError_t attend_tc_set_smem_limits() {
   return e;
 }
 
-bool make_maps(const Pool& c, Maps* m) {
+bool make_tc_maps(const Pool& c, Maps* m) {
   const int es = c.e4m3 ? 1 : 2;
   const int64_t dim[4] = {c.d, c.page_len, c.H, c.n_pages};
   const int64_t stride[3] = {(int64_t)c.d * es, (int64_t)c.page_len * c.d * es, (int64_t)c.H * c.page_len * c.d * es};
   const int box[4] = {c.e4m3 ? c.d : 64, std::min(c.page_len, BK), 1, 1};
-  const bool swizzle = !c.e4m3 || c.d == 128;   // (see widen_tile)
+  const int swizzle = !c.e4m3 || c.d == 128 ? 128 : 0;   // (see widen_tile)
   return make_map_4d(&m->k, c.k, es, dim, stride, box, swizzle) && make_map_4d(&m->v, c.v, es, dim, stride, box, swizzle);
 }
 
@@ -956,7 +956,7 @@ cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, con
   const int64_t head = q.head ? q.head : c.d, row = q.row ? q.row : c.d;   // (one head or row: any stride)
   const int64_t stride[3] = {head * 2, row * 2, G * head * 2};
   const int box[4] = {64, G, TQ, 1};
-  if (!make_map_4d(&mq, q.p, 2, dim, stride, box, true)) return cudaErrorInvalidValue;
+  if (!make_map_4d(&mq, q.p, 2, dim, stride, box, 128)) return cudaErrorInvalidValue;
   Job job{c, s, m, o, G, TQ, max_rows, 1, static_cast<int4*>(scratch),
           reinterpret_cast<float*>(static_cast<char*>(scratch) + 256)};
   if (c.d == 128)

@@ -1441,9 +1441,9 @@ bool make_map_rows(CUtensorMap* m, const void* base, int64_t rows, int64_t heads
 }
 
 // Any 4-D tensor of 1- or 2-byte elements (strides in bytes, of dimensions 1 to 3): boxes of box[0] x box[1] x
-// box[2] x box[3] elements, 128-byte swizzle or none; out-of-range places read as zeros.
+// box[2] x box[3] elements, swizzled over 128 or 64 bytes or not at all (0); out-of-range places read as zeros.
 bool make_map_4d(CUtensorMap* m, const void* base, int elem_bytes, const int64_t (&dim)[4], const int64_t (&stride)[3],
-                 const int (&box)[4], bool swizzle) {
+                 const int (&box)[4], int swizzle) {
   EncodeTiledFn fn = encode_fn();
   if (!fn) return false;
   cuuint64_t dims[4], strides[3];
@@ -1455,7 +1455,9 @@ bool make_map_4d(CUtensorMap* m, const void* base, int elem_bytes, const int64_t
   }
   return fn(m, elem_bytes == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4,
             const_cast<void*>(base), dims, strides, boxes, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-            swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            swizzle == 128 ? CU_TENSOR_MAP_SWIZZLE_128B
+            : swizzle == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                            : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
