@@ -8,7 +8,9 @@
 // takes an equal stretch of it, whatever units it belongs to: no warp waits for another, and the
 // split over a long cache, over many sequences and over ragged lengths is the same one.  A unit inside one
 // stretch is finished there; one that a boundary cuts leaves a partial result for each warp that
-// holds some of it, joined by rows_merge.
+// holds some of it: a CTA joins its own warps' parts, and of the CTAs that share a unit the one that is
+// done last joins theirs, in the order of the CTAs (a second kernel for it took 2 us of the GPU's time
+// and 3 of the host's, as long as the rest of a small call).
 //
 // A warp streams its stages through a ring of its own (TMA boxes of one page, 128-byte swizzled;
 // one lane issues, a barrier a slot), scores them with mma.sync m16n8k16 (16 rows fill one such
@@ -25,6 +27,7 @@
 #include "tc_ptx.cuh"
 
 #include <algorithm>
+#include <atomic>
 
 namespace dkv {
 
@@ -42,7 +45,19 @@ constexpr int MAX_CTAS = 152;
 constexpr int WORKERS = WARPS * MAX_CTAS;
 constexpr int ROWS = 16;
 constexpr float RESCALE_LOG2 = 8.0f;
-constexpr int MIN_STAGES = 4;    // stages of a stretch, at least: below that the joining costs more
+constexpr int MIN_STAGES = 1;    // stages of a warp, at least
+
+// What a worker's stretch leaves unfinished.
+struct Stretch {
+  int head;            // 1: a part of a unit that began before it
+  int head_smem;       //   and its part is in the warp's ring: the stretch's last unit, nothing follows
+  int head_ends;       //   that ends in it
+  int tail;            // 1: a first part of a unit that goes on behind it
+  int first, last;     // CTAs of the head's unit's first stage and of the tail's unit's last one
+  int hlast;           // CTA of the head's unit's last stage
+  int h, tile, rows, r0;      // of the tail's unit
+  int hh, htile, hrows, hr0;  // of the head's
+};
 
 template <int D, bool E4M3>
 struct Lay {
@@ -55,8 +70,10 @@ struct Lay {
   static constexpr int RING = SLOTS * SLOT;                // a warp's
   static constexpr int SCALES = WARPS * RING;              // [warps][slots][2][KT] scale bytes
   static constexpr int BARS = SCALES + (E4M3 ? WARPS * SLOTS * 2 * KT : 0);
-  static constexpr int BYTES = BARS + WARPS * SLOTS * 8;
+  static constexpr int INFO = BARS + WARPS * SLOTS * 8;
+  static constexpr int BYTES = INFO + WARPS * (int)sizeof(Stretch) + 16;
   static_assert(BYTES <= 227 * 1024, "shared memory per CTA");
+  static_assert(ROWS * (D + 4) * 4 <= RING, "a part in the ring");
 };
 
 struct Job {
@@ -66,10 +83,12 @@ struct Job {
   Packed q, o;
   int G, max_rows;
   int part_rows;     // rows of a partial result
-  int4* meta;        // [WORKERS][2] the unit that is cut first in the worker's stretch: {sequence, key head, row tile,
-                     //   its last worker}, {rows, -, -, -}; .w < 0: none
-  float* parts;      // [2 WORKERS][part_rows][D + 4] (outputs, then a sum's logarithm a row): a stretch's first unit,
-                     //   its last one
+  float* parts;      // partial results, [part_rows][D + 4] each (outputs, then the logarithm of a row's sum): one of every
+                     //   worker (a unit that its stretch begins in the middle of and goes on behind; its last unit's
+                     //   stays in shared memory), then two of every CTA (a unit from before it, one that goes on behind)
+  unsigned long long* arrived;   // [MAX_CTAS] CTAs that are done with the unit that begins in a CTA and goes on behind it: the
+                     //   call's number << 16 | their count; anything else counts as none (the scratch comes as it is)
+  unsigned long long call;
 };
 
 // One sequence's share of the range.
@@ -105,41 +124,47 @@ __device__ __forceinline__ Span span_of(const Job& j, int b) {
   return x;
 }
 
-__device__ __forceinline__ int64_t stages_of(const Job& j, const Span& x) { return (int64_t)x.tiles * j.c.H * x.stages; }
+__device__ __forceinline__ int stages_of(const Job& j, const Span& x) { return x.tiles * j.c.H * x.stages; }
 
-// All lanes of a warp.
+// Stages of the whole range; `first`: the span of sequence `lane`.  All lanes of a warp.
 template <int KT>
-__device__ int64_t total_stages(const Job& j) {
+__device__ int total_stages(const Job& j, Span& first) {
+  const int lane = threadIdx.x & 31;
   int64_t mine = 0;
-  for (int b = threadIdx.x & 31; b < j.s.n; b += 32) {
+  first = Span{};
+  for (int b = lane; b < j.s.n; b += 32) {
     const Span x = span_of<KT>(j, b);
+    if (b == lane) first = x;
     if (x.n > j.max_rows) fail(j.c.status, DEV_INCONSISTENT, SITE_CHUNK);
-    mine += stages_of(j, x);
+    mine += (int64_t)x.tiles * j.c.H * x.stages;
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-  return mine;
+  if (mine > 0x7fffffff) {   // 2^31 stages: more than 17 TB of keys and values
+    fail(j.c.status, DEV_INCONSISTENT, SITE_LEN);
+    return 0;
+  }
+  return (int)mine;
 }
 
 // Sequence that holds stage `at` of the range, and where its stages begin.  All lanes of a warp.
 struct Place {
-  int b;
-  int64_t begin;
+  int b, begin;
   Span x;
 };
 template <int KT>
-__device__ Place find(const Job& j, int64_t at) {
+__device__ Place find(const Job& j, int at, const Span& first) {
   const int lane = threadIdx.x & 31;
-  int64_t begin = 0;
+  int begin = 0;
   for (int b0 = 0;; b0 += 32) {
     const int b = b0 + lane;
-    Span x{};
-    if (b < j.s.n) x = span_of<KT>(j, b);
-    const int64_t mine = stages_of(j, x);
-    int64_t incl = mine;
+    Span x = first;
+    if (b0 > 0) x = b < j.s.n ? span_of<KT>(j, b) : Span{};
+    const int mine = stages_of(j, x);
+    int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t v = __shfl_up_sync(0xffffffffu, incl, o);
+      const int v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
     const unsigned past = __ballot_sync(0xffffffffu, b < j.s.n && begin + incl > at);
@@ -198,6 +223,122 @@ __device__ __forceinline__ int chunk_at(int r, int c) {
 
 __device__ __forceinline__ bool sees(int p, int end, int lo, int sk) { return p < end && (p >= lo || p < sk); }
 
+// A unit's count of CTAs that are done with it: call << 16 | count once somebody has put it there, before that
+// whatever the memory held.  begin_count, early: the CTA in which the unit begins does so; should another be done
+// before that, it sees that the number is not the call's.
+__device__ __forceinline__ void begin_count(unsigned long long* at, unsigned long long call) {
+  const unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(at);
+  if ((old >> 16) != call) atomicCAS(at, old, call << 16);
+}
+// One more of n; true for the last one, which leaves nothing behind.  (One trip to L2 as a rule; taking turns with
+// compare and swap instead cost 13 CTAs 6 us.)
+__device__ bool arrive(unsigned long long* at, unsigned long long call, int n) {
+  for (;;) {
+    unsigned long long old = atomicAdd(at, 1ull);
+    if ((old >> 16) == call) {
+      if ((int)(old & 0xffffu) + 1 < n) return false;
+      atomicExch(at, 0ull);
+      return true;
+    }
+    // nobody's count yet: the number that was added to was not one; put the call's there, or see that it is
+    old = *reinterpret_cast<volatile unsigned long long*>(at);
+    while ((old >> 16) != call) {
+      const unsigned long long got = atomicCAS(at, old, call << 16);
+      if (got == old) break;
+      old = got;
+    }
+  }
+}
+
+// One warp's sum of parts p = first, first + step, .. < n of a row (at(p): outputs [D], then the row's logarithm at
+// `log`): m, l and o (columns c * 32 + lane) as a softmax over them, in their order.  Short loops: these
+// instructions run once or twice, and fetching them is most of what they cost.
+template <int D, typename At>
+__device__ __forceinline__ void sum_parts(At at, int first, int n, int step, int log, float& m, float& l, float (&o)[D / 32]) {
+  const int lane = threadIdx.x & 31;
+  m = -INFINITY;
+  l = 0.f;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) o[c] = 0.f;
+#pragma unroll 1
+  for (int p0 = first; p0 < n; p0 += 32 * step) {
+    const int mine = p0 + lane * step, count = min(32, (n - p0 + step - 1) / step);
+    const float z = mine < n ? __ldcg(at(mine) + log) : -INFINITY;
+    float top = fmaxf(m, z);
+#pragma unroll
+    for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+    const float a = m == -INFINITY ? 0.f : exp2f(m - top);
+    const float weight = z == -INFINITY ? 0.f : exp2f(z - top);   // (nothing seen: 0; a NaN stays one)
+    m = top;
+    l *= a;
+#pragma unroll
+    for (int c = 0; c < D / 32; ++c) o[c] *= a;
+#pragma unroll 4
+    for (int k = 0; k < count; ++k) {
+      const float w = __shfl_sync(0xffffffffu, weight, k);
+      const float* x = at(p0 + k * step) + lane;
+      l += w;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) {
+        const float v = __ldcg(x + c * 32);
+        if (w != 0.f) o[c] = fmaf(w, v, o[c]);
+      }
+    }
+  }
+}
+
+template <int D>
+__device__ __forceinline__ void store_row(const Job& j, int h, int tile, int r0, int r, float l, const float (&o)[D / 32]) {
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const int lane = threadIdx.x & 31, i = tile * ROWS + r, tok = i / j.G, hq = i - tok * j.G;
+  __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + hq) * j.o.head + (int64_t)(r0 + tok) * j.o.row;
+#pragma unroll
+  for (int c = 0; c < D / 32; ++c) dst[c * 32 + lane] = __float2bfloat16_rn(o[c] * inv);
+}
+
+// Joins the n CTAs' parts of a unit, the first one's from CTA `first`, in the CTAs' order: a row a warp, or, where the
+// parts are many for one warp, all warps at a row.  All threads of the CTA; room: shared memory.
+template <int D>
+__device__ void join(const Job& j, int h, int tile, int rows, int r0, int first, int n, float* room) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool shared = n > 32;
+  auto at = [&](int p) { return j.parts + (int64_t)(WORKERS + 2 * (first + p) + (p == 0 ? 1 : 0)) * j.part_rows * (D + 4); };
+#pragma unroll 1
+  for (int r = shared ? 0 : warp; r < rows; r += shared ? 1 : WARPS) {
+    float m, l, o[D / 32];
+    auto row_at = [&](int p) { return at(p) + r * D; };
+    sum_parts<D>(row_at, shared ? warp : 0, n, shared ? WARPS : 1, j.part_rows * D + r - r * D, m, l, o);
+    if (shared) {                          // the warps' sums, as parts again
+      __syncthreads();
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) room[warp * (D + 1) + c * 32 + lane] = o[c] * inv;
+      if (lane == 0) room[warp * (D + 1) + D] = l == 0.f ? -INFINITY : m + log2f(l);
+      __syncthreads();
+      if (warp != 0) continue;
+      m = -INFINITY;
+      const float z = lane < WARPS ? room[lane * (D + 1) + D] : -INFINITY;
+      float top = z;
+#pragma unroll
+      for (int w = 16; w; w >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+      const float weight = z == -INFINITY ? 0.f : exp2f(z - top);
+      l = 0.f;
+#pragma unroll
+      for (int c = 0; c < D / 32; ++c) o[c] = 0.f;
+#pragma unroll 1
+      for (int w = 0; w < WARPS; ++w) {
+        const float a = __shfl_sync(0xffffffffu, weight, w);
+        l += a;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c)
+          if (a != 0.f) o[c] = fmaf(a, room[w * (D + 1) + c * 32 + lane], o[c]);
+      }
+    }
+    store_row<D>(j, h, tile, r0, r, l, o);
+  }
+  __syncthreads();
+}
+
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(WARPS * 32, 1)
     cache_attend_rows(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -213,94 +354,56 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   uint8_t* ring = smem + warp * L::RING;
   uint8_t* scales = smem + L::SCALES + warp * (L::SLOTS * 2 * KT);
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::BARS) + warp * L::SLOTS;
+  Stretch* info = reinterpret_cast<Stretch*>(smem + L::INFO);
   if (lane == 0) {
     for (int i = 0; i < L::SLOTS; ++i) mbar_init(bars + i, 1);
     fence_barrier_init();
   }
+  if (threadIdx.x == 0) begin_count(j.arrived + blockIdx.x, j.call);
   __syncwarp();
-  pdl_trigger();
 
-  // neighbouring stretches on different SMs: where there are few, each has an SM to itself
-  const int worker = warp * gridDim.x + blockIdx.x;
-  const int64_t total = total_stages<KT>(j);
-  const int64_t most = (total + MIN_STAGES - 1) / MIN_STAGES;
-  const int workers = (int)min(most, (int64_t)(WARPS * gridDim.x));
-  int64_t at = 0, stop = 0;
-  if (worker < workers) {
-    at = total * worker / workers;
-    stop = total * (worker + 1) / workers;
+  // The CTAs' stretches follow one another, a CTA's warps' too, so that a unit's parts are joined in the CTA
+  // first; where there are few stages, few warps of every CTA have one.
+  Span first;
+  const int total = total_stages<KT>(j, first);
+  const int per = min(WARPS, max(1, total / (MIN_STAGES * (int)gridDim.x)));   // warps at work
+  const int workers = min(total, per * (int)gridDim.x);
+  const int worker = (int)blockIdx.x * per + warp;
+  // the first `more` stretches have one stage more than the others
+  const int least = workers > 0 ? (int)((unsigned)total / (unsigned)workers) : 0, more = total - least * workers;
+  int at = 0, stop = 0;
+  if (warp < per && worker < workers) {
+    at = worker * least + min(worker, more);
+    stop = at + least + (worker < more ? 1 : 0);
   }
-  int4 cut0 = make_int4(0, 0, 0, -1), cut1 = make_int4(0, 0, 0, 0);
+  if (lane == 0) info[warp].head = info[warp].tail = 0;
   uint32_t issued = 0, used = 0;          // stages, over all segments: slot and phase of the ring
   volatile int no_abort = 0;
   bool ok = true;
 
   while (ok && at < stop) {
     // ---- the segment: stages [k0, k1) of a unit's list
-    const Place pl = find<KT>(j, at);
+    const Place pl = find<KT>(j, at, first);
     const Span& x = pl.x;
-    const int64_t rel = at - pl.begin;
-    const int unit = (int)(rel / x.stages), k0 = (int)(rel % x.stages);
-    const int h = unit / x.tiles, tile = unit % x.tiles;
-    const int k1 = (int)min((int64_t)x.stages, k0 + (stop - at));
+    const int unit = (int)((unsigned)(at - pl.begin) / (unsigned)x.stages), k0 = at - pl.begin - unit * x.stages;
+    const int h = (int)((unsigned)unit / (unsigned)x.tiles), tile = unit - h * x.tiles;
+    const int k1 = min(x.stages, k0 + (stop - at));
     const int rows = min(ROWS, x.n * j.G - tile * ROWS);
-    const int boxr = min(KT, j.c.page_len), nbox = KT / boxr;
+    const int boxr = min(KT, j.c.page_len), box_log2 = min(KT == 16 ? 4 : 5, j.c.page_log2);
+    const int nbox_log2 = (KT == 16 ? 4 : 5) - box_log2, nbox = 1 << nbox_log2;   // boxes of a stage: 1 or 2
 
-    // page of box i of the segment, 32 at a time with the lanes; nobody's where no token sees into it
-    auto page_of = [&](int i) -> int {
-      const int k = k0 + i / nbox;
-      const int p = (k < x.ns ? k : x.w0 + (k - x.ns)) * KT + (i % nbox) * boxr;
-      if (k >= k1 || p >= x.end || !(p + boxr > x.lo || p < x.sk)) return j.c.n_pages;
-      const int page = __ldg(j.s.table + (int64_t)pl.b * j.s.max_pages + (p >> j.c.page_log2));
-      if ((unsigned)page >= (unsigned)j.c.n_pages) {
-        fail(j.c.status, DEV_INCONSISTENT, SITE_PAGE);
-        return j.c.n_pages;
-      }
-      return page;
+    // first position of box i of the segment, and whether some token sees into it
+    auto place_of = [&](int i) {
+      const int k = k0 + (i >> nbox_log2);
+      return (k < x.ns ? k : x.w0 + (k - x.ns)) * KT + ((i & (nbox - 1)) << box_log2);
     };
-    int pages = page_of(lane), pages_next = page_of(32 + lane), base = 0;
-    auto issue = [&](int k) {             // stage k0 + k into the ring
-      const int slot = issued % L::SLOTS;
-      ++issued;
-      const int first = k * nbox;
-      if (first - base >= 32) {           // (32 is a multiple of nbox)
-        base += 32;
-        pages = pages_next;
-        pages_next = page_of(base + 32 + lane);
-      }
-      int pg[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) pg[i] = i < nbox ? __shfl_sync(0xffffffffu, pages, first - base + i) : j.c.n_pages;
-      if (lane != 0) return;
-      const int kk = k0 + k, p = (kk < x.ns ? kk : x.w0 + (kk - x.ns)) * KT;
-      uint32_t bytes = 2 * L::TILE;
-      if (E4M3)
-        for (int i = 0; i < nbox; ++i) bytes += pg[i] < j.c.n_pages ? 2 * boxr : 0;
-      mbar_arrive_expect_tx(bars + slot, bytes);
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        if (i >= nbox) break;
-        const int sl = (p + i * boxr) & (j.c.page_len - 1);
-        uint8_t* dst = ring + slot * L::SLOT;
-        if (E4M3) {
-          tma_load_4d(dst + i * boxr * D, &tmK, bars + slot, 0, sl, h, pg[i]);
-          tma_load_4d(dst + L::TILE + i * boxr * D, &tmV, bars + slot, 0, sl, h, pg[i]);
-          if (pg[i] < j.c.n_pages) {
-            const int64_t row = (((int64_t)pg[i] * j.c.H + h) << j.c.page_log2) + sl;
-            bulk_load(scales + slot * 2 * KT + i * boxr, j.c.ks + row, boxr, bars + slot);
-            bulk_load(scales + slot * 2 * KT + KT + i * boxr, j.c.vs + row, boxr, bars + slot);
-          }
-        } else {
-#pragma unroll
-          for (int n = 0; n < D / 64; ++n) {
-            tma_load_4d(dst + n * L::PANEL + i * boxr * 128, &tmK, bars + slot, n * 64, sl, h, pg[i]);
-            tma_load_4d(dst + L::TILE + n * L::PANEL + i * boxr * 128, &tmV, bars + slot, n * 64, sl, h, pg[i]);
-          }
-        }
-      }
+    auto wanted = [&](int p) { return p < x.end && (p + boxr > x.lo || p < x.sk); };
+    // its page, 32 boxes at a time with the lanes (looked at when the box is issued)
+    auto entry_of = [&](int i) -> int {
+      const int p = place_of(i);
+      return k0 + (i >> nbox_log2) < k1 && wanted(p) ? __ldg(j.s.table + (int64_t)pl.b * j.s.max_pages + (p >> j.c.page_log2)) : 0;
     };
-    const int count = k1 - k0;
-    for (int k = 0; k < min(count, L::SLOTS); ++k) issue(k);
+    int pages = entry_of(lane), pages_next = entry_of(32 + lane), base = 0;
 
     // ---- the queries, in the order of d that the keys' registers have
     uint32_t qa[KS][4];
@@ -321,6 +424,44 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
         qa[kk][2 + u] = on ? __ldg(src + w1) : 0u;
       }
     }
+    // stage k0 + k into the ring, a lane a copy: of keys and values (lane bit 0), boxes and panels
+    auto issue = [&](int k) {
+      const int slot = issued % L::SLOTS;
+      ++issued;
+      if ((k << nbox_log2) - base >= 32) {   // (32 is a multiple of nbox)
+        base += 32;
+        pages = pages_next;
+        pages_next = entry_of(base + 32 + lane);
+      }
+      const int c = lane >> 1, box = c & (nbox - 1), panel = c >> nbox_log2;
+      const int p = place_of((k << nbox_log2) + box), sl = p & (j.c.page_len - 1);
+      int page = __shfl_sync(0xffffffffu, pages, ((k << nbox_log2) - base + box) & 31);
+      const bool mine = panel < (E4M3 ? 1 : D / 64);
+      if (!wanted(p)) {
+        page = j.c.n_pages;                  // nobody's: zeros
+      } else if ((unsigned)page >= (unsigned)j.c.n_pages) {
+        fail(j.c.status, DEV_INCONSISTENT, SITE_PAGE);
+        page = j.c.n_pages;
+      }
+      uint32_t bytes = 2 * L::TILE;
+      if (E4M3) bytes += __popc(__ballot_sync(0xffffffffu, mine && page < j.c.n_pages)) << box_log2;
+      if (lane == 0) mbar_arrive_expect_tx(bars + slot, bytes);
+      __syncwarp();
+      if (!mine) return;
+      const CUtensorMap* map = lane & 1 ? &tmV : &tmK;
+      uint8_t* dst = ring + slot * L::SLOT + (lane & 1) * L::TILE;
+      if (E4M3) {
+        tma_load_4d(dst + (box << box_log2) * D, map, bars + slot, 0, sl, h, page);
+        if (page < j.c.n_pages)
+          bulk_load(scales + slot * 2 * KT + (lane & 1) * KT + (box << box_log2),
+                    (lane & 1 ? j.c.vs : j.c.ks) + (((int64_t)page * j.c.H + h) << j.c.page_log2) + sl, boxr, bars + slot);
+      } else {
+        tma_load_4d(dst + panel * L::PANEL + (box << box_log2) * 128, map, bars + slot, panel * 64, sl, h, page);
+      }
+    };
+    const int count = k1 - k0;
+    for (int k = 0; k < min(count, L::SLOTS); ++k) issue(k);
+
     const int sk = j.m.window ? j.m.sinks : 0;
     float o[D / 8][4], mrun[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
@@ -346,26 +487,32 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
 #pragma unroll
         for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
       if (E4M3) {
+        uint32_t w[NB][D / 16], big = 0;
+        __nv_bfloat162 f[NB];
 #pragma unroll
         for (int n = 0; n < NB; ++n) {
           const int key = n * 8 + gr;
           const uint32_t b = sc[key];
-          uint32_t w[D / 16];
 #pragma unroll
           for (int i = 0; i < D / 64; ++i) {
             const uint4 y = *reinterpret_cast<const uint4*>(kt + chunk_at<D, E4M3>(key, t * (D / 64) + i));
-            w[4 * i] = y.x; w[4 * i + 1] = y.y; w[4 * i + 2] = y.z; w[4 * i + 3] = y.w;
+            w[n][4 * i] = y.x; w[n][4 * i + 1] = y.y; w[n][4 * i + 2] = y.z; w[n][4 * i + 3] = y.w;
           }
           // 2^120 times the scale in one factor where it is a bf16 number, else by itself on the sums' side
-          const bool two = b > 134u;
-          const __nv_bfloat162 f = bf2((two ? 247u : b + 120u) * 0x00800080u);
+          big |= b > 134u;
+          f[n] = bf2((b > 134u ? 247u : b + 120u) * 0x00800080u);
+        }
 #pragma unroll
-          for (int kk = 0; kk < KS; ++kk) {
+        for (int kk = 0; kk < KS; ++kk)
+#pragma unroll
+          for (int n = 0; n < NB; ++n) {
             uint32_t b0, b1;
-            widen<0x5140, 0x7362>(w[kk], f, b0, b1);
+            widen<0x5140, 0x7362>(w[n][kk], f[n], b0, b1);
             mma(s[n], qa[kk], b0, b1);
           }
-          if (__any_sync(0xffffffffu, two)) {   // columns 2t, 2t + 1 of this block
+        if (__any_sync(0xffffffffu, big != 0)) {
+#pragma unroll
+          for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const uint32_t c = sc[n * 8 + 2 * t + e];
@@ -373,9 +520,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
               s[n][e] *= g;
               s[n][2 + e] *= g;
             }
-          }
         }
       } else {
+        float s2[NB][4];                     // (two sums of half the products each: shorter chains)
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s2[n][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
@@ -383,9 +534,13 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
             uint32_t b[4];
             const int m = lane >> 3, key = n2 * 16 + (m >> 1) * 8 + (lane & 7);
             ldsm(ka + chunk_at<D, E4M3>(key, kk * 2 + (m & 1)), b);
-            mma(s[2 * n2], qa[kk], b[0], b[1]);
-            mma(s[2 * n2 + 1], qa[kk], b[2], b[3]);
+            mma(kk & 1 ? s2[2 * n2] : s[2 * n2], qa[kk], b[0], b[1]);
+            mma(kk & 1 ? s2[2 * n2 + 1] : s[2 * n2 + 1], qa[kk], b[2], b[3]);
           }
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][e] += s2[n][e];
       }
       if (partial) {
 #pragma unroll
@@ -516,12 +671,27 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
       l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
     }
     const bool whole = count == x.stages;
-    if (!whole && k0 == 0) {              // the unit's first part
-      const int64_t last = pl.begin + (int64_t)(unit + 1) * x.stages;
-      cut0 = make_int4(pl.b, h, tile, (int)((last * workers + total - 1) / total) - 1);
-      cut1 = make_int4(rows, x.r0, 0, 0);
+    if (!whole && lane == 0) {
+      Stretch& y = info[warp];
+      auto cta_of = [&](int stage) {        // who has it
+        return (stage < more * (least + 1) ? stage / (least + 1) : more + (stage - more * (least + 1)) / least) / per;
+      };
+      const int begin = pl.begin + unit * x.stages, last = begin + x.stages - 1;
+      if (k0 == 0) {                      // the unit's first part
+        y.tail = 1;
+        y.last = cta_of(last);
+        y.h = h; y.tile = tile; y.rows = rows; y.r0 = x.r0;
+      } else {
+        y.head = 1;
+        y.head_ends = k1 == x.stages;
+        y.head_smem = at + count >= stop;
+        y.first = cta_of(begin);
+        y.hlast = cta_of(last);
+        y.hh = h; y.htile = tile; y.hrows = rows; y.hr0 = x.r0;
+      }
     }
-    float* part = j.parts + (int64_t)(2 * worker + (k0 == 0 ? 1 : 0)) * j.part_rows * (D + 4);
+    // a part goes where the stages were (the last one: the ring is the warp's own and empty), or into the scratch
+    float* part = at + count >= stop ? reinterpret_cast<float*>(ring) : j.parts + (int64_t)worker * j.part_rows * (D + 4);
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const int r = gr + 8 * u;
@@ -559,99 +729,95 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     const uint64_t t0 = globaltimer_ns();   // copies may be in flight: far longer than one takes
     while (globaltimer_ns() - t0 < 50000ull) {
     }
-    cut0.w = -1;
+    if (lane == 0) info[warp].tail = info[warp].head = 0;
   }
-  if (lane == 0) {
-    j.meta[2 * worker] = cut0;
-    j.meta[2 * worker + 1] = cut1;
-  }
-}
 
-// Joins the parts of cut units: O = sum 2^(lse - max) O_part / sum 2^(lse - max).  Block (x, y) looks at
-// the eight workers x, x + gridDim.x, .. and takes the rows y, y + gridDim.y, .. of the units whose first part
-// they hold; its warps share a row's parts.
-constexpr int MERGE_Y = 4;
-
-template <int D>
-__global__ void __launch_bounds__(256) rows_merge(const __grid_constant__ Job j) {
-  pdl_wait();
-  constexpr int N = D / 32;
-  __shared__ float so[8][D], sm[8], sl[8];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  for (int k = 0; k < WARPS; ++k) {
-    const int first = k * gridDim.x + blockIdx.x;
-    const int4 u = j.meta[2 * first];
-    if (u.w < first || u.w >= WARPS * (int)gridDim.x) continue;
-    const int4 v = j.meta[2 * first + 1];
-    const int rows = min(v.x, j.part_rows), n = u.w - first + 1;
-    for (int r = blockIdx.y; r < rows; r += MERGE_Y) {
-      float m = -INFINITY, l = 0.f, o[N];
-#pragma unroll
-      for (int i = 0; i < N; ++i) o[i] = 0.f;
-      constexpr int UN = 4;
-      for (int p0 = warp; p0 < n; p0 += 8 * UN) {
-        float x[UN][N], z[UN];
-#pragma unroll
-        for (int i = 0; i < UN; ++i) {
-          const int p = p0 + 8 * i;
-          z[i] = -INFINITY;
-          if (p < n) {
-            const float* part = j.parts + (int64_t)(p == 0 ? 2 * first + 1 : 2 * (first + p)) * j.part_rows * (D + 4);
-            z[i] = part[j.part_rows * D + r];
-#pragma unroll
-            for (int c = 0; c < N; ++c) x[i][c] = part[r * D + c * 32 + lane];
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < UN; ++i) {
-          if (z[i] == -INFINITY) continue;   // nothing seen
-          if (z[i] > m) {
-            const float a = exp2f(m - z[i]);
-            m = z[i];
-            l *= a;
-#pragma unroll
-            for (int c = 0; c < N; ++c) o[c] *= a;
-          }
-          const float w = exp2f(z[i] - m);   // (a NaN stays one)
-          l += w;
-#pragma unroll
-          for (int c = 0; c < N; ++c) o[c] = fmaf(w, x[i][c], o[c]);
-        }
-      }
-#pragma unroll
-      for (int c = 0; c < N; ++c) so[warp][c * 32 + lane] = o[c];
-      if (lane == 0) {
-        sm[warp] = m;
-        sl[warp] = l;
-      }
-      __syncthreads();
-      if (threadIdx.x < D) {
-        float mx = -INFINITY, den = 0.f, y = 0.f;
-#pragma unroll
-        for (int w = 0; w < 8; ++w) mx = fmaxf(mx, sm[w]);
-#pragma unroll
-        for (int w = 0; w < 8; ++w) {
-          if (sl[w] == 0.f) continue;
-          const float a = exp2f(sm[w] - mx);
-          den = fmaf(a, sl[w], den);
-          y = fmaf(a, so[w][threadIdx.x], y);
-        }
-        const int i = u.z * ROWS + r, tok = i / j.G, hq = i - tok * j.G;
-        static_cast<__nv_bfloat16*>(j.o.p)[(int64_t)(u.y * j.G + hq) * j.o.head + (int64_t)(v.y + tok) * j.o.row + threadIdx.x] =
-            __float2bfloat16_rn(den == 0.f ? 0.f : y / den);
-      }
-      __syncthreads();
+  // ---- the CTA's parts joined: one chain for each tail, and one for a unit from before the CTA.  A chain's
+  // parts are a tail (or the first warp's head) and the heads of the warps behind it up to the unit's end.
+  __syncthreads();
+  auto worker_part = [&](int w, bool tail) -> const float* {
+    return tail || info[w].head_smem ? reinterpret_cast<const float*>(smem + w * L::RING)
+                                     : j.parts + (int64_t)((int)blockIdx.x * per + w) * j.part_rows * (D + 4);
+  };
+  int open = -1;                          // the chain of a unit that goes on behind the CTA
+  int todo = 0;                           // (chain, row) pairs so far: warps take them in turn
+#pragma unroll 1
+  for (int c = -1; c < per; ++c) {        // -1: the first warp's head
+    if (c < 0 ? !info[0].head : !info[c].tail) continue;
+    const Stretch& y = info[max(c, 0)];
+    const int h = c < 0 ? y.hh : y.h, tile = c < 0 ? y.htile : y.tile;
+    const int rows = min(c < 0 ? y.hrows : y.rows, j.part_rows), r0 = c < 0 ? y.hr0 : y.r0;
+    int n = 1;                            // parts
+    bool ends = c < 0 && y.head_ends;
+    while (!ends && max(c, 0) + n < per && info[max(c, 0) + n].head) {
+      ends = info[max(c, 0) + n].head_ends;
+      ++n;
     }
+    if (c >= 0 && !ends) open = c;        // (one at most: the last chain)
+    // rows in turn with the other chains' (a warp's first: (warp - todo) mod 8)
+#pragma unroll 1
+    for (int r = (warp - todo) & (WARPS - 1); r < rows; r += WARPS) {
+      float m, l, o[D / 32];
+      // (every part's address by itself: some are in shared memory)
+      const int log = j.part_rows * D + r;
+      const float z = lane < n ? worker_part(max(c, 0) + lane, lane == 0 && c >= 0)[log] : -INFINITY;
+      m = z;
+#pragma unroll
+      for (int w = 16; w; w >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+      const float weight = z == -INFINITY ? 0.f : exp2f(z - m);   // (nothing seen: 0; a NaN stays one)
+      l = 0.f;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) o[i] = 0.f;
+#pragma unroll 1
+      for (int p = 0; p < n; ++p) {
+        const float w = __shfl_sync(0xffffffffu, weight, p);
+        const float* x = worker_part(max(c, 0) + p, p == 0 && c >= 0) + r * D + lane;
+        l += w;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i)
+          if (w != 0.f) o[i] = fmaf(w, x[i * 32], o[i]);
+      }
+      if (c >= 0 && ends) {
+        store_row<D>(j, h, tile, r0, r, l, o);
+      } else {
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        float* part = j.parts + (int64_t)(WORKERS + 2 * (int)blockIdx.x + (c < 0 ? 0 : 1)) * j.part_rows * (D + 4);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) part[r * D + i * 32 + lane] = o[i] * inv;
+        if (lane == 0) part[log] = l == 0.f ? -INFINITY : m + log2f(l);
+      }
+    }
+    todo += rows;
+  }
+
+  // ---- units that other CTAs hold parts of: the last of them to come joins the parts
+  const bool from_before = info[0].head != 0;
+  if (!from_before && open < 0) return;   // uniform
+  __syncthreads();
+  int* last = reinterpret_cast<int*>(info + WARPS);   // [2]
+  if (lane == 0 && warp < 2) {            // (both trips at once)
+    __threadfence();
+    const Stretch& y = info[max(open, 0)];
+    last[warp] = (warp == 0 ? from_before : open >= 0) &&
+                 arrive(j.arrived + (warp == 0 ? info[0].first : (int)blockIdx.x), j.call,
+                        warp == 0 ? info[0].hlast - info[0].first + 1 : y.last - (int)blockIdx.x + 1);
+    __threadfence();
+  }
+  __syncthreads();
+  float* room = reinterpret_cast<float*>(smem);
+  if (last[0])
+    join<D>(j, info[0].hh, info[0].htile, min(info[0].hrows, j.part_rows), info[0].hr0, info[0].first,
+            info[0].hlast - info[0].first + 1, room);
+  if (last[1]) {
+    const Stretch& y = info[max(open, 0)];
+    join<D>(j, y.h, y.tile, min(y.rows, j.part_rows), y.r0, blockIdx.x, y.last - (int)blockIdx.x + 1, room);
   }
 }
 
 template <int D, bool E4M3>
 cudaError_t launch_d(const Maps& maps, const Job& job, int ctas, cudaStream_t st) {
-  cudaError_t e = launch_kernel(cache_attend_rows<D, E4M3>, dim3(ctas), WARPS * 32, Lay<D, E4M3>::BYTES, 1, false, st,
-                                maps.rk, maps.rv, job);
-  if (e == cudaSuccess)
-    e = launch_kernel(rows_merge<D>, dim3(ctas, std::min(MERGE_Y, job.part_rows)), 256, 0, 1, true, st, job);
-  return e;
+  return launch_kernel(cache_attend_rows<D, E4M3>, dim3(ctas), WARPS * 32, Lay<D, E4M3>::BYTES, 1, false, st, maps.rk,
+                       maps.rv, job);
 }
 
 template <int D, bool E4M3>
@@ -688,15 +854,19 @@ bool make_rows_maps(const Pool& c, Maps* m) {
 }
 
 size_t attend_rows_scratch(const Pool& c, int G, int max_rows) {
-  return sizeof(int4) * 2 * WORKERS + sizeof(float) * 2 * (size_t)WORKERS * part_rows(G, max_rows) * (c.d + 4);
+  return sizeof(unsigned long long) * MAX_CTAS + sizeof(float) * (size_t)(WORKERS + 2 * MAX_CTAS) * part_rows(G, max_rows) * (c.d + 4);
 }
 
 cudaError_t launch_attend_rows(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
                                int max_rows, const Mask& m, void* scratch, cudaStream_t st) {
   const int n_sm = std::min(sm_count(), MAX_CTAS), G = Hq / c.H;
   if (n_sm <= 0) return cudaErrorInvalidDevice;
-  const Job job{c, s, m, q, o, G, max_rows, part_rows(G, max_rows), static_cast<int4*>(scratch),
-                reinterpret_cast<float*>(static_cast<int4*>(scratch) + 2 * WORKERS)};
+  // numbers the calls, so that a count that another call left in the same memory is not taken for this one's (a captured
+  // call keeps its number: its replays, one after the other, each find the count cleared by the one before)
+  static std::atomic<unsigned long long> calls{0};
+  unsigned long long* const arrived = static_cast<unsigned long long*>(scratch);
+  const Job job{c, s, m, q, o, G, max_rows, part_rows(G, max_rows), reinterpret_cast<float*>(arrived + MAX_CTAS), arrived,
+                (calls.fetch_add(1) + 1) & 0xffffffffffffull};
   if (c.d == 128)
     return c.e4m3 ? launch_d<128, true>(maps, job, n_sm, st) : launch_d<128, false>(maps, job, n_sm, st);
   return c.e4m3 ? launch_d<64, true>(maps, job, n_sm, st) : launch_d<64, false>(maps, job, n_sm, st);

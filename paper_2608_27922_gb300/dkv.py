@@ -510,6 +510,12 @@ DKV_CACHE_BF16, DKV_CACHE_E4M3 = 0, 1
 _CACHE_FORMAT = {"bf16": DKV_CACHE_BF16, "e4m3": DKV_CACHE_E4M3}
 
 
+def _raw_stream(device: int) -> int:
+    """cuda_stream of the device's current stream (torch's own query, without a Stream object around it)."""
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(device) if get is not None else torch.cuda.current_stream(device).cuda_stream
+
+
 class CacheSeqs:
     """The sequences of a cache call (device int32 tensors, see include/dkv.h): block_table
     [n_seq][max_pages], seq_len [n_seq], row_start [n_seq + 1].  The tensors are kept and read when
@@ -568,8 +574,8 @@ class PagedCache:
             _check(lib().dkv_cache_create(ctypes.byref(h), H, d, page_len, n_pages, _CACHE_FORMAT[fmt],
                                           ctypes.byref(bufs)), "dkv_cache_create")
         self.handle = h.value
-        self._scratch_size: Dict[Tuple[int, int, int, int], int] = {}
-        self._how: Dict[tuple, dkv_cache_attend_t] = {}
+        self._plans: Dict[tuple, tuple] = {}
+        self._attend = lib().dkv_cache_attend
 
     def close(self):
         if getattr(self, "handle", None):
@@ -591,14 +597,14 @@ class PagedCache:
         return s
 
     def _on(self, stream):
-        """The stream of a call, and a context in which torch allocates for it."""
+        """The stream of a call, and a context in which torch allocates for it (None: the current one)."""
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream, None
+            return _raw_stream(self.device.index), None
         if not isinstance(stream, torch.cuda.Stream):
             stream = torch.cuda.ExternalStream(int(stream), device=self.device)
         return stream.cuda_stream, torch.cuda.stream(stream)
 
-    def _new(self, ctx, *shape, dtype=torch.bfloat16):
+    def _new(self, ctx, shape, dtype):
         if ctx is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
         with ctx:
@@ -625,7 +631,10 @@ class PagedCache:
                 or first.device != self.device):
             raise ValueError(f"first: expected contiguous {torch.int32} {(seqs.n_seq,)} on {self.device}")
         s, ctx = self._on(stream)
-        K, V = out if out is not None else (self._new(ctx, self.H, rows, self.d), self._new(ctx, self.H, rows, self.d))
+        if out is not None:
+            K, V = out
+        else:
+            K, V = (self._new(ctx, (self.H, rows, self.d), torch.bfloat16) for _ in range(2))
         k, v = self._packed(K, self.H, rows, "K"), self._packed(V, self.H, rows, "V")
         _check(lib().dkv_cache_read(self.handle, self._seqs(seqs), first.data_ptr(), K.data_ptr(), V.data_ptr(), rows,
                                     k[0], k[1], v[0], v[1], s), "dkv_cache_read")
@@ -638,31 +647,35 @@ class PagedCache:
         mask of dkv_cache_attend_t).  max_rows: the most tokens of any one sequence, 1 when every
         sequence brings one (default: all rows)."""
         Hq, rows = Q.shape[0], Q.shape[1]
+        key = (seqs.n_seq, Hq, rows, scale, window, sinks, block, max_rows)
+        plan = self._plans.get(key)
+        if plan is None:
+            plan = self._plan(key)
+        size, most, how, _ = plan
         q = self._packed(Q, Hq, rows, "Q")
-        most = rows if max_rows is None else min(int(max_rows), rows)
-        key = (seqs.n_seq, Hq, rows, most)
-        size = self._scratch_size.get(key)
-        if size is None:
-            if len(self._scratch_size) > 4096:
-                self._scratch_size.clear()
-            size = self._scratch_size[key] = int(lib().dkv_cache_attend_scratch_size(self.handle, *key))
-        how = (scale, window, sinks, block, most)
-        h = self._how.get(how)
-        if h is None:
-            if scale is not None and not scale > 0.0:
-                raise ValueError("scale: expected a positive number")
-            if len(self._how) > 4096:
-                self._how.clear()
-            h = self._how[how] = dkv_cache_attend_t(0.0 if scale is None else scale, window, sinks, block, most)
         s, ctx = self._on(stream)
         if out is None:
-            out = self._new(ctx, Hq, rows, self.d)
+            out = self._new(ctx, (Hq, rows, self.d), torch.bfloat16)
         o = self._packed(out, Hq, rows, "out")
-        scratch = self._new(ctx, size, dtype=torch.uint8)
-        _check(lib().dkv_cache_attend(self.handle, self._seqs(seqs), Q.data_ptr(), Hq, rows, q[0], q[1],
-                                      out.data_ptr(), o[0], o[1], ctypes.byref(h), scratch.data_ptr(), size, s),
-               "dkv_cache_attend")
+        scratch = self._new(ctx, size, torch.uint8)
+        st = self._attend(self.handle, self._seqs(seqs), Q.data_ptr(), Hq, rows, q[0], q[1], out.data_ptr(), o[0], o[1],
+                          how, scratch.data_ptr(), size, s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_attend")
         return out
+
+    def _plan(self, key):
+        """Scratch bytes and the C structure of an attend call's sizes and options, kept for the next one."""
+        n_seq, Hq, rows, scale, window, sinks, block, max_rows = key
+        if scale is not None and not scale > 0.0:
+            raise ValueError("scale: expected a positive number")
+        most = rows if max_rows is None else min(int(max_rows), rows)
+        size = int(lib().dkv_cache_attend_scratch_size(self.handle, n_seq, Hq, rows, most))
+        how = dkv_cache_attend_t(0.0 if scale is None else scale, window, sinks, block, most)
+        if len(self._plans) > 4096:
+            self._plans.clear()
+        plan = self._plans[key] = (size, most, ctypes.byref(how), how)
+        return plan
 
     def sync(self) -> None:
         _check(lib().dkv_cache_sync(self.handle), "dkv_cache_sync")
