@@ -3,8 +3,8 @@
 // HBM bounds it (4 d bytes a position and key head in bf16, 2 d + 2 in e4m3); the arithmetic only
 // has to keep out of the way.
 //
-// A unit is 16 query rows of one sequence and one key head, row = token * G + head.  The visible
-// positions of all units, in stages of KT, form one range, and each of the GPU's 8 x 152 warps
+// A unit is 8 or 16 query rows of one sequence and one key head, row = token * G + head.  The visible
+// positions of all units, in stages of KT, form one range, and each of the GPU's warps
 // takes an equal stretch of it, whatever units it belongs to: no warp waits for another, and the
 // split over a long cache, over many sequences and over ragged lengths is the same one.  A unit inside one
 // stretch is finished there; one that a boundary cuts leaves a partial result for each warp that
@@ -13,18 +13,24 @@
 // and 3 of the host's, as long as the rest of a small call).
 //
 // A warp streams its stages through a ring of its own (TMA boxes of one page, 128-byte swizzled;
-// one lane issues, a barrier a slot), scores them with mma.sync m16n8k16 (16 rows fill one such
-// product; the tensor cores' tile of 128 rows would be an eighth full at best and add its latencies), and
-// keeps the running maximum, sum and 16 x d outputs in registers.  Scores' accumulators are the
-// weights' operand layout, so weights never leave the registers.
+// a lane issues each, a barrier a slot) and works on them with mma.sync m16n8k16, turned round: the 16 rows
+// of a product are keys or columns of the values and its 8 columns the query rows,
+//   S^T = K Q^T,   O^T += V^T P^T,
+// so that 8 query rows (a single token's group of heads) fill a product; with the query rows as its 16 rows
+// every product, weight and register was at least half empty (and the tensor cores' tiles of 128 rows
+// would be empty but for a sixteenth).  The weights' registers become an operand by one
+// transposing move for 8 keys.  Running maximum, sum and outputs stay in registers.
 //
-// e4m3: the codes become bf16 in the registers.  A key row's 128 codes lie with four lanes, 32
-// neighbouring ones each, and the queries' registers are loaded in that order of d instead of the product's own; of the
-// values, a transposed load gives pairs of d of one position, which widen into the even and the odd
-// columns of 16.
+// e4m3: the codes become fp16 in the registers, one conversion for two.  A key row's 128 codes lie
+// with four lanes, 32 neighbouring ones each, and the queries' registers are loaded in that order of d
+// instead of the product's own; of the values, a transposed load gives pairs of d of one position, which
+// widen into the even and the odd ones of 16.  (As bf16, by bit operations, the codes took half of
+// all instructions.)
 #include "attn_math.cuh"
 #include "cache_internal.h"
 #include "tc_ptx.cuh"
+
+#include <cuda_fp16.h>
 
 #include <algorithm>
 #include <atomic>
@@ -40,10 +46,9 @@ namespace {
 
 using namespace tc;
 
-constexpr int WARPS = 8;
 constexpr int MAX_CTAS = 152;
-constexpr int WORKERS = WARPS * MAX_CTAS;
-constexpr int ROWS = 16;
+constexpr int MAX_WARPS = 12;
+constexpr int WORKERS = MAX_WARPS * MAX_CTAS;
 constexpr float RESCALE_LOG2 = 8.0f;
 constexpr int MIN_STAGES = 1;    // stages of a warp, at least
 
@@ -59,13 +64,14 @@ struct Stretch {
   int hh, htile, hrows, hr0;  // of the head's
 };
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, int NR>
 struct Lay {
   static constexpr int ES = E4M3 ? 1 : 2;
   static constexpr int KT = !E4M3 && D == 128 ? 16 : 32;   // positions of a stage
   static constexpr int PANEL = KT * (E4M3 ? D : 128);      // bytes of a panel (64 columns; codes: all)
   static constexpr int TILE = KT * D * ES;                 // bytes of a stage's keys
-  static constexpr int SLOTS = 3;
+  static constexpr int WARPS = NR == 1 ? 12 : 8;           // (as many as the registers allow)
+  static constexpr int SLOTS = NR == 1 ? 2 : 3;
   static constexpr int SLOT = 2 * TILE;                    // keys, values
   static constexpr int RING = SLOTS * SLOT;                // a warp's
   static constexpr int SCALES = WARPS * RING;              // [warps][slots][2][KT] scale bytes
@@ -73,7 +79,7 @@ struct Lay {
   static constexpr int INFO = BARS + WARPS * SLOTS * 8;
   static constexpr int BYTES = INFO + WARPS * (int)sizeof(Stretch) + 16;
   static_assert(BYTES <= 227 * 1024, "shared memory per CTA");
-  static_assert(ROWS * (D + 4) * 4 <= RING, "a part in the ring");
+  static_assert(16 * (D + 4) * 4 <= RING, "a part in the ring");
 };
 
 struct Job {
@@ -82,6 +88,7 @@ struct Job {
   Mask m;
   Packed q, o;
   int G, max_rows;
+  int unit;          // rows of a unit
   int part_rows;     // rows of a partial result
   float* parts;      // partial results, [part_rows][D + 4] each (outputs, then the logarithm of a row's sum): one of every
                      //   worker (a unit that its stretch begins in the middle of and goes on behind; its last unit's
@@ -108,7 +115,7 @@ __device__ __forceinline__ Span span_of(const Job& j, int b) {
   x.n = q.n;
   x.len = q.len;
   if (q.n == 0) return x;
-  x.tiles = (q.n * j.G + ROWS - 1) / ROWS;
+  x.tiles = (q.n * j.G + j.unit - 1) / j.unit;
   x.stages = 1;
   const int p0 = q.len - q.n, pl = q.len - 1;
   if (pl < 0) return x;
@@ -201,23 +208,43 @@ __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint3
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ __nv_bfloat162 bf2(uint32_t bits) { return *reinterpret_cast<const __nv_bfloat162*>(&bits); }
-__device__ __forceinline__ uint32_t times(uint32_t x, __nv_bfloat162 f) {
-  const __nv_bfloat162 y = __hmul2(bf2(x), f);
-  return *reinterpret_cast<const uint32_t*>(&y);
+// An 8 x 8 matrix of 16-bit elements, a row's pairs with four lanes, to its transpose.
+__device__ __forceinline__ uint32_t transpose(uint32_t x) {
+  uint32_t y;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
-// Four codes as bf16 fields (their values times 2^-120) in two pairs, taken by the byte selectors.
-template <uint32_t S0, uint32_t S1>
-__device__ __forceinline__ void widen(uint32_t w, __nv_bfloat162 f, uint32_t& a, uint32_t& b) {
-  const uint32_t hi = (w & 0x80808080u) | ((w >> 4) & 0x07070707u), lo = (w << 4) & 0xf0f0f0f0u;
-  a = times(__byte_perm(lo, hi, S0), f);
-  b = times(__byte_perm(lo, hi, S1), f);
+__device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// Two fp16 from the two codes in the low or the high half of x.
+__device__ __forceinline__ uint32_t widen_lo(uint32_t x) {
+  uint32_t y;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t widen_hi(uint32_t x) {
+  uint32_t y;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ uint32_t pack_f16(float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+// The two bf16 of x times f, as fp16.
+__device__ __forceinline__ uint32_t to_f16(uint32_t x, float f) {
+  const float2 v = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x));
+  return pack_f16(v.x * f, v.y * f);
 }
 
 // Byte offset of 16-byte chunk c of row r in a tile.
 template <int D, bool E4M3>
 __device__ __forceinline__ int chunk_at(int r, int c) {
-  if (!E4M3) return (c >> 3) * Lay<D, E4M3>::PANEL + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+  if (!E4M3) return (c >> 3) * Lay<D, E4M3, 1>::PANEL + r * 128 + (((c & 7) ^ (r & 7)) << 4);
   return D == 128 ? r * 128 + ((c ^ (r & 7)) << 4) : r * 64 + ((c ^ ((r >> 1) & 3)) << 4);
 }
 
@@ -290,7 +317,7 @@ __device__ __forceinline__ void sum_parts(At at, int first, int n, int step, int
 template <int D>
 __device__ __forceinline__ void store_row(const Job& j, int h, int tile, int r0, int r, float l, const float (&o)[D / 32]) {
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int lane = threadIdx.x & 31, i = tile * ROWS + r, tok = i / j.G, hq = i - tok * j.G;
+  const int lane = threadIdx.x & 31, i = tile * j.unit + r, tok = i / j.G, hq = i - tok * j.G;
   __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + hq) * j.o.head + (int64_t)(r0 + tok) * j.o.row;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) dst[c * 32 + lane] = __float2bfloat16_rn(o[c] * inv);
@@ -298,7 +325,7 @@ __device__ __forceinline__ void store_row(const Job& j, int h, int tile, int r0,
 
 // Joins the n CTAs' parts of a unit, the first one's from CTA `first`, in the CTAs' order: a row a warp, or, where the
 // parts are many for one warp, all warps at a row.  All threads of the CTA; room: shared memory.
-template <int D>
+template <int D, int WARPS>
 __device__ void join(const Job& j, int h, int tile, int rows, int r0, int first, int n, float* room) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool shared = n > 32;
@@ -339,12 +366,12 @@ __device__ void join(const Job& j, int h, int tile, int rows, int r0, int first,
   __syncthreads();
 }
 
-template <int D, bool E4M3>
-__global__ void __launch_bounds__(WARPS * 32, 1)
+template <int D, bool E4M3, int NR>
+__global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
     cache_attend_rows(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                       const __grid_constant__ Job j) {
-  using L = Lay<D, E4M3>;
-  constexpr int KT = L::KT, KS = D / 16, NB = KT / 8;
+  using L = Lay<D, E4M3, NR>;
+  constexpr int WARPS = L::WARPS, KT = L::KT, KS = D / 16, NB = KT / 8, UNIT = 8 * NR;
   extern __shared__ __align__(1024) uint8_t smem[];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gr = lane >> 2, t = lane & 3;
   if ((smem_u32(smem) & 1023u) != 0u) {
@@ -388,7 +415,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     const int unit = (int)((unsigned)(at - pl.begin) / (unsigned)x.stages), k0 = at - pl.begin - unit * x.stages;
     const int h = (int)((unsigned)unit / (unsigned)x.tiles), tile = unit - h * x.tiles;
     const int k1 = min(x.stages, k0 + (stop - at));
-    const int rows = min(ROWS, x.n * j.G - tile * ROWS);
+    const int rows = min(UNIT, x.n * j.G - tile * UNIT);
     const int boxr = min(KT, j.c.page_len), box_log2 = min(KT == 16 ? 4 : 5, j.c.page_log2);
     const int nbox_log2 = (KT == 16 ? 4 : 5) - box_log2, nbox = 1 << nbox_log2;   // boxes of a stage: 1 or 2
 
@@ -405,25 +432,31 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     };
     int pages = entry_of(lane), pages_next = entry_of(32 + lane), base = 0;
 
-    // ---- the queries, in the order of d that the keys' registers have
-    uint32_t qa[KS][4];
-    int end[2], lo[2];
+    // ---- the queries: operand columns gr + 8 u, in the order of d that the keys' registers have
+    uint32_t qb[NR][KS][2];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = gr + 8 * u, i = tile * ROWS + r, tok = i / j.G, hq = i - tok * j.G;
+    for (int u = 0; u < NR; ++u) {
+      const int r = gr + 8 * u, i = tile * UNIT + r, tok = i / j.G, hq = i - tok * j.G;
       const bool on = r < rows;
-      const int p = x.len - x.n + tok;
-      end[u] = on && p >= 0 ? visible_end(j.m, p, x.len) : 0;
-      lo[u] = window_first(j.m, end[u]);
       const uint32_t* src = reinterpret_cast<const uint32_t*>(
           static_cast<const __nv_bfloat16*>(j.q.p) + (int64_t)(h * j.G + hq) * j.q.head + (int64_t)(x.r0 + tok) * j.q.row);
 #pragma unroll
       for (int kk = 0; kk < KS; ++kk) {
         const int w0 = E4M3 ? t * (D / 8) + 2 * kk : kk * 8 + t, w1 = E4M3 ? w0 + 1 : w0 + 4;
-        qa[kk][u] = on ? __ldg(src + w0) : 0u;
-        qa[kk][2 + u] = on ? __ldg(src + w1) : 0u;
+        qb[u][kk][0] = on ? __ldg(src + w0) : 0u;
+        qb[u][kk][1] = on ? __ldg(src + w1) : 0u;
       }
     }
+    // the rows whose scores and outputs this thread holds: 2 t, 2 t + 1 (and 8 more), what they see
+    int end[NR][2], lo[NR][2];
+#pragma unroll
+    for (int u = 0; u < NR; ++u)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * u + 2 * t + e, p = x.len - x.n + (tile * UNIT + r) / j.G;
+        end[u][e] = r < rows && p >= 0 ? visible_end(j.m, p, x.len) : 0;
+        lo[u][e] = window_first(j.m, end[u][e]);
+      }
     // stage k0 + k into the ring, a lane a copy: of keys and values (lane bit 0), boxes and panels
     auto issue = [&](int k) {
       const int slot = issued % L::SLOTS;
@@ -463,11 +496,44 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     for (int k = 0; k < min(count, L::SLOTS); ++k) issue(k);
 
     const int sk = j.m.window ? j.m.sinks : 0;
-    float o[D / 8][4], mrun[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    // e4m3: the products are fp16, which holds every code exactly; a row of queries too, times the power of
+    // two that puts its largest magnitude at 2^7 .. 2^8 (what lies 2^-31 below that is rounded, to within 2^-33 of it)
+    float rs[NR][2];                        // of a row's products, in the exponent of 2
 #pragma unroll
-    for (int n = 0; n < D / 8; ++n)
+    for (int u = 0; u < NR; ++u) {
+      rs[u][0] = rs[u][1] = j.m.sl2;
+      if constexpr (E4M3) {
+        uint32_t big = 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
+        for (int kk = 0; kk < KS; ++kk) big = __vmaxu2(__vmaxu2(big, qb[u][kk][0] & 0x7fff7fffu), qb[u][kk][1] & 0x7fff7fffu);
+        big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, 1));
+        big = __vmaxu2(big, __shfl_xor_sync(0xffffffffu, big, 2));
+        const int e = max((int)(max(big & 0xffffu, big >> 16) >> 7), 16) - 134;   // (-118 .. 121)
+        const float f = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+        for (int kk = 0; kk < KS; ++kk) {
+          qb[u][kk][0] = to_f16(qb[u][kk][0], f);
+          qb[u][kk][1] = to_f16(qb[u][kk][1], f);
+        }
+        const float back = __uint_as_float((uint32_t)(127 + e) << 23);   // row gr's; rows 2 t, 2 t + 1 lie with lanes 8 t, 8 t + 4
+        rs[u][0] *= __shfl_sync(0xffffffffu, back, 8 * t);
+        rs[u][1] *= __shfl_sync(0xffffffffu, back, 8 * t + 4);
+      }
+    }
+    // o[c][u]: columns of the values 16 c + gr, + 8 (e4m3: 16 c + 2 gr, + 1) of rows 8 u + 2 t, + 1
+    float o[D / 16][NR][4], mrun[NR][2], msum[NR][2], l[NR][2];
+#pragma unroll
+    for (int u = 0; u < NR; ++u) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        mrun[u][e] = msum[u][e] = -INFINITY;
+        l[u][e] = 0.f;
+      }
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[c][u][e] = 0.f;
+    }
 
     for (int k = 0; k < count; ++k) {
       const int slot = used % L::SLOTS;
@@ -480,123 +546,170 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
       const uint32_t ka = smem_u32(kt), va = smem_u32(vt);
       const uint8_t* sc = scales + slot * 2 * KT;
 
-      // ---- scores
-      float s[NB][4];
+      // ---- scores: s[g][u][e]: position 16 g + gr (e < 2) or 8 more, row 8 u + 2 t + (e & 1)
+      float s[KT / 16][NR][4];
 #pragma unroll
-      for (int n = 0; n < NB; ++n)
+      for (int g = 0; g < KT / 16; ++g)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) s[n][e] = 0.f;
-      if (E4M3) {
-        uint32_t w[NB][D / 16], big = 0;
-        __nv_bfloat162 f[NB];
+        for (int u = 0; u < NR; ++u)
 #pragma unroll
-        for (int n = 0; n < NB; ++n) {
-          const int key = n * 8 + gr;
-          const uint32_t b = sc[key];
+          for (int e = 0; e < 4; ++e) s[g][u][e] = 0.f;
+      if constexpr (E4M3) {
+        uint32_t w[NB][D / 16];
+#pragma unroll
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
           for (int i = 0; i < D / 64; ++i) {
-            const uint4 y = *reinterpret_cast<const uint4*>(kt + chunk_at<D, E4M3>(key, t * (D / 64) + i));
+            const uint4 y = *reinterpret_cast<const uint4*>(kt + chunk_at<D, E4M3>(n * 8 + gr, t * (D / 64) + i));
             w[n][4 * i] = y.x; w[n][4 * i + 1] = y.y; w[n][4 * i + 2] = y.z; w[n][4 * i + 3] = y.w;
           }
-          // 2^120 times the scale in one factor where it is a bf16 number, else by itself on the sums' side
-          big |= b > 134u;
-          f[n] = bf2((b > 134u ? 247u : b + 120u) * 0x00800080u);
-        }
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
-          for (int n = 0; n < NB; ++n) {
-            uint32_t b0, b1;
-            widen<0x5140, 0x7362>(w[n][kk], f[n], b0, b1);
-            mma(s[n], qa[kk], b0, b1);
+          for (int g = 0; g < KT / 16; ++g) {
+            const uint32_t a[4] = {widen_lo(w[2 * g][kk]), widen_lo(w[2 * g + 1][kk]), widen_hi(w[2 * g][kk]), widen_hi(w[2 * g + 1][kk])};
+#pragma unroll
+            for (int u = 0; u < NR; ++u) mma_f16(s[g][u], a, qb[u][kk][0], qb[u][kk][1]);
           }
-        if (__any_sync(0xffffffffu, big != 0)) {
-#pragma unroll
-          for (int n = 0; n < NB; ++n)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const uint32_t c = sc[n * 8 + 2 * t + e];
-              const float g = c > 134u ? scale_of(c) : 1.0f;
-              s[n][e] *= g;
-              s[n][2 + e] *= g;
-            }
-        }
       } else {
-        float s2[NB][4];                     // (two sums of half the products each: shorter chains)
+        float s2[KT / 16][NR][4];            // (two sums of half the products each: shorter chains)
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int g = 0; g < KT / 16; ++g)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s2[n][e] = 0.f;
+          for (int u = 0; u < NR; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s2[g][u][e] = 0.f;
 #pragma unroll
         for (int kk = 0; kk < KS; ++kk)
 #pragma unroll
-          for (int n2 = 0; n2 < NB / 2; ++n2) {
-            uint32_t b[4];
-            const int m = lane >> 3, key = n2 * 16 + (m >> 1) * 8 + (lane & 7);
-            ldsm(ka + chunk_at<D, E4M3>(key, kk * 2 + (m & 1)), b);
-            mma(kk & 1 ? s2[2 * n2] : s[2 * n2], qa[kk], b[0], b[1]);
-            mma(kk & 1 ? s2[2 * n2 + 1] : s[2 * n2 + 1], qa[kk], b[2], b[3]);
+          for (int g = 0; g < KT / 16; ++g) {
+            uint32_t a[4];
+            const int m = lane >> 3, key = g * 16 + (m & 1) * 8 + (lane & 7);
+            ldsm(ka + chunk_at<D, E4M3>(key, kk * 2 + (m >> 1)), a);
+#pragma unroll
+            for (int u = 0; u < NR; ++u) mma(kk & 1 ? s2[g][u] : s[g][u], a, qb[u][kk][0], qb[u][kk][1]);
           }
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int g = 0; g < KT / 16; ++g)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s[n][e] += s2[n][e];
+          for (int u = 0; u < NR; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[g][u][e] += s2[g][u][e];
       }
+      // into exponents of 2, with the keys' scales
+#pragma unroll
+      for (int g = 0; g < KT / 16; ++g)
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const float ck = E4M3 ? scale_of(sc[g * 16 + v * 8 + gr]) : 1.0f;
+#pragma unroll
+          for (int u = 0; u < NR; ++u)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) s[g][u][2 * v + e] *= E4M3 ? ck * rs[u][e] : j.m.sl2;
+        }
       if (partial) {
 #pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int g = 0; g < KT / 16; ++g)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (!sees(p0 + n * 8 + 2 * t + (e & 1), end[e >> 1], lo[e >> 1], sk)) s[n][e] = -INFINITY;
+          for (int u = 0; u < NR; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (!sees(p0 + g * 16 + (e >> 1) * 8 + gr, end[u][e & 1], lo[u][e & 1], sk)) s[g][u][e] = -INFINITY;
       }
-      // ---- running maximum of rows gr and gr + 8 (four lanes each)
-      float nm[2];
-      bool raised = false;
-      float alpha[2];
+      // e4m3: the values' scales join the exponents, so that a weight carries its value's scale and the running
+      // maximum is that of the products: no weight leaves fp16's range, however the scales differ.  The sums
+      // of the weights themselves have a maximum of their own (each thread's).
+      if constexpr (E4M3) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int n = 0; n < NB; ++n) mx = fmaxf(mx, fmaxf(s[n][2 * u], s[n][2 * u + 1]));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        mx *= j.m.sl2;
-        const bool raise = mx > mrun[u] + RESCALE_LOG2 || (mrun[u] == -INFINITY && mx > -INFINITY);
-        alpha[u] = raise ? (mrun[u] == -INFINITY ? 0.f : ex2(mrun[u] - mx)) : 1.f;
-        if (raise) {
-          raised |= mrun[u] != -INFINITY;   // (nothing to scale before the first visible key)
-          l[u] *= alpha[u];
-          mrun[u] = mx;
-        }
-        nm[u] = mrun[u] == -INFINITY ? 0.f : -mrun[u];
-      }
-      if (__any_sync(0xffffffffu, raised)) {
-#pragma unroll
-        for (int n = 0; n < D / 8; ++n) {
-          o[n][0] *= alpha[0]; o[n][1] *= alpha[0];
-          o[n][2] *= alpha[1]; o[n][3] *= alpha[1];
-        }
-      }
-      // ---- weights
-#pragma unroll
-      for (int n = 0; n < NB; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          s[n][e] = ex2(fmaf(s[n][e], j.m.sl2, nm[e >> 1]));
-          l[e >> 1] += s[n][e];
-        }
-      if (E4M3) {   // the values' scales (a hidden row's may be NaN)
-#pragma unroll
-        for (int n = 0; n < NB; ++n)
+        for (int u = 0; u < NR; ++u)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float g = scale_of(sc[KT + n * 8 + 2 * t + e]);
-            s[n][e] = s[n][e] == 0.f ? 0.f : s[n][e] * g;
-            s[n][2 + e] = s[n][2 + e] == 0.f ? 0.f : s[n][2 + e] * g;
+            float mx = -INFINITY;
+#pragma unroll
+            for (int g = 0; g < KT / 16; ++g) mx = max3(mx, s[g][u][e], s[g][u][2 + e]);
+            if (mx > msum[u][e] + RESCALE_LOG2 || (msum[u][e] == -INFINITY && mx > -INFINITY)) {
+              l[u][e] *= msum[u][e] == -INFINITY ? 0.f : ex2(msum[u][e] - mx);
+              msum[u][e] = mx;
+            }
+            const float nm = msum[u][e] == -INFINITY ? 0.f : -msum[u][e];
+#pragma unroll
+            for (int g = 0; g < KT / 16; ++g) l[u][e] += ex2(s[g][u][e] + nm) + ex2(s[g][u][2 + e] + nm);
+          }
+#pragma unroll
+        for (int g = 0; g < KT / 16; ++g)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const uint32_t b = sc[KT + g * 16 + v * 8 + gr];
+            const float ev = b == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(0x4b000000u | b) - 8388735.0f;
+#pragma unroll
+            for (int u = 0; u < NR; ++u)
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (!partial || s[g][u][2 * v + e] != -INFINITY) s[g][u][2 * v + e] += ev;   // (a hidden row's may be NaN)
           }
       }
+      // ---- running maximum of a row (the eight lanes of the same t)
+      float nm[NR][2], alpha[NR][2];
+      bool raised = false;
+#pragma unroll
+      for (int u = 0; u < NR; ++u)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float mx = -INFINITY;
+#pragma unroll
+          for (int g = 0; g < KT / 16; ++g) mx = max3(mx, s[g][u][e], s[g][u][2 + e]);
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          const float before = mrun[u][e];
+          const bool raise = mx > before + RESCALE_LOG2 || (before == -INFINITY && mx > -INFINITY);
+          alpha[u][e] = raise ? (before == -INFINITY ? 0.f : ex2(before - mx)) : 1.f;
+          if (raise) {
+            raised |= before != -INFINITY;   // (nothing to scale before the first visible key)
+            if (!E4M3) l[u][e] *= alpha[u][e];
+            mrun[u][e] = mx;
+          }
+          nm[u][e] = mrun[u][e] == -INFINITY ? 0.f : -mrun[u][e];
+        }
+      if (__any_sync(0xffffffffu, raised)) {
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+          for (int u = 0; u < NR; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[c][u][e] *= alpha[u][e & 1];
+      }
+      // ---- weights, as an operand: pb[g][u]: positions 16 g + 2 t, + 1 (and 8 more) of row 8 u + gr
+      uint32_t pb[KT / 16][NR][2];
+#pragma unroll
+      for (int g = 0; g < KT / 16; ++g)
+#pragma unroll
+        for (int u = 0; u < NR; ++u)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const float a = ex2(s[g][u][2 * v] + nm[u][0]), b = ex2(s[g][u][2 * v + 1] + nm[u][1]);
+            if (!E4M3) {
+              l[u][0] += a;
+              l[u][1] += b;
+            }
+            pb[g][u][v] = transpose(E4M3 ? pack_f16(a, b) : pack_bf16(a, b));
+          }
       // ---- values that are not finite, in a stage that some row does not see whole: into the outputs of the rows
       // that see them, and out of the tile (their weight elsewhere is 0, and 0 times them NaN)
+      if (E4M3 && partial) {                // (NaN codes: their rows' scales already are NaN to those that see them)
+#pragma unroll 1
+        for (int i = 0; i < L::TILE / 16 / 32; ++i) {
+          uint4* w = reinterpret_cast<uint4*>(vt) + i * 32 + lane;
+          uint4 y = *w;
+          auto clear = [](uint32_t c) {
+            const uint32_t bad = ((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+            return c & ~((bad >> 7) * 0xffu);
+          };
+          *w = make_uint4(clear(y.x), clear(y.y), clear(y.z), clear(y.w));
+        }
+        fence_async_smem();                 // (the next copy into the slot follows)
+        __syncwarp();
+      }
       if (!E4M3 && partial) {
         uint32_t any = 0;
 #pragma unroll
@@ -608,13 +721,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
         if (__any_sync(0xffffffffu, (any & 0x80008000u) != 0)) {
           for (int key = 0; key < KT; ++key)
 #pragma unroll
-            for (int n = 0; n < D / 8; ++n)
+            for (int c = 0; c < D / 16; ++c)
 #pragma unroll
-              for (int e = 0; e < 2; ++e) {
-                const float v = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(vt + chunk_at<D, E4M3>(key, n) + (2 * t + e) * 2));
-                if (!isfinite(v)) {
-                  if (sees(p0 + key, end[0], lo[0], sk)) o[n][e] += v;
-                  if (sees(p0 + key, end[1], lo[1], sk)) o[n][2 + e] += v;
+              for (int v = 0; v < 2; ++v) {
+                const float y = __bfloat162float(*reinterpret_cast<const __nv_bfloat16*>(vt + chunk_at<D, E4M3>(key, 2 * c + v) + gr * 2));
+                if (!isfinite(y)) {
+#pragma unroll
+                  for (int u = 0; u < NR; ++u)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                      if (sees(p0 + key, end[u][e], lo[u][e], sk)) o[c][u][2 * v + e] += y;
                 }
               }
           __syncwarp();
@@ -623,39 +739,34 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
             const uint32_t bad = ((*w & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
             *w &= ~(((bad >> 15) & 0x00010001u) * 0xffffu);
           }
-          fence_async_smem();             // (the next copy into the slot follows)
+          fence_async_smem();               // (the next copy into the slot follows)
           __syncwarp();
         }
       }
       // ---- outputs
 #pragma unroll
-      for (int g2 = 0; g2 < KT / 16; ++g2) {
-        const uint32_t pa[4] = {pack_bf16(s[2 * g2][0], s[2 * g2][1]), pack_bf16(s[2 * g2][2], s[2 * g2][3]),
-                                pack_bf16(s[2 * g2 + 1][0], s[2 * g2 + 1][1]), pack_bf16(s[2 * g2 + 1][2], s[2 * g2 + 1][3])};
-        if (E4M3) {
-          const __nv_bfloat162 f = bf2(247u * 0x00800080u);
+      for (int g = 0; g < KT / 16; ++g) {
+        const int m = lane >> 3;
+        if constexpr (E4M3) {
 #pragma unroll
           for (int c2 = 0; c2 < D / 32; ++c2) {
             uint32_t b[4];
-            const int m = lane >> 3, key = g2 * 16 + (m & 1) * 8 + (lane & 7);
-            ldsm_t(va + chunk_at<D, E4M3>(key, c2 * 2 + (m >> 1)), b);
+            ldsm_t(va + chunk_at<D, E4M3>(g * 16 + (m & 1) * 8 + (lane & 7), c2 * 2 + (m >> 1)), b);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-              uint32_t e0, o0, e1, o1;
-              widen<0x6240, 0x7351>(b[2 * i], f, e0, o0);
-              widen<0x6240, 0x7351>(b[2 * i + 1], f, e1, o1);
-              mma(o[4 * c2 + 2 * i], pa, e0, e1);
-              mma(o[4 * c2 + 2 * i + 1], pa, o0, o1);
+            for (int i = 0; i < 2; ++i) {   // bytes: (position 0: d, d + 1), (position 1: d, d + 1)
+              const uint32_t x0 = __byte_perm(b[2 * i], 0, 0x3120), x1 = __byte_perm(b[2 * i + 1], 0, 0x3120);
+              const uint32_t a[4] = {widen_lo(x0), widen_hi(x0), widen_lo(x1), widen_hi(x1)};
+#pragma unroll
+              for (int u = 0; u < NR; ++u) mma_f16(o[2 * c2 + i][u], a, pb[g][u][0], pb[g][u][1]);
             }
           }
         } else {
 #pragma unroll
-          for (int c2 = 0; c2 < D / 16; ++c2) {
-            uint32_t b[4];
-            const int m = lane >> 3, key = g2 * 16 + (m & 1) * 8 + (lane & 7);
-            ldsm_t(va + chunk_at<D, E4M3>(key, c2 * 2 + (m >> 1)), b);
-            mma(o[2 * c2], pa, b[0], b[1]);
-            mma(o[2 * c2 + 1], pa, b[2], b[3]);
+          for (int c = 0; c < D / 16; ++c) {
+            uint32_t a[4];
+            ldsm_t(va + chunk_at<D, E4M3>(g * 16 + (m >> 1) * 8 + (lane & 7), c * 2 + (m & 1)), a);
+#pragma unroll
+            for (int u = 0; u < NR; ++u) mma(o[c][u], a, pb[g][u][0], pb[g][u][1]);
           }
         }
       }
@@ -665,11 +776,21 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     if (!ok) break;
 
     // ---- the segment's result
+    float lse[NR][2];                     // of l: its base's exponent
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      l[u] += __shfl_xor_sync(0xffffffffu, l[u], 1);
-      l[u] += __shfl_xor_sync(0xffffffffu, l[u], 2);
-    }
+    for (int u = 0; u < NR; ++u)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        lse[u][e] = mrun[u][e];
+        if (E4M3) {                       // the eight threads' sums to one base
+          lse[u][e] = msum[u][e];
+#pragma unroll
+          for (int w = 4; w <= 16; w <<= 1) lse[u][e] = fmaxf(lse[u][e], __shfl_xor_sync(0xffffffffu, lse[u][e], w));
+          if (msum[u][e] != lse[u][e]) l[u][e] *= ex2(msum[u][e] - lse[u][e]);   // (-inf: l is 0)
+        }
+#pragma unroll
+        for (int w = 4; w <= 16; w <<= 1) l[u][e] += __shfl_xor_sync(0xffffffffu, l[u][e], w);
+      }
     const bool whole = count == x.stages;
     if (!whole && lane == 0) {
       Stretch& y = info[warp];
@@ -693,35 +814,32 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
     // a part goes where the stages were (the last one: the ring is the warp's own and empty), or into the scratch
     float* part = at + count >= stop ? reinterpret_cast<float*>(ring) : j.parts + (int64_t)worker * j.part_rows * (D + 4);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int r = gr + 8 * u;
-      if (r >= rows || (!whole && r >= j.part_rows)) continue;
-      const float inv = l[u] == 0.f ? 0.f : 1.0f / l[u];
-      const int i = tile * ROWS + r, tok = i / j.G, hq = i - tok * j.G;
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + hq) * j.o.head + (int64_t)(x.r0 + tok) * j.o.row;
-      float* pd = part + r * D;
-      if (!whole && t == 0) part[j.part_rows * D + r] = l[u] == 0.f ? -INFINITY : mrun[u] + log2f(l[u]);
-      if (E4M3) {
+    for (int u = 0; u < NR; ++u)
 #pragma unroll
-        for (int c = 0; c < D / 16; ++c) {   // columns 16 c + 4 t ..
-          const float4 y = make_float4(o[2 * c][2 * u] * inv, o[2 * c + 1][2 * u] * inv, o[2 * c][2 * u + 1] * inv,
-                                       o[2 * c + 1][2 * u + 1] * inv);
-          if (whole)
-            *reinterpret_cast<uint2*>(dst + 16 * c + 4 * t) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
-          else
-            *reinterpret_cast<float4*>(pd + 16 * c + 4 * t) = y;
-        }
-      } else {
+      for (int e = 0; e < 2; ++e) {
+        const int r = 8 * u + 2 * t + e;
+        if (r >= rows || (!whole && r >= j.part_rows)) continue;
+        const float inv = l[u][e] == 0.f ? 0.f : E4M3 ? ex2(mrun[u][e] - lse[u][e]) / l[u][e] : 1.0f / l[u][e];
+        const int i = tile * UNIT + r, tok = i / j.G, hq = i - tok * j.G;
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + hq) * j.o.head + (int64_t)(x.r0 + tok) * j.o.row;
+        float* pd = part + r * D;
+        if (!whole && gr == 0) part[j.part_rows * D + r] = l[u][e] == 0.f ? -INFINITY : lse[u][e] + log2f(l[u][e]);
 #pragma unroll
-        for (int n = 0; n < D / 8; ++n) {
-          const float a = o[n][2 * u] * inv, b = o[n][2 * u + 1] * inv;
-          if (whole)
-            *reinterpret_cast<uint32_t*>(dst + 8 * n + 2 * t) = pack_bf16(a, b);
-          else
-            *reinterpret_cast<float2*>(pd + 8 * n + 2 * t) = make_float2(a, b);
+        for (int c = 0; c < D / 16; ++c) {
+          const float a = o[c][u][e] * inv, b = o[c][u][2 + e] * inv;
+          if (E4M3 && whole) {
+            *reinterpret_cast<uint32_t*>(dst + 16 * c + 2 * gr) = pack_bf16(a, b);
+          } else if (E4M3) {
+            *reinterpret_cast<float2*>(pd + 16 * c + 2 * gr) = make_float2(a, b);
+          } else if (whole) {
+            dst[16 * c + gr] = __float2bfloat16_rn(a);
+            dst[16 * c + 8 + gr] = __float2bfloat16_rn(b);
+          } else {
+            pd[16 * c + gr] = a;
+            pd[16 * c + 8 + gr] = b;
+          }
         }
       }
-    }
     at += count;
   }
   if (!ok) {
@@ -754,9 +872,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
       ++n;
     }
     if (c >= 0 && !ends) open = c;        // (one at most: the last chain)
-    // rows in turn with the other chains' (a warp's first: (warp - todo) mod 8)
+    // rows in turn with the other chains' (a warp's first: warp - todo, modulo their number)
 #pragma unroll 1
-    for (int r = (warp - todo) & (WARPS - 1); r < rows; r += WARPS) {
+    for (int r = (warp + 16 * WARPS - todo % WARPS) % WARPS; r < rows; r += WARPS) {
       float m, l, o[D / 32];
       // (every part's address by itself: some are in shared memory)
       const int log = j.part_rows * D + r;
@@ -806,29 +924,38 @@ __global__ void __launch_bounds__(WARPS * 32, 1)
   __syncthreads();
   float* room = reinterpret_cast<float*>(smem);
   if (last[0])
-    join<D>(j, info[0].hh, info[0].htile, min(info[0].hrows, j.part_rows), info[0].hr0, info[0].first,
+    join<D, WARPS>(j, info[0].hh, info[0].htile, min(info[0].hrows, j.part_rows), info[0].hr0, info[0].first,
             info[0].hlast - info[0].first + 1, room);
   if (last[1]) {
     const Stretch& y = info[max(open, 0)];
-    join<D>(j, y.h, y.tile, min(y.rows, j.part_rows), y.r0, blockIdx.x, y.last - (int)blockIdx.x + 1, room);
+    join<D, WARPS>(j, y.h, y.tile, min(y.rows, j.part_rows), y.r0, blockIdx.x, y.last - (int)blockIdx.x + 1, room);
   }
 }
 
+template <int D, bool E4M3, int NR>
+cudaError_t launch_n(const Maps& maps, const Job& job, int ctas, cudaStream_t st) {
+  using L = Lay<D, E4M3, NR>;
+  return launch_kernel(cache_attend_rows<D, E4M3, NR>, dim3(ctas), L::WARPS * 32, L::BYTES, 1, false, st, maps.rk, maps.rv, job);
+}
 template <int D, bool E4M3>
 cudaError_t launch_d(const Maps& maps, const Job& job, int ctas, cudaStream_t st) {
-  return launch_kernel(cache_attend_rows<D, E4M3>, dim3(ctas), WARPS * 32, Lay<D, E4M3>::BYTES, 1, false, st, maps.rk,
-                       maps.rv, job);
+  return job.unit == 8 ? launch_n<D, E4M3, 1>(maps, job, ctas, st) : launch_n<D, E4M3, 2>(maps, job, ctas, st);
 }
 
+template <int D, bool E4M3, int NR>
+cudaError_t set_limit_n() {
+  return taken(cudaFuncSetAttribute(cache_attend_rows<D, E4M3, NR>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                    Lay<D, E4M3, NR>::BYTES));
+}
 template <int D, bool E4M3>
 cudaError_t set_limit() {
-  return taken(cudaFuncSetAttribute(cache_attend_rows<D, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                    Lay<D, E4M3>::BYTES));
+  const cudaError_t e = set_limit_n<D, E4M3, 1>();
+  return e != cudaSuccess ? e : set_limit_n<D, E4M3, 2>();
 }
 
 template <int D, bool E4M3>
 bool make_d(const Pool& c, Maps* m) {
-  using L = Lay<D, E4M3>;
+  using L = Lay<D, E4M3, 1>;
   const int64_t dim[4] = {D, c.page_len, c.H, c.n_pages};
   const int64_t stride[3] = {(int64_t)D * L::ES, (int64_t)c.page_len * D * L::ES, (int64_t)c.H * c.page_len * D * L::ES};
   const int box[4] = {E4M3 ? D : 64, std::min(c.page_len, L::KT), 1, 1};
@@ -836,7 +963,9 @@ bool make_d(const Pool& c, Maps* m) {
   return make_map_4d(&m->rk, c.k, L::ES, dim, stride, box, swizzle) && make_map_4d(&m->rv, c.v, L::ES, dim, stride, box, swizzle);
 }
 
-int part_rows(int G, int max_rows) { return std::min(ROWS, std::min(max_rows, ROWS) * G); }
+// Query rows of a unit, and of a partial result.
+int unit_rows(int G, int max_rows) { return (int64_t)max_rows * G <= 8 ? 8 : 16; }
+int part_rows(int G, int max_rows) { return (int)std::min<int64_t>(unit_rows(G, max_rows), (int64_t)max_rows * G); }
 
 }  // namespace
 
@@ -865,7 +994,7 @@ cudaError_t launch_attend_rows(const Pool& c, const Maps& maps, const Seqs& s, c
   // call keeps its number: its replays, one after the other, each find the count cleared by the one before)
   static std::atomic<unsigned long long> calls{0};
   unsigned long long* const arrived = static_cast<unsigned long long*>(scratch);
-  const Job job{c, s, m, q, o, G, max_rows, part_rows(G, max_rows), reinterpret_cast<float*>(arrived + MAX_CTAS), arrived,
+  const Job job{c, s, m, q, o, G, max_rows, unit_rows(G, max_rows), part_rows(G, max_rows), reinterpret_cast<float*>(arrived + MAX_CTAS), arrived,
                 (calls.fetch_add(1) + 1) & 0xffffffffffffull};
   if (c.d == 128)
     return c.e4m3 ? launch_d<128, true>(maps, job, n_sm, st) : launch_d<128, false>(maps, job, n_sm, st);

@@ -217,6 +217,26 @@ def test_large_scores(dkv, fmt, n):
     verify(dkv, c, 2, scale=0.003, rows={0, n - 1, n, 2 * n - 1})
 
 
+@pytest.mark.parametrize("n", [1, 150])
+@pytest.mark.parametrize("qs,ks", [(0, 0), (90, -90), (-90, 90), (-100, 60)])
+def test_row_magnitudes(dkv, n, qs, ks):
+    """Quantised rows and queries of very different magnitudes: scales from 2^-100 to 2^100 side by side, which
+    no 16-bit product could hold as they are."""
+    c = R.Case([(n, 130 + n), (n, 333)], 2, 128, 32, "e4m3", seed=n + 7)
+    rng = np.random.default_rng(n)
+    kb, vb = (rng.integers(-3, 3, c.ks.shape) for _ in range(2))
+    vb = np.where(rng.random(c.vs.shape) < 0.3, rng.integers(-100, 100, c.vs.shape), vb)
+    c.ks, c.vs = (c.ks + kb + ks).astype(np.uint8), (c.vs + vb).astype(np.uint8)
+    c.k, c.v = R.decode(c.kc, c.ks), R.decode(c.vc, c.vs)
+    Q = R.bf16(rng.standard_normal((4, c.rows, 128)) * 2.0 ** (qs + rng.integers(-3, 3, (4, c.rows, 1))))
+    cache, s = c.cache(dkv), c.device_seqs(dkv)
+    scale = 2.0 ** -(qs + ks) / 11.0
+    O = cache.attend(dev(Q), s, max_rows=n, scale=scale)
+    cache.sync()
+    R.check(O, R.attend(c, Q, scale=scale, rows=set(range(0, 2 * n, 11))))
+    cache.close()
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("n", [1, 5, 200])
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
