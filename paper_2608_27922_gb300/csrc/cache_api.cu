@@ -178,7 +178,7 @@ dkv_status_t dkv_cache_attend(dkv_cache_t c, const dkv_cache_seqs_t* seqs, const
   const int max_rows = how->max_rows < rows ? how->max_rows : rows;
   if (scratch_bytes < scratch_of(c->pool, H_q, max_rows)) return DKV_ERR_NOMEM;
   const float scale = how->scale > 0.f ? how->scale : 1.0f / std::sqrt((float)c->pool.d);
-  const cache::Mask m{scale * 1.4426950408889634f, how->window, how->sinks, how->block};
+  const cache::Mask m{scale * 1.4426950408889634f, how->window, how->sinks, how->block, cache::inverse_of(how->block)};
   OnDevice on(c->device);
   if (!on.ok) return DKV_ERR_CUDA;
   c->last = (cudaStream_t)stream;

@@ -41,7 +41,9 @@ struct Packed {
 struct Mask {
   float sl2;   // scale * log2(e)
   int window, sinks, block;
+  uint64_t inverse;   // ceil(2^64 / block), block >= 2: p / block is the high half of p times it (p < 2^32)
 };
+inline uint64_t inverse_of(int block) { return block >= 2 ? ~(uint64_t)0 / (uint64_t)block + 1 : 0; }
 
 enum : int { SITE_ROWS = 1, SITE_LEN = 2, SITE_PAGE = 3, SITE_CHUNK = 4, SITE_WAIT = 400 };
 
@@ -106,7 +108,13 @@ __device__ __forceinline__ float scale_of(uint32_t byte) {
 // end(p) of include/dkv.h.
 __host__ __device__ __forceinline__ int visible_end(const Mask& m, int p, int len) {
   if (m.block == 0) return len;
-  const int64_t e = ((int64_t)(p / m.block) + 1) * m.block;
+  if (m.block == 1) return p < len ? p + 1 : len;
+#ifdef __CUDA_ARCH__
+  const int q = (int)__umul64hi((uint64_t)(uint32_t)p, m.inverse);
+#else
+  const int q = (int)(((unsigned __int128)(uint32_t)p * m.inverse) >> 64);
+#endif
+  const int64_t e = ((int64_t)q + 1) * m.block;
   return e < len ? (int)e : len;
 }
 // First position of the window that ends there (the sinks before it are visible too).

@@ -15,8 +15,9 @@
 // of the copy: code bits shifted into bf16's fields are the value times 2^-120, one product with
 // 2^120 times the row's scale makes it exact (bf16 holds every code times its scale).
 //
-// Persistent: one CTA an SM walks items (whole units; the last ones, where they do not fill the SMs, cut
-// into equal parts of their key tiles, joined by cache_merge).  The producer warp runs one item
+// Persistent: one CTA an SM takes items, the first by its number and then whichever is next: whole units, or,
+// where there are few of them, parts of C key tiles each, joined by cache_merge.  A sequence's last
+// tokens come first, which see most, so that the last items are short ones.  The producer warp runs one item
 // ahead and every barrier runs on from item to item, so that an item's first products are
 // issued while the previous one's outputs are still being stored.
 //
@@ -28,7 +29,7 @@
 #include "tc_ptx.cuh"
 
 #include <algorithm>
-#include <type_traits>
+#include <atomic>
 
 namespace dkv {
 
@@ -46,12 +47,14 @@ constexpr int PANEL = 128 * 128;         // bytes of a 64-column panel of 128 ro
 constexpr uint32_t TMEM_COLS = 512;      // S_0 [0,128), O_0 [128,256), S_1 [256,384), O_1 [384,512)
 constexpr float RESCALE_LOG2 = 8.0f;
 constexpr int MAX_CTAS = 152;            // persistent CTAs (the SMs of the GPU): sizes the scratch
-constexpr int MAX_PARTS = 3 * MAX_CTAS;  // parts of cut units
+constexpr int CUT_ROUNDS = 4;            // this many units a CTA, or more, are not cut: little is left to even out
+constexpr int MAX_PARTS = 4 * MAX_CTAS;  // partial results
+constexpr int MAX_ITEMS = 16 * MAX_CTAS; // items of a call that cuts units
 constexpr int MAX_CUT = 32;              // parts of one unit
 constexpr int MIN_PART = 4;              // key tiles of a part, at least
-// What an item costs beside its key tiles, and the joining of parts, in key tiles (1.1 us each at
-// two query tiles of 128 dimensions)
-constexpr int ITEM_TILES = 2, JOIN_TILES = 6;
+// What an item costs beside its key tiles, a part (which stores its outputs in 32 bits) more than that, and the joining of
+// parts, in key tiles (1.6 us each at two query tiles of 128 dimensions)
+constexpr int ITEM_TILES = 2, PART_TILES = 2, JOIN_TILES = 6;
 
 template <int D, bool E4M3>
 struct Lay {
@@ -83,9 +86,13 @@ struct Job {
   Mask m;
   Packed o;
   int G, TQ, max_rows;
-  int cut;            // units may be cut
-  int4* plan;         // {whole units, cut units, parts of each, -}, for cache_merge
-  float* parts;       // [MAX_PARTS][(D + 1) * 256]
+  int cut;                     // units may be cut: cache_merge follows
+  int wide;                    // every output row is 32-byte aligned
+  unsigned long long call;     // the call's number
+  unsigned long long* count;   // [3] items taken beside each CTA's first, CTAs done, partial results: call << 24 | count (see take)
+  int4* plan;                  // {units (0: none is cut), tiles of a part, whole ones, -}, for cache_merge
+  int* slot;                   // [MAX_ITEMS] place of an item's partial result
+  float* parts;                // [MAX_PARTS][(D + 1) * 256]
 };
 
 // One item: a unit's key tiles [i0, i1) of its list.
@@ -137,114 +144,213 @@ __device__ __forceinline__ int tile_of(const Item& it, int i) { return i < it.ns
 struct List {
   int ns, w0, n, lo, end, sk;
 };
-__device__ __forceinline__ List list_of(const Mask& m, int tokens, int p0, int len, int TQ) {
-  const Span a = span_of(m, tokens, p0, len, 0, TQ), z = span_of(m, tokens, p0, len, 1, TQ);
+__device__ __forceinline__ List list_of(const Mask& m, int tokens, int p0, int len) {
   List l{};
-  if (a.n == 0 && z.n == 0) return l;
-  l.lo = a.n ? a.lo : z.lo;
-  l.end = z.n ? z.end : a.end;
-  l.sk = z.n ? z.sk : a.sk;
+  const int pl = p0 + tokens - 1;
+  if (tokens <= 0 || pl < 0) return l;
+  l.end = visible_end(m, pl, len);
+  l.lo = window_first(m, visible_end(m, max(p0, 0), len));
+  l.sk = m.window ? min(m.sinks, l.end) : 0;
   l.ns = (l.sk + BK - 1) / BK;
   l.w0 = max(l.ns, l.lo / BK);
   l.n = l.ns + max(0, (l.end + BK - 1) / BK - l.w0);
   return l;
 }
 
-// ------------------------------------------------------------------ the walk over items
-// Units, sequence by sequence, key head by key head, last tokens first (they see most); U whole
-// ones, then R cut into S parts each (part s of all of them before part s + 1: the parts that read
-// the same keys run side by side).
-struct Plan {
-  int U, R, S;
-};
-
-__device__ __forceinline__ int units_of(const Job& j, const Seq& q) { return (q.n + 2 * j.TQ - 1) / (2 * j.TQ); }
-
-// All lanes of one warp.
-__device__ Plan make_plan(const Job& j, int ctas) {
-  const int lane = threadIdx.x & 31;
-  int units = 0, longest = 0;
-  for (int b = lane; b < j.s.n; b += 32) {
-    const Seq q = seq_at(j.c, j.s, b);
-    if (q.n > j.max_rows) fail(j.c.status, DEV_INCONSISTENT, SITE_CHUNK);
-    const int nu = units_of(j, q);
-    units += nu * j.c.H;
-    if (nu > 0) {
-      const int t0 = (nu - 1) * 2 * j.TQ;
-      longest = max(longest, list_of(j.m, q.n - t0, q.len - q.n + t0, q.len, j.TQ).n);
+// ------------------------------------------------------------------ the items
+// A count in scratch memory that nobody has cleared: call << 24 | count once somebody has put that there.  One more;
+// the count before it.
+__device__ __forceinline__ void begin_count(unsigned long long* at, unsigned long long call) {
+  const unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(at);
+  if ((old >> 24) != call) atomicCAS(at, old, call << 24);
+}
+__device__ int taken_as(unsigned long long* at, unsigned long long call, unsigned long long old) {   // (old: of the addition)
+  for (;; old = atomicAdd(at, 1ull)) {
+    if ((old >> 24) == call) return (int)(old & 0xffffffu);
+    // what was added to was no count of this call's yet: put it there, or see that it is
+    old = *reinterpret_cast<volatile unsigned long long*>(at);
+    while ((old >> 24) != call) {
+      const unsigned long long got = atomicCAS(at, old, call << 24);
+      if (got == old) break;
+      old = got;
     }
   }
+}
+__device__ __forceinline__ int take(unsigned long long* at, unsigned long long call) {
+  return taken_as(at, call, atomicAdd(at, 1ull));
+}
+
+// Units: sequence by sequence, key head by key head, last tokens first.  Items are the units, or, where those are few:
+//   all of one length: as many whole units as go round the CTAs evenly, then the others in equal parts (part s of all
+//   of them before part s + 1: those that read the same keys run side by side);
+//   else: parts of C tiles of every unit that is longer; S is the sequence's, from its last unit (a head's parts s before
+//   its parts s + 1), and shorter units have empty parts, which are passed over.
+struct Plan {
+  int units, items;
+  int C;       // tiles of a part, 0: no unit is cut
+  int whole;   // units of one length: how many are whole; else -1
+};
+
+__device__ __forceinline__ int tiles_at(const Job& j, const Seq& q, int t) {
+  const int t0 = t * 2 * j.TQ;
+  return list_of(j.m, min(q.n - t0, 2 * j.TQ), q.len - q.n + t0, q.len).n;
+}
+__device__ __forceinline__ int parts_of(int tiles, int C) {
+  return C == 0 || tiles <= C ? 1 : min((int)((unsigned)(tiles + C - 1) / (unsigned)C), MAX_CUT);
+}
+
+// A sequence with its units (of a key head) and the tiles of the first and the last one.
+struct Known {
+  Seq q;
+  int nu, first, last;
+};
+__device__ __forceinline__ Known known(const Job& j, int b) {
+  Known k{};
+  if (b >= j.s.n) return k;
+  k.q = seq_at(j.c, j.s, b);
+  if (k.q.n == 0) return k;
+  k.nu = (int)((unsigned)(k.q.n + 2 * j.TQ - 1) / (unsigned)(2 * j.TQ));
+  k.first = tiles_at(j, k.q, 0);
+  k.last = k.nu > 1 ? tiles_at(j, k.q, k.nu - 1) : k.first;
+  return k;
+}
+
+// All lanes of one warp; mine: sequence `lane`.
+__device__ Plan make_plan(const Job& j, int ctas, Known& mine) {
+  const int lane = threadIdx.x & 31;
+  int units = 0, longest = 0;
+  bool even = true;      // units of one length
+  float tiles = 0.f;     // of all units, about
+  mine = known(j, lane);
+  for (int b = lane; b < j.s.n; b += 32) {
+    const Known k = b == lane ? mine : known(j, b);
+    if (k.q.n > j.max_rows) fail(j.c.status, DEV_INCONSISTENT, SITE_CHUNK);
+    if (k.nu == 0) continue;
+    units += k.nu * j.c.H;
+    tiles += 0.5f * (k.first + k.last) * k.nu * j.c.H;
+    even &= k.first == k.last && (longest == 0 || longest == k.last);
+    longest = max(longest, k.last);
+  }
+  const int most = longest;
   units = __reduce_add_sync(0xffffffffu, units);
   longest = __reduce_max_sync(0xffffffffu, longest);
-  Plan p{units / ctas * ctas, units % ctas, 1};
-  if (p.R > 0 && j.cut) {
-    // lane: S = lane + 1 parts; the units that do not fill the CTAs take ceil(R S / ctas) rounds of longest / S tiles
-    const int S = lane + 1;
-    const bool fits = S == 1 || (longest >= S * MIN_PART && p.R * S <= MAX_PARTS);
-    const int rounds = (p.R * S + ctas - 1) / ctas;
-    const int est = rounds * ((longest + S - 1) / S + ITEM_TILES) + (S > 1 ? JOIN_TILES : 0);
-    const unsigned best = __reduce_min_sync(0xffffffffu, fits ? ((unsigned)min(est, 1 << 24) << 6) | S : 0xffffffffu);
-    p.S = best & 63;
+  even = __all_sync(0xffffffffu, even && (most == 0 || most == longest));
+  Plan p{units, units, 0, 0};
+  if (units == 0 || !j.cut) return p;
+  // lane: the longest unit in S = lane + 1 parts
+  const int S = lane + 1, C = (int)((unsigned)(longest + S - 1) / (unsigned)S);
+  const int rounds = (int)((unsigned)units / (unsigned)ctas), rest = units - rounds * ctas;
+  int length = 0;
+  float est;
+  bool fits;
+  if (even) {
+    length = rounds * ctas + rest * S;
+    fits = S == 1 || (C >= MIN_PART && rest * S <= MAX_PARTS);
+    est = (float)(rounds * (longest + ITEM_TILES));
+    if (rest > 0)
+      est += S == 1 ? (float)(longest + ITEM_TILES)
+                    : (float)((rest * S + ctas - 1) / ctas) * (C + ITEM_TILES + PART_TILES) + JOIN_TILES;
+  } else {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
+    int parts = 0, most_parts = 0;
+#pragma unroll 1
+    for (int b = 0; b < j.s.n; ++b) {
+      Known k = mine;
+      if (b >= 32) k = known(j, b);
+      const int nu = __shfl_sync(0xffffffffu, k.nu, b & 31) * j.c.H, first = __shfl_sync(0xffffffffu, k.first, b & 31),
+                last = __shfl_sync(0xffffffffu, k.last, b & 31);
+      const int sb = parts_of(last, C), mid = parts_of((first + last + 1) / 2, C);
+      length += nu * sb;                                         // with empty ones
+      most_parts += sb > 1 ? nu * sb : 0;
+      parts += sb == 1 ? 0 : mid > 1 ? nu * mid : nu / 2;
+    }
+    fits = S == 1 || (C >= MIN_PART && most_parts <= MAX_PARTS && length <= MAX_ITEMS);
+    // the CTAs are busy to the end but for about a third of the longest item, and at least as long as it
+    est = fmaxf((float)(C + ITEM_TILES), (tiles + (float)(units * ITEM_TILES + parts * (ITEM_TILES + PART_TILES))) / ctas + 0.35f * C) +
+          (S > 1 ? JOIN_TILES : 0);
+  }
+  const unsigned best = __reduce_min_sync(0xffffffffu, fits ? ((unsigned)min((int)(est * 4.f), 1 << 24) << 6) | S : 0xffffffffu);
+  const int s = best & 63;
+  if (s > 1) {
+    p.C = __shfl_sync(0xffffffffu, C, s - 1);
+    p.items = __shfl_sync(0xffffffffu, length, s - 1);
+    p.whole = even ? rounds * ctas : -1;
   }
   return p;
 }
 
-// Unit u -> its sequence and place; all lanes of one warp.
+// Item (or, with C = 0, unit) i -> its sequence and place; before: items of earlier sequences.  All lanes of one warp,
+// mine: sequence `lane`.
 struct Unit {
-  int b, h, t;
+  int b, h, t, s, S, nu, before;
   Seq q;
 };
-__device__ Unit find_unit(const Job& j, int u) {
+__device__ Unit find_unit(const Job& j, int i, int C, const Known& mine) {
   const int lane = threadIdx.x & 31;
+  int before = 0;
   for (int b0 = 0;; b0 += 32) {
-    const int b = b0 + lane;
-    Seq q{};
-    if (b < j.s.n) q = seq_at(j.c, j.s, b);
-    const int nu = units_of(j, q);
-    int incl = nu * j.c.H;
+    Known k = mine;
+    if (b0 > 0) k = known(j, b0 + lane);
+    const int S = parts_of(k.last, C), here = k.nu * j.c.H * S;
+    int incl = here;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
-    const unsigned past = __ballot_sync(0xffffffffu, b < j.s.n && incl > u);
+    const unsigned past = __ballot_sync(0xffffffffu, before + incl > i);
     if (past || b0 + 32 >= j.s.n) {
-      const int k = past ? __ffs(past) - 1 : 31;   // (u is below the sum of all)
-      const int before = __shfl_sync(0xffffffffu, incl - nu * j.c.H, k);
+      const int w = past ? __ffs(past) - 1 : 31;   // (i is below the sum of all)
       Unit r;
-      r.b = min(b0 + k, j.s.n - 1);
-      r.q.r0 = __shfl_sync(0xffffffffu, q.r0, k);
-      r.q.n = __shfl_sync(0xffffffffu, q.n, k);
-      r.q.len = __shfl_sync(0xffffffffu, q.len, k);
-      const int n = max(1, units_of(j, r.q)), rem = u - before;
-      r.h = min(rem / n, j.c.H - 1);
-      r.t = max(0, n - 1 - rem % n);
+      r.b = min(b0 + w, j.s.n - 1);
+      r.before = before + __shfl_sync(0xffffffffu, incl - here, w);
+      r.S = __shfl_sync(0xffffffffu, S, w);
+      r.nu = max(1, __shfl_sync(0xffffffffu, k.nu, w));
+      r.q.r0 = __shfl_sync(0xffffffffu, k.q.r0, w);
+      r.q.n = __shfl_sync(0xffffffffu, k.q.n, w);
+      r.q.len = __shfl_sync(0xffffffffu, k.q.len, w);
+      const unsigned rem = (unsigned)(i - r.before), hs = rem / (unsigned)r.nu, h = r.S == 1 ? hs : hs / (unsigned)r.S;
+      r.t = max(0, r.nu - 1 - (int)(rem - hs * r.nu));
+      r.h = min((int)h, j.c.H - 1);
+      r.s = (int)(hs - h * r.S);
       return r;
     }
-    u -= __shfl_sync(0xffffffffu, incl, 31);
+    before += __shfl_sync(0xffffffffu, incl, 31);
   }
 }
 
-__device__ Item make_item(const Job& j, const Plan& p, int it) {
-  const bool whole = it < p.U;
-  const int k = it - p.U;
-  const int part = whole ? 0 : k / p.R, S = whole ? 1 : p.S;
-  const Unit u = find_unit(j, whole ? it : p.U + k % p.R);
+// Item i and its list; state 0 where it is an empty part.  (Its partial result's place is taken when it is handed out.)
+__device__ Item make_item(const Job& j, const Plan& p, int i, const Known& mine, List& l) {
+  // (units of one length: part s of the R that are cut)
+  int unit = i, s = 0, S = 1;
+  if (p.C > 0 && p.whole >= 0 && i >= p.whole) {
+    const int R = p.units - p.whole, k = i - p.whole;
+    s = (int)((unsigned)k / (unsigned)R);
+    unit = p.whole + k - s * R;
+    S = MAX_CUT;
+  }
+  const Unit u = find_unit(j, unit, p.whole < 0 ? p.C : 0, mine);
+  if (p.whole < 0) {
+    s = u.s;
+    S = u.S;
+  }
   const int t0 = u.t * 2 * j.TQ;
   Item x;
-  x.state = 1;
   x.b = u.b;
   x.h = u.h;
   x.r0 = u.q.r0 + t0;
   x.n = min(u.q.n - t0, 2 * j.TQ);
   x.p0 = u.q.len - u.q.n + t0;
   x.len = u.q.len;
-  const List l = list_of(j.m, x.n, x.p0, x.len, j.TQ);
+  l = list_of(j.m, x.n, x.p0, x.len);
   x.ns = l.ns;
   x.w0 = l.w0;
-  x.i0 = (int)((int64_t)l.n * part / S);
-  x.i1 = (int)((int64_t)l.n * (part + 1) / S);
-  x.part = S > 1 ? k : -1;
+  S = min(S, parts_of(l.n, p.C));
+  x.i0 = s * p.C;
+  x.i1 = s + 1 < S ? x.i0 + p.C : l.n;
+  x.part = S > 1 ? 0 : -1;
+  x.state = s < S;
   return x;
 }
 
@@ -300,6 +406,14 @@ __device__ __noinline__ Wild wild_masks(const Job& j, const Item& it, int end, i
     }
   }
   return w;
+}
+
+// 32 bytes in one store.  (A row a thread, a warp's store is 32 lines whatever its width, a cycle each, and what
+// else the SM's load and store unit has to do waits: as 16-byte stores an item's outputs took 5,000 cycles.)
+__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
 }
 
 // Bits k < x.
@@ -432,6 +546,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
     fence_barrier_init();
   }
   if (warp == 1) tmem_alloc(tmem_holder, TMEM_COLS);
+  if (blockIdx.x == 0 && threadIdx.x < 3) begin_count(j.count + threadIdx.x, j.call);
   pdl_trigger();   // cache_merge's blocks start as SMs free up, and wait there
   fence_before_sync();
   __syncthreads();
@@ -458,19 +573,41 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
     regs_lower<L::REGS_IO>();
     if (warp == 0) {
       // ---------------- producer: items; Q, then K(0), V(0), K(1), ..
-      const Plan plan = make_plan(j, gridDim.x);
-      if (blockIdx.x == 0 && lane == 0) *j.plan = make_int4(plan.U, plan.R, plan.S, 0);
-      const int total = plan.U + plan.R * plan.S;
+      Known mine;
+      const Plan plan = make_plan(j, gridDim.x, mine);
+      if (blockIdx.x == 0 && lane == 0) *j.plan = make_int4(plan.C > 0 ? plan.units : 0, plan.C, plan.whole, 0);
       const int rows = min(j.c.page_len, BK), np = BK / rows;   // rows and boxes of a tile
       uint32_t tc = 0, nq = 0, ni = 0, cc = 0;
       bool ok = true;
-      for (int it = blockIdx.x;; it += gridDim.x, ++ni) {
+      // the next item's number: asked for (and waited for only where it is wanted), wanted
+      unsigned long long ticket = 0;
+      auto ask = [&]() {
+        if (lane == 0) ticket = atomicAdd(j.count, 1ull);
+      };
+      auto next = [&]() {
+        int i = 0;
+        if (lane == 0) i = (int)gridDim.x + taken_as(j.count, j.call, ticket);
+        return __shfl_sync(0xffffffffu, i, 0);
+      };
+      for (int it = blockIdx.x;; ++ni) {
         Item x;
         x.state = 0;
         List l{};
-        if (it < total) {
-          x = make_item(j, plan, it);
-          l = list_of(j.m, x.n, x.p0, x.len, j.TQ);
+        while (it < plan.items) {
+          x = make_item(j, plan, it, mine, l);
+          if (x.state) break;
+          ask();
+          it = next();
+        }
+        if (x.state) {
+          if (x.part >= 0) {
+            int slot = 0;
+            if (lane == 0) {
+              slot = min(take(j.count + 2, j.call), MAX_PARTS - 1);
+              j.slot[it] = slot;
+            }
+            x.part = __shfl_sync(0xffffffffu, slot, 0);
+          }
         }
         if (ni >= 2) ok = mbar_wait_warp(it_empty + (ni & 1), ((ni >> 1) & 1) ^ 1, abort_flag);
         if (!ok) break;
@@ -481,7 +618,11 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         __syncwarp();
         if (x.state == 0) break;
         const int n = x.i1 - x.i0;
-        if (n <= 0) continue;
+        if (n <= 0) {
+          ask();
+          it = next();
+          continue;
+        }
         if (nq > 0 && !(ok = mbar_wait_warp(q_empty, (nq - 1) & 1, abort_flag))) break;
         ++nq;
         if (lane == 0) {
@@ -492,20 +633,32 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
               tma_load_4d(smem + L::Q + g * L::TB + p * PANEL, &tmQ, q_full, p * 64, 0, x.r0 + g * j.TQ, x.h);
         }
         __syncwarp();
+        // pages of the list's tiles, 32 boxes at a time with the lanes: box (i - base) np + .. of tile i
+        const int np_log2 = __ffs(np) - 1, batch = 32 >> np_log2;
+        auto entry_of = [&](int first) -> int {
+          const int i = first + (lane >> np_log2), k0 = tile_of(x, i) * BK + (lane & (np - 1)) * rows;
+          return i < x.i1 && k0 < l.end && (k0 + rows > l.lo || k0 < l.sk)
+                     ? __ldg(j.s.table + (int64_t)x.b * j.s.max_pages + (k0 >> j.c.page_log2)) : 0;
+        };
+        int base = x.i0, pages = entry_of(base), pages_next = entry_of(base + batch);
         // one tile of K or V: a lane a box
         auto load = [&](bool is_k, int i) -> bool {
           const int kt = tile_of(x, i);
           const uint32_t t = tc + (uint32_t)(i - x.i0);
           const int box = E4M3 ? lane : lane / L::NP, panel = E4M3 ? 0 : lane % L::NP;
+          if (i - base >= batch) {          // (K comes first to a tile)
+            base += batch;
+            pages = pages_next;
+            pages_next = entry_of(base + batch);
+          }
           // the box's page; nobody's (zeros) where no row of the unit sees into it
           const int k0 = kt * BK + box * rows;
-          int page = j.c.n_pages;
-          if (box < np && k0 < l.end && (k0 + rows > l.lo || k0 < l.sk)) {
-            page = __ldg(j.s.table + (int64_t)x.b * j.s.max_pages + (k0 >> j.c.page_log2));
-            if ((unsigned)page >= (unsigned)j.c.n_pages) {
-              fail(j.c.status, DEV_INCONSISTENT, SITE_PAGE);
-              page = j.c.n_pages;
-            }
+          int page = __shfl_sync(0xffffffffu, pages, (((i - base) << np_log2) + box) & 31);
+          if (!(box < np && k0 < l.end && (k0 + rows > l.lo || k0 < l.sk))) {
+            page = j.c.n_pages;
+          } else if ((unsigned)page >= (unsigned)j.c.n_pages) {
+            fail(j.c.status, DEV_INCONSISTENT, SITE_PAGE);
+            page = j.c.n_pages;
           }
           const int slot = k0 & (j.c.page_len - 1);
           if (E4M3) {
@@ -536,12 +689,18 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         };
         ok = load(true, x.i0);
         for (int i = x.i0; ok && i < x.i1; ++i) {
+          // (as late as its number's way to here allows: CTAs with short items take more)
+          if (i == max(x.i0, x.i1 - 2)) ask();
           ok = load(false, i);
           if (ok && i + 1 < x.i1) ok = load(true, i + 1);
         }
         tc += n;
         if (!ok) break;
+        it = next();
       }
+      // the last CTA to run out of items clears the counts (a replayed graph's next call has the same number)
+      if (lane == 0 && take(j.count + 1, j.call) == (int)gridDim.x - 1)
+        for (int i = 0; i < 3; ++i) atomicExch(j.count + i, 0ull);
       if (!ok) {
         if (lane == 0) give_up(0);
         // copies may be in flight that nobody waits for any more: far longer than one takes
@@ -802,12 +961,18 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
 #pragma unroll
           for (int k = 0; k < 8; ++k) dst[k * 256] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
         } else if (mine) {
-          uint4* dst = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(x.h * j.G + hq) * j.o.head +
-                                                (int64_t)(x.r0 + token) * j.o.row + c * 32);
+          uint32_t w[16];
 #pragma unroll
-          for (int k = 0; k < 4; ++k)
-            dst[k] = make_uint4(pack_bf16(v[8 * k], v[8 * k + 1]), pack_bf16(v[8 * k + 2], v[8 * k + 3]),
-                                pack_bf16(v[8 * k + 4], v[8 * k + 5]), pack_bf16(v[8 * k + 6], v[8 * k + 7]));
+          for (int k = 0; k < 16; ++k) w[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+          __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(x.h * j.G + hq) * j.o.head +
+                               (int64_t)(x.r0 + token) * j.o.row + c * 32;
+          if (j.wide) {
+            store32(dst, w);
+            store32(dst + 16, w + 8);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(dst)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+          }
         }
       }
       fence_before_sync();   // O_g read before the next item's products overwrite it (they wait for its weights)
@@ -867,21 +1032,48 @@ template <int D>
 __global__ void __launch_bounds__(256) cache_merge(const __grid_constant__ Job j) {
   pdl_wait();
   const int4 p = *j.plan;
-  if (p.z < 2 || (int)blockIdx.x >= p.y) return;
   __shared__ float lse[MAX_CUT][MG_ROWS];
+  __shared__ int slots[MAX_CUT];
   __shared__ Unit su;
+  __shared__ int sS;
+  for (int unit = max(p.z, 0) + blockIdx.x; unit < p.x; unit += gridDim.x) {   // uniform
+  __syncthreads();
   if (threadIdx.x < 32) {
-    const Unit u = find_unit(j, p.x + blockIdx.x);
-    if (threadIdx.x == 0) su = u;
+    const int lane = threadIdx.x;
+    const Known mine = known(j, lane);
+    const Unit u = find_unit(j, unit, 0, mine);
+    int n = parts_of(tiles_at(j, u.q, u.t), p.y), at, step;   // the item of part 0, and from one to the next
+    if (p.z >= 0) {
+      at = unit;
+      step = p.x - p.z;
+    } else {   // those of the sequences before it, then (head, part, unit)
+      int before = 0;
+      for (int b = lane; b < u.b; b += 32) {
+        const Known k = b == lane ? mine : known(j, b);
+        before += k.nu * j.c.H * parts_of(k.last, p.y);
+      }
+      before = __reduce_add_sync(0xffffffffu, before);
+      const int SB = parts_of(tiles_at(j, u.q, u.nu - 1), p.y);
+      n = min(n, SB);
+      at = before + u.h * SB * u.nu + (u.nu - 1 - u.t);
+      step = u.nu;
+    }
+    if (n > 1 && lane < n) slots[lane] = j.slot[at + lane * step];
+    if (lane == 0) {
+      su = u;
+      sS = n;
+    }
   }
-  const int S = min(p.z, MAX_CUT), R = p.y, row0 = blockIdx.y * MG_ROWS;
-  auto part = [&](int s) { return j.parts + (int64_t)(s * R + (int)blockIdx.x) * (256 * (D + 1)); };
+  __syncthreads();
+  const int S = sS, row0 = blockIdx.y * MG_ROWS;
+  if (S < 2) continue;
+  auto part = [&](int s) { return j.parts + (int64_t)slots[s] * (256 * (D + 1)); };
   for (int e = threadIdx.x; e < S * MG_ROWS; e += 256) lse[e / MG_ROWS][e % MG_ROWS] = part(e / MG_ROWS)[256 * D + row0 + e % MG_ROWS];
   __syncthreads();
   const Unit u = su;
   const int rl = threadIdx.x % MG_ROWS, row = row0 + rl, q = threadIdx.x / MG_ROWS;   // 8 column groups
   const int g = row / BQ, r = row % BQ, tok = r / j.G, token = g * j.TQ + tok;
-  if (tok >= j.TQ || u.t * 2 * j.TQ + token >= u.q.n) return;
+  if (tok >= j.TQ || u.t * 2 * j.TQ + token >= u.q.n) continue;
   float mx = -INFINITY, den = 0.f;
   for (int s = 0; s < S; ++s) mx = fmaxf(mx, lse[s][rl]);
   float o[D / 8];
@@ -908,6 +1100,7 @@ __global__ void __launch_bounds__(256) cache_merge(const __grid_constant__ Job j
                                               (int64_t)(u.q.r0 + u.t * 2 * j.TQ + token) * j.o.row + q * (D / 8));
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) dst[k] = pack_bf16(o[2 * k] * inv, o[2 * k + 1] * inv);
+  }
 }
 
 template <int D, bool E4M3>
@@ -945,7 +1138,9 @@ bool make_tc_maps(const Pool& c, Maps* m) {
   return make_map_4d(&m->k, c.k, es, dim, stride, box, swizzle) && make_map_4d(&m->v, c.v, es, dim, stride, box, swizzle);
 }
 
-size_t attend_tc_scratch(const Pool& c) { return 256 + sizeof(float) * (size_t)MAX_PARTS * 256 * (c.d + 1); }
+size_t attend_tc_scratch(const Pool& c) {
+  return 256 + sizeof(int) * (size_t)MAX_ITEMS + sizeof(float) * (size_t)MAX_PARTS * 256 * (c.d + 1);
+}
 
 cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
                              int max_rows, const Mask& m, void* scratch, cudaStream_t st) {
@@ -957,8 +1152,16 @@ cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, con
   const int64_t stride[3] = {head * 2, row * 2, G * head * 2};
   const int box[4] = {64, G, TQ, 1};
   if (!make_map_4d(&mq, q.p, 2, dim, stride, box, 128)) return cudaErrorInvalidValue;
-  Job job{c, s, m, o, G, TQ, max_rows, 1, static_cast<int4*>(scratch),
-          reinterpret_cast<float*>(static_cast<char*>(scratch) + 256)};
+  // numbers the calls, so that what another call left in the same memory is not taken for a count of this one's (a
+  // captured call keeps its number: its replays, one after the other, each find the counts cleared by the one before)
+  static std::atomic<unsigned long long> calls{0};
+  char* const at = static_cast<char*>(scratch);
+  // (several sequences make more units than one with all their rows)
+  const bool cut = (int64_t)c.H * ((s.rows + 2 * TQ - 1) / (2 * TQ)) < CUT_ROUNDS * n_sm;
+  const Job job{c, s, m, o, G, TQ, max_rows, cut ? 1 : 0,
+                (uintptr_t)o.p % 32 == 0 && o.head % 16 == 0 && o.row % 16 == 0, (calls.fetch_add(1) + 1) & 0xffffffffffull, reinterpret_cast<unsigned long long*>(at),
+                reinterpret_cast<int4*>(at + 64), reinterpret_cast<int*>(at + 256),
+                reinterpret_cast<float*>(at + 256 + sizeof(int) * MAX_ITEMS)};
   if (c.d == 128)
     return c.e4m3 ? launch_d<128, true>(maps, job, mq, n_sm, st) : launch_d<128, false>(maps, job, mq, n_sm, st);
   return c.e4m3 ? launch_d<64, true>(maps, job, mq, n_sm, st) : launch_d<64, false>(maps, job, mq, n_sm, st);

@@ -47,12 +47,12 @@ int main() {
           }
         }
   // the mask, against its definition
-  for (int block : {0, 1, 3, 16, 2147483647})
+  for (int block : {0, 1, 2, 3, 7, 16, 4680, 2147483646, 2147483647})
     for (int window : {0, 1, 5, 2147483647})
       for (int len : {1, 2, 17, 1 << 30})
-        for (int p : {0, 1, 15, 16, (1 << 30) - 1}) {
+        for (int p : {0, 1, 2, 6, 7, 15, 16, 4679, 4680, (1 << 30) - 2, (1 << 30) - 1}) {
           if (p >= len) continue;
-          const Mask m{1.f, window, 0, block};
+          const Mask m{1.f, window, 0, block, inverse_of(block)};
           const int e = visible_end(m, p, len);
           const int64_t want = block == 0 ? len : ((int64_t)p / block + 1) * block;
           if (e != (want < len ? want : len)) return 8;
