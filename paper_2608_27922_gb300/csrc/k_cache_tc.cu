@@ -444,12 +444,12 @@ __device__ __forceinline__ uint32_t times(uint32_t x, __nv_bfloat162 f) {
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// A [128][D] tile of codes and its rows' scales into a swizzled bf16 tile (W warps).  Eight
-// neighbouring threads take 64 columns of two rows, chosen so that neither the 16-byte loads (128-byte
+// A [128][D] tile of codes and its rows' scales into a swizzled bf16 tile (W warps); whether a row of
+// the warp's is NaN.  Eight neighbouring threads take 64 columns of two rows, chosen so that neither the 16-byte loads (128-byte
 // swizzled codes at D = 128, plain ones at 64) nor the 16-byte stores of a quarter warp share a bank: rows r
 // and r ^ 5 at D = 128, two adjacent ones at 64.
 template <int D, int W>
-__device__ __forceinline__ void widen_tile(const uint8_t* codes, const uint8_t* scales, uint8_t* tile, int t) {
+__device__ __forceinline__ bool widen_tile(const uint8_t* codes, const uint8_t* scales, uint8_t* tile, int t) {
   constexpr int PANELS = D / 64, UNITS = 16 * PANELS / W;   // units of (8 rows, 64 columns): a warp's
   static_assert(W % PANELS == 0, "a warp stays in its panel");
   constexpr int ROWS = W / PANELS * 8;                // rows from one of them to the next
@@ -477,6 +477,7 @@ __device__ __forceinline__ void widen_tile(const uint8_t* codes, const uint8_t* 
       *reinterpret_cast<uint4*>(lo + k * ROWS * 128) = make_uint4(times(y0.x, f2), times(y0.y, f2), times(y1.x, f2), times(y1.y, f2));
       *reinterpret_cast<uint4*>(hi + k * ROWS * 128) = make_uint4(times(y2.x, f2), times(y2.y, f2), times(y3.x, f2), times(y3.y, f2));
     }
+    return __any_sync(0xffffffffu, big == 255u);
   } else {
 #pragma unroll
     for (int k = 0; k < UNITS; ++k) {
@@ -486,6 +487,7 @@ __device__ __forceinline__ void widen_tile(const uint8_t* codes, const uint8_t* 
       *reinterpret_cast<uint4*>(lo + k * ROWS * 128) = make_uint4(y0.x, y0.y, y1.x, y1.y);
       *reinterpret_cast<uint4*>(hi + k * ROWS * 128) = make_uint4(y2.x, y2.y, y3.x, y3.y);
     }
+    return false;
   }
 }
 
@@ -517,9 +519,11 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
   uint64_t* done = bars + 26;
   Item* items = reinterpret_cast<Item*>(bars + 28);                        // [2]
   volatile int* wild = reinterpret_cast<volatile int*>(items + 2);         // [2] number of the last item with values cleared
-  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(items + 2) + 2;
+  // [2] e4m3: a byte a widening warp, not 0 where it met a NaN row of the slot's values
+  volatile unsigned long long* nan_rows = reinterpret_cast<volatile unsigned long long*>(items + 2) + 1;
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(items + 2) + 6;
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_holder + 1);
-  static_assert(28 * 8 + 2 * sizeof(Item) + 16 <= 512, "control block");
+  static_assert(28 * 8 + 2 * sizeof(Item) + 32 <= 512, "control block");
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 64) {
@@ -849,24 +853,16 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         if (partial) {
           const uint32_t t = tc + (uint32_t)(i - x.i0);
           if (!(ok = mbar_wait_warp(v_full + t % L::NV, (t / L::NV) & 1, abort_flag))) break;
-          if (clear_row<D>(smem + L::V + (t % L::NV) * L::TB, r)) wild[ni & 1] = (int)ni + 1;
+          if ((!E4M3 || nan_rows[t % L::NV] != 0) && clear_row<D>(smem + L::V + (t % L::NV) * L::TB, r)) wild[ni & 1] = (int)ni + 1;
           fence_async_smem();
         }
         if (!(ok = mbar_wait_warp(s_full + g, ns & 1, abort_flag))) break;
         ++ns;
         fence_after_sync();
         // the row's 128 scores, 64 at a time and read twice (maximum, weights): fewer registers and
-        // half the instructions than the whole row at once, which the instruction caches repay
+        // half the instructions than the whole row at once, which the instruction caches repay.  Masked ones go
+        // back into their place in between.
         const int k0 = kt * BK;
-        auto scores = [&](int half, float (&a)[32], float (&b)[32]) {
-          tmem_ld32(sc + half * 64, a);
-          tmem_ld32(sc + half * 64 + 32, b);
-          tmem_wait_ld();
-          if (partial) {
-            mask_row(a, k0 + half * 64, end, lo, sk);
-            mask_row(b, k0 + half * 64 + 32, end, lo, sk);
-          }
-        };
         float tmax;
         {
           float t[8];
@@ -875,10 +871,19 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
             float a[32], b[32];
-            scores(half, a, b);
+            tmem_ld32(sc + half * 64, a);
+            tmem_ld32(sc + half * 64 + 32, b);
+            tmem_wait_ld();
+            if (partial) {
+              mask_row(a, k0 + half * 64, end, lo, sk);
+              mask_row(b, k0 + half * 64 + 32, end, lo, sk);
+              tmem_st32(sc + half * 64, reinterpret_cast<uint32_t(&)[32]>(a));
+              tmem_st32(sc + half * 64 + 32, reinterpret_cast<uint32_t(&)[32]>(b));
+            }
             max_acc(t, a);
             max_acc(t, b);
           }
+          if (partial) tmem_wait_st();
           tmax = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
         }
         tmax *= j.m.sl2;
@@ -895,7 +900,9 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         for (int half = 0; half < 2; ++half) {
           float a[32], b[32];
           uint32_t pk[32];
-          scores(half, a, b);
+          tmem_ld32(sc + half * 64, a);
+          tmem_ld32(sc + half * 64 + 32, b);
+          tmem_wait_ld();
           exp_pack(a, b, j.m.sl2, nm, lab, pk);
           tmem_st32(sc + half * 32, pk);
         }
@@ -992,8 +999,9 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       const uint32_t nb = is_k ? L::NK : L::NV, sl = t % nb;
       if (!mbar_wait_warp(c_full + (c & 1), (c >> 1) & 1, abort_flag)) return false;
       if (t >= nb && !mbar_wait_warp((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
-      widen_tile<D, L::CONV>(smem + L::CODES + (c & 1) * 128 * D, smem + L::SCALES + (c & 1) * 128,
+      const bool nan = widen_tile<D, L::CONV>(smem + L::CODES + (c & 1) * 128 * D, smem + L::SCALES + (c & 1) * 128,
                     smem + (is_k ? L::K : L::V) + sl * L::TB, tid);
+      if (!is_k && lane == 0) reinterpret_cast<volatile uint8_t*>(nan_rows + sl)[warp - L::CONV0] = nan;
       fence_async_smem();
       __syncwarp();
       if (lane == 0) {
