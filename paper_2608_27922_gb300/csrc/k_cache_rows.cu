@@ -135,7 +135,7 @@ __device__ __forceinline__ int stages_of(const Job& j, const Span& x) { return x
 
 // Stages of the whole range; `first`: the span of sequence `lane`.  All lanes of a warp.
 template <int KT>
-__device__ int total_stages(const Job& j, Span& first) {
+__device__ __forceinline__ int total_stages(const Job& j, Span& first) {
   const int lane = threadIdx.x & 31;
   int64_t mine = 0;
   first = Span{};
@@ -160,7 +160,7 @@ struct Place {
   Span x;
 };
 template <int KT>
-__device__ Place find(const Job& j, int at, const Span& first) {
+__device__ __forceinline__ Place find(const Job& j, int at, const Span& first) {
   const int lane = threadIdx.x & 31;
   int begin = 0;
   for (int b0 = 0;; b0 += 32) {
@@ -259,7 +259,7 @@ __device__ __forceinline__ void begin_count(unsigned long long* at, unsigned lon
 }
 // One more of n; true for the last one, which leaves nothing behind.  (One trip to L2 as a rule; taking turns with
 // compare and swap instead cost 13 CTAs 6 us.)
-__device__ bool arrive(unsigned long long* at, unsigned long long call, int n) {
+__device__ __forceinline__ bool arrive(unsigned long long* at, unsigned long long call, int n) {
   for (;;) {
     unsigned long long old = atomicAdd(at, 1ull);
     if ((old >> 16) == call) {
@@ -326,7 +326,7 @@ __device__ __forceinline__ void store_row(const Job& j, int h, int tile, int r0,
 // Joins the n CTAs' parts of a unit, the first one's from CTA `first`, in the CTAs' order: a row a warp, or, where the
 // parts are many for one warp, all warps at a row.  All threads of the CTA; room: shared memory.
 template <int D, int WARPS>
-__device__ void join(const Job& j, int h, int tile, int rows, int r0, int first, int n, float* room) {
+__device__ __forceinline__ void join(const Job& j, int h, int tile, int rows, int r0, int first, int n, float* room) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool shared = n > 32;
   auto at = [&](int p) { return j.parts + (int64_t)(WORKERS + 2 * (first + p) + (p == 0 ? 1 : 0)) * j.part_rows * (D + 4); };
@@ -537,7 +537,7 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
 
     for (int k = 0; k < count; ++k) {
       const int slot = used % L::SLOTS;
-      if (!(ok = mbar_wait_warp(bars + slot, (used / L::SLOTS) & 1, &no_abort))) break;
+      if (!(ok = mbar_wait_warp_short(bars + slot, (used / L::SLOTS) & 1, &no_abort))) break;
       ++used;
       const int kk0 = k0 + k, p0 = (kk0 < x.ns ? kk0 : x.w0 + (kk0 - x.ns)) * KT;
       const bool partial = !(p0 + KT <= x.all_end && (p0 >= x.all_lo || p0 + KT <= sk));

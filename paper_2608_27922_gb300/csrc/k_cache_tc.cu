@@ -74,7 +74,7 @@ struct Lay {
   static constexpr int THREADS = (12 + CONV) * 32;
   // registers a thread of the first four warps, of the softmax warps and of the converting ones; the
   // launch gives every thread 96 (640 threads) or 168 (384)
-  static constexpr int REGS_IO = 80, REGS_SOFT = E4M3 ? 144 : 208, REGS_CONV = 56;
+  static constexpr int REGS_IO = E4M3 ? 80 : 88, REGS_SOFT = E4M3 ? 144 : 208, REGS_CONV = 56;
   static_assert(REGS_IO + 2 * REGS_SOFT + (E4M3 ? 2 * REGS_CONV : 0) <= (E4M3 ? 5 * 96 : 3 * 168), "register split");
   static constexpr int READERS = 1 + 8 + CONV;   // warps that follow the producer's items
   static_assert(BYTES <= 227 * 1024, "shared memory per CTA");
@@ -164,7 +164,7 @@ __device__ __forceinline__ void begin_count(unsigned long long* at, unsigned lon
   const unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(at);
   if ((old >> 24) != call) atomicCAS(at, old, call << 24);
 }
-__device__ int taken_as(unsigned long long* at, unsigned long long call, unsigned long long old) {   // (old: of the addition)
+__device__ __forceinline__ int taken_as(unsigned long long* at, unsigned long long call, unsigned long long old) {   // (old: of the addition)
   for (;; old = atomicAdd(at, 1ull)) {
     if ((old >> 24) == call) return (int)(old & 0xffffffu);
     // what was added to was no count of this call's yet: put it there, or see that it is
@@ -216,7 +216,7 @@ __device__ __forceinline__ Known known(const Job& j, int b) {
 }
 
 // All lanes of one warp; mine: sequence `lane`.
-__device__ Plan make_plan(const Job& j, int ctas, Known& mine) {
+__device__ __forceinline__ Plan make_plan(const Job& j, int ctas, Known& mine) {
   const int lane = threadIdx.x & 31;
   int units = 0, longest = 0;
   bool even = true;      // units of one length
@@ -286,7 +286,7 @@ struct Unit {
   int b, h, t, s, S, nu, before;
   Seq q;
 };
-__device__ Unit find_unit(const Job& j, int i, int C, const Known& mine) {
+__device__ __forceinline__ Unit find_unit(const Job& j, int i, int C, const Known& mine) {
   const int lane = threadIdx.x & 31;
   int before = 0;
   for (int b0 = 0;; b0 += 32) {
@@ -321,7 +321,7 @@ __device__ Unit find_unit(const Job& j, int i, int C, const Known& mine) {
 }
 
 // Item i and its list; state 0 where it is an empty part.  (Its partial result's place is taken when it is handed out.)
-__device__ Item make_item(const Job& j, const Plan& p, int i, const Known& mine, List& l) {
+__device__ __forceinline__ Item make_item(const Job& j, const Plan& p, int i, const Known& mine, List& l) {
   // (units of one length: part s of the R that are cut)
   int unit = i, s = 0, S = 1;
   if (p.C > 0 && p.whole >= 0 && i >= p.whole) {
@@ -368,6 +368,7 @@ __device__ __forceinline__ bool clear_row(uint8_t* tile, int row) {
            ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
   }
   if ((any & 0x80008000u) == 0) return false;
+#pragma unroll 1
   for (int c = 0; c < D / 2; ++c) {
     uint32_t* p = reinterpret_cast<uint32_t*>(tile + (c >> 5) * PANEL + row * 128 + ((((c >> 2) & 7) ^ (row & 7)) << 4)) + (c & 3);
     const uint32_t x = *p, bad = ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
@@ -385,9 +386,11 @@ template <int D, bool E4M3>
 __device__ __noinline__ Wild wild_masks(const Job& j, const Item& it, int end, int lo, int c0) {
   Wild w{0, 0, 0};
   const Span a = span_of(j.m, it.n, it.p0, it.len, 0, j.TQ), z = span_of(j.m, it.n, it.p0, it.len, 1, j.TQ);
+#pragma unroll 1
   for (int i = it.i0; i < it.i1; ++i) {
     const int kt = tile_of(it, i);
     if ((!active(a, kt) || all_seen(a, kt)) && (!active(z, kt) || all_seen(z, kt))) continue;
+#pragma unroll 1
     for (int p = kt * BK; p < min(end, kt * BK + BK); ++p) {
       if (p < lo && !(j.m.window && p < j.m.sinks)) continue;
       const int64_t at = pool_row(j.c, j.s, it.b, it.h, p);
@@ -397,6 +400,7 @@ __device__ __noinline__ Wild wild_masks(const Job& j, const Item& it, int end, i
         continue;
       }
       const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(j.c.v) + at * D + c0;
+#pragma unroll 1
       for (int k = 0; k < 32; ++k) {
         const float x = __bfloat162float(v[k]);
         if (isnan(x)) w.nan |= 1u << k;
@@ -565,7 +569,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
   auto next_item = [&](uint32_t n) -> Item {
     Item x;
     x.state = 0;
-    if (mbar_wait_warp(it_full + (n & 1), (n >> 1) & 1, abort_flag)) {
+    if (mbar_wait_warp_short(it_full + (n & 1), (n >> 1) & 1, abort_flag)) {
       x = items[n & 1];
       __syncwarp();
       if (lane == 0) mbar_arrive(it_empty + (n & 1));
@@ -593,10 +597,12 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         if (lane == 0) i = (int)gridDim.x + taken_as(j.count, j.call, ticket);
         return __shfl_sync(0xffffffffu, i, 0);
       };
+#pragma unroll 1
       for (int it = blockIdx.x;; ++ni) {
         Item x;
         x.state = 0;
         List l{};
+#pragma unroll 1
         while (it < plan.items) {
           x = make_item(j, plan, it, mine, l);
           if (x.state) break;
@@ -613,7 +619,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
             x.part = __shfl_sync(0xffffffffu, slot, 0);
           }
         }
-        if (ni >= 2) ok = mbar_wait_warp(it_empty + (ni & 1), ((ni >> 1) & 1) ^ 1, abort_flag);
+        if (ni >= 2) ok = mbar_wait_warp_short(it_empty + (ni & 1), ((ni >> 1) & 1) ^ 1, abort_flag);
         if (!ok) break;
         if (lane == 0) {
           items[ni & 1] = x;
@@ -627,7 +633,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
           it = next();
           continue;
         }
-        if (nq > 0 && !(ok = mbar_wait_warp(q_empty, (nq - 1) & 1, abort_flag))) break;
+        if (nq > 0 && !(ok = mbar_wait_warp_short(q_empty, (nq - 1) & 1, abort_flag))) break;
         ++nq;
         if (lane == 0) {
           const int groups = x.n > j.TQ ? 2 : 1, bytes = j.TQ * j.G * 128;
@@ -668,7 +674,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
           if (E4M3) {
             const uint32_t c = cc++;
             uint64_t* bar = c_full + (c & 1);
-            if (c >= 2 && !mbar_wait_warp(c_empty + (c & 1), ((c >> 1) & 1) ^ 1, abort_flag)) return false;
+            if (c >= 2 && !mbar_wait_warp_short(c_empty + (c & 1), ((c >> 1) & 1) ^ 1, abort_flag)) return false;
             const unsigned named = __ballot_sync(0xffffffffu, page < j.c.n_pages);
             if (lane == 0) mbar_arrive_expect_tx(bar, BK * D + __popc(named) * rows);
             __syncwarp();
@@ -681,7 +687,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
           } else {
             const uint32_t nb = is_k ? L::NK : L::NV, sl = t % nb;
             uint64_t* bar = (is_k ? k_full : v_full) + sl;
-            if (t >= nb && !mbar_wait_warp((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
+            if (t >= nb && !mbar_wait_warp_short((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
             if (lane == 0) mbar_arrive_expect_tx(bar, L::TB);
             __syncwarp();
             if (box < np)
@@ -693,7 +699,6 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         };
         ok = load(true, x.i0);
         for (int i = x.i0; ok && i < x.i1; ++i) {
-          // (as late as its number's way to here allows: CTAs with short items take more)
           if (i == max(x.i0, x.i1 - 2)) ask();
           ok = load(false, i);
           if (ok && i + 1 < x.i1) ok = load(true, i + 1);
@@ -772,8 +777,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
           const int kt = sp[g].any_end - 1;
           last[g] = kt < x.ns ? kt : x.ns + (kt - x.w0);
         }
-        ok = mbar_wait_warp(q_full, nq & 1, abort_flag) &&
-             mbar_wait_warp(k_full + ks, kph, abort_flag);
+        ok = mbar_wait_warp_short(q_full, nq & 1, abort_flag) &&
+             mbar_wait_warp_short(k_full + ks, kph, abort_flag);
         ++nq;
         if (!ok) break;
         fence_after_sync();
@@ -788,11 +793,11 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
           const bool next = i + 1 < x.i1;
           kt = tile_of(x, i + 1);
           const bool actn[2] = {next && active(sp[0], kt), next && active(sp[1], kt)};
-          if (!(ok = mbar_wait_warp(v_full + vs, vph, abort_flag))) break;
+          if (!(ok = mbar_wait_warp_short(v_full + vs, vph, abort_flag))) break;
 #pragma unroll
           for (int g = 0; g < 2; ++g) {
             if (act[g]) {
-              if (!(ok = mbar_wait_warp(p_full + g, pph[g], abort_flag))) break;
+              if (!(ok = mbar_wait_warp_short(p_full + g, pph[g], abort_flag))) break;
               pph[g] ^= 1;
               fence_after_sync();
               issue_pv(g, vs, fresh[g]);
@@ -800,7 +805,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
               if (i == last[g]) commit(o_full + g);
             }
             if (g == 0 && next) {
-              if (!(ok = mbar_wait_warp(k_full + ks, kph, abort_flag))) break;
+              if (!(ok = mbar_wait_warp_short(k_full + ks, kph, abort_flag))) break;
               fence_after_sync();
             }
             if (actn[g]) issue_s(g, ks);
@@ -837,7 +842,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
     bool ok = true;
     for (uint32_t ni = 0; ok; ++ni) {
       // (the item stays in its slot until its outputs are stored: fewer registers)
-      if (!mbar_wait_warp(it_full + (ni & 1), (ni >> 1) & 1, abort_flag)) break;
+      if (!mbar_wait_warp_short(it_full + (ni & 1), (ni >> 1) & 1, abort_flag)) break;
       const Item& x = items[ni & 1];
       if (x.state == 0) break;
       const Span sp = span_of(j.m, x.n, x.p0, x.len, g, j.TQ);
@@ -852,11 +857,11 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         const bool partial = !all_seen(sp, kt);
         if (partial) {
           const uint32_t t = tc + (uint32_t)(i - x.i0);
-          if (!(ok = mbar_wait_warp(v_full + t % L::NV, (t / L::NV) & 1, abort_flag))) break;
+          if (!(ok = mbar_wait_warp_short(v_full + t % L::NV, (t / L::NV) & 1, abort_flag))) break;
           if ((!E4M3 || nan_rows[t % L::NV] != 0) && clear_row<D>(smem + L::V + (t % L::NV) * L::TB, r)) wild[ni & 1] = (int)ni + 1;
           fence_async_smem();
         }
-        if (!(ok = mbar_wait_warp(s_full + g, ns & 1, abort_flag))) break;
+        if (!(ok = mbar_wait_warp_short(s_full + g, ns & 1, abort_flag))) break;
         ++ns;
         fence_after_sync();
         // the row's 128 scores, 64 at a time and read twice (maximum, weights): fewer registers and
@@ -932,7 +937,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       }
       tc += (uint32_t)max(0, x.i1 - x.i0);
       if (ok && some) {
-        ok = mbar_wait_warp(o_full + g, no & 1, abort_flag);
+        ok = mbar_wait_warp_short(o_full + g, no & 1, abort_flag);
         ++no;
       }
       if (!ok) break;
@@ -997,8 +1002,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
     auto turn = [&](bool is_k, uint32_t t) -> bool {
       const uint32_t c = cc++;
       const uint32_t nb = is_k ? L::NK : L::NV, sl = t % nb;
-      if (!mbar_wait_warp(c_full + (c & 1), (c >> 1) & 1, abort_flag)) return false;
-      if (t >= nb && !mbar_wait_warp((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
+      if (!mbar_wait_warp_short(c_full + (c & 1), (c >> 1) & 1, abort_flag)) return false;
+      if (t >= nb && !mbar_wait_warp_short((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
       const bool nan = widen_tile<D, L::CONV>(smem + L::CODES + (c & 1) * 128 * D, smem + L::SCALES + (c & 1) * 128,
                     smem + (is_k ? L::K : L::V) + sl * L::TB, tid);
       if (!is_k && lane == 0) reinterpret_cast<volatile uint8_t*>(nan_rows + sl)[warp - L::CONV0] = nan;
@@ -1015,11 +1020,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       if (x.state == 0) break;
       const int n = x.i1 - x.i0;
       if (n <= 0) continue;
-      ok = turn(true, tc);
-      for (int i = 0; ok && i < n; ++i) {
-        ok = turn(false, tc + i);
-        if (ok && i + 1 < n) ok = turn(true, tc + i + 1);
-      }
+#pragma unroll 1
+      for (int k = 0; ok && k < 2 * n; ++k) ok = turn((k & 1) == 0, tc + (k >> 1));
       tc += n;
     }
     if (!ok && lane == 0) give_up(3);

@@ -79,6 +79,16 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, v
   return __all_sync(0xffffffffu, mbar_wait_limit(bar, parity, abort, kWaitNs));
 }
 
+// The same in few instructions, limited by a count of tries instead of the clock (a try takes 20 cycles at
+// least, more where the hardware suspends the thread): kernels with many waits, whose instructions would
+// otherwise be mostly these loops.
+__device__ __forceinline__ bool mbar_wait_warp_short(uint64_t* bar, uint32_t parity, volatile int* abort) {
+  bool ok = mbar_try_wait(bar, parity);
+#pragma unroll 1
+  for (uint32_t tries = 1u << 26; !ok && tries && !*abort; --tries) ok = mbar_try_wait(bar, parity);
+  return __all_sync(0xffffffffu, ok);
+}
+
 // True in one lane of a converged warp, the same lane every time.  The MMA issuers run as
 // a whole warp and put only the tcgen05 instructions under this predicate: descriptors,
 // TMEM addresses and loop state then stay warp-uniform, where the instructions take them,
