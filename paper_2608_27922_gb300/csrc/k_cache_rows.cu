@@ -88,6 +88,7 @@ struct Job {
   Mask m;
   Packed q, o;
   int G, max_rows;
+  uint32_t g_inverse;   // ceil(2^32 / G): i / G is the high half of i times it (i < 2^24)
   int unit;          // rows of a unit
   int part_rows;     // rows of a partial result
   float* parts;      // partial results, [part_rows][D + 4] each (outputs, then the logarithm of a row's sum): one of every
@@ -115,7 +116,7 @@ __device__ __forceinline__ Span span_of(const Job& j, int b) {
   x.n = q.n;
   x.len = q.len;
   if (q.n == 0) return x;
-  x.tiles = (q.n * j.G + j.unit - 1) / j.unit;
+  x.tiles = (q.n * j.G + j.unit - 1) >> (j.unit == 8 ? 3 : 4);
   x.stages = 1;
   const int p0 = q.len - q.n, pl = q.len - 1;
   if (pl < 0) return x;
@@ -130,6 +131,8 @@ __device__ __forceinline__ Span span_of(const Job& j, int b) {
   x.stages = max(1, x.ns + max(0, (x.end + KT - 1) / KT - x.w0));
   return x;
 }
+
+__device__ __forceinline__ int token_of(const Job& j, int i) { return j.G == 1 ? i : (int)__umulhi((uint32_t)i, j.g_inverse); }
 
 __device__ __forceinline__ int stages_of(const Job& j, const Span& x) { return x.tiles * j.c.H * x.stages; }
 
@@ -317,7 +320,7 @@ __device__ __forceinline__ void sum_parts(At at, int first, int n, int step, int
 template <int D>
 __device__ __forceinline__ void store_row(const Job& j, int h, int tile, int r0, int r, float l, const float (&o)[D / 32]) {
   const float inv = l == 0.f ? 0.f : 1.0f / l;
-  const int lane = threadIdx.x & 31, i = tile * j.unit + r, tok = i / j.G, hq = i - tok * j.G;
+  const int lane = threadIdx.x & 31, i = tile * j.unit + r, tok = token_of(j, i), hq = i - tok * j.G;
   __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + hq) * j.o.head + (int64_t)(r0 + tok) * j.o.row;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) dst[c * 32 + lane] = __float2bfloat16_rn(o[c] * inv);
@@ -436,7 +439,7 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
     uint32_t qb[NR][KS][2];
 #pragma unroll
     for (int u = 0; u < NR; ++u) {
-      const int r = gr + 8 * u, i = tile * UNIT + r, tok = i / j.G, hq = i - tok * j.G;
+      const int r = gr + 8 * u, i = tile * UNIT + r, tok = token_of(j, i), hq = i - tok * j.G;
       const bool on = r < rows;
       const uint32_t* src = reinterpret_cast<const uint32_t*>(
           static_cast<const __nv_bfloat16*>(j.q.p) + (int64_t)(h * j.G + hq) * j.q.head + (int64_t)(x.r0 + tok) * j.q.row);
@@ -453,7 +456,7 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
     for (int u = 0; u < NR; ++u)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int r = 8 * u + 2 * t + e, p = x.len - x.n + (tile * UNIT + r) / j.G;
+        const int r = 8 * u + 2 * t + e, p = x.len - x.n + token_of(j, tile * UNIT + r);
         end[u][e] = r < rows && p >= 0 ? visible_end(j.m, p, x.len) : 0;
         lo[u][e] = window_first(j.m, end[u][e]);
       }
@@ -820,7 +823,7 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
         const int r = 8 * u + 2 * t + e;
         if (r >= rows || (!whole && r >= j.part_rows)) continue;
         const float inv = l[u][e] == 0.f ? 0.f : E4M3 ? ex2(mrun[u][e] - lse[u][e]) / l[u][e] : 1.0f / l[u][e];
-        const int i = tile * UNIT + r, tok = i / j.G, hq = i - tok * j.G;
+        const int i = tile * UNIT + r, tok = token_of(j, i), hq = i - tok * j.G;
         __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + hq) * j.o.head + (int64_t)(x.r0 + tok) * j.o.row;
         float* pd = part + r * D;
         if (!whole && gr == 0) part[j.part_rows * D + r] = l[u][e] == 0.f ? -INFINITY : lse[u][e] + log2f(l[u][e]);
@@ -857,20 +860,22 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
     return tail || info[w].head_smem ? reinterpret_cast<const float*>(smem + w * L::RING)
                                      : j.parts + (int64_t)((int)blockIdx.x * per + w) * j.part_rows * (D + 4);
   };
+  // (a bit a warp: has a head, its head ends in it, has a tail)
+  const unsigned heads = __ballot_sync(0xffffffffu, lane < per && info[lane < per ? lane : 0].head);
+  const unsigned ending = __ballot_sync(0xffffffffu, lane < per && info[lane < per ? lane : 0].head_ends) & heads;
+  const unsigned tails = __ballot_sync(0xffffffffu, lane < per && info[lane < per ? lane : 0].tail);
   int open = -1;                          // the chain of a unit that goes on behind the CTA
   int todo = 0;                           // (chain, row) pairs so far: warps take them in turn
 #pragma unroll 1
-  for (int c = -1; c < per; ++c) {        // -1: the first warp's head
-    if (c < 0 ? !info[0].head : !info[c].tail) continue;
-    const Stretch& y = info[max(c, 0)];
+  for (unsigned left = (tails << 1) | (heads & 1u); left; left &= left - 1) {
+    const int c = __ffs(left) - 2, c0 = max(c, 0);   // -1: the first warp's head
+    const Stretch& y = info[c0];
     const int h = c < 0 ? y.hh : y.h, tile = c < 0 ? y.htile : y.tile;
     const int rows = min(c < 0 ? y.hrows : y.rows, j.part_rows), r0 = c < 0 ? y.hr0 : y.r0;
-    int n = 1;                            // parts
-    bool ends = c < 0 && y.head_ends;
-    while (!ends && max(c, 0) + n < per && info[max(c, 0) + n].head) {
-      ends = info[max(c, 0) + n].head_ends;
-      ++n;
-    }
+    // parts: up to the first warp behind whose head ends there, or before the first without a head
+    const int after = c < 0 ? 0 : c + 1, stop = __ffs((~heads | ending) >> after) - 1 + after;
+    const bool ends = stop < per && ((ending >> stop) & 1u);
+    const int n = min(stop, per) - c0 + (ends ? 1 : 0);
     if (c >= 0 && !ends) open = c;        // (one at most: the last chain)
     // rows in turn with the other chains' (a warp's first: warp - todo, modulo their number)
 #pragma unroll 1
@@ -994,7 +999,7 @@ cudaError_t launch_attend_rows(const Pool& c, const Maps& maps, const Seqs& s, c
   // call keeps its number: its replays, one after the other, each find the count cleared by the one before)
   static std::atomic<unsigned long long> calls{0};
   unsigned long long* const arrived = static_cast<unsigned long long*>(scratch);
-  const Job job{c, s, m, q, o, G, max_rows, unit_rows(G, max_rows), part_rows(G, max_rows), reinterpret_cast<float*>(arrived + MAX_CTAS), arrived,
+  const Job job{c, s, m, q, o, G, max_rows, (uint32_t)((0xffffffffull + G) / G), unit_rows(G, max_rows), part_rows(G, max_rows), reinterpret_cast<float*>(arrived + MAX_CTAS), arrived,
                 (calls.fetch_add(1) + 1) & 0xffffffffffffull};
   if (c.d == 128)
     return c.e4m3 ? launch_d<128, true>(maps, job, n_sm, st) : launch_d<128, false>(maps, job, n_sm, st);
