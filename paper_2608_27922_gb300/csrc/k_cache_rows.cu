@@ -157,39 +157,42 @@ __device__ __forceinline__ int total_stages(const Job& j, Span& first) {
   return (int)mine;
 }
 
-// Sequence that holds stage `at` of the range, and where its stages begin.  All lanes of a warp.
+// Sequence that holds stage `at` of the range, and where its stages begin.  All lanes of a warp; the search goes on from
+// the 32 sequences where the last one ended (stretches are walked upwards), this lane's of them in x.
+struct Cursor {
+  int b0, begin;
+  Span x;
+};
 struct Place {
   int b, begin;
   Span x;
 };
 template <int KT>
-__device__ __forceinline__ Place find(const Job& j, int at, const Span& first) {
+__device__ __forceinline__ Place find(const Job& j, int at, Cursor& c) {
   const int lane = threadIdx.x & 31;
-  int begin = 0;
-  for (int b0 = 0;; b0 += 32) {
-    const int b = b0 + lane;
-    Span x = first;
-    if (b0 > 0) x = b < j.s.n ? span_of<KT>(j, b) : Span{};
-    const int mine = stages_of(j, x);
+  for (;;) {
+    const int mine = stages_of(j, c.x);
     int incl = mine;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
-    const unsigned past = __ballot_sync(0xffffffffu, b < j.s.n && begin + incl > at);
-    if (past || b0 + 32 >= j.s.n) {
+    const unsigned past = __ballot_sync(0xffffffffu, c.begin + incl > at);
+    if (past || c.b0 + 32 >= j.s.n) {
       const int k = past ? __ffs(past) - 1 : 31;   // (there is one: `at` lies in the range)
       Place p;
-      p.b = min(b0 + k, j.s.n - 1);
-      p.begin = begin + __shfl_sync(0xffffffffu, incl - mine, k);
+      p.b = min(c.b0 + k, j.s.n - 1);
+      p.begin = c.begin + __shfl_sync(0xffffffffu, incl - mine, k);
       int* to = reinterpret_cast<int*>(&p.x);
-      const int* from = reinterpret_cast<const int*>(&x);
+      const int* from = reinterpret_cast<const int*>(&c.x);
 #pragma unroll
       for (int i = 0; i < (int)(sizeof(Span) / 4); ++i) to[i] = __shfl_sync(0xffffffffu, from[i], k);
       return p;
     }
-    begin += __shfl_sync(0xffffffffu, incl, 31);
+    c.begin += __shfl_sync(0xffffffffu, incl, 31);
+    c.b0 += 32;
+    c.x = c.b0 + lane < j.s.n ? span_of<KT>(j, c.b0 + lane) : Span{};
   }
 }
 
@@ -394,8 +397,8 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
 
   // The CTAs' stretches follow one another, a CTA's warps' too, so that a unit's parts are joined in the CTA
   // first; where there are few stages, few warps of every CTA have one.
-  Span first;
-  const int total = total_stages<KT>(j, first);
+  Cursor cursor{};
+  const int total = total_stages<KT>(j, cursor.x);
   const int per = min(WARPS, max(1, total / (MIN_STAGES * (int)gridDim.x)));   // warps at work
   const int workers = min(total, per * (int)gridDim.x);
   const int worker = (int)blockIdx.x * per + warp;
@@ -413,7 +416,7 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
 
   while (ok && at < stop) {
     // ---- the segment: stages [k0, k1) of a unit's list
-    const Place pl = find<KT>(j, at, first);
+    const Place pl = find<KT>(j, at, cursor);
     const Span& x = pl.x;
     const int unit = (int)((unsigned)(at - pl.begin) / (unsigned)x.stages), k0 = at - pl.begin - unit * x.stages;
     const int h = (int)((unsigned)unit / (unsigned)x.tiles), tile = unit - h * x.tiles;

@@ -236,7 +236,8 @@ __device__ __forceinline__ Plan make_plan(const Job& j, int ctas, Known& mine) {
   longest = __reduce_max_sync(0xffffffffu, longest);
   even = __all_sync(0xffffffffu, even && (most == 0 || most == longest));
   Plan p{units, units, 0, 0};
-  if (units == 0 || !j.cut) return p;
+  // (the choice below looks at every sequence in turn: many sequences are many units anyway)
+  if (units == 0 || !j.cut || units >= CUT_ROUNDS * ctas || (!even && j.s.n > 64)) return p;
   // lane: the longest unit in S = lane + 1 parts
   const int S = lane + 1, C = (int)((unsigned)(longest + S - 1) / (unsigned)S);
   const int rounds = (int)((unsigned)units / (unsigned)ctas), rest = units - rounds * ctas;
@@ -280,48 +281,55 @@ __device__ __forceinline__ Plan make_plan(const Job& j, int ctas, Known& mine) {
   return p;
 }
 
-// Item (or, with C = 0, unit) i -> its sequence and place; before: items of earlier sequences.  All lanes of one warp,
-// mine: sequence `lane`.
+// Item (or, with C = 0, unit) i -> its sequence and place; before: items of earlier sequences.  All lanes of one warp; the
+// search goes on from the 32 sequences where the last one ended (items are mostly taken in order), this lane's in k.
 struct Unit {
   int b, h, t, s, S, nu, before;
   Seq q;
 };
-__device__ __forceinline__ Unit find_unit(const Job& j, int i, int C, const Known& mine) {
+struct Cursor {
+  int b0, before;
+  Known k;
+};
+__device__ __forceinline__ Unit find_unit(const Job& j, int i, int C, Cursor& c) {
   const int lane = threadIdx.x & 31;
-  int before = 0;
-  for (int b0 = 0;; b0 += 32) {
-    Known k = mine;
-    if (b0 > 0) k = known(j, b0 + lane);
-    const int S = parts_of(k.last, C), here = k.nu * j.c.H * S;
+  if (i < c.before) {
+    c.b0 = c.before = 0;
+    c.k = known(j, lane);
+  }
+  for (;;) {
+    const int S = parts_of(c.k.last, C), here = c.k.nu * j.c.H * S;
     int incl = here;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
       const int v = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += v;
     }
-    const unsigned past = __ballot_sync(0xffffffffu, before + incl > i);
-    if (past || b0 + 32 >= j.s.n) {
+    const unsigned past = __ballot_sync(0xffffffffu, c.before + incl > i);
+    if (past || c.b0 + 32 >= j.s.n) {
       const int w = past ? __ffs(past) - 1 : 31;   // (i is below the sum of all)
       Unit r;
-      r.b = min(b0 + w, j.s.n - 1);
-      r.before = before + __shfl_sync(0xffffffffu, incl - here, w);
+      r.b = min(c.b0 + w, j.s.n - 1);
+      r.before = c.before + __shfl_sync(0xffffffffu, incl - here, w);
       r.S = __shfl_sync(0xffffffffu, S, w);
-      r.nu = max(1, __shfl_sync(0xffffffffu, k.nu, w));
-      r.q.r0 = __shfl_sync(0xffffffffu, k.q.r0, w);
-      r.q.n = __shfl_sync(0xffffffffu, k.q.n, w);
-      r.q.len = __shfl_sync(0xffffffffu, k.q.len, w);
+      r.nu = max(1, __shfl_sync(0xffffffffu, c.k.nu, w));
+      r.q.r0 = __shfl_sync(0xffffffffu, c.k.q.r0, w);
+      r.q.n = __shfl_sync(0xffffffffu, c.k.q.n, w);
+      r.q.len = __shfl_sync(0xffffffffu, c.k.q.len, w);
       const unsigned rem = (unsigned)(i - r.before), hs = rem / (unsigned)r.nu, h = r.S == 1 ? hs : hs / (unsigned)r.S;
       r.t = max(0, r.nu - 1 - (int)(rem - hs * r.nu));
       r.h = min((int)h, j.c.H - 1);
       r.s = (int)(hs - h * r.S);
       return r;
     }
-    before += __shfl_sync(0xffffffffu, incl, 31);
+    c.before += __shfl_sync(0xffffffffu, incl, 31);
+    c.b0 += 32;
+    c.k = known(j, c.b0 + lane);
   }
 }
 
 // Item i and its list; state 0 where it is an empty part.  (Its partial result's place is taken when it is handed out.)
-__device__ __forceinline__ Item make_item(const Job& j, const Plan& p, int i, const Known& mine, List& l) {
+__device__ __forceinline__ Item make_item(const Job& j, const Plan& p, int i, Cursor& cursor, List& l) {
   // (units of one length: part s of the R that are cut)
   int unit = i, s = 0, S = 1;
   if (p.C > 0 && p.whole >= 0 && i >= p.whole) {
@@ -330,7 +338,7 @@ __device__ __forceinline__ Item make_item(const Job& j, const Plan& p, int i, co
     unit = p.whole + k - s * R;
     S = MAX_CUT;
   }
-  const Unit u = find_unit(j, unit, p.whole < 0 ? p.C : 0, mine);
+  const Unit u = find_unit(j, unit, p.whole < 0 ? p.C : 0, cursor);
   if (p.whole < 0) {
     s = u.s;
     S = u.S;
@@ -355,9 +363,10 @@ __device__ __forceinline__ Item make_item(const Job& j, const Plan& p, int i, co
 }
 
 // ------------------------------------------------------------------ values that are not finite
-// Clears what is not finite in one bf16 row (128-byte swizzled panels); whether there was any.
+// Clears what is not finite in one bf16 row (128-byte swizzled panels), and says so in *met before it does: the other
+// query tile's products may meet the cleared row at once, and its outputs wait for nothing else.
 template <int D>
-__device__ __forceinline__ bool clear_row(uint8_t* tile, int row) {
+__device__ __forceinline__ void clear_row(uint8_t* tile, int row, volatile int* met, int item) {
   uint32_t any = 0;
 #pragma unroll
   for (int c = 0; c < D / 8; ++c) {
@@ -367,14 +376,15 @@ __device__ __forceinline__ bool clear_row(uint8_t* tile, int row) {
     any |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) |
            ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
   }
-  if ((any & 0x80008000u) == 0) return false;
+  if ((any & 0x80008000u) == 0) return;
+  *met = item;
+  __threadfence_block();
 #pragma unroll 1
   for (int c = 0; c < D / 2; ++c) {
     uint32_t* p = reinterpret_cast<uint32_t*>(tile + (c >> 5) * PANEL + row * 128 + ((((c >> 2) & 7) ^ (row & 7)) << 4)) + (c & 3);
     const uint32_t x = *p, bad = ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
     if (bad) *p = x & ~(((bad >> 15) & 0x00010001u) * 0xffffu);
   }
-  return true;
 }
 
 // The columns [c0, c0 + 32) in which row (position range [lo, end) and sinks) meets a NaN, +inf, -inf in the tiles
@@ -581,8 +591,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
     regs_lower<L::REGS_IO>();
     if (warp == 0) {
       // ---------------- producer: items; Q, then K(0), V(0), K(1), ..
-      Known mine;
-      const Plan plan = make_plan(j, gridDim.x, mine);
+      Cursor cursor{};
+      const Plan plan = make_plan(j, gridDim.x, cursor.k);
       if (blockIdx.x == 0 && lane == 0) *j.plan = make_int4(plan.C > 0 ? plan.units : 0, plan.C, plan.whole, 0);
       const int rows = min(j.c.page_len, BK), np = BK / rows;   // rows and boxes of a tile
       uint32_t tc = 0, nq = 0, ni = 0, cc = 0;
@@ -604,7 +614,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         List l{};
 #pragma unroll 1
         while (it < plan.items) {
-          x = make_item(j, plan, it, mine, l);
+          x = make_item(j, plan, it, cursor, l);
           if (x.state) break;
           ask();
           it = next();
@@ -858,7 +868,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         if (partial) {
           const uint32_t t = tc + (uint32_t)(i - x.i0);
           if (!(ok = mbar_wait_warp_short(v_full + t % L::NV, (t / L::NV) & 1, abort_flag))) break;
-          if ((!E4M3 || nan_rows[t % L::NV] != 0) && clear_row<D>(smem + L::V + (t % L::NV) * L::TB, r)) wild[ni & 1] = (int)ni + 1;
+          if (!E4M3 || nan_rows[t % L::NV] != 0) clear_row<D>(smem + L::V + (t % L::NV) * L::TB, r, wild + (ni & 1), (int)ni + 1);
           fence_async_smem();
         }
         if (!(ok = mbar_wait_warp_short(s_full + g, ns & 1, abort_flag))) break;
@@ -1051,7 +1061,8 @@ __global__ void __launch_bounds__(256) cache_merge(const __grid_constant__ Job j
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
     const Known mine = known(j, lane);
-    const Unit u = find_unit(j, unit, 0, mine);
+    Cursor cursor{0, 0, mine};
+    const Unit u = find_unit(j, unit, 0, cursor);
     int n = parts_of(tiles_at(j, u.q, u.t), p.y), at, step;   // the item of part 0, and from one to the next
     if (p.z >= 0) {
       at = unit;

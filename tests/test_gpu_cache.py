@@ -217,6 +217,97 @@ def test_large_scores(dkv, fmt, n):
     verify(dkv, c, 2, scale=0.003, rows={0, n - 1, n, 2 * n - 1})
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_far_pages(dkv, fmt):
+    """Pages whose place in the pool passes 2^31 elements: written, read and attended as near ones are."""
+    H, d, page = 8, 128, 256
+    n_pages = (1 << 31) // (H * page * d) + 40             # 2.2e9 elements of keys
+    cache = dkv.PagedCache(H, d, page, n_pages, fmt)
+    near = R.Case([(1, 700), (3, 300), (200, 500)], H, d, page, fmt, seed=9)
+    small, s0 = near.cache(dkv), near.device_seqs(dkv)
+    far = torch.arange(near.n_pages, device="cuda") + (n_pages - near.n_pages)
+    table = torch.where(s0.block_table >= 0, s0.block_table + (n_pages - near.n_pages), s0.block_table)
+    s1 = dkv.CacheSeqs(table, s0.seq_len, s0.row_start)
+    g = np.random.default_rng(0)
+    Q, K, V = (dev(R.bf16(g.standard_normal((H, near.rows, d)))) for _ in range(3))
+    view = lambda x: x.view(torch.uint8) if x.dtype == torch.float8_e4m3fn else x
+    for a, b in ((cache.k, small.k), (cache.v, small.v), (cache.k_scale, small.k_scale), (cache.v_scale, small.v_scale)):
+        if a is not None:
+            view(a)[far] = view(b)
+    for c, s in ((small, s0), (cache, s1)):
+        c.write(K, V, s)
+    first = dev(near.len - np.diff(near.row_start) - 100, torch.int32)
+    for a, b in zip(small.read(s0, first, near.rows), cache.read(s1, first, near.rows)):
+        assert torch.equal(a, b) and bool(a.any())
+    for most in (200, near.rows):
+        assert torch.equal(small.attend(Q, s0, max_rows=most), cache.attend(Q, s1, max_rows=most))
+    one = [dkv.CacheSeqs(s.block_table[:1].contiguous(), s.seq_len[:1].contiguous(), s.row_start[:2].contiguous())
+           for s in (s0, s1)]
+    assert torch.equal(small.attend(Q[:, :1], one[0], max_rows=1), cache.attend(Q[:, :1], one[1], max_rows=1))
+    assert not bool(cache.k[:8].view(torch.uint8 if fmt == "e4m3" else torch.bfloat16).any())   # nothing wrapped round
+    small.sync()
+    cache.sync()
+    cache.close()
+    small.close()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_scratch_of_any_content(dkv, fmt):
+    """The scratch comes uncleared: whatever it holds, also what another call left in it, the outputs keep their bits
+    (single tokens and chunks that are cut into parts, in turn in the same memory)."""
+    import ctypes
+    L = dkv.lib()
+    H, Hq, d = 2, 4, 128
+    c = R.Case([(1, 9000), (200, 6000)], H, d, 64, fmt, seed=4)
+    cache = c.cache(dkv)
+    t = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    both = c.device_seqs(dkv)
+    calls = []
+    for rows, start, b, n in ((1, [0, 1], 0, 1), (200, [0, 200], 1, 200), (201, [0, 1, 201], None, 200)):
+        s = both if b is None else dkv.CacheSeqs(both.block_table[b:b + 1].contiguous(), both.seq_len[b:b + 1].contiguous(), t(start))
+        calls.append((rows, s, n))
+    Q = dev(R.bf16(np.random.default_rng(1).standard_normal((Hq, 201, d))))
+    size = max(int(L.dkv_cache_attend_scratch_size(cache.handle, s.n_seq, Hq, rows, n)) for rows, s, n in calls)
+    scratch = torch.empty(size, dtype=torch.uint8, device="cuda")
+    stream = torch.cuda.current_stream().cuda_stream
+
+    def run(rows, s, n):
+        q = Q[:, :rows].contiguous()
+        out = torch.full_like(q, 9.0)
+        how = dkv.dkv_cache_attend_t(0.0, 0, 0, 1, n)
+        st = L.dkv_cache_attend(cache.handle, s._ref, q.data_ptr(), Hq, rows, rows * d, d, out.data_ptr(), rows * d, d,
+                                ctypes.byref(how), scratch.data_ptr(), size, stream)
+        assert st == 0
+        return out
+
+    want = None
+    for fill in (0, 255, 1, None, None, 127):
+        if fill is not None:
+            scratch.fill_(fill)
+        got = [run(*x) for x in calls]
+        torch.cuda.synchronize()
+        if want is None:
+            want = got
+            ref = R.attend(c, Q.double().cpu().numpy(), rows={0, 1, 100, 200})
+            R.check(got[2], ref)
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), fill
+    cache.sync()
+    cache.close()
+
+
+@pytest.mark.parametrize("n", [1, 40])
+def test_many_sequences(dkv, n):
+    """More sequences than a warp's lanes, lengths of all kinds, some without tokens or positions."""
+    g = np.random.default_rng(n)
+    seqs = []
+    for b in range(150):
+        L = int(g.integers(0, 300)) if b % 7 else 0
+        seqs.append((int(g.integers(0, n + 1)), L))
+    c = R.Case(seqs, 1, 64, 16, "e4m3", seed=1)
+    verify(dkv, c, 2, heads=[1], rows=set(range(0, c.rows, 1 + c.rows // 90)), window=100, sinks=9, max_rows=n)
+    verify(dkv, c, 2, heads=[0], rows=set(range(0, c.rows, 1 + c.rows // 90)), max_rows=n)
+
+
 @pytest.mark.parametrize("n", [1, 150])
 @pytest.mark.parametrize("qs,ks", [(0, 0), (90, -90), (-90, 90), (-100, 60)])
 def test_row_magnitudes(dkv, n, qs, ks):
