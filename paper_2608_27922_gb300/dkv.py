@@ -575,7 +575,8 @@ class PagedCache:
                                           ctypes.byref(bufs)), "dkv_cache_create")
         self.handle = h.value
         self._plans: Dict[tuple, tuple] = {}
-        self._attend = lib().dkv_cache_attend
+        L = lib()
+        self._write, self._read, self._attend = L.dkv_cache_write, L.dkv_cache_read, L.dkv_cache_attend
 
     def close(self):
         if getattr(self, "handle", None):
@@ -620,24 +621,28 @@ class PagedCache:
         rows = K.shape[1]
         k, v = self._packed(K, self.H, rows, "K"), self._packed(V, self.H, rows, "V")
         s, _ = self._on(stream)
-        _check(lib().dkv_cache_write(self.handle, self._seqs(seqs), K.data_ptr(), V.data_ptr(), rows, k[0], k[1], v[0],
-                                     v[1], s), "dkv_cache_write")
+        st = self._write(self.handle, self._seqs(seqs), K.data_ptr(), V.data_ptr(), rows, k[0], k[1], v[0], v[1], s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_write")
 
     def read(self, seqs: CacheSeqs, first: torch.Tensor, rows: int, out: Optional[Tuple[torch.Tensor, torch.Tensor]] = None,
              stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """Positions first[b], first[b] + 1, .. of every sequence as rows row_start[b] .. of K, V
         [H][rows][d]; positions that a sequence does not hold are zeros."""
-        if (first.dtype != torch.int32 or tuple(first.shape) != (seqs.n_seq,) or not first.is_contiguous()
-                or first.device != self.device):
+        if first.dtype != torch.int32 or first.shape != (seqs.n_seq,) or not first.is_contiguous() or first.device != self.device:
             raise ValueError(f"first: expected contiguous {torch.int32} {(seqs.n_seq,)} on {self.device}")
         s, ctx = self._on(stream)
-        if out is not None:
-            K, V = out
+        if out is None:
+            shape = (self.H, rows, self.d)
+            K, V = self._new(ctx, shape, torch.bfloat16), self._new(ctx, shape, torch.bfloat16)
+            k = v = (rows * self.d, self.d)
         else:
-            K, V = (self._new(ctx, (self.H, rows, self.d), torch.bfloat16) for _ in range(2))
-        k, v = self._packed(K, self.H, rows, "K"), self._packed(V, self.H, rows, "V")
-        _check(lib().dkv_cache_read(self.handle, self._seqs(seqs), first.data_ptr(), K.data_ptr(), V.data_ptr(), rows,
-                                    k[0], k[1], v[0], v[1], s), "dkv_cache_read")
+            K, V = out
+            k, v = self._packed(K, self.H, rows, "K"), self._packed(V, self.H, rows, "V")
+        st = self._read(self.handle, self._seqs(seqs), first.data_ptr(), K.data_ptr(), V.data_ptr(), rows, k[0], k[1], v[0],
+                        v[1], s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_read")
         return K, V
 
     def attend(self, Q: torch.Tensor, seqs: CacheSeqs, window: int = 0, sinks: int = 0, block: int = 1,
