@@ -50,6 +50,7 @@ constexpr int MAX_CTAS = 152;            // persistent CTAs (the SMs of the GPU)
 constexpr int CUT_ROUNDS = 4;            // this many units a CTA, or more, are not cut: little is left to even out
 constexpr int MAX_PARTS = 4 * MAX_CTAS;  // partial results
 constexpr int MAX_ITEMS = 16 * MAX_CTAS; // items of a call that cuts units
+constexpr unsigned CALLS = 0xff800000u;   // the calls' numbers are this and 23 bits more: in the upper half of a word a NaN as bf16, fp32
 constexpr int MAX_CUT = 32;              // parts of one unit
 constexpr int MIN_PART = 4;              // key tiles of a part, at least
 // What an item costs beside its key tiles, a part (which stores its outputs in 32 bits) more than that, and the joining of
@@ -89,7 +90,7 @@ struct Job {
   int cut;                     // units may be cut: cache_merge follows
   int wide;                    // every output row is 32-byte aligned
   unsigned long long call;     // the call's number
-  unsigned long long* count;   // [3] items taken beside each CTA's first, CTAs done, partial results: call << 24 | count (see take)
+  unsigned long long* count;   // [3] items taken beside each CTA's first, CTAs done, partial results: call << 32 | count (see take)
   int4* plan;                  // {units (0: none is cut), tiles of a part, whole ones, -}, for cache_merge
   int* slot;                   // [MAX_ITEMS] place of an item's partial result
   float* parts;                // [MAX_PARTS][(D + 1) * 256]
@@ -158,19 +159,19 @@ __device__ __forceinline__ List list_of(const Mask& m, int tokens, int p0, int l
 }
 
 // ------------------------------------------------------------------ the items
-// A count in scratch memory that nobody has cleared: call << 24 | count once somebody has put that there.  One more;
+// A count in scratch memory that nobody has cleared: call << 32 | count once somebody has put that there.  One more;
 // the count before it.
 __device__ __forceinline__ void begin_count(unsigned long long* at, unsigned long long call) {
   const unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(at);
-  if ((old >> 24) != call) atomicCAS(at, old, call << 24);
+  if ((old >> 32) != call) atomicCAS(at, old, call << 32);
 }
 __device__ __forceinline__ int taken_as(unsigned long long* at, unsigned long long call, unsigned long long old) {   // (old: of the addition)
   for (;; old = atomicAdd(at, 1ull)) {
-    if ((old >> 24) == call) return (int)(old & 0xffffffu);
+    if ((old >> 32) == call) return (int)(old & 0x7fffffffu);
     // what was added to was no count of this call's yet: put it there, or see that it is
     old = *reinterpret_cast<volatile unsigned long long*>(at);
-    while ((old >> 24) != call) {
-      const unsigned long long got = atomicCAS(at, old, call << 24);
+    while ((old >> 32) != call) {
+      const unsigned long long got = atomicCAS(at, old, call << 32);
       if (got == old) break;
       old = got;
     }
@@ -1167,6 +1168,8 @@ cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, con
                              int max_rows, const Mask& m, void* scratch, cudaStream_t st) {
   const int G = Hq / c.H, TQ = BQ / G, n_sm = std::min(sm_count(), MAX_CTAS);
   if (n_sm <= 0) return cudaErrorInvalidDevice;
+  // items are counted in 31 bits (only outputs whose rows overlap could make more)
+  if ((int64_t)c.H * (s.rows / (2 * TQ) + s.n) >= (1ll << 31) - 4096) return cudaErrorInvalidValue;
   CUtensorMap mq;
   const int64_t dim[4] = {c.d, G, s.rows, c.H};
   const int64_t head = q.head ? q.head : c.d, row = q.row ? q.row : c.d;   // (one head or row: any stride)
@@ -1174,13 +1177,14 @@ cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, con
   const int box[4] = {64, G, TQ, 1};
   if (!make_map_4d(&mq, q.p, 2, dim, stride, box, 128)) return cudaErrorInvalidValue;
   // numbers the calls, so that what another call left in the same memory is not taken for a count of this one's (a
-  // captured call keeps its number: its replays, one after the other, each find the counts cleared by the one before)
-  static std::atomic<unsigned long long> calls{0};
+  // captured call keeps its number: its replays, one after the other, each find the counts cleared by the one before);
+  // no ordinary contents of the memory, small integers above all, pass for one
+  static std::atomic<unsigned> calls{0};
   char* const at = static_cast<char*>(scratch);
   // (several sequences make more units than one with all their rows)
   const bool cut = (int64_t)c.H * ((s.rows + 2 * TQ - 1) / (2 * TQ)) < CUT_ROUNDS * n_sm;
   const Job job{c, s, m, o, G, TQ, max_rows, cut ? 1 : 0,
-                (uintptr_t)o.p % 32 == 0 && o.head % 16 == 0 && o.row % 16 == 0, (calls.fetch_add(1) + 1) & 0xffffffffffull, reinterpret_cast<unsigned long long*>(at),
+                (uintptr_t)o.p % 32 == 0 && o.head % 16 == 0 && o.row % 16 == 0, CALLS | (calls.fetch_add(1) & ~CALLS), reinterpret_cast<unsigned long long*>(at),
                 reinterpret_cast<int4*>(at + 64), reinterpret_cast<int*>(at + 256),
                 reinterpret_cast<float*>(at + 256 + sizeof(int) * MAX_ITEMS)};
   if (c.d == 128)

@@ -1,5 +1,8 @@
 """The paged cache on the GPU: write, read and attend against plain 64-bit arithmetic (cache_ref.py)."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -8,6 +11,7 @@ import torch
 import cache_ref as R
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -293,6 +297,42 @@ def test_scratch_of_any_content(dkv, fmt):
         assert all(torch.equal(a, b) for a, b in zip(got, want)), fill
     cache.sync()
     cache.close()
+
+
+@pytest.mark.parametrize("rows", [1, 200])
+def test_scratch_of_small_integers(dkv, rows):
+    """The first attention of a process, its scratch full of words that are 1 in their upper 48 or 32 bits and in their
+    lower ones: a call's number and a count there would be just that, were the numbers to begin at 1."""
+    code = f"""
+import ctypes, sys, torch
+sys.path.insert(0, {str(ROOT)!r})
+from paper_2608_27922_gb300 import dkv
+H, d, n, rows = 2, 128, 6000, {rows}
+cache = dkv.PagedCache(H, d, 64, 94, "bf16")
+t = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+seqs = dkv.CacheSeqs(torch.arange(94, dtype=torch.int32, device="cuda")[None], t([n]), t([0, n]))
+torch.manual_seed(0)
+K, V, Q = (torch.randn(H, n, d, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+cache.write(K, V, seqs)
+seqs = dkv.CacheSeqs(seqs.block_table, seqs.seq_len, t([0, rows]))
+Q = Q[:, :rows].contiguous()
+L = dkv.lib()
+size = int(L.dkv_cache_attend_scratch_size(cache.handle, 1, H, rows, rows))
+scratch = torch.empty(size // 8, dtype=torch.int64, device="cuda")
+got = []
+for fill in ((1 << (16 if rows == 1 else 32)) + 1, 0):
+    scratch.fill_(fill)
+    out = torch.full_like(Q, 9.0)
+    how = dkv.dkv_cache_attend_t(0.0, 0, 0, 1, rows)
+    assert L.dkv_cache_attend(cache.handle, seqs._ref, Q.data_ptr(), H, rows, rows * d, d, out.data_ptr(), rows * d, d,
+                              ctypes.byref(how), scratch.data_ptr(), size, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    got.append(out)
+cache.sync()
+assert torch.equal(*got) and not bool((got[0] == 9.0).all())
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
 
 
 @pytest.mark.parametrize("n", [1, 40])
