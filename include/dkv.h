@@ -458,8 +458,9 @@ dkv_status_t dkv_candidate_order_noalloc(const void* K_bank, const float* base, 
  * work, so a captured call follows what they hold when it is replayed.
  *
  * A row_start that decreases or passes the call's rows, a length above max_pages * page_len,
- * a page outside [0, n_pages) in a touched place, or more than max_rows tokens in one
- * sequence set the sticky error word (DKV_ERR_DEVICE, see dkv_cache_sync); the call
+ * a page outside [0, n_pages) in a touched place, more than max_rows tokens in one
+ * sequence, or sequences that together see more than 2^34 positions in an attend call of few
+ * rows (counted once a key head) set the sticky error word (DKV_ERR_DEVICE, see dkv_cache_sync); the call
  * stays inside its buffers, and what it does for the sequences at fault is unspecified.
  *
  * Packed tensors are [heads][rows][d] bf16 with any strides (in elements) between heads and
@@ -477,7 +478,9 @@ typedef struct dkv_cache_s* dkv_cache_t;
  * max |x| <= 448 2^e, 0 for a row of zeros, and code = x 2^-e to nearest, ties to even (a
  * code that would stand for 2^128, more than bf16 holds, is the one below).  A row that
  * holds a NaN or an infinity gets the byte 255 and reads back as NaN in all d places.  code 2^e
- * is exact in bf16, so reading back and attending see the same numbers.                  */
+ * is exact in bf16, so reading back and attending see the same numbers.  (Pages filled by
+ * other means hold such numbers too: the codes 0x7f and 0xff only in rows of byte 255, and
+ * no scale byte below 17 or from 248 to 254; what others give is unspecified.)           */
 typedef enum { DKV_CACHE_BF16 = 0, DKV_CACHE_E4M3 = 1 } dkv_cache_format_t;
 
 typedef struct {

@@ -259,7 +259,7 @@ const char* dkv_status_str(dkv_status_t s) {
   return "unknown status";
 }
 
-int32_t dkv_version(void) { return 200; }   // 0.2.0: dkv_params_t.descriptor, admit_rope
+int32_t dkv_version(void) { return 300; }   // 0.3.0: the paged cache (dkv_cache_*)
 
 dkv_status_t dkv_params_default(dkv_params_t* out, int32_t d) {
   if (!out || d <= 0) return DKV_ERR_ARG;

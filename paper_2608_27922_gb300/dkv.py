@@ -540,7 +540,8 @@ class PagedCache:
     """Keys and values of H heads in pages of page_len positions, bf16 or quantised to e4m3
     ("bf16" / "e4m3"): allocates the pages with torch, or takes them (k, v and, for e4m3, k_scale,
     v_scale), and drives the C ABI.  Packed tensors are [heads][rows][d] bf16 with any strides that
-    are multiples of 8 between heads and rows.  All methods enqueue on the current (or given)
+    are multiples of 8 between heads and rows; rows behind the last sequence's are not written, so in an
+    output that a method allocates itself they hold nothing in particular.  All methods enqueue on the current (or given)
     stream; a call on another stream than the one its tensors were made on is ordered by the caller."""
 
     def __init__(self, H: int, d: int, page_len: int, n_pages: int, fmt: str = "bf16", device="cuda",
