@@ -239,6 +239,13 @@ __device__ __forceinline__ Plan make_plan(const Job& j, int ctas, Known& mine) {
   Plan p{units, units, 0, 0};
   // (the choice below looks at every sequence in turn: many sequences are many units anyway)
   if (units == 0 || !j.cut || units >= CUT_ROUNDS * ctas || (!even && j.s.n > 64)) return p;
+  // (uneven units:) no cut gains more than its joining costs
+  if (!even) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
+    const float least = (tiles + (float)(units * ITEM_TILES)) / ctas;
+    if (fmaxf((float)(longest + ITEM_TILES), least + 0.35f * longest) <= least + 0.35f * MIN_PART + JOIN_TILES) return p;
+  }
   // lane: the longest unit in S = lane + 1 parts
   const int S = lane + 1, C = (int)((unsigned)(longest + S - 1) / (unsigned)S);
   const int rounds = (int)((unsigned)units / (unsigned)ctas), rest = units - rounds * ctas;
@@ -253,8 +260,6 @@ __device__ __forceinline__ Plan make_plan(const Job& j, int ctas, Known& mine) {
       est += S == 1 ? (float)(longest + ITEM_TILES)
                     : (float)((rest * S + ctas - 1) / ctas) * (C + ITEM_TILES + PART_TILES) + JOIN_TILES;
   } else {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) tiles += __shfl_xor_sync(0xffffffffu, tiles, o);
     int parts = 0, most_parts = 0;
 #pragma unroll 1
     for (int b = 0; b < j.s.n; ++b) {
@@ -431,6 +436,15 @@ __device__ __forceinline__ void store32(void* p, const uint32_t* w) {
                : "memory");
 }
 
+// 16 bytes to shared memory (the first `bytes` of them copied, the rest zeros); copies_arrive: an arrival at bar when
+// the thread's copies so far are there.
+__device__ __forceinline__ void copy16(void* to, const void* from, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_arrive(uint64_t* bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+}
+
 // Bits k < x.
 __device__ __forceinline__ uint32_t below(int x) { return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; }
 
@@ -547,7 +561,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(k_full + i, E4M3 ? L::CONV : 1);
       mbar_init(k_empty + i, 1);
-      mbar_init(c_full + i, 1);
+      mbar_init(c_full + i, 1 + 32);   // the codes', and each of the producer's lanes for its scales
       mbar_init(c_empty + i, E4M3 ? L::CONV : 1);
       mbar_init(s_full + i, 1);
       mbar_init(p_full + i, 4);
@@ -644,6 +658,14 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
           it = next();
           continue;
         }
+        // pages of the list's tiles, 32 boxes at a time with the lanes: box (i - base) np + .. of tile i
+        const int np_log2 = __ffs(np) - 1, batch = 32 >> np_log2;
+        auto entry_of = [&](int first) -> int {
+          const int i = first + (lane >> np_log2), k0 = tile_of(x, i) * BK + (lane & (np - 1)) * rows;
+          return i < x.i1 && k0 < l.end && (k0 + rows > l.lo || k0 < l.sk)
+                     ? __ldg(j.s.table + (int64_t)x.b * j.s.max_pages + (k0 >> j.c.page_log2)) : 0;
+        };
+        int base = x.i0, pages = entry_of(base), pages_next = entry_of(base + batch);
         if (nq > 0 && !(ok = mbar_wait_warp_short(q_empty, (nq - 1) & 1, abort_flag))) break;
         ++nq;
         if (lane == 0) {
@@ -654,14 +676,6 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
               tma_load_4d(smem + L::Q + g * L::TB + p * PANEL, &tmQ, q_full, p * 64, 0, x.r0 + g * j.TQ, x.h);
         }
         __syncwarp();
-        // pages of the list's tiles, 32 boxes at a time with the lanes: box (i - base) np + .. of tile i
-        const int np_log2 = __ffs(np) - 1, batch = 32 >> np_log2;
-        auto entry_of = [&](int first) -> int {
-          const int i = first + (lane >> np_log2), k0 = tile_of(x, i) * BK + (lane & (np - 1)) * rows;
-          return i < x.i1 && k0 < l.end && (k0 + rows > l.lo || k0 < l.sk)
-                     ? __ldg(j.s.table + (int64_t)x.b * j.s.max_pages + (k0 >> j.c.page_log2)) : 0;
-        };
-        int base = x.i0, pages = entry_of(base), pages_next = entry_of(base + batch);
         // one tile of K or V: a lane a box
         auto load = [&](bool is_k, int i) -> bool {
           const int kt = tile_of(x, i);
@@ -686,15 +700,18 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
             const uint32_t c = cc++;
             uint64_t* bar = c_full + (c & 1);
             if (c >= 2 && !mbar_wait_warp_short(c_empty + (c & 1), ((c >> 1) & 1) ^ 1, abort_flag)) return false;
-            const unsigned named = __ballot_sync(0xffffffffu, page < j.c.n_pages);
-            if (lane == 0) mbar_arrive_expect_tx(bar, BK * D + __popc(named) * rows);
+            if (lane == 0) mbar_arrive_expect_tx(bar, BK * D);
             __syncwarp();
-            if (box < np) {
+            if (box < np)
               tma_load_4d(smem + L::CODES + (c & 1) * 128 * D + box * rows * D, is_k ? &tmK : &tmV, bar, 0, slot, x.h, page);
-              if (page < j.c.n_pages)
-                bulk_load(smem + L::SCALES + (c & 1) * 128 + box * rows,
-                          (is_k ? j.c.ks : j.c.vs) + (((int64_t)page * j.c.H + x.h) << j.c.page_log2) + slot, rows, bar);
-            }
+            // the scales, 16 bytes a lane (zeros where the page is nobody's)
+            page = __shfl_sync(0xffffffffu, page, (lane * 16) >> (7 - np_log2) & 31);
+            if (lane < 8)
+              copy16(smem + L::SCALES + (c & 1) * 128 + lane * 16,
+                     (is_k ? j.c.ks : j.c.vs) + (page < j.c.n_pages
+                         ? (((int64_t)page * j.c.H + x.h) << j.c.page_log2) + ((kt * BK + lane * 16) & (j.c.page_len - 1)) : 0),
+                     page < j.c.n_pages ? 16 : 0);
+            copies_arrive(bar);
           } else {
             const uint32_t nb = is_k ? L::NK : L::NV, sl = t % nb;
             uint64_t* bar = (is_k ? k_full : v_full) + sl;
