@@ -335,6 +335,21 @@ assert torch.equal(*got) and not bool((got[0] == 9.0).all())
     assert r.returncode == 0, r.stderr[-2000:]
 
 
+def test_whole_units_in_either_order(dkv):
+    """More units than are cut, of two short sequences (round the heads) and one of more than 192 MB of keys and values
+    (head by head) between them."""
+    seqs = [(90, 600), (512, 9900), (33, 2000)]
+    c = R.Case(seqs, 40, 128, 256, "bf16", seed=3)
+    cache = c.cache(dkv)
+    Q = R.bf16(np.random.default_rng(5).standard_normal((320, c.rows, 128)))
+    out = cache.attend(dev(Q), c.device_seqs(dkv), max_rows=512)
+    cache.sync()
+    rows = {0, 31, 32, 89, 90, 91, 345, 601, 602, 634}
+    R.check(out, R.attend(c, Q, heads=[0, 7, 8, 163, 319], rows=rows))
+    assert bool(out.isfinite().all())
+    cache.close()
+
+
 @pytest.mark.parametrize("n", [1, 40])
 def test_many_sequences(dkv, n):
     """More sequences than a warp's lanes, lengths of all kinds, some without tokens or positions."""
