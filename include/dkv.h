@@ -544,7 +544,7 @@ size_t dkv_cache_attend_scratch_size(dkv_cache_t cache, int32_t n_seq, int32_t H
  *   scratch : device, 256-byte aligned, >= dkv_cache_attend_scratch_size(); in use until the
  *             call's work has completed.
  * A token that sees no position (a negative position of its own, an empty sequence) gets
- * zeros.  Rows from row_start[n_seq] on are left as they were.  What lies in places that a
+ * zeros, and so does one whose scores are all -infinity.  Rows from row_start[n_seq] on are left as they were.  What lies in places that a
  * token does not see, NaN and infinities too, does not reach its output.  Scores, sums and
  * outputs are held in fp32; the weights are rounded to bf16 before they meet the values.
  * The order of the sums follows from the sizes and arrays of the call and from the device.  */

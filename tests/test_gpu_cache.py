@@ -351,6 +351,33 @@ def test_whole_units_in_either_order(dkv):
 
 
 @pytest.mark.parametrize("n", [1, 40])
+def test_scores_of_minus_infinity(dkv, n):
+    """Keys whose scores are -infinity have no weight; a token that sees no other gets zeros.  Tolerance: the weights' and
+    the output's rounding to bf16, and 2^-10 for the scores (128 products and sums of 32 bits, sum |q k| scale < 40)."""
+    H, d, L = 2, 128, 5000
+    g = np.random.default_rng(2)
+    K, V, Q = (R.bf16(g.standard_normal((H, m, d))) for m in (L, L, n))
+    Q[:, :, 0] = 1.0
+    t = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    for hidden in (3000, L):
+        K[:, :hidden, 0] = -np.inf
+        cache = dkv.PagedCache(H, d, 16, -(-L // 16), "bf16")
+        table = torch.arange(cache.n_pages, dtype=torch.int32, device="cuda")[None]
+        cache.write(dev(K), dev(V), dkv.CacheSeqs(table, t([L]), t([0, L])))
+        out = cache.attend(dev(Q), dkv.CacheSeqs(table, t([L]), t([0, n])), block=0).double().cpu().numpy()
+        cache.sync()
+        cache.close()
+        if hidden == L:
+            assert not out.any()
+            continue
+        s = Q @ K[:, hidden:].transpose(0, 2, 1) / math.sqrt(d)
+        w = np.exp(s - s.max(-1, keepdims=True))
+        w /= w.sum(-1, keepdims=True)
+        o, v = w @ V[:, hidden:], w @ np.abs(V[:, hidden:])
+        assert (np.abs(out - o) <= v * (2.0 ** -8 + 2.0 ** -10) + 2.0 ** -8 * np.abs(o) + 1e-30).all()
+
+
+@pytest.mark.parametrize("n", [1, 40])
 def test_many_sequences(dkv, n):
     """More sequences than a warp's lanes, lengths of all kinds, some without tokens or positions."""
     g = np.random.default_rng(n)
