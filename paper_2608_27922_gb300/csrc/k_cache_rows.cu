@@ -54,7 +54,7 @@ constexpr int MAX_CTAS = 152;
 constexpr int MAX_WARPS = 12;
 constexpr int WORKERS = MAX_WARPS * MAX_CTAS;
 constexpr float RESCALE_LOG2 = 8.0f;
-constexpr int MIN_STAGES = 1;    // stages of a warp, at least
+constexpr int MIN_STAGES = 1;    // stages of a warp, at least (one token over 1,561 positions: with 1 11 us, 2 15, 4 19)
 constexpr unsigned long long FIRST_CALL = 0xffb700000001ull;   // in the upper 48 bits of a word: a NaN as bf16, fp32
 
 // What a worker's stretch leaves unfinished.

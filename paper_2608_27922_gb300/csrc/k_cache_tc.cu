@@ -52,7 +52,9 @@ constexpr int PANEL = 128 * 128;         // bytes of a 64-column panel of 128 ro
 constexpr uint32_t TMEM_COLS = 512;      // S_0 [0,128), O_0 [128,256), S_1 [256,384), O_1 [384,512)
 constexpr float RESCALE_LOG2 = 8.0f;
 constexpr int MAX_CTAS = 152;            // persistent CTAs (the SMs of the GPU): sizes the scratch
-constexpr int CUT_ROUNDS = 4;            // this many units a CTA, or more, are not cut: little is left to even out
+// This many units a CTA, or more, are not cut: little is left to even out (prompts with 5.5 a CTA 257 us, cut 260; with 3
+// a CTA 167 cut and 164 not, but units of one length would then go 3 rounds where 2.1 are due).
+constexpr int CUT_ROUNDS = 4;
 constexpr int MAX_PARTS = 4 * MAX_CTAS;  // partial results
 constexpr int MAX_ITEMS = 16 * MAX_CTAS; // items of a call that cuts units
 constexpr unsigned CALLS = 0xff800000u;   // the calls' numbers are this and 23 bits more: in the upper half of a word a NaN as bf16, fp32
@@ -62,7 +64,7 @@ constexpr unsigned CALLS = 0xff800000u;   // the calls' numbers are this and 23 
 // 2,102 against 2,058.
 constexpr int64_t NEAR = 192 << 20;
 constexpr int MAX_CUT = 32;              // parts of one unit
-constexpr int MIN_PART = 4;              // key tiles of a part, at least
+constexpr int MIN_PART = 4;              // key tiles of a part, at least (256 tokens over 2,256 keys, 8 heads: with 4 27 us, 2 28, 8 32)
 // What an item costs beside its key tiles, a part (which stores its outputs in 32 bits) more than that, and the joining of
 // parts, in key tiles (1.6 us each at two query tiles of 128 dimensions)
 constexpr int ITEM_TILES = 2, PART_TILES = 2, JOIN_TILES = 6;
