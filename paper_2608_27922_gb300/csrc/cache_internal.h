@@ -45,7 +45,7 @@ struct Mask {
 };
 inline uint64_t inverse_of(int block) { return block >= 2 ? ~(uint64_t)0 / (uint64_t)block + 1 : 0; }
 
-enum : int { SITE_ROWS = 1, SITE_LEN = 2, SITE_PAGE = 3, SITE_CHUNK = 4, SITE_WAIT = 400 };
+enum : int { SITE_ROWS = 1, SITE_LEN = 2, SITE_PAGE = 3, SITE_CHUNK = 4, SITE_PART = 5, SITE_WAIT = 400 };
 
 #ifdef __CUDACC__
 // (The index arithmetic below also compiles for the host, where a test walks its bounds.)

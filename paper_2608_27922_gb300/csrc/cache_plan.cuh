@@ -413,6 +413,14 @@ __host__ __device__ __forceinline__ Joined joined(const Job& j, const int4& p, i
   return x;
 }
 
+// Place of item i's partial result, -1: none.  (Where a CTA gave up waiting, its items have stored no place, and what
+// the uncleared scratch holds in its stead is any number.)
+__host__ __device__ __forceinline__ int slot_of(const int* slot, int i) {
+  if (i < 0 || i >= MAX_ITEMS) return -1;
+  const int at = slot[i];
+  return at >= 0 && at < MAX_PARTS ? at : -1;
+}
+
 }  // namespace chunk
 }  // namespace cache
 }  // namespace dkv

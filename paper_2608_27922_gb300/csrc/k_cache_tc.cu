@@ -841,12 +841,16 @@ __global__ void __launch_bounds__(256) cache_merge(const __grid_constant__ Job j
   __shared__ int slots[MAX_CUT];
   __shared__ Unit su;
   __shared__ int sS;
-  for (int unit = max(p.z, 0) + blockIdx.x; unit < p.x; unit += gridDim.x) {   // uniform
+  const int units = min(p.x, CUT_ROUNDS * (int)gridDim.x);   // (no call that cuts has more)
+  for (int unit = max(p.z, 0) + blockIdx.x; unit < units; unit += gridDim.x) {   // uniform
   __syncthreads();
   if (threadIdx.x < 32) {
     const int lane = threadIdx.x;
     const Joined x = joined(j, p, unit);
-    if (x.n > 1 && lane < x.n) slots[lane] = j.slot[x.at + lane * x.step];
+    if (x.n > 1 && lane < x.n) {
+      slots[lane] = slot_of(j.slot, x.at + lane * x.step);
+      if (slots[lane] < 0) fail(j.c.status, DEV_INCONSISTENT, SITE_PART);
+    }
     if (lane == 0) {
       su = x.u;
       sS = x.n;
@@ -856,7 +860,8 @@ __global__ void __launch_bounds__(256) cache_merge(const __grid_constant__ Job j
   const int S = sS, row0 = blockIdx.y * MG_ROWS;
   if (S < 2) continue;
   auto part = [&](int s) { return j.parts + (int64_t)slots[s] * (256 * (D + 1)); };
-  for (int e = threadIdx.x; e < S * MG_ROWS; e += 256) lse[e / MG_ROWS][e % MG_ROWS] = part(e / MG_ROWS)[256 * D + row0 + e % MG_ROWS];
+  for (int e = threadIdx.x; e < S * MG_ROWS; e += 256)
+    lse[e / MG_ROWS][e % MG_ROWS] = slots[e / MG_ROWS] < 0 ? -INFINITY : part(e / MG_ROWS)[256 * D + row0 + e % MG_ROWS];
   __syncthreads();
   const Unit u = su;
   const int rl = threadIdx.x % MG_ROWS, row = row0 + rl, q = threadIdx.x / MG_ROWS;   // 8 column groups

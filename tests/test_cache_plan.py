@@ -199,9 +199,22 @@ static int check(const std::vector<std::pair<int, int>>& seqs, int H, int G, int
   return 0;
 }
 
+// Places of partial results that no item has stored: whatever is there instead, none outside the array.
+static int check_slots() {
+  std::vector<int> slot(MAX_ITEMS);
+  const int junk[] = {-1, -7, MAX_PARTS, MAX_PARTS + 1, 2147483647, -2147483647 - 1, (int)0xff800000u, 0x7fc00000};
+  for (int i = 0; i < MAX_ITEMS; ++i) slot[i] = i % 3 ? junk[i % 8] : i % MAX_PARTS;
+  for (int i : {-2147483647 - 1, -1, MAX_ITEMS, MAX_ITEMS + 5, 2147483647})
+    if (slot_of(slot.data(), i) != -1) return 1;
+  for (int i = 0; i < MAX_ITEMS; ++i)
+    if (slot_of(slot.data(), i) != (i % 3 ? -1 : i % MAX_PARTS)) return 2;
+  return 0;
+}
+
 static Mask mask(int window, int sinks, int block) { return Mask{1.f, window, sinks, block, inverse_of(block)}; }
 
 int main(int argc, char** argv) {
+  if (argc == 1) return check_slots();
   Seen seen{};
   // one unit in the middle straddles two blocks and sees more than the first and the last one
   if (int e = check({{824, 11264}}, 8, 1, 152, mask(2048, 0, 512), seen)) return printf("straddling unit: %d\n", e), 1;
@@ -252,3 +265,8 @@ def test_items_make_up_the_units(walk, seed):
     assert r.returncode == 0, r.stdout + r.stderr
     uncut, even, longer, uneven = map(int, r.stdout.split())
     assert uncut > 20 and even > 20 and longer > 2 and uneven > 20   # plans of every kind were walked
+
+
+def test_places_that_no_item_stored(walk):
+    """After a CTA has given up waiting, the joining kernel finds anything in the places of partial results."""
+    assert subprocess.run([walk], timeout=60).returncode == 0
