@@ -461,7 +461,8 @@ dkv_status_t dkv_candidate_order_noalloc(const void* K_bank, const float* base, 
  * a page outside [0, n_pages) in a touched place, more than max_rows tokens in one
  * sequence, or sequences that together see more than 2^34 positions in an attend call of few
  * rows (counted once a key head) set the sticky error word (DKV_ERR_DEVICE, see dkv_cache_sync); the call
- * stays inside its buffers, and what it does for the sequences at fault is unspecified.
+ * stays inside its buffers, and what it does for the sequences at fault is unspecified.  (An attend call whose
+ * sequences together claim more rows than it has, row_start going back and forth, writes no outputs.)
  *
  * Packed tensors are [heads][rows][d] bf16 with any strides (in elements) between heads and
  * rows that are multiples of 8; d is contiguous and the address 16-byte aligned.

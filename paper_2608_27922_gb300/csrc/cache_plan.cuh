@@ -201,6 +201,7 @@ __host__ __device__ __forceinline__ Known known(const Job& j, int b) {
 __host__ __device__ __forceinline__ Plan make_plan(const Job& j, int ctas, Known& mine) {
   const int lane = lane_of();
   int units = 0, longest = 0;
+  unsigned claimed = 0;  // rows of all sequences
   bool even = true;      // units of one length
   float tiles = 0.f;     // of all units, about
   mine = known(j, lane);
@@ -208,6 +209,7 @@ __host__ __device__ __forceinline__ Plan make_plan(const Job& j, int ctas, Known
     const Known k = b == lane ? mine : known(j, b);
     if (k.q.n > j.max_rows) fail(j.c.status, DEV_INCONSISTENT, SITE_CHUNK);
     if (k.nu == 0) continue;
+    claimed += (unsigned)k.q.n;
     units += k.nu * j.c.H;
     tiles += 0.5f * (k.first + k.last) * k.nu * j.c.H;
     even &= k.first == k.last && (longest == 0 || longest == k.last);
@@ -218,6 +220,11 @@ __host__ __device__ __forceinline__ Plan make_plan(const Job& j, int ctas, Known
   longest = max_of(longest);
   even = all_of(even && (most == 0 || most == longest));
   Plan p{units, units, 0, 0, 1};
+  // (a row_start that goes back and forth: the work would be that of up to n_seq / 2 times the call's rows)
+  if ((unsigned)sum_of((int)claimed) > (unsigned)j.s.rows) {
+    fail(j.c.status, DEV_INCONSISTENT, SITE_ROWS);
+    return Plan{0, 0, 0, 0, 1};
+  }
   // (the choice below looks at every sequence in turn: many sequences are many units anyway)
   if (units == 0 || !j.cut || units >= CUT_ROUNDS * ctas || (!even && j.s.n > 64)) return p;
   // (uneven units:) no cut gains more than its joining costs

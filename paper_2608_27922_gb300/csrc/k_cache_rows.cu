@@ -141,20 +141,27 @@ __device__ __forceinline__ int token_of(const Job& j, int i) { return j.G == 1 ?
 
 __device__ __forceinline__ int stages_of(const Job& j, const Span& x) { return x.tiles * j.c.H * x.stages; }
 
-// Stages of the whole range; `first`: the span of sequence `lane`.  All lanes of a warp.
+// Stages of the whole range; `first`: the span of sequence `lane`.  All lanes of a warp.  None where a row_start that goes
+// back and forth gives the sequences more rows than the call has.
 template <int KT>
 __device__ __forceinline__ int total_stages(const Job& j, Span& first) {
   const int lane = threadIdx.x & 31;
   int64_t mine = 0;
+  unsigned claimed = 0;
   first = Span{};
   for (int b = lane; b < j.s.n; b += 32) {
     const Span x = span_of<KT>(j, b);
     if (b == lane) first = x;
     if (x.n > j.max_rows) fail(j.c.status, DEV_INCONSISTENT, SITE_CHUNK);
+    claimed += (unsigned)x.n;
     mine += (int64_t)x.tiles * j.c.H * x.stages;
   }
 #pragma unroll
   for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  if (__reduce_add_sync(0xffffffffu, claimed) > (unsigned)j.s.rows) {
+    fail(j.c.status, DEV_INCONSISTENT, SITE_ROWS);
+    return 0;
+  }
   if (mine > 0x7fffffff) {   // 2^31 stages: more than 17 TB of keys and values
     fail(j.c.status, DEV_INCONSISTENT, SITE_LEN);
     return 0;

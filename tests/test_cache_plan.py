@@ -211,10 +211,39 @@ static int check_slots() {
   return 0;
 }
 
+// Sequences that claim the same rows over and over: no work, an error.
+static int check_claims() {
+  for (int pairs : {1, 2, 40, 2048}) {
+    const int rows = 1000;
+    int32_t status[2] = {0, 0};
+    std::vector<int32_t> row{0}, len, table(2 * pairs, 0);
+    for (int i = 0; i < pairs; ++i) {
+      row.push_back(rows);                                  // all rows, then back to the first one
+      row.push_back(0);
+      len.push_back(9000);
+      len.push_back(9000);
+    }
+    Job j{};
+    j.c.status = status; j.c.H = 2; j.c.d = 128; j.c.page_len = 16; j.c.page_log2 = 4; j.c.n_pages = 4;
+    j.s = Seqs{table.data(), len.data(), row.data(), 2 * pairs, 1 << 20, rows};
+    j.G = 1; j.TQ = BQ; j.max_rows = rows; j.cut = 1;
+    Plan plan{};
+    run_warp([&](int lane) {
+      Known k{};
+      const Plan p = make_plan(j, 152, k);
+      if (lane == 0) plan = p;
+    });
+    if (status[0] == 0) return 1;
+    if (pairs > 1 ? plan.units != 0 || plan.items != 0 : plan.units != 8) return 2;
+  }
+  return 0;
+}
+
 static Mask mask(int window, int sinks, int block) { return Mask{1.f, window, sinks, block, inverse_of(block)}; }
 
 int main(int argc, char** argv) {
   if (argc == 1) return check_slots();
+  if (argc == 2) return check_claims();
   Seen seen{};
   // one unit in the middle straddles two blocks and sees more than the first and the last one
   if (int e = check({{824, 11264}}, 8, 1, 152, mask(2048, 0, 512), seen)) return printf("straddling unit: %d\n", e), 1;
@@ -270,3 +299,8 @@ def test_items_make_up_the_units(walk, seed):
 def test_places_that_no_item_stored(walk):
     """After a CTA has given up waiting, the joining kernel finds anything in the places of partial results."""
     assert subprocess.run([walk], timeout=60).returncode == 0
+
+
+def test_rows_claimed_more_than_once(walk):
+    """A row_start that goes back and forth gives every other sequence all rows: the call's work stays that of its rows."""
+    assert subprocess.run([walk, "claims"], timeout=60).returncode == 0

@@ -22,6 +22,27 @@ def dev(x, dtype=torch.bfloat16):
     return torch.from_numpy(np.ascontiguousarray(x)).to("cuda", dtype)
 
 
+# ---------------------------------------------------------------- arrays that contradict themselves
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n", [1, 200])
+def test_rows_claimed_more_than_once(dkv, fmt, n):
+    """Every other of 40 sequences has all of a call's rows: an error and no outputs, instead of 20 times the work."""
+    c = R.Case([(n, 300)] * 2, 2, 128, 32, fmt, seed=n)
+    cache, s = c.cache(dkv), c.device_seqs(dkv)
+    t = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    bad = dkv.CacheSeqs(s.block_table[:1].repeat(40, 1), t([300] * 40), t([0] + [2 * n, 0] * 20))
+    Q = torch.zeros(2, 2 * n, 128, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(Q, 3.0)
+    cache.attend(Q, bad, max_rows=2 * n, out=out)
+    with pytest.raises(dkv.DkvError) as e:
+        cache.sync()
+    assert e.value.status == 8 and bool((out == 3.0).all())
+    cache.attend(Q, s, max_rows=n, out=out)
+    cache.sync()
+    assert not bool((out == 3.0).any())
+    cache.close()
+
+
 # ---------------------------------------------------------------- cut units
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("seqs,H,Hq,mask", [
