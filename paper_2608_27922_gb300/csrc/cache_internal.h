@@ -47,6 +47,23 @@ inline uint64_t inverse_of(int block) { return block >= 2 ? ~(uint64_t)0 / (uint
 
 enum : int { SITE_ROWS = 1, SITE_LEN = 2, SITE_PAGE = 3, SITE_CHUNK = 4, SITE_PART = 5, SITE_WAIT = 400 };
 
+// Counts in scratch memory that nobody has cleared: a word is the call's number << COUNT_BITS | a count once a block of
+// the call has put that there, and whatever else it holds is no count yet.  A call clears its counts or leaves them at 0, so
+// that what an earlier call of the same kernel left is taken for no more than that even where the number comes round again;
+// what anybody else left must not look like a number at all.  So the upper 16 bits of the few-row kernel's words are 0x7f81 ..
+// 0x7fbe and those of the chunks' 0xff81 .. 0xffbe: never the other kernel's, and as the upper half of an fp32, as bf16 or
+// as fp16 NaNs that no arithmetic gives (infinities and the usual NaNs, 0x7f80, 0x7fc0, 0x7fff and their negatives, lie
+// outside), as integers far from small ones of either sign.  Beside them 38 bits or more have to agree.
+constexpr int ROWS_COUNT_BITS = 16;    // CTAs that share a unit
+constexpr int CHUNK_COUNT_BITS = 26;   // items of a call, CTAs, partial results
+constexpr uint64_t NUMBER_TOPS = 62;
+constexpr uint64_t rows_number(uint64_t call) {
+  return (0x7f81ull << (48 - ROWS_COUNT_BITS)) + call % (NUMBER_TOPS << (48 - ROWS_COUNT_BITS));
+}
+constexpr uint64_t chunk_number(uint64_t call) {
+  return (0xff81ull << (48 - CHUNK_COUNT_BITS)) + call % (NUMBER_TOPS << (48 - CHUNK_COUNT_BITS));
+}
+
 #ifdef __CUDACC__
 // (The index arithmetic below also compiles for the host, where a test walks its bounds.)
 __host__ __device__ __forceinline__ void fail(int32_t* status, int32_t code, int32_t site) {

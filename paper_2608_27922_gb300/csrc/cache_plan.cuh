@@ -123,7 +123,7 @@ struct Job {
   int cut;                     // units may be cut: cache_merge follows
   int wide;                    // every output row is 32-byte aligned
   unsigned long long call;     // the call's number
-  unsigned long long* count;   // [3] items taken beside each CTA's first, CTAs done, partial results: call << 32 | count (see take)
+  unsigned long long* count;   // [3] items taken beside each CTA's first, CTAs done, partial results: call << CHUNK_COUNT_BITS | count (see take)
   int4* plan;                  // stored_plan, for cache_merge
   int* slot;                   // [MAX_ITEMS] place of an item's partial result
   float* parts;                // [MAX_PARTS][(D + 1) * 256]

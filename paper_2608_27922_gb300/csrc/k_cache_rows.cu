@@ -55,7 +55,6 @@ constexpr int MAX_WARPS = 12;
 constexpr int WORKERS = MAX_WARPS * MAX_CTAS;
 constexpr float RESCALE_LOG2 = 8.0f;
 constexpr int MIN_STAGES = 1;    // stages of a warp, at least (one token over 1,561 positions: with 1 11 us, 2 15, 4 19)
-constexpr unsigned long long FIRST_CALL = 0xffb700000001ull;   // in the upper 48 bits of a word: a NaN as bf16, fp32
 
 // What a worker's stretch leaves unfinished.
 struct Stretch {
@@ -100,7 +99,7 @@ struct Job {
                      //   worker (a unit that its stretch begins in the middle of and goes on behind; its last unit's
                      //   stays in shared memory), then two of every CTA (a unit from before it, one that goes on behind)
   unsigned long long* arrived;   // [MAX_CTAS] CTAs that are done with the unit that begins in a CTA and goes on behind it: the
-                     //   call's number << 16 | their count; anything else counts as none (the scratch comes as it is)
+                     //   call's number << ROWS_COUNT_BITS | their count; anything else counts as none (the scratch comes as it is)
   unsigned long long call;
 };
 
@@ -268,27 +267,27 @@ __device__ __forceinline__ int chunk_at(int r, int c) {
 
 __device__ __forceinline__ bool sees(int p, int end, int lo, int sk) { return p < end && (p >= lo || p < sk); }
 
-// A unit's count of CTAs that are done with it: call << 16 | count once somebody has put it there, before that
+// A unit's count of CTAs that are done with it: call << ROWS_COUNT_BITS | count once somebody has put it there, before that
 // whatever the memory held.  begin_count, early: the CTA in which the unit begins does so; should another be done
 // before that, it sees that the number is not the call's.
 __device__ __forceinline__ void begin_count(unsigned long long* at, unsigned long long call) {
   const unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(at);
-  if ((old >> 16) != call) atomicCAS(at, old, call << 16);
+  if ((old >> ROWS_COUNT_BITS) != call) atomicCAS(at, old, call << ROWS_COUNT_BITS);
 }
 // One more of n; true for the last one, which leaves nothing behind.  (One trip to L2 as a rule; taking turns with
 // compare and swap instead cost 13 CTAs 6 us.)
 __device__ __forceinline__ bool arrive(unsigned long long* at, unsigned long long call, int n) {
   for (;;) {
     unsigned long long old = atomicAdd(at, 1ull);
-    if ((old >> 16) == call) {
-      if ((int)(old & 0xffffu) + 1 < n) return false;
+    if ((old >> ROWS_COUNT_BITS) == call) {
+      if ((int)(old & ((1u << ROWS_COUNT_BITS) - 1u)) + 1 < n) return false;
       atomicExch(at, 0ull);
       return true;
     }
     // nobody's count yet: the number that was added to was not one; put the call's there, or see that it is
     old = *reinterpret_cast<volatile unsigned long long*>(at);
-    while ((old >> 16) != call) {
-      const unsigned long long got = atomicCAS(at, old, call << 16);
+    while ((old >> ROWS_COUNT_BITS) != call) {
+      const unsigned long long got = atomicCAS(at, old, call << ROWS_COUNT_BITS);
       if (got == old) break;
       old = got;
     }
@@ -1011,12 +1010,11 @@ cudaError_t launch_attend_rows(const Pool& c, const Maps& maps, const Seqs& s, c
   const int n_sm = std::min(sm_count(), MAX_CTAS), G = Hq / c.H;
   if (n_sm <= 0) return cudaErrorInvalidDevice;
   // numbers the calls, so that a count that another call left in the same memory is not taken for this one's (a captured
-  // call keeps its number: its replays, one after the other, each find the count cleared by the one before); they begin
-  // at FIRST_CALL, so that no ordinary contents of the memory, small integers above all, pass for one
-  static std::atomic<unsigned long long> calls{FIRST_CALL};
+  // call keeps its number: its replays, one after the other, each find the count cleared by the one before)
+  static std::atomic<uint64_t> calls{0};
   unsigned long long* const arrived = static_cast<unsigned long long*>(scratch);
   const Job job{c, s, m, q, o, G, max_rows, (uint32_t)((0xffffffffull + G) / G), unit_rows(G, max_rows), part_rows(G, max_rows), reinterpret_cast<float*>(arrived + MAX_CTAS), arrived,
-                calls.fetch_add(1) & 0xffffffffffffull};
+                rows_number(calls.fetch_add(1))};
   if (c.d == 128)
     return c.e4m3 ? launch_d<128, true>(maps, job, n_sm, st) : launch_d<128, false>(maps, job, n_sm, st);
   return c.e4m3 ? launch_d<64, true>(maps, job, n_sm, st) : launch_d<64, false>(maps, job, n_sm, st);

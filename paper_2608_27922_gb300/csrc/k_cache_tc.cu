@@ -52,7 +52,7 @@ using namespace chunk;
 constexpr int PANEL = 128 * 128;         // bytes of a 64-column panel of 128 rows
 constexpr uint32_t TMEM_COLS = 512;      // S_0 [0,128), O_0 [128,256), S_1 [256,384), O_1 [384,512)
 constexpr float RESCALE_LOG2 = 8.0f;
-constexpr unsigned CALLS = 0xff800000u;   // the calls' numbers are this and 23 bits more: in the upper half of a word a NaN as bf16, fp32
+
 template <int D, bool E4M3>
 struct Lay {
   static constexpr int NP = D / 64;                    // panels of a row
@@ -112,19 +112,19 @@ __device__ __forceinline__ bool all_seen(const Span& s, int kt) {
   return kt < s.all_end && (kt >= s.all_lo || kt < s.all_sk);
 }
 // ------------------------------------------------------------------ the items
-// A count in scratch memory that nobody has cleared: call << 32 | count once somebody has put that there.  One more;
+// A count in scratch memory that nobody has cleared: call << CHUNK_COUNT_BITS | count once somebody has put that there.  One more;
 // the count before it.
 __device__ __forceinline__ void begin_count(unsigned long long* at, unsigned long long call) {
   const unsigned long long old = *reinterpret_cast<volatile unsigned long long*>(at);
-  if ((old >> 32) != call) atomicCAS(at, old, call << 32);
+  if ((old >> CHUNK_COUNT_BITS) != call) atomicCAS(at, old, call << CHUNK_COUNT_BITS);
 }
 __device__ __forceinline__ int taken_as(unsigned long long* at, unsigned long long call, unsigned long long old) {   // (old: of the addition)
   for (;; old = atomicAdd(at, 1ull)) {
-    if ((old >> 32) == call) return (int)(old & 0x7fffffffu);
+    if ((old >> CHUNK_COUNT_BITS) == call) return (int)(old & ((1u << CHUNK_COUNT_BITS) - 1u));
     // what was added to was no count of this call's yet: put it there, or see that it is
     old = *reinterpret_cast<volatile unsigned long long*>(at);
-    while ((old >> 32) != call) {
-      const unsigned long long got = atomicCAS(at, old, call << 32);
+    while ((old >> CHUNK_COUNT_BITS) != call) {
+      const unsigned long long got = atomicCAS(at, old, call << CHUNK_COUNT_BITS);
       if (got == old) break;
       old = got;
     }
@@ -939,8 +939,9 @@ cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, con
                              int max_rows, const Mask& m, void* scratch, cudaStream_t st) {
   const int G = Hq / c.H, TQ = BQ / G, n_sm = std::min(sm_count(), MAX_CTAS);
   if (n_sm <= 0) return cudaErrorInvalidDevice;
-  // items are counted in 31 bits (only outputs whose rows overlap could make more)
-  if ((int64_t)c.H * (s.rows / (2 * TQ) + s.n) >= (1ll << 31) - 4096) return cudaErrorInvalidValue;
+  // items are counted in CHUNK_COUNT_BITS bits (only outputs whose rows overlap could make more: 2.3e9 rows of 64 fill the
+  // memory, a unit has 130 rows or more but for a sequence's last, and there are 4,096 x 4,096 of those)
+  if ((int64_t)c.H * (s.rows / (2 * TQ) + s.n) >= (1ll << CHUNK_COUNT_BITS) - 4096) return cudaErrorInvalidValue;
   CUtensorMap mq;
   const int64_t dim[4] = {c.d, G, s.rows, c.H};
   const int64_t head = q.head ? q.head : c.d, row = q.row ? q.row : c.d;   // (one head or row: any stride)
@@ -948,14 +949,13 @@ cudaError_t launch_attend_tc(const Pool& c, const Maps& maps, const Seqs& s, con
   const int box[4] = {64, G, TQ, 1};
   if (!make_map_4d(&mq, q.p, 2, dim, stride, box, 128)) return cudaErrorInvalidValue;
   // numbers the calls, so that what another call left in the same memory is not taken for a count of this one's (a
-  // captured call keeps its number: its replays, one after the other, each find the counts cleared by the one before);
-  // no ordinary contents of the memory, small integers above all, pass for one
-  static std::atomic<unsigned> calls{0};
+  // captured call keeps its number: its replays, one after the other, each find the counts cleared by the one before)
+  static std::atomic<uint64_t> calls{0};
   char* const at = static_cast<char*>(scratch);
   // (several sequences make more units than one with all their rows)
   const bool cut = (int64_t)c.H * ((s.rows + 2 * TQ - 1) / (2 * TQ)) < CUT_ROUNDS * n_sm;
   const Job job{c, s, m, o, G, TQ, max_rows, cut ? 1 : 0,
-                (uintptr_t)o.p % 32 == 0 && o.head % 16 == 0 && o.row % 16 == 0, CALLS | (calls.fetch_add(1) & ~CALLS), reinterpret_cast<unsigned long long*>(at),
+                (uintptr_t)o.p % 32 == 0 && o.head % 16 == 0 && o.row % 16 == 0, chunk_number(calls.fetch_add(1)), reinterpret_cast<unsigned long long*>(at),
                 reinterpret_cast<int4*>(at + 64), reinterpret_cast<int*>(at + 256),
                 reinterpret_cast<float*>(at + 256 + sizeof(int) * MAX_ITEMS)};
   if (c.d == 128)

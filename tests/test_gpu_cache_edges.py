@@ -1,4 +1,8 @@
 """The paged cache on the GPU where its plans, scratch, scales and waits can go wrong (reference: cache_ref.py)."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -6,6 +10,7 @@ import torch
 import cache_ref as R
 
 pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -41,6 +46,44 @@ def test_rows_claimed_more_than_once(dkv, fmt, n):
     cache.sync()
     assert not bool((out == 3.0).any())
     cache.close()
+
+
+# ---------------------------------------------------------------- scratch
+@pytest.mark.parametrize("rows", [1, 200])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_scratch_of_infinities(dkv, rows, dtype):
+    """The first attentions of a process in memory that held a mask of -infinity."""
+    code = f"""
+import ctypes, sys, torch
+sys.path.insert(0, {str(ROOT)!r})
+from paper_2608_27922_gb300 import dkv
+H, d, n, rows = 2, 128, 6000, {rows}
+cache = dkv.PagedCache(H, d, 64, 94, "bf16")
+t = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")
+table = torch.arange(94, dtype=torch.int32, device="cuda")[None]
+torch.manual_seed(0)
+K, V, Q = (torch.randn(H, n, d, device="cuda", dtype=torch.bfloat16) for _ in range(3))
+cache.write(K, V, dkv.CacheSeqs(table, t([n]), t([0, n])))
+seqs = dkv.CacheSeqs(table, t([n]), t([0, rows]))
+Q = Q[:, :rows].contiguous()
+L = dkv.lib()
+size = int(L.dkv_cache_attend_scratch_size(cache.handle, 1, H, rows, rows))
+scratch = torch.empty(size, dtype=torch.uint8, device="cuda")
+size = scratch.numel()
+got = []
+for fill in (float("-inf"), float("-inf"), 0.0):
+    scratch[:size // 4 * 4].view(torch.{dtype}).fill_(fill)
+    out = torch.full_like(Q, 9.0)
+    how = dkv.dkv_cache_attend_t(0.0, 0, 0, 1, rows)
+    assert L.dkv_cache_attend(cache.handle, seqs._ref, Q.data_ptr(), H, rows, rows * d, d, out.data_ptr(), rows * d, d,
+                              ctypes.byref(how), scratch.data_ptr(), size, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    got.append(out)
+cache.sync()
+assert all(torch.equal(x, got[2]) for x in got) and not bool((got[0] == 9.0).all(-1).any())
+"""
+    r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0, r.stderr[-2000:]
 
 
 # ---------------------------------------------------------------- cut units
