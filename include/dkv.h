@@ -547,7 +547,9 @@ size_t dkv_cache_attend_scratch_size(dkv_cache_t cache, int32_t n_seq, int32_t H
  * A token that sees no position (a negative position of its own, an empty sequence) gets
  * zeros, and so does one whose scores are all -infinity.  Rows from row_start[n_seq] on are left as they were.  What lies in places that a
  * token does not see, NaN and infinities too, does not reach its output.  Scores, sums and
- * outputs are held in fp32; the weights are rounded to bf16 before they meet the values.
+ * outputs are held in fp32; the weights are rounded to bf16 before they meet the values.  (Over an e4m3
+ * cache a call of few rows meets its keys with queries in fp16, each row times a power of two: of a row's elements those
+ * smaller than 2^-24 of its largest magnitude are rounded, to within 2^-32 of that.)
  * The order of the sums follows from the sizes and arrays of the call and from the device.  */
 dkv_status_t dkv_cache_attend(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const void* Q, int32_t H_q,
                               int32_t rows, int64_t q_head_stride, int64_t q_row_stride, void* O,

@@ -21,11 +21,13 @@
 // would be empty but for a sixteenth).  The weights' registers become an operand by one
 // transposing move for 8 keys.  Running maximum, sum and outputs stay in registers.
 //
-// e4m3: the codes become fp16 in the registers, one conversion for two.  A key row's 128 codes lie
-// with four lanes, 32 neighbouring ones each, and the queries' registers are loaded in that order of d
-// instead of the product's own; of the values, a transposed load gives pairs of d of one position, which
-// widen into the even and the odd ones of 16.  (As bf16, by bit operations, the codes took half of
-// all instructions.)
+// e4m3: the keys' codes become fp16 in the registers, one conversion for two; the scales join the scores.  A key row's 128
+// codes lie with four lanes, 32 neighbouring ones each, and the queries' registers are loaded in that order of d
+// instead of the product's own.  The values become bf16 with their scales in them, by bit operations (widen_values), for
+// weights in bf16 as a bf16 cache has them: in fp16 the weights would have to carry the scales, relative to the largest such
+// product, and what is 2^-24 below that would be lost (beside a row of zeros, whose scale is 2^0, all of a row of ordinary
+// size).  Of the values, a transposed load gives pairs of d of one position, which widen into the even and the odd ones of 16.
+// (With fp16 weights, whose sums had to be kept apart, 32 tokens of 40 on 8 heads took as long: 70.6 us a call for 70.4.)
 //
 // Measured: one token of 12 heads over 131,001 positions in bf16 127 us, 6.3 TB/s of the 6.8 that a copy reaches (in
 // e4m3 77 us, 5.3); 32 tokens of 40 on 8 heads over up to 9,360 positions in e4m3 68 us (5.1 TB/s), in bf16 113 (6.1).
@@ -256,6 +258,21 @@ __device__ __forceinline__ uint32_t pack_f16(float a, float b) {
 __device__ __forceinline__ uint32_t to_f16(uint32_t x, float f) {
   const float2 v = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&x));
   return pack_f16(v.x * f, v.y * f);
+}
+
+// Four codes of the values, two positions of two neighbouring columns d, d + 1 (bytes: position 0: d, d + 1, position 1:
+// d, d + 1), as bf16: a code's bits in bf16's fields (its sign spread over a byte above it, all but one of those bits cleared)
+// are its value times 2^-120, subnormal codes included; f holds 2^120 times the positions' scales.
+__device__ __forceinline__ void widen_values(uint32_t w, __nv_bfloat162 f, uint32_t& d0, uint32_t& d1) {
+  uint32_t a, b;
+  asm("prmt.b32 %0, %1, 0, 0xa280;" : "=r"(a) : "r"(w));   // (a selector's upper bit: that byte's sign, eight times)
+  asm("prmt.b32 %0, %1, 0, 0xb391;" : "=r"(b) : "r"(w));
+  a = (a << 4) & 0x87f087f0u;
+  b = (b << 4) & 0x87f087f0u;
+  const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), f);
+  const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), f);
+  d0 = *reinterpret_cast<const uint32_t*>(&x);
+  d1 = *reinterpret_cast<const uint32_t*>(&y);
 }
 
 // Byte offset of 16-byte chunk c of row r in a tile.
@@ -514,7 +531,8 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
 
     const int sk = j.m.window ? j.m.sinks : 0;
     // e4m3: the products are fp16, which holds every code exactly; a row of queries too, times the power of
-    // two that puts its largest magnitude at 2^7 .. 2^8 (what lies 2^-31 below that is rounded, to within 2^-33 of it)
+    // two that puts its largest magnitude at 2^7 .. 2^8 (what lies 2^-24 below that is rounded, to within 2^-32 of it: fp16's
+    // steps are 2^-24 there)
     float rs[NR][2];                        // of a row's products, in the exponent of 2
 #pragma unroll
     for (int u = 0; u < NR; ++u) {
@@ -538,12 +556,12 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
       }
     }
     // o[c][u]: columns of the values 16 c + gr, + 8 (e4m3: 16 c + 2 gr, + 1) of rows 8 u + 2 t, + 1
-    float o[D / 16][NR][4], mrun[NR][2], msum[NR][2], l[NR][2];
+    float o[D / 16][NR][4], mrun[NR][2], l[NR][2];
 #pragma unroll
     for (int u = 0; u < NR; ++u) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        mrun[u][e] = msum[u][e] = -INFINITY;
+        mrun[u][e] = -INFINITY;
         l[u][e] = 0.f;
       }
 #pragma unroll
@@ -613,6 +631,23 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e) s[g][u][e] += s2[g][u][e];
       }
+      // e4m3: 2^120 times the values' scales (positions 16 g + 8 v + 2 t and the next).  Where that is more than bf16 holds
+      // (far: scales above 2^7), as much of it as bf16 does hold; the rest goes to the weights.  A row of byte 255 is NaN to
+      // those that see it by its score; its codes are left finite for the others, whose weight is 0.
+      uint32_t vf[KT / 16][2];
+      bool far = false;
+      if constexpr (E4M3) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int g = 0; g < KT / 16; ++g)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            const uint32_t b = __byte_perm(*reinterpret_cast<const uint16_t*>(sc + KT + g * 16 + v * 8 + 2 * t), 0, 0x4140);
+            most = __vmaxu2(most, b);
+            vf[g][v] = (b + 0x00780078u) << 7;
+          }
+        far = __any_sync(0xffffffffu, max(most & 0xffffu, most >> 16) > 134u);
+      }
       // into exponents of 2, with the keys' scales
 #pragma unroll
       for (int g = 0; g < KT / 16; ++g)
@@ -624,6 +659,17 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
 #pragma unroll
             for (int e = 0; e < 2; ++e) s[g][u][2 * v + e] *= E4M3 ? ck * rs[u][e] : j.m.sl2;
         }
+      if (E4M3 && far) {
+#pragma unroll
+        for (int g = 0; g < KT / 16; ++g)
+#pragma unroll
+          for (int v = 0; v < 2; ++v) {
+            vf[g][v] = (__vminu2(vf[g][v] >> 7, 0x00fe00feu)) << 7;
+            if (sc[KT + g * 16 + v * 8 + gr] != 255u) continue;
+#pragma unroll
+            for (int u = 0; u < NR; ++u) s[g][u][2 * v] = s[g][u][2 * v + 1] = __int_as_float(0x7fffffff);
+          }
+      }
       if (partial) {
 #pragma unroll
         for (int g = 0; g < KT / 16; ++g)
@@ -632,38 +678,6 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
 #pragma unroll
             for (int e = 0; e < 4; ++e)
               if (!sees(p0 + g * 16 + (e >> 1) * 8 + gr, end[u][e & 1], lo[u][e & 1], sk)) s[g][u][e] = -INFINITY;
-      }
-      // e4m3: the values' scales join the exponents, so that a weight carries its value's scale and the running
-      // maximum is that of the products: no weight leaves fp16's range, however the scales differ.  The sums
-      // of the weights themselves have a maximum of their own (each thread's).
-      if constexpr (E4M3) {
-#pragma unroll
-        for (int u = 0; u < NR; ++u)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float mx = -INFINITY;
-#pragma unroll
-            for (int g = 0; g < KT / 16; ++g) mx = max3(mx, s[g][u][e], s[g][u][2 + e]);
-            if (mx > msum[u][e] + RESCALE_LOG2 || (msum[u][e] == -INFINITY && mx > -INFINITY)) {
-              l[u][e] *= msum[u][e] == -INFINITY ? 0.f : ex2(msum[u][e] - mx);
-              msum[u][e] = mx;
-            }
-            const float nm = msum[u][e] == -INFINITY ? 0.f : -msum[u][e];
-#pragma unroll
-            for (int g = 0; g < KT / 16; ++g) l[u][e] += ex2(s[g][u][e] + nm) + ex2(s[g][u][2 + e] + nm);
-          }
-#pragma unroll
-        for (int g = 0; g < KT / 16; ++g)
-#pragma unroll
-          for (int v = 0; v < 2; ++v) {
-            const uint32_t b = sc[KT + g * 16 + v * 8 + gr];
-            const float ev = b == 255u ? __int_as_float(0x7fffffff) : __uint_as_float(0x4b000000u | b) - 8388735.0f;
-#pragma unroll
-            for (int u = 0; u < NR; ++u)
-#pragma unroll
-              for (int e = 0; e < 2; ++e)
-                if (!partial || s[g][u][2 * v + e] != -INFINITY) s[g][u][2 * v + e] += ev;   // (a hidden row's may be NaN)
-          }
       }
       // ---- running maximum of a row (the eight lanes of the same t)
       float nm[NR][2], alpha[NR][2];
@@ -683,7 +697,7 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
           alpha[u][e] = raise ? (before == -INFINITY ? 0.f : ex2(before - mx)) : 1.f;
           if (raise) {
             raised |= before != -INFINITY;   // (nothing to scale before the first visible key)
-            if (!E4M3) l[u][e] *= alpha[u][e];
+            l[u][e] *= alpha[u][e];
             mrun[u][e] = mx;
           }
           nm[u][e] = mrun[u][e] == -INFINITY ? 0.f : -mrun[u][e];
@@ -704,29 +718,19 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
         for (int u = 0; u < NR; ++u)
 #pragma unroll
           for (int v = 0; v < 2; ++v) {
-            const float a = ex2(s[g][u][2 * v] + nm[u][0]), b = ex2(s[g][u][2 * v + 1] + nm[u][1]);
-            if (!E4M3) {
-              l[u][0] += a;
-              l[u][1] += b;
+            float a = ex2(s[g][u][2 * v] + nm[u][0]), b = ex2(s[g][u][2 * v + 1] + nm[u][1]);
+            l[u][0] += a;
+            l[u][1] += b;
+            if (E4M3 && far) {              // (a weight is 2^8 at most, the rest of a scale 2^113)
+              const uint32_t y = sc[KT + g * 16 + v * 8 + gr];
+              const float rest = y > 134u && y != 255u ? __uint_as_float((y - 7u) << 23) : 1.0f;
+              a *= rest;
+              b *= rest;
             }
-            pb[g][u][v] = transpose(E4M3 ? pack_f16(a, b) : pack_bf16(a, b));
+            pb[g][u][v] = transpose(pack_bf16(a, b));
           }
       // ---- values that are not finite, in a stage that some row does not see whole: into the outputs of the rows
       // that see them, and out of the tile (their weight elsewhere is 0, and 0 times them NaN)
-      if (E4M3 && partial) {                // (NaN codes: their rows' scales already are NaN to those that see them)
-#pragma unroll 1
-        for (int i = 0; i < L::TILE / 16 / 32; ++i) {
-          uint4* w = reinterpret_cast<uint4*>(vt) + i * 32 + lane;
-          uint4 y = *w;
-          auto clear = [](uint32_t c) {
-            const uint32_t bad = ((c & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-            return c & ~((bad >> 7) * 0xffu);
-          };
-          *w = make_uint4(clear(y.x), clear(y.y), clear(y.z), clear(y.w));
-        }
-        fence_async_smem();                 // (the next copy into the slot follows)
-        __syncwarp();
-      }
       if (!E4M3 && partial) {
         uint32_t any = 0;
 #pragma unroll
@@ -770,11 +774,12 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
             uint32_t b[4];
             ldsm_t(va + chunk_at<D, E4M3>(g * 16 + (m & 1) * 8 + (lane & 7), c2 * 2 + (m >> 1)), b);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {   // bytes: (position 0: d, d + 1), (position 1: d, d + 1)
-              const uint32_t x0 = __byte_perm(b[2 * i], 0, 0x3120), x1 = __byte_perm(b[2 * i + 1], 0, 0x3120);
-              const uint32_t a[4] = {widen_lo(x0), widen_hi(x0), widen_lo(x1), widen_hi(x1)};
+            for (int i = 0; i < 2; ++i) {
+              uint32_t a[4];
+              widen_values(b[2 * i], *reinterpret_cast<const __nv_bfloat162*>(&vf[g][0]), a[0], a[1]);
+              widen_values(b[2 * i + 1], *reinterpret_cast<const __nv_bfloat162*>(&vf[g][1]), a[2], a[3]);
 #pragma unroll
-              for (int u = 0; u < NR; ++u) mma_f16(o[2 * c2 + i][u], a, pb[g][u][0], pb[g][u][1]);
+              for (int u = 0; u < NR; ++u) mma(o[2 * c2 + i][u], a, pb[g][u][0], pb[g][u][1]);
             }
           }
         } else {
@@ -793,21 +798,12 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
     if (!ok) break;
 
     // ---- the segment's result
-    float lse[NR][2];                     // of l: its base's exponent
 #pragma unroll
     for (int u = 0; u < NR; ++u)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        lse[u][e] = mrun[u][e];
-        if (E4M3) {                       // the eight threads' sums to one base
-          lse[u][e] = msum[u][e];
-#pragma unroll
-          for (int w = 4; w <= 16; w <<= 1) lse[u][e] = fmaxf(lse[u][e], __shfl_xor_sync(0xffffffffu, lse[u][e], w));
-          if (msum[u][e] != lse[u][e]) l[u][e] *= ex2(msum[u][e] - lse[u][e]);   // (-inf: l is 0)
-        }
+      for (int e = 0; e < 2; ++e)
 #pragma unroll
         for (int w = 4; w <= 16; w <<= 1) l[u][e] += __shfl_xor_sync(0xffffffffu, l[u][e], w);
-      }
     const bool whole = count == x.stages;
     if (!whole && lane == 0) {
       Stretch& y = info[warp];
@@ -836,11 +832,11 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
       for (int e = 0; e < 2; ++e) {
         const int r = 8 * u + 2 * t + e;
         if (r >= rows || (!whole && r >= j.part_rows)) continue;
-        const float inv = l[u][e] == 0.f ? 0.f : E4M3 ? ex2(mrun[u][e] - lse[u][e]) / l[u][e] : 1.0f / l[u][e];
+        const float inv = l[u][e] == 0.f ? 0.f : 1.0f / l[u][e];
         const int i = tile * UNIT + r, tok = token_of(j, i), hq = i - tok * j.G;
         __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + hq) * j.o.head + (int64_t)(x.r0 + tok) * j.o.row;
         float* pd = part + r * D;
-        if (!whole && gr == 0) part[j.part_rows * D + r] = l[u][e] == 0.f ? -INFINITY : lse[u][e] + log2f(l[u][e]);
+        if (!whole && gr == 0) part[j.part_rows * D + r] = l[u][e] == 0.f ? -INFINITY : mrun[u][e] + log2f(l[u][e]);
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
           const float a = o[c][u][e] * inv, b = o[c][u][2 + e] * inv;

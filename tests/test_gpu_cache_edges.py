@@ -86,6 +86,78 @@ assert all(torch.equal(x, got[2]) for x in got) and not bool((got[0] == 9.0).all
     assert r.returncode == 0, r.stderr[-2000:]
 
 
+# ---------------------------------------------------------------- quantised values of different magnitudes
+def quantised(c):
+    (c.kc, c.ks), (c.vc, c.vs) = R.quantise(c.k), R.quantise(c.v)
+    c.k, c.v = R.decode(c.kc, c.ks), R.decode(c.vc, c.vs)
+
+
+ROWS = [(1, 1, 1), (5, 2, 6), (40, 1, 2)]              # tokens, key heads, query heads: 8-row and 16-row units, chunks
+
+
+def attend_and_check(dkv, c, Hq, Q, n):
+    cache, s = c.cache(dkv), c.device_seqs(dkv)
+    out = cache.attend(dev(Q), s, max_rows=n)
+    cache.sync()
+    cache.close()
+    R.check(out, R.attend(c, Q, rows={0, n - 1, c.rows - 1}))
+
+
+@pytest.mark.parametrize("n,H,Hq", ROWS)
+@pytest.mark.parametrize("size", [1.0, 0.1, 0.01, 0.001, 2.0 ** -90])
+def test_zero_value_rows(dkv, n, H, Hq, size):
+    """A key that most of a softmax goes to and whose value is a row of zeros (a sink): its scale byte, 127, is far above
+    the other rows', and none of their weight is lost to it."""
+    c = R.Case([(n, 1561), (n, 300 + n)], H, 128, 64, "bf16", seed=n)
+    c.fmt = "e4m3"
+    c.v *= size
+    g = np.random.default_rng(7)
+    Q = R.bf16(g.standard_normal((Hq, c.rows, 128)))
+    for b, j in ((0, 0), (0, 777), (1, 3)):            # scores of 10 and more for all rows
+        p, sl = c.table[b, j // 64], j % 64
+        c.v[p, :, sl] = 0.0
+        c.k[p, :, sl] = 0.0
+        c.k[p, :, sl, 0] = 30.0
+    Q[:, :, 0] = R.bf16(np.full(Q.shape[:2], 4.0))
+    quantised(c)
+    attend_and_check(dkv, c, Hq, Q, n)
+
+
+@pytest.mark.parametrize("n,H,Hq", ROWS)
+@pytest.mark.parametrize("top", [2.0 ** 12, 2.0 ** 30, 2.0 ** 100])
+def test_large_values_in_one_column(dkv, n, H, Hq, top):
+    """Rows of values that are large in one column and zero in the others: the other columns' outputs are made of small rows'
+    values, whose products with their weights lie far below the large ones."""
+    c = R.Case([(n, 900), (n, 2000)], H, 128, 32, "bf16", seed=n + 1)
+    c.fmt = "e4m3"
+    g = np.random.default_rng(8)
+    big = g.random(c.v.shape[:3]) < 0.1
+    c.v[big] = 0.0
+    c.v[..., 77][big] = top * R.bf16(g.standard_normal(int(big.sum())))
+    c.v = R.bf16(c.v)
+    quantised(c)
+    attend_and_check(dkv, c, Hq, R.bf16(g.standard_normal((Hq, c.rows, 128)) * 2.0), n)
+
+
+@pytest.mark.parametrize("n,H,Hq", ROWS)
+def test_many_small_weights(dkv, n, H, Hq):
+    """A key that nearly all of a softmax goes to, with a value that is zero but in one column, and thousands of keys of weights
+    around 2^-26 of its: their sum is all that the other columns hold."""
+    c = R.Case([(n, 20000)], H, 128, 64, "bf16", seed=n + 2)
+    c.fmt = "e4m3"
+    p, sl = c.table[0, 99], 5
+    c.k *= 0.25
+    c.k[p, :, sl] = 0.0
+    c.k[p, :, sl, 0] = 16.0
+    c.v[p, :, sl] = 0.0
+    c.v[p, :, sl, 3] = 1.0
+    c.v = np.abs(c.v)
+    quantised(c)
+    Q = R.bf16(np.random.default_rng(9).standard_normal((Hq, n, 128)))
+    Q[:, :, 0] = 12.75                                  # 16 * 12.75 / sqrt(128) = 18.0 = 26 log(2)
+    attend_and_check(dkv, c, Hq, Q, n)
+
+
 # ---------------------------------------------------------------- cut units
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("seqs,H,Hq,mask", [
