@@ -386,8 +386,10 @@ dkv_status_t dkv_bank_kernel_times(dkv_bank_t bank, int32_t max_kernels, char* n
  * barrier nothing arrives on; after limit_us microseconds (1 .. 1e6) the wait gives
  * up, the kernel records the timeout and returns.  Returns DKV_ERR_TIMEOUT when the
  * wait gave up as designed (the expected result), and writes the measured wait
- * duration to *elapsed_ns (host).  Synchronises the device; allocates 16 bytes of
- * device memory for the duration of the call.  The context stays usable.          */
+ * duration to *elapsed_ns (host).  A second warp waits in the form that the paged cache's
+ * attention uses, which ends when another warp has given up; both have to.  Synchronises the
+ * device; allocates 24 bytes of device memory for the duration of the call.  The context
+ * stays usable.                                                                    */
 dkv_status_t dkv_selftest_wait_timeout(int32_t limit_us, int64_t* elapsed_ns);
 
 /* Largest candidate count accepted by dkv_candidate_order_noalloc. */
@@ -557,7 +559,8 @@ dkv_status_t dkv_cache_attend(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, c
                               void* scratch, size_t scratch_bytes, void* stream);
 
 /* Waits for the stream of the handle's last call, then reports and clears the error word
- * (as dkv_bank_sync).                                                                     */
+ * (as dkv_bank_sync).  After DKV_ERR_TIMEOUT the scratch of a captured attend call is cleared
+ * before the graph is replayed: a call that gave up may leave its counts in it.            */
 dkv_status_t dkv_cache_sync(dkv_cache_t cache);
 
 #ifdef __cplusplus

@@ -572,7 +572,7 @@ __global__ void __launch_bounds__((Lay<D, E4M3, NR>::WARPS * 32), 1)
 
     for (int k = 0; k < count; ++k) {
       const int slot = used % L::SLOTS;
-      if (!(ok = mbar_wait_warp_short(bars + slot, (used / L::SLOTS) & 1, &no_abort))) break;
+      if (!(ok = mbar_wait_warp(bars + slot, (used / L::SLOTS) & 1, &no_abort))) break;
       ++used;
       const int kk0 = k0 + k, p0 = (kk0 < x.ns ? kk0 : x.w0 + (kk0 - x.ns)) * KT;
       const bool partial = !(p0 + KT <= x.all_end && (p0 >= x.all_lo || p0 + KT <= sk));

@@ -312,6 +312,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
   uint64_t* it_full = bars + 22;    // [2] items
   uint64_t* it_empty = bars + 24;   // [2]
   uint64_t* done = bars + 26;
+  uint64_t* over = bars + 27;       // every role but the producer has ended
   Item* items = reinterpret_cast<Item*>(bars + 28);                        // [2]
   volatile int* wild = reinterpret_cast<volatile int*>(items + 2);         // [2] number of the last item with values cleared
   // [2] e4m3: a byte a widening warp, not 0 where it met a NaN row of the slot's values
@@ -341,6 +342,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       mbar_init(v_empty + i, 1);
     }
     mbar_init(done, 1);
+    mbar_init(over, 1 + 8 + L::CONV);
     *abort_flag = 0;
     fence_barrier_init();
   }
@@ -371,7 +373,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
   if (warp < L::SOFT0) {
     regs_lower<L::REGS_IO>();
     if (warp == 0) {
-      // ---------------- producer: items; Q, then K(0), V(0), K(1), ..
+      // ---------------- producer: items; Q, then K(0), V(0), K(1), ..  It also watches the time for all roles' waits: its
+      // own wait for their work, tile by tile, and at last for their end.
       Cursor cursor{};
       const Plan plan = make_plan(j, gridDim.x, cursor.k);
       if (plan.C == 0 && j.s.n > 1 && j.s.n <= 32) order(cursor.k, j.s.n);
@@ -411,7 +414,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
             x.part = __shfl_sync(0xffffffffu, slot, 0);
           }
         }
-        if (ni >= 2) ok = mbar_wait_warp_short(it_empty + (ni & 1), ((ni >> 1) & 1) ^ 1, abort_flag);
+        if (ni >= 2) ok = mbar_wait_warp(it_empty + (ni & 1), ((ni >> 1) & 1) ^ 1, abort_flag);
         if (!ok) break;
         if (lane == 0) {
           items[ni & 1] = x;
@@ -433,7 +436,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
                      ? __ldg(j.s.table + (int64_t)x.b * j.s.max_pages + (k0 >> j.c.page_log2)) : 0;
         };
         int base = x.i0, pages = entry_of(base), pages_next = entry_of(base + batch);
-        if (nq > 0 && !(ok = mbar_wait_warp_short(q_empty, (nq - 1) & 1, abort_flag))) break;
+        if (nq > 0 && !(ok = mbar_wait_warp(q_empty, (nq - 1) & 1, abort_flag))) break;
         ++nq;
         if (lane == 0) {
           const int groups = x.n > j.TQ ? 2 : 1, bytes = j.TQ * j.G * 128;
@@ -466,7 +469,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
           if (E4M3) {
             const uint32_t c = cc++;
             uint64_t* bar = c_full + (c & 1);
-            if (c >= 2 && !mbar_wait_warp_short(c_empty + (c & 1), ((c >> 1) & 1) ^ 1, abort_flag)) return false;
+            if (c >= 2 && !mbar_wait_warp(c_empty + (c & 1), ((c >> 1) & 1) ^ 1, abort_flag)) return false;
             if (lane == 0) mbar_arrive_expect_tx(bar, BK * D);
             __syncwarp();
             if (box < np)
@@ -482,7 +485,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
           } else {
             const uint32_t nb = is_k ? L::NK : L::NV, sl = t % nb;
             uint64_t* bar = (is_k ? k_full : v_full) + sl;
-            if (t >= nb && !mbar_wait_warp_short((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
+            if (t >= nb && !mbar_wait_warp((is_k ? k_empty : v_empty) + sl, (t / nb - 1) & 1, abort_flag)) return false;
             if (lane == 0) mbar_arrive_expect_tx(bar, L::TB);
             __syncwarp();
             if (box < np)
@@ -505,6 +508,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       // the last CTA to run out of items clears the counts (a replayed graph's next call has the same number)
       if (lane == 0 && take(j.count + 1, j.call) == (int)gridDim.x - 1)
         for (int i = 0; i < 3; ++i) atomicExch(j.count + i, 0ull);
+      if (ok) ok = mbar_wait_warp(over, 0, abort_flag);
       if (!ok) {
         if (lane == 0) give_up(0);
         // copies may be in flight that nobody waits for any more: far longer than one takes
@@ -625,6 +629,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       commit(done);
       volatile int no_abort = 0;
       mbar_wait(done, 0, &no_abort);
+      if (lane == 0) mbar_arrive(over);
     }
   } else if (warp < L::CONV0) {
     regs_raise<L::REGS_SOFT>();
@@ -787,6 +792,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       if (lane == 0) mbar_arrive(it_empty + (ni & 1));
     }
     if (!ok && lane == 0) give_up(2);
+    if (lane == 0) mbar_arrive(over);
   } else if constexpr (E4M3) {
     regs_lower<L::REGS_CONV>();
     // ---------------- codes into bf16, in the order of the copies: K(0), V(0), K(1), V(1), .. (V(i) is wanted
@@ -820,6 +826,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       tc += n;
     }
     if (!ok && lane == 0) give_up(3);
+    if (lane == 0) mbar_arrive(over);
   }
   fence_before_sync();
   __syncthreads();

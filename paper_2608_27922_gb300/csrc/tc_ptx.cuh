@@ -79,13 +79,15 @@ __device__ __forceinline__ bool mbar_wait_warp(uint64_t* bar, uint32_t parity, v
   return __all_sync(0xffffffffu, mbar_wait_limit(bar, parity, abort, kWaitNs));
 }
 
-// The same in few instructions, limited by a count of tries instead of the clock (a try takes 20 cycles at
-// least, more where the hardware suspends the thread): kernels with many waits, whose instructions would
-// otherwise be mostly these loops.
+// The same in few instructions, for kernels with many waits, whose instructions would otherwise be mostly these loops: one
+// warp of the CTA, which all the others' work holds up sooner or later, waits by the clock (mbar_wait_warp) to the end of
+// that work and sets *abort for the others.  Their own limit, a count of tries, is for the case that it does not: 40 s at
+// least (a try takes 20 cycles), by an unknown factor more where the hardware suspends the thread.  (With the clock in each of
+// these loops ragged prompts took 265 us for 258; with it in a warp of its own, 260.)
 __device__ __forceinline__ bool mbar_wait_warp_short(uint64_t* bar, uint32_t parity, volatile int* abort) {
   bool ok = mbar_try_wait(bar, parity);
 #pragma unroll 1
-  for (uint32_t tries = 1u << 26; !ok && tries && !*abort; --tries) ok = mbar_try_wait(bar, parity);
+  for (uint32_t tries = 0xffffffffu; !ok && tries && !*abort; --tries) ok = mbar_try_wait(bar, parity);
   return __all_sync(0xffffffffu, ok);
 }
 

@@ -48,6 +48,21 @@ def test_rows_claimed_more_than_once(dkv, fmt, n):
     cache.close()
 
 
+# ---------------------------------------------------------------- waits
+def test_waits_give_up(dkv):
+    """On a barrier that nothing arrives on, the wait that goes by the clock gives up after 2 ms, and the wait without a clock
+    (all of the chunks' roles but one) with it; the host reads the status, and the cache's attention still runs."""
+    st, el = dkv.dkv_selftest_wait_timeout(2000)
+    assert st == 6 and 2_000_000 <= el < 100_000_000, (st, el)
+    c = R.Case([(40, 300)], 1, 128, 32, "bf16", seed=1)
+    cache, s = c.cache(dkv), c.device_seqs(dkv)
+    Q = R.bf16(np.random.default_rng(0).standard_normal((2, 40, 128)))
+    out = cache.attend(dev(Q), s, max_rows=40)
+    cache.sync()
+    R.check(out, R.attend(c, Q))
+    cache.close()
+
+
 # ---------------------------------------------------------------- scratch
 @pytest.mark.parametrize("rows", [1, 200])
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
