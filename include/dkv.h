@@ -548,7 +548,8 @@ size_t dkv_cache_attend_scratch_size(dkv_cache_t cache, int32_t n_seq, int32_t H
  *             call's work has completed.
  * A token that sees no position (a negative position of its own, an empty sequence) gets
  * zeros, and so does one whose scores are all -infinity.  Rows from row_start[n_seq] on are left as they were.  What lies in places that a
- * token does not see, NaN and infinities too, does not reach its output.  Scores, sums and
+ * token does not see, NaN and infinities too, does not reach its output; a value that is not
+ * finite in a place that it does see makes its output infinite or NaN.  Scores, sums and
  * outputs are held in fp32; the weights are rounded to bf16 before they meet the values.  (Over an e4m3
  * cache a call of few rows meets its keys with queries in fp16, each row times a power of two: of a row's elements those
  * smaller than 2^-24 of its largest magnitude are rounded, to within 2^-32 of that.)

@@ -140,6 +140,56 @@ struct Item {
 
 __host__ __device__ __forceinline__ int tile_of(const Item& it, int i) { return i < it.ns ? i : it.w0 + (i - it.ns); }
 
+// What the tokens of one query tile see, in key tiles: tile kt has a key that some row sees if
+// kt < any_end and (kt >= any_lo or kt < any_sk), and every row sees all of it if
+// kt < all_end and (kt >= all_lo or kt < all_sk).
+struct Span {
+  int n;                          // tokens with a position among them, 0: none
+  int any_end, any_lo, any_sk;
+  int all_end, all_lo, all_sk;
+  int lo, end, sk;                // in positions: the first token's window, the last one's end and sinks
+};
+
+__host__ __device__ __forceinline__ Span span_of(const Mask& m, int tokens, int p0, int len, int g, int TQ) {
+  Span s{};
+  const int at = g * TQ, n = min(tokens - at, TQ), pf = p0 + at, pl = pf + n - 1;
+  if (n <= 0 || pl < 0) return s;
+  s.n = n;
+  const int e0 = visible_end(m, max(pf, 0), len), l1 = window_first(m, visible_end(m, pl, len));
+  s.end = visible_end(m, pl, len);
+  s.lo = window_first(m, e0);
+  s.sk = m.window ? min(m.sinks, s.end) : 0;
+  s.any_end = (s.end + BK - 1) / BK;
+  s.any_lo = s.lo / BK;
+  s.any_sk = (s.sk + BK - 1) / BK;
+  s.all_end = pf >= 0 ? e0 / BK : 0;
+  s.all_lo = (l1 + BK - 1) / BK;
+  s.all_sk = m.window ? m.sinks / BK : 0;
+  return s;
+}
+
+__host__ __device__ __forceinline__ bool active(const Span& s, int kt) {
+  return kt < s.any_end && (kt >= s.any_lo || kt < s.any_sk);
+}
+__host__ __device__ __forceinline__ bool all_seen(const Span& s, int kt) {
+  return kt < s.all_end && (kt >= s.all_lo || kt < s.all_sk);
+}
+
+// Key tiles that one query tile of a unit sees whole and in which the other one does not: the kernel treats values that are
+// not finite there as in a tile that both see partly, so that what becomes of them is no matter of who comes first.  (The
+// second tile's tokens lie behind the first one's, and so do the ends of their windows: seen whole by the second, it is the
+// first one's ends that cut a tile; by the first, the beginning of the second one's window and its last sinks.)
+struct Edges {
+  int from, to, sink;   // tiles [from, to) and sink
+};
+__host__ __device__ __forceinline__ Edges edges_of(const Span& other, int g) {   // other: of tile 1 - g
+  if (other.n == 0) return Edges{0, 0, -1};
+  if (g == 1) return Edges{other.all_end, other.any_end, -1};
+  return Edges{max(other.any_lo, other.all_sk), other.all_lo,
+               other.any_sk > other.all_sk && other.all_lo > other.all_sk ? other.all_sk : -1};
+}
+__host__ __device__ __forceinline__ bool in(const Edges& e, int kt) { return (kt >= e.from && kt < e.to) || kt == e.sink; }
+
 // The list of a unit's key tiles: ns, w0 and how many in all; lo and end of what its rows see beside the sinks.
 struct List {
   int ns, w0, n, lo, end, sk;

@@ -22,8 +22,9 @@
 // issued while the previous one's outputs are still being stored.
 //
 // Values in places that a row does not see meet its weight 0, and 0 times a NaN or an infinity
-// is NaN.  So in a tile that some row does not see whole, the softmax warps first clear what is
-// not finite in V's tile; rows that do see such a value get it back at the end (wild_masks).
+// is NaN.  So in a tile that some row of either query tile does not see whole, the softmax warps first clear what is
+// not finite in V's tile, those of both (each before its own product); rows that do see such a value get it back at
+// the end (wild_masks).
 //
 // Measured: 4,680 tokens of 40 heads over 14,040 keys in bf16 817 us, 1.65 PFLOP/s of 1.92 (tensor pipe 70% active; of a
 // key tile's 2,960 cycles the issuing warp waits 480; back to back 882, at the power limit).  12 heads' block over its
@@ -77,40 +78,6 @@ struct Lay {
   static_assert(BYTES <= 227 * 1024, "shared memory per CTA");
 };
 
-// What the tokens of one query tile see, in key tiles: tile kt has a key that some row sees if
-// kt < any_end and (kt >= any_lo or kt < any_sk), and every row sees all of it if
-// kt < all_end and (kt >= all_lo or kt < all_sk).
-struct Span {
-  int n;                          // tokens with a position among them, 0: none
-  int any_end, any_lo, any_sk;
-  int all_end, all_lo, all_sk;
-  int lo, end, sk;                // in positions: the first token's window, the last one's end and sinks
-};
-
-__device__ __forceinline__ Span span_of(const Mask& m, int tokens, int p0, int len, int g, int TQ) {
-  Span s{};
-  const int at = g * TQ, n = min(tokens - at, TQ), pf = p0 + at, pl = pf + n - 1;
-  if (n <= 0 || pl < 0) return s;
-  s.n = n;
-  const int e0 = visible_end(m, max(pf, 0), len), l1 = window_first(m, visible_end(m, pl, len));
-  s.end = visible_end(m, pl, len);
-  s.lo = window_first(m, e0);
-  s.sk = m.window ? min(m.sinks, s.end) : 0;
-  s.any_end = (s.end + BK - 1) / BK;
-  s.any_lo = s.lo / BK;
-  s.any_sk = (s.sk + BK - 1) / BK;
-  s.all_end = pf >= 0 ? e0 / BK : 0;
-  s.all_lo = (l1 + BK - 1) / BK;
-  s.all_sk = m.window ? m.sinks / BK : 0;
-  return s;
-}
-
-__device__ __forceinline__ bool active(const Span& s, int kt) {
-  return kt < s.any_end && (kt >= s.any_lo || kt < s.any_sk);
-}
-__device__ __forceinline__ bool all_seen(const Span& s, int kt) {
-  return kt < s.all_end && (kt >= s.all_lo || kt < s.all_sk);
-}
 // ------------------------------------------------------------------ the items
 // A count in scratch memory that nobody has cleared: call << CHUNK_COUNT_BITS | count once somebody has put that there.  One more;
 // the count before it.
@@ -646,6 +613,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
       const Item& x = items[ni & 1];
       if (x.state == 0) break;
       const Span sp = span_of(j.m, x.n, x.p0, x.len, g, j.TQ);
+      const Edges others = edges_of(span_of(j.m, x.n, x.p0, x.len, 1 - g, j.TQ), g);
       const int p = x.p0 + g * j.TQ + tok;                // the row's position
       const int end = p >= 0 ? visible_end(j.m, p, x.len) : 0, lo = window_first(j.m, end);
       const int sk = j.m.window ? j.m.sinks : 0;
@@ -655,7 +623,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 1)
         const int kt = tile_of(x, i);
         if (!active(sp, kt)) continue;
         const bool partial = !all_seen(sp, kt);
-        if (partial) {
+        if (partial || in(others, kt)) {
           const uint32_t t = tc + (uint32_t)(i - x.i0);
           if (!(ok = mbar_wait_warp_short(v_full + t % L::NV, (t / L::NV) & 1, abort_flag))) break;
           if (!E4M3 || nan_rows[t % L::NV] != 0) clear_row<D>(smem + L::V + (t % L::NV) * L::TB, r, wild + (ni & 1), (int)ni + 1);

@@ -239,11 +239,57 @@ static int check_claims() {
   return 0;
 }
 
+// What the query tiles of a sequence's units see: key tiles that some token sees a key of, that all see all of.
+static int check_spans(int n, int L, int G, Mask m) {
+  const int TQ = BQ / G;
+  for (int t0 = 0; t0 < n; t0 += 2 * TQ) {
+    const int k = n - t0 < 2 * TQ ? n - t0 : 2 * TQ, p0 = L - n + t0;
+    const Span sp[2] = {span_of(m, k, p0, L, 0, TQ), span_of(m, k, p0, L, 1, TQ)};
+    const Edges others[2] = {edges_of(sp[1], 0), edges_of(sp[0], 1)};
+    for (int kt = 0; kt * BK < L; ++kt) {
+      bool some[2] = {false, false}, every[2] = {true, true};
+      for (int i = 0; i < k; ++i) {
+        const int g = i / TQ, p = p0 + i;
+        if (p < 0) {
+          every[g] = false;
+          continue;
+        }
+        const int64_t e0 = m.block ? ((int64_t)p / m.block + 1) * m.block : L;
+        const int end = e0 < L ? (int)e0 : L, lo = m.window && m.window < end ? end - m.window : 0;
+        const int a = kt * BK, z = a + BK, sk = m.window ? m.sinks : 0;
+        some[g] |= a < end && (z > lo || a < sk);
+        every[g] &= z <= end && (a >= lo || z <= sk);   // (by window and sinks together: counts as partly)
+      }
+      bool partly = false;
+      for (int g = 0; g < 2; ++g) {
+        if (some[g] && !active(sp[g], kt)) return 1;
+        if (active(sp[g], kt) && all_seen(sp[g], kt) && !every[g]) return 2;
+        partly |= active(sp[g], kt) && !all_seen(sp[g], kt);
+      }
+      for (int g = 0; g < 2; ++g)                       // both treat a tile as one does
+        if (active(sp[g], kt) && (!all_seen(sp[g], kt) || in(others[g], kt)) != partly) return 3;
+    }
+  }
+  return 0;
+}
+
 static Mask mask(int window, int sinks, int block) { return Mask{1.f, window, sinks, block, inverse_of(block)}; }
 
 int main(int argc, char** argv) {
   if (argc == 1) return check_slots();
   if (argc == 2) return check_claims();
+  if (argc == 4) {
+    std::mt19937 g(atoi(argv[1]));
+    auto upto = [&](int lo, int hi) { return lo + (int)(g() % (unsigned)(hi - lo + 1)); };
+    for (int i = 0; i < atoi(argv[2]); ++i) {
+      const int G = upto(1, 3) < 3 ? upto(1, 8) : 1, n = upto(1, 700), L = upto(0, 9) ? n + upto(0, 1500) : upto(0, n);
+      const int window = upto(0, 4) ? upto(1, 1500) : 0, sinks = upto(0, 2) ? upto(0, 1500) : 0;
+      const int kind = upto(0, 4), block = kind == 0 ? 0 : kind < 3 ? 1 : upto(2, 600);
+      if (int e = check_spans(n, L, G, mask(window, sinks, block)))
+        return printf("case %d: %d (%d tokens of %d, groups of %d, window %d, sinks %d, block %d)\n", i, e, n, L, G, window, sinks, block), 1;
+    }
+    return 0;
+  }
   Seen seen{};
   // one unit in the middle straddles two blocks and sees more than the first and the last one
   if (int e = check({{824, 11264}}, 8, 1, 152, mask(2048, 0, 512), seen)) return printf("straddling unit: %d\n", e), 1;
@@ -304,3 +350,11 @@ def test_places_that_no_item_stored(walk):
 def test_rows_claimed_more_than_once(walk):
     """A row_start that goes back and forth gives every other sequence all rows: the call's work stays that of its rows."""
     assert subprocess.run([walk, "claims"], timeout=60).returncode == 0
+
+
+@pytest.mark.parametrize("seed", range(2))
+def test_tiles_that_are_seen(walk, seed):
+    """Which key tiles a query tile sees, in part and whole, and that both query tiles of a unit agree on those in which
+    some row's view ends."""
+    r = subprocess.run([walk, str(seed), "3000", "spans"], capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0, r.stdout + r.stderr

@@ -48,6 +48,39 @@ def test_rows_claimed_more_than_once(dkv, fmt, n):
     cache.close()
 
 
+# ---------------------------------------------------------------- infinities at no weight
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,mask", [(1, dict(window=700)), (1, dict(block=128, window=640)), (3, dict(window=300, sinks=200)),
+                                     (1, dict())])
+def test_infinities_at_no_weight_repeat(dkv, fmt, Hq, mask):
+    """Values that are not finite where the weights have fallen to 0 (keys 150 nats below the others): whatever a token
+    that sees them gets, it gets every time, also where half of its unit sees less of the keys around them."""
+    n, L = 512, 1500
+    c = R.Case([(n, L)], 1, 128, 64, "bf16", seed=3)
+    c.fmt = fmt
+    g = np.random.default_rng(4)
+    for j in range(L - n - 800, L, 16):
+        p, sl = c.table[0, j // 64], j % 64
+        c.v[p, 0, sl, g.integers(0, 128)] = [np.inf, -np.inf][j // 16 % 2] if fmt == "bf16" else np.nan
+        c.k[p, 0, sl] = 0.0
+        c.k[p, 0, sl, 0] = -100.0
+    if fmt == "e4m3":
+        quantised(c)
+    Q = R.bf16(g.standard_normal((Hq, n, 128)))
+    Q[:, :, 0] = 17.0                                   # -100 * 17 / sqrt(128) = -150
+    cache, s = c.cache(dkv), c.device_seqs(dkv)
+    q, first = dev(Q), None
+    other = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    for i in range(60):
+        if i % 3 == 1:
+            other.add_(1)                               # (the pages come from HBM again, or beside other work)
+        out = cache.attend(q, s, max_rows=n, **mask).view(torch.int16)
+        first = out.clone() if first is None else first
+        assert torch.equal(out, first), i
+    cache.sync()
+    cache.close()
+
+
 # ---------------------------------------------------------------- waits
 def test_waits_give_up(dkv):
     """On a barrier that nothing arrives on, the wait that goes by the clock gives up after 2 ms, and the wait without a clock
