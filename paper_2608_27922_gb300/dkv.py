@@ -675,6 +675,9 @@ class PagedCache:
         n_seq, Hq, rows, scale, window, sinks, block, max_rows = key
         if scale is not None and not scale > 0.0:
             raise ValueError("scale: expected a positive number")
+        for name, x in (("window", window), ("sinks", sinks), ("block", block)):
+            if not -2 ** 31 <= x < 2 ** 31:            # (ctypes would take it modulo 2^32)
+                raise ValueError(f"{name}: expected a 32-bit integer, got {x}")
         most = rows if max_rows is None else min(int(max_rows), rows)
         size = int(lib().dkv_cache_attend_scratch_size(self.handle, n_seq, Hq, rows, most))
         how = dkv_cache_attend_t(0.0 if scale is None else scale, window, sinks, block, most)
