@@ -467,7 +467,9 @@ dkv_status_t dkv_candidate_order_noalloc(const void* K_bank, const float* base, 
  * sequences together claim more rows than it has, row_start going back and forth, writes no outputs.)
  *
  * Packed tensors are [heads][rows][d] bf16 with any strides (in elements) between heads and
- * rows that are multiples of 8; d is contiguous and the address 16-byte aligned.
+ * rows that are multiples of 8; d is contiguous and the address 16-byte aligned.  The strides of
+ * outputs are d at least, those of queries not 0; K and V of a write may be broadcast (0).  (A
+ * stride between one row or one head is not looked at.)
  *
  * A handle keeps no state between calls but the error word.  Calls on it may run at once
  * on several streams, in graphs too, each attend with scratch of its own; a write and the

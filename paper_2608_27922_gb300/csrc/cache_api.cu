@@ -72,14 +72,14 @@ dkv_status_t check_seqs(const cache::Pool& c, const dkv_cache_seqs_t* s, int32_t
   return DKV_OK;
 }
 
-// A packed tensor's address and strides; a stride between one row or head says nothing.
-dkv_status_t check_packed(const void* p, int heads, int rows, int64_t head, int64_t row, bool distinct,
-                          cache::Packed* out) {
+// A packed tensor's address and strides, the least of which is `least`; a stride between one row or head says nothing.
+// Inputs of the write may be broadcast (0), queries come by TMA, whose strides are not 0, and the rows of outputs lie apart.
+dkv_status_t check_packed(const void* p, int heads, int rows, int64_t head, int64_t row, int64_t least, cache::Packed* out) {
   if (!p || !aligned(p, 16)) return DKV_ERR_ARG;
   if (heads == 1) head = 0;
   if (rows == 1) row = 0;
   if (head < 0 || row < 0 || head % 8 || row % 8) return DKV_ERR_ARG;
-  if (distinct && ((heads > 1 && head == 0) || (rows > 1 && row == 0))) return DKV_ERR_ARG;
+  if ((heads > 1 && head < least) || (rows > 1 && row < least)) return DKV_ERR_ARG;
   *out = cache::Packed{const_cast<void*>(p), head, row};
   return DKV_OK;
 }
@@ -132,8 +132,8 @@ dkv_status_t dkv_cache_write(dkv_cache_t c, const dkv_cache_seqs_t* seqs, const 
   cache::Seqs s;
   cache::Packed k, v;
   dkv_status_t st = check_seqs(c->pool, seqs, rows, &s);
-  if (st == DKV_OK) st = check_packed(K, c->pool.H, rows, k_head, k_row, false, &k);
-  if (st == DKV_OK) st = check_packed(V, c->pool.H, rows, v_head, v_row, false, &v);
+  if (st == DKV_OK) st = check_packed(K, c->pool.H, rows, k_head, k_row, 0, &k);
+  if (st == DKV_OK) st = check_packed(V, c->pool.H, rows, v_head, v_row, 0, &v);
   if (st != DKV_OK) return st;
   OnDevice on(c->device);
   if (!on.ok) return DKV_ERR_CUDA;
@@ -148,8 +148,8 @@ dkv_status_t dkv_cache_read(dkv_cache_t c, const dkv_cache_seqs_t* seqs, const i
   cache::Seqs s;
   cache::Packed k, v;
   dkv_status_t st = check_seqs(c->pool, seqs, rows, &s);
-  if (st == DKV_OK) st = check_packed(K, c->pool.H, rows, k_head, k_row, true, &k);
-  if (st == DKV_OK) st = check_packed(V, c->pool.H, rows, v_head, v_row, true, &v);
+  if (st == DKV_OK) st = check_packed(K, c->pool.H, rows, k_head, k_row, c->pool.d, &k);
+  if (st == DKV_OK) st = check_packed(V, c->pool.H, rows, v_head, v_row, c->pool.d, &v);
   if (st != DKV_OK) return st;
   OnDevice on(c->device);
   if (!on.ok) return DKV_ERR_CUDA;
@@ -175,8 +175,8 @@ dkv_status_t dkv_cache_attend(dkv_cache_t c, const dkv_cache_seqs_t* seqs, const
   if (H_q < c->pool.H || H_q % c->pool.H || H_q / c->pool.H > kMaxGroup) return DKV_ERR_SHAPE;
   if (how->window < 0 || how->sinks < 0 || how->block < 0 || how->max_rows < 1 || !std::isfinite(how->scale))
     return DKV_ERR_ARG;
-  st = check_packed(Q, H_q, rows, q_head, q_row, true, &q);
-  if (st == DKV_OK) st = check_packed(O, H_q, rows, o_head, o_row, true, &o);
+  st = check_packed(Q, H_q, rows, q_head, q_row, 8, &q);
+  if (st == DKV_OK) st = check_packed(O, H_q, rows, o_head, o_row, c->pool.d, &o);
   if (st != DKV_OK) return st;
   const int max_rows = how->max_rows < rows ? how->max_rows : rows;
   if (scratch_bytes < scratch_of(c->pool, H_q, max_rows)) return DKV_ERR_NOMEM;

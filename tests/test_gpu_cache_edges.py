@@ -206,6 +206,32 @@ def test_many_small_weights(dkv, n, H, Hq):
     attend_and_check(dkv, c, Hq, Q, n)
 
 
+# ---------------------------------------------------------------- strides
+def test_outputs_that_overlap_are_refused(dkv):
+    """Rows or heads of an output that begin inside one another: no order of the writes could make them right.  Keys and
+    values of a write may be one row for all."""
+    H, d, n = 2, 64, 5
+    c = R.Case([(n, 20)], H, d, 16, "bf16")
+    cache, s = c.cache(dkv), c.device_seqs(dkv)
+    Q = torch.zeros(H, n, d, dtype=torch.bfloat16, device="cuda")
+    flat = torch.zeros(4096, dtype=torch.bfloat16, device="cuda")
+    first = torch.zeros(1, dtype=torch.int32, device="cuda")
+    for strides in ((n * d, d - 8, 1), (d - 16, H * d, 1), (8, 8, 1), (n * d, 0, 1), (0, d, 1)):
+        bad = torch.as_strided(flat, (H, n, d), strides)
+        for call in (lambda: cache.attend(Q, s, out=bad), lambda: cache.read(s, first, n, out=(bad, Q)),
+                     lambda: cache.read(s, first, n, out=(Q, bad))):
+            with pytest.raises(dkv.DkvError) as e:
+                call()
+            assert e.value.status == 1
+    one = dev(R.bf16(np.random.default_rng(0).standard_normal((1, 1, d))))
+    cache.write(one.expand(H, n, d), one.expand(H, n, d), s)
+    k, v = cache.read(s, torch.full_like(first, 20 - n), n)
+    cache.sync()
+    assert torch.equal(k, one.expand(H, n, d)) and torch.equal(v, k)
+    assert not bool(flat.any())
+    cache.close()
+
+
 # ---------------------------------------------------------------- cut units
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("seqs,H,Hq,mask", [
