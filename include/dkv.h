@@ -562,7 +562,8 @@ dkv_status_t dkv_cache_attend(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, c
                               void* scratch, size_t scratch_bytes, void* stream);
 
 /* Waits for the stream of the handle's last call, then reports and clears the error word
- * (as dkv_bank_sync).  After DKV_ERR_TIMEOUT the scratch of a captured attend call is cleared
+ * (as dkv_bank_sync).  Calls on other streams and replayed graphs are the caller's to wait for: what
+ * they find wrong later is reported by a later sync.  After DKV_ERR_TIMEOUT the scratch of a captured attend call is cleared
  * before the graph is replayed: a call that gave up may leave its counts in it.            */
 dkv_status_t dkv_cache_sync(dkv_cache_t cache);
 

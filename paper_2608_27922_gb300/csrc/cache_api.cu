@@ -51,8 +51,8 @@ bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 
 // Which attention kernel: the one for few rows where a sequence's tokens and the heads that share a key head make
 // no more than ROWS_MOST, the most rows that read a key once there (16 rows a unit).  32 sequences of 5,000
-// positions, 8 key heads, few rows against tensor cores: with 16 rows 124 us against 123 in bf16 and 86 against 153 in
-// e4m3, with 25 or 32 rows 223 against 125 and 152 against 153 (the keys are read twice); a single such sequence 27
+// positions, 8 key heads, few rows against tensor cores: with 16 rows 125 us against 126 in bf16 and 88 against 156 in
+// e4m3, with 25 or 32 rows 225 against 127 and 157 against 158 (the keys are read twice); a single such sequence 27
 // to 30 us either way.
 constexpr int ROWS_MOST = 16;
 bool few_rows(const cache::Pool& c, int Hq, int max_rows) { return (int64_t)max_rows * (Hq / c.H) <= ROWS_MOST; }

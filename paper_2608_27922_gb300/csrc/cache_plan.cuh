@@ -111,7 +111,8 @@ constexpr int64_t NEAR = 192 << 20;
 constexpr int MAX_CUT = 32;              // parts of one unit
 constexpr int MIN_PART = 4;              // key tiles of a part, at least (256 tokens over 2,256 keys, 8 heads: with 4 27 us, 2 28, 8 32)
 // What an item costs beside its key tiles, a part (which stores its outputs in 32 bits) more than that, and the joining of
-// parts, in key tiles (1.6 us each at two query tiles of 128 dimensions)
+// parts, in key tiles (1.6 us each at two query tiles of 128 dimensions; with 64 a tile takes about two thirds of that, and
+// the same numbers are used)
 constexpr int ITEM_TILES = 2, PART_TILES = 2, JOIN_TILES = 6;
 
 struct Job {

@@ -30,7 +30,7 @@
 // (With fp16 weights, whose sums had to be kept apart, 32 tokens of 40 on 8 heads took as long: 70.6 us a call for 70.4.)
 //
 // Measured: one token of 12 heads over 131,001 positions in bf16 127 us, 6.3 TB/s of the 6.8 that a copy reaches (in
-// e4m3 77 us, 5.3); 32 tokens of 40 on 8 heads over up to 9,360 positions in e4m3 68 us (5.1 TB/s), in bf16 113 (6.1).
+// e4m3 75 us, 5.4); 32 tokens of 40 on 8 heads over up to 9,360 positions in e4m3 68 us (5.1 TB/s), in bf16 115 (6.0).
 // About 9 us of each are fixed (reading the arrays, the first keys' way, the joining): one token over 1,561 positions 11 us.
 #include "attn_math.cuh"
 #include "cache_internal.h"

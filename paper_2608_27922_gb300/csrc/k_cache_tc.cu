@@ -27,8 +27,8 @@
 // the end (wild_masks).
 //
 // Measured: 4,680 tokens of 40 heads over 14,040 keys in bf16 817 us, 1.65 PFLOP/s of 1.92 (tensor pipe 70% active; of a
-// key tile's 2,960 cycles the issuing warp waits 480; back to back 882, at the power limit).  12 heads' block over its
-// window of 14,040 keys in e4m3 342 us, 1.18 PFLOP/s (pipe 52%, issue slots 59%), in bf16 270.  A call of one item a
+// key tile's 2,960 cycles the issuing warp waits 480; back to back 880, at the power limit).  12 heads' block over its
+// window of 14,040 keys in e4m3 343 us, 1.18 PFLOP/s (pipe 52%, issue slots 59%), in bf16 271.  A call of one item a
 // CTA takes about 13 us beside its key tiles, and an item after another 3,000 cycles of outputs.
 #include "attn_math.cuh"
 #include "cache_internal.h"
