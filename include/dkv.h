@@ -68,7 +68,7 @@ typedef enum {
   DKV_ERR_SHAPE = 2,        /* size outside what the handle / library supports           */
   DKV_ERR_STATE = 3,        /* call out of order (admit twice, compress without admit)   */
   DKV_ERR_CUDA = 4,         /* a CUDA runtime call or launch failed                      */
-  DKV_ERR_NOMEM = 5,        /* workspace smaller than dkv_bank_workspace_size_ex()       */
+  DKV_ERR_NOMEM = 5,        /* workspace smaller than dkv_bank_workspace_size_ex(); pages  */
   DKV_ERR_TIMEOUT = 6,      /* a bounded device-side wait gave up (sticky, see sync)     */
   DKV_ERR_UNSUPPORTED = 7,  /* feature not available for this dtype / d / device         */
   DKV_ERR_DEVICE = 8        /* device-side consistency check failed (sticky, see sync)   */
@@ -435,6 +435,42 @@ dkv_status_t dkv_candidate_order_noalloc(const void* K_bank, const float* base, 
                                          float* scores_out, int32_t* perm_out, void* stream);
 
 /* ------------------------------------------------------------------------------------
+ * Norm and rotation of queries and keys.
+ *
+ * The backbones norm the queries and keys of each head and rotate them to their token's
+ * position before attention reads them and before the window keeps them (App. A,
+ * "Attention-logit" setup: keys are post-RoPE).  Both in one pass, for a row x of d values
+ * of one head at coordinates c:
+ *     y = x w / sqrt(mean(x^2) + eps)                 (norm = 0: y = x)
+ *     pair (y0, y1) -> (y0 cos a - y1 sin a, y0 sin a + y1 cos a),   a = c[axis] theta[pair]
+ * in fp32, rounded once to bf16 (to nearest, ties to even).  Angles are reduced to one turn in 64-bit whole numbers
+ * and off by no more than 2^-22 + |a| 2^-51 radians, at any coordinate.  The squares of a row whose sum passes fp32
+ * are taken again at a smaller scale; a row that holds a NaN or an infinity gives NaN.  dkv_bank_admit_rope takes the
+ * temporal rotation off again.                                                            */
+typedef struct {
+  const float* theta;      /* device [d / 2] angular frequency of each rotation pair, finite; 0: not
+                              rotated                                                      */
+  const float* q_weight;   /* device [d] fp32, NULL: ones (ignored with norm = 0)          */
+  const float* k_weight;
+  float eps;               /* > 0 and finite (ignored with norm = 0)                       */
+  int32_t norm;            /* 1: root-mean-square norm of each row; 0: none                */
+  int32_t layout;          /* dkv_rope_layout_t                                            */
+  int32_t n_axes;          /* 1 .. 4 coordinates of a token (time, row, column)            */
+  int32_t axis_pairs[4];   /* pairs that follow each axis, in order; together d / 2        */
+} dkv_norm_rope_t;
+
+/* Qo[h][i] := norm and rotation of Q[h][i], and the same for Ko and K (with k_weight).
+ *   coord : device int32 [n_axes][rows], the coordinates of every row's token.
+ *   Q, Qo : device [H_q][rows][d] bf16, K, Ko : [H_k][rows][d]; strides as those of a packed tensor below (inputs may be
+ *           broadcast); d in {64, 128}; 1 <= rows <= 1<<20; 0 <= H_q, H_k <= 4096, not both 0 (Q or K is
+ *           then ignored).  An output may be its input, with the same strides; it must not overlap it in other ways.
+ * Runs on the current device.                                                             */
+dkv_status_t dkv_norm_rope(int32_t d, const dkv_norm_rope_t* how, const int32_t* coord, int32_t rows, int32_t H_q,
+                           const void* Q, int64_t q_head_stride, int64_t q_row_stride, void* Qo, int64_t qo_head_stride,
+                           int64_t qo_row_stride, int32_t H_k, const void* K, int64_t k_head_stride, int64_t k_row_stride,
+                           void* Ko, int64_t ko_head_stride, int64_t ko_row_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------
  * Paged cache of the window's keys and values.
  *
  * The window that attention reads beside the bank (Sec. 4.1, App. D: one sink frame and
@@ -561,8 +597,147 @@ dkv_status_t dkv_cache_attend(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, c
                               int64_t o_head_stride, int64_t o_row_stride, const dkv_cache_attend_t* how,
                               void* scratch, size_t scratch_bytes, void* stream);
 
+/* dkv_norm_rope for the newest tokens, whose keys go straight into their pages: Qo[h][i] := norm and
+ * rotation of Q[h][i]; the cache gets the normed and rotated keys (rounded to bf16, then as dkv_cache_write
+ * stores them) and the values as they are.
+ *   coord : device int32 [n_axes][rows], or NULL with one axis: a token's position in its sequence.
+ *   Q, Qo : device [H_q][rows][d] (H_q = 0: ignored; 0 <= H_q <= 4096); K, V : device [H][rows][d].
+ * Rows from row_start[n_seq] on are left as they were in Qo, and ignored otherwise; a token at a negative
+ * position gets its query but is not stored.                                              */
+dkv_status_t dkv_cache_write_norm_rope(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const dkv_norm_rope_t* how,
+                                       const int32_t* coord, int32_t rows, int32_t H_q, const void* Q, int64_t q_head_stride,
+                                       int64_t q_row_stride, void* Qo, int64_t qo_head_stride, int64_t qo_row_stride,
+                                       const void* K, int64_t k_head_stride, int64_t k_row_stride, const void* V,
+                                       int64_t v_head_stride, int64_t v_row_stride, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Pages of several sequences: forked, grown, given back, compacted.
+ *
+ * refs (device int32 [n_pages], 16-byte aligned) counts for every page the table entries that name it; a page
+ * is free when nobody does.  The calls below keep it and the tables in step, on the device and
+ * without the host: a program begins with refs all 0, tables all -1 and lengths 0.  Sequence b's table
+ * row holds its pages in the entries 0 .. ceil(length / page_len) - 1 but for those given back in the
+ * middle, and negative numbers everywhere else.  Fresh pages are the lowest free ones, in the order
+ * (sequence, entry), so that what a call does follows from its arrays alone.
+ *
+ * What contradicts itself (a page outside the pool, a held page that refs calls free, a length outside the
+ * table, a negative number of tokens) sets the sticky error word (DKV_ERR_DEVICE); too few free pages
+ * set it to DKV_ERR_NOMEM.  extend and compact look first and then do nothing at all; fork and release leave out what
+ * names no page.  Calls stay inside their buffers in every case.  refs, tables and
+ * lengths are changed by one call at a time (the caller orders the streams).              */
+typedef struct {
+  int32_t* block_table;    /* device [n_seq][max_pages]                                    */
+  int32_t* seq_len;        /* device [n_seq]                                               */
+  int32_t n_seq;           /* 1 .. 4096                                                    */
+  int32_t max_pages;       /* >= 1, max_pages * page_len <= 2^30                           */
+} dkv_cache_table_t;
+
+/* Sequence i of `to` goes on from sequence parent[i] of `from` (device int32 [to->n_seq]; -1: it is empty), sharing its
+ * pages; `from` is given up, and its pages with it where no child holds them.  One call forks, reorders, drops
+ * and frees sequences: any map will do.  Needs to->max_pages >= from->max_pages; the two tables (and lengths)
+ * must not overlap.  Every entry of `to` is written.                                      */
+dkv_status_t dkv_cache_fork(dkv_cache_t cache, int32_t* refs, const dkv_cache_table_t* from, const int32_t* parent,
+                            const dkv_cache_table_t* to, void* stream);
+
+/* Room for add[b] (device int32 [n_seq], >= 0) more positions of every sequence: fresh pages for them, seq_len[b] +=
+ * add[b].  A partly filled last page that the new positions begin on is first made the sequence's own: where
+ * other entries hold it too, its filled rows (keys, values, scales) are copied to a fresh page. (Of sequences that share it,
+ * and are all in the call with add > 0, the last one keeps the page itself.)  add[b] = 0 leaves sequence b alone.
+ * scratch : device, 256-byte aligned, >= dkv_cache_extend_scratch_size(cache, n_seq), in use until the call's work is done. */
+size_t dkv_cache_extend_scratch_size(dkv_cache_t cache, int32_t n_seq);
+dkv_status_t dkv_cache_extend(dkv_cache_t cache, int32_t* refs, const dkv_cache_table_t* seqs, const int32_t* add,
+                              void* scratch, size_t scratch_bytes, void* stream);
+
+/* Gives back the pages of sequence b all of whose held positions lie in [first[b], last[b]) (device int32 [n_seq]): their
+ * entries become -1.  Where last[b] >= seq_len[b] the sequence ends at first[b] (rejected tokens; first = 0: all of
+ * it); else its length stays, and later calls must not touch the positions given back (those that a
+ * window has left).                                                                       */
+dkv_status_t dkv_cache_release(dkv_cache_t cache, int32_t* refs, const dkv_cache_table_t* seqs, const int32_t* first,
+                               const int32_t* last, void* stream);
+
+/* Position i of sequence b of `to` := position keep[keep_start[b] + i] of sequence b of `from`, for the positions kept (any
+ * order, the same one more than once too); `from` is given up.  Leading pages whose positions all stay in place are
+ * kept as they are, the others are fresh ones and their rows copied, so the pool has to hold both for
+ * the time being.  Keys keep the rotation that they have.
+ *   keep : device int32 [n_keep], keep_start : device int32 [n_seq + 1], ascending from 0 to at most n_keep;
+ *   0 <= n_keep <= 2^26.  from->n_seq = to->n_seq; tables as for dkv_cache_fork.
+ * A kept position outside [0, seq_len[b]) or on a page that was given back is an error (the call does nothing).
+ * scratch : as for extend, dkv_cache_compact_scratch_size(cache, n_seq).                  */
+size_t dkv_cache_compact_scratch_size(dkv_cache_t cache, int32_t n_seq);
+dkv_status_t dkv_cache_compact(dkv_cache_t cache, int32_t* refs, const dkv_cache_table_t* from, const int32_t* keep,
+                               int32_t n_keep, const int32_t* keep_start, const dkv_cache_table_t* to, void* scratch,
+                               size_t scratch_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------
+ * Attention over chosen pages.
+ *
+ * A long past need not be read whole: an 8-bit mean key of every page and head tells which pages a token's
+ * queries point to, and attention reads those.
+ *
+ *   dkv_cache_summarise       summaries of pages, after their positions have been written
+ *   dkv_cache_choose          for each tile of tokens and key head the pages with the best scores
+ *   dkv_cache_attend_chosen   softmax attention over the listed pages
+ *
+ * Codes of 8 bits: for a row m of d numbers e is the smallest integer >= -50 with max |m| <= 127 2^e and
+ * c = m 2^-e to nearest, ties to even, so m is about c 2^e.  A row that is not finite or reaches 2^40 in magnitude has no codes
+ * (c = 0 and, in a summary, the scale byte 255).
+ *
+ * Tiles.  The n_b tokens of sequence b in a call lie in tiles of `tile` from its first on; tile t has slot
+ * row_start[b] / tile + b + t (rounded down) of [0, rows / tile + n_seq).                 */
+typedef struct {
+  int8_t* code;        /* device [n_pages][H][d], 16-byte aligned                          */
+  uint8_t* scale;      /* device [n_pages][H]: the byte e + 127                            */
+} dkv_cache_summaries_t;
+
+/* Summaries of the pages of sequence b that hold a position >= first[b] (device int32 [n_seq]; NULL: the
+ * positions of the call's tokens): the mean of the page's key rows at positions < seq_len[b] in codes of 8 bits, the
+ * sums exact to 2^-40 of the largest magnitude in a column.  Sequences may share pages that both summarise only where they
+ * hold the same positions of them.                                                        */
+dkv_status_t dkv_cache_summarise(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const int32_t* first,
+                                 const dkv_cache_summaries_t* summaries, void* stream);
+
+typedef struct {
+  int32_t tile;          /* tokens of a tile, 1 .. 128                                     */
+  int32_t block;         /* >= 0: visibility end(p) as in dkv_cache_attend_t               */
+  int32_t sink_pages;    /* >= 0: pages from the sequence's first on that are always listed */
+  int32_t local_pages;   /* >= 1: likewise the pages up to and with the token's own one    */
+  int32_t top;           /* >= 0: pages listed for their score                             */
+  int32_t width;         /* entries of a list, 1 .. 1024, at least
+                            sink_pages + local_pages + (tile + page_len - 2) / page_len + top */
+} dkv_cache_choose_t;
+
+/* lists[h][slot][0 .. width): the pages (indices into the sequence's table row) that the tile attends to in key head h,
+ * ascending, -1 behind the last; -1 in slots of no tile.  With a page "seen" when all its held positions lie before the
+ * end of what the tile's first token sees (end(p), at positions >= 0), they are
+ *   - the local pages: from local_pages - 1 before the first token's page up to the last token's page;
+ *   - seen pages below sink_pages;
+ *   - of the other seen pages the `top` with the best scores, equal ones in the order of their numbers.
+ * score(page) = max over the tile's tokens and the head's group of queries of (c_q . c_page) 2^(e_q + e_page), with Q's rows in
+ * codes of 8 bits like the summaries: whole numbers times powers of two, so every choice is exact.  Queries and pages
+ * without codes count as -infinity, and such a score is not listed.  A tile whose tokens all lie at negative positions has an empty list.
+ *   Q : device [H_q][rows][d] bf16 as for dkv_cache_attend;  lists : device int32 [H][rows / tile + n_seq][width].  */
+dkv_status_t dkv_cache_choose(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const dkv_cache_summaries_t* summaries,
+                              const void* Q, int32_t H_q, int32_t rows, int64_t q_head_stride, int64_t q_row_stride,
+                              const dkv_cache_choose_t* how, int32_t* lists, void* stream);
+
+typedef struct {
+  float scale;           /* of q.k; <= 0 selects 1 / sqrt(d)                               */
+  int32_t tile;          /* of the lists                                                   */
+  int32_t block;         /* as in dkv_cache_attend_t                                       */
+  int32_t width;         /* of the lists, 1 .. 1024                                        */
+} dkv_cache_chosen_t;
+
+/* O[h][i] = sum_j softmax_j(scale Q[h][i] . K[j]) V[j] over the positions j < end(p) on the pages that lists[h / (H_q / H)]
+ * names for the token's tile (a list ends at its first negative entry).  Arguments, masks, numbers that are not
+ * finite, rows that see nothing and rounding as in dkv_cache_attend (over an e4m3 cache the keys are widened to bf16).  Entries that do not ascend or lie
+ * behind the sequence's last page set the error word (DKV_ERR_DEVICE); what the tile's tokens get is then unspecified.  */
+dkv_status_t dkv_cache_attend_chosen(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const void* Q, int32_t H_q,
+                                     int32_t rows, int64_t q_head_stride, int64_t q_row_stride, void* O,
+                                     int64_t o_head_stride, int64_t o_row_stride, const int32_t* lists,
+                                     const dkv_cache_chosen_t* how, void* stream);
+
 /* Waits for the stream of the handle's last call, then reports and clears the error word
- * (as dkv_bank_sync).  Calls on other streams and replayed graphs are the caller's to wait for: what
+ * (as dkv_bank_sync; DKV_ERR_NOMEM: extend or compact found too few free pages).  Calls on other streams and replayed graphs are the caller's to wait for: what
  * they find wrong later is reported by a later sync.  After DKV_ERR_TIMEOUT the scratch of a captured attend call is cleared
  * before the graph is replayed: a call that gave up may leave its counts in it.            */
 dkv_status_t dkv_cache_sync(dkv_cache_t cache);

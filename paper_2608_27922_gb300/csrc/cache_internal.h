@@ -32,6 +32,13 @@ struct Seqs {
   int rows;   // packed rows of the call's tensors
 };
 
+// A table that calls change.
+struct Table {
+  int32_t* table;
+  int32_t* len;
+  int n, max_pages;
+};
+
 // Packed tensors [heads][rows][d].
 struct Packed {
   void* p;
@@ -45,7 +52,7 @@ struct Mask {
 };
 inline uint64_t inverse_of(int block) { return block >= 2 ? ~(uint64_t)0 / (uint64_t)block + 1 : 0; }
 
-enum : int { SITE_ROWS = 1, SITE_LEN = 2, SITE_PAGE = 3, SITE_CHUNK = 4, SITE_PART = 5, SITE_WAIT = 400 };
+enum : int { SITE_ROWS = 1, SITE_LEN = 2, SITE_PAGE = 3, SITE_CHUNK = 4, SITE_PART = 5, SITE_REFS = 6, SITE_LIST = 7, SITE_WAIT = 400 };
 
 // Counts in scratch memory that nobody has cleared: a word is the call's number << COUNT_BITS | a count once a block of
 // the call has put that there, and whatever else it holds is no count yet.  A call clears its counts or leaves them at 0, so
@@ -94,6 +101,20 @@ __host__ __device__ __forceinline__ Seq seq_at(const Pool& c, const Seqs& s, int
   if (a < 0 || z < a || z > s.rows) fail(c.status, DEV_INCONSISTENT, SITE_ROWS);
   if (len < 0 || len > cap) fail(c.status, DEV_INCONSISTENT, SITE_LEN);
   return q;
+}
+
+// Tiles of new tokens: the slots of sequence b begin at row_start[b] / tile + b, which ascends by 1 or more.
+__host__ __device__ __forceinline__ int first_slot(const Seqs& s, int tile, int b) { return clamp(s.row_start[b], 0, s.rows) / tile + b; }
+
+// The sequence whose tiles a slot may be one of: the last b with first_slot(b) <= slot (row starts that do not ascend give
+// some sequence).
+__host__ __device__ __forceinline__ int seq_of_slot(const Seqs& s, int tile, int slot) {
+  int lo = 0, hi = s.n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first_slot(s, tile, mid) <= slot) lo = mid; else hi = mid;
+  }
+  return lo;
 }
 
 // The sequence of a packed row (row < row_start[n]): the last b with row_start[b] <= row.
@@ -149,6 +170,48 @@ struct Maps {
 cudaError_t launch_write(const Pool& c, const Seqs& s, const Packed& k, const Packed& v, cudaStream_t st);
 cudaError_t launch_read(const Pool& c, const Seqs& s, const int32_t* first, const Packed& k, const Packed& v,
                         cudaStream_t st);
+
+// norm and rotation (dkv_norm_rope_t as the kernel takes it)
+struct RopeHow {
+  const int32_t* coord;   // [axes][rows], or null: positions
+  const float* theta;
+  const float* q_weight;
+  const float* k_weight;
+  float eps;
+  int norm, half;
+  int pair_end[3];   // pairs of the axes up to 0, 1, 2 (d / 2 past the last one)
+};
+// (dense: of c only d counts, of s only rows; ko takes the keys.  Else the pages take keys and values)
+cudaError_t launch_norm_rope(const Pool& c, const Seqs& s, bool dense, const RopeHow& how, int Hq, const Packed& q,
+                             const Packed& qo, int Hk, const Packed& k, const Packed& ko, const Packed& v, cudaStream_t st);
+
+// pages
+cudaError_t pages_set_smem_limits();   // on the current device
+size_t extend_scratch(int n_seq);
+size_t compact_scratch(int n_seq);
+cudaError_t launch_fork(const Pool& c, int32_t* refs, const Table& from, const int32_t* parent, const Table& to, cudaStream_t st);
+cudaError_t launch_release(const Pool& c, int32_t* refs, const Table& s, const int32_t* first, const int32_t* last, cudaStream_t st);
+cudaError_t launch_extend(const Pool& c, int32_t* refs, const Table& s, const int32_t* add, void* scratch, cudaStream_t st);
+cudaError_t launch_compact(const Pool& c, int32_t* refs, const Table& from, const int32_t* keep, int n_keep,
+                           const int32_t* keep_start, const Table& to, void* scratch, cudaStream_t st);
+
+// choice of pages and attention over them
+struct Choose {
+  int tile, block, sinks, local, top, width;
+  uint64_t inverse;   // of the block, as Mask's
+};
+struct Chosen {
+  const int32_t* lists;
+  int tile, width, slots;
+};
+cudaError_t choose_set_smem_limits();   // on the current device
+cudaError_t launch_summarise(const Pool& c, const Seqs& s, const int32_t* first, int8_t* code, uint8_t* scale, cudaStream_t st);
+cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, const uint8_t* scale, const Packed& q, int Hq,
+                          const Choose& how, int32_t* lists, cudaStream_t st);
+
+cudaError_t launch_chosen_rows(const Pool& c, const Seqs& s, const Packed& q, const Packed& o, int Hq, const Mask& m,
+                               const Chosen& how, cudaStream_t st);
+
 // chunks of tokens, on the tensor cores
 bool make_tc_maps(const Pool& c, Maps* m);
 cudaError_t attend_tc_set_smem_limits();     // on the current device

@@ -251,7 +251,7 @@ const char* dkv_status_str(dkv_status_t s) {
     case DKV_ERR_SHAPE: return "unsupported shape";
     case DKV_ERR_STATE: return "call out of order";
     case DKV_ERR_CUDA: return "CUDA error";
-    case DKV_ERR_NOMEM: return "workspace too small";
+    case DKV_ERR_NOMEM: return "workspace too small, or too few free pages";
     case DKV_ERR_TIMEOUT: return "device wait timed out";
     case DKV_ERR_UNSUPPORTED: return "unsupported on this device or dtype";
     case DKV_ERR_DEVICE: return "device-side consistency check failed";

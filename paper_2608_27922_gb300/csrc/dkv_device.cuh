@@ -14,7 +14,7 @@
 namespace dkv {
 
 // Device error word codes (mirrors dkv_status_t values for the sticky errors).
-enum : int32_t { DEV_OK = 0, DEV_TIMEOUT = 6, DEV_INCONSISTENT = 8 };
+enum : int32_t { DEV_OK = 0, DEV_NO_PAGES = 5, DEV_TIMEOUT = 6, DEV_INCONSISTENT = 8 };
 
 // Per-layer device state, written by the update kernels.
 struct DevLayer {

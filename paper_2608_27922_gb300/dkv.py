@@ -76,6 +76,30 @@ class dkv_cache_attend_t(ctypes.Structure):
                 ("block", ctypes.c_int32), ("max_rows", ctypes.c_int32)]
 
 
+class dkv_norm_rope_t(ctypes.Structure):
+    _fields_ = [("theta", ctypes.c_void_p), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("eps", ctypes.c_float), ("norm", ctypes.c_int32), ("layout", ctypes.c_int32), ("n_axes", ctypes.c_int32),
+                ("axis_pairs", ctypes.c_int32 * 4)]
+
+
+class dkv_cache_table_t(ctypes.Structure):
+    _fields_ = [("block_table", ctypes.c_void_p), ("seq_len", ctypes.c_void_p), ("n_seq", ctypes.c_int32),
+                ("max_pages", ctypes.c_int32)]
+
+
+class dkv_cache_summaries_t(ctypes.Structure):
+    _fields_ = [("code", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class dkv_cache_choose_t(ctypes.Structure):
+    _fields_ = [("tile", ctypes.c_int32), ("block", ctypes.c_int32), ("sink_pages", ctypes.c_int32),
+                ("local_pages", ctypes.c_int32), ("top", ctypes.c_int32), ("width", ctypes.c_int32)]
+
+
+class dkv_cache_chosen_t(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("tile", ctypes.c_int32), ("block", ctypes.c_int32), ("width", ctypes.c_int32)]
+
+
 # (name, restype, argtypes) of every exported symbol declared in include/dkv.h
 _P = ctypes.c_void_p
 _I = ctypes.c_int32
@@ -118,6 +142,22 @@ SIGNATURES = [
     ("dkv_cache_attend", _I, [_P, ctypes.POINTER(dkv_cache_seqs_t), _P, _I, _I, _L, _L, _P, _L, _L,
                               ctypes.POINTER(dkv_cache_attend_t), _P, ctypes.c_size_t, _P]),
     ("dkv_cache_sync", _I, [_P]),
+    ("dkv_norm_rope", _I, [_I, ctypes.POINTER(dkv_norm_rope_t), _P, _I, _I, _P, _L, _L, _P, _L, _L, _I, _P, _L, _L, _P, _L, _L,
+                           _P]),
+    ("dkv_cache_write_norm_rope", _I, [_P, ctypes.POINTER(dkv_cache_seqs_t), ctypes.POINTER(dkv_norm_rope_t), _P, _I, _I, _P, _L,
+                                       _L, _P, _L, _L, _P, _L, _L, _P, _L, _L, _P]),
+    ("dkv_cache_fork", _I, [_P, _P, ctypes.POINTER(dkv_cache_table_t), _P, ctypes.POINTER(dkv_cache_table_t), _P]),
+    ("dkv_cache_extend_scratch_size", ctypes.c_size_t, [_P, _I]),
+    ("dkv_cache_extend", _I, [_P, _P, ctypes.POINTER(dkv_cache_table_t), _P, _P, ctypes.c_size_t, _P]),
+    ("dkv_cache_release", _I, [_P, _P, ctypes.POINTER(dkv_cache_table_t), _P, _P, _P]),
+    ("dkv_cache_compact_scratch_size", ctypes.c_size_t, [_P, _I]),
+    ("dkv_cache_compact", _I, [_P, _P, ctypes.POINTER(dkv_cache_table_t), _P, _I, _P, ctypes.POINTER(dkv_cache_table_t), _P,
+                               ctypes.c_size_t, _P]),
+    ("dkv_cache_summarise", _I, [_P, ctypes.POINTER(dkv_cache_seqs_t), _P, ctypes.POINTER(dkv_cache_summaries_t), _P]),
+    ("dkv_cache_choose", _I, [_P, ctypes.POINTER(dkv_cache_seqs_t), ctypes.POINTER(dkv_cache_summaries_t), _P, _I, _I, _L, _L,
+                              ctypes.POINTER(dkv_cache_choose_t), _P, _P]),
+    ("dkv_cache_attend_chosen", _I, [_P, ctypes.POINTER(dkv_cache_seqs_t), _P, _I, _I, _L, _L, _P, _L, _L, _P,
+                                     ctypes.POINTER(dkv_cache_chosen_t), _P]),
 ]
 
 DKV_NOALLOC_MAX_N = 16384
@@ -536,6 +576,126 @@ class CacheSeqs:
         self._ref = ctypes.byref(self._c)
 
 
+class PageTable:
+    """Pages of several sequences for the calls that change them (device int32 tensors, see include/dkv.h):
+    block_table [n_seq][max_pages], seq_len [n_seq].  The tensors are kept and changed in place; a CacheSeqs on the
+    same ones sees what the calls made of them."""
+
+    def __init__(self, block_table: torch.Tensor, seq_len: torch.Tensor):
+        n = seq_len.numel()
+        _check_i32(block_table, (n, block_table.shape[-1]), "block_table", seq_len.device)
+        _check_i32(seq_len, (n,), "seq_len", seq_len.device)
+        if not seq_len.is_cuda:
+            raise ValueError(f"seq_len: expected a CUDA tensor, got {seq_len.device}")
+        self.block_table, self.seq_len, self.n_seq, self.device = block_table, seq_len, n, seq_len.device
+        self._c = dkv_cache_table_t(block_table.data_ptr(), seq_len.data_ptr(), n, block_table.shape[-1])
+        self._ref = ctypes.byref(self._c)
+
+
+def _check_i32(t: torch.Tensor, shape, name: str, device) -> None:
+    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: expected contiguous {torch.int32} {shape} on {device}, "
+                         f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+
+
+def _check_32(**values) -> None:
+    for name, x in values.items():
+        if not -2 ** 31 <= x < 2 ** 31:                # (ctypes would take it modulo 2^32)
+            raise ValueError(f"{name}: expected a 32-bit integer, got {x}")
+
+
+def _check_rows(t: torch.Tensor, heads: int, rows: int, d: int, device, name: str):
+    """Strides of a packed tensor between heads and rows."""
+    s = t.stride()
+    if t.dtype != torch.bfloat16 or t.shape != (heads, rows, d) or t.device != device or s[2] != 1:
+        raise ValueError(f"{name}: expected {torch.bfloat16} {(heads, rows, d)} with contiguous rows on "
+                         f"{device}, got {t.dtype} {tuple(t.shape)}, strides {s}, on {t.device}")
+    return s
+
+
+class NormRope:
+    """How queries and keys are normed and rotated (dkv_norm_rope_t): theta [d / 2] fp32, the frequency of each pair;
+    axis_pairs, how many pairs follow each coordinate of a token (default: one coordinate); layout DKV_ROPE_INTERLEAVED
+    or DKV_ROPE_HALF; norm with q_weight and k_weight [d] fp32 (None: ones) and eps.  The tensors are kept."""
+
+    def __init__(self, d: int, theta: torch.Tensor, axis_pairs: Optional[Sequence[int]] = None,
+                 layout: int = DKV_ROPE_INTERLEAVED, norm: bool = True, eps: float = 1e-6,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None):
+        pairs = [d // 2] if axis_pairs is None else [int(x) for x in axis_pairs]
+        if not 1 <= len(pairs) <= 4 or min(pairs) < 0 or sum(pairs) != d // 2:
+            raise ValueError(f"axis_pairs: expected 1 to 4 numbers of pairs, {d // 2} together, got {pairs}")
+        for t, n, name in ((theta, d // 2, "theta"), (q_weight, d, "q_weight"), (k_weight, d, "k_weight")):
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (n,) or not t.is_contiguous()
+                                  or t.device != theta.device or not t.is_cuda):
+                raise ValueError(f"{name}: expected contiguous {torch.float32} {(n,)} on one CUDA device, "
+                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        self.d, self.n_axes, self.device = d, len(pairs), theta.device
+        self._tensors = (theta, q_weight, k_weight)
+        ptr = [0 if t is None else t.data_ptr() for t in self._tensors]
+        self._c = dkv_norm_rope_t(*ptr, eps, int(bool(norm)), layout, len(pairs), (ctypes.c_int32 * 4)(*pairs))
+        self._ref = ctypes.byref(self._c)
+
+
+def norm_rope(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], how: NormRope, coord: torch.Tensor,
+              out: Optional[Tuple[Optional[torch.Tensor], Optional[torch.Tensor]]] = None, stream=None):
+    """Queries Q [H_q][rows][d] and keys K [H_k][rows][d] (either may be None) normed and rotated to the coordinates
+    coord [n_axes][rows] (int32) of their rows: (Q', K'), new tensors or those of `out` (which may be the inputs)."""
+    some = Q if Q is not None else K
+    if some is None:
+        raise ValueError("norm_rope: neither queries nor keys")
+    rows, device = some.shape[1], some.device
+    if how.device != device:
+        raise ValueError(f"how: expected tensors on {device}, got {how.device}")
+    _check_i32(coord, (how.n_axes, rows), "coord", device)
+    raw, ctx = _on_stream(stream, device)
+    outs, args = [], []
+    for x, given, name in ((Q, out[0] if out else None, "Q"), (K, out[1] if out else None, "K")):
+        if x is None:
+            outs.append(None)
+            args += [0, None, 0, 0, None, 0, 0]
+            continue
+        a = _check_rows(x, x.shape[0], rows, how.d, device, name)
+        y = _empty(ctx, x.shape, torch.bfloat16, device) if given is None else given
+        z = _check_rows(y, x.shape[0], rows, how.d, device, "out")
+        outs.append(y)
+        args += [x.shape[0], x.data_ptr(), a[0], a[1], y.data_ptr(), z[0], z[1]]
+    with torch.cuda.device(device):
+        _check(lib().dkv_norm_rope(how.d, how._ref, coord.data_ptr(), rows, *args, raw), "dkv_norm_rope")
+    return tuple(outs)
+
+
+def _on_stream(stream, device):
+    """The stream of a call on a device, and a context in which torch allocates for it (None: the current one)."""
+    if stream is None:
+        return _raw_stream(device.index), None
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream), device=device)
+    return stream.cuda_stream, torch.cuda.stream(stream)
+
+
+def _empty(ctx, shape, dtype, device):
+    if ctx is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with ctx:
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+class Summaries:
+    """8-bit mean keys of a cache's pages: code [n_pages][H][d] int8 and scale [n_pages][H] uint8, allocated or taken."""
+
+    def __init__(self, cache: "PagedCache", code: Optional[torch.Tensor] = None, scale: Optional[torch.Tensor] = None):
+        shape = (cache.n_pages, cache.H, cache.d)
+        self.code = torch.zeros(shape, dtype=torch.int8, device=cache.device) if code is None else code
+        self.scale = torch.full(shape[:2], 77, dtype=torch.uint8, device=cache.device) if scale is None else scale
+        for t, want, dtype, name in ((self.code, shape, torch.int8, "code"), (self.scale, shape[:2], torch.uint8, "scale")):
+            if t.dtype != dtype or tuple(t.shape) != want or not t.is_contiguous() or t.device != cache.device:
+                raise ValueError(f"{name}: expected contiguous {dtype} {want} on {cache.device}, "
+                                 f"got {t.dtype} {tuple(t.shape)} on {t.device}")
+        self.shape, self.device = shape, cache.device
+        self._c = dkv_cache_summaries_t(self.code.data_ptr(), self.scale.data_ptr())
+        self._ref = ctypes.byref(self._c)
+
+
 class PagedCache:
     """Keys and values of H heads in pages of page_len positions, bf16 or quantised to e4m3
     ("bf16" / "e4m3"): allocates the pages with torch, or takes them (k, v and, for e4m3, k_scale,
@@ -578,6 +738,9 @@ class PagedCache:
         self._plans: Dict[tuple, tuple] = {}
         L = lib()
         self._write, self._read, self._attend = L.dkv_cache_write, L.dkv_cache_read, L.dkv_cache_attend
+        self._write_norm_rope, self._summarise = L.dkv_cache_write_norm_rope, L.dkv_cache_summarise
+        self._fork, self._extend, self._release = L.dkv_cache_fork, L.dkv_cache_extend, L.dkv_cache_release
+        self._compact, self._choose, self._attend_chosen = L.dkv_cache_compact, L.dkv_cache_choose, L.dkv_cache_attend_chosen
 
     def close(self):
         if getattr(self, "handle", None):
@@ -591,26 +754,13 @@ class PagedCache:
             pass
 
     def _packed(self, t: torch.Tensor, heads: int, rows: int, name: str):
-        """Strides of a packed tensor between heads and rows."""
-        s = t.stride()
-        if t.dtype != torch.bfloat16 or t.shape != (heads, rows, self.d) or t.device != self.device or s[2] != 1:
-            raise ValueError(f"{name}: expected {torch.bfloat16} {(heads, rows, self.d)} with contiguous rows on "
-                             f"{self.device}, got {t.dtype} {tuple(t.shape)}, strides {s}, on {t.device}")
-        return s
+        return _check_rows(t, heads, rows, self.d, self.device, name)
 
     def _on(self, stream):
-        """The stream of a call, and a context in which torch allocates for it (None: the current one)."""
-        if stream is None:
-            return _raw_stream(self.device.index), None
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(int(stream), device=self.device)
-        return stream.cuda_stream, torch.cuda.stream(stream)
+        return _on_stream(stream, self.device)
 
     def _new(self, ctx, shape, dtype):
-        if ctx is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        with ctx:
-            return torch.empty(shape, dtype=dtype, device=self.device)
+        return _empty(ctx, shape, dtype, self.device)
 
     def _seqs(self, seqs: CacheSeqs):
         if seqs.device != self.device:
@@ -675,16 +825,169 @@ class PagedCache:
         n_seq, Hq, rows, scale, window, sinks, block, max_rows = key
         if scale is not None and not scale > 0.0:
             raise ValueError("scale: expected a positive number")
-        for name, x in (("window", window), ("sinks", sinks), ("block", block)):
-            if not -2 ** 31 <= x < 2 ** 31:            # (ctypes would take it modulo 2^32)
-                raise ValueError(f"{name}: expected a 32-bit integer, got {x}")
+        _check_32(window=window, sinks=sinks, block=block)
         most = rows if max_rows is None else min(int(max_rows), rows)
         size = int(lib().dkv_cache_attend_scratch_size(self.handle, n_seq, Hq, rows, most))
         how = dkv_cache_attend_t(0.0 if scale is None else scale, window, sinks, block, most)
+        return self._keep_plan(key, (size, most, ctypes.byref(how), how))
+
+    def _keep_plan(self, key, plan):
         if len(self._plans) > 4096:
             self._plans.clear()
-        plan = self._plans[key] = (size, most, ctypes.byref(how), how)
+        self._plans[key] = plan
         return plan
 
     def sync(self) -> None:
         _check(lib().dkv_cache_sync(self.handle), "dkv_cache_sync")
+
+    # ------------------------------------------------------------- norm and rotation on the way in
+    def write_norm_rope(self, Q: Optional[torch.Tensor], K: torch.Tensor, V: torch.Tensor, seqs: CacheSeqs, how: NormRope,
+                        coord: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                        stream=None) -> Optional[torch.Tensor]:
+        """The sequences' newest tokens: keys K normed, rotated and written into their pages beside the values V, queries Q
+        [H_q][rows][d] (or None) normed and rotated into `out` or a new tensor, which is returned.  coord [n_axes][rows]
+        int32: the tokens' coordinates (None: their positions)."""
+        rows = K.shape[1]
+        if how.d != self.d or how.device != self.device:
+            raise ValueError(f"how: expected one of d = {self.d} on {self.device}, got {how.d} on {how.device}")
+        if coord is not None:
+            _check_i32(coord, (how.n_axes, rows), "coord", self.device)
+        k, v = self._packed(K, self.H, rows, "K"), self._packed(V, self.H, rows, "V")
+        s, ctx = self._on(stream)
+        queries = (0, None, 0, 0, None, 0, 0)
+        if Q is not None:
+            q = self._packed(Q, Q.shape[0], rows, "Q")
+            if out is None:
+                out = self._new(ctx, Q.shape, torch.bfloat16)
+            o = self._packed(out, Q.shape[0], rows, "out")
+            queries = (Q.shape[0], Q.data_ptr(), q[0], q[1], out.data_ptr(), o[0], o[1])
+        st = self._write_norm_rope(self.handle, self._seqs(seqs), how._ref, None if coord is None else coord.data_ptr(), rows,
+                                   *queries, K.data_ptr(), k[0], k[1], V.data_ptr(), v[0], v[1], s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_write_norm_rope")
+        return out if Q is not None else None
+
+    # ------------------------------------------------------------- pages
+    def new_refs(self) -> torch.Tensor:
+        """Counts for the calls below: every page free."""
+        return torch.zeros(self.n_pages, dtype=torch.int32, device=self.device)
+
+    def _table(self, t: PageTable):
+        if t.device != self.device:
+            raise ValueError(f"table: expected tensors on {self.device}, got {t.device}")
+        return t._ref
+
+    def _refs(self, refs: torch.Tensor) -> int:
+        _check_i32(refs, (self.n_pages,), "refs", self.device)
+        return refs.data_ptr()
+
+    def fork(self, refs: torch.Tensor, src: PageTable, parent: torch.Tensor, dst: PageTable, stream=None) -> None:
+        """Sequence i of dst goes on from sequence parent[i] (int32, -1: empty) of src, sharing its pages; src is given up."""
+        _check_i32(parent, (dst.n_seq,), "parent", self.device)
+        s, _ = self._on(stream)
+        st = self._fork(self.handle, self._refs(refs), self._table(src), parent.data_ptr(), self._table(dst), s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_fork")
+
+    def extend(self, refs: torch.Tensor, seqs: PageTable, add: torch.Tensor, stream=None) -> None:
+        """Room for add[b] (int32) more positions of every sequence: pages, lengths, and a copy of a shared last page."""
+        _check_i32(add, (seqs.n_seq,), "add", self.device)
+        s, ctx = self._on(stream)
+        scratch = self._new(ctx, 16 * seqs.n_seq, torch.uint8)
+        st = self._extend(self.handle, self._refs(refs), self._table(seqs), add.data_ptr(), scratch.data_ptr(), scratch.numel(), s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_extend")
+
+    def release(self, refs: torch.Tensor, seqs: PageTable, first: torch.Tensor, last: torch.Tensor, stream=None) -> None:
+        """Gives back the pages whose positions all lie in [first[b], last[b]) (int32); last[b] >= seq_len[b] ends the sequence at first[b]."""
+        _check_i32(first, (seqs.n_seq,), "first", self.device)
+        _check_i32(last, (seqs.n_seq,), "last", self.device)
+        s, _ = self._on(stream)
+        st = self._release(self.handle, self._refs(refs), self._table(seqs), first.data_ptr(), last.data_ptr(), s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_release")
+
+    def compact(self, refs: torch.Tensor, src: PageTable, keep: torch.Tensor, keep_start: torch.Tensor, dst: PageTable,
+                stream=None) -> None:
+        """Position i of sequence b of dst := position keep[keep_start[b] + i] of sequence b of src (int32); src is given up."""
+        _check_i32(keep, (keep.numel(),), "keep", self.device)
+        _check_i32(keep_start, (src.n_seq + 1,), "keep_start", self.device)
+        s, ctx = self._on(stream)
+        scratch = self._new(ctx, 4 * src.n_seq, torch.uint8)
+        st = self._compact(self.handle, self._refs(refs), self._table(src), keep.data_ptr(), keep.numel(), keep_start.data_ptr(),
+                           self._table(dst), scratch.data_ptr(), scratch.numel(), s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_compact")
+
+    # ------------------------------------------------------------- chosen pages
+    def _sums(self, summaries: Summaries):
+        if summaries.shape != (self.n_pages, self.H, self.d) or summaries.device != self.device:
+            raise ValueError(f"summaries: expected those of a cache of {(self.n_pages, self.H, self.d)} on {self.device}, "
+                             f"got {summaries.shape} on {summaries.device}")
+        return summaries._ref
+
+    def summarise(self, seqs: CacheSeqs, summaries: Summaries, first: Optional[torch.Tensor] = None, stream=None) -> None:
+        """8-bit mean keys of the pages that hold positions from first[b] (int32; None: the newest tokens') on."""
+        if first is not None:
+            _check_i32(first, (seqs.n_seq,), "first", self.device)
+        s, _ = self._on(stream)
+        st = self._summarise(self.handle, self._seqs(seqs), None if first is None else first.data_ptr(), self._sums(summaries), s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_summarise")
+
+    def choose(self, Q: torch.Tensor, seqs: CacheSeqs, summaries: Summaries, top: int, tile: int = 1, block: int = 1,
+               sink_pages: int = 1, local_pages: int = 2, width: Optional[int] = None, out: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+        """Lists [H][rows // tile + n_seq][width] (int32, -1 behind the last page) of the pages that each tile of `tile` tokens
+        attends to in each key head: sinks, local ones and the `top` best by their summaries (see dkv_cache_choose)."""
+        Hq, rows = Q.shape[0], Q.shape[1]
+        if width is None:
+            width = max(1, sink_pages + local_pages + (tile + self.page_len - 2) // self.page_len + top)
+        key = ("choose", tile, block, sink_pages, local_pages, top, width)
+        plan = self._plans.get(key)
+        if plan is None:
+            _check_32(tile=tile, block=block, sink_pages=sink_pages, local_pages=local_pages, top=top, width=width)
+            if tile < 1:
+                raise ValueError(f"tile: expected a positive number, got {tile}")
+            how = dkv_cache_choose_t(tile, block, sink_pages, local_pages, top, width)
+            plan = self._keep_plan(key, (ctypes.byref(how), how))
+        q = self._packed(Q, Hq, rows, "Q")
+        s, ctx = self._on(stream)
+        shape = (self.H, rows // tile + seqs.n_seq, width)
+        if out is None:
+            out = self._new(ctx, shape, torch.int32)
+        else:
+            _check_i32(out, shape, "out", self.device)
+        st = self._choose(self.handle, self._seqs(seqs), self._sums(summaries), Q.data_ptr(), Hq, rows, q[0], q[1], plan[0],
+                          out.data_ptr(), s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_choose")
+        return out
+
+    def attend_chosen(self, Q: torch.Tensor, seqs: CacheSeqs, lists: torch.Tensor, tile: int = 1, block: int = 1,
+                      scale: Optional[float] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """Attention of the sequences' newest tokens Q [H_q][rows][d] over the pages that `lists` (as choose returns
+        them, for the same tile) names for their tile and key head."""
+        Hq, rows = Q.shape[0], Q.shape[1]
+        width = lists.shape[-1]
+        key = ("chosen", scale, tile, block, width)
+        plan = self._plans.get(key)
+        if plan is None:
+            if scale is not None and not scale > 0.0:
+                raise ValueError("scale: expected a positive number")
+            _check_32(tile=tile, block=block)
+            if tile < 1:
+                raise ValueError(f"tile: expected a positive number, got {tile}")
+            how = dkv_cache_chosen_t(0.0 if scale is None else scale, tile, block, width)
+            plan = self._keep_plan(key, (ctypes.byref(how), how))
+        _check_i32(lists, (self.H, rows // tile + seqs.n_seq, width), "lists", self.device)
+        q = self._packed(Q, Hq, rows, "Q")
+        s, ctx = self._on(stream)
+        if out is None:
+            out = self._new(ctx, (Hq, rows, self.d), torch.bfloat16)
+        o = self._packed(out, Hq, rows, "out")
+        st = self._attend_chosen(self.handle, self._seqs(seqs), Q.data_ptr(), Hq, rows, q[0], q[1], out.data_ptr(), o[0], o[1],
+                                 lists.data_ptr(), plan[0], s)
+        if st != DKV_OK:
+            _check(st, "dkv_cache_attend_chosen")
+        return out
