@@ -60,6 +60,8 @@ bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
 constexpr int ROWS_MOST = 16;
 bool few_rows(const cache::Pool& c, int Hq, int max_rows) { return (int64_t)max_rows * (Hq / c.H) <= ROWS_MOST; }
 
+constexpr int CHOSEN_ROWS_MOST = 16;
+
 size_t scratch_of(const cache::Pool& c, int Hq, int max_rows) {
   return few_rows(c, Hq, max_rows) ? cache::attend_rows_scratch(c, Hq / c.H, max_rows) : cache::attend_tc_scratch(c);
 }
@@ -157,7 +159,8 @@ dkv_status_t dkv_cache_create(dkv_cache_t* out, int32_t H, int32_t d, int32_t pa
   if (taken(cudaGetDeviceProperties(&prop, dev)) != cudaSuccess) return DKV_ERR_CUDA;
   if (prop.major != 10 || prop.minor != 3) return DKV_ERR_UNSUPPORTED;   // built for sm_103a only
   if (cache::attend_tc_set_smem_limits() != cudaSuccess || cache::attend_rows_set_smem_limits() != cudaSuccess ||
-      cache::pages_set_smem_limits() != cudaSuccess || cache::choose_set_smem_limits() != cudaSuccess)
+      cache::pages_set_smem_limits() != cudaSuccess || cache::choose_set_smem_limits() != cudaSuccess ||
+      cache::chosen_tc_set_smem_limits() != cudaSuccess)
     return DKV_ERR_CUDA;
   if (taken(cudaMemset(buf->status, 0, 2 * sizeof(int32_t))) != cudaSuccess) return DKV_ERR_CUDA;
   dkv_cache_s* c = new (std::nothrow) dkv_cache_s();
@@ -430,7 +433,9 @@ dkv_status_t dkv_cache_attend_chosen(dkv_cache_t c, const dkv_cache_seqs_t* seqs
   OnDevice on(c->device);
   if (!on.ok) return DKV_ERR_CUDA;
   c->last = (cudaStream_t)stream;
-  return status_of(cache::launch_chosen_rows(c->pool, s, q, o, H_q, m, ch, (cudaStream_t)stream));
+  if ((int64_t)(how->tile < rows ? how->tile : rows) * (H_q / c->pool.H) <= CHOSEN_ROWS_MOST)
+    return status_of(cache::launch_chosen_rows(c->pool, s, q, o, H_q, m, ch, (cudaStream_t)stream));
+  return status_of(cache::launch_chosen_tc(c->pool, c->maps, s, q, o, H_q, m, ch, (cudaStream_t)stream));
 }
 
 }  // extern "C"

@@ -209,6 +209,10 @@ cudaError_t launch_summarise(const Pool& c, const Seqs& s, const int32_t* first,
 cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, const uint8_t* scale, const Packed& q, int Hq,
                           const Choose& how, int32_t* lists, cudaStream_t st);
 
+cudaError_t chosen_tc_set_smem_limits();   // on the current device
+struct Maps;
+cudaError_t launch_chosen_tc(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
+                             const Mask& m, const Chosen& how, cudaStream_t st);
 cudaError_t launch_chosen_rows(const Pool& c, const Seqs& s, const Packed& q, const Packed& o, int Hq, const Mask& m,
                                const Chosen& how, cudaStream_t st);
 

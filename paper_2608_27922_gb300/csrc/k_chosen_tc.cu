@@ -1,0 +1,673 @@
+// Attention over chosen pages on the tensor cores (include/dkv.h: dkv_cache_attend_chosen), many query rows a tile.
+//
+// A unit is 128 query rows of one tile of tokens and one key head, row = token * G + head, TQ = 128 / G tokens.  The pages that
+// the tile's list names, one behind the other, form the unit's keys; in tiles of 128 they stream past the query rows:
+//   S = Q K^T             tcgen05.mma into TMEM; thread = query row
+//   P = exp2(S scale log2(e) - m)   packed bf16 over S in TMEM; what a row does not see is 0
+//   O += P V              tcgen05.mma with A = P from TMEM
+// with the running maximum raised only when a tile's exceeds it by more than 2^8 (O is then rescaled in TMEM).  Bound by the
+// tensor pipe (4 d flops a row and key) and close to it by the exponentials.
+//
+// One CTA a unit (or a cluster, whose CTAs share its key tiles and join their parts on chip) and two CTAs an SM: while one's
+// softmax runs, the other's products do, and one's first loads hide behind the other's work, without a schedule of
+// items.  Each has half of the SM's memory (a tile of Q, one of K and one of V at d = 128) and of its TMEM.
+//
+// bf16 pages come in by TMA, one box a page and 64-column panel; the pages of the tile after next are asked into L2
+// meanwhile.  Codes come by plain loads, one tile ahead in the registers of four warps, which write them as bf16 with their
+// scales in them: code bits in bf16's fields are the value times 2^-120, one product with 2^120 times the scale makes it
+// exact.
+//
+// Values in places that a row does not see meet its weight 0, and 0 times a NaN or an infinity is NaN: in the tiles that some
+// row does not see whole, the softmax threads clear what is not finite in V's tile, and rows that do see such a value get
+// it back at the end (wild_in).
+#include "attn_math.cuh"
+#include "cache_internal.h"
+#include "tc_ptx.cuh"
+
+#include <cooperative_groups.h>
+
+#include <algorithm>
+
+namespace cg = cooperative_groups;
+
+namespace dkv {
+
+bool make_map_4d(CUtensorMap* m, const void* base, int elem_bytes, const int64_t (&dim)[4], const int64_t (&stride)[3],
+                 const int (&box)[4], int swizzle);
+
+namespace cache {
+
+namespace {
+
+using namespace tc;
+
+constexpr int BQ = 128, BK = 128;
+constexpr int PANEL = 128 * 128;         // bytes of a 64-column panel of 128 rows
+constexpr uint32_t TMEM_COLS = 256;      // S [0, 128), O [128, 128 + d)
+constexpr float RESCALE_LOG2 = 8.0f;
+constexpr int MAX_WIDTH = 1024;
+constexpr int SITE = 10;                 // of waits, beside the other kernels'
+
+template <int D, bool E4M3>
+struct Lay {
+  static constexpr int NP = D / 64;
+  static constexpr int TB = NP * PANEL;                // bytes of a 128-row tile
+  static constexpr int N = D == 128 ? 1 : 2;           // tiles of K, and of V
+  static constexpr int Q = 0;
+  static constexpr int K = TB;
+  static constexpr int V = K + N * TB;
+  static constexpr int LIST = V + N * TB;              // [MAX_WIDTH] entries, [MAX_WIDTH] pages
+  static constexpr int CTRL = LIST + 2 * MAX_WIDTH * 4;
+  static constexpr int STATS = CTRL + 256;             // [128] maximum, sum (a cluster's join)
+  static constexpr size_t BYTES = STATS + 128 * 8;
+  static constexpr int JOIN = K;                       // a part's outputs, [D / 4][128 rows] of 16 bytes
+  static constexpr int THREADS = (8 + (E4M3 ? 4 : 0)) * 32;
+  // registers a thread: the first four warps, the softmax, the conversion; the launch gives 128 (80) each
+  static constexpr int REGS_IO = E4M3 ? 40 : 56, REGS_SOFT = E4M3 ? 128 : 200, REGS_CONV = 72;
+  static_assert(REGS_IO + REGS_SOFT + (E4M3 ? REGS_CONV : 0) <= (E4M3 ? 3 * 80 : 2 * 128), "register split");
+  static_assert(2 * N * TB >= D * BQ * 4, "a part in the tiles' place");
+  static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two CTAs an SM");
+};
+
+struct Job {
+  Pool c;
+  Seqs s;
+  Mask m;
+  Packed o;
+  Chosen how;
+  int G, TQ, tiles;   // query tiles of a slot
+  int wide;           // rows of the outputs 32-byte aligned
+};
+
+// The unit's keys: the first `count` entries of its list, page by page.
+struct Keys {
+  const int* entry;   // shared memory
+  const int* page;    // -1: not to be read
+  int count;
+  int log2, len;      // of a page
+  // position of place u of the keys; -1: none
+  __device__ __forceinline__ int pos(int u) const {
+    const int k = u >> log2;
+    return k < count && page[k] >= 0 ? (entry[k] << log2) + (u & (len - 1)) : -1;
+  }
+};
+
+__device__ __forceinline__ uint32_t below(int x) { return x <= 0 ? 0u : x >= 32 ? 0xffffffffu : (1u << x) - 1u; }
+
+// Which of the places u .. u + 31 a row that sees up to `end` sees.
+__device__ __forceinline__ uint32_t seen32(const Keys& k, int u, int end) {
+  const int a = k.pos(u);
+  if (k.len >= 32) return a < 0 ? 0u : below(end - a);
+  const int z = k.pos(u + 16);
+  return (a < 0 ? 0u : below(end - a) & 0xffffu) | (z < 0 ? 0u : (below(end - z) & 0xffffu) << 16);
+}
+
+__device__ __forceinline__ void mask_row(float (&v)[32], uint32_t see) {
+#pragma unroll
+  for (int k = 0; k < 32; ++k)
+    if (!((see >> k) & 1u)) v[k] = -INFINITY;
+}
+
+// Clears what is not finite in one bf16 row (128-byte swizzled panels), and says so in *met.
+template <int D>
+__device__ __forceinline__ void clear_row(uint8_t* tile, int row, volatile int* met) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int c = 0; c < D / 8; ++c) {
+    const uint4 x = *reinterpret_cast<uint4*>(tile + (c >> 3) * PANEL + row * 128 + (((c & 7) ^ (row & 7)) << 4));
+    any |= ((x.x & 0x7f807f80u) + 0x00800080u) | ((x.y & 0x7f807f80u) + 0x00800080u) |
+           ((x.z & 0x7f807f80u) + 0x00800080u) | ((x.w & 0x7f807f80u) + 0x00800080u);
+  }
+  if ((any & 0x80008000u) == 0) return;
+  *met = 1;
+#pragma unroll 1
+  for (int c = 0; c < D / 2; ++c) {
+    uint32_t* p = reinterpret_cast<uint32_t*>(tile + (c >> 5) * PANEL + row * 128 + ((((c >> 2) & 7) ^ (row & 7)) << 4)) + (c & 3);
+    const uint32_t x = *p, bad = ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+    if (bad) *p = x & ~(((bad >> 15) & 0x00010001u) * 0xffffu);
+  }
+}
+
+// The columns [c0, c0 + 32) in which a row that sees up to `end` meets a NaN, +inf, -inf in the places [u0, u1).
+struct Wild {
+  uint32_t nan, pos, neg;
+};
+template <int D, bool E4M3>
+__device__ __noinline__ Wild wild_in(const Pool& c, const Keys& keys, int h, int u0, int u1, int end, int c0) {
+  Wild w{0, 0, 0};
+#pragma unroll 1
+  for (int u = u0; u < u1; ++u) {
+    const int p = keys.pos(u);
+    if (p < 0 || p >= end) continue;
+    const int64_t at = (((int64_t)keys.page[u >> keys.log2] * c.H + h) << c.page_log2) + (p & (c.page_len - 1));
+    if (E4M3) {
+      if (c.vs[at] == 255) w.nan = 0xffffffffu;
+      continue;
+    }
+    const __nv_bfloat16* v = static_cast<const __nv_bfloat16*>(c.v) + at * D + c0;
+#pragma unroll 1
+    for (int k = 0; k < 32; ++k) {
+      const float x = __bfloat162float(v[k]);
+      if (isnan(x)) w.nan |= 1u << k;
+      if (x == INFINITY) w.pos |= 1u << k;
+      if (x == -INFINITY) w.neg |= 1u << k;
+    }
+  }
+  return w;
+}
+
+__device__ __forceinline__ void store32(void* p, const uint32_t* w) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
+               "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
+               : "memory");
+}
+
+__device__ __forceinline__ void prefetch_4d(const CUtensorMap* map, int x, int y, int z, int w) {
+  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(map)),
+               "r"(x), "r"(y), "r"(z), "r"(w)
+               : "memory");
+}
+
+// Four bf16 from four codes; f holds 2^120 times the scale.
+__device__ __forceinline__ uint2 widen(uint32_t w, __nv_bfloat162 f) {
+  const uint32_t hi = (w & 0x80808080u) | ((w >> 4) & 0x07070707u), lo = (w << 4) & 0xf0f0f0f0u;
+  const uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);
+  const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), f);
+  const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), f);
+  return make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
+}
+__device__ __forceinline__ __nv_bfloat162 bf2(uint32_t bits) { return *reinterpret_cast<const __nv_bfloat162*>(&bits); }
+__device__ __forceinline__ uint32_t times(uint32_t x, __nv_bfloat162 f) {
+  const __nv_bfloat162 y = __hmul2(bf2(x), f);
+  return *reinterpret_cast<const uint32_t*>(&y);
+}
+
+// A thread's codes of a tile: 16 bytes of rows r0, r0 + STEP, .. and their scale bytes.
+template <int D>
+struct Codes {
+  static constexpr int LANES = D / 16, STEP = 128 / LANES, N = 128 / STEP;   // 128 threads
+  uint4 x[N];
+  uint8_t s[N];
+};
+
+template <int D, bool E4M3>
+__global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
+    chosen_tc(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK,
+              const __grid_constant__ CUtensorMap tmV, const __grid_constant__ Job j) {
+  using L = Lay<D, E4M3>;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = cluster.num_blocks(), rank = cluster.block_rank();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  // ---- the unit
+  const int unit = blockIdx.x / C, slot = unit / j.tiles, qt = unit - slot * j.tiles, h = blockIdx.y;
+  if (blockIdx.x == 0 && h == 0)
+    for (int b = tid; b < j.s.n; b += L::THREADS) seq_at(j.c, j.s, b);
+  const int b = seq_of_slot(j.s, j.how.tile, slot);
+  const Seq q = seq_at(j.c, j.s, b);
+  const int i0 = (slot - first_slot(j.s, j.how.tile, b)) * j.how.tile;
+  const int first = i0 + qt * j.TQ;                                        // its first token
+  const int tokens = i0 < 0 ? 0 : min(min(j.how.tile - qt * j.TQ, j.TQ), q.n - first);
+  if (tokens <= 0) return;                                                 // (the whole cluster)
+  if ((smem_u32(smem) & 1023u) != 0u) {   // 128-byte-swizzled tiles need 1024-byte alignment
+    if (tid == 0) fail(j.c.status, DEV_INCONSISTENT, 9904);
+    return;
+  }
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::CTRL);
+  uint64_t* q_full = bars + 0;
+  uint64_t* k_full = bars + 1;      // [N]
+  uint64_t* k_empty = bars + 3;     // [N]
+  uint64_t* v_full = bars + 5;      // [N]
+  uint64_t* v_empty = bars + 7;     // [N]
+  uint64_t* s_full = bars + 9;
+  uint64_t* p_full = bars + 10;
+  uint64_t* o_full = bars + 11;
+  uint64_t* over = bars + 12;       // every role but the producer has ended
+  uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bars + 14);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 15);
+  volatile int* wild = abort_flag + 1;
+  int* bounds = reinterpret_cast<int*>(bars + 16);   // entries listed, leading ones that all rows see whole
+  int* entry = reinterpret_cast<int*>(smem + L::LIST);
+  int* page = entry + MAX_WIDTH;
+  if (tid == 64) {
+    mbar_init(q_full, 1);
+    for (int i = 0; i < L::N; ++i) {
+      mbar_init(k_full + i, E4M3 ? 4 : 1);
+      mbar_init(k_empty + i, 1);
+      mbar_init(v_full + i, E4M3 ? 4 : 1);
+      mbar_init(v_empty + i, 1);
+    }
+    mbar_init(s_full, 1);
+    mbar_init(p_full, 4);
+    mbar_init(o_full, 1);
+    mbar_init(over, 1 + 4 + (E4M3 ? 4 : 0));
+    *abort_flag = 0;
+    *wild = 0;
+    bounds[0] = bounds[1] = j.how.width;
+    fence_barrier_init();
+  }
+  if (warp == 1) tmem_alloc(tmem_holder, TMEM_COLS);
+  auto end_of = [&](int token) {
+    const int p = q.len - q.n + first + token;
+    return p < 0 ? 0 : visible_end(j.m, p, q.len);
+  };
+  const int all_end = end_of(0), any_end = end_of(tokens - 1);
+  __syncthreads();
+  {
+    const int32_t* line = j.how.lists + ((int64_t)h * j.how.slots + slot) * j.how.width;
+    for (int k = tid; k < j.how.width; k += L::THREADS) {
+      const int e = __ldg(line + k), before = k ? __ldg(line + k - 1) : -1;
+      int at = -1;
+      if (e < 0) {
+        atomicMin(bounds, k);
+      } else if ((k && before >= 0 && e <= before) || e >= (q.len + j.c.page_len - 1) >> j.c.page_log2) {
+        fail(j.c.status, DEV_INCONSISTENT, SITE_LIST);
+      } else if (((int64_t)e << j.c.page_log2) >= any_end) {
+        atomicMin(bounds, k);   // (the rest of an ascending list lies behind it)
+      } else {
+        at = j.s.table[(int64_t)b * j.s.max_pages + e];
+        if ((unsigned)at >= (unsigned)j.c.n_pages) {
+          fail(j.c.status, DEV_INCONSISTENT, SITE_PAGE);
+          at = -1;
+        }
+      }
+      if (at < 0 || ((int64_t)e + 1) << j.c.page_log2 > all_end) atomicMin(bounds + 1, k);
+      entry[k] = e;
+      page[k] = at;
+    }
+  }
+  fence_before_sync();
+  __syncthreads();
+  fence_after_sync();
+  const uint32_t tmem = *tmem_holder;
+  const Keys keys{entry, page, bounds[0], j.c.page_log2, j.c.page_len};
+  const int whole_to = min(bounds[1], bounds[0]) << j.c.page_log2;   // places that every row sees
+  const int NT = ((keys.count << j.c.page_log2) + BK - 1) / BK;
+  const int t0 = (int)((int64_t)NT * rank / C), t1 = (int)((int64_t)NT * (rank + 1) / C), n = t1 - t0;
+
+  auto give_up = [&](int site) {
+    *abort_flag = 1;
+    fail(j.c.status, DEV_TIMEOUT, SITE_WAIT + SITE + site);
+  };
+  // of the softmax threads, kept for the join
+  float mrun = -INFINITY, l = 0.f;
+  bool ok = true;
+  const int r = tid & 127, tok = r / j.G, hq = r - tok * j.G;   // row of a softmax thread
+  const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+  const uint32_t sc = tmem + lane_off, oc = sc + 128;
+  const bool mine = tok < j.TQ && tok < tokens;
+  const int end = mine ? end_of(tok) : 0;
+
+  if (warp < 4) {
+    regs_lower<L::REGS_IO>();
+    if (warp == 0) {
+      // ---------------- producer: Q, K(0), V(0), K(1), ..  It also watches the time for all roles' waits.
+      const int rows = min(j.c.page_len, BK), np = BK / rows;   // rows and boxes of a tile
+      if (n > 0 && lane == 0) {
+        mbar_arrive_expect_tx(q_full, L::NP * j.TQ * j.G * 128);
+        for (int p = 0; p < L::NP; ++p) tma_load_4d(smem + L::Q + p * PANEL, &tmQ, q_full, p * 64, 0, q.r0 + first, h);
+      }
+      __syncwarp();
+      if constexpr (!E4M3) {
+        const int box = lane / L::NP, panel = lane % L::NP;
+        auto place = [&](int i, int& at, int& slot_in) {   // the lane's box of tile t0 + i
+          const int u = (t0 + i) * BK + box * rows, k = u >> j.c.page_log2;
+          at = box < np && i < n && k < keys.count ? page[k] : -1;
+          slot_in = u & (j.c.page_len - 1);
+        };
+        auto load = [&](bool is_k, int i) -> bool {
+          const int sl = i % L::N;
+          uint64_t* bar = (is_k ? k_full : v_full) + sl;
+          if (i >= L::N && !mbar_wait_warp((is_k ? k_empty : v_empty) + sl, (i / L::N - 1) & 1, abort_flag)) return false;
+          if (lane == 0) mbar_arrive_expect_tx(bar, L::TB);
+          __syncwarp();
+          int at, in;
+          place(i, at, in);
+          if (box < np)   // (nobody's page: zeros)
+            tma_load_4d(smem + (is_k ? L::K : L::V) + sl * L::TB + panel * PANEL + box * rows * 128, is_k ? &tmK : &tmV, bar,
+                        panel * 64, in, h, at < 0 ? j.c.n_pages : at);
+          // the tile after next, into L2
+          place(i + 2, at, in);
+          if (at >= 0) prefetch_4d(is_k ? &tmK : &tmV, panel * 64, in, h, at);
+          __syncwarp();
+          return true;
+        };
+        if (n > 0) ok = load(true, 0);
+        for (int i = 0; ok && i < n; ++i) {
+          ok = load(false, i);
+          if (ok && i + 1 < n) ok = load(true, i + 1);
+        }
+      }
+      if (ok) ok = mbar_wait_warp(over, 0, abort_flag);
+      if (!ok) {
+        if (lane == 0) give_up(0);
+        // copies may be in flight that nobody waits for any more: far longer than one takes
+        const uint64_t since = globaltimer_ns();
+        while (globaltimer_ns() - since < 50000ull) {
+        }
+      }
+    } else if (warp == 1) {
+      // ---------------- MMA issuer (the whole warp, one elected lane issues)
+      constexpr uint32_t id_s = idesc_bf16(BQ, BK), id_o = idesc_bf16(BQ, D, /*b_mn_major=*/true);
+      const uint64_t qd = desc_sw128(smem_u32(smem + L::Q)), kd0 = desc_sw128(smem_u32(smem + L::K));
+      const uint64_t vd0 = desc_sw128_mn(smem_u32(smem + L::V), PANEL, 1024);
+      if (n > 0) ok = mbar_wait_warp_short(q_full, 0, abort_flag);
+      for (int i = 0; ok && i < n; ++i) {
+        const int sl = i % L::N;
+        if (!(ok = mbar_wait_warp_short(k_full + sl, (i / L::N) & 1, abort_flag))) break;
+        fence_after_sync();
+        // (S's place holds the last tile's P: its product was issued before)
+        const uint64_t kd = desc_add(kd0, sl * L::TB);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk) {
+            const uint32_t off = (kk >> 2) * PANEL + (kk & 3) * 32;
+            mma_bf16(tmem, desc_add(qd, off), desc_add(kd, off), id_s, kk > 0);
+          }
+          mma_commit(s_full);
+          mma_commit(k_empty + sl);
+        }
+        __syncwarp();
+        if (!(ok = mbar_wait_warp_short(v_full + sl, (i / L::N) & 1, abort_flag))) break;
+        if (!(ok = mbar_wait_warp_short(p_full, i & 1, abort_flag))) break;
+        fence_after_sync();
+        const uint64_t vd = desc_add(vd0, sl * L::TB);
+        if (elect_one()) {
+#pragma unroll
+          for (int kk = 0; kk < 8; ++kk)
+            mma_bf16_ts(tmem + 128, tmem + kk * 8, desc_add(vd, kk * 2048), id_o, i > 0 || kk > 0 ? 1u : 0u);
+          mma_commit(v_empty + sl);
+          if (i + 1 == n) mma_commit(o_full);
+        }
+        __syncwarp();
+      }
+      if (!ok && lane == 0) give_up(1);
+      if (!ok) {   // every product complete before TMEM is freed
+        if (elect_one()) mma_commit(o_full);
+        __syncwarp();
+        volatile int no_abort = 0;
+        mbar_wait(o_full, 0, &no_abort);
+      }
+      if (lane == 0) mbar_arrive(over);
+    }
+  } else if (warp < 8) {
+    regs_raise<L::REGS_SOFT>();
+    // ---------------- softmax, thread = query row = TMEM lane
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      const int sl = i % L::N, u0 = (t0 + i) * BK;
+      const bool partial = u0 + BK > whole_to;
+      if (partial) {
+        if (!(ok = mbar_wait_warp_short(v_full + sl, (i / L::N) & 1, abort_flag))) break;
+        clear_row<D>(smem + L::V + sl * L::TB, r, wild);
+        fence_async_smem();
+      }
+      if (!(ok = mbar_wait_warp_short(s_full, i & 1, abort_flag))) break;
+      fence_after_sync();
+      float tmax;
+      {
+        float t[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) t[k] = -INFINITY;
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+          float a[32], z[32];
+          tmem_ld32(sc + half * 64, a);
+          tmem_ld32(sc + half * 64 + 32, z);
+          tmem_wait_ld();
+          if (partial) {
+            mask_row(a, seen32(keys, u0 + half * 64, end));
+            mask_row(z, seen32(keys, u0 + half * 64 + 32, end));
+            tmem_st32(sc + half * 64, reinterpret_cast<uint32_t(&)[32]>(a));
+            tmem_st32(sc + half * 64 + 32, reinterpret_cast<uint32_t(&)[32]>(z));
+          }
+          max_acc(t, a);
+          max_acc(t, z);
+        }
+        if (partial) tmem_wait_st();
+        tmax = fmaxf(fmaxf(fmaxf(t[0], t[1]), fmaxf(t[2], t[3])), fmaxf(fmaxf(t[4], t[5]), fmaxf(t[6], t[7])));
+      }
+      tmax *= j.m.sl2;
+      // S of this tile complete implies O of the one before complete (issued earlier by one thread)
+      const bool raise = tmax > mrun + RESCALE_LOG2 || (mrun == -INFINITY && tmax > -INFINITY);
+      const float mprev = mrun;
+      if (raise) {
+        l *= i > 0 ? ex2(mrun - tmax) : 0.f;
+        mrun = tmax;
+      }
+      const float nm = mrun == -INFINITY ? 0.f : -mrun;   // (a row that has seen nothing yet: all weights 0)
+      float2 lab = make_float2(0.f, 0.f);
+#pragma unroll 1
+      for (int half = 0; half < 2; ++half) {
+        float a[32], z[32];
+        uint32_t pk[32];
+        tmem_ld32(sc + half * 64, a);
+        tmem_ld32(sc + half * 64 + 32, z);
+        tmem_wait_ld();
+        exp_pack(a, z, j.m.sl2, nm, lab, pk);
+        tmem_st32(sc + half * 32, pk);
+      }
+      if (i > 0 && __any_sync(0xffffffffu, raise)) {
+        const float alpha = raise ? ex2(mprev - mrun) : 1.0f;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          float v[32];
+          tmem_ld32(oc + c * 32, v);
+          tmem_wait_ld();
+          uint32_t w32[32];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) {
+            const float2 y = __fmul2_rn(make_float2(v[2 * k], v[2 * k + 1]), make_float2(alpha, alpha));
+            w32[2 * k] = __float_as_uint(y.x);
+            w32[2 * k + 1] = __float_as_uint(y.y);
+          }
+          tmem_st32(oc + c * 32, w32);
+        }
+      }
+      l += lab.x + lab.y;
+      tmem_wait_st();
+      fence_before_sync();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(p_full);
+    }
+    if (ok && n > 0) ok = mbar_wait_warp_short(o_full, 0, abort_flag);
+    fence_after_sync();
+    if (!ok && lane == 0) give_up(2);
+    // ---- outputs, or a part of them into the tiles' place
+    if (ok) {
+      const bool fix = *wild != 0 && l != 0.f;
+      const float f = C > 1 ? 1.f : l == 0.f ? 0.f : 1.0f / l;         // (a NaN stays one)
+#pragma unroll 1
+      for (int c = 0; c < D / 32; ++c) {
+        float v[32];
+        if (n > 0) {
+          tmem_ld32(oc + c * 32, v);
+          tmem_wait_ld();
+        }
+#pragma unroll
+        for (int k = 0; k < 32; ++k) v[k] = n > 0 && l != 0.f ? v[k] * f : 0.f;
+        if (fix) {
+          const Wild w = wild_in<D, E4M3>(j.c, keys, h, max(t0 * BK, whole_to / BK * BK), t1 * BK, end, c * 32);
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            if ((w.pos >> k) & 1u) v[k] += INFINITY;
+            if ((w.neg >> k) & 1u) v[k] -= INFINITY;
+            if ((w.nan >> k) & 1u) v[k] = __int_as_float(0x7fffffff);
+          }
+        }
+        if (C > 1) {
+          float4* dst = reinterpret_cast<float4*>(smem + L::JOIN) + (c * 8) * BQ + r;
+#pragma unroll
+          for (int k = 0; k < 8; ++k) dst[k * BQ] = make_float4(v[4 * k], v[4 * k + 1], v[4 * k + 2], v[4 * k + 3]);
+        } else if (mine) {
+          uint32_t w[16];
+#pragma unroll
+          for (int k = 0; k < 16; ++k) w[k] = pack_bf16(v[2 * k], v[2 * k + 1]);
+          __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + hq) * j.o.head +
+                               (int64_t)(q.r0 + first + tok) * j.o.row + c * 32;
+          if (j.wide) {
+            store32(dst, w);
+            store32(dst + 16, w + 8);
+          } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) reinterpret_cast<uint4*>(dst)[k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+          }
+        }
+      }
+    }
+    if (C > 1) reinterpret_cast<float2*>(smem + L::STATS)[r] = ok ? make_float2(mrun, l) : make_float2(-INFINITY, 0.f);
+    fence_before_sync();
+    __syncwarp();
+    if (lane == 0) mbar_arrive(over);
+  } else if constexpr (E4M3) {
+    regs_lower<L::REGS_CONV>();
+    // ---------------- codes into bf16: K(0), V(0), K(1), ..; the next tile's codes are on their way meanwhile
+    using W = Codes<D>;
+    const int ct = tid - 256, cl = ct % W::LANES, r0 = ct / W::LANES;
+    auto fetch = [&](bool is_k, int i, W& w) {
+      const uint8_t* pool = static_cast<const uint8_t*>(is_k ? j.c.k : j.c.v);
+      const uint8_t* scales = is_k ? j.c.ks : j.c.vs;
+#pragma unroll
+      for (int k = 0; k < W::N; ++k) {
+        const int u = (t0 + i) * BK + r0 + k * W::STEP, e = u >> j.c.page_log2;
+        const int at = i < n && e < keys.count ? page[e] : -1;
+        if (at >= 0) {
+          const int64_t row = (((int64_t)at * j.c.H + h) << j.c.page_log2) + (u & (j.c.page_len - 1));
+          w.x[k] = __ldg(reinterpret_cast<const uint4*>(pool + row * D) + cl);
+          w.s[k] = __ldg(scales + row);
+        } else {
+          w.x[k] = make_uint4(0, 0, 0, 0);
+          w.s[k] = 127;
+        }
+      }
+    };
+    auto put = [&](bool is_k, int i, const W& w) -> bool {
+      const int sl = i % L::N;
+      if (i >= L::N && !mbar_wait_warp_short((is_k ? k_empty : v_empty) + sl, (i / L::N - 1) & 1, abort_flag)) return false;
+      uint8_t* tile = smem + (is_k ? L::K : L::V) + sl * L::TB;
+      uint32_t big = 0;
+#pragma unroll
+      for (int k = 0; k < W::N; ++k) big = max(big, (uint32_t)w.s[k]);
+      const bool two = __any_sync(0xffffffffu, big > 134u);
+#pragma unroll
+      for (int k = 0; k < W::N; ++k) {
+        const uint32_t s = w.s[k];
+        const __nv_bfloat162 f = bf2((s > 134u ? 247u : s + 120u) * 0x00800080u);
+        uint2 y0 = widen(w.x[k].x, f), y1 = widen(w.x[k].y, f), y2 = widen(w.x[k].z, f), y3 = widen(w.x[k].w, f);
+        if (two) {
+          const __nv_bfloat162 f2 = bf2(s == 255u ? 0x7fff7fffu : (s > 134u ? s : 127u) * 0x00800080u);
+          y0 = make_uint2(times(y0.x, f2), times(y0.y, f2));
+          y1 = make_uint2(times(y1.x, f2), times(y1.y, f2));
+          y2 = make_uint2(times(y2.x, f2), times(y2.y, f2));
+          y3 = make_uint2(times(y3.x, f2), times(y3.y, f2));
+        }
+        // 16-byte chunks 2 cl and 2 cl + 1 of the row; the second panel's threads the odd one first (banks)
+        const int row = r0 + k * W::STEP, p = cl >> 2, c = (cl & 3) * 2;
+        uint8_t* at = tile + p * PANEL + row * 128;
+        const uint4 a = make_uint4(y0.x, y0.y, y1.x, y1.y), z = make_uint4(y2.x, y2.y, y3.x, y3.y);
+        *reinterpret_cast<uint4*>(at + (((c + (p & 1)) ^ (row & 7)) << 4)) = p & 1 ? z : a;
+        *reinterpret_cast<uint4*>(at + (((c + 1 - (p & 1)) ^ (row & 7)) << 4)) = p & 1 ? a : z;
+      }
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive((is_k ? k_full : v_full) + sl);
+      return true;
+    };
+    W w;
+    if (n > 0) fetch(true, 0, w);
+#pragma unroll 1
+    for (int k = 0; ok && k < 2 * n; ++k) {
+      W next;
+      fetch((k & 1) != 0, (k + 1) >> 1, next);
+      ok = put((k & 1) == 0, k >> 1, w);
+      w = next;
+    }
+    if (!ok && lane == 0) give_up(3);
+    if (lane == 0) mbar_arrive(over);
+  }
+  fence_before_sync();
+  __syncthreads();
+  if (warp == 1) {
+    fence_after_sync();
+    tmem_dealloc(tmem, TMEM_COLS);
+  }
+  if (C == 1) return;
+  // ---- the cluster's parts: each CTA joins its share of the rows, a thread a row and D / C columns
+  cluster.sync();
+  if (warp >= 4 && warp < 8) {
+    const int share = BQ / C, row = rank * share + r % share, g = r / share, cols = D / C;
+    const int t2 = row / j.G, h2 = row - t2 * j.G;
+    if (t2 < j.TQ && t2 < tokens) {
+      float M = -INFINITY, sum = 0.f;
+      for (int x = 0; x < C; ++x) M = fmaxf(M, cluster.map_shared_rank(reinterpret_cast<float2*>(smem + L::STATS), x)[row].x);
+      float f[8];
+      for (int x = 0; x < C; ++x) {
+        const float2 y = cluster.map_shared_rank(reinterpret_cast<float2*>(smem + L::STATS), x)[row];
+        f[x] = y.x == -INFINITY && y.y == 0.f ? 0.f : y.x == M || y.x == -INFINITY ? 1.f : ex2(y.x - M);
+        sum = fmaf(f[x], y.y, sum);
+      }
+      const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + h2) * j.o.head +
+                           (int64_t)(q.r0 + first + t2) * j.o.row + g * cols;
+      for (int c = 0; c < cols; c += 8) {
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        for (int x = 0; x < C; ++x) {
+          if (f[x] == 0.f) continue;
+          const float4* src = cluster.map_shared_rank(reinterpret_cast<float4*>(smem + L::JOIN), x) + ((g * cols + c) / 4) * BQ + row;
+          const float4 a = src[0], z = src[BQ];
+          v[0] = fmaf(f[x], a.x, v[0]); v[1] = fmaf(f[x], a.y, v[1]); v[2] = fmaf(f[x], a.z, v[2]); v[3] = fmaf(f[x], a.w, v[3]);
+          v[4] = fmaf(f[x], z.x, v[4]); v[5] = fmaf(f[x], z.y, v[5]); v[6] = fmaf(f[x], z.z, v[6]); v[7] = fmaf(f[x], z.w, v[7]);
+        }
+        *reinterpret_cast<uint4*>(dst + c) = make_uint4(pack_bf16(v[0] * inv, v[1] * inv), pack_bf16(v[2] * inv, v[3] * inv),
+                                                        pack_bf16(v[4] * inv, v[5] * inv), pack_bf16(v[6] * inv, v[7] * inv));
+      }
+    }
+  }
+  cluster.sync();
+}
+
+template <int D, bool E4M3>
+cudaError_t launch_d(const Maps& maps, const Job& job, const CUtensorMap& mq, dim3 grid, int C, cudaStream_t st) {
+  using L = Lay<D, E4M3>;
+  return launch_kernel(chosen_tc<D, E4M3>, grid, L::THREADS, L::BYTES, C, false, st, mq, maps.k, maps.v, job);
+}
+
+template <int D, bool E4M3>
+cudaError_t set_limit() {
+  return taken(cudaFuncSetAttribute(chosen_tc<D, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Lay<D, E4M3>::BYTES));
+}
+
+}  // namespace
+
+cudaError_t chosen_tc_set_smem_limits() {
+  cudaError_t e = set_limit<128, false>();
+  if (e == cudaSuccess) e = set_limit<128, true>();
+  if (e == cudaSuccess) e = set_limit<64, false>();
+  if (e == cudaSuccess) e = set_limit<64, true>();
+  return e;
+}
+
+cudaError_t launch_chosen_tc(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
+                             const Mask& m, const Chosen& how, cudaStream_t st) {
+  const int G = Hq / c.H, TQ = BQ / G, n_sm = sm_count(), tiles = (how.tile + TQ - 1) / TQ;
+  if (n_sm <= 0) return cudaErrorInvalidDevice;
+  CUtensorMap mq;
+  const int64_t dim[4] = {c.d, G, s.rows, c.H};
+  const int64_t head = q.head ? q.head : c.d, row = q.row ? q.row : c.d;   // (one head or row: any stride)
+  const int64_t stride[3] = {head * 2, row * 2, G * head * 2};
+  const int box[4] = {64, G, TQ, 1};
+  if (!make_map_4d(&mq, q.p, 2, dim, stride, box, 128)) return cudaErrorInvalidValue;
+  const Job job{c, s, m, o, how, G, TQ, tiles, (uintptr_t)o.p % 32 == 0 && o.head % 16 == 0 && o.row % 16 == 0};
+  // few units: a cluster each, while its CTAs have four key tiles or more
+  const int64_t units = (int64_t)how.slots * tiles * c.H, key_tiles = (int64_t)how.width * c.page_len / BK;
+  int C = 1;
+  while (C < 4 && units * C <= n_sm && key_tiles >= 8 * C) C *= 2;
+  if ((int64_t)how.slots * tiles * C > 0x7fffffff) return cudaErrorInvalidValue;
+  const dim3 grid(how.slots * tiles * C, c.H);
+  if (c.d == 128)
+    return c.e4m3 ? launch_d<128, true>(maps, job, mq, grid, C, st) : launch_d<128, false>(maps, job, mq, grid, C, st);
+  return c.e4m3 ? launch_d<64, true>(maps, job, mq, grid, C, st) : launch_d<64, false>(maps, job, mq, grid, C, st);
+}
+
+}  // namespace cache
+}  // namespace dkv

@@ -186,7 +186,9 @@ def test_attend(dkv, fmt, d, page, Hq, H, tile, block):
     (5, 1, [(1, 4000), (1, 77)], 16, 1, 240),
     (128, 1, [(2, 600)], 16, 2, 30),               # 256 rows a tile
     (3, 3, [(300, 1200)], 128, 128, 10),
-    (40, 8, [(130, 400)], 32, 64, 12)])
+    (40, 8, [(130, 400)], 32, 64, 12),
+    (2, 1, [(100, 3000), (3, 2900)], 16, 32, 180),  # clusters of four share a tile's list
+    (1, 1, [(128, 1500)], 128, 128, 9)])
 def test_attend_large(dkv, fmt, Hq, H, seqs, page, tile, width):
     case = cache_ref.Case(seqs, H, 128, page, fmt, seed=1)
     c, s = case.cache(dkv), case.device_seqs(dkv)
@@ -212,22 +214,25 @@ def test_every_page_listed_is_dense_attention(dkv, fmt, tile):
     cache_ref.check(O, cache_ref.attend(case, Q))
 
 
-@pytest.mark.parametrize("tile", [1, 2, 5, 64])
+@pytest.mark.parametrize("tile,pages", [(1, 7), (2, 7), (5, 7), (64, 7), (16, 7), (40, 70), (1, 70)])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
-def test_what_is_not_finite(dkv, fmt, tile):
+def test_what_is_not_finite(dkv, fmt, tile, pages):
     """Infinities and NaN in keys and values: they reach the rows that see them, and no others."""
-    case = cache_ref.Case([(40, 100)], 1, 64, 16, fmt, seed=3)
-    at = case.table[0]
+    case = cache_ref.Case([(40, 16 * pages - 12)], 1, 64, 16, fmt, seed=3)
+    at = case.table[0][:pages]
     if fmt == "bf16":
-        case.v[at[4], 0, 2, 5], case.v[at[5], 0, 3, 9], case.v[at[4], 0, 9, 1] = np.inf, np.nan, -np.inf
-        case.k[at[6], 0, 1, 3] = np.nan
-        case.v[at[6], 0, 6:], case.k[at[6], 0, 6:] = np.nan, np.inf      # behind the end
+        case.v[at[-3], 0, 2, 5], case.v[at[-2], 0, 3, 9], case.v[at[-3], 0, 9, 1] = np.inf, np.nan, -np.inf
+        case.k[at[-1], 0, 1, 3] = np.nan
+        case.v[at[-1], 0, 6:], case.k[at[-1], 0, 6:] = np.nan, np.inf      # behind the end
     else:
         for x, xs, full in ((case.vc, case.vs, case.v), (case.kc, case.ks, case.k)):
-            for p, i in ((at[4], 2), (at[6], 1), (at[6], 9)):
+            for p, i in ((at[-3], 2), (at[-1], 1), (at[-1], 9)):
                 x[p, 0, i], xs[p, 0, i], full[p, 0, i] = 0x7F, 255, np.nan
+    else_seen = pages > 60                                            # an infinity that every row sees
+    if else_seen and fmt == "bf16":
+        case.v[at[2], 0, 0, 40] = np.inf
     c, s = case.cache(dkv), case.device_seqs(dkv)
-    lists = random_lists(case, tile, 7, most=7)
+    lists = random_lists(case, tile, pages, most=pages)
     Q = queries(case, 2)
     O = c.attend_chosen(bf(Q), s, t32(lists), tile=tile).double().cpu().numpy()
     want = ref.attend(case, Q, lists, tile)
@@ -235,7 +240,7 @@ def test_what_is_not_finite(dkv, fmt, tile):
         fine = np.isfinite(o)
         assert not np.isfinite(O[h, row][~fine]).any(), (h, row)
         assert (np.abs(O[h, row][fine] - o[fine]) <= tol[fine]).all(), (h, row)
-    assert any(np.isfinite(o).all() for o, _ in want.values()) and any(not np.isfinite(o).all() for o, _ in want.values())
+    assert else_seen or any(np.isfinite(o).all() for o, _ in want.values()) and any(not np.isfinite(o).all() for o, _ in want.values())
 
 
 @pytest.mark.parametrize("tile", [1, 40])
