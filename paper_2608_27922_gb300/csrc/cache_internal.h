@@ -117,6 +117,22 @@ __host__ __device__ __forceinline__ int seq_of_slot(const Seqs& s, int tile, int
   return lo;
 }
 
+#ifdef __CUDACC__
+// The same by a warp: its lanes look at 32 sequences at a time (one or two dependent reads instead of one a halving).
+__device__ __forceinline__ int seq_of_slot_warp(const Seqs& s, int tile, int slot) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0, n = s.n;
+  while (n > 1) {
+    const int step = (n + 31) / 32, b = lo + lane * step;
+    const bool past = b < lo + n && first_slot(s, tile, b) <= slot;
+    const int k = max(__popc(__ballot_sync(0xffffffffu, past)) - 1, 0) * step;   // (in range whatever the array holds)
+    lo += k;
+    n = min(step, n - k);
+  }
+  return lo;
+}
+#endif
+
 // The sequence of a packed row (row < row_start[n]): the last b with row_start[b] <= row.
 __host__ __device__ __forceinline__ int seq_of_row(const Seqs& s, int row) {
   int lo = 0, hi = s.n;

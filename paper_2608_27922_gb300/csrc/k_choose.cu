@@ -50,99 +50,102 @@ __device__ __forceinline__ float scaled(uint32_t code, float f) {   // an e4m3 c
   return (code & 0x80u ? -x : x) * f;
 }
 
-constexpr int SUM_THREADS = 128;
+constexpr int SUM_THREADS = 256;
 
-// Block: pages of one sequence (blockIdx.y), each with one head, in turn.  A row lies with d / 8 threads.
+__device__ __forceinline__ void add(Two& s, const Two& y) {
+  add(s, y.hi);
+  s.lo = __fadd_rn(s.lo, y.lo);
+}
+
+// Block: pages of one sequence (blockIdx.y), each with one head, in turn.  A row lies with d / 8 threads; the rows' sums
+// go over the warp, then one thread a column joins the warps'.
 template <int D, bool E4M3>
 __global__ void __launch_bounds__(SUM_THREADS) summarise(Pool c, Seqs s, const int32_t* first, int8_t* code, uint8_t* scale) {
-  constexpr int LANES = D / 8, ROWS = SUM_THREADS / LANES;
-  __shared__ Two part[ROWS][D];
-  for (int b = blockIdx.y; b < s.n; b += gridDim.y) {
-    const Seq q = seq_at(c, s, b);
-    const int from = max(first ? first[b] : q.len - q.n, 0) >> c.page_log2, pages = (q.len + c.page_len - 1) >> c.page_log2;
-    if (!first && q.n == 0) continue;
-    const int64_t units = (int64_t)max(pages - from, 0) * c.H;
-    for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-      const int h = (int)(u % c.H), k = from + (int)(u / c.H);
-      const int64_t at = pool_row(c, s, b, h, k << c.page_log2);   // (the same for all threads)
-      if (at < 0) continue;
-      const int held = min(c.page_len, q.len - (k << c.page_log2));
-      const int lane = threadIdx.x % LANES, r0 = threadIdx.x / LANES;
-      Two sum[8];
+  constexpr int LANES = D / 8, ROWS = SUM_THREADS / LANES, WARPS = SUM_THREADS / 32;
+  __shared__ Two part[WARPS][D];
+  __shared__ float tops[D / 32];
+  const int b = blockIdx.y, tid = threadIdx.x, lane = tid % LANES, r0 = tid / LANES;
+  const Seq q = seq_at(c, s, b);
+  const int from = max(first ? first[b] : q.len - q.n, 0) >> c.page_log2, pages = (q.len + c.page_len - 1) >> c.page_log2;
+  if (!first && q.n == 0) return;
+  const int64_t units = (int64_t)max(pages - from, 0) * c.H;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int h = (int)(u % c.H), k = from + (int)(u / c.H);
+    const int64_t at = pool_row(c, s, b, h, k << c.page_log2);   // (the same for all threads)
+    if (at < 0) continue;
+    const int held = min(c.page_len, q.len - (k << c.page_log2));
+    Two sum[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] = Two{0.f, 0.f};
+    for (int i = 0; i < 8; ++i) sum[i] = Two{0.f, 0.f};
 #pragma unroll 4
-      for (int r = r0; r < held; r += ROWS) {
-        float x[8];
-        if (E4M3) {
-          const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.k) + (at + r) * D) + lane);
-          const float f = scale_of(c.ks[at + r]);
+    for (int r = r0; r < held; r += ROWS) {
+      float x[8];
+      if (E4M3) {
+        const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.k) + (at + r) * D) + lane);
+        const float f = scale_of(c.ks[at + r]);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = scaled((i < 4 ? v.x >> (8 * i) : v.y >> (8 * i - 32)) & 0xffu, f);
-        } else {
-          const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(c.k) + (at + r) * D) + lane);
-          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+        for (int i = 0; i < 8; ++i) x[i] = scaled((i < 4 ? v.x >> (8 * i) : v.y >> (8 * i - 32)) & 0xffu, f);
+      } else {
+        const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(c.k) + (at + r) * D) + lane);
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-          }
+        for (int i = 0; i < 4; ++i) {
+          x[2 * i] = __uint_as_float(w[i] << 16);
+          x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) add(sum[i], x[i]);
       }
-      __syncthreads();   // (the last unit's sums have been read)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) part[r0][lane * 8 + i] = sum[i];
-      __syncthreads();
-      if (threadIdx.x < 32) {
-        constexpr int COLS = D / 32;
-        Two mean[COLS];
-        float top = 0.f;
-        bool fine = true;
+      for (int i = 0; i < 8; ++i) add(sum[i], x[i]);
+    }
 #pragma unroll
-        for (int i = 0; i < COLS; ++i) {
-          Two m = part[0][threadIdx.x * COLS + i];
-#pragma unroll 1
-          for (int r = 1; r < ROWS; ++r) {
-            const Two y = part[r][threadIdx.x * COLS + i];
-            add(m, y.hi);
-            m.lo = __fadd_rn(m.lo, y.lo);
-          }
-          m = settled(m);
-          if ((held & (held - 1)) == 0) {
-            const float f = 1.0f / (float)held;
-            m.hi *= f;
-            m.lo *= f;
-          } else {
-            const double y = ((double)m.hi + (double)m.lo) / (double)held;
-            m.hi = (float)y;
-            m.lo = (float)(y - (double)m.hi);
-          }
-          mean[i] = m;
-          fine = fine && fabsf(m.hi) < WILD;   // (false for a NaN)
-          // a magnitude that lies above hi's counts as the next float
-          const float a = fabsf(m.hi);
-          const bool above = m.hi < 0.f ? m.lo < 0.f : m.lo > 0.f;
-          top = fmaxf(top, above && (__float_as_uint(a) & 0x7fffffu) == 0x7e0000u ? __uint_as_float(__float_as_uint(a) + 1) : a);
-        }
+    for (int i = 0; i < 8; ++i) {
 #pragma unroll
-        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-        fine = __all_sync(0xffffffffu, fine);
-        const int e = fine ? exponent_of(top) : 0;
-        uint32_t packed = 0;
+      for (int o = LANES; o < 32; o <<= 1)
+        add(sum[i], Two{__shfl_xor_sync(0xffffffffu, sum[i].hi, o), __shfl_xor_sync(0xffffffffu, sum[i].lo, o)});
+    }
+    __syncthreads();   // (the last unit's sums have been read)
+    if (tid % 32 < LANES) {
 #pragma unroll
-        for (int i = 0; i < COLS; ++i) {
-          const float y = mean[i].hi * pow2(-e);
-          float r = rintf(y);
-          if (fabsf(y - r) == 0.5f && mean[i].lo != 0.f) r = mean[i].lo > 0.f ? floorf(y) + 1.f : floorf(y);   // no tie
-          packed |= (uint32_t)((fine ? (int)r : 0) & 0xff) << (8 * i);
-        }
-        const int64_t row = at >> c.page_log2;   // page * H + h
-        if (COLS == 4) reinterpret_cast<uint32_t*>(code + row * D)[threadIdx.x] = packed;
-        else reinterpret_cast<uint16_t*>(code + row * D)[threadIdx.x] = (uint16_t)packed;
-        if (threadIdx.x == 0) scale[row] = fine ? (uint8_t)(e + 127) : 255;
+      for (int i = 0; i < 8; ++i) part[tid / 32][lane * 8 + i] = sum[i];
+    }
+    __syncthreads();
+    Two m{0.f, 0.f};
+    if (tid < D) {
+      m = part[0][tid];
+#pragma unroll
+      for (int w = 1; w < WARPS; ++w) add(m, part[w][tid]);
+      m = settled(m);
+      if ((held & (held - 1)) == 0) {
+        const float f = 1.0f / (float)held;
+        m.hi *= f;
+        m.lo *= f;
+      } else {
+        const double y = ((double)m.hi + (double)m.lo) / (double)held;
+        m.hi = (float)y;
+        m.lo = (float)(y - (double)m.hi);
       }
+      // a magnitude that lies above hi's counts as the next float; one without codes as an infinity
+      const float a = fabsf(m.hi);
+      const bool above = m.hi < 0.f ? m.lo < 0.f : m.lo > 0.f;
+      float top = above && (__float_as_uint(a) & 0x7fffffu) == 0x7e0000u ? __uint_as_float(__float_as_uint(a) + 1) : a;
+      if (!(a < WILD)) top = INFINITY;
+#pragma unroll
+      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+      if (tid % 32 == 0) tops[tid / 32] = top;
+    }
+    __syncthreads();
+    if (tid < D) {
+      float top = tops[0];
+#pragma unroll
+      for (int w = 1; w < D / 32; ++w) top = fmaxf(top, tops[w]);
+      const bool fine = top < INFINITY;
+      const int e = fine ? exponent_of(top) : 0;
+      const float y = m.hi * pow2(-e);
+      float r = rintf(y);
+      if (fabsf(y - r) == 0.5f && m.lo != 0.f) r = m.lo > 0.f ? floorf(y) + 1.f : floorf(y);   // no tie
+      const int64_t row = at >> c.page_log2;   // page * H + h
+      code[row * D + tid] = fine ? (int8_t)(int)r : 0;
+      if (tid == 0) scale[row] = fine ? (uint8_t)(e + 127) : 255;
     }
   }
 }
@@ -151,6 +154,7 @@ __global__ void __launch_bounds__(SUM_THREADS) summarise(Pool c, Seqs s, const i
 constexpr int CH_THREADS = 256;
 constexpr int CAP = 2048;        // pages looked at in one go
 constexpr int MAX_TOP = 1024;
+constexpr int PLACES = CAP + MAX_TOP;
 
 // Order of scores as unsigned numbers; 0: not to be listed.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -162,14 +166,16 @@ template <int D>
 struct Work {
   static constexpr int STRIDE = D + 4;   // halves of a row: 8-byte reads of 4 lanes x 4 rows touch every bank once
   __half q[64][STRIDE];
-  float unit[64];                // 2^e of a row, 0: none
-  uint32_t key[MAX_TOP + CAP];   // what has been kept so far, then this part's pages
-  int page[MAX_TOP + CAP];       //   ascending
+  float unit[64];            // 2^e of a row, 0: none
+  alignas(16) uint32_t key[PLACES];      // what has been kept so far, then this part's pages (first their best scores)
+  int page[PLACES];          //   ascending
+  int at[CAP];               // of this part's pages: place in the pool
+  float scale[CAP];          //   and 2^e of the summary, 0: not to be listed
   uint32_t kept_key[MAX_TOP];
   int kept_page[MAX_TOP];
-  int hist[256];
-  int warp_sum[2][8];
-  int kept, digit, below;
+  uint32_t lo[8], hi[8];
+  int total[8];
+  int kept, below;
 };
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
@@ -188,89 +194,111 @@ __device__ __forceinline__ void widen4(uint32_t w, uint32_t& a, uint32_t& b) {
   b = *reinterpret_cast<const uint32_t*>(&q);
 }
 
-// The `top` largest of key[0 .. n) (equal ones: the first), in their order, into kept_key and kept_page.
-template <int D>
-__device__ __forceinline__ void keep_best(Work<D>& w, int n, int top) {
+// The `top` largest of key[0 .. n), equal ones: the first, in their order, into kept_key and kept_page.  Thread t holds
+// places t PER ..; halving the range of the keys with counts over the block finds a bound with `top` keys above
+// it, or the top-th key itself where others equal it.
+template <int PER, typename W>
+__device__ __forceinline__ void keep_best(W& w, int n, int top) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  // the top-th largest key T, digit by digit, and how many of those equal to it are kept
-  uint32_t T = 0;
-  int need = top;
-#pragma unroll 1
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    w.hist[tid] = 0;
-    __syncthreads();
-    for (int i = tid; i < n; i += CH_THREADS) {
-      const uint32_t k = w.key[i];
-      if (k && (shift == 24 || (k >> (shift + 8)) == (T >> (shift + 8)))) atomicAdd(&w.hist[(k >> shift) & 255], 1);
-    }
-    __syncthreads();
-    if (warp == 0) {   // lane: digits 255 - 8 lane, .. downwards
-      int own = 0, c[8];
+  uint32_t k[PER], least = 0xffffffffu, most = 0;
+  int valid = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) own += c[i] = w.hist[255 - lane * 8 - i];
-      int incl = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += y;
-      }
-      const unsigned past = __ballot_sync(0xffffffffu, incl >= need);
-      if (past == 0) {
-        if (lane == 0) w.digit = -1;   // fewer than `top` in all (first digit only)
-      } else if (lane == __ffs(past) - 1) {
-        int above = incl - own, i = 0;
-        while (above + c[i] < need) above += c[i++];
-        w.digit = 255 - lane * 8 - i;
-        w.below = above;
-      }
+  for (int i = 0; i < PER; ++i) {
+    k[i] = tid * PER + i < n ? w.key[tid * PER + i] : 0;
+    if (k[i]) {
+      least = min(least, k[i]);
+      most = max(most, k[i]);
+      ++valid;
     }
-    __syncthreads();
-    if (w.digit < 0) {
-      T = 0;
-      break;
-    }
-    T |= (uint32_t)w.digit << shift;
-    need -= w.below;
-    __syncthreads();
   }
-  // (T = 0: all keys but 0 are kept)
-  if (tid == 0) w.kept = 0;
-  int equal = 0, out = 0;
-  for (int base = 0; base < n; base += CH_THREADS) {
-    const int i = base + tid;
-    const uint32_t k = i < n ? w.key[i] : 0;
-    const bool eq = T && k == T;
-    const unsigned e = __ballot_sync(0xffffffffu, eq), g = __ballot_sync(0xffffffffu, k > T);
-    __syncthreads();
-    if (lane == 0) {
-      w.warp_sum[0][warp] = __popc(e);
-      w.warp_sum[1][warp] = __popc(g);
-    }
-    __syncthreads();
-    int eq_before = equal, gt_before = 0, eq_all = 0, gt_all = 0;
-#pragma unroll
-    for (int x = 0; x < 8; ++x) {
-      if (x < warp) {
-        eq_before += w.warp_sum[0][x];
-        gt_before += w.warp_sum[1][x];
-      }
-      eq_all += w.warp_sum[0][x];
-      gt_all += w.warp_sum[1][x];
-    }
-    const unsigned lt = (1u << lane) - 1u;
-    eq_before += __popc(e & lt);
-    gt_before += __popc(g & lt);
-    // kept before this place: the larger ones and the first `need` equal ones
-    const int at = out + gt_before + (min(eq_before, need) - min(equal, need));
-    if (k > T || (eq && eq_before < need)) {
-      w.kept_key[at] = k;
-      w.kept_page[at] = w.page[i];
-    }
-    out += gt_all + (min(equal + eq_all, need) - min(equal, need));
-    equal += eq_all;
+  least = __reduce_min_sync(0xffffffffu, least);
+  most = __reduce_max_sync(0xffffffffu, most);
+  valid = __reduce_add_sync(0xffffffffu, valid);
+  if (lane == 0) {
+    w.lo[warp] = least;
+    w.hi[warp] = most;
+    w.total[warp] = valid;
   }
-  if (tid == 0) w.kept = out;
   __syncthreads();
+  valid = 0;
+#pragma unroll
+  for (int x = 0; x < CH_THREADS / 32; ++x) {
+    least = min(least, w.lo[x]);
+    most = max(most, w.hi[x]);
+    valid += w.total[x];
+  }
+  // keys > T are kept, and `need` of those equal to T
+  uint32_t T = 0;
+  int need = 0;
+  if (valid > top) {
+    // lo: more than `top` keys >= lo; hi: at most `top` keys >= hi
+    uint32_t lo = least, hi = most + 1;   // (no key is 0xffffffff: that would be a NaN)
+    int above = 0;                        // keys >= hi
+#pragma unroll 1
+    while (hi - lo > 1 && above != top) {
+      const uint32_t mid = lo + (hi - lo) / 2;
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) c += k[i] >= mid;
+      c = __reduce_add_sync(0xffffffffu, c);
+      __syncthreads();
+      if (lane == 0) w.total[warp] = c;
+      __syncthreads();
+      c = 0;
+#pragma unroll
+      for (int x = 0; x < CH_THREADS / 32; ++x) c += w.total[x];
+      if (c > top) {
+        lo = mid;
+      } else {
+        hi = mid;
+        above = c;
+      }
+    }
+    T = hi - 1;
+    need = top - above;   // (0 unless hi = lo + 1: then T = lo is the top-th key)
+  }
+  int eq = 0, gt = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    eq += T && k[i] == T;
+    gt += k[i] > T;
+  }
+  // sums over the threads before: equal ones in the upper half
+  const int mine = eq << 16 | gt;
+  int incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += y;
+  }
+  __syncthreads();
+  if (lane == 31) w.total[warp] = incl;
+  __syncthreads();
+  int before = incl - mine, all = 0;
+#pragma unroll
+  for (int x = 0; x < CH_THREADS / 32; ++x) {
+    if (x < warp) before += w.total[x];
+    all += w.total[x];
+  }
+  int eq_before = before >> 16, gt_before = before & 0xffff;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const bool same = T && k[i] == T;
+    if (k[i] > T || (same && eq_before < need)) {
+      const int at = gt_before + min(eq_before, need);
+      w.kept_key[at] = k[i];
+      w.kept_page[at] = w.page[tid * PER + i];
+    }
+    eq_before += same;
+    gt_before += k[i] > T;
+  }
+  if (tid == 0) w.kept = (all & 0xffff) + min(all >> 16, need);
+  __syncthreads();
+}
+template <typename W>
+__device__ __forceinline__ void keep_best(W& w, int n, int top) {
+  if (n <= 4 * CH_THREADS) keep_best<4>(w, n, top);
+  else keep_best<PLACES / CH_THREADS>(w, n, top);
 }
 
 // Cluster: one list (slot blockIdx.x / CTAs of the cluster, head blockIdx.y); its CTAs share the seen pages.
@@ -285,7 +313,7 @@ __global__ void __launch_bounds__(CH_THREADS) choose(Pool c, Seqs s, const int8_
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   if (blockIdx.x == 0 && h == 0)
     for (int b = tid; b < s.n; b += CH_THREADS) seq_at(c, s, b);
-  const int b = seq_of_slot(s, how.tile, slot);
+  const int b = seq_of_slot_warp(s, how.tile, slot);
   const Seq q = seq_at(c, s, b);
   const int i0 = (slot - first_slot(s, how.tile, b)) * how.tile;
   int32_t* line = lists + ((int64_t)h * slots + slot) * how.width;
@@ -308,17 +336,28 @@ __global__ void __launch_bounds__(CH_THREADS) choose(Pool c, Seqs s, const int8_
 #pragma unroll 1
     for (int k0 = a; k0 < z; k0 += CAP) {
       const int n = min(CAP, z - k0);
+      float* score = reinterpret_cast<float*>(w.key + kept);
+      for (int i = tid; i < n; i += CH_THREADS) {
+        const int k = k0 + i;
+        const int64_t row = pool_row(c, s, b, h, k << c.page_log2);
+        const int64_t at = row >> c.page_log2;   // page * H + h
+        const uint32_t byte = row >= 0 ? scale[at] : 255u;
+        const bool listed = k < sinks || (k >= lo && k <= own);
+        w.at[i] = row >= 0 ? (int)(at / c.H) : -1;
+        w.scale[i] = listed || byte == 255u ? 0.f : scale_of(byte);
+        w.page[kept + i] = k;
+        score[i] = -INFINITY;
+      }
       for (int i = tid; i < kept; i += CH_THREADS) {
         w.key[i] = w.kept_key[i];
         w.page[i] = w.kept_page[i];
       }
-      float* score = reinterpret_cast<float*>(w.key + kept);
-      for (int i = tid; i < n; i += CH_THREADS) score[i] = -INFINITY;
 #pragma unroll 1
       for (int r0 = 0; r0 < R; r0 += 64) {
-        const int rows = min(64, R - r0);
+        const int rows = min(64, R - r0), used = (rows + 15) & ~15;
         __syncthreads();   // (the last rows have been used)
-        for (int r = warp; r < 64; r += CH_THREADS / 32) {   // codes of the rows
+#pragma unroll 4
+        for (int r = warp; r < used; r += CH_THREADS / 32) {   // codes of the rows
           float x[D / 32];
           if (r < rows) {
             const int i = (r0 + r) / G, hq = h * G + (r0 + r) - i * G;
@@ -338,61 +377,55 @@ __global__ void __launch_bounds__(CH_THREADS) choose(Pool c, Seqs s, const int8_
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) x[k] = __int_as_float(0x7fffffff);
           }
-          float top = 0.f;
-          bool fine = true;
+          uint32_t top = 0;   // (bits of magnitudes order like the magnitudes, NaN above infinity)
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k) {
-            fine = fine && fabsf(x[k]) < WILD;
-            top = fmaxf(top, fabsf(x[k]));
-          }
-#pragma unroll
-          for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-          fine = __all_sync(0xffffffffu, fine);
-          const int e = fine ? exponent_of(top) : 0;
+          for (int k = 0; k < D / 32; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+          top = __reduce_max_sync(0xffffffffu, top);
+          const bool fine = top < __float_as_uint(WILD);
+          const int e = fine ? exponent_of(__uint_as_float(top)) : 0;
           const float f = fine ? pow2(-e) : 0.f;
 #pragma unroll
           for (int k = 0; k < D / 32; ++k) w.q[r][lane * (D / 32) + k] = __float2half_rn(fine ? rintf(x[k] * f) : 0.f);
           if (lane == 0) w.unit[r] = fine ? pow2(e) : 0.f;
         }
         __syncthreads();
-        const int tiles = (rows + 15) / 16;
+        // eight pages a warp: page j + g's codes, 16 bytes at 16 t (and at 64 + 16 t), the next eight's on their way
+        auto codes = [&](int j, uint4 (&v)[D / 64]) {
+          const int at = j + g < n ? w.at[j + g] : -1;
+#pragma unroll
+          for (int x = 0; x < D / 64; ++x)
+            v[x] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(code + ((int64_t)at * c.H + h) * D + x * 64) + t) : make_uint4(0, 0, 0, 0);
+        };
+        uint4 v[D / 64];
+        codes(warp * 8, v);
 #pragma unroll 1
         for (int j0 = warp * 8; j0 < n; j0 += CH_THREADS / 32 * 8) {
-          // page j0 + g's codes: 16 bytes at 16 t (and at 64 + 16 t)
-          const int j = k0 + j0 + g;
-          int64_t row = -1;
-          if (j0 + g < n) {
-            row = pool_row(c, s, b, h, j << c.page_log2);
-            if (row >= 0) row >>= c.page_log2;
-          }
-          uint32_t w8[D / 16];
+          uint32_t B[D / 8];
 #pragma unroll
           for (int x = 0; x < D / 64; ++x) {
-            const uint4 v = row >= 0 ? __ldg(reinterpret_cast<const uint4*>(code + row * D + x * 64) + t) : make_uint4(0, 0, 0, 0);
-            w8[4 * x] = v.x;
-            w8[4 * x + 1] = v.y;
-            w8[4 * x + 2] = v.z;
-            w8[4 * x + 3] = v.w;
+            widen4(v[x].x, B[8 * x], B[8 * x + 1]);
+            widen4(v[x].y, B[8 * x + 2], B[8 * x + 3]);
+            widen4(v[x].z, B[8 * x + 4], B[8 * x + 5]);
+            widen4(v[x].w, B[8 * x + 6], B[8 * x + 7]);
           }
+          codes(j0 + CH_THREADS / 32 * 8, v);
           float best[2] = {-INFINITY, -INFINITY};
 #pragma unroll 1
-          for (int mt = 0; mt < tiles; ++mt) {
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+          for (int mt = 0; mt < used; mt += 16) {
+            float acc[4] = {0.f, 0.f, 0.f, 0.f}, ac2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int i = 0; i < D / 16; ++i) {
               const int col = (i >> 2) * 64 + t * 16 + (i & 3) * 4;
-              const uint2 x = *reinterpret_cast<const uint2*>(&w.q[mt * 16 + g][col]);
-              const uint2 y = *reinterpret_cast<const uint2*>(&w.q[mt * 16 + g + 8][col]);
+              const uint2 x = *reinterpret_cast<const uint2*>(&w.q[mt + g][col]);
+              const uint2 y = *reinterpret_cast<const uint2*>(&w.q[mt + g + 8][col]);
               const uint32_t A[4] = {x.x, y.x, x.y, y.y};
-              uint32_t b0, b1;
-              widen4(w8[i], b0, b1);
-              mma_f16(acc, A, b0, b1);
+              mma_f16(i & 1 ? ac2 : acc, A, B[2 * i], B[2 * i + 1]);
             }
-            const float u0 = w.unit[mt * 16 + g], u1 = w.unit[mt * 16 + g + 8];
+            const float u0 = w.unit[mt + g], u1 = w.unit[mt + g + 8];
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
-              if (u0 != 0.f) best[x] = fmaxf(best[x], acc[x] * u0);
-              if (u1 != 0.f) best[x] = fmaxf(best[x], acc[2 + x] * u1);
+              if (u0 != 0.f) best[x] = fmaxf(best[x], (acc[x] + ac2[x]) * u0);
+              if (u1 != 0.f) best[x] = fmaxf(best[x], (acc[2 + x] + ac2[2 + x]) * u1);
             }
           }
 #pragma unroll
@@ -402,29 +435,21 @@ __global__ void __launch_bounds__(CH_THREADS) choose(Pool c, Seqs s, const int8_
           }
           if (g < 2) {   // page 2 t + g of the eight
             const int x = j0 + 2 * t + g;
-            if (x < n) score[x] = fmaxf(score[x], best[g]);
+            if (x < n) {
+              const float y = fmaxf(score[x], best[g]);
+              if (r0 + 64 < R) score[x] = y;
+              else w.key[kept + x] = w.scale[x] != 0.f && y > -INFINITY ? key_of(y * w.scale[x]) : 0;   // the last rows
+            }
           }
         }
-      }
-      __syncthreads();
-      for (int i = tid; i < n; i += CH_THREADS) {
-        const int k = k0 + i;
-        float x = score[i];
-        const int64_t row = pool_row(c, s, b, h, k << c.page_log2);
-        const uint32_t byte = row >= 0 ? scale[row >> c.page_log2] : 255u;
-        const bool listed = k < sinks || (k >= lo && k <= own);
-        uint32_t key = 0;
-        if (!listed && byte != 255u && x > -INFINITY) key = key_of(x * scale_of(byte));
-        w.key[kept + i] = key;
-        w.page[kept + i] = k;
       }
       __syncthreads();
       keep_best(w, kept + n, how.top);
       kept = w.kept;
     }
   }
-  if (tid == 0) w.kept = kept;
   if (C > 1) {
+    if (tid == 0) w.kept = kept;
     cluster.sync();
     if (rank == 0) {   // the shares' best, in their order, and the best of those
       int n = 0;
@@ -445,15 +470,12 @@ __global__ void __launch_bounds__(CH_THREADS) choose(Pool c, Seqs s, const int8_
     if (rank) return;
   }
   // sinks, then the chosen pages and the local ones as they ascend
-  __syncthreads();
   const int l0 = max(lo, sinks), locals = max(own - l0 + 1, 0);
-  if (tid == 0) w.below = 0;
-  __syncthreads();
-  int before = 0;
-  for (int i = tid; i < kept; i += CH_THREADS) before += w.kept_page[i] < l0;
-  if (before) atomicAdd(&w.below, before);
-  __syncthreads();
-  before = w.below;
+  int before = 0;   // chosen pages before the local ones: a halving search
+  for (int top = kept; before < top;) {
+    const int mid = (before + top) / 2;
+    if (w.kept_page[mid] < l0) before = mid + 1; else top = mid;
+  }
   const int count = sinks + kept + locals;
   for (int i = tid; i < sinks; i += CH_THREADS) line[i] = i;
   for (int i = tid; i < locals; i += CH_THREADS) line[sinks + before + i] = l0 + i;
@@ -486,7 +508,8 @@ cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, cons
   if (n_sm <= 0) return cudaErrorInvalidDevice;
   const int slots = s.rows / how.tile + s.n;
   int C = 1;
-  while (C < 8 && (int64_t)slots * c.H * C * 2 <= 2 * n_sm && s.max_pages / C > 128 && 2 * C * how.top <= MAX_TOP + CAP) C *= 2;
+  const int64_t lines = (int64_t)std::min(slots, s.rows) * c.H;   // (a tile has a row or more)
+  while (C < 8 && lines * C <= n_sm && s.max_pages / C > 128 && 2 * C * how.top <= MAX_TOP + CAP) C *= 2;
   const dim3 grid(slots * C, c.H);
   if (c.d == 128)
     return launch_kernel(choose<128>, grid, CH_THREADS, sizeof(Work<128>), C, false, st, c, s, code, scale, q, Hq / c.H, how, lists);

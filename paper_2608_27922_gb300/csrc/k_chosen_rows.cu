@@ -28,7 +28,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int WARPS = 8, THREADS = WARPS * 32, MAX_WIDTH = 1024;
+constexpr int WARPS = 6, THREADS = WARPS * 32, MAX_WIDTH = 1024;
 constexpr float RAISE_LOG2 = 8.0f;   // how far a score may pass the running maximum before that is raised
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
   const int unit = blockIdx.x / C, slot = unit / blocks, r0 = (unit - slot * blocks) * 8, h = blockIdx.y;
   if (blockIdx.x == 0 && h == 0)
     for (int b = tid; b < s.n; b += THREADS) seq_at(c, s, b);
-  const int b = seq_of_slot(s, how.tile, slot);
+  const int b = seq_of_slot_warp(s, how.tile, slot);
   const Seq q = seq_at(c, s, b);
   const int i0 = (slot - first_slot(s, how.tile, b)) * how.tile;
   const int tokens = min(how.tile, q.n - i0), R = tokens * G;
@@ -202,16 +202,27 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
   float o[D / 16][4], mrun[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
+  // a step's place: its first position, and lane g's row of the pool (-1: nothing to be read)
+  auto place = [&](int st, int& pos0, int64_t& at) {
+    pos0 = 0x40000000;
+    at = -1;
+    if (st >= last) return;
+    const int k = st >> sub, in = (st & ((1 << sub) - 1)) * 16;
+    if (w.page[k] < 0) return;
+    pos0 = (w.entry[k] << c.page_log2) + in;
+    at = ((int64_t)w.page[k] << c.page_log2) + in + g;
+  };
+  // Keys (values) of the next step are asked for as soon as this one's have gone into their product.  (Positions
+  // that nobody sees may lie behind the sequence: keys there are read, the page is there, and masked.)
+  int pos0, next0;
+  int64_t at, next;
+  place(first, pos0, at);
+  Raw<D, E4M3> k0 = fetch<D, E4M3>(c.k, c.ks, at, t), k1 = fetch<D, E4M3>(c.k, c.ks, at < 0 ? at : at + 8, t);
+  Raw<D, E4M3> v0 = fetch<D, E4M3>(c.v, c.vs, pos0 + g < any_end ? at : -1, t);
+  Raw<D, E4M3> v1 = fetch<D, E4M3>(c.v, c.vs, pos0 + g + 8 < any_end ? at + 8 : -1, t);
 #pragma unroll 1
-  for (int st = first; st < last; ++st) {
-    const int k = st >> sub, slot0 = (st & ((1 << sub) - 1)) * 16, pos0 = (w.entry[k] << c.page_log2) + slot0;
-    const int page = w.page[k];
-    if (page < 0 || pos0 >= any_end) continue;   // (the same for the warp)
-    const int64_t at = ((int64_t)page << c.page_log2) + slot0 + g;
-    // positions that nobody sees may lie behind the sequence: they are read (the page is there) and masked
-    const Raw<D, E4M3> k0 = fetch<D, E4M3>(c.k, c.ks, at, t), k1 = fetch<D, E4M3>(c.k, c.ks, at + 8, t);
-    const Raw<D, E4M3> v0 = fetch<D, E4M3>(c.v, c.vs, pos0 + g < any_end ? at : -1, t);
-    const Raw<D, E4M3> v1 = fetch<D, E4M3>(c.v, c.vs, pos0 + g + 8 < any_end ? at + 8 : -1, t);
+  for (int st = first; st < last; ++st, pos0 = next0, at = next) {
+    place(st + 1, next0, next);
     float sc[4] = {0.f, 0.f, 0.f, 0.f}, sd[4] = {0.f, 0.f, 0.f, 0.f};
     {
       const Frag<D> a = numbers<D, E4M3>(k0), z = numbers<D, E4M3>(k1);
@@ -221,6 +232,8 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
         mma(sd, a.w[2 * i + 2], z.w[2 * i + 2], a.w[2 * i + 3], z.w[2 * i + 3], Q.w[2 * i + 2], Q.w[2 * i + 3]);
       }
     }
+    k0 = fetch<D, E4M3>(c.k, c.ks, next, t);
+    k1 = fetch<D, E4M3>(c.k, c.ks, next < 0 ? next : next + 8, t);
 #pragma unroll
     for (int e = 0; e < 4; ++e) sc[e] += sd[e];
     const bool partial = pos0 + 16 > all_end;
@@ -274,6 +287,8 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
 #pragma unroll
     for (int k2 = 0; k2 < D / 16; ++k2)
       mma(o[k2], transpose(a.w[2 * k2]), transpose(a.w[2 * k2 + 1]), transpose(z.w[2 * k2]), transpose(z.w[2 * k2 + 1]), b0, b1);
+    v0 = fetch<D, E4M3>(c.v, c.vs, next0 + g < any_end ? next : -1, t);
+    v1 = fetch<D, E4M3>(c.v, c.vs, next0 + g + 8 < any_end ? next + 8 : -1, t);
     // values that are not finite, where some row may not see them: to the rows that do
     if (partial && __any_sync(0xffffffffu, wild)) {
 #pragma unroll 1
@@ -326,30 +341,38 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
       for (int k = 0; k < D / 32; ++k) x[k] = fmaf(f, y[lane * (D / 32) + k], x[k]);
     }
   };
-  float M, L, x[D / 32];
-  join([&](int i) -> const float* { return w.part[i][warp]; }, WARPS, M, L, x);   // (row `warp`)
-  if (C > 1) {
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) w.joined[warp][lane * (D / 32) + k] = x[k];
-    if (lane == 0) {
-      w.joined[warp][D] = M;
-      w.joined[warp][D + 1] = L;
+  auto store = [&](int row, float L, const float (&x)[D / 32]) {
+    if (row >= rows) return;
+    const float inv = L == 0.f ? 0.f : 1.0f / L;   // (a NaN stays one)
+    const int r = r0 + row, i = r / G, hq = h * G + r - i * G;
+    __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(op.p) + hq * op.head + (int64_t)(q.r0 + i0 + i) * op.row + lane * (D / 32);
+    if (D == 128) {
+      *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[D / 32 - 2] * inv, x[D / 32 - 1] * inv));
+    } else {
+      *reinterpret_cast<uint32_t*>(dst) = pack_bf16(x[0] * inv, x[1] * inv);
     }
-    cluster.sync();
-    if (rank == 0)
-      join([&](int i) -> const float* { return cluster.map_shared_rank(&w, i)->joined[warp]; }, C, M, L, x);
-    cluster.sync();
-    if (rank) return;
+  };
+  float M, L, x[D / 32];
+  for (int row = warp; row < rows; row += WARPS) {
+    join([&](int i) -> const float* { return w.part[i][row]; }, WARPS, M, L, x);
+    if (C == 1) {
+      store(row, L, x);
+      continue;
+    }
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) w.joined[row][lane * (D / 32) + k] = x[k];
+    if (lane == 0) {
+      w.joined[row][D] = M;
+      w.joined[row][D + 1] = L;
+    }
   }
-  if (warp >= rows) return;
-  const float inv = L == 0.f ? 0.f : 1.0f / L;   // (a NaN stays one)
-  const int r = r0 + warp, i = r / G, hq = h * G + r - i * G;
-  __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(op.p) + hq * op.head + (int64_t)(q.r0 + i0 + i) * op.row + lane * (D / 32);
-  if (D == 128) {
-    *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(x[0] * inv, x[1] * inv), pack_bf16(x[D / 32 - 2] * inv, x[D / 32 - 1] * inv));
-  } else {
-    *reinterpret_cast<uint32_t*>(dst) = pack_bf16(x[0] * inv, x[1] * inv);
+  if (C == 1) return;
+  cluster.sync();
+  for (int row = rank + C * warp; row < rows; row += C * WARPS) {   // (the CTAs share the rows)
+    join([&](int i) -> const float* { return cluster.map_shared_rank(&w, i)->joined[row]; }, C, M, L, x);
+    store(row, L, x);
   }
+  cluster.sync();
 }
 
 }  // namespace
@@ -361,7 +384,8 @@ cudaError_t launch_chosen_rows(const Pool& c, const Seqs& s, const Packed& q, co
   const int blocks = (how.tile * G + 7) / 8;
   // a cluster for each unit, as large as leaves two CTAs an SM and a warp a step or more
   int C = 1;
-  while (C < 8 && (int64_t)how.slots * blocks * c.H * C <= n_sm && how.width * (c.page_len / 16) >= 2 * C * WARPS) C *= 2;
+  const int64_t units = (int64_t)std::min(how.slots, s.rows) * blocks * c.H;   // (a tile has a row or more)
+  while (C < 8 && units * C <= n_sm && how.width * (c.page_len / 16) >= 2 * C * WARPS) C *= 2;
   if ((int64_t)how.slots * blocks * C > 0x7fffffff) return cudaErrorInvalidValue;
   const dim3 grid(how.slots * blocks * C, c.H);
   auto* f = c.d == 128 ? (c.e4m3 ? chosen_rows<128, true> : chosen_rows<128, false>)

@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   const int unit = blockIdx.x / C, slot = unit / j.tiles, qt = unit - slot * j.tiles, h = blockIdx.y;
   if (blockIdx.x == 0 && h == 0)
     for (int b = tid; b < j.s.n; b += L::THREADS) seq_at(j.c, j.s, b);
-  const int b = seq_of_slot(j.s, j.how.tile, slot);
+  const int b = seq_of_slot_warp(j.s, j.how.tile, slot);
   const Seq q = seq_at(j.c, j.s, b);
   const int i0 = (slot - first_slot(j.s, j.how.tile, b)) * j.how.tile;
   const int first = i0 + qt * j.TQ;                                        // its first token
@@ -659,7 +659,7 @@ cudaError_t launch_chosen_tc(const Pool& c, const Maps& maps, const Seqs& s, con
   if (!make_map_4d(&mq, q.p, 2, dim, stride, box, 128)) return cudaErrorInvalidValue;
   const Job job{c, s, m, o, how, G, TQ, tiles, (uintptr_t)o.p % 32 == 0 && o.head % 16 == 0 && o.row % 16 == 0};
   // few units: a cluster each, while its CTAs have four key tiles or more
-  const int64_t units = (int64_t)how.slots * tiles * c.H, key_tiles = (int64_t)how.width * c.page_len / BK;
+  const int64_t units = (int64_t)std::min(how.slots, s.rows) * tiles * c.H, key_tiles = (int64_t)how.width * c.page_len / BK;
   int C = 1;
   while (C < 4 && units * C <= n_sm && key_tiles >= 8 * C) C *= 2;
   if ((int64_t)how.slots * tiles * C > 0x7fffffff) return cudaErrorInvalidValue;

@@ -19,7 +19,7 @@ namespace cache {
 
 namespace {
 
-constexpr int PLANNERS = 8;       // CTAs of a cluster that plan a call
+constexpr int PLANNERS = 8;       // CTAs that plan a call on a large pool
 constexpr int PLAN_THREADS = 1024;
 constexpr int MAX_SEQS = 4096;
 constexpr int COPY_THREADS = 256;
@@ -99,91 +99,112 @@ __global__ void __launch_bounds__(128) cache_release(Pool c, int32_t* refs, Tabl
 }
 
 // ------------------------------------------------------------------ fresh pages
-// What a sequence asks for in a plan: `fresh` pages for the entries k0, k0 + 1, ..
-struct Ask {
-  int k0, fresh;
+// Inclusive sums over the block of two numbers; part: 32 of each.
+struct Pair {
+  int64_t a, b;
 };
-
-// Inclusive sum over the block; every thread gets its own.  `part`: 32 numbers of shared memory.
-__device__ __forceinline__ int64_t block_sum(int64_t x, int64_t* part) {
+__device__ __forceinline__ Pair block_sums(Pair x, Pair* part) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
+    const int64_t a = __shfl_up_sync(0xffffffffu, x.a, o), b = __shfl_up_sync(0xffffffffu, x.b, o);
+    if (lane >= o) x.a += a, x.b += b;
   }
-  __syncthreads();
   if (lane == 31) part[warp] = x;
   __syncthreads();
-  if (warp == 0) {
-    int64_t y = lane < PLAN_THREADS / 32 ? part[lane] : 0;
+  Pair y = part[lane];   // (of PLAN_THREADS / 32 = 32 warps)
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t z = __shfl_up_sync(0xffffffffu, y, o);
-      if (lane >= o) y += z;
-    }
-    part[lane] = y;
+  for (int o = 1; o < 32; o <<= 1) {
+    const int64_t a = __shfl_up_sync(0xffffffffu, y.a, o), b = __shfl_up_sync(0xffffffffu, y.b, o);
+    if (lane >= o) y.a += a, y.b += b;
   }
-  __syncthreads();
-  return warp ? x + part[warp - 1] : x;
+  const int before = max(warp - 1, 0);
+  const int64_t a = __shfl_sync(0xffffffffu, y.a, before), b = __shfl_sync(0xffffffffu, y.b, before);
+  if (warp) x.a += a, x.b += b;
+  return x;
 }
 
+constexpr int OWN = MAX_SEQS / PLAN_THREADS;   // sequences of a thread at most, one behind the other
+__device__ __forceinline__ int own_of(int n_seq) { return (n_seq + PLAN_THREADS - 1) / PLAN_THREADS; }
+
 struct Planner {
-  int64_t part[32];
-  int64_t before[MAX_SEQS + 1];   // fresh pages of the sequences before
-  int k0[MAX_SEQS];
-  alignas(16) int held[MAX_SEQS]; // extend: the shared page that the sequence's new positions begin on, -1; compact: pages kept
-  long long counted;              // free pages of this CTA's part
-  int fault;                      // of this CTA: site, 0 none
+  Pair part[32];
+  int64_t need, counted;   // fresh pages asked for; free pages of this CTA's part
+  int fault;               // of this CTA: site, 0 none
+  int before[MAX_SEQS];    // fresh pages of the sequences before (where the sum is no more than there are)
+  int k0[MAX_SEQS];        // the entry that a sequence's first one is for
+  alignas(16) int held[MAX_SEQS];   // extend: the shared page that the sequence's new positions begin on, -1
+  int given[MAX_SEQS];     // extend, in the cluster's first CTA: the page that takes its place
 };
 
-// One CTA of a cluster: sums of what the sequences ask for (thread t has those of sequences 4 t .. 4 t + 3 in ask), the
-// free pages counted, and if all is well each of them to whom it is due: give(b, k, page).  False: nothing was given.
+// A thread's run of refs: per pages from p0 on.
+__device__ __forceinline__ int free4(const int32_t* refs, int64_t p, int64_t end) {
+  if (p + 4 <= end) {
+    const int4 x = *reinterpret_cast<const int4*>(refs + p);
+    return (x.x == 0) | (x.y == 0) << 1 | (x.z == 0) << 2 | (x.w == 0) << 3;
+  }
+  int f = 0;
+  for (int i = 0; p + i < end; ++i) f |= (refs[p + i] == 0) << i;
+  return f;
+}
+struct Run {
+  int64_t p0, p1;
+  int64_t free;   // free pages in it
+};
+__device__ __forceinline__ Run count_free(const Pool& c, const int32_t* refs, int ctas, int rank) {
+  const int64_t threads = (int64_t)ctas * PLAN_THREADS, per = ((c.n_pages + threads - 1) / threads + 3) / 4 * 4;
+  Run r;
+  r.p0 = min(((int64_t)rank * PLAN_THREADS + threadIdx.x) * per, (int64_t)c.n_pages);
+  r.p1 = min(r.p0 + per, (int64_t)c.n_pages);
+  r.free = 0;
+#pragma unroll 4
+  for (int64_t p = r.p0; p < r.p1; p += 4) r.free += __popc(free4(refs, p, r.p1));
+  return r;
+}
+
+// All CTAs of a cluster: what the sequences ask for summed up (thread t has the k0 and number of fresh pages of its OWN
+// sequences), the free pages likewise, and if all is well each fresh page to whom it is due: give(b, k, page).
+// False: nothing was given.  Every read of what a plan goes by lies before the cluster's first barrier here.
 template <typename Give>
-__device__ __forceinline__ bool give_pages(const Pool& c, int32_t* refs, Planner& m, const Ask (&ask)[4], Give give) {
+__device__ __forceinline__ bool give_pages(const Pool& c, int32_t* refs, int n_seq, Planner& m, const Run& run, const int (&k0)[OWN],
+                                           const int (&fresh)[OWN], Give give) {
   cg::cluster_group cluster = cg::this_cluster();
-  const int rank = cluster.block_rank();
-  int64_t mine = 0;
+  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), own = own_of(n_seq);
+  int64_t asked = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) mine += ask[i].fresh;
-  const int64_t incl = block_sum(mine, m.part);
-  int64_t at = incl - mine;
+  for (int i = 0; i < OWN; ++i) asked += fresh[i];
+  const Pair sums = block_sums(Pair{asked, run.free}, m.part);
+  int64_t at = sums.a - asked;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int b = threadIdx.x * 4 + i;
-    m.before[b] = at;
-    m.k0[b] = ask[i].k0;
-    at += ask[i].fresh;
+  for (int i = 0; i < OWN; ++i) {
+    const int b = threadIdx.x * own + i;
+    if (i >= own || b >= n_seq) break;
+    m.before[b] = (int)min(at, (int64_t)0x7fffffff);
+    m.k0[b] = k0[i];
+    at += fresh[i];
   }
-  if (threadIdx.x == PLAN_THREADS - 1) m.before[MAX_SEQS] = incl;
-  // this CTA's part of refs
-  const int per = ((c.n_pages + PLANNERS - 1) / PLANNERS + 3) / 4 * 4;
-  const int64_t p0 = min((int64_t)rank * per, (int64_t)c.n_pages), p1 = min(p0 + per, (int64_t)c.n_pages);
-  // a thread looks at 4 pages a round, its neighbours at the next ones
-  auto free4 = [&](int64_t p) -> int {
-    if (p + 4 <= p1) {
-      const int4 x = *reinterpret_cast<const int4*>(refs + p);
-      return (x.x == 0) | (x.y == 0) << 1 | (x.z == 0) << 2 | (x.w == 0) << 3;
-    }
-    int f = 0;
-    for (int i = 0; p + i < p1; ++i) f |= (refs[p + i] == 0) << i;
-    return f;
-  };
-  int64_t free_pages = 0;
-  for (int64_t p = p0 + threadIdx.x * 4; p < p1; p += PLAN_THREADS * 4) free_pages += __popc(free4(p));
-  const int64_t upto = block_sum(free_pages, m.part);
-  if (threadIdx.x == PLAN_THREADS - 1) m.counted = upto;
-  cluster.sync();   // every CTA has read what the plan goes by, and counted
-  int64_t first = 0, total = 0;
+  if (threadIdx.x == PLAN_THREADS - 1) {
+    m.need = sums.a;
+    m.counted = sums.b;
+  }
+  int64_t first = sums.b - run.free, total = 0;
   int fault = 0;
-  for (int r = 0; r < PLANNERS; ++r) {
-    const Planner* o = cluster.map_shared_rank(&m, r);
-    if (r < rank) first += o->counted;
-    total += o->counted;
-    if (o->fault) fault = o->fault;
+  if (ctas == 1) {
+    __syncthreads();
+    total = m.counted;
+    fault = m.fault;
+  } else {
+    cluster.sync();
+    for (int r = 0; r < ctas; ++r) {
+      const Planner* o = cluster.map_shared_rank(&m, r);
+      const int64_t x = o->counted;
+      if (r < rank) first += x;
+      total += x;
+      if (o->fault) fault = o->fault;
+    }
+    cluster.sync();   // (nobody's shared memory is looked at any more)
   }
-  cluster.sync();   // (nobody's shared memory is looked at any more)
-  const int64_t need = m.before[MAX_SEQS];
+  const int64_t need = m.need;
   if (fault || need > total) {
     if (rank == 0 && threadIdx.x == 0) {
       if (fault) fail(c.status, DEV_INCONSISTENT, fault);
@@ -191,30 +212,27 @@ __device__ __forceinline__ bool give_pages(const Pool& c, int32_t* refs, Planner
     }
     return false;
   }
-  for (int64_t base = p0; base < p1 && first < need; base += PLAN_THREADS * 4) {
-    const int64_t p = base + threadIdx.x * 4;
-    const int f = p < p1 ? free4(p) : 0;
-    const int64_t incl4 = block_sum(__popc(f), m.part);
-    int64_t rank_of = first + incl4 - __popc(f);
-    first += m.part[31];
-    __syncthreads();
-#pragma unroll
+  if (run.free == 0) return true;
+  for (int64_t p = run.p0; p < run.p1 && first < need; p += 4) {
+    const int f = free4(refs, p, run.p1);
     for (int i = 0; i < 4; ++i) {
-      if (!((f >> i) & 1)) continue;
-      if (rank_of < need) {
-        int lo = 0, hi = MAX_SEQS;   // the last sequence with before <= rank_of that asks for any
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (m.before[mid] <= rank_of) lo = mid; else hi = mid;
-        }
-        refs[p + i] = 1;
-        give(lo, m.k0[lo] + (int)(rank_of - m.before[lo]), (int)(p + i));
+      if (!((f >> i) & 1) || first >= need) continue;
+      int lo = 0, hi = n_seq;   // the last sequence with before <= first: one that asks for some
+      while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (m.before[mid] <= first) lo = mid; else hi = mid;
       }
-      ++rank_of;
+      refs[p + i] = 1;
+      give(lo, m.k0[lo] + (int)(first - m.before[lo]), (int)(p + i));
+      ++first;
     }
   }
   return true;
 }
+
+// One CTA plans for small pools, a cluster for large ones (32,768 pages: 32 pages a thread).
+constexpr int ALONE_MOST = 32768;
+int planners(const Pool& c) { return c.n_pages <= ALONE_MOST ? 1 : PLANNERS; }
 
 // What the second kernel moves for a sequence.
 struct Move {
@@ -222,122 +240,139 @@ struct Move {
 };
 
 // ------------------------------------------------------------------ extend
-__global__ void __cluster_dims__(PLANNERS, 1, 1) __launch_bounds__(PLAN_THREADS)
-    extend_plan(Pool c, int32_t* refs, Table s, const int32_t* add, Move* moves) {
+__global__ void __launch_bounds__(PLAN_THREADS, 1) extend_plan(Pool c, int32_t* refs, Table s, const int32_t* add, Move* moves) {
   extern __shared__ __align__(16) uint8_t raw[];
   Planner& m = *reinterpret_cast<Planner*>(raw);
-  const int rank = cg::this_cluster().block_rank();
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), own = own_of(s.n);
   pdl_trigger();
+  const Run run = count_free(c, refs, ctas, rank);
   if (threadIdx.x == 0) m.fault = 0;
-  for (int b = threadIdx.x; b < MAX_SEQS; b += PLAN_THREADS) m.held[b] = -1;
+  for (int b = threadIdx.x; b < s.n + 3; b += PLAN_THREADS)
+    if (b < MAX_SEQS) m.held[b] = -1;
   __syncthreads();
   const int64_t cap = (int64_t)s.max_pages << c.page_log2;
-  Ask ask[4];
-  int len4[4], add4[4], page4[4], refs4[4];
+  int k0[OWN], fresh[OWN], len[OWN], more[OWN], page[OWN], count[OWN];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int b = threadIdx.x * 4 + i;
-    ask[i] = Ask{0, 0};
-    len4[i] = add4[i] = refs4[i] = 0;
-    page4[i] = -1;
-    if (b >= s.n) continue;
-    const int len = s.len[b], more = add[b];
-    if (len < 0 || len > cap || more < 0 || (int64_t)len + more > cap) {
+  for (int i = 0; i < OWN; ++i) {
+    const int b = threadIdx.x * own + i;
+    k0[i] = fresh[i] = len[i] = more[i] = count[i] = 0;
+    page[i] = -1;
+    if (i >= own || b >= s.n) continue;
+    len[i] = s.len[b];
+    more[i] = add[b];
+    if (len[i] < 0 || len[i] > cap || more[i] < 0 || (int64_t)len[i] + more[i] > cap) {
       m.fault = SITE_LEN;
-      continue;
+      more[i] = 0;
     }
-    if (more == 0) continue;
-    len4[i] = len;
-    add4[i] = more;
-    ask[i] = Ask{pages_of(c, len), pages_of(c, len + more) - pages_of(c, len)};
-    if (len & (c.page_len - 1)) {
-      const int page = s.table[(int64_t)b * s.max_pages + (len >> c.page_log2)];
-      if (!in_pool(c, page)) {
+    if (more[i] == 0) continue;
+    k0[i] = pages_of(c, len[i]);
+    fresh[i] = pages_of(c, len[i] + more[i]) - k0[i];
+    const int32_t* row = s.table + (int64_t)b * s.max_pages;
+    if (len[i] & (c.page_len - 1)) {
+      page[i] = row[k0[i] - 1];
+      if (!in_pool(c, page[i])) {
         m.fault = SITE_PAGE;
-        continue;
+        page[i] = -1;
       }
-      page4[i] = page;
-      refs4[i] = refs[page];
-      if (refs4[i] < 1) m.fault = SITE_REFS;
-      if (refs4[i] > 1) m.held[b] = page;
+    }
+    // the entries that pages are to go to hold none (the many of a long growth: below)
+    for (int k = 0; k < min(fresh[i], 4); ++k)
+      if (row[k0[i] + k] >= 0) m.fault = SITE_PAGE;
+  }
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) {
+    if (page[i] < 0) continue;
+    count[i] = refs[page[i]];
+    if (count[i] < 1) m.fault = SITE_REFS;
+    if (count[i] > 1) m.held[threadIdx.x * own + i] = page[i];
+  }
+  // (a warp looks through its lanes' long growths together)
+#pragma unroll
+  for (int i = 0; i < OWN; ++i) {
+    for (unsigned who = __ballot_sync(0xffffffffu, fresh[i] > 4); who; who &= who - 1) {
+      const int src = __ffs(who) - 1;
+      const int b = ((threadIdx.x & ~31) + src) * own + i, a = __shfl_sync(0xffffffffu, k0[i], src), n = __shfl_sync(0xffffffffu, fresh[i], src);
+      for (int k = a + 4 + (threadIdx.x & 31); k < a + n; k += 32)
+        if (s.table[(int64_t)b * s.max_pages + k] >= 0) m.fault = SITE_PAGE;
     }
   }
   __syncthreads();
   // A shared page: the last of its sequences keeps it, if nobody else holds it.
-  int moved4[4];
+  bool moved[OWN];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    moved4[i] = 0;
-    if (refs4[i] <= 1) continue;
-    const int b = threadIdx.x * 4 + i, page = page4[i];
+  for (int i = 0; i < OWN; ++i) {
+    moved[i] = false;
+    if (count[i] <= 1) continue;
+    const int b = threadIdx.x * own + i;
     int holders = 0, last = b;
     for (int k = 0; k < (s.n + 3) / 4; ++k) {
       const int4 x = reinterpret_cast<const int4*>(m.held)[k];
-      if (x.x == page) ++holders, last = max(last, 4 * k);
-      if (x.y == page) ++holders, last = max(last, 4 * k + 1);
-      if (x.z == page) ++holders, last = max(last, 4 * k + 2);
-      if (x.w == page) ++holders, last = max(last, 4 * k + 3);
+      if (x.x == page[i]) ++holders, last = max(last, 4 * k);
+      if (x.y == page[i]) ++holders, last = max(last, 4 * k + 1);
+      if (x.z == page[i]) ++holders, last = max(last, 4 * k + 2);
+      if (x.w == page[i]) ++holders, last = max(last, 4 * k + 3);
     }
-    if (holders > refs4[i]) m.fault = SITE_REFS;
-    if (holders == refs4[i] && last == b) continue;
-    moved4[i] = 1;
-    ask[i].k0 -= 1;
-    ask[i].fresh += 1;
-  }
-  // the entries that pages are to go to hold none (a warp a sequence, the cluster's CTAs taking turns)
-  for (int b = rank + PLANNERS * (threadIdx.x >> 5); b < s.n; b += PLANNERS * (PLAN_THREADS / 32)) {
-    const int len = s.len[b], more = add[b];
-    if (len < 0 || more <= 0 || (int64_t)len + more > cap) continue;
-    for (int k = pages_of(c, len) + (threadIdx.x & 31); k < pages_of(c, len + more); k += 32)
-      if (s.table[(int64_t)b * s.max_pages + k] >= 0) m.fault = SITE_PAGE;
+    if (holders > count[i]) m.fault = SITE_REFS;
+    if (holders == count[i] && last == b) continue;
+    moved[i] = true;
+    --k0[i];
+    ++fresh[i];
   }
   __syncthreads();
-  const bool ok = give_pages(c, refs, m, ask, [&](int b, int k, int page) { s.table[(int64_t)b * s.max_pages + k] = page; });
-  cg::this_cluster().sync();   // (the tables are written)
+  int* given = cluster.map_shared_rank(m.given, 0);
+  const bool ok = give_pages(c, refs, s.n, m, run, k0, fresh, [&](int b, int k, int p) {
+    s.table[(int64_t)b * s.max_pages + k] = p;
+    if (k == m.k0[b]) given[b] = p;
+  });
+  if (ctas == 1) __syncthreads();
+  else cluster.sync();   // (the first CTA has all pages given)
   if (rank) return;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int b = threadIdx.x * 4 + i;
-    if (b >= s.n) continue;
+  for (int i = 0; i < OWN; ++i) {
+    const int b = threadIdx.x * own + i;
+    if (i >= own || b >= s.n) break;
     Move v{0, 0, 0, 0};
-    if (ok && add4[i] > 0) {
-      s.len[b] = len4[i] + add4[i];
-      if (moved4[i]) {
-        v = Move{page4[i], s.table[(int64_t)b * s.max_pages + (len4[i] >> c.page_log2)], len4[i] & (c.page_len - 1), 0};
-        atomicSub(refs + page4[i], 1);
+    if (ok && more[i] > 0) {
+      s.len[b] = len[i] + more[i];
+      if (moved[i]) {
+        v = Move{page[i], m.given[b], len[i] & (c.page_len - 1), 0};
+        atomicSub(refs + page[i], 1);
       }
     }
-    moves[b] = v;
+    *reinterpret_cast<int4*>(moves + b) = make_int4(v.src, v.dst, v.rows, 0);
   }
 }
 
-// A sequence's shared page into its own: block (parts of a head's rows, head, sequence).
-__device__ __forceinline__ void copy_bytes(void* to, const void* from, int bytes, int t, int n) {
-  uint4* d = static_cast<uint4*>(to);
-  const uint4* s = static_cast<const uint4*>(from);
-  const int m = bytes / 16;
-  int i = t;
-  for (; i + 3 * n < m; i += 4 * n) {
-    const uint4 a = __ldcs(s + i), b = __ldcs(s + i + n), x = __ldcs(s + i + 2 * n), y = __ldcs(s + i + 3 * n);
-    d[i] = a;
-    d[i + n] = b;
-    d[i + 2 * n] = x;
-    d[i + 3 * n] = y;
-  }
-  for (; i < m; i += n) d[i] = __ldcs(s + i);
-}
-
+// A sequence's shared page into its own: block (head, sequence), keys and values side by side.
 __global__ void __launch_bounds__(COPY_THREADS) extend_copy(Pool c, const Move* moves, int n) {
   pdl_wait();
-  const int h = blockIdx.x;
-  const int row = c.d * (c.e4m3 ? 1 : 2);
+  const int h = blockIdx.x, row16 = c.d * (c.e4m3 ? 1 : 2) / 16;
   for (int b = blockIdx.y; b < n; b += gridDim.y) {
-    const Move v = moves[b];
-    if (v.rows == 0) continue;
-    const int64_t from = ((int64_t)v.src * c.H + h) << c.page_log2, to = ((int64_t)v.dst * c.H + h) << c.page_log2;
-    copy_bytes(static_cast<char*>(c.k) + to * row, static_cast<char*>(c.k) + from * row, v.rows * row, threadIdx.x, COPY_THREADS);
-    copy_bytes(static_cast<char*>(c.v) + to * row, static_cast<char*>(c.v) + from * row, v.rows * row, threadIdx.x, COPY_THREADS);
-    if (c.e4m3 && threadIdx.x < v.rows) {   // (at most 255 rows)
+    const int4 v = *reinterpret_cast<const int4*>(moves + b);
+    if (v.z == 0) continue;
+    const int64_t from = ((int64_t)v.x * c.H + h) << c.page_log2, to = ((int64_t)v.y * c.H + h) << c.page_log2;
+    const uint4* ks = static_cast<const uint4*>(c.k) + from * row16;
+    const uint4* vs = static_cast<const uint4*>(c.v) + from * row16;
+    uint4* kd = static_cast<uint4*>(c.k) + to * row16;
+    uint4* vd = static_cast<uint4*>(c.v) + to * row16;
+    const int m = v.z * row16;
+    for (int i = threadIdx.x; i < m; i += 4 * COPY_THREADS) {
+      uint4 x[4], y[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + k * COPY_THREADS < m) {
+          x[k] = __ldcs(ks + i + k * COPY_THREADS);
+          y[k] = __ldcs(vs + i + k * COPY_THREADS);
+        }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (i + k * COPY_THREADS < m) {
+          kd[i + k * COPY_THREADS] = x[k];
+          vd[i + k * COPY_THREADS] = y[k];
+        }
+    }
+    if (c.e4m3 && threadIdx.x < v.z) {   // (at most 255 rows)
       c.ks[to + threadIdx.x] = c.ks[from + threadIdx.x];
       c.vs[to + threadIdx.x] = c.vs[from + threadIdx.x];
     }
@@ -345,111 +380,126 @@ __global__ void __launch_bounds__(COPY_THREADS) extend_copy(Pool c, const Move* 
 }
 
 // ------------------------------------------------------------------ compact
-// same[b]: positions from the first on that stay where they are; -1: a fault.  A block a sequence.
-__global__ void __launch_bounds__(256) compact_look(Pool c, Table from, const int32_t* keep, int n_keep, const int32_t* keep_start,
-                                                    Table to, int32_t* same) {
+// Block (sequence, part): same[b * parts + part] := the first place of the part's (every parts-th group of
+// LOOK_THREADS places) whose position moves, or the number of places; minus a site: a fault.
+constexpr int LOOK_THREADS = 256, MAX_LOOKS = 32;
+__global__ void __launch_bounds__(LOOK_THREADS) compact_look(Pool c, const int32_t* refs, Table from, const int32_t* keep,
+                                                             int n_keep, const int32_t* keep_start, Table to, int32_t* same) {
   pdl_trigger();
-  const int b = blockIdx.x, len = from.len[b], a = keep_start[b], z = keep_start[b + 1];
-  __shared__ int stay, wrong;
-  if (threadIdx.x == 0) {
-    stay = z - a;
-    wrong = a < 0 || z < a || z > n_keep || z - a > ((int64_t)to.max_pages << c.page_log2) || (b == 0 && a != 0) ? SITE_ROWS :
-            len < 0 || len > ((int64_t)from.max_pages << c.page_log2) ? SITE_LEN : 0;
-  }
-  __syncthreads();
+  const int b = blockIdx.x, part = blockIdx.y, parts = gridDim.y;
+  const int len = from.len[b], a = keep_start[b], z = keep_start[b + 1], n = z - a;
+  const int32_t* row = from.table + (int64_t)b * from.max_pages;
+  int wrong = a < 0 || z < a || z > n_keep || n > ((int64_t)to.max_pages << c.page_log2) || (b == 0 && a != 0) ? SITE_ROWS :
+              len < 0 || len > ((int64_t)from.max_pages << c.page_log2) ? SITE_LEN : 0;
+  int mine = n;
   if (wrong == 0) {
-    int mine = z - a, bad = 0;
-    for (int i = threadIdx.x; i < z - a; i += 256) {
+#pragma unroll 4
+    for (int i = part * LOOK_THREADS + threadIdx.x; i < n; i += parts * LOOK_THREADS) {
       const int j = keep[a + i];
       if (j != i) mine = min(mine, i);
       if (j < 0 || j >= len) {
-        bad = SITE_LEN;
-      } else if (!in_pool(c, from.table[(int64_t)b * from.max_pages + (j >> c.page_log2)])) {
-        bad = SITE_PAGE;
+        wrong = SITE_LEN;
+      } else if (!in_pool(c, row[j >> c.page_log2])) {
+        wrong = SITE_PAGE;
       }
     }
-    if (mine < z - a) atomicMin(&stay, mine);
-    if (bad) wrong = bad;
-    // every page that is given up has to be one
-    for (int k = threadIdx.x; k < from.max_pages; k += 256)
-      if (from.table[(int64_t)b * from.max_pages + k] >= c.n_pages) wrong = SITE_PAGE;
+    // the pages that are given up are pages, and held
+#pragma unroll 4
+    for (int k = part * LOOK_THREADS + threadIdx.x; k < from.max_pages; k += parts * LOOK_THREADS) {
+      const int page = row[k];
+      if (page >= c.n_pages) wrong = SITE_PAGE;
+      else if (page >= 0 && refs[page] < 1) wrong = SITE_REFS;
+    }
+  }
+  __shared__ int best[LOOK_THREADS / 32], site[LOOK_THREADS / 32];
+  mine = __reduce_min_sync(0xffffffffu, mine);
+  wrong = __reduce_max_sync(0xffffffffu, wrong);
+  if (threadIdx.x % 32 == 0) {
+    best[threadIdx.x / 32] = mine;
+    site[threadIdx.x / 32] = wrong;
   }
   __syncthreads();
-  if (threadIdx.x == 0) same[b] = wrong ? -wrong : stay;
+  if (threadIdx.x == 0) {
+    for (int x = 1; x < LOOK_THREADS / 32; ++x) {
+      mine = min(mine, best[x]);
+      wrong = max(wrong, site[x]);
+    }
+    same[(int64_t)b * parts + part] = wrong ? -wrong : mine;
+  }
 }
 
-__global__ void __cluster_dims__(PLANNERS, 1, 1) __launch_bounds__(PLAN_THREADS)
-    compact_plan(Pool c, int32_t* refs, Table from, const int32_t* keep_start, Table to, int32_t* same) {
+// kept[b] := leading pages of sequence b that stay; kept[0] = -1: nothing is done.
+__global__ void __launch_bounds__(PLAN_THREADS, 1) compact_plan(Pool c, int32_t* refs, Table from, const int32_t* keep_start, Table to,
+                                                                const int32_t* same, int parts, int32_t* kept) {
   extern __shared__ __align__(16) uint8_t raw[];
   Planner& m = *reinterpret_cast<Planner*>(raw);
-  const int rank = cg::this_cluster().block_rank();
-  pdl_wait();
-  pdl_trigger();
+  cg::cluster_group cluster = cg::this_cluster();
+  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), own = own_of(from.n);
+  const Run run = count_free(c, refs, ctas, rank);   // (the kernel before this one does not change them)
   if (threadIdx.x == 0) m.fault = 0;
   __syncthreads();
-  Ask ask[4];
+  pdl_wait();
+  pdl_trigger();
+  int k0[OWN], fresh[OWN];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int b = threadIdx.x * 4 + i;
-    ask[i] = Ask{0, 0};
-    m.held[b] = 0;
-    if (b >= from.n) continue;
-    const int stay = same[b];
+  for (int i = 0; i < OWN; ++i) {
+    const int b = threadIdx.x * own + i;
+    k0[i] = fresh[i] = 0;
+    if (i >= own || b >= from.n) continue;
+    const int n = keep_start[b + 1] - keep_start[b], all = pages_of(c, n);
+    int stay = 0x7fffffff;
+#pragma unroll 8
+    for (int x = 0; x < parts; ++x) stay = min(stay, same[(int64_t)b * parts + x]);
     if (stay < 0) {
       m.fault = -stay;
       continue;
     }
-    const int n = keep_start[b + 1] - keep_start[b], all = pages_of(c, n);
-    const int kept = stay == n ? all : stay >> c.page_log2;   // pages that stay
-    ask[i] = Ask{kept, all - kept};
-    m.held[b] = kept;
+    k0[i] = stay == n ? all : stay >> c.page_log2;
+    fresh[i] = all - k0[i];
   }
   __syncthreads();
-  // refs of pages held: none free (a warp a sequence)
-  for (int b = rank + PLANNERS * (threadIdx.x >> 5); b < from.n; b += PLANNERS * (PLAN_THREADS / 32))
-    for (int k = threadIdx.x & 31; k < from.max_pages; k += 32) {
-      const int page = from.table[(int64_t)b * from.max_pages + k];
-      if (in_pool(c, page) && refs[page] < 1) m.fault = SITE_REFS;
+  const bool ok = give_pages(c, refs, from.n, m, run, k0, fresh,
+                             [&](int b, int k, int p) { to.table[(int64_t)b * to.max_pages + k] = p; });
+  if (rank == 0) {
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+      const int b = threadIdx.x * own + i;
+      if (i < own && b < from.n) kept[b] = ok ? k0[i] : -1;
     }
-  __syncthreads();
-  const bool ok = give_pages(c, refs, m, ask, [&](int b, int k, int page) { to.table[(int64_t)b * to.max_pages + k] = page; });
-  if (!ok) {
-    if (rank == 0)
-      for (int b = threadIdx.x; b < from.n; b += PLAN_THREADS) same[b] = -1;   // nothing to move
-    return;
-  }
-  cg::this_cluster().sync();   // (nobody counts free pages any more)
-  for (int b = rank + PLANNERS * (threadIdx.x >> 5); b < from.n; b += PLANNERS * (PLAN_THREADS / 32)) {
-    const int kept = m.held[b], n = keep_start[b + 1] - keep_start[b], all = pages_of(c, n);
-    for (int k = threadIdx.x & 31; k < max(from.max_pages, to.max_pages); k += 32) {
-      const int page = k < from.max_pages ? from.table[(int64_t)b * from.max_pages + k] : -1;
-      if (k < kept) to.table[(int64_t)b * to.max_pages + k] = page;
-      else if (page >= 0) atomicSub(refs + page, 1);
-      if (k >= all && k < to.max_pages) to.table[(int64_t)b * to.max_pages + k] = -1;
-    }
-    if ((threadIdx.x & 31) == 0) to.len[b] = n;
   }
 }
 
-// Rows [blockIdx.x * ROWS, ..) of keep, head blockIdx.y.
+// Block x: rows [x % groups * MOVE_ROWS, ..) of keep, head x / groups; behind those, one block a sequence, the tables and counts (the
+// pages that stay, the entries behind the last page, what is given up).
 constexpr int MOVE_ROWS = 64;
-__global__ void __launch_bounds__(COPY_THREADS) compact_copy(Pool c, Table from, const int32_t* keep, int n_keep,
-                                                             const int32_t* keep_start, Table to, const int32_t* same) {
+__global__ void __launch_bounds__(COPY_THREADS) compact_copy(Pool c, int32_t* refs, Table from, const int32_t* keep, int n_keep,
+                                                             const int32_t* keep_start, Table to, const int32_t* kept, int groups) {
   pdl_wait();
+  if (kept[0] == -1) return;
+  if ((int)blockIdx.x >= groups * c.H) {
+    const int b = blockIdx.x - groups * c.H, stay = kept[b], n = keep_start[b + 1] - keep_start[b], all = pages_of(c, n);
+    for (int k = threadIdx.x; k < max(from.max_pages, to.max_pages); k += COPY_THREADS) {
+      const int page = k < from.max_pages ? from.table[(int64_t)b * from.max_pages + k] : -1;
+      if (k < stay) to.table[(int64_t)b * to.max_pages + k] = page;
+      else if (page >= 0) atomicSub(refs + page, 1);
+      if (k >= all && k < to.max_pages) to.table[(int64_t)b * to.max_pages + k] = -1;
+    }
+    if (threadIdx.x == 0) to.len[b] = n;
+    return;
+  }
   __shared__ int64_t src[MOVE_ROWS], dst[MOVE_ROWS];   // rows of the pool for head 0, -1: stays
-  const int i0 = blockIdx.x * MOVE_ROWS;
+  const int h = blockIdx.x / groups, i0 = (blockIdx.x - h * groups) * MOVE_ROWS;
   if (threadIdx.x < MOVE_ROWS) {
     const int i = i0 + threadIdx.x;
     int64_t a = -1, z = -1;
-    if (same[0] != -1 && i < n_keep && i < keep_start[from.n] && i >= keep_start[0]) {
+    if (i < n_keep && i < keep_start[from.n]) {
       int lo = 0, hi = from.n;
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (keep_start[mid] <= i) lo = mid; else hi = mid;
       }
-      const int pos = i - keep_start[lo], n = keep_start[lo + 1] - keep_start[lo], stay = same[lo];
-      const int kept = stay == n ? pages_of(c, n) : stay >> c.page_log2;
-      if ((pos >> c.page_log2) >= kept) {
+      const int pos = i - keep_start[lo];
+      if ((pos >> c.page_log2) >= kept[lo]) {
         const int j = keep[i];
         a = (((int64_t)from.table[(int64_t)lo * from.max_pages + (j >> c.page_log2)] * c.H) << c.page_log2) + (j & (c.page_len - 1));
         z = (((int64_t)to.table[(int64_t)lo * to.max_pages + (pos >> c.page_log2)] * c.H) << c.page_log2) + (pos & (c.page_len - 1));
@@ -460,7 +510,7 @@ __global__ void __launch_bounds__(COPY_THREADS) compact_copy(Pool c, Table from,
   }
   __syncthreads();
   const int row16 = c.d * (c.e4m3 ? 1 : 2) / 16;   // 4, 8 or 16 threads a row
-  const int64_t head = (int64_t)blockIdx.y << c.page_log2;
+  const int64_t head = (int64_t)h << c.page_log2;
   const int t = threadIdx.x % row16, per = COPY_THREADS / row16;
   const uint4* k = static_cast<const uint4*>(c.k);
   const uint4* v = static_cast<const uint4*>(c.v);
@@ -489,7 +539,7 @@ cudaError_t pages_set_smem_limits() {
 }
 
 size_t extend_scratch(int n_seq) { return sizeof(Move) * (size_t)n_seq; }
-size_t compact_scratch(int n_seq) { return sizeof(int32_t) * (size_t)n_seq; }
+size_t compact_scratch(int n_seq) { return sizeof(int32_t) * (size_t)n_seq * (MAX_LOOKS + 1); }
 
 cudaError_t launch_fork(const Pool& c, int32_t* refs, const Table& from, const int32_t* parent, const Table& to, cudaStream_t st) {
   return launch_kernel(cache_fork, dim3(from.n + to.n), 256, 0, 1, false, st, c, refs, from, parent, to);
@@ -501,20 +551,30 @@ cudaError_t launch_release(const Pool& c, int32_t* refs, const Table& s, const i
 
 cudaError_t launch_extend(const Pool& c, int32_t* refs, const Table& s, const int32_t* add, void* scratch, cudaStream_t st) {
   Move* moves = static_cast<Move*>(scratch);
-  const cudaError_t e = launch_kernel(extend_plan, dim3(PLANNERS), PLAN_THREADS, sizeof(Planner), 1, false, st, c, refs, s, add, moves);
+  const int P = planners(c);
+  const cudaError_t e = launch_kernel(extend_plan, dim3(P), PLAN_THREADS, sizeof(Planner), P, false, st, c, refs, s, add, moves);
   if (e != cudaSuccess) return e;
   return launch_kernel(extend_copy, dim3(c.H, std::min(s.n, 1024)), COPY_THREADS, 0, 1, true, st, c, moves, s.n);
 }
 
 cudaError_t launch_compact(const Pool& c, int32_t* refs, const Table& from, const int32_t* keep, int n_keep,
                            const int32_t* keep_start, const Table& to, void* scratch, cudaStream_t st) {
-  int32_t* same = static_cast<int32_t*>(scratch);
-  cudaError_t e = launch_kernel(compact_look, dim3(from.n), 256, 0, 1, false, st, c, from, keep, n_keep, keep_start, to, same);
+  const int n_sm = sm_count(), P = planners(c);
+  if (n_sm <= 0) return cudaErrorInvalidDevice;
+  int32_t* const kept = static_cast<int32_t*>(scratch);
+  int32_t* const same = kept + from.n;
+  // parts of a sequence: four blocks an SM in all, and no more than the work is good for
+  const int most = std::max(n_keep, from.max_pages) / (4 * LOOK_THREADS) + 1;
+  const int parts = std::max(1, std::min({MAX_LOOKS, 4 * n_sm / from.n, most}));
+  const int groups = (n_keep + MOVE_ROWS - 1) / MOVE_ROWS;
+  if ((int64_t)groups * c.H + from.n > 0x7fffffff) return cudaErrorInvalidValue;   // (more than any memory holds)
+  cudaError_t e = launch_kernel(compact_look, dim3(from.n, parts), LOOK_THREADS, 0, 1, false, st, c, refs, from, keep, n_keep,
+                                keep_start, to, same);
   if (e == cudaSuccess)
-    e = launch_kernel(compact_plan, dim3(PLANNERS), PLAN_THREADS, sizeof(Planner), 1, true, st, c, refs, from, keep_start, to, same);
-  if (e == cudaSuccess && n_keep > 0)
-    e = launch_kernel(compact_copy, dim3((n_keep + MOVE_ROWS - 1) / MOVE_ROWS, c.H), COPY_THREADS, 0, 1, true, st, c, from, keep,
-                      n_keep, keep_start, to, same);
+    e = launch_kernel(compact_plan, dim3(P), PLAN_THREADS, sizeof(Planner), P, true, st, c, refs, from, keep_start, to, same, parts, kept);
+  if (e == cudaSuccess)
+    e = launch_kernel(compact_copy, dim3(groups * c.H + from.n), COPY_THREADS, 0, 1, true, st, c, refs, from, keep, n_keep,
+                      keep_start, to, kept, groups);
   return e;
 }
 

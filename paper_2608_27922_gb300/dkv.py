@@ -893,7 +893,7 @@ class PagedCache:
         """Room for add[b] (int32) more positions of every sequence: pages, lengths, and a copy of a shared last page."""
         _check_i32(add, (seqs.n_seq,), "add", self.device)
         s, ctx = self._on(stream)
-        scratch = self._new(ctx, 16 * seqs.n_seq, torch.uint8)
+        scratch = self._new(ctx, int(lib().dkv_cache_extend_scratch_size(self.handle, seqs.n_seq)), torch.uint8)
         st = self._extend(self.handle, self._refs(refs), self._table(seqs), add.data_ptr(), scratch.data_ptr(), scratch.numel(), s)
         if st != DKV_OK:
             _check(st, "dkv_cache_extend")
@@ -913,7 +913,7 @@ class PagedCache:
         _check_i32(keep, (keep.numel(),), "keep", self.device)
         _check_i32(keep_start, (src.n_seq + 1,), "keep_start", self.device)
         s, ctx = self._on(stream)
-        scratch = self._new(ctx, 4 * src.n_seq, torch.uint8)
+        scratch = self._new(ctx, int(lib().dkv_cache_compact_scratch_size(self.handle, src.n_seq)), torch.uint8)
         st = self._compact(self.handle, self._refs(refs), self._table(src), keep.data_ptr(), keep.numel(), keep_start.data_ptr(),
                            self._table(dst), scratch.data_ptr(), scratch.numel(), s)
         if st != DKV_OK:
