@@ -4,7 +4,9 @@
 // score of a query row and a page is a product of whole numbers (magnitudes up to 127, sums of d of them below 2^21) times
 // a power of two: fp16 holds the numbers, the tensor cores' fp32 sums of them are exact in whatever order, and so
 // the choice does not depend on how the work is split.
+#include "attn_math.cuh"
 #include "cache_internal.h"
+#include "tc_ptx.cuh"
 
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -162,21 +164,37 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-template <int D>
+// A CTA's pages in shared memory.  `cap` pages are looked at in one go, behind what has been kept so far.
 struct Work {
-  static constexpr int STRIDE = D + 4;   // halves of a row: 8-byte reads of 4 lanes x 4 rows touch every bank once
-  __half q[64][STRIDE];
-  float unit[64];            // 2^e of a row, 0: none
-  alignas(16) uint32_t key[PLACES];      // what has been kept so far, then this part's pages (first their best scores)
-  int page[PLACES];          //   ascending
-  int at[CAP];               // of this part's pages: place in the pool
-  float scale[CAP];          //   and 2^e of the summary, 0: not to be listed
-  uint32_t kept_key[MAX_TOP];
-  int kept_page[MAX_TOP];
-  uint32_t lo[8], hi[8];
-  int total[8];
-  int kept, below;
+  uint32_t* key;      // [places] what has been kept, then this part's pages (first their best scores)
+  int* page;          // [places]   ascending
+  int* at;            // [cap] of this part's pages: place in the pool, -1
+  float* scale;       // [cap]   and 2^e of the summary, 0: not to be listed
+  float* other;       // [cap]   and the best scores of the second half of the rows (tensor cores)
+  uint32_t* kept_key;   // [top]
+  int* kept_page;
+  struct Sums {
+    uint32_t lo[8], hi[8];
+    int total[8];
+    int kept;
+  }* sums;
 };
+struct Sizes {
+  int cap, places, top;   // each a multiple of 4
+};
+__host__ __device__ inline size_t work_bytes(const Sizes& z) { return 8 * (size_t)z.places + 12 * (size_t)z.cap + 8 * (size_t)z.top + 128; }
+__device__ __forceinline__ Work work_in(uint8_t* p, const Sizes& z) {
+  Work w;
+  w.sums = reinterpret_cast<Work::Sums*>(p);
+  w.key = reinterpret_cast<uint32_t*>(p + 128);
+  w.page = reinterpret_cast<int*>(w.key + z.places);
+  w.at = w.page + z.places;
+  w.scale = reinterpret_cast<float*>(w.at + z.cap);
+  w.other = w.scale + z.cap;
+  w.kept_key = reinterpret_cast<uint32_t*>(w.other + z.cap);
+  w.kept_page = reinterpret_cast<int*>(w.kept_key + z.top);
+  return w;
+}
 
 __device__ __forceinline__ void mma_f16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -197,8 +215,8 @@ __device__ __forceinline__ void widen4(uint32_t w, uint32_t& a, uint32_t& b) {
 // The `top` largest of key[0 .. n), equal ones: the first, in their order, into kept_key and kept_page.  Thread t holds
 // places t PER ..; halving the range of the keys with counts over the block finds a bound with `top` keys above
 // it, or the top-th key itself where others equal it.
-template <int PER, typename W>
-__device__ __forceinline__ void keep_best(W& w, int n, int top) {
+template <int PER>
+__device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint32_t k[PER], least = 0xffffffffu, most = 0;
   int valid = 0;
@@ -215,17 +233,17 @@ __device__ __forceinline__ void keep_best(W& w, int n, int top) {
   most = __reduce_max_sync(0xffffffffu, most);
   valid = __reduce_add_sync(0xffffffffu, valid);
   if (lane == 0) {
-    w.lo[warp] = least;
-    w.hi[warp] = most;
-    w.total[warp] = valid;
+    w.sums->lo[warp] = least;
+    w.sums->hi[warp] = most;
+    w.sums->total[warp] = valid;
   }
   __syncthreads();
   valid = 0;
 #pragma unroll
   for (int x = 0; x < CH_THREADS / 32; ++x) {
-    least = min(least, w.lo[x]);
-    most = max(most, w.hi[x]);
-    valid += w.total[x];
+    least = min(least, w.sums->lo[x]);
+    most = max(most, w.sums->hi[x]);
+    valid += w.sums->total[x];
   }
   // keys > T are kept, and `need` of those equal to T
   uint32_t T = 0;
@@ -242,11 +260,11 @@ __device__ __forceinline__ void keep_best(W& w, int n, int top) {
       for (int i = 0; i < PER; ++i) c += k[i] >= mid;
       c = __reduce_add_sync(0xffffffffu, c);
       __syncthreads();
-      if (lane == 0) w.total[warp] = c;
+      if (lane == 0) w.sums->total[warp] = c;
       __syncthreads();
       c = 0;
 #pragma unroll
-      for (int x = 0; x < CH_THREADS / 32; ++x) c += w.total[x];
+      for (int x = 0; x < CH_THREADS / 32; ++x) c += w.sums->total[x];
       if (c > top) {
         lo = mid;
       } else {
@@ -272,13 +290,13 @@ __device__ __forceinline__ void keep_best(W& w, int n, int top) {
     if (lane >= o) incl += y;
   }
   __syncthreads();
-  if (lane == 31) w.total[warp] = incl;
+  if (lane == 31) w.sums->total[warp] = incl;
   __syncthreads();
   int before = incl - mine, all = 0;
 #pragma unroll
   for (int x = 0; x < CH_THREADS / 32; ++x) {
-    if (x < warp) before += w.total[x];
-    all += w.total[x];
+    if (x < warp) before += w.sums->total[x];
+    all += w.sums->total[x];
   }
   int eq_before = before >> 16, gt_before = before & 0xffff;
 #pragma unroll
@@ -292,204 +310,449 @@ __device__ __forceinline__ void keep_best(W& w, int n, int top) {
     eq_before += same;
     gt_before += k[i] > T;
   }
-  if (tid == 0) w.kept = (all & 0xffff) + min(all >> 16, need);
+  if (tid == 0) w.sums->kept = (all & 0xffff) + min(all >> 16, need);
   __syncthreads();
 }
-template <typename W>
-__device__ __forceinline__ void keep_best(W& w, int n, int top) {
+__device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
   if (n <= 4 * CH_THREADS) keep_best<4>(w, n, top);
   else keep_best<PLACES / CH_THREADS>(w, n, top);
 }
 
-// Cluster: one list (slot blockIdx.x / CTAs of the cluster, head blockIdx.y); its CTAs share the seen pages.
-template <int D>
-__global__ void __launch_bounds__(CH_THREADS) choose(Pool c, Seqs s, const int8_t* code, const uint8_t* scale, Packed qp, int G,
-                                                     Choose how, int32_t* lists) {
-  extern __shared__ __align__(16) uint8_t raw[];
-  Work<D>& w = *reinterpret_cast<Work<D>*>(raw);
-  cg::cluster_group cluster = cg::this_cluster();
-  const int C = cluster.num_blocks(), rank = cluster.block_rank();
-  const int slot = blockIdx.x / C, h = blockIdx.y, slots = gridDim.x / C;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  if (blockIdx.x == 0 && h == 0)
-    for (int b = tid; b < s.n; b += CH_THREADS) seq_at(c, s, b);
-  const int b = seq_of_slot_warp(s, how.tile, slot);
-  const Seq q = seq_at(c, s, b);
-  const int i0 = (slot - first_slot(s, how.tile, b)) * how.tile;
-  int32_t* line = lists + ((int64_t)h * slots + slot) * how.width;
-  const int m = min(how.tile, q.n - i0), p1 = q.len - q.n + i0 + m - 1;
-  if (i0 < 0 || m <= 0 || p1 < 0) {   // no tile, or one that sees nothing (the whole cluster)
-    if (rank == 0)
-      for (int k = tid; k < how.width; k += CH_THREADS) line[k] = -1;
-    return;
-  }
-  const int p0 = max(p1 - m + 1, 0);
+// One list: its tile of tokens and the pages that are listed anyway.
+struct Line {
+  int b, i0, m;       // sequence, first token, tokens
+  Seq q;
+  int whole;          // seen pages
+  int lo, own;        // local pages
+  int sinks;
+  bool any;           // false: no tile, or one that sees nothing
+};
+__device__ __forceinline__ Line line_of(const Pool& c, const Seqs& s, const Choose& how, int slot) {
+  Line l{};
+  l.b = seq_of_slot_warp(s, how.tile, slot);
+  l.q = seq_at(c, s, l.b);
+  l.i0 = (slot - first_slot(s, how.tile, l.b)) * how.tile;
+  l.m = min(how.tile, l.q.n - l.i0);
+  const int p1 = l.q.len - l.q.n + l.i0 + l.m - 1, p0 = max(p1 - l.m + 1, 0);
+  l.any = l.i0 >= 0 && l.m > 0 && p1 >= 0;
+  if (!l.any) return l;
   const Mask mask{0.f, 0, 0, how.block, how.inverse};
-  const int end = visible_end(mask, p0, q.len);
-  const int whole = end == q.len ? (q.len + c.page_len - 1) >> c.page_log2 : end >> c.page_log2;
-  const int own = p1 >> c.page_log2, lo = max(0, (p0 >> c.page_log2) - (how.local - 1)), sinks = min(how.sinks, whole);
-  const int R = m * G;
-  // this CTA's share of the seen pages
-  const int per = (whole + C - 1) / C, a = min(rank * per, whole), z = min(a + per, whole);
-  int kept = 0;
-  if (how.top > 0) {
-#pragma unroll 1
-    for (int k0 = a; k0 < z; k0 += CAP) {
-      const int n = min(CAP, z - k0);
-      float* score = reinterpret_cast<float*>(w.key + kept);
-      for (int i = tid; i < n; i += CH_THREADS) {
-        const int k = k0 + i;
-        const int64_t row = pool_row(c, s, b, h, k << c.page_log2);
-        const int64_t at = row >> c.page_log2;   // page * H + h
-        const uint32_t byte = row >= 0 ? scale[at] : 255u;
-        const bool listed = k < sinks || (k >= lo && k <= own);
-        w.at[i] = row >= 0 ? (int)(at / c.H) : -1;
-        w.scale[i] = listed || byte == 255u ? 0.f : scale_of(byte);
-        w.page[kept + i] = k;
-        score[i] = -INFINITY;
-      }
-      for (int i = tid; i < kept; i += CH_THREADS) {
-        w.key[i] = w.kept_key[i];
-        w.page[i] = w.kept_page[i];
-      }
-#pragma unroll 1
-      for (int r0 = 0; r0 < R; r0 += 64) {
-        const int rows = min(64, R - r0), used = (rows + 15) & ~15;
-        __syncthreads();   // (the last rows have been used)
-#pragma unroll 4
-        for (int r = warp; r < used; r += CH_THREADS / 32) {   // codes of the rows
-          float x[D / 32];
-          if (r < rows) {
-            const int i = (r0 + r) / G, hq = h * G + (r0 + r) - i * G;
-            const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(qp.p) + hq * qp.head + (int64_t)(q.r0 + i0 + i) * qp.row + lane * (D / 32);
-            if (D == 128) {
-              const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-              x[0] = __uint_as_float(v.x << 16);
-              x[1] = __uint_as_float(v.x & 0xffff0000u);
-              x[D / 32 - 2] = __uint_as_float(v.y << 16);
-              x[D / 32 - 1] = __uint_as_float(v.y & 0xffff0000u);
-            } else {
-              const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(p));
-              x[0] = __uint_as_float(v << 16);
-              x[1] = __uint_as_float(v & 0xffff0000u);
-            }
-          } else {
-#pragma unroll
-            for (int k = 0; k < D / 32; ++k) x[k] = __int_as_float(0x7fffffff);
-          }
-          uint32_t top = 0;   // (bits of magnitudes order like the magnitudes, NaN above infinity)
-#pragma unroll
-          for (int k = 0; k < D / 32; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-          top = __reduce_max_sync(0xffffffffu, top);
-          const bool fine = top < __float_as_uint(WILD);
-          const int e = fine ? exponent_of(__uint_as_float(top)) : 0;
-          const float f = fine ? pow2(-e) : 0.f;
-#pragma unroll
-          for (int k = 0; k < D / 32; ++k) w.q[r][lane * (D / 32) + k] = __float2half_rn(fine ? rintf(x[k] * f) : 0.f);
-          if (lane == 0) w.unit[r] = fine ? pow2(e) : 0.f;
-        }
-        __syncthreads();
-        // eight pages a warp: page j + g's codes, 16 bytes at 16 t (and at 64 + 16 t), the next eight's on their way
-        auto codes = [&](int j, uint4 (&v)[D / 64]) {
-          const int at = j + g < n ? w.at[j + g] : -1;
-#pragma unroll
-          for (int x = 0; x < D / 64; ++x)
-            v[x] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(code + ((int64_t)at * c.H + h) * D + x * 64) + t) : make_uint4(0, 0, 0, 0);
-        };
-        uint4 v[D / 64];
-        codes(warp * 8, v);
-#pragma unroll 1
-        for (int j0 = warp * 8; j0 < n; j0 += CH_THREADS / 32 * 8) {
-          uint32_t B[D / 8];
-#pragma unroll
-          for (int x = 0; x < D / 64; ++x) {
-            widen4(v[x].x, B[8 * x], B[8 * x + 1]);
-            widen4(v[x].y, B[8 * x + 2], B[8 * x + 3]);
-            widen4(v[x].z, B[8 * x + 4], B[8 * x + 5]);
-            widen4(v[x].w, B[8 * x + 6], B[8 * x + 7]);
-          }
-          codes(j0 + CH_THREADS / 32 * 8, v);
-          float best[2] = {-INFINITY, -INFINITY};
-#pragma unroll 1
-          for (int mt = 0; mt < used; mt += 16) {
-            float acc[4] = {0.f, 0.f, 0.f, 0.f}, ac2[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) {
-              const int col = (i >> 2) * 64 + t * 16 + (i & 3) * 4;
-              const uint2 x = *reinterpret_cast<const uint2*>(&w.q[mt + g][col]);
-              const uint2 y = *reinterpret_cast<const uint2*>(&w.q[mt + g + 8][col]);
-              const uint32_t A[4] = {x.x, y.x, x.y, y.y};
-              mma_f16(i & 1 ? ac2 : acc, A, B[2 * i], B[2 * i + 1]);
-            }
-            const float u0 = w.unit[mt + g], u1 = w.unit[mt + g + 8];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              if (u0 != 0.f) best[x] = fmaxf(best[x], (acc[x] + ac2[x]) * u0);
-              if (u1 != 0.f) best[x] = fmaxf(best[x], (acc[2 + x] + ac2[2 + x]) * u1);
-            }
-          }
-#pragma unroll
-          for (int o = 4; o < 32; o <<= 1) {
-            best[0] = fmaxf(best[0], __shfl_xor_sync(0xffffffffu, best[0], o));
-            best[1] = fmaxf(best[1], __shfl_xor_sync(0xffffffffu, best[1], o));
-          }
-          if (g < 2) {   // page 2 t + g of the eight
-            const int x = j0 + 2 * t + g;
-            if (x < n) {
-              const float y = fmaxf(score[x], best[g]);
-              if (r0 + 64 < R) score[x] = y;
-              else w.key[kept + x] = w.scale[x] != 0.f && y > -INFINITY ? key_of(y * w.scale[x]) : 0;   // the last rows
-            }
-          }
-        }
-      }
-      __syncthreads();
-      keep_best(w, kept + n, how.top);
-      kept = w.kept;
-    }
+  const int end = visible_end(mask, p0, l.q.len);
+  l.whole = end == l.q.len ? (l.q.len + c.page_len - 1) >> c.page_log2 : end >> c.page_log2;
+  l.own = p1 >> c.page_log2;
+  l.lo = max(0, (p0 >> c.page_log2) - (how.local - 1));
+  l.sinks = min(how.sinks, l.whole);
+  return l;
+}
+
+// Pages k0 .. k0 + n - 1 looked up, behind the `kept` ones.
+__device__ __forceinline__ void look_up(const Pool& c, const Seqs& s, const Work& w, const Line& l, const uint8_t* scale, int h,
+                                        int k0, int n, int kept) {
+  for (int i = threadIdx.x; i < n; i += CH_THREADS) {
+    const int k = k0 + i;
+    const int64_t row = pool_row(c, s, l.b, h, k << c.page_log2), at = row >> c.page_log2;   // page * H + h
+    const uint32_t byte = row >= 0 ? scale[at] : 255u;
+    const bool listed = k < l.sinks || (k >= l.lo && k <= l.own);
+    w.at[i] = row >= 0 ? (int)(at / c.H) : -1;
+    w.scale[i] = listed || byte == 255u ? 0.f : scale_of(byte);
+    w.other[i] = -INFINITY;
+    w.page[kept + i] = k;
+    reinterpret_cast<float*>(w.key)[kept + i] = -INFINITY;
   }
+  for (int i = threadIdx.x; i < kept; i += CH_THREADS) {
+    w.key[i] = w.kept_key[i];
+    w.page[i] = w.kept_page[i];
+  }
+}
+
+// A warp's query row r of the tile (row = token * G + head): lane's D / 32 numbers as whole ones, its exponent's power of
+// two (0: no codes).
+template <int D>
+__device__ __forceinline__ float row_codes(const Packed& qp, const Line& l, int G, int h, int r, int R, float (&x)[D / 32]) {
+  const int lane = threadIdx.x & 31;
+  uint32_t top = 0x7f800000u;   // (a row behind the last has none)
+  if (r < R) {
+    const int i = r / G, hq = h * G + r - i * G;
+    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(qp.p) + hq * qp.head + (int64_t)(l.q.r0 + l.i0 + i) * qp.row + lane * (D / 32);
+    if (D == 128) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+      x[0] = __uint_as_float(v.x << 16);
+      x[1] = __uint_as_float(v.x & 0xffff0000u);
+      x[D / 32 - 2] = __uint_as_float(v.y << 16);
+      x[D / 32 - 1] = __uint_as_float(v.y & 0xffff0000u);
+    } else {
+      const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(p));
+      x[0] = __uint_as_float(v << 16);
+      x[1] = __uint_as_float(v & 0xffff0000u);
+    }
+    top = 0;   // (bits of magnitudes order like the magnitudes, NaN above infinity)
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
+  } else {
+#pragma unroll
+    for (int k = 0; k < D / 32; ++k) x[k] = 0.f;
+  }
+  top = __reduce_max_sync(0xffffffffu, top);
+  const bool fine = top < __float_as_uint(WILD);
+  const int e = fine ? exponent_of(__uint_as_float(top)) : 0;
+  const float f = fine ? pow2(-e) : 0.f;
+#pragma unroll
+  for (int k = 0; k < D / 32; ++k) x[k] = fine ? rintf(x[k] * f) : 0.f;
+  return fine ? pow2(e) : 0.f;
+}
+
+// The cluster's shares joined, and the list written: sinks, then the chosen pages and the local ones as they ascend.
+__device__ __forceinline__ void finish(const Work& w, const Line& l, int kept, int top, int32_t* line, int width) {
+  cg::cluster_group cluster = cg::this_cluster();
+  const int C = cluster.num_blocks(), rank = cluster.block_rank(), tid = threadIdx.x;
   if (C > 1) {
-    if (tid == 0) w.kept = kept;
+    if (tid == 0) w.sums->kept = kept;
     cluster.sync();
     if (rank == 0) {   // the shares' best, in their order, and the best of those
       int n = 0;
       for (int r = 0; r < C; ++r) {
-        Work<D>* o = cluster.map_shared_rank(&w, r);
-        const int m2 = o->kept;
+        const uint32_t* key = cluster.map_shared_rank(w.kept_key, r);
+        const int* page = cluster.map_shared_rank(w.kept_page, r);
+        const int m2 = cluster.map_shared_rank(w.sums, r)->kept;
         for (int i = tid; i < m2; i += CH_THREADS) {
-          w.key[n + i] = o->kept_key[i];
-          w.page[n + i] = o->kept_page[i];
+          w.key[n + i] = key[i];
+          w.page[n + i] = page[i];
         }
         n += m2;
       }
       __syncthreads();
-      keep_best(w, n, how.top);
-      kept = w.kept;
+      keep_best(w, n, top);
+      kept = w.sums->kept;
     }
     cluster.sync();
     if (rank) return;
   }
-  // sinks, then the chosen pages and the local ones as they ascend
-  const int l0 = max(lo, sinks), locals = max(own - l0 + 1, 0);
+  const int l0 = max(l.lo, l.sinks), locals = max(l.own - l0 + 1, 0);
   int before = 0;   // chosen pages before the local ones: a halving search
-  for (int top = kept; before < top;) {
-    const int mid = (before + top) / 2;
-    if (w.kept_page[mid] < l0) before = mid + 1; else top = mid;
+  for (int z = kept; before < z;) {
+    const int mid = (before + z) / 2;
+    if (w.kept_page[mid] < l0) before = mid + 1; else z = mid;
   }
-  const int count = sinks + kept + locals;
-  for (int i = tid; i < sinks; i += CH_THREADS) line[i] = i;
-  for (int i = tid; i < locals; i += CH_THREADS) line[sinks + before + i] = l0 + i;
-  for (int i = tid; i < kept; i += CH_THREADS) line[sinks + i + (i < before ? 0 : locals)] = w.kept_page[i];
-  for (int i = count + tid; i < how.width; i += CH_THREADS) line[i] = -1;
+  const int count = l.sinks + kept + locals;
+  for (int i = tid; i < l.sinks; i += CH_THREADS) line[i] = i;
+  for (int i = tid; i < locals; i += CH_THREADS) line[l.sinks + before + i] = l0 + i;
+  for (int i = tid; i < kept; i += CH_THREADS) line[l.sinks + i + (i < before ? 0 : locals)] = w.kept_page[i];
+  for (int i = count + tid; i < width; i += CH_THREADS) line[i] = -1;
+}
+
+struct Job {
+  Pool c;
+  Seqs s;
+  const int8_t* code;
+  const uint8_t* scale;
+  Packed q;
+  int G;
+  Choose how;
+  int32_t* lists;
+  Sizes z;
+};
+
+// Cluster: one list (slot blockIdx.x / CTAs of the cluster, head blockIdx.y); its CTAs share the seen pages.  Few query
+// rows (a single token's group): mma.sync, the rows its 16, the pages its 8 columns.
+constexpr int FEW = 16;
+
+template <int D>
+__global__ void __launch_bounds__(CH_THREADS) choose(const __grid_constant__ Job j) {
+  constexpr int STRIDE = D + 4;   // halves of a row: 8-byte reads of 4 lanes x 4 rows touch every bank once
+  extern __shared__ __align__(16) uint8_t raw[];
+  __half* qs = reinterpret_cast<__half*>(raw);                              // [FEW][STRIDE]
+  float* unit = reinterpret_cast<float*>(raw + FEW * STRIDE * 2);           // 2^e of a row, 0: none
+  const Work w = work_in(raw + FEW * STRIDE * 2 + FEW * 4, j.z);
+  const Pool& c = j.c;
+  const int C = cg::this_cluster().num_blocks(), rank = cg::this_cluster().block_rank();
+  const int slot = blockIdx.x / C, h = blockIdx.y, slots = gridDim.x / C;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+  if (blockIdx.x == 0 && h == 0)
+    for (int b = tid; b < j.s.n; b += CH_THREADS) seq_at(c, j.s, b);
+  const Line l = line_of(c, j.s, j.how, slot);
+  int32_t* line = j.lists + ((int64_t)h * slots + slot) * j.how.width;
+  if (!l.any) {   // (the whole cluster)
+    if (rank == 0)
+      for (int k = tid; k < j.how.width; k += CH_THREADS) line[k] = -1;
+    return;
+  }
+  const int R = l.m * j.G;   // <= FEW
+  // this CTA's share of the seen pages
+  const int per = (l.whole + C - 1) / C, a = min(rank * per, l.whole), z = min(a + per, l.whole);
+  int kept = 0;
+  if (j.how.top > 0) {
+    for (int r = warp; r < FEW; r += CH_THREADS / 32) {
+      float x[D / 32];
+      const float u = row_codes<D>(j.q, l, j.G, h, r, R, x);
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) qs[r * STRIDE + lane * (D / 32) + k] = __float2half_rn(x[k]);
+      if (lane == 0) unit[r] = u;
+    }
+#pragma unroll 1
+    for (int k0 = a; k0 < z; k0 += j.z.cap) {
+      const int n = min(j.z.cap, z - k0);
+      look_up(c, j.s, w, l, j.scale, h, k0, n, kept);
+      __syncthreads();
+      // eight pages a warp: page i + g's codes, 16 bytes at 16 t (and at 64 + 16 t), the next eight's on their way
+      auto codes = [&](int i, uint4 (&v)[D / 64]) {
+        const int at = i + g < n ? w.at[i + g] : -1;
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x)
+          v[x] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(j.code + ((int64_t)at * c.H + h) * D + x * 64) + t) : make_uint4(0, 0, 0, 0);
+      };
+      uint4 v[D / 64];
+      codes(warp * 8, v);
+      const float u0 = unit[g], u1 = unit[g + 8];
+#pragma unroll 1
+      for (int i0 = warp * 8; i0 < n; i0 += CH_THREADS / 32 * 8) {
+        uint32_t B[D / 8];
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) {
+          widen4(v[x].x, B[8 * x], B[8 * x + 1]);
+          widen4(v[x].y, B[8 * x + 2], B[8 * x + 3]);
+          widen4(v[x].z, B[8 * x + 4], B[8 * x + 5]);
+          widen4(v[x].w, B[8 * x + 6], B[8 * x + 7]);
+        }
+        codes(i0 + CH_THREADS / 32 * 8, v);
+        float acc[4] = {0.f, 0.f, 0.f, 0.f}, ac2[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {
+          const int col = (i >> 2) * 64 + t * 16 + (i & 3) * 4;
+          const uint2 x = *reinterpret_cast<const uint2*>(qs + g * STRIDE + col);
+          const uint2 y = *reinterpret_cast<const uint2*>(qs + (g + 8) * STRIDE + col);
+          const uint32_t A[4] = {x.x, y.x, x.y, y.y};
+          mma_f16(i & 1 ? ac2 : acc, A, B[2 * i], B[2 * i + 1]);
+        }
+        float best[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (u0 != 0.f) best[x] = (acc[x] + ac2[x]) * u0;
+          if (u1 != 0.f) best[x] = fmaxf(best[x], (acc[2 + x] + ac2[2 + x]) * u1);
+        }
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) {
+          best[0] = fmaxf(best[0], __shfl_xor_sync(0xffffffffu, best[0], o));
+          best[1] = fmaxf(best[1], __shfl_xor_sync(0xffffffffu, best[1], o));
+        }
+        if (g < 2) {   // page 2 t + g of the eight
+          const int x = i0 + 2 * t + g;
+          if (x < n) w.key[kept + x] = w.scale[x] != 0.f && best[g] > -INFINITY ? key_of(best[g] * w.scale[x]) : 0;
+        }
+      }
+      __syncthreads();
+      keep_best(w, kept + n, j.how.top);
+      kept = w.sums->kept;
+    }
+  }
+  finish(w, l, kept, j.how.top, line, j.how.width);
+}
+
+// The same for many query rows on the tensor cores, turned round: 128 pages are the rows of tcgen05.mma, 64 query rows its
+// columns, so that a thread's part of the result is one page, whose best score it finds by itself.  Two halves of the
+// threads take half of the query rows each.  Codes are widened to fp16 by all threads; a tile's product runs
+// while the last one's result is looked through.
+template <int D>
+struct TcLay {
+  static constexpr int NP = D / 64;
+  static constexpr int A = 0;                            // [NP][128 pages][64] swizzled
+  static constexpr int B = NP * 128 * 128;               // [NP][64 rows][64]
+  static constexpr int UNIT = B + NP * 64 * 128;         // [64] 2^e, [64] 0 or -inf
+  static constexpr int CTRL = UNIT + 512;
+  static constexpr int WORK = CTRL + 32;
+};
+constexpr uint32_t CH_TMEM = 128;   // two results of 64 columns
+
+template <int D>
+__global__ void __launch_bounds__(CH_THREADS) choose_tc(const __grid_constant__ Job j) {
+  using namespace tc;
+  using L = TcLay<D>;
+  extern __shared__ __align__(1024) uint8_t tile[];
+  const Work w = work_in(tile + L::WORK, j.z);
+  float* unit = reinterpret_cast<float*>(tile + L::UNIT);
+  uint64_t* done = reinterpret_cast<uint64_t*>(tile + L::CTRL);
+  uint32_t* holder = reinterpret_cast<uint32_t*>(done + 1);
+  const Pool& c = j.c;
+  const int C = cg::this_cluster().num_blocks(), rank = cg::this_cluster().block_rank();
+  const int slot = blockIdx.x / C, h = blockIdx.y, slots = gridDim.x / C;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  if (blockIdx.x == 0 && h == 0)
+    for (int b = tid; b < j.s.n; b += CH_THREADS) seq_at(c, j.s, b);
+  const Line l = line_of(c, j.s, j.how, slot);
+  int32_t* line = j.lists + ((int64_t)h * slots + slot) * j.how.width;
+  if (!l.any) {   // (the whole cluster)
+    if (rank == 0)
+      for (int k = tid; k < j.how.width; k += CH_THREADS) line[k] = -1;
+    return;
+  }
+  if ((smem_u32(tile) & 1023u) != 0u) {   // 128-byte-swizzled tiles need 1024-byte alignment
+    if (tid == 0) fail(c.status, DEV_INCONSISTENT, 9905);
+    return;
+  }
+  if (tid == 0) {
+    mbar_init(done, 1);
+    fence_barrier_init();
+  }
+  if (warp == 0) tmem_alloc(holder, CH_TMEM);
+  fence_before_sync();
+  __syncthreads();
+  fence_after_sync();
+  const uint32_t tmem = *holder;
+  constexpr uint32_t idesc = idesc_bf16(128, 64) & ~((1u << 7) | (1u << 10));   // fp16
+  const uint64_t ad = desc_sw128(smem_u32(tile + L::A)), bd = desc_sw128(smem_u32(tile + L::B));
+  const int R = l.m * j.G;
+  const int per = (l.whole + C - 1) / C, a = min(rank * per, l.whole), z = min(a + per, l.whole);
+  const int half = warp >> 2;
+  const uint32_t lane_off = (uint32_t)((warp & 3) * 32) << 16;
+  volatile int no_abort = 0;
+  int kept = 0;
+  uint32_t phase = 0;
+  bool ok = true;
+  if (j.how.top > 0) {
+#pragma unroll 1
+    for (int k0 = a; ok && k0 < z; k0 += j.z.cap) {
+      const int n = min(j.z.cap, z - k0);
+      look_up(c, j.s, w, l, j.scale, h, k0, n, kept);
+      float* score = half ? w.other : reinterpret_cast<float*>(w.key) + kept;
+#pragma unroll 1
+      for (int r0 = 0; ok && r0 < R; r0 += 64) {
+        // (the products that read the last rows are complete)
+#pragma unroll 4
+        for (int r = warp; r < 64; r += CH_THREADS / 32) {
+          float x[D / 32];
+          const float u = row_codes<D>(j.q, l, j.G, h, r0 + r, R, x);
+          const int col = lane * (D / 32), at = (col >> 6) * (64 * 128) + r * 128 + ((((col & 63) >> 3) ^ (r & 7)) << 4) + (col & 7) * 2;
+          const __half2 y = __floats2half2_rn(x[0], x[1]);
+          if (D == 128) {
+            const __half2 y2 = __floats2half2_rn(x[D / 32 - 2], x[D / 32 - 1]);
+            *reinterpret_cast<uint2*>(tile + L::B + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&y), *reinterpret_cast<const uint32_t*>(&y2));
+          } else {
+            *reinterpret_cast<uint32_t*>(tile + L::B + at) = *reinterpret_cast<const uint32_t*>(&y);
+          }
+          if (lane == 0) {
+            unit[r] = u;
+            unit[64 + r] = u != 0.f ? 0.f : -INFINITY;
+          }
+        }
+        __syncthreads();   // (the pages are looked up, too)
+        constexpr int V = 128 * (D / 16) / CH_THREADS;   // 16-byte parts of a tile's codes with one thread
+        const int part = tid % (D / 16), p0 = tid / (D / 16);
+        auto codes = [&](int i0, uint4 (&v)[V]) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            const int i = i0 + p0 + k * (CH_THREADS / (D / 16)), at = i < n ? w.at[i] : -1;
+            v[k] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(j.code + ((int64_t)at * c.H + h) * D) + part) : make_uint4(0, 0, 0, 0);
+          }
+        };
+        auto look = [&](int i0, uint32_t buf) {   // the best of the half's 32 rows for this thread's page
+          if (half * 32 >= R - r0) return;
+          float x[32];
+          tmem_ld32(tmem + lane_off + buf * 64 + half * 32, x);
+          tmem_wait_ld();
+          float best = -INFINITY;
+#pragma unroll
+          for (int k = 0; k < 32; k += 4) {
+            const float4 u = *reinterpret_cast<const float4*>(unit + half * 32 + k), o = *reinterpret_cast<const float4*>(unit + 64 + half * 32 + k);
+            const float2 y = __ffma2_rn(make_float2(x[k], x[k + 1]), make_float2(u.x, u.y), make_float2(o.x, o.y));
+            const float2 y2 = __ffma2_rn(make_float2(x[k + 2], x[k + 3]), make_float2(u.z, u.w), make_float2(o.z, o.w));
+            best = max3(max3(best, y.x, y.y), y2.x, y2.y);
+          }
+          const int i = i0 + (warp & 3) * 32 + lane;
+          if (i < n) score[i] = fmaxf(score[i], best);
+        };
+        uint4 v[V];
+        codes(0, v);
+        uint32_t buf = 0;
+#pragma unroll 1
+        for (int i0 = 0; ok && i0 < n; i0 += 128, buf ^= 1) {
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            uint32_t x[8];
+            widen4(v[k].x, x[0], x[1]);
+            widen4(v[k].y, x[2], x[3]);
+            widen4(v[k].z, x[4], x[5]);
+            widen4(v[k].w, x[6], x[7]);
+            const int p = p0 + k * (CH_THREADS / (D / 16)), ch = (part & 3) * 2, odd = (part >> 2) & 1;   // (the second panel's threads the odd chunk first: banks)
+            uint8_t* at = tile + L::A + (part >> 2) * (128 * 128) + p * 128;
+            const uint4 y0 = make_uint4(x[0], x[1], x[2], x[3]), y1 = make_uint4(x[4], x[5], x[6], x[7]);
+            *reinterpret_cast<uint4*>(at + (((ch + odd) ^ (p & 7)) << 4)) = odd ? y1 : y0;
+            *reinterpret_cast<uint4*>(at + (((ch + 1 - odd) ^ (p & 7)) << 4)) = odd ? y0 : y1;
+          }
+          fence_async_smem();
+          fence_before_sync();   // (results looked through before they are overwritten)
+          __syncthreads();
+          if (warp == 0) {
+            fence_after_sync();
+            if (elect_one()) {
+#pragma unroll
+              for (int kk = 0; kk < D / 16; ++kk)
+                mma_bf16(tmem + buf * 64, desc_add(ad, (kk >> 2) * (128 * 128) + (kk & 3) * 32),
+                         desc_add(bd, (kk >> 2) * (64 * 128) + (kk & 3) * 32), idesc, kk > 0);
+              mma_commit(done);
+            }
+            __syncwarp();
+          }
+          codes(i0 + 128, v);
+          if (i0 > 0) {
+            fence_after_sync();
+            look(i0 - 128, buf ^ 1);
+          }
+          ok = mbar_wait(done, phase, &no_abort);
+          phase ^= 1;
+          ok = __syncthreads_and(ok) != 0;
+          fence_after_sync();
+        }
+        if (ok) look((n - 1) / 128 * 128, buf ^ 1);
+        fence_before_sync();
+        __syncthreads();
+      }
+      for (int i = tid; i < n; i += CH_THREADS) {
+        const float x = fmaxf(reinterpret_cast<float*>(w.key)[kept + i], w.other[i]);
+        w.key[kept + i] = w.scale[i] != 0.f && x > -INFINITY ? key_of(x * w.scale[i]) : 0;
+      }
+      __syncthreads();
+      keep_best(w, kept + n, j.how.top);
+      kept = w.sums->kept;
+    }
+  }
+  if (!ok && tid == 0) fail(c.status, DEV_TIMEOUT, SITE_WAIT + 20);
+  __syncthreads();
+  if (warp == 0) {
+    fence_after_sync();
+    tmem_dealloc(tmem, CH_TMEM);
+  }
+  finish(w, l, kept, j.how.top, line, j.how.width);
 }
 
 }  // namespace
 
-cudaError_t choose_set_smem_limits() {
-  cudaError_t e = taken(cudaFuncSetAttribute(choose<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Work<128>)));
+namespace {
+template <int D>
+size_t few_bytes(const Sizes& z) {
+  return FEW * (D + 4) * 2 + FEW * 4 + work_bytes(z);
+}
+template <int D>
+size_t tc_bytes(const Sizes& z) {
+  return TcLay<D>::WORK + work_bytes(z);
+}
+template <int D>
+cudaError_t choose_limits() {
+  const Sizes z{CAP, PLACES, MAX_TOP};
+  cudaError_t e = taken(cudaFuncSetAttribute(choose<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes<D>(z)));
   if (e == cudaSuccess)
-    e = taken(cudaFuncSetAttribute(choose<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(Work<64>)));
+    e = taken(cudaFuncSetAttribute(choose_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_bytes<D>(z)));
   return e;
+}
+template <int D>
+cudaError_t launch_choose_d(const Job& job, int slots, int C, bool few, cudaStream_t st) {
+  const dim3 grid(slots * C, job.c.H);
+  if (few) return launch_kernel(choose<D>, grid, CH_THREADS, few_bytes<D>(job.z), C, false, st, job);
+  return launch_kernel(choose_tc<D>, grid, CH_THREADS, tc_bytes<D>(job.z), C, false, st, job);
+}
+}  // namespace
+
+cudaError_t choose_set_smem_limits() {
+  const cudaError_t e = choose_limits<128>();
+  return e == cudaSuccess ? choose_limits<64>() : e;
 }
 
 cudaError_t launch_summarise(const Pool& c, const Seqs& s, const int32_t* first, int8_t* code, uint8_t* scale, cudaStream_t st) {
@@ -506,14 +769,18 @@ cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, cons
                           const Choose& how, int32_t* lists, cudaStream_t st) {
   const int n_sm = sm_count();
   if (n_sm <= 0) return cudaErrorInvalidDevice;
-  const int slots = s.rows / how.tile + s.n;
-  int C = 1;
+  const int slots = s.rows / how.tile + s.n, G = Hq / c.H;
   const int64_t lines = (int64_t)std::min(slots, s.rows) * c.H;   // (a tile has a row or more)
-  while (C < 8 && lines * C <= n_sm && s.max_pages / C > 128 && 2 * C * how.top <= MAX_TOP + CAP) C *= 2;
-  const dim3 grid(slots * C, c.H);
-  if (c.d == 128)
-    return launch_kernel(choose<128>, grid, CH_THREADS, sizeof(Work<128>), C, false, st, c, s, code, scale, q, Hq / c.H, how, lists);
-  return launch_kernel(choose<64>, grid, CH_THREADS, sizeof(Work<64>), C, false, st, c, s, code, scale, q, Hq / c.H, how, lists);
+  int C = 1;
+  while (C < 8 && lines * C <= n_sm && s.max_pages / C > 128 && 2 * C * how.top <= PLACES) C *= 2;
+  auto four = [](int x) { return (x + 3) / 4 * 4; };
+  Sizes z;
+  z.top = four(how.top);
+  z.cap = std::min(CAP, four((s.max_pages + C - 1) / C));
+  z.places = std::max(z.cap + z.top, four(C * how.top));
+  const Job job{c, s, code, scale, q, G, how, lists, z};
+  const bool few = (int64_t)std::min(how.tile, s.rows) * G <= FEW;
+  return c.d == 128 ? launch_choose_d<128>(job, slots, C, few, st) : launch_choose_d<64>(job, slots, C, few, st);
 }
 
 }  // namespace cache
