@@ -118,17 +118,36 @@ __host__ __device__ __forceinline__ int seq_of_slot(const Seqs& s, int tile, int
 }
 
 #ifdef __CUDACC__
-// The same by a warp: its lanes look at 32 sequences at a time (one or two dependent reads instead of one a halving).
-__device__ __forceinline__ int seq_of_slot_warp(const Seqs& s, int tile, int slot) {
+// The same by a warp, and the sequence itself as the call may use it: the lanes look at 32 sequences at a time (one or two
+// dependent reads instead of one a halving, and the length comes with the last).
+__device__ __forceinline__ int seq_of_slot_warp(const Pool& c, const Seqs& s, int tile, int slot, Seq& q) {
   const int lane = threadIdx.x & 31;
-  int lo = 0, n = s.n;
-  while (n > 1) {
-    const int step = (n + 31) / 32, b = lo + lane * step;
-    const bool past = b < lo + n && first_slot(s, tile, b) <= slot;
-    const int k = max(__popc(__ballot_sync(0xffffffffu, past)) - 1, 0) * step;   // (in range whatever the array holds)
-    lo += k;
-    n = min(step, n - k);
+  int lo = 0, n = s.n, start = 0, end = 0, len = 0;
+  for (;;) {
+    const int step = (n + 31) / 32, b = min(lo + lane * step, s.n - 1);
+    start = __ldg(s.row_start + b);
+    if (step == 1) {
+      end = __ldg(s.row_start + b + 1);
+      len = __ldg(s.len + b);
+    }
+    const bool past = lane * step < n && clamp(start, 0, s.rows) / tile + b <= slot;
+    const int k = max(__popc(__ballot_sync(0xffffffffu, past)) - 1, 0);   // (in range whatever the array holds)
+    if (step == 1) {
+      start = __shfl_sync(0xffffffffu, start, k);
+      end = __shfl_sync(0xffffffffu, end, k);
+      len = __shfl_sync(0xffffffffu, len, k);
+      lo = min(lo + k, s.n - 1);
+      break;
+    }
+    lo += k * step;
+    n = min(step, n - k * step);
   }
+  const int64_t cap = (int64_t)s.max_pages << c.page_log2;
+  q.r0 = clamp(start, 0, s.rows);
+  q.n = clamp(end, q.r0, s.rows) - q.r0;
+  q.len = clamp(len, 0, (int)cap);
+  if (start < 0 || end < start || end > s.rows) fail(c.status, DEV_INCONSISTENT, SITE_ROWS);
+  if (len < 0 || len > cap) fail(c.status, DEV_INCONSISTENT, SITE_LEN);
   return lo;
 }
 #endif

@@ -176,17 +176,19 @@ struct Work {
   struct Sums {
     uint32_t lo[8], hi[8];
     int total[8];
-    int kept;
+    int kept, step, here, above;
   }* sums;
+  int* hist;          // [256]
 };
 struct Sizes {
   int cap, places, top;   // each a multiple of 4
 };
-__host__ __device__ inline size_t work_bytes(const Sizes& z) { return 8 * (size_t)z.places + 12 * (size_t)z.cap + 8 * (size_t)z.top + 128; }
+__host__ __device__ inline size_t work_bytes(const Sizes& z) { return 8 * (size_t)z.places + 12 * (size_t)z.cap + 8 * (size_t)z.top + 128 + 1024; }
 __device__ __forceinline__ Work work_in(uint8_t* p, const Sizes& z) {
   Work w;
   w.sums = reinterpret_cast<Work::Sums*>(p);
-  w.key = reinterpret_cast<uint32_t*>(p + 128);
+  w.hist = reinterpret_cast<int*>(p + 128);
+  w.key = reinterpret_cast<uint32_t*>(p + 128 + 1024);
   w.page = reinterpret_cast<int*>(w.key + z.places);
   w.at = w.page + z.places;
   w.scale = reinterpret_cast<float*>(w.at + z.cap);
@@ -212,9 +214,18 @@ __device__ __forceinline__ void widen4(uint32_t w, uint32_t& a, uint32_t& b) {
   b = *reinterpret_cast<const uint32_t*>(&q);
 }
 
+// Four signed bytes c as two pairs of fp16 numbers (c + 128) 2^-24: the byte is the mantissa of a subnormal number.  (Sums of d of
+// them times whole numbers up to 127 stay below 2^22 2^-24, exact in fp32; 128 times the other factors' sum goes off again.)
+__device__ __forceinline__ void biased4(uint32_t w, uint32_t& a, uint32_t& b) {
+  w ^= 0x80808080u;
+  a = __byte_perm(w, 0u, 0x4140);
+  b = __byte_perm(w, 0u, 0x4342);
+}
+
 // The `top` largest of key[0 .. n), equal ones: the first, in their order, into kept_key and kept_page.  Thread t holds
-// places t PER ..; halving the range of the keys with counts over the block finds a bound with `top` keys above
-// it, or the top-th key itself where others equal it.
+// places t PER ..; counts of the keys in 256 even steps between the least and the largest, then in 256 steps of the one that the
+// top-th key lies in, and so on (two or three rounds as a rule), end at a bound with `top` keys above it, or at the top-th key
+// itself where others equal it.
 template <int PER>
 __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -237,6 +248,7 @@ __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
     w.sums->hi[warp] = most;
     w.sums->total[warp] = valid;
   }
+  w.hist[tid] = 0;
   __syncthreads();
   valid = 0;
 #pragma unroll
@@ -249,31 +261,59 @@ __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
   uint32_t T = 0;
   int need = 0;
   if (valid > top) {
-    // lo: more than `top` keys >= lo; hi: at most `top` keys >= hi
-    uint32_t lo = least, hi = most + 1;   // (no key is 0xffffffff: that would be a NaN)
-    int above = 0;                        // keys >= hi
+    uint32_t lo = least, span = most - least;   // (as a difference: what lies above lo may pass 32 bits)
+    int shift = max(0, 24 - __clz(span)), left = top;   // (most - least) >> shift < 256; keys wanted from lo .. on
 #pragma unroll 1
-    while (hi - lo > 1 && above != top) {
-      const uint32_t mid = lo + (hi - lo) / 2;
-      int c = 0;
+    for (;;) {
 #pragma unroll
-      for (int i = 0; i < PER; ++i) c += k[i] >= mid;
-      c = __reduce_add_sync(0xffffffffu, c);
+      for (int i = 0; i < PER; ++i)
+        if (k[i] >= lo && k[i] - lo <= span) atomicAdd(&w.hist[(k[i] - lo) >> shift], 1);
       __syncthreads();
-      if (lane == 0) w.sums->total[warp] = c;
-      __syncthreads();
-      c = 0;
+      if (warp == 0) {   // lane: steps 255 - 8 lane, .. downwards
+        int own = 0, c[8];
 #pragma unroll
-      for (int x = 0; x < CH_THREADS / 32; ++x) c += w.sums->total[x];
-      if (c > top) {
-        lo = mid;
-      } else {
-        hi = mid;
-        above = c;
+        for (int i = 0; i < 8; ++i) own += c[i] = w.hist[255 - lane * 8 - i];
+        int incl = own;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, incl, o);
+          if (lane >= o) incl += y;
+        }
+        if (lane == __ffs(__ballot_sync(0xffffffffu, incl >= left)) - 1) {   // (there is one)
+          int above = incl - own, step = 255 - lane * 8, here = 0;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {   // (not by an index that varies)
+            if (above + c[i] >= left) {
+              here = c[i];
+              break;
+            }
+            above += c[i];
+            --step;
+          }
+          w.sums->step = step;
+          w.sums->here = here;
+          w.sums->above = above;
+        }
       }
+      __syncthreads();
+      const int step = w.sums->step, here = w.sums->here;
+      left -= w.sums->above;   // wanted of the step's
+      lo += (uint32_t)step << shift;
+      if (here == left) {      // all of them
+        T = lo - 1;
+        need = 0;
+        break;
+      }
+      if (shift == 0) {        // equal ones
+        T = lo;
+        need = left;
+        break;
+      }
+      span = (1u << shift) - 1;
+      shift = max(0, shift - 8);
+      w.hist[tid] = 0;
+      __syncthreads();
     }
-    T = hi - 1;
-    need = top - above;   // (0 unless hi = lo + 1: then T = lo is the top-th key)
   }
   int eq = 0, gt = 0;
 #pragma unroll
@@ -329,9 +369,8 @@ struct Line {
 };
 __device__ __forceinline__ Line line_of(const Pool& c, const Seqs& s, const Choose& how, int slot) {
   Line l{};
-  l.b = seq_of_slot_warp(s, how.tile, slot);
-  l.q = seq_at(c, s, l.b);
-  l.i0 = (slot - first_slot(s, how.tile, l.b)) * how.tile;
+  l.b = seq_of_slot_warp(c, s, how.tile, slot, l.q);
+  l.i0 = (slot - l.q.r0 / how.tile - l.b) * how.tile;
   l.m = min(how.tile, l.q.n - l.i0);
   const int p1 = l.q.len - l.q.n + l.i0 + l.m - 1, p0 = max(p1 - l.m + 1, 0);
   l.any = l.i0 >= 0 && l.m > 0 && p1 >= 0;
@@ -350,10 +389,14 @@ __device__ __forceinline__ void look_up(const Pool& c, const Seqs& s, const Work
                                         int k0, int n, int kept) {
   for (int i = threadIdx.x; i < n; i += CH_THREADS) {
     const int k = k0 + i;
-    const int64_t row = pool_row(c, s, l.b, h, k << c.page_log2), at = row >> c.page_log2;   // page * H + h
-    const uint32_t byte = row >= 0 ? scale[at] : 255u;
+    int page = s.table[(int64_t)l.b * s.max_pages + k];
+    if ((unsigned)page >= (unsigned)c.n_pages) {
+      fail(c.status, DEV_INCONSISTENT, SITE_PAGE);
+      page = -1;
+    }
+    const uint32_t byte = page >= 0 ? __ldg(scale + (int64_t)page * c.H + h) : 255u;
     const bool listed = k < l.sinks || (k >= l.lo && k <= l.own);
-    w.at[i] = row >= 0 ? (int)(at / c.H) : -1;
+    w.at[i] = page;
     w.scale[i] = listed || byte == 255u ? 0.f : scale_of(byte);
     w.other[i] = -INFINITY;
     w.page[kept + i] = k;
@@ -365,14 +408,28 @@ __device__ __forceinline__ void look_up(const Pool& c, const Seqs& s, const Work
   }
 }
 
+struct Job {
+  Pool c;
+  Seqs s;
+  const int8_t* code;
+  const uint8_t* scale;
+  Packed q;
+  int G;
+  uint32_t g_inverse;   // ceil(2^32 / G): r / G is the high half of r times it (G > 1, r < 2^14)
+  Choose how;
+  int32_t* lists;
+  Sizes z;
+};
+
 // A warp's query row r of the tile (row = token * G + head): lane's D / 32 numbers as whole ones, its exponent's power of
 // two (0: no codes).
 template <int D>
-__device__ __forceinline__ float row_codes(const Packed& qp, const Line& l, int G, int h, int r, int R, float (&x)[D / 32]) {
+__device__ __forceinline__ float row_codes(const Job& j, const Line& l, int h, int r, int R, float (&x)[D / 32]) {
   const int lane = threadIdx.x & 31;
+  const Packed& qp = j.q;
   uint32_t top = 0x7f800000u;   // (a row behind the last has none)
   if (r < R) {
-    const int i = r / G, hq = h * G + r - i * G;
+    const int i = j.G == 1 ? r : (int)__umulhi((uint32_t)r, j.g_inverse), hq = h * j.G + r - i * j.G;
     const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(qp.p) + hq * qp.head + (int64_t)(l.q.r0 + l.i0 + i) * qp.row + lane * (D / 32);
     if (D == 128) {
       const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
@@ -440,24 +497,12 @@ __device__ __forceinline__ void finish(const Work& w, const Line& l, int kept, i
   for (int i = count + tid; i < width; i += CH_THREADS) line[i] = -1;
 }
 
-struct Job {
-  Pool c;
-  Seqs s;
-  const int8_t* code;
-  const uint8_t* scale;
-  Packed q;
-  int G;
-  Choose how;
-  int32_t* lists;
-  Sizes z;
-};
-
 // Cluster: one list (slot blockIdx.x / CTAs of the cluster, head blockIdx.y); its CTAs share the seen pages.  Few query
 // rows (a single token's group): mma.sync, the rows its 16, the pages its 8 columns.
 constexpr int FEW = 16;
 
 template <int D>
-__global__ void __launch_bounds__(CH_THREADS) choose(const __grid_constant__ Job j) {
+__global__ void __launch_bounds__(CH_THREADS, 3) choose(const __grid_constant__ Job j) {
   constexpr int STRIDE = D + 4;   // halves of a row: 8-byte reads of 4 lanes x 4 rows touch every bank once
   extern __shared__ __align__(16) uint8_t raw[];
   __half* qs = reinterpret_cast<__half*>(raw);                              // [FEW][STRIDE]
@@ -483,7 +528,7 @@ __global__ void __launch_bounds__(CH_THREADS) choose(const __grid_constant__ Job
   if (j.how.top > 0) {
     for (int r = warp; r < FEW; r += CH_THREADS / 32) {
       float x[D / 32];
-      const float u = row_codes<D>(j.q, l, j.G, h, r, R, x);
+      const float u = row_codes<D>(j, l, h, r, R, x);
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) qs[r * STRIDE + lane * (D / 32) + k] = __float2half_rn(x[k]);
       if (lane == 0) unit[r] = u;
@@ -563,7 +608,7 @@ struct TcLay {
 constexpr uint32_t CH_TMEM = 128;   // two results of 64 columns
 
 template <int D>
-__global__ void __launch_bounds__(CH_THREADS) choose_tc(const __grid_constant__ Job j) {
+__global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant__ Job j) {
   using namespace tc;
   using L = TcLay<D>;
   extern __shared__ __align__(1024) uint8_t tile[];
@@ -619,7 +664,7 @@ __global__ void __launch_bounds__(CH_THREADS) choose_tc(const __grid_constant__ 
 #pragma unroll 4
         for (int r = warp; r < 64; r += CH_THREADS / 32) {
           float x[D / 32];
-          const float u = row_codes<D>(j.q, l, j.G, h, r0 + r, R, x);
+          const float u = row_codes<D>(j, l, h, r0 + r, R, x);
           const int col = lane * (D / 32), at = (col >> 6) * (64 * 128) + r * 128 + ((((col & 63) >> 3) ^ (r & 7)) << 4) + (col & 7) * 2;
           const __half2 y = __floats2half2_rn(x[0], x[1]);
           if (D == 128) {
@@ -628,19 +673,26 @@ __global__ void __launch_bounds__(CH_THREADS) choose_tc(const __grid_constant__ 
           } else {
             *reinterpret_cast<uint32_t*>(tile + L::B + at) = *reinterpret_cast<const uint32_t*>(&y);
           }
+          float sum = 0.f;   // (whole numbers)
+#pragma unroll
+          for (int k = 0; k < D / 32; ++k) sum += x[k];
+          sum = (float)__reduce_add_sync(0xffffffffu, (int)sum);
           if (lane == 0) {
-            unit[r] = u;
-            unit[64 + r] = u != 0.f ? 0.f : -INFINITY;
+            unit[r] = u * 0x1p24f;
+            unit[64 + r] = u != 0.f ? -128.f * sum * u : -INFINITY;
           }
         }
         __syncthreads();   // (the pages are looked up, too)
-        constexpr int V = 128 * (D / 16) / CH_THREADS;   // 16-byte parts of a tile's codes with one thread
-        const int part = tid % (D / 16), p0 = tid / (D / 16);
+        // 16-byte parts of a tile's codes: eight threads take four parts (64 columns) of two neighbouring rows, so that their
+        // stores, swizzled by the row, touch every bank once
+        constexpr int V = 128 * (D / 16) / CH_THREADS, STEP = CH_THREADS / 4 / L::NP;
+        const int part = tid & 3, panel = (tid >> 3) % L::NP, p0 = (tid >> 3) / L::NP * 2 + ((tid >> 2) & 1);
+        const int8_t* const from = j.code + (int64_t)h * D + panel * 64 + part * 16;
         auto codes = [&](int i0, uint4 (&v)[V]) {
 #pragma unroll
           for (int k = 0; k < V; ++k) {
-            const int i = i0 + p0 + k * (CH_THREADS / (D / 16)), at = i < n ? w.at[i] : -1;
-            v[k] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(j.code + ((int64_t)at * c.H + h) * D) + part) : make_uint4(0, 0, 0, 0);
+            const int i = i0 + p0 + k * STEP, at = i < n ? w.at[i] : -1;
+            v[k] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(from + (int64_t)at * (c.H * D))) : make_uint4(0, 0, 0, 0);
           }
         };
         auto look = [&](int i0, uint32_t buf) {   // the best of the half's 32 rows for this thread's page
@@ -664,18 +716,17 @@ __global__ void __launch_bounds__(CH_THREADS) choose_tc(const __grid_constant__ 
         uint32_t buf = 0;
 #pragma unroll 1
         for (int i0 = 0; ok && i0 < n; i0 += 128, buf ^= 1) {
+          uint8_t* const to = tile + L::A + panel * (128 * 128) + p0 * 128;
 #pragma unroll
           for (int k = 0; k < V; ++k) {
             uint32_t x[8];
-            widen4(v[k].x, x[0], x[1]);
-            widen4(v[k].y, x[2], x[3]);
-            widen4(v[k].z, x[4], x[5]);
-            widen4(v[k].w, x[6], x[7]);
-            const int p = p0 + k * (CH_THREADS / (D / 16)), ch = (part & 3) * 2, odd = (part >> 2) & 1;   // (the second panel's threads the odd chunk first: banks)
-            uint8_t* at = tile + L::A + (part >> 2) * (128 * 128) + p * 128;
-            const uint4 y0 = make_uint4(x[0], x[1], x[2], x[3]), y1 = make_uint4(x[4], x[5], x[6], x[7]);
-            *reinterpret_cast<uint4*>(at + (((ch + odd) ^ (p & 7)) << 4)) = odd ? y1 : y0;
-            *reinterpret_cast<uint4*>(at + (((ch + 1 - odd) ^ (p & 7)) << 4)) = odd ? y0 : y1;
+            biased4(v[k].x, x[0], x[1]);
+            biased4(v[k].y, x[2], x[3]);
+            biased4(v[k].z, x[4], x[5]);
+            biased4(v[k].w, x[6], x[7]);
+            static_assert(STEP % 8 == 0, "a thread's rows share their swizzle");
+            *reinterpret_cast<uint4*>(to + k * STEP * 128 + (((2 * part) ^ (p0 & 7)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+            *reinterpret_cast<uint4*>(to + k * STEP * 128 + (((2 * part + 1) ^ (p0 & 7)) << 4)) = make_uint4(x[4], x[5], x[6], x[7]);
           }
           fence_async_smem();
           fence_before_sync();   // (results looked through before they are overwritten)
@@ -778,7 +829,7 @@ cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, cons
   z.top = four(how.top);
   z.cap = std::min(CAP, four((s.max_pages + C - 1) / C));
   z.places = std::max(z.cap + z.top, four(C * how.top));
-  const Job job{c, s, code, scale, q, G, how, lists, z};
+  const Job job{c, s, code, scale, q, G, (uint32_t)((0x100000000ull + G - 1) / G), how, lists, z};
   const bool few = (int64_t)std::min(how.tile, s.rows) * G <= FEW;
   return c.d == 128 ? launch_choose_d<128>(job, slots, C, few, st) : launch_choose_d<64>(job, slots, C, few, st);
 }

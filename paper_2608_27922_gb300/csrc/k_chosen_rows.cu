@@ -16,6 +16,7 @@
 #include "cache_internal.h"
 
 #include <cooperative_groups.h>
+#include <cuda_fp16.h>
 
 #include <algorithm>
 
@@ -28,11 +29,22 @@ namespace {
 
 using namespace tc;
 
-constexpr int WARPS = 6, THREADS = WARPS * 32, MAX_WIDTH = 1024;
+constexpr int MAX_WIDTH = 1024;
+// Warps of a CTA, CTAs of an SM (registers), times 16 positions of a warp's step.
+template <int D, bool E4M3>
+struct Cfg {
+  static constexpr int WARPS = !E4M3 && D == 128 ? 6 : 8, CTAS = 2, NH = E4M3 ? 128 / D : 1;
+  static constexpr int THREADS = 32 * WARPS;
+};
 constexpr float RAISE_LOG2 = 8.0f;   // how far a score may pass the running maximum before that is raised
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -42,7 +54,7 @@ __device__ __forceinline__ uint32_t transpose(uint32_t x) {
   return y;
 }
 
-// A row's numbers with one lane of its four: NW registers of bf16 pairs.  bf16: load p of 16 bytes holds d = 32 p + 8 t ..;
+// A row's numbers with one lane of its four: registers of pairs.  bf16: load p of 16 bytes holds d = 32 p + 8 t ..;
 // codes: load p holds d = 64 p + 16 t ..
 template <int D>
 struct Frag {
@@ -55,71 +67,61 @@ __device__ __forceinline__ int dim_of(int r, int t, int e) {
   return E4M3 ? (r >> 3) * 64 + t * 16 + (r & 7) * 2 + e : (r >> 2) * 32 + t * 8 + (r & 3) * 2 + e;
 }
 
+// d of row g (half 1: g + 8) of outputs block i.  bf16: words 2 i and 2 i + 1 were transposed, whose columns 2 t' + e are d of
+// lane t''s number e.  Codes: word i, whose columns t' .. are pairs: row g is the pair of lane g / 2, the two numbers of which
+// (word halves) are columns 2 (g / 2) and 2 (g / 2) + 1 of the block; the pair's first code goes to row g, its second to g + 8.
+template <bool E4M3>
+__device__ __forceinline__ int column(int i, int half, int g) {
+  return E4M3 ? dim_of<E4M3>(2 * i + (g & 1), g >> 1, half) : dim_of<E4M3>(2 * i + half, g >> 1, g & 1);
+}
+
 template <int D, bool E4M3>
 struct Raw {
   uint4 v[E4M3 ? D / 64 : D / 32];
-  uint32_t scale;
 };
 
+// Row `at` (of d numbers) of a pool: lane t's share.
 template <int D, bool E4M3>
-__device__ __forceinline__ Raw<D, E4M3> fetch(const void* pool, const uint8_t* scales, int64_t at, int t) {
+__device__ __forceinline__ Raw<D, E4M3> fetch(const void* pool, int64_t at, int t) {
   Raw<D, E4M3> x;
-  x.scale = 127u;
-  if (at < 0) {   // nobody's
-#pragma unroll
-    for (int p = 0; p < (int)(sizeof(x.v) / 16); ++p) x.v[p] = make_uint4(0, 0, 0, 0);
-    return x;
-  }
   const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint8_t*>(pool) + at * (E4M3 ? D : 2 * D)) + t;
 #pragma unroll
   for (int p = 0; p < (int)(sizeof(x.v) / 16); ++p) x.v[p] = __ldg(src + 4 * p);
-  if (E4M3) x.scale = __ldg(scales + at);
   return x;
 }
+template <int D, bool E4M3>
+__device__ __forceinline__ uint32_t word(const Raw<D, E4M3>& x, int i) {
+  const uint4& v = x.v[i >> 2];
+  return (i & 3) == 0 ? v.x : (i & 3) == 1 ? v.y : (i & 3) == 2 ? v.z : v.w;
+}
 
-// Four bf16 from four codes: a code's bits in bf16's fields are its value times 2^-120; f holds 2^120 times the scale.
-__device__ __forceinline__ void widen(uint32_t w, __nv_bfloat162 f, uint32_t& a, uint32_t& b) {
-  const uint32_t hi = (w & 0x80808080u) | ((w >> 4) & 0x07070707u), lo = (w << 4) & 0xf0f0f0f0u;
-  const uint32_t x = __byte_perm(lo, hi, 0x5140), y = __byte_perm(lo, hi, 0x7362);
-  const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&x), f);
-  const __nv_bfloat162 q = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&y), f);
-  a = *reinterpret_cast<const uint32_t*>(&p);
-  b = *reinterpret_cast<const uint32_t*>(&q);
+// Four fp16 from four codes (exact).
+__device__ __forceinline__ void widen_f16(uint32_t w, uint32_t& a, uint32_t& b) {
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(a), "=r"(b) : "r"(w));
+}
+
+// Two positions of two neighbouring columns (bytes: position 0: d, d + 1, position 1: d, d + 1) as bf16, a register for each
+// column: a code's bits in bf16's fields (its sign spread over a byte above it, all but one of those bits cleared) are its
+// value times 2^-120; f holds 2^120 times the positions' scales.
+__device__ __forceinline__ void widen_values(uint32_t w, __nv_bfloat162 f, uint32_t& d0, uint32_t& d1) {
+  uint32_t a, b;
+  asm("prmt.b32 %0, %1, 0, 0xa280;" : "=r"(a) : "r"(w));   // (a selector's upper bit: that byte's sign, eight times)
+  asm("prmt.b32 %0, %1, 0, 0xb391;" : "=r"(b) : "r"(w));
+  a = (a << 4) & 0x87f087f0u;
+  b = (b << 4) & 0x87f087f0u;
+  const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), f);
+  const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), f);
+  d0 = *reinterpret_cast<const uint32_t*>(&x);
+  d1 = *reinterpret_cast<const uint32_t*>(&y);
 }
 __device__ __forceinline__ __nv_bfloat162 bf2(uint32_t bits) { return *reinterpret_cast<const __nv_bfloat162*>(&bits); }
-
-template <int D, bool E4M3>
-__device__ __forceinline__ Frag<D> numbers(const Raw<D, E4M3>& x) {
-  Frag<D> y;
-  if (!E4M3) {
-#pragma unroll
-    for (int p = 0; p < D / 32; ++p) {
-      y.w[4 * p] = x.v[p].x;
-      y.w[4 * p + 1] = x.v[p].y;
-      y.w[4 * p + 2] = x.v[p].z;
-      y.w[4 * p + 3] = x.v[p].w;
-    }
-    return y;
-  }
-  // one factor where 2^120 times the scale is a bf16 number; else two, the scale by itself (255: NaN)
-  const uint32_t s = x.scale;
-  const __nv_bfloat162 f = bf2((s > 134u ? 247u : s + 120u) * 0x00800080u);
-#pragma unroll
-  for (int p = 0; p < (int)(sizeof(x.v) / 16); ++p) {
-    widen(x.v[p].x, f, y.w[8 * p], y.w[8 * p + 1]);
-    widen(x.v[p].y, f, y.w[8 * p + 2], y.w[8 * p + 3]);
-    widen(x.v[p].z, f, y.w[8 * p + 4], y.w[8 * p + 5]);
-    widen(x.v[p].w, f, y.w[8 * p + 6], y.w[8 * p + 7]);
-  }
-  if (__any_sync(0xffffffffu, s > 134u)) {
-    const __nv_bfloat162 f2 = bf2(s == 255u ? 0x7fff7fffu : (s > 134u ? s : 127u) * 0x00800080u);
-#pragma unroll
-    for (int r = 0; r < D / 8; ++r) {
-      const __nv_bfloat162 z = __hmul2(bf2(y.w[r]), f2);
-      y.w[r] = *reinterpret_cast<const uint32_t*>(&z);
-    }
-  }
-  return y;
+// 2^120 times the scales of two bytes (low and high half), as far as bf16 holds it; the rest (255: NaN).
+__device__ __forceinline__ __nv_bfloat162 factor(uint32_t s0, uint32_t s1) {
+  return bf2((s0 > 134u ? 247u : s0 + 120u) << 7 | (s1 > 134u ? 247u : s1 + 120u) << 23);
+}
+__device__ __forceinline__ __nv_bfloat162 factor_rest(uint32_t s0, uint32_t s1) {
+  auto one = [](uint32_t s) { return s == 255u ? 0x7fffu : (s > 134u ? s : 127u) << 7; };
+  return bf2(one(s0) | one(s1) << 16);
 }
 
 // Clears what is not finite in a pair; true where there was any.
@@ -135,7 +137,21 @@ __device__ __noinline__ float value_at(const Pool& c, int64_t at, int d) {
   return c.vs[at] == 255 ? __int_as_float(0x7fffffff) : 0.f;   // (a code is finite)
 }
 
-template <int D>
+__device__ __forceinline__ uint32_t times(uint32_t x, __nv_bfloat162 f) {
+  const __nv_bfloat162 y = __hmul2(bf2(x), f);
+  return *reinterpret_cast<const uint32_t*>(&y);
+}
+// Element i of a small array in registers.
+template <typename T, int N>
+__device__ __forceinline__ T place_of(const T (&x)[N], int i) {
+  T y = x[0];
+#pragma unroll
+  for (int k = 1; k < N; ++k)
+    if (i == k) y = x[k];
+  return y;
+}
+
+template <int D, int WARPS>
 struct Smem {
   int page[MAX_WIDTH], entry[MAX_WIDTH];
   float part[WARPS][8][D + 4];   // outputs, maximum, sum
@@ -144,17 +160,21 @@ struct Smem {
 };
 
 template <int D, bool E4M3>
-__global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed qp, Packed op, int G, Mask m, Chosen how, int blocks) {
-  __shared__ Smem<D> w;
+__global__ void __launch_bounds__(Cfg<D, E4M3>::THREADS, (Cfg<D, E4M3>::CTAS)) chosen_rows(Pool c, Seqs s, Packed qp, Packed op, int G, Mask m, Chosen how, int blocks) {
+  constexpr int WARPS = Cfg<D, E4M3>::WARPS, THREADS = Cfg<D, E4M3>::THREADS, NH = Cfg<D, E4M3>::NH;
+  __shared__ Smem<D, WARPS> w;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = cluster.num_blocks(), rank = cluster.block_rank();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   const int unit = blockIdx.x / C, slot = unit / blocks, r0 = (unit - slot * blocks) * 8, h = blockIdx.y;
   if (blockIdx.x == 0 && h == 0)
     for (int b = tid; b < s.n; b += THREADS) seq_at(c, s, b);
-  const int b = seq_of_slot_warp(s, how.tile, slot);
-  const Seq q = seq_at(c, s, b);
-  const int i0 = (slot - first_slot(s, how.tile, b)) * how.tile;
+  // (the list's first entries are asked for before the sequence is known)
+  const int32_t* line = how.lists + ((int64_t)h * how.slots + slot) * how.width;
+  const int early = tid < how.width ? __ldg(line + tid) : -1, early_before = tid && tid < how.width ? __ldg(line + tid - 1) : -1;
+  Seq q;
+  const int b = seq_of_slot_warp(c, s, how.tile, slot, q);
+  const int i0 = (slot - q.r0 / how.tile - b) * how.tile;
   const int tokens = min(how.tile, q.n - i0), R = tokens * G;
   if (i0 < 0 || r0 >= R) return;   // (the whole cluster)
   const int rows = min(8, R - r0), p0 = q.len - q.n + i0;
@@ -164,11 +184,10 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
   };
   const int all_end = end_of(0), any_end = end_of(rows - 1);
   // the list: pages of the pool
-  const int32_t* line = how.lists + ((int64_t)h * how.slots + slot) * how.width;
   if (tid == 0) w.count = how.width;
   __syncthreads();
   for (int k = tid; k < how.width; k += THREADS) {
-    const int e = __ldg(line + k), before = k ? __ldg(line + k - 1) : -1;
+    const int e = k == tid ? early : __ldg(line + k), before = k == tid ? early_before : __ldg(line + k - 1);
     int page = -1;
     if (e < 0) {
       atomicMin(&w.count, k);
@@ -198,11 +217,32 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
       Q.w[k + 3] = x.w;
     }
   }
+  // codes are met by queries in fp16, each row times a power of two that brings its largest magnitude to 2^14 .. 2^15: what is
+  // 2^-28 of that or more stays exact, smaller numbers are off by 2^-39 of it at most
+  float mul[2] = {m.sl2, m.sl2};   // of the columns' scores, times log2(e)
+  if constexpr (E4M3) {
+    uint32_t top = 0;   // (bits of magnitudes order like the magnitudes)
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) top = __vmaxu2(top, Q.w[k] & 0x7fff7fffu);
+    top = max(top & 0xffffu, top >> 16);
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    const int x = top >= 0x7f80u ? 14 : max((int)(top >> 7) - 127, -100);
+    const float f = __uint_as_float((uint32_t)(127 + 14 - x) << 23);
+#pragma unroll
+    for (int k = 0; k < D / 8; ++k) {
+      const __half2 y = __floats2half2_rn(__uint_as_float(Q.w[k] << 16) * f, __uint_as_float(Q.w[k] & 0xffff0000u) * f);
+      Q.w[k] = *reinterpret_cast<const uint32_t*>(&y);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e) mul[e] *= __uint_as_float((uint32_t)(127 - 14 + __shfl_sync(0xffffffffu, x, 4 * (2 * t + e))) << 23);
+  }
   const int end[2] = {2 * t < rows ? end_of(2 * t) : 0, 2 * t + 1 < rows ? end_of(2 * t + 1) : 0};
   float o[D / 16][4], mrun[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) o[k][0] = o[k][1] = o[k][2] = o[k][3] = 0.f;
-  // a step's place: its first position, and lane g's row of the pool (-1: nothing to be read)
+  // the place of 16 positions: the first one, and its row of the pool (nothing to be read: a position that nobody sees, and
+  // whatever row is there)
   auto place = [&](int st, int& pos0, int64_t& at) {
     pos0 = 0x40000000;
     at = -1;
@@ -210,39 +250,93 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
     const int k = st >> sub, in = (st & ((1 << sub) - 1)) * 16;
     if (w.page[k] < 0) return;
     pos0 = (w.entry[k] << c.page_log2) + in;
-    at = ((int64_t)w.page[k] << c.page_log2) + in + g;
+    at = ((int64_t)w.page[k] << c.page_log2) + in;
   };
-  // Keys (values) of the next step are asked for as soon as this one's have gone into their product.  (Positions
-  // that nobody sees may lie behind the sequence: keys there are read, the page is there, and masked.)
-  int pos0, next0;
-  int64_t at, next;
-  place(first, pos0, at);
-  Raw<D, E4M3> k0 = fetch<D, E4M3>(c.k, c.ks, at, t), k1 = fetch<D, E4M3>(c.k, c.ks, at < 0 ? at : at + 8, t);
-  Raw<D, E4M3> v0 = fetch<D, E4M3>(c.v, c.vs, pos0 + g < any_end ? at : -1, t);
-  Raw<D, E4M3> v1 = fetch<D, E4M3>(c.v, c.vs, pos0 + g + 8 < any_end ? at + 8 : -1, t);
-#pragma unroll 1
-  for (int st = first; st < last; ++st, pos0 = next0, at = next) {
-    place(st + 1, next0, next);
-    float sc[4] = {0.f, 0.f, 0.f, 0.f}, sd[4] = {0.f, 0.f, 0.f, 0.f};
-    {
-      const Frag<D> a = numbers<D, E4M3>(k0), z = numbers<D, E4M3>(k1);
+  // A warp takes NH times 16 positions a step: as many as the registers hold.  Keys (values) of the next step are asked for as
+  // soon as this one's have gone into their product.  (Positions that nobody sees are read, their page is there, and masked.)
+  int pos0[NH], next0[NH];
+  int64_t at[NH], next[NH];
+  using R1 = Raw<D, E4M3>;
+  R1 k0[NH]{}, k1[NH]{}, v0[NH]{}, v1[NH]{};
+  uint32_t ks0[NH]{}, ks1[NH]{}, vs0[NH]{}, vs1[NH]{};   // scale bytes: keys g, g + 8; values 2 t, 2 t + 1 and those + 8
+  auto load_keys = [&](const int64_t (&x)[NH]) {
 #pragma unroll
-      for (int i = 0; i < D / 16; i += 2) {
-        mma(sc, a.w[2 * i], z.w[2 * i], a.w[2 * i + 1], z.w[2 * i + 1], Q.w[2 * i], Q.w[2 * i + 1]);
-        mma(sd, a.w[2 * i + 2], z.w[2 * i + 2], a.w[2 * i + 3], z.w[2 * i + 3], Q.w[2 * i + 2], Q.w[2 * i + 3]);
+    for (int n = 0; n < NH; ++n) {
+      if (x[n] < 0) continue;
+      k0[n] = fetch<D, E4M3>(c.k, x[n] + g, t);
+      k1[n] = fetch<D, E4M3>(c.k, x[n] + g + 8, t);
+    }
+  };
+  auto load_values = [&](const int64_t (&x)[NH]) {
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      if (x[n] < 0) continue;
+      v0[n] = fetch<D, E4M3>(c.v, x[n] + g, t);
+      v1[n] = fetch<D, E4M3>(c.v, x[n] + g + 8, t);
+    }
+  };
+  auto load_scales = [&](const int64_t (&x)[NH]) {
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      if (x[n] < 0) continue;
+      ks0[n] = __ldg(c.ks + x[n] + g);
+      ks1[n] = __ldg(c.ks + x[n] + g + 8);
+      vs0[n] = __ldg(reinterpret_cast<const uint16_t*>(c.vs + x[n]) + t);
+      vs1[n] = __ldg(reinterpret_cast<const uint16_t*>(c.vs + x[n] + 8) + t);
+    }
+  };
+#pragma unroll
+  for (int n = 0; n < NH; ++n) place(first + n, pos0[n], at[n]);
+  load_keys(at);
+  load_values(at);
+  if constexpr (E4M3) load_scales(at);
+#pragma unroll 1
+  for (int st = first; st < last; st += NH) {
+    bool partial = false;
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      place(st + NH + n, next0[n], next[n]);
+      partial = partial || pos0[n] + 16 > all_end;
+    }
+    float sc[NH][4];
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      float sd[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sc[n][e] = 0.f;
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i) {   // a word of codes: a step of 16
+          uint32_t a0, a2, a1, a3;
+          widen_f16(word(k0[n], i), a0, a2);
+          widen_f16(word(k1[n], i), a1, a3);
+          mma_f16(i & 1 ? sd : sc[n], a0, a1, a2, a3, Q.w[2 * i], Q.w[2 * i + 1]);
+        }
+        const float f0 = scale_of(ks0[n]), f1 = scale_of(ks1[n]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[n][e] = (sc[n][e] + sd[e]) * (e < 2 ? f0 : f1);
+      } else {
+#pragma unroll
+        for (int i = 0; i < D / 16; ++i)
+          mma(i & 1 ? sd : sc[n], word(k0[n], 2 * i), word(k1[n], 2 * i), word(k0[n], 2 * i + 1), word(k1[n], 2 * i + 1), Q.w[2 * i], Q.w[2 * i + 1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[n][e] += sd[e];
       }
     }
-    k0 = fetch<D, E4M3>(c.k, c.ks, next, t);
-    k1 = fetch<D, E4M3>(c.k, c.ks, next < 0 ? next : next + 8, t);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sc[e] += sd[e];
-    const bool partial = pos0 + 16 > all_end;
+    load_keys(next);
     if (partial) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (pos0 + g + (e >> 1) * 8 >= end[e & 1]) sc[e] = -INFINITY;
+      for (int n = 0; n < NH; ++n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (pos0[n] + g + (e >> 1) * 8 >= end[e & 1]) sc[n][e] = -INFINITY;
     }
-    float mx[2] = {fmaxf(sc[0], sc[2]), fmaxf(sc[1], sc[3])};
+    float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      mx[0] = max3(mx[0], sc[n][0], sc[n][2]);
+      mx[1] = max3(mx[1], sc[n][1], sc[n][3]);
+    }
 #pragma unroll
     for (int x = 4; x < 32; x <<= 1) {
       mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], x));
@@ -252,7 +346,7 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
     float alpha[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      mx[e] *= m.sl2;
+      mx[e] *= mul[e];
       raise[e] = mx[e] > mrun[e] + RAISE_LOG2 || (mrun[e] == -INFINITY && mx[e] > -INFINITY);
       alpha[e] = raise[e] ? (mrun[e] == -INFINITY ? 0.f : ex2(mrun[e] - mx[e])) : 1.f;
       if (raise[e]) mrun[e] = mx[e];
@@ -262,49 +356,92 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
       for (int e = 0; e < 2; ++e) {
         l[e] *= alpha[e];
 #pragma unroll
-        for (int k2 = 0; k2 < D / 16; ++k2) {
-          o[k2][e] *= alpha[e];
-          o[k2][2 + e] *= alpha[e];
+        for (int i = 0; i < D / 16; ++i) {
+          o[i][e] *= alpha[e];
+          o[i][2 + e] *= alpha[e];
         }
       }
     }
-    float p[4];
+    uint32_t b0[NH], b1[NH];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      p[e] = ex2(fmaf(sc[e], m.sl2, mrun[e & 1] == -INFINITY ? 0.f : -mrun[e & 1]));
-      l[e & 1] += p[e];
+    for (int n = 0; n < NH; ++n) {
+      float p[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        p[e] = ex2(fmaf(sc[n][e], mul[e & 1], mrun[e & 1] == -INFINITY ? 0.f : -mrun[e & 1]));
+        l[e & 1] += p[e];
+      }
+      b0[n] = transpose(pack_bf16(p[0], p[1]));
+      b1[n] = transpose(pack_bf16(p[2], p[3]));
     }
-    const uint32_t b0 = transpose(pack_bf16(p[0], p[1])), b1 = transpose(pack_bf16(p[2], p[3]));
-    Frag<D> a = numbers<D, E4M3>(v0), z = numbers<D, E4M3>(v1);
     bool wild = false;
-    if (partial) {
+    uint32_t large = 0;
+    if constexpr (E4M3) {
 #pragma unroll
-      for (int r = 0; r < D / 8; ++r) {
-        wild = clear_wild(a.w[r]) || wild;
-        wild = clear_wild(z.w[r]) || wild;
+      for (int n = 0; n < NH; ++n) large = max(large, max(max(vs0[n] & 0xffu, vs0[n] >> 8), max(vs1[n] & 0xffu, vs1[n] >> 8)));
+    }
+    const bool two = E4M3 && __any_sync(0xffffffffu, large > 134u);
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      __nv_bfloat162 f0 = bf2(0), f1 = f0;
+      if constexpr (E4M3) {
+        f0 = factor(vs0[n] & 0xffu, vs0[n] >> 8);
+        f1 = factor(vs1[n] & 0xffu, vs1[n] >> 8);
+      }
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        uint32_t a0, a1, a2, a3;
+        if constexpr (E4M3) {
+          widen_values(transpose(word(v0[n], i)), f0, a0, a1);
+          widen_values(transpose(word(v1[n], i)), f1, a2, a3);
+          if (two) {
+            const __nv_bfloat162 h0 = factor_rest(vs0[n] & 0xffu, vs0[n] >> 8), h1 = factor_rest(vs1[n] & 0xffu, vs1[n] >> 8);
+            a0 = times(a0, h0);
+            a1 = times(a1, h0);
+            a2 = times(a2, h1);
+            a3 = times(a3, h1);
+          }
+        } else {
+          a0 = transpose(word(v0[n], 2 * i));
+          a1 = transpose(word(v0[n], 2 * i + 1));
+          a2 = transpose(word(v1[n], 2 * i));
+          a3 = transpose(word(v1[n], 2 * i + 1));
+        }
+        if (partial) {
+          wild = clear_wild(a0) || wild;
+          wild = clear_wild(a1) || wild;
+          wild = clear_wild(a2) || wild;
+          wild = clear_wild(a3) || wild;
+        }
+        mma(o[i], a0, a1, a2, a3, b0[n], b1[n]);
       }
     }
-#pragma unroll
-    for (int k2 = 0; k2 < D / 16; ++k2)
-      mma(o[k2], transpose(a.w[2 * k2]), transpose(a.w[2 * k2 + 1]), transpose(z.w[2 * k2]), transpose(z.w[2 * k2 + 1]), b0, b1);
-    v0 = fetch<D, E4M3>(c.v, c.vs, next0 + g < any_end ? next : -1, t);
-    v1 = fetch<D, E4M3>(c.v, c.vs, next0 + g + 8 < any_end ? next + 8 : -1, t);
+    load_values(next);
+    if constexpr (E4M3) load_scales(next);
     // values that are not finite, where some row may not see them: to the rows that do
     if (partial && __any_sync(0xffffffffu, wild)) {
 #pragma unroll 1
-      for (int x = 0; x < 16 && pos0 + x < any_end; ++x) {
+      for (int x = 0; x < 16 * NH; ++x) {
+        const int p = NH == 1 || x < 16 ? pos0[0] : place_of(pos0, x >> 4);
+        const int64_t row = NH == 1 || x < 16 ? at[0] : place_of(at, x >> 4);
+        if (p + (x & 15) >= any_end) continue;
 #pragma unroll
-        for (int k2 = 0; k2 < D / 16; ++k2) {
+        for (int i = 0; i < D / 16; ++i) {
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            const float y = value_at<D, E4M3>(c, at - g + x, dim_of<E4M3>(2 * k2 + half, g >> 1, g & 1));
+            const float y = value_at<D, E4M3>(c, row + (x & 15), column<E4M3>(i, half, g));
             if (isfinite(y)) continue;
 #pragma unroll
             for (int e = 0; e < 2; ++e)
-              if (pos0 + x < end[e]) o[k2][2 * half + e] += y;
+              if (p + (x & 15) < end[e]) o[i][2 * half + e] += y;
           }
         }
       }
+    }
+#pragma unroll
+    for (int n = 0; n < NH; ++n) {
+      pos0[n] = next0[n];
+      at[n] = next[n];
     }
   }
   // ---- parts into shared memory, joined
@@ -315,8 +452,8 @@ __global__ void __launch_bounds__(THREADS, 2) chosen_rows(Pool c, Seqs s, Packed
     float* to = w.part[warp][2 * t + e];
 #pragma unroll
     for (int k2 = 0; k2 < D / 16; ++k2) {
-      to[dim_of<E4M3>(2 * k2, g >> 1, g & 1)] = o[k2][e];
-      to[dim_of<E4M3>(2 * k2 + 1, g >> 1, g & 1)] = o[k2][2 + e];
+      to[column<E4M3>(k2, 0, g)] = o[k2][e];
+      to[column<E4M3>(k2, 1, g)] = o[k2][2 + e];
     }
     if (g == 0) {
       to[D] = mrun[e];
@@ -385,12 +522,14 @@ cudaError_t launch_chosen_rows(const Pool& c, const Seqs& s, const Packed& q, co
   // a cluster for each unit, as large as leaves two CTAs an SM and a warp a step or more
   int C = 1;
   const int64_t units = (int64_t)std::min(how.slots, s.rows) * blocks * c.H;   // (a tile has a row or more)
-  while (C < 8 && units * C <= n_sm && how.width * (c.page_len / 16) >= 2 * C * WARPS) C *= 2;
+  while (C < 8 && units * C <= n_sm && how.width * (c.page_len / 16) >= 16 * C) C *= 2;
   if ((int64_t)how.slots * blocks * C > 0x7fffffff) return cudaErrorInvalidValue;
   const dim3 grid(how.slots * blocks * C, c.H);
-  auto* f = c.d == 128 ? (c.e4m3 ? chosen_rows<128, true> : chosen_rows<128, false>)
-                       : (c.e4m3 ? chosen_rows<64, true> : chosen_rows<64, false>);
-  return launch_kernel(f, grid, THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks);
+  if (c.d == 128)
+    return c.e4m3 ? launch_kernel(chosen_rows<128, true>, grid, Cfg<128, true>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks)
+                  : launch_kernel(chosen_rows<128, false>, grid, Cfg<128, false>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks);
+  return c.e4m3 ? launch_kernel(chosen_rows<64, true>, grid, Cfg<64, true>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks)
+                : launch_kernel(chosen_rows<64, false>, grid, Cfg<64, false>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks);
 }
 
 }  // namespace cache

@@ -203,9 +203,9 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   const int unit = blockIdx.x / C, slot = unit / j.tiles, qt = unit - slot * j.tiles, h = blockIdx.y;
   if (blockIdx.x == 0 && h == 0)
     for (int b = tid; b < j.s.n; b += L::THREADS) seq_at(j.c, j.s, b);
-  const int b = seq_of_slot_warp(j.s, j.how.tile, slot);
-  const Seq q = seq_at(j.c, j.s, b);
-  const int i0 = (slot - first_slot(j.s, j.how.tile, b)) * j.how.tile;
+  Seq q;
+  const int b = seq_of_slot_warp(j.c, j.s, j.how.tile, slot, q);
+  const int i0 = (slot - q.r0 / j.how.tile - b) * j.how.tile;
   const int first = i0 + qt * j.TQ;                                        // its first token
   const int tokens = i0 < 0 ? 0 : min(min(j.how.tile - qt * j.TQ, j.TQ), q.n - first);
   if (tokens <= 0) return;                                                 // (the whole cluster)
