@@ -182,12 +182,14 @@ __device__ __forceinline__ uint32_t times(uint32_t x, __nv_bfloat162 f) {
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// A thread's codes of a tile: 16 bytes of rows r0, r0 + STEP, .. and their scale bytes.
+// A thread's codes of a tile: 16 bytes of rows r0, r0 + STEP, .. and their scale bytes.  Each is asked for again, for the tile
+// after, as soon as it has been used (two sets of registers did not fit: a block of 40 heads took 2,005 us; half a tile ahead
+// 658).
 template <int D>
 struct Codes {
   static constexpr int LANES = D / 16, STEP = 128 / LANES, N = 128 / STEP;   // 128 threads
   uint4 x[N];
-  uint8_t s[N];
+  uint32_t s[N];
 };
 
 template <int D, bool E4M3>
@@ -199,10 +201,12 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   cg::cluster_group cluster = cg::this_cluster();
   const int C = cluster.num_blocks(), rank = cluster.block_rank();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  // ---- the unit
+  // ---- the unit (its list's first entries are asked for before the sequence is known)
   const int unit = blockIdx.x / C, slot = unit / j.tiles, qt = unit - slot * j.tiles, h = blockIdx.y;
   if (blockIdx.x == 0 && h == 0)
     for (int b = tid; b < j.s.n; b += L::THREADS) seq_at(j.c, j.s, b);
+  const int32_t* const line = j.how.lists + ((int64_t)h * j.how.slots + slot) * j.how.width;
+  const int early = tid < j.how.width ? __ldg(line + tid) : -1, early_before = tid && tid < j.how.width ? __ldg(line + tid - 1) : -1;
   Seq q;
   const int b = seq_of_slot_warp(j.c, j.s, j.how.tile, slot, q);
   const int i0 = (slot - q.r0 / j.how.tile - b) * j.how.tile;
@@ -245,6 +249,9 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
     *wild = 0;
     bounds[0] = bounds[1] = j.how.width;
     fence_barrier_init();
+    // Q is on its way while the list is looked through
+    mbar_arrive_expect_tx(q_full, L::NP * j.TQ * j.G * 128);
+    for (int p = 0; p < L::NP; ++p) tma_load_4d(smem + L::Q + p * PANEL, &tmQ, q_full, p * 64, 0, q.r0 + first, h);
   }
   if (warp == 1) tmem_alloc(tmem_holder, TMEM_COLS);
   auto end_of = [&](int token) {
@@ -254,9 +261,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   const int all_end = end_of(0), any_end = end_of(tokens - 1);
   __syncthreads();
   {
-    const int32_t* line = j.how.lists + ((int64_t)h * j.how.slots + slot) * j.how.width;
     for (int k = tid; k < j.how.width; k += L::THREADS) {
-      const int e = __ldg(line + k), before = k ? __ldg(line + k - 1) : -1;
+      const int e = k == tid ? early : __ldg(line + k), before = k == tid ? early_before : __ldg(line + k - 1);
       int at = -1;
       if (e < 0) {
         atomicMin(bounds, k);
@@ -301,13 +307,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   if (warp < 4) {
     regs_lower<L::REGS_IO>();
     if (warp == 0) {
-      // ---------------- producer: Q, K(0), V(0), K(1), ..  It also watches the time for all roles' waits.
+      // ---------------- producer: K(0), V(0), K(1), ..  It also watches the time for all roles' waits.
       const int rows = min(j.c.page_len, BK), np = BK / rows;   // rows and boxes of a tile
-      if (n > 0 && lane == 0) {
-        mbar_arrive_expect_tx(q_full, L::NP * j.TQ * j.G * 128);
-        for (int p = 0; p < L::NP; ++p) tma_load_4d(smem + L::Q + p * PANEL, &tmQ, q_full, p * 64, 0, q.r0 + first, h);
-      }
-      __syncwarp();
       if constexpr (!E4M3) {
         const int box = lane / L::NP, panel = lane % L::NP;
         auto place = [&](int i, int& at, int& slot_in) {   // the lane's box of tile t0 + i
@@ -351,7 +352,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
       constexpr uint32_t id_s = idesc_bf16(BQ, BK), id_o = idesc_bf16(BQ, D, /*b_mn_major=*/true);
       const uint64_t qd = desc_sw128(smem_u32(smem + L::Q)), kd0 = desc_sw128(smem_u32(smem + L::K));
       const uint64_t vd0 = desc_sw128_mn(smem_u32(smem + L::V), PANEL, 1024);
-      if (n > 0) ok = mbar_wait_warp_short(q_full, 0, abort_flag);
+      ok = mbar_wait_warp_short(q_full, 0, abort_flag);   // (also where there are no keys: the copy ends before the CTA)
       for (int i = 0; ok && i < n; ++i) {
         const int sl = i % L::N;
         if (!(ok = mbar_wait_warp_short(k_full + sl, (i / L::N) & 1, abort_flag))) break;
@@ -524,63 +525,53 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
     // ---------------- codes into bf16: K(0), V(0), K(1), ..; the next tile's codes are on their way meanwhile
     using W = Codes<D>;
     const int ct = tid - 256, cl = ct % W::LANES, r0 = ct / W::LANES;
-    auto fetch = [&](bool is_k, int i, W& w) {
-      const uint8_t* pool = static_cast<const uint8_t*>(is_k ? j.c.k : j.c.v);
-      const uint8_t* scales = is_k ? j.c.ks : j.c.vs;
-#pragma unroll
-      for (int k = 0; k < W::N; ++k) {
-        const int u = (t0 + i) * BK + r0 + k * W::STEP, e = u >> j.c.page_log2;
-        const int at = i < n && e < keys.count ? page[e] : -1;
-        if (at >= 0) {
-          const int64_t row = (((int64_t)at * j.c.H + h) << j.c.page_log2) + (u & (j.c.page_len - 1));
-          w.x[k] = __ldg(reinterpret_cast<const uint4*>(pool + row * D) + cl);
-          w.s[k] = __ldg(scales + row);
-        } else {
-          w.x[k] = make_uint4(0, 0, 0, 0);
-          w.s[k] = 127;
-        }
+    const uint8_t* const kp = static_cast<const uint8_t*>(j.c.k) + cl * 16;
+    const uint8_t* const vp = static_cast<const uint8_t*>(j.c.v) + cl * 16;
+    W w;
+    auto fetch = [&](int turn, int k) {   // turn: tile * 2, values 1
+      const int u = (t0 + (turn >> 1)) * BK + r0 + k * W::STEP, e = u >> j.c.page_log2;
+      const int at = (turn >> 1) < n && e < keys.count ? page[e] : -1;
+      w.x[k] = make_uint4(0, 0, 0, 0);
+      w.s[k] = 127;
+      if (at >= 0) {
+        const int64_t row = (((int64_t)at * j.c.H + h) << j.c.page_log2) + (u & (j.c.page_len - 1));
+        w.x[k] = __ldg(reinterpret_cast<const uint4*>((turn & 1 ? vp : kp) + row * D));
+        w.s[k] = __ldg((turn & 1 ? j.c.vs : j.c.ks) + row);
       }
     };
-    auto put = [&](bool is_k, int i, const W& w) -> bool {
-      const int sl = i % L::N;
-      if (i >= L::N && !mbar_wait_warp_short((is_k ? k_empty : v_empty) + sl, (i / L::N - 1) & 1, abort_flag)) return false;
-      uint8_t* tile = smem + (is_k ? L::K : L::V) + sl * L::TB;
-      uint32_t big = 0;
+    // 16-byte chunks 2 cl and 2 cl + 1 of a row; the second panel's threads the odd one first (banks)
+    const int odd = (cl >> 2) & 1, c0 = (cl & 3) * 2;
+    uint8_t* const to = smem + (cl >> 2) * PANEL + r0 * 128;
+    const int at0 = ((c0 + odd) ^ (r0 & 7)) << 4, at1 = ((c0 + 1 - odd) ^ (r0 & 7)) << 4;   // (rows of a thread share their swizzle)
+    static_assert(W::STEP % 8 == 0, "");
 #pragma unroll
-      for (int k = 0; k < W::N; ++k) big = max(big, (uint32_t)w.s[k]);
-      const bool two = __any_sync(0xffffffffu, big > 134u);
+    for (int k = 0; k < W::N; ++k) fetch(0, k);
+#pragma unroll 1
+    for (int turn = 0; turn < 2 * n; ++turn) {
+      const bool is_k = (turn & 1) == 0;
+      const int i = turn >> 1, sl = i % L::N;
+      if (i >= L::N && !(ok = mbar_wait_warp_short((is_k ? k_empty : v_empty) + sl, (i / L::N - 1) & 1, abort_flag))) break;
+      uint8_t* const tile = to + (is_k ? L::K : L::V) + sl * L::TB;
 #pragma unroll
       for (int k = 0; k < W::N; ++k) {
         const uint32_t s = w.s[k];
         const __nv_bfloat162 f = bf2((s > 134u ? 247u : s + 120u) * 0x00800080u);
         uint2 y0 = widen(w.x[k].x, f), y1 = widen(w.x[k].y, f), y2 = widen(w.x[k].z, f), y3 = widen(w.x[k].w, f);
-        if (two) {
-          const __nv_bfloat162 f2 = bf2(s == 255u ? 0x7fff7fffu : (s > 134u ? s : 127u) * 0x00800080u);
+        if (s > 134u) {
+          const __nv_bfloat162 f2 = bf2(s == 255u ? 0x7fff7fffu : s * 0x00800080u);
           y0 = make_uint2(times(y0.x, f2), times(y0.y, f2));
           y1 = make_uint2(times(y1.x, f2), times(y1.y, f2));
           y2 = make_uint2(times(y2.x, f2), times(y2.y, f2));
           y3 = make_uint2(times(y3.x, f2), times(y3.y, f2));
         }
-        // 16-byte chunks 2 cl and 2 cl + 1 of the row; the second panel's threads the odd one first (banks)
-        const int row = r0 + k * W::STEP, p = cl >> 2, c = (cl & 3) * 2;
-        uint8_t* at = tile + p * PANEL + row * 128;
         const uint4 a = make_uint4(y0.x, y0.y, y1.x, y1.y), z = make_uint4(y2.x, y2.y, y3.x, y3.y);
-        *reinterpret_cast<uint4*>(at + (((c + (p & 1)) ^ (row & 7)) << 4)) = p & 1 ? z : a;
-        *reinterpret_cast<uint4*>(at + (((c + 1 - (p & 1)) ^ (row & 7)) << 4)) = p & 1 ? a : z;
+        *reinterpret_cast<uint4*>(tile + k * W::STEP * 128 + at0) = odd ? z : a;
+        *reinterpret_cast<uint4*>(tile + k * W::STEP * 128 + at1) = odd ? a : z;
+        fetch(turn + 1, k);
       }
       fence_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive((is_k ? k_full : v_full) + sl);
-      return true;
-    };
-    W w;
-    if (n > 0) fetch(true, 0, w);
-#pragma unroll 1
-    for (int k = 0; ok && k < 2 * n; ++k) {
-      W next;
-      fetch((k & 1) != 0, (k + 1) >> 1, next);
-      ok = put((k & 1) == 0, k >> 1, w);
-      w = next;
     }
     if (!ok && lane == 0) give_up(3);
     if (lane == 0) mbar_arrive(over);
