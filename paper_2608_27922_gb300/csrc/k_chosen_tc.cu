@@ -139,7 +139,7 @@ __device__ __noinline__ Wild wild_in(const Pool& c, const Keys& keys, int h, int
   for (int u = u0; u < u1; ++u) {
     const int p = keys.pos(u);
     if (p < 0 || p >= end) continue;
-    const int64_t at = (((int64_t)keys.page[u >> keys.log2] * c.H + h) << c.page_log2) + (p & (c.page_len - 1));
+    const int64_t page = keys.page[u >> keys.log2], at = ((E4M3 ? page : page * c.H + h) << c.page_log2) + (p & (c.page_len - 1));
     if (E4M3) {
       if (c.vs[at] == 255) w.nan = 0xffffffffu;
       continue;
@@ -168,10 +168,14 @@ __device__ __forceinline__ void prefetch_4d(const CUtensorMap* map, int x, int y
                : "memory");
 }
 
-// Four bf16 from four codes; f holds 2^120 times the scale.
+// Four bf16 from four codes (the sign spread over a byte above each, all but one of those bits cleared); f holds 2^120 times
+// the scale.
 __device__ __forceinline__ uint2 widen(uint32_t w, __nv_bfloat162 f) {
-  const uint32_t hi = (w & 0x80808080u) | ((w >> 4) & 0x07070707u), lo = (w << 4) & 0xf0f0f0f0u;
-  const uint32_t a = __byte_perm(lo, hi, 0x5140), b = __byte_perm(lo, hi, 0x7362);
+  uint32_t a, b;
+  asm("prmt.b32 %0, %1, 0, 0x9180;" : "=r"(a) : "r"(w));   // (a selector's upper bit: that byte's sign, eight times)
+  asm("prmt.b32 %0, %1, 0, 0xb3a2;" : "=r"(b) : "r"(w));
+  a = (a << 4) & 0x87f087f0u;
+  b = (b << 4) & 0x87f087f0u;
   const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), f);
   const __nv_bfloat162 y = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&b), f);
   return make_uint2(*reinterpret_cast<const uint32_t*>(&x), *reinterpret_cast<const uint32_t*>(&y));
@@ -182,12 +186,13 @@ __device__ __forceinline__ uint32_t times(uint32_t x, __nv_bfloat162 f) {
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// A thread's codes of a tile: 16 bytes of rows r0, r0 + STEP, .. and their scale bytes.  Each is asked for again, for the tile
-// after, as soon as it has been used (two sets of registers did not fit: a block of 40 heads took 2,005 us; half a tile ahead
-// 658).
+// Codes into bf16, 128 threads: eight neighbouring ones take four 16-byte parts (64 columns) of two neighbouring rows, so that
+// their stores, swizzled by the row, touch every bank once.  A thread has N such parts, rows STEP apart; each is asked for
+// again, for the tile after, as soon as it has been used.  (Two sets of registers did not fit: a block of 40 heads took 2,005 us.)
 template <int D>
 struct Codes {
-  static constexpr int LANES = D / 16, STEP = 128 / LANES, N = 128 / STEP;   // 128 threads
+  static constexpr int NP = D / 64, STEP = 32 / NP, N = 128 / STEP;
+  static_assert(STEP % 8 == 0, "a thread's rows share their swizzle");
   uint4 x[N];
   uint32_t s[N];
 };
@@ -279,7 +284,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
       }
       if (at < 0 || ((int64_t)e + 1) << j.c.page_log2 > all_end) atomicMin(bounds + 1, k);
       entry[k] = e;
-      page[k] = at;
+      page[k] = E4M3 && at >= 0 ? at * j.c.H + h : at;   // (codes: place of the head's rows; memory holds fewer than 2^31)
     }
   }
   fence_before_sync();
@@ -524,50 +529,56 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
     regs_lower<L::REGS_CONV>();
     // ---------------- codes into bf16: K(0), V(0), K(1), ..; the next tile's codes are on their way meanwhile
     using W = Codes<D>;
-    const int ct = tid - 256, cl = ct % W::LANES, r0 = ct / W::LANES;
-    const uint8_t* const kp = static_cast<const uint8_t*>(j.c.k) + cl * 16;
-    const uint8_t* const vp = static_cast<const uint8_t*>(j.c.v) + cl * 16;
+    const int ct = tid - 256, part = ct & 3, panel = (ct >> 3) % W::NP, r0 = (ct >> 3) / W::NP * 2 + ((ct >> 2) & 1);
+    const uint32_t page_bytes = (uint32_t)D << j.c.page_log2;   // of a head
+    const uint8_t* const kp = static_cast<const uint8_t*>(j.c.k) + panel * 64 + part * 16;
+    const uint8_t* const vp = static_cast<const uint8_t*>(j.c.v) + panel * 64 + part * 16;
     W w;
-    auto fetch = [&](int turn, int k) {   // turn: tile * 2, values 1
-      const int u = (t0 + (turn >> 1)) * BK + r0 + k * W::STEP, e = u >> j.c.page_log2;
-      const int at = (turn >> 1) < n && e < keys.count ? page[e] : -1;
-      w.x[k] = make_uint4(0, 0, 0, 0);
-      w.s[k] = 127;
+    // (a place behind the last, or of no page: what the registers hold stays, and is masked)
+    auto fetch = [&](const uint8_t* pool, const uint8_t* scales, int u, int k) {
+      const int e = u >> j.c.page_log2, in = u & (j.c.page_len - 1);
+      const int at = e < keys.count ? page[e] : -1;   // (page * H + head: see where it is set)
       if (at >= 0) {
-        const int64_t row = (((int64_t)at * j.c.H + h) << j.c.page_log2) + (u & (j.c.page_len - 1));
-        w.x[k] = __ldg(reinterpret_cast<const uint4*>((turn & 1 ? vp : kp) + row * D));
-        w.s[k] = __ldg((turn & 1 ? j.c.vs : j.c.ks) + row);
+        w.x[k] = __ldg(reinterpret_cast<const uint4*>(pool + (int64_t)at * page_bytes + in * D));
+        w.s[k] = __ldg(scales + ((int64_t)at << j.c.page_log2) + in);
       }
     };
-    // 16-byte chunks 2 cl and 2 cl + 1 of a row; the second panel's threads the odd one first (banks)
-    const int odd = (cl >> 2) & 1, c0 = (cl & 3) * 2;
-    uint8_t* const to = smem + (cl >> 2) * PANEL + r0 * 128;
-    const int at0 = ((c0 + odd) ^ (r0 & 7)) << 4, at1 = ((c0 + 1 - odd) ^ (r0 & 7)) << 4;   // (rows of a thread share their swizzle)
-    static_assert(W::STEP % 8 == 0, "");
+    uint8_t* const to = smem + panel * PANEL + r0 * 128;
+    const int at0 = ((2 * part) ^ (r0 & 7)) << 4, at1 = ((2 * part + 1) ^ (r0 & 7)) << 4;
 #pragma unroll
-    for (int k = 0; k < W::N; ++k) fetch(0, k);
+    for (int k = 0; k < W::N; ++k) {
+      w.x[k] = make_uint4(0, 0, 0, 0);
+      w.s[k] = 127;
+      if (n > 0) fetch(kp, j.c.ks, t0 * BK + r0 + k * W::STEP, k);
+    }
 #pragma unroll 1
     for (int turn = 0; turn < 2 * n; ++turn) {
       const bool is_k = (turn & 1) == 0;
       const int i = turn >> 1, sl = i % L::N;
       if (i >= L::N && !(ok = mbar_wait_warp_short((is_k ? k_empty : v_empty) + sl, (i / L::N - 1) & 1, abort_flag))) break;
       uint8_t* const tile = to + (is_k ? L::K : L::V) + sl * L::TB;
+      const uint8_t* const next = is_k ? vp : kp;
+      const uint8_t* const next_scales = is_k ? j.c.vs : j.c.ks;
+      const int u0 = (t0 + ((turn + 1) >> 1)) * BK + r0;
+      uint32_t big = 0;
+#pragma unroll
+      for (int k = 0; k < W::N; ++k) big = max(big, w.s[k]);
+      const bool two = __any_sync(0xffffffffu, big > 134u);
 #pragma unroll
       for (int k = 0; k < W::N; ++k) {
         const uint32_t s = w.s[k];
-        const __nv_bfloat162 f = bf2((s > 134u ? 247u : s + 120u) * 0x00800080u);
+        const __nv_bfloat162 f = bf2((two && s > 134u ? 247u : s + 120u) * 0x00800080u);
         uint2 y0 = widen(w.x[k].x, f), y1 = widen(w.x[k].y, f), y2 = widen(w.x[k].z, f), y3 = widen(w.x[k].w, f);
-        if (s > 134u) {
-          const __nv_bfloat162 f2 = bf2(s == 255u ? 0x7fff7fffu : s * 0x00800080u);
+        if (two) {
+          const __nv_bfloat162 f2 = bf2(s == 255u ? 0x7fff7fffu : (s > 134u ? s : 127u) * 0x00800080u);
           y0 = make_uint2(times(y0.x, f2), times(y0.y, f2));
           y1 = make_uint2(times(y1.x, f2), times(y1.y, f2));
           y2 = make_uint2(times(y2.x, f2), times(y2.y, f2));
           y3 = make_uint2(times(y3.x, f2), times(y3.y, f2));
         }
-        const uint4 a = make_uint4(y0.x, y0.y, y1.x, y1.y), z = make_uint4(y2.x, y2.y, y3.x, y3.y);
-        *reinterpret_cast<uint4*>(tile + k * W::STEP * 128 + at0) = odd ? z : a;
-        *reinterpret_cast<uint4*>(tile + k * W::STEP * 128 + at1) = odd ? a : z;
-        fetch(turn + 1, k);
+        *reinterpret_cast<uint4*>(tile + k * W::STEP * 128 + at0) = make_uint4(y0.x, y0.y, y1.x, y1.y);
+        *reinterpret_cast<uint4*>(tile + k * W::STEP * 128 + at1) = make_uint4(y2.x, y2.y, y3.x, y3.y);
+        fetch(next, next_scales, u0 + k * W::STEP, k);
       }
       fence_async_smem();
       __syncwarp();
