@@ -593,7 +593,7 @@ class PageTable:
 
 
 def _check_i32(t: torch.Tensor, shape, name: str, device) -> None:
-    if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name}: expected contiguous {torch.int32} {shape} on {device}, "
                          f"got {t.dtype} {tuple(t.shape)} on {t.device}")
 
@@ -607,7 +607,7 @@ def _check_32(**values) -> None:
 def _check_rows(t: torch.Tensor, heads: int, rows: int, d: int, device, name: str):
     """Strides of a packed tensor between heads and rows."""
     s = t.stride()
-    if t.dtype != torch.bfloat16 or t.shape != (heads, rows, d) or t.device != device or s[2] != 1:
+    if t.dtype is not torch.bfloat16 or t.shape != (heads, rows, d) or t.device != device or s[2] != 1:
         raise ValueError(f"{name}: expected {torch.bfloat16} {(heads, rows, d)} with contiguous rows on "
                          f"{device}, got {t.dtype} {tuple(t.shape)}, strides {s}, on {t.device}")
     return s
@@ -659,8 +659,14 @@ def norm_rope(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], how: NormRop
         z = _check_rows(y, x.shape[0], rows, how.d, device, "out")
         outs.append(y)
         args += [x.shape[0], x.data_ptr(), a[0], a[1], y.data_ptr(), z[0], z[1]]
-    with torch.cuda.device(device):
-        _check(lib().dkv_norm_rope(how.d, how._ref, coord.data_ptr(), rows, *args, raw), "dkv_norm_rope")
+    call = lib().dkv_norm_rope
+    if torch.cuda.current_device() == device.index:
+        st = call(how.d, how._ref, coord.data_ptr(), rows, *args, raw)
+    else:
+        with torch.cuda.device(device):
+            st = call(how.d, how._ref, coord.data_ptr(), rows, *args, raw)
+    if st != DKV_OK:
+        _check(st, "dkv_norm_rope")
     return tuple(outs)
 
 
@@ -881,6 +887,12 @@ class PagedCache:
         _check_i32(refs, (self.n_pages,), "refs", self.device)
         return refs.data_ptr()
 
+    def _scratch(self, call: str, n_seq: int) -> int:
+        size = self._plans.get((call, n_seq))
+        if size is None:
+            size = self._keep_plan((call, n_seq), int(getattr(lib(), f"dkv_cache_{call}_scratch_size")(self.handle, n_seq)))
+        return size
+
     def fork(self, refs: torch.Tensor, src: PageTable, parent: torch.Tensor, dst: PageTable, stream=None) -> None:
         """Sequence i of dst goes on from sequence parent[i] (int32, -1: empty) of src, sharing its pages; src is given up."""
         _check_i32(parent, (dst.n_seq,), "parent", self.device)
@@ -893,8 +905,9 @@ class PagedCache:
         """Room for add[b] (int32) more positions of every sequence: pages, lengths, and a copy of a shared last page."""
         _check_i32(add, (seqs.n_seq,), "add", self.device)
         s, ctx = self._on(stream)
-        scratch = self._new(ctx, int(lib().dkv_cache_extend_scratch_size(self.handle, seqs.n_seq)), torch.uint8)
-        st = self._extend(self.handle, self._refs(refs), self._table(seqs), add.data_ptr(), scratch.data_ptr(), scratch.numel(), s)
+        size = self._scratch("extend", seqs.n_seq)
+        scratch = self._new(ctx, size, torch.uint8)
+        st = self._extend(self.handle, self._refs(refs), self._table(seqs), add.data_ptr(), scratch.data_ptr(), size, s)
         if st != DKV_OK:
             _check(st, "dkv_cache_extend")
 
@@ -913,9 +926,10 @@ class PagedCache:
         _check_i32(keep, (keep.numel(),), "keep", self.device)
         _check_i32(keep_start, (src.n_seq + 1,), "keep_start", self.device)
         s, ctx = self._on(stream)
-        scratch = self._new(ctx, int(lib().dkv_cache_compact_scratch_size(self.handle, src.n_seq)), torch.uint8)
+        size = self._scratch("compact", src.n_seq)
+        scratch = self._new(ctx, size, torch.uint8)
         st = self._compact(self.handle, self._refs(refs), self._table(src), keep.data_ptr(), keep.numel(), keep_start.data_ptr(),
-                           self._table(dst), scratch.data_ptr(), scratch.numel(), s)
+                           self._table(dst), scratch.data_ptr(), size, s)
         if st != DKV_OK:
             _check(st, "dkv_cache_compact")
 
