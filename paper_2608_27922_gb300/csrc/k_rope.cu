@@ -2,7 +2,8 @@
 //
 // For a row x of d values: y = x w rsqrt(mean x^2 + eps), and each pair of y turned by its token's angle.  Every
 // byte moves once, so HBM bounds large calls and the launch small ones.  A row lies with d / 16 neighbouring
-// threads, 16 values each, the two elements of every pair in one thread (interleaved: 16 in a row; halves: 8 and 8).
+// threads, thread l's 16 values being 8 l .. and d / 2 + 8 l ..: both elements of every pair, whichever the layout, and
+// 16-byte accesses side by side.
 // A thread keeps its token: the angles' sines and cosines are worked out once and serve all the heads that
 // it walks over, whose rows come in one head ahead of their use.
 //
@@ -20,6 +21,7 @@ namespace cache {
 namespace {
 
 constexpr int THREADS = 256;
+constexpr int BLOCKS = 4;   // of an SM: 64 registers a thread (a block of 40 heads 55 us; with 3 of 80 registers 64)
 enum { DENSE = 0, PAGES_BF16 = 1, PAGES_E4M3 = 2 };
 
 struct Tensors {
@@ -37,24 +39,30 @@ __device__ __forceinline__ uint32_t pack(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-template <bool HALF>
 __device__ __forceinline__ Vals load_row(const Packed& t, int h, int row, int lane, int d) {
-  const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(t.p) + h * t.head + row * t.row;
   // (ordinary loads: an output may be its input)
-  const uint4* a = reinterpret_cast<const uint4*>(p + lane * (HALF ? 8 : 16));
-  return Vals{__ldcs(a), __ldcs(HALF ? reinterpret_cast<const uint4*>(p + d / 2 + lane * 8) : a + 1)};
+  const uint4* p = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(t.p) + h * t.head + row * t.row);
+  return Vals{__ldcs(p + lane), __ldcs(p + d / 16 + lane)};
 }
 
-template <bool HALF>
 __device__ __forceinline__ void store_row(__nv_bfloat16* p, const Vals& x, int lane, int d) {
-  uint4* a = reinterpret_cast<uint4*>(p + lane * (HALF ? 8 : 16));
-  a[0] = x.a;
-  *reinterpret_cast<uint4*>(HALF ? p + d / 2 + lane * 8 : reinterpret_cast<__nv_bfloat16*>(a + 1)) = x.b;
+  reinterpret_cast<uint4*>(p)[lane] = x.a;
+  reinterpret_cast<uint4*>(p)[d / 16 + lane] = x.b;
 }
 
-// The 16 values normed (w: the thread's weights in shared memory, ones where there are none) and rotated.
+// Of thread l: the rotation pair of its values 2 i and 2 i + 1, and the element that value m is.
 template <int D, bool HALF>
-__device__ __forceinline__ Vals turned(const Vals& x, const float* w, bool norm, float eps, const float (&cs)[8],
+__device__ __forceinline__ int pair_index(int l, int i) {
+  return HALF ? l * 8 + i : (i >> 2) * (D / 4) + l * 4 + (i & 3);
+}
+template <int D, bool HALF>
+__device__ __forceinline__ int element(int l, int m) {
+  return HALF ? (m & 1) * (D / 2) + l * 8 + (m >> 1) : (m >> 3) * (D / 2) + l * 8 + (m & 7);
+}
+
+// The 16 values normed (w: four of the thread's weights every D / 16 places, ones where there are none) and rotated.
+template <int D, bool HALF>
+__device__ __forceinline__ Vals turned(const Vals& x, const float4* w, bool norm, float eps, const float (&cs)[8],
                                        const float (&sn)[8]) {
   constexpr int LANES = D / 16;
   float v[16];   // pair i: v[2 i], v[2 i + 1]
@@ -90,7 +98,7 @@ __device__ __forceinline__ Vals turned(const Vals& x, const float* w, bool norm,
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const float4 f = reinterpret_cast<const float4*>(w)[k];
+      const float4 f = w[k * LANES];
       v[4 * k] *= r * f.x; v[4 * k + 1] *= r * f.y; v[4 * k + 2] *= r * f.z; v[4 * k + 3] *= r * f.w;
     }
   }
@@ -112,21 +120,20 @@ __device__ __forceinline__ Vals turned(const Vals& x, const float* w, bool norm,
 }
 
 template <int D, bool HALF, int MODE>
-__global__ void __launch_bounds__(THREADS) norm_rope(Pool c, Seqs s, const __grid_constant__ RopeHow how,
+__global__ void __launch_bounds__(THREADS, BLOCKS) norm_rope(Pool c, Seqs s, const __grid_constant__ RopeHow how,
                                                      const __grid_constant__ Tensors t) {
   constexpr int LANES = D / 16, SLOTS = THREADS / LANES;
   __shared__ int64_t turns[D / 2];
-  __shared__ float weights[2][D];   // in the order of a thread's pairs
+  __shared__ float4 weights[2][D / 4];   // four values of all threads, then the next four (side by side: no bank twice)
   if (threadIdx.x < D / 2) {
     double f = (double)how.theta[threadIdx.x] * 0.15915494309189533577;   // 1 / (2 pi)
     f -= rint(f);
     turns[threadIdx.x] = __double2ll_rn(f * 18446744073709551616.0);
   }
   for (int e = threadIdx.x; e < 2 * D; e += THREADS) {
-    const int k = e % D, lane = k >> 4, i = k & 15;
-    const int at = HALF ? lane * 8 + (i >> 1) + (i & 1) * (D / 2) : k;
+    const int k = e % D, l = (k >> 2) % LANES, m = (k >> 2) / LANES * 4 + (k & 3);
     const float* w = e < D ? how.q_weight : how.k_weight;
-    weights[e / D][k] = w ? w[at] : 1.0f;
+    reinterpret_cast<float*>(weights[e / D])[k] = w ? w[element<D, HALF>(l, m)] : 1.0f;
   }
   if (MODE != DENSE && blockIdx.x == 0 && blockIdx.y == 0)
     for (int b = threadIdx.x; b < s.n; b += THREADS) seq_at(c, s, b);
@@ -150,7 +157,7 @@ __global__ void __launch_bounds__(THREADS) norm_rope(Pool c, Seqs s, const __gri
   float cs[8], sn[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
-    const int j = lane * 8 + i;
+    const int j = pair_index<D, HALF>(lane, i);
     int a = 0;
     for (int k = 0; k < 3; ++k) a += j >= how.pair_end[k];   // (ends past the last axis' are d / 2)
     const int x = !on ? 0 : how.coord ? __ldg(how.coord + (int64_t)a * s.rows + row) : pos;
@@ -161,9 +168,9 @@ __global__ void __launch_bounds__(THREADS) norm_rope(Pool c, Seqs s, const __gri
   const int end = min(heads, ((int)blockIdx.y + 1) * t.per);
   int h = blockIdx.y * t.per + (slot >> t.rows_log2);
   auto load = [&](int i) -> Vals {
-    if (i < t.Hq) return load_row<HALF>(t.q, i, row, lane, D);
-    if (MODE == DENSE || i < t.Hq + t.Hk) return load_row<HALF>(t.k, i - t.Hq, row, lane, D);
-    return load_row<false>(t.v, i - t.Hq - t.Hk, row, lane, D);
+    if (i < t.Hq) return load_row(t.q, i, row, lane, D);
+    if (MODE == DENSE || i < t.Hq + t.Hk) return load_row(t.k, i - t.Hq, row, lane, D);
+    return load_row(t.v, i - t.Hq - t.Hk, row, lane, D);
   };
   Vals next{};
   if (on && h < end) next = load(h);
@@ -175,13 +182,13 @@ __global__ void __launch_bounds__(THREADS) norm_rope(Pool c, Seqs s, const __gri
     if (on && h + step < end) next = load(h + step);
     const bool value = MODE != DENSE && h >= t.Hq + t.Hk, query = h < t.Hq;
     if (MODE == DENSE || !__all_sync(0xffffffffu, value)) {
-      const Vals y = turned<D, HALF>(x, weights[query ? 0 : 1] + lane * 16, how.norm != 0, how.eps, cs, sn);
+      const Vals y = turned<D, HALF>(x, weights[query ? 0 : 1] + lane, how.norm != 0, how.eps, cs, sn);
       if (!value) x = y;
     }
     if (MODE == DENSE || query) {
       if (mine) {
         const Packed& o = query ? t.qo : t.ko;
-        store_row<HALF>(static_cast<__nv_bfloat16*>(o.p) + (query ? h : h - t.Hq) * o.head + row * o.row, x, lane, D);
+        store_row(static_cast<__nv_bfloat16*>(o.p) + (query ? h : h - t.Hq) * o.head + row * o.row, x, lane, D);
       }
       if (MODE != PAGES_E4M3) continue;   // (whole warps stay together for the codes' shuffles)
     }
@@ -191,23 +198,14 @@ __global__ void __launch_bounds__(THREADS) norm_rope(Pool c, Seqs s, const __gri
     const int64_t to = at + ((int64_t)hk << c.page_log2);
     if (MODE == PAGES_BF16) {
       if (!keep) continue;
-      __nv_bfloat16* p = static_cast<__nv_bfloat16*>(value ? c.v : c.k) + to * D;
-      if (value) {
-        store_wide(p + lane * 16, x);
-      } else {
-        store_row<HALF>(p, x, lane, D);
-      }
+      store_row(static_cast<__nv_bfloat16*>(value ? c.v : c.k) + to * D, x, lane, D);
     } else {
       uint8_t byte;
       const uint4 codes = codes_e4m3<LANES>(x, byte);
       if (!keep) continue;
       uint8_t* p = static_cast<uint8_t*>(value ? c.v : c.k) + to * D;
-      if (value || !HALF) {
-        *reinterpret_cast<uint4*>(p + lane * 16) = codes;
-      } else {
-        *reinterpret_cast<uint2*>(p + lane * 8) = make_uint2(codes.x, codes.y);
-        *reinterpret_cast<uint2*>(p + D / 2 + lane * 8) = make_uint2(codes.z, codes.w);
-      }
+      *reinterpret_cast<uint2*>(p + lane * 8) = make_uint2(codes.x, codes.y);
+      *reinterpret_cast<uint2*>(p + D / 2 + lane * 8) = make_uint2(codes.z, codes.w);
       if (lane == 0) (value ? c.vs : c.ks)[to] = byte;
     }
   }
@@ -228,8 +226,9 @@ cudaError_t launch_norm_rope(const Pool& c, const Seqs& s, bool dense, const Rop
   Tensors t{q, qo, k, ko, v, Hq, Hk, 0, 0};
   while ((1 << t.rows_log2) < std::min(s.rows, slots)) ++t.rows_log2;
   const int groups = (s.rows + (1 << t.rows_log2) - 1) >> t.rows_log2, step = slots >> t.rows_log2;
-  // heads of a block: as many as leave every SM four blocks
-  t.per = std::max(1, heads / std::max(1, 4 * n_sm / groups));
+  // heads of a block: so many that all blocks run at once (a frame of 32 heads of 64: two heads a block 8.3 us, one 10.4)
+  const int64_t room = (int64_t)BLOCKS * n_sm;
+  t.per = (int)(((int64_t)heads * groups + room - 1) / room);
   t.per = (t.per + step - 1) / step * step;
   const dim3 grid(groups, (heads + t.per - 1) / t.per);
   auto* f = c.d == 128 ? (how.half ? pick<128, true>(mode) : pick<128, false>(mode))
