@@ -20,7 +20,7 @@ namespace cache {
 namespace {
 
 constexpr int PLANNERS = 8;       // CTAs that plan a call on a large pool
-constexpr int PLAN_THREADS = 1024;
+constexpr int PLAN_THREADS = 512;
 constexpr int MAX_SEQS = 4096;
 constexpr int COPY_THREADS = 256;
 
@@ -99,43 +99,34 @@ __global__ void __launch_bounds__(128) cache_release(Pool c, int32_t* refs, Tabl
 }
 
 // ------------------------------------------------------------------ fresh pages
-// Inclusive sums over the block of two numbers; part: 32 of each.
-struct Pair {
-  int64_t a, b;
-};
-__device__ __forceinline__ Pair block_sums(Pair x, Pair* part) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t a = __shfl_up_sync(0xffffffffu, x.a, o), b = __shfl_up_sync(0xffffffffu, x.b, o);
-    if (lane >= o) x.a += a, x.b += b;
-  }
-  if (lane == 31) part[warp] = x;
-  __syncthreads();
-  Pair y = part[lane];   // (of PLAN_THREADS / 32 = 32 warps)
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t a = __shfl_up_sync(0xffffffffu, y.a, o), b = __shfl_up_sync(0xffffffffu, y.b, o);
-    if (lane >= o) y.a += a, y.b += b;
-  }
-  const int before = max(warp - 1, 0);
-  const int64_t a = __shfl_sync(0xffffffffu, y.a, before), b = __shfl_sync(0xffffffffu, y.b, before);
-  if (warp) x.a += a, x.b += b;
-  return x;
-}
-
-constexpr int OWN = MAX_SEQS / PLAN_THREADS;   // sequences of a thread at most, one behind the other
-__device__ __forceinline__ int own_of(int n_seq) { return (n_seq + PLAN_THREADS - 1) / PLAN_THREADS; }
-
+// (Short loops, not unrolled: these kernels are one CTA that runs its instructions once or twice, and fetching them is much of
+// what they cost.)
 struct Planner {
-  Pair part[32];
+  int part[32];
+  int base;                // fresh pages of the chunks of sequences before
   int64_t need, counted;   // fresh pages asked for; free pages of this CTA's part
   int fault;               // of this CTA: site, 0 none
   int before[MAX_SEQS];    // fresh pages of the sequences before (where the sum is no more than there are)
   int k0[MAX_SEQS];        // the entry that a sequence's first one is for
+  int fresh[MAX_SEQS];     // how many it asks for
   alignas(16) int held[MAX_SEQS];   // extend: the shared page that the sequence's new positions begin on, -1
-  int given[MAX_SEQS];     // extend, in the cluster's first CTA: the page that takes its place
+  int given[MAX_SEQS];     // extend: how many hold that page; then, in the cluster's first CTA, the page that takes its place
 };
+
+// Inclusive sum over the block.
+__device__ __forceinline__ int block_sum(int x, int* part) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int a = __shfl_up_sync(0xffffffffu, x, o);
+    if (lane >= o) x += a;
+  }
+  __syncthreads();
+  if (lane == 31) part[warp] = x;
+  __syncthreads();
+  const int y = lane < warp ? part[lane] : 0;
+  return x + __reduce_add_sync(0xffffffffu, y);
+}
 
 // A thread's run of refs: per pages from p0 on.
 __device__ __forceinline__ int free4(const int32_t* refs, int64_t p, int64_t end) {
@@ -149,7 +140,7 @@ __device__ __forceinline__ int free4(const int32_t* refs, int64_t p, int64_t end
 }
 struct Run {
   int64_t p0, p1;
-  int64_t free;   // free pages in it
+  int free;   // free pages in it
 };
 __device__ __forceinline__ Run count_free(const Pool& c, const int32_t* refs, int ctas, int rank) {
   const int64_t threads = (int64_t)ctas * PLAN_THREADS, per = ((c.n_pages + threads - 1) / threads + 3) / 4 * 4;
@@ -162,32 +153,30 @@ __device__ __forceinline__ Run count_free(const Pool& c, const int32_t* refs, in
   return r;
 }
 
-// All CTAs of a cluster: what the sequences ask for summed up (thread t has the k0 and number of fresh pages of its OWN
-// sequences), the free pages likewise, and if all is well each fresh page to whom it is due: give(b, k, page).
-// False: nothing was given.  Every read of what a plan goes by lies before the cluster's first barrier here.
+// All CTAs of a cluster: what the sequences ask for (k0, fresh) summed up, the free pages likewise, and if all is well each fresh
+// page to whom it is due: give(b, k, page).  False: nothing was given.  Every read of what a plan goes by lies
+// before the cluster's first barrier here.
 template <typename Give>
-__device__ __forceinline__ bool give_pages(const Pool& c, int32_t* refs, int n_seq, Planner& m, const Run& run, const int (&k0)[OWN],
-                                           const int (&fresh)[OWN], Give give) {
+__device__ __forceinline__ bool give_pages(const Pool& c, int32_t* refs, int n_seq, Planner& m, const Run& run, Give give) {
   cg::cluster_group cluster = cg::this_cluster();
-  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), own = own_of(n_seq);
-  int64_t asked = 0;
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) asked += fresh[i];
-  const Pair sums = block_sums(Pair{asked, run.free}, m.part);
-  int64_t at = sums.a - asked;
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) {
-    const int b = threadIdx.x * own + i;
-    if (i >= own || b >= n_seq) break;
-    m.before[b] = (int)min(at, (int64_t)0x7fffffff);
-    m.k0[b] = k0[i];
-    at += fresh[i];
+  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), tid = threadIdx.x;
+  if (tid == 0) {
+    m.base = 0;
+    m.need = 0;
   }
-  if (threadIdx.x == PLAN_THREADS - 1) {
-    m.need = sums.a;
-    m.counted = sums.b;
+#pragma unroll 1
+  for (int b0 = 0; b0 < n_seq; b0 += PLAN_THREADS) {
+    const int b = b0 + tid, x = b < n_seq ? m.fresh[b] : 0;
+    const int incl = block_sum(x, m.part);   // (wraps only where the 64-bit sum below says that there are too few pages)
+    if (b < n_seq) m.before[b] = m.base + incl - x;
+    const int lo = __reduce_add_sync(0xffffffffu, x & 0xffff), hi = __reduce_add_sync(0xffffffffu, (int)((unsigned)x >> 16));
+    if (tid % 32 == 0) atomicAdd(reinterpret_cast<unsigned long long*>(&m.need), ((unsigned long long)hi << 16) + lo);
+    __syncthreads();
+    if (tid == PLAN_THREADS - 1) m.base += incl;
   }
-  int64_t first = sums.b - run.free, total = 0;
+  const int upto = block_sum(run.free, m.part);
+  if (tid == PLAN_THREADS - 1) m.counted = upto;
+  int64_t first = upto - run.free, total = 0;
   int fault = 0;
   if (ctas == 1) {
     __syncthreads();
@@ -195,6 +184,7 @@ __device__ __forceinline__ bool give_pages(const Pool& c, int32_t* refs, int n_s
     fault = m.fault;
   } else {
     cluster.sync();
+#pragma unroll 1
     for (int r = 0; r < ctas; ++r) {
       const Planner* o = cluster.map_shared_rank(&m, r);
       const int64_t x = o->counted;
@@ -206,31 +196,28 @@ __device__ __forceinline__ bool give_pages(const Pool& c, int32_t* refs, int n_s
   }
   const int64_t need = m.need;
   if (fault || need > total) {
-    if (rank == 0 && threadIdx.x == 0) {
-      if (fault) fail(c.status, DEV_INCONSISTENT, fault);
-      else fail(c.status, DEV_NO_PAGES, SITE_PAGE);
-    }
+    if (rank == 0 && tid == 0) fail(c.status, fault ? DEV_INCONSISTENT : DEV_NO_PAGES, fault ? fault : SITE_PAGE);
     return false;
   }
   if (run.free == 0) return true;
+#pragma unroll 1
   for (int64_t p = run.p0; p < run.p1 && first < need; p += 4) {
-    const int f = free4(refs, p, run.p1);
-    for (int i = 0; i < 4; ++i) {
-      if (!((f >> i) & 1) || first >= need) continue;
+#pragma unroll 1
+    for (int f = free4(refs, p, run.p1); f && first < need; f &= f - 1, ++first) {
+      const int at = (int)p + __ffs(f) - 1;
       int lo = 0, hi = n_seq;   // the last sequence with before <= first: one that asks for some
       while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (m.before[mid] <= first) lo = mid; else hi = mid;
       }
-      refs[p + i] = 1;
-      give(lo, m.k0[lo] + (int)(first - m.before[lo]), (int)(p + i));
-      ++first;
+      refs[at] = 1;
+      give(lo, m.k0[lo] + (int)first - m.before[lo], at);
     }
   }
   return true;
 }
 
-// One CTA plans for small pools, a cluster for large ones (32,768 pages: 32 pages a thread).
+// One CTA plans for small pools, a cluster for large ones (32,768 pages: 64 pages a thread).
 constexpr int ALONE_MOST = 32768;
 int planners(const Pool& c) { return c.n_pages <= ALONE_MOST ? 1 : PLANNERS; }
 
@@ -244,103 +231,96 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) extend_plan(Pool c, int32_t* 
   extern __shared__ __align__(16) uint8_t raw[];
   Planner& m = *reinterpret_cast<Planner*>(raw);
   cg::cluster_group cluster = cg::this_cluster();
-  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), own = own_of(s.n);
+  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), tid = threadIdx.x;
   pdl_trigger();
   const Run run = count_free(c, refs, ctas, rank);
-  if (threadIdx.x == 0) m.fault = 0;
-  for (int b = threadIdx.x; b < s.n + 3; b += PLAN_THREADS)
-    if (b < MAX_SEQS) m.held[b] = -1;
+  if (tid == 0) m.fault = 0;
   __syncthreads();
   const int64_t cap = (int64_t)s.max_pages << c.page_log2;
-  int k0[OWN], fresh[OWN], len[OWN], more[OWN], page[OWN], count[OWN];
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) {
-    const int b = threadIdx.x * own + i;
-    k0[i] = fresh[i] = len[i] = more[i] = count[i] = 0;
-    page[i] = -1;
-    if (i >= own || b >= s.n) continue;
-    len[i] = s.len[b];
-    more[i] = add[b];
-    if (len[i] < 0 || len[i] > cap || more[i] < 0 || (int64_t)len[i] + more[i] > cap) {
+  bool any_long = false, any_shared = false;
+#pragma unroll 1
+  for (int b = tid; b < (s.n + 3) / 4 * 4; b += PLAN_THREADS) {
+    int k0 = 0, fresh = 0, held = -1, count = 0;
+    const int len = b < s.n ? s.len[b] : 0, more = b < s.n ? add[b] : 0;
+    if (len < 0 || len > cap || more < 0 || (int64_t)len + more > cap) {
       m.fault = SITE_LEN;
-      more[i] = 0;
+    } else if (more) {
+      const int32_t* row = s.table + (int64_t)b * s.max_pages;
+      k0 = pages_of(c, len);
+      fresh = pages_of(c, len + more) - k0;
+      if (len & (c.page_len - 1)) {
+        const int page = row[k0 - 1];
+        if (!in_pool(c, page)) {
+          m.fault = SITE_PAGE;
+        } else {
+          count = refs[page];
+          if (count < 1) m.fault = SITE_REFS;
+          if (count > 1) held = page;
+        }
+      }
+      // the entries that pages are to go to hold none (the many of a long growth: below)
+      for (int k = 0; k < min(fresh, 4); ++k)
+        if (row[k0 + k] >= 0) m.fault = SITE_PAGE;
+      any_long = any_long || fresh > 4;
     }
-    if (more[i] == 0) continue;
-    k0[i] = pages_of(c, len[i]);
-    fresh[i] = pages_of(c, len[i] + more[i]) - k0[i];
-    const int32_t* row = s.table + (int64_t)b * s.max_pages;
-    if (len[i] & (c.page_len - 1)) {
-      page[i] = row[k0[i] - 1];
-      if (!in_pool(c, page[i])) {
-        m.fault = SITE_PAGE;
-        page[i] = -1;
+    m.k0[b] = k0;
+    m.fresh[b] = fresh;
+    m.held[b] = held;
+    m.given[b] = count;
+    any_shared = any_shared || held >= 0;
+  }
+  any_shared = __syncthreads_or(any_shared);
+  if (__syncthreads_or(any_long)) {   // a warp a sequence, the cluster's CTAs taking turns
+#pragma unroll 1
+    for (int b = rank + ctas * (tid >> 5); b < s.n; b += ctas * (PLAN_THREADS / 32))
+      for (int k = m.k0[b] + 4 + (tid & 31); k < m.k0[b] + m.fresh[b]; k += 32)
+        if (s.table[(int64_t)b * s.max_pages + k] >= 0) m.fault = SITE_PAGE;
+    __syncthreads();
+  }
+  // A shared page: the last of its sequences keeps it, if nobody else holds it.
+  if (any_shared) {
+#pragma unroll 1
+    for (int b = tid; b < s.n; b += PLAN_THREADS) {
+      const int page = m.held[b];
+      if (page < 0) continue;
+      int holders = 0, last = b;
+#pragma unroll 4
+      for (int k = 0; k < (s.n + 3) / 4; ++k) {
+        const int4 x = reinterpret_cast<const int4*>(m.held)[k];
+        holders += (x.x == page) + (x.y == page) + (x.z == page) + (x.w == page);
+        last = x.w == page ? 4 * k + 3 : x.z == page ? 4 * k + 2 : x.y == page ? 4 * k + 1 : x.x == page ? 4 * k : last;
+      }
+      if (holders > m.given[b]) m.fault = SITE_REFS;
+      if (holders == m.given[b] && last == b) {
+        m.given[b] = 0;   // stays
+      } else {
+        --m.k0[b];
+        ++m.fresh[b];
       }
     }
-    // the entries that pages are to go to hold none (the many of a long growth: below)
-    for (int k = 0; k < min(fresh[i], 4); ++k)
-      if (row[k0[i] + k] >= 0) m.fault = SITE_PAGE;
+    __syncthreads();
   }
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) {
-    if (page[i] < 0) continue;
-    count[i] = refs[page[i]];
-    if (count[i] < 1) m.fault = SITE_REFS;
-    if (count[i] > 1) m.held[threadIdx.x * own + i] = page[i];
-  }
-  // (a warp looks through its lanes' long growths together)
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) {
-    for (unsigned who = __ballot_sync(0xffffffffu, fresh[i] > 4); who; who &= who - 1) {
-      const int src = __ffs(who) - 1;
-      const int b = ((threadIdx.x & ~31) + src) * own + i, a = __shfl_sync(0xffffffffu, k0[i], src), n = __shfl_sync(0xffffffffu, fresh[i], src);
-      for (int k = a + 4 + (threadIdx.x & 31); k < a + n; k += 32)
-        if (s.table[(int64_t)b * s.max_pages + k] >= 0) m.fault = SITE_PAGE;
-    }
-  }
-  __syncthreads();
-  // A shared page: the last of its sequences keeps it, if nobody else holds it.
-  bool moved[OWN];
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) {
-    moved[i] = false;
-    if (count[i] <= 1) continue;
-    const int b = threadIdx.x * own + i;
-    int holders = 0, last = b;
-    for (int k = 0; k < (s.n + 3) / 4; ++k) {
-      const int4 x = reinterpret_cast<const int4*>(m.held)[k];
-      if (x.x == page[i]) ++holders, last = max(last, 4 * k);
-      if (x.y == page[i]) ++holders, last = max(last, 4 * k + 1);
-      if (x.z == page[i]) ++holders, last = max(last, 4 * k + 2);
-      if (x.w == page[i]) ++holders, last = max(last, 4 * k + 3);
-    }
-    if (holders > count[i]) m.fault = SITE_REFS;
-    if (holders == count[i] && last == b) continue;
-    moved[i] = true;
-    --k0[i];
-    ++fresh[i];
-  }
-  __syncthreads();
   int* given = cluster.map_shared_rank(m.given, 0);
-  const bool ok = give_pages(c, refs, s.n, m, run, k0, fresh, [&](int b, int k, int p) {
+  const bool ok = give_pages(c, refs, s.n, m, run, [&](int b, int k, int p) {
     s.table[(int64_t)b * s.max_pages + k] = p;
-    if (k == m.k0[b]) given[b] = p;
+    if (k == m.k0[b] && m.held[b] >= 0 && m.given[b] != 0) given[b] = ~p;   // (counts are positive)
   });
   if (ctas == 1) __syncthreads();
   else cluster.sync();   // (the first CTA has all pages given)
   if (rank) return;
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) {
-    const int b = threadIdx.x * own + i;
-    if (i >= own || b >= s.n) break;
-    Move v{0, 0, 0, 0};
-    if (ok && more[i] > 0) {
-      s.len[b] = len[i] + more[i];
-      if (moved[i]) {
-        v = Move{page[i], m.given[b], len[i] & (c.page_len - 1), 0};
-        atomicSub(refs + page[i], 1);
+#pragma unroll 1
+  for (int b = tid; b < s.n; b += PLAN_THREADS) {
+    int4 v = make_int4(0, 0, 0, 0);
+    const int more = add[b];
+    if (ok && more > 0) {
+      const int len = s.len[b];
+      s.len[b] = len + more;
+      if (m.given[b] < 0) {
+        v = make_int4(m.held[b], ~m.given[b], len & (c.page_len - 1), 0);
+        atomicSub(refs + v.x, 1);
       }
     }
-    *reinterpret_cast<int4*>(moves + b) = make_int4(v.src, v.dst, v.rows, 0);
+    *reinterpret_cast<int4*>(moves + b) = v;
   }
 }
 
@@ -434,39 +414,26 @@ __global__ void __launch_bounds__(PLAN_THREADS, 1) compact_plan(Pool c, int32_t*
   extern __shared__ __align__(16) uint8_t raw[];
   Planner& m = *reinterpret_cast<Planner*>(raw);
   cg::cluster_group cluster = cg::this_cluster();
-  const int rank = cluster.block_rank(), ctas = cluster.num_blocks(), own = own_of(from.n);
+  const int rank = cluster.block_rank(), ctas = cluster.num_blocks();
   const Run run = count_free(c, refs, ctas, rank);   // (the kernel before this one does not change them)
   if (threadIdx.x == 0) m.fault = 0;
   __syncthreads();
   pdl_wait();
   pdl_trigger();
-  int k0[OWN], fresh[OWN];
-#pragma unroll
-  for (int i = 0; i < OWN; ++i) {
-    const int b = threadIdx.x * own + i;
-    k0[i] = fresh[i] = 0;
-    if (i >= own || b >= from.n) continue;
+#pragma unroll 1
+  for (int b = threadIdx.x; b < from.n; b += PLAN_THREADS) {
     const int n = keep_start[b + 1] - keep_start[b], all = pages_of(c, n);
     int stay = 0x7fffffff;
-#pragma unroll 8
+#pragma unroll 4
     for (int x = 0; x < parts; ++x) stay = min(stay, same[(int64_t)b * parts + x]);
-    if (stay < 0) {
-      m.fault = -stay;
-      continue;
-    }
-    k0[i] = stay == n ? all : stay >> c.page_log2;
-    fresh[i] = all - k0[i];
+    if (stay < 0) m.fault = -stay;
+    m.k0[b] = stay < 0 ? 0 : stay == n ? all : stay >> c.page_log2;
+    m.fresh[b] = stay < 0 ? 0 : all - m.k0[b];
   }
   __syncthreads();
-  const bool ok = give_pages(c, refs, from.n, m, run, k0, fresh,
-                             [&](int b, int k, int p) { to.table[(int64_t)b * to.max_pages + k] = p; });
-  if (rank == 0) {
-#pragma unroll
-    for (int i = 0; i < OWN; ++i) {
-      const int b = threadIdx.x * own + i;
-      if (i < own && b < from.n) kept[b] = ok ? k0[i] : -1;
-    }
-  }
+  const bool ok = give_pages(c, refs, from.n, m, run, [&](int b, int k, int p) { to.table[(int64_t)b * to.max_pages + k] = p; });
+  if (rank == 0)
+    for (int b = threadIdx.x; b < from.n; b += PLAN_THREADS) kept[b] = ok ? m.k0[b] : -1;
 }
 
 // Block x: rows [x % groups * MOVE_ROWS, ..) of keep, head x / groups; behind those, one block a sequence, the tables and counts (the
