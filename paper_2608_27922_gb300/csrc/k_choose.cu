@@ -59,23 +59,43 @@ __device__ __forceinline__ void add(Two& s, const Two& y) {
   s.lo = __fadd_rn(s.lo, y.lo);
 }
 
-// Block: pages of one sequence (blockIdx.y), each with one head, in turn.  A row lies with d / 8 threads; the rows' sums
+// Units, a page and a head each, one sequence's behind the other's, go round the blocks (so many that all run at once; which
+// sequence a unit is of, every warp finds from 32 sequences at a time).  A row lies with d / 8 threads; the rows' sums
 // go over the warp, then one thread a column joins the warps'.
+constexpr int SUM_BLOCKS = 6;   // of an SM
+
 template <int D, bool E4M3>
-__global__ void __launch_bounds__(SUM_THREADS) summarise(Pool c, Seqs s, const int32_t* first, int8_t* code, uint8_t* scale) {
+__global__ void __launch_bounds__(SUM_THREADS, SUM_BLOCKS) summarise(Pool c, Seqs s, const int32_t* first, int8_t* code, uint8_t* scale) {
   constexpr int LANES = D / 8, ROWS = SUM_THREADS / LANES, WARPS = SUM_THREADS / 32;
   __shared__ Two part[WARPS][D];
   __shared__ float tops[D / 32];
-  const int b = blockIdx.y, tid = threadIdx.x, lane = tid % LANES, r0 = tid / LANES;
-  const Seq q = seq_at(c, s, b);
-  const int from = max(first ? first[b] : q.len - q.n, 0) >> c.page_log2, pages = (q.len + c.page_len - 1) >> c.page_log2;
-  if (!first && q.n == 0) return;
-  const int64_t units = (int64_t)max(pages - from, 0) * c.H;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int h = (int)(u % c.H), k = from + (int)(u / c.H);
+  const int tid = threadIdx.x, lane = tid % LANES, r0 = tid / LANES;
+  int64_t u = blockIdx.x;   // the block's next unit
+#pragma unroll 1
+  for (int b0 = 0; b0 < s.n; b0 += 32) {
+  const int mine = b0 + (tid & 31);
+  int from = 0, len = 0, pages = 0;
+  if (mine < s.n) {
+    const Seq q = seq_at(c, s, mine);
+    len = q.len;
+    from = max(first ? first[mine] : q.len - q.n, 0) >> c.page_log2;
+    if (first || q.n > 0) pages = max(((len + c.page_len - 1) >> c.page_log2) - from, 0);
+  }
+  int incl = pages;   // (4,096 x 2^26: below 2^31 for 32 of them)
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, incl, o);
+    if ((tid & 31) >= o) incl += y;
+  }
+  const int64_t units = (int64_t)__shfl_sync(0xffffffffu, incl, 31) * c.H;
+#pragma unroll 1
+  for (; u < units; u += gridDim.x) {
+    const int h = (int)(u % c.H), place = (int)(u / c.H);
+    const int src = __ffs(__ballot_sync(0xffffffffu, incl > place)) - 1, b = b0 + src;
+    const int k = place - __shfl_sync(0xffffffffu, incl - pages, src) + __shfl_sync(0xffffffffu, from, src);
     const int64_t at = pool_row(c, s, b, h, k << c.page_log2);   // (the same for all threads)
+    const int held = min(c.page_len, __shfl_sync(0xffffffffu, len, src) - (k << c.page_log2));
     if (at < 0) continue;
-    const int held = min(c.page_len, q.len - (k << c.page_log2));
     Two sum[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = Two{0.f, 0.f};
@@ -149,6 +169,8 @@ __global__ void __launch_bounds__(SUM_THREADS) summarise(Pool c, Seqs s, const i
       code[row * D + tid] = fine ? (int8_t)(int)r : 0;
       if (tid == 0) scale[row] = fine ? (uint8_t)(e + 127) : 255;
     }
+  }
+  u -= units;
   }
 }
 
@@ -809,8 +831,8 @@ cudaError_t choose_set_smem_limits() {
 cudaError_t launch_summarise(const Pool& c, const Seqs& s, const int32_t* first, int8_t* code, uint8_t* scale, cudaStream_t st) {
   const int n_sm = sm_count();
   if (n_sm <= 0) return cudaErrorInvalidDevice;
-  const int64_t units = (int64_t)s.max_pages * c.H;
-  const dim3 grid((unsigned)std::min<int64_t>(units, std::max(1, 8 * n_sm / s.n)), s.n);
+  const int64_t most = (int64_t)s.max_pages * c.H * s.n;
+  const dim3 grid((unsigned)std::min<int64_t>(most, SUM_BLOCKS * n_sm));
   auto* f = c.d == 128 ? (c.e4m3 ? summarise<128, true> : summarise<128, false>)
                        : (c.e4m3 ? summarise<64, true> : summarise<64, false>);
   return launch_kernel(f, grid, SUM_THREADS, 0, 1, false, st, c, s, first, code, scale);
