@@ -463,7 +463,7 @@ typedef struct {
  *   coord : device int32 [n_axes][rows], the coordinates of every row's token.
  *   Q, Qo : device [H_q][rows][d] bf16, K, Ko : [H_k][rows][d]; strides as those of a packed tensor below (inputs may be
  *           broadcast); d in {64, 128}; 1 <= rows <= 1<<20; 0 <= H_q, H_k <= 4096, not both 0 (Q or K is
- *           then ignored).  An output may be its input, with the same strides; it must not overlap it in other ways.
+ *           then ignored).  An output may be its input, with the same strides; otherwise outputs overlap nothing.
  * Runs on the current device.                                                             */
 dkv_status_t dkv_norm_rope(int32_t d, const dkv_norm_rope_t* how, const int32_t* coord, int32_t rows, int32_t H_q,
                            const void* Q, int64_t q_head_stride, int64_t q_row_stride, void* Qo, int64_t qo_head_stride,
@@ -691,8 +691,8 @@ typedef struct {
 
 /* Summaries of the pages of sequence b that hold a position >= first[b] (device int32 [n_seq]; NULL: the
  * positions of the call's tokens): the mean of the page's key rows at positions < seq_len[b] in codes of 8 bits, the
- * sums exact to 2^-40 of the largest magnitude in a column.  Sequences may share pages that both summarise only where they
- * hold the same positions of them.                                                        */
+ * sums exact to 2^-40 of the largest magnitude in a column.  Pages given back (negative entries of the table) are passed by.
+ * Sequences may share pages that both summarise only where they hold the same positions of them.  */
 dkv_status_t dkv_cache_summarise(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const int32_t* first,
                                  const dkv_cache_summaries_t* summaries, void* stream);
 
@@ -714,7 +714,7 @@ typedef struct {
  *   - of the other seen pages the `top` with the best scores, equal ones in the order of their numbers.
  * score(page) = max over the tile's tokens and the head's group of queries of (c_q . c_page) 2^(e_q + e_page), with Q's rows in
  * codes of 8 bits like the summaries: whole numbers times powers of two, so every choice is exact.  Queries and pages
- * without codes count as -infinity, and such a score is not listed.  A tile whose tokens all lie at negative positions has an empty list.
+ * without codes count as -infinity, so do pages given back, and such a score is not listed.  A tile whose tokens all lie at negative positions has an empty list.
  *   Q : device [H_q][rows][d] bf16 as for dkv_cache_attend;  lists : device int32 [H][rows / tile + n_seq][width].  */
 dkv_status_t dkv_cache_choose(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const dkv_cache_summaries_t* summaries,
                               const void* Q, int32_t H_q, int32_t rows, int64_t q_head_stride, int64_t q_row_stride,
@@ -728,8 +728,9 @@ typedef struct {
 } dkv_cache_chosen_t;
 
 /* O[h][i] = sum_j softmax_j(scale Q[h][i] . K[j]) V[j] over the positions j < end(p) on the pages that lists[h / (H_q / H)]
- * names for the token's tile (a list ends at its first negative entry).  Arguments, masks, numbers that are not
- * finite, rows that see nothing and rounding as in dkv_cache_attend (over an e4m3 cache the keys are widened to bf16).  Entries that do not ascend or lie
+ * names for the token's tile (a list ends at its first negative entry).  Arguments, numbers that are not
+ * finite, rows that see nothing and rounding as in dkv_cache_attend, the few-row rounding of queries over an e4m3 cache among it
+ * (where a tile's tokens and the group's heads make at most 16 rows); a place whose score is -infinity counts as not seen.  Entries that do not ascend or lie
  * behind the sequence's last page set the error word (DKV_ERR_DEVICE); what the tile's tokens get is then unspecified.  */
 dkv_status_t dkv_cache_attend_chosen(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const void* Q, int32_t H_q,
                                      int32_t rows, int64_t q_head_stride, int64_t q_row_stride, void* O,

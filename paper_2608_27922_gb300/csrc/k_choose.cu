@@ -73,104 +73,107 @@ __global__ void __launch_bounds__(SUM_THREADS, SUM_BLOCKS) summarise(Pool c, Seq
   int64_t u = blockIdx.x;   // the block's next unit
 #pragma unroll 1
   for (int b0 = 0; b0 < s.n; b0 += 32) {
-  const int mine = b0 + (tid & 31);
-  int from = 0, len = 0, pages = 0;
-  if (mine < s.n) {
-    const Seq q = seq_at(c, s, mine);
-    len = q.len;
-    from = max(first ? first[mine] : q.len - q.n, 0) >> c.page_log2;
-    if (first || q.n > 0) pages = max(((len + c.page_len - 1) >> c.page_log2) - from, 0);
-  }
-  int incl = pages;   // (4,096 x 2^26: below 2^31 for 32 of them)
+    const int mine = b0 + (tid & 31);
+    int from = 0, len = 0, pages = 0;
+    if (mine < s.n) {
+      const Seq q = seq_at(c, s, mine);
+      len = q.len;
+      from = max(first ? first[mine] : q.len - q.n, 0) >> c.page_log2;
+      if (first || q.n > 0) pages = max(((len + c.page_len - 1) >> c.page_log2) - from, 0);
+    }
+    unsigned incl = pages;   // (32 of up to 2^26)
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, incl, o);
-    if ((tid & 31) >= o) incl += y;
-  }
-  const int64_t units = (int64_t)__shfl_sync(0xffffffffu, incl, 31) * c.H;
+    for (int o = 1; o < 32; o <<= 1) {
+      const unsigned y = __shfl_up_sync(0xffffffffu, incl, o);
+      if ((tid & 31) >= o) incl += y;
+    }
+    const int64_t units = (int64_t)__shfl_sync(0xffffffffu, incl, 31) * c.H;
 #pragma unroll 1
-  for (; u < units; u += gridDim.x) {
-    const int h = (int)(u % c.H), place = (int)(u / c.H);
-    const int src = __ffs(__ballot_sync(0xffffffffu, incl > place)) - 1, b = b0 + src;
-    const int k = place - __shfl_sync(0xffffffffu, incl - pages, src) + __shfl_sync(0xffffffffu, from, src);
-    const int64_t at = pool_row(c, s, b, h, k << c.page_log2);   // (the same for all threads)
-    const int held = min(c.page_len, __shfl_sync(0xffffffffu, len, src) - (k << c.page_log2));
-    if (at < 0) continue;
-    Two sum[8];
+    for (; u < units; u += gridDim.x) {
+      const int h = (int)(u % c.H);
+      const unsigned place = (unsigned)(u / c.H);
+      const int src = __ffs(__ballot_sync(0xffffffffu, incl > place)) - 1, b = b0 + src;
+      const int k = (int)(place - __shfl_sync(0xffffffffu, incl - pages, src)) + __shfl_sync(0xffffffffu, from, src);
+      const int page = s.table[(int64_t)b * s.max_pages + k];   // (the same for all threads; negative: given back)
+      if (page >= c.n_pages) fail(c.status, DEV_INCONSISTENT, SITE_PAGE);
+      const int64_t at = (unsigned)page < (unsigned)c.n_pages ? ((int64_t)page * c.H + h) << c.page_log2 : -1;
+      const int held = min(c.page_len, __shfl_sync(0xffffffffu, len, src) - (k << c.page_log2));
+      if (at < 0) continue;
+      Two sum[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] = Two{0.f, 0.f};
+      for (int i = 0; i < 8; ++i) sum[i] = Two{0.f, 0.f};
 #pragma unroll 4
-    for (int r = r0; r < held; r += ROWS) {
-      float x[8];
-      if (E4M3) {
-        const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.k) + (at + r) * D) + lane);
-        const float f = scale_of(c.ks[at + r]);
+      for (int r = r0; r < held; r += ROWS) {
+        float x[8];
+        if (E4M3) {
+          const uint2 v = __ldg(reinterpret_cast<const uint2*>(static_cast<const uint8_t*>(c.k) + (at + r) * D) + lane);
+          const float f = scale_of(c.ks[at + r]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = scaled((i < 4 ? v.x >> (8 * i) : v.y >> (8 * i - 32)) & 0xffu, f);
-      } else {
-        const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(c.k) + (at + r) * D) + lane);
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+          for (int i = 0; i < 8; ++i) x[i] = scaled((i < 4 ? v.x >> (8 * i) : v.y >> (8 * i - 32)) & 0xffu, f);
+        } else {
+          const uint4 v = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(c.k) + (at + r) * D) + lane);
+          const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[2 * i] = __uint_as_float(w[i] << 16);
-          x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+          for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+          }
         }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) add(sum[i], x[i]);
       }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) add(sum[i], x[i]);
-    }
+      for (int i = 0; i < 8; ++i) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-#pragma unroll
-      for (int o = LANES; o < 32; o <<= 1)
-        add(sum[i], Two{__shfl_xor_sync(0xffffffffu, sum[i].hi, o), __shfl_xor_sync(0xffffffffu, sum[i].lo, o)});
-    }
-    __syncthreads();   // (the last unit's sums have been read)
-    if (tid % 32 < LANES) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) part[tid / 32][lane * 8 + i] = sum[i];
-    }
-    __syncthreads();
-    Two m{0.f, 0.f};
-    if (tid < D) {
-      m = part[0][tid];
-#pragma unroll
-      for (int w = 1; w < WARPS; ++w) add(m, part[w][tid]);
-      m = settled(m);
-      if ((held & (held - 1)) == 0) {
-        const float f = 1.0f / (float)held;
-        m.hi *= f;
-        m.lo *= f;
-      } else {
-        const double y = ((double)m.hi + (double)m.lo) / (double)held;
-        m.hi = (float)y;
-        m.lo = (float)(y - (double)m.hi);
+        for (int o = LANES; o < 32; o <<= 1)
+          add(sum[i], Two{__shfl_xor_sync(0xffffffffu, sum[i].hi, o), __shfl_xor_sync(0xffffffffu, sum[i].lo, o)});
       }
-      // a magnitude that lies above hi's counts as the next float; one without codes as an infinity
-      const float a = fabsf(m.hi);
-      const bool above = m.hi < 0.f ? m.lo < 0.f : m.lo > 0.f;
-      float top = above && (__float_as_uint(a) & 0x7fffffu) == 0x7e0000u ? __uint_as_float(__float_as_uint(a) + 1) : a;
-      if (!(a < WILD)) top = INFINITY;
+      __syncthreads();   // (the last unit's sums have been read)
+      if (tid % 32 < LANES) {
 #pragma unroll
-      for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-      if (tid % 32 == 0) tops[tid / 32] = top;
-    }
-    __syncthreads();
-    if (tid < D) {
-      float top = tops[0];
+        for (int i = 0; i < 8; ++i) part[tid / 32][lane * 8 + i] = sum[i];
+      }
+      __syncthreads();
+      Two m{0.f, 0.f};
+      if (tid < D) {
+        m = part[0][tid];
 #pragma unroll
-      for (int w = 1; w < D / 32; ++w) top = fmaxf(top, tops[w]);
-      const bool fine = top < INFINITY;
-      const int e = fine ? exponent_of(top) : 0;
-      const float y = m.hi * pow2(-e);
-      float r = rintf(y);
-      if (fabsf(y - r) == 0.5f && m.lo != 0.f) r = m.lo > 0.f ? floorf(y) + 1.f : floorf(y);   // no tie
-      const int64_t row = at >> c.page_log2;   // page * H + h
-      code[row * D + tid] = fine ? (int8_t)(int)r : 0;
-      if (tid == 0) scale[row] = fine ? (uint8_t)(e + 127) : 255;
+        for (int w = 1; w < WARPS; ++w) add(m, part[w][tid]);
+        m = settled(m);
+        if ((held & (held - 1)) == 0) {
+          const float f = 1.0f / (float)held;
+          m.hi *= f;
+          m.lo *= f;
+        } else {
+          const double y = ((double)m.hi + (double)m.lo) / (double)held;
+          m.hi = (float)y;
+          m.lo = (float)(y - (double)m.hi);
+        }
+        // a magnitude that lies above hi's counts as the next float; one without codes as an infinity
+        const float a = fabsf(m.hi);
+        const bool above = m.hi < 0.f ? m.lo < 0.f : m.lo > 0.f;
+        float top = above && (__float_as_uint(a) & 0x7fffffu) == 0x7e0000u ? __uint_as_float(__float_as_uint(a) + 1) : a;
+        if (!(a < WILD)) top = INFINITY;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (tid % 32 == 0) tops[tid / 32] = top;
+      }
+      __syncthreads();
+      if (tid < D) {
+        float top = tops[0];
+#pragma unroll
+        for (int w = 1; w < D / 32; ++w) top = fmaxf(top, tops[w]);
+        const bool fine = top < INFINITY;
+        const int e = fine ? exponent_of(top) : 0;
+        const float y = m.hi * pow2(-e);
+        float r = rintf(y);
+        if (fabsf(y - r) == 0.5f && m.lo != 0.f) r = m.lo > 0.f ? floorf(y) + 1.f : floorf(y);   // no tie
+        const int64_t row = at >> c.page_log2;   // page * H + h
+        code[row * D + tid] = fine ? (int8_t)(int)r : 0;
+        if (tid == 0) scale[row] = fine ? (uint8_t)(e + 127) : 255;
+      }
     }
-  }
-  u -= units;
+    u -= units;
   }
 }
 
@@ -411,11 +414,12 @@ __device__ __forceinline__ void look_up(const Pool& c, const Seqs& s, const Work
                                         int k0, int n, int kept) {
   for (int i = threadIdx.x; i < n; i += CH_THREADS) {
     const int k = k0 + i;
-    int page = s.table[(int64_t)l.b * s.max_pages + k];
-    if ((unsigned)page >= (unsigned)c.n_pages) {
+    int page = s.table[(int64_t)l.b * s.max_pages + k];   // (negative: given back)
+    if (page >= c.n_pages) {
       fail(c.status, DEV_INCONSISTENT, SITE_PAGE);
       page = -1;
     }
+    page = max(page, -1);
     const uint32_t byte = page >= 0 ? __ldg(scale + (int64_t)page * c.H + h) : 255u;
     const bool listed = k < l.sinks || (k >= l.lo && k <= l.own);
     w.at[i] = page;

@@ -403,12 +403,12 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
     for (int i = 0; i < n; ++i) {
       const int sl = i % L::N, u0 = (t0 + i) * BK;
       const bool partial = u0 + BK > whole_to;
-      if (partial) {
+      if (!(ok = mbar_wait_warp_short(s_full, i & 1, abort_flag))) break;
+      if (partial) {   // (after the scores: before them the values' barrier may still be a phase behind)
         if (!(ok = mbar_wait_warp_short(v_full + sl, (i / L::N) & 1, abort_flag))) break;
         clear_row<D>(smem + L::V + sl * L::TB, r, wild);
         fence_async_smem();
       }
-      if (!(ok = mbar_wait_warp_short(s_full, i & 1, abort_flag))) break;
       fence_after_sync();
       float tmax;
       {

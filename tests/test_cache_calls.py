@@ -1,6 +1,7 @@
 """Refusals and structures of the calls on pages, norms and chosen pages, on the CPU; slots of tiles."""
 import ctypes
 import os
+import random
 import shutil
 import subprocess
 import tempfile
@@ -122,3 +123,98 @@ def test_slots_of_tiles(tmp_path):
     src.write_text(SRC)
     subprocess.check_call([nvcc, *B.ARCH, "-std=c++17", "-I", B.ROOT + "/include", "-I", B.CSRC, str(src), "-o", str(exe)])
     assert subprocess.run([str(exe)]).returncode == 0
+
+
+class _Bar:
+    def __init__(self, n):
+        self.n = self.c = n
+        self.phase = 0
+
+    def arrive(self):
+        self.c -= 1
+        if self.c == 0:
+            self.c, self.phase = self.n, self.phase + 1
+
+    def passed(self, parity):
+        return (self.phase & 1) != parity
+
+
+def _walk(n, N, seed):
+    """The barriers of attention over chosen pages (k_chosen_tc.cu) on n key tiles with N tiles of K and of V, its roles taking
+    turns at random, copies and products ending late: nobody is stuck, and nothing is read or overwritten too soon."""
+    r = random.Random(seed)
+    kf, ke, vf, ve = ([_Bar(1) for _ in range(N)] for _ in range(4))
+    sf, pf, of = _Bar(1), _Bar(4), _Bar(1)
+    pipe, copies, arriving = [], [], []
+    s_done, o_done, landed = [False] * n, [False] * n, {}
+
+    def produce():
+        order = [("k", 0)] if n else []
+        for i in range(n):
+            order += [("v", i)] + ([("k", i + 1)] if i + 1 < n else [])
+        for what, i in order:
+            while i >= N and not (ke if what == "k" else ve)[i % N].passed((i // N - 1) & 1):
+                yield
+            assert i < N or (s_done if what == "k" else o_done)[i - N]
+            copies.append((what, i))
+            yield
+
+    def issue():
+        for i in range(n):
+            while not kf[i % N].passed((i // N) & 1):
+                yield
+            assert landed["k", i % N] == i
+            pipe.append((s_done, i, [sf, ke[i % N]]))
+            while not vf[i % N].passed((i // N) & 1):
+                yield
+            while not pf.passed(i & 1):
+                yield
+            assert landed["v", i % N] == i
+            pipe.append((o_done, i, [ve[i % N]] + ([of] if i + 1 == n else [])))
+
+    def soft():
+        for i in range(n):
+            while not sf.passed(i & 1):
+                yield
+            assert s_done[i] and (i == 0 or o_done[i - 1]) and not o_done[i]
+            if r.random() < 0.3:                       # a tile that some row does not see whole
+                while not vf[i % N].passed((i // N) & 1):
+                    yield
+                assert landed["v", i % N] == i and not o_done[i]
+            pf.arrive()
+            yield
+        while n and not of.passed(0):
+            yield
+        assert all(o_done)
+
+    roles = [produce(), issue()] + [soft() for _ in range(4)]
+    for step in range(100000):
+        if not roles:
+            return
+        k = r.randrange(len(roles) + 3)
+        if k < len(roles):
+            try:
+                next(roles[k])
+            except StopIteration:
+                roles.pop(k)
+        elif k == len(roles) and pipe:
+            done, i, bars = pipe.pop(0)
+            done[i] = True
+            r.shuffle(bars)
+            arriving.append(bars)
+        elif k == len(roles) + 1 and arriving:
+            arriving[0].pop(0).arrive()
+            if not arriving[0]:
+                arriving.pop(0)
+        elif k == len(roles) + 2 and copies:
+            what, i = copies.pop(r.randrange(len(copies)))
+            landed[what, i % N] = i
+            (kf if what == "k" else vf)[i % N].arrive()
+    raise AssertionError(("stuck", n, N, seed))
+
+
+@pytest.mark.parametrize("N", [1, 2])
+def test_barriers_of_attention_over_chosen_pages(N):
+    for n in range(9):
+        for seed in range(40):
+            _walk(n, N, seed)

@@ -116,10 +116,56 @@ def test_choose(dkv, fmt, d, top, tile, block, sinks, local):
     (2, 10, [(1, 9000), (1, 16), (1, 5000)], 16, 60, 1),
     (1, 128, [(1, 700)], 16, 7, 1),              # 128 query heads: two rounds of rows
     (1, 3, [(90, 1700)], 32, 9, 64),             # 192 rows
-    (1, 1, [(1, 70000)], 16, 1000, 1)])          # more pages than one go takes, a long list
+    (1, 1, [(1, 70000)], 16, 1000, 1),           # more pages than one go takes, a long list
+    (1, 1, [(32, 67000)], 16, 400, 32)])         # the same for many rows
 def test_choose_large(dkv, H, Hq, seqs, page, top, tile):
     case = cache_ref.Case(seqs, H, 64, page, "bf16", seed=2)
     run_choose(dkv, case, Hq, top, tile, 1, 1, 2)
+
+
+def test_many_sequences(dkv):
+    """1,500 sequences of no, one or a few tokens: every tile is found, and nothing else is written."""
+    g = np.random.default_rng(3)
+    seqs = []
+    for _ in range(1500):
+        n = int(g.choice([0, 1, 1, 2, 5]))
+        seqs.append((n, n + int(g.integers(0, 50))))
+    case = cache_ref.Case(seqs, 1, 64, 16, "bf16", seed=7)
+    c, s = case.cache(dkv), case.device_seqs(dkv)
+    sums = dkv.Summaries(c)
+    c.summarise(s, sums, first=t32([0] * 1500))
+    code, scale = ref.summaries(case)
+    assert np.array_equal(sums.code.cpu().numpy(), code) and np.array_equal(sums.scale.cpu().numpy(), scale)
+    for tile, Hq in ((1, 2), (2, 1), (3, 9)):
+        Q = queries(case, Hq)
+        lists = c.choose(bf(Q), s, sums, 1, tile=tile, sink_pages=0, local_pages=1)
+        want = ref.choose(case, Q, code, scale, 1, tile, 1, 0, 1, lists.shape[-1])
+        assert np.array_equal(lists.cpu().numpy(), want)
+        O = c.attend_chosen(bf(Q), s, lists, tile=tile)
+        cache_ref.check(O, ref.attend(case, Q, want, tile))
+    c.sync()
+
+
+def test_pages_given_back(dkv):
+    """Pages that a window has left are neither summarised nor listed, and are no error."""
+    case = cache_ref.Case([(2, 16 * 20)], 2, 64, 16, "bf16", seed=8)
+    c, s = case.cache(dkv), case.device_seqs(dkv)
+    gone = [3, 4, 5, 6, 11]
+    s.block_table[0, gone] = -1
+    sums = dkv.Summaries(c)
+    sums.code.fill_(3)
+    c.summarise(s, sums, first=t32([0]))
+    at = case.table[0, gone]
+    assert bool((sums.code[torch.from_numpy(at).long().cuda()] == 3).all())
+    code, scale = ref.summaries(case)
+    scale[at] = 255
+    for Hq in (2, 40):
+        Q = queries(case, Hq)
+        lists = c.choose(bf(Q), s, sums, 20, tile=2)
+        want = ref.choose(case, Q, code, scale, 20, 2, 1, 1, 2, lists.shape[-1])
+        assert np.array_equal(lists.cpu().numpy(), want) and not np.isin(want, gone).any()
+        cache_ref.check(c.attend_chosen(bf(Q), s, lists, tile=2), ref.attend(case, Q, want, 2))
+    c.sync()
 
 
 def test_choose_ties_and_what_has_no_codes(dkv):
@@ -188,7 +234,8 @@ def test_attend(dkv, fmt, d, page, Hq, H, tile, block):
     (3, 3, [(300, 1200)], 128, 128, 10),
     (40, 8, [(130, 400)], 32, 64, 12),
     (2, 1, [(100, 3000), (3, 2900)], 16, 32, 180),  # clusters of four share a tile's list
-    (1, 1, [(128, 1500)], 128, 128, 9)])
+    (1, 1, [(128, 1500)], 128, 128, 9),
+    (1, 1, [(33, 5000)], 16, 64, 300)])             # a list longer than a CTA has threads
 def test_attend_large(dkv, fmt, Hq, H, seqs, page, tile, width):
     case = cache_ref.Case(seqs, H, 128, page, fmt, seed=1)
     c, s = case.cache(dkv), case.device_seqs(dkv)
@@ -216,9 +263,10 @@ def test_every_page_listed_is_dense_attention(dkv, fmt, tile):
 
 @pytest.mark.parametrize("tile,pages", [(1, 7), (2, 7), (5, 7), (64, 7), (16, 7), (40, 70), (1, 70)])
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
-def test_what_is_not_finite(dkv, fmt, tile, pages):
+@pytest.mark.parametrize("d", [64, 128])
+def test_what_is_not_finite(dkv, fmt, d, tile, pages):
     """Infinities and NaN in keys and values: they reach the rows that see them, and no others."""
-    case = cache_ref.Case([(40, 16 * pages - 12)], 1, 64, 16, fmt, seed=3)
+    case = cache_ref.Case([(40, 16 * pages - 12)], 1, d, 16, fmt, seed=3)
     at = case.table[0][:pages]
     if fmt == "bf16":
         case.v[at[-3], 0, 2, 5], case.v[at[-2], 0, 3, 9], case.v[at[-3], 0, 9, 1] = np.inf, np.nan, -np.inf
