@@ -643,31 +643,38 @@ def norm_rope(Q: Optional[torch.Tensor], K: Optional[torch.Tensor], how: NormRop
     some = Q if Q is not None else K
     if some is None:
         raise ValueError("norm_rope: neither queries nor keys")
-    rows, device = some.shape[1], some.device
+    rows, device, d = some.shape[1], some.device, how.d
     if how.device != device:
         raise ValueError(f"how: expected tensors on {device}, got {how.device}")
     _check_i32(coord, (how.n_axes, rows), "coord", device)
     raw, ctx = _on_stream(stream, device)
-    outs, args = [], []
-    for x, given, name in ((Q, out[0] if out else None, "Q"), (K, out[1] if out else None, "K")):
-        if x is None:
-            outs.append(None)
-            args += [0, None, 0, 0, None, 0, 0]
-            continue
-        a = _check_rows(x, x.shape[0], rows, how.d, device, name)
-        y = _empty(ctx, x.shape, torch.bfloat16, device) if given is None else given
-        z = _check_rows(y, x.shape[0], rows, how.d, device, "out")
-        outs.append(y)
-        args += [x.shape[0], x.data_ptr(), a[0], a[1], y.data_ptr(), z[0], z[1]]
+    Qo, Ko = out if out is not None else (None, None)
+    q = k = (0, None, 0, 0, None, 0, 0)
+    if Q is not None:
+        heads = Q.shape[0]
+        a = _check_rows(Q, heads, rows, d, device, "Q")
+        if Qo is None:
+            Qo, z = _empty(ctx, (heads, rows, d), torch.bfloat16, device), (rows * d, d)
+        else:
+            z = _check_rows(Qo, heads, rows, d, device, "out")
+        q = (heads, Q.data_ptr(), a[0], a[1], Qo.data_ptr(), z[0], z[1])
+    if K is not None:
+        heads = K.shape[0]
+        a = _check_rows(K, heads, rows, d, device, "K")
+        if Ko is None:
+            Ko, z = _empty(ctx, (heads, rows, d), torch.bfloat16, device), (rows * d, d)
+        else:
+            z = _check_rows(Ko, heads, rows, d, device, "out")
+        k = (heads, K.data_ptr(), a[0], a[1], Ko.data_ptr(), z[0], z[1])
     call = lib().dkv_norm_rope
     if torch.cuda.current_device() == device.index:
-        st = call(how.d, how._ref, coord.data_ptr(), rows, *args, raw)
+        st = call(d, how._ref, coord.data_ptr(), rows, *q, *k, raw)
     else:
         with torch.cuda.device(device):
-            st = call(how.d, how._ref, coord.data_ptr(), rows, *args, raw)
+            st = call(d, how._ref, coord.data_ptr(), rows, *q, *k, raw)
     if st != DKV_OK:
         _check(st, "dkv_norm_rope")
-    return tuple(outs)
+    return (Qo if Q is not None else None), (Ko if K is not None else None)
 
 
 def _on_stream(stream, device):
@@ -862,11 +869,13 @@ class PagedCache:
         s, ctx = self._on(stream)
         queries = (0, None, 0, 0, None, 0, 0)
         if Q is not None:
-            q = self._packed(Q, Q.shape[0], rows, "Q")
+            heads = Q.shape[0]
+            q = self._packed(Q, heads, rows, "Q")
             if out is None:
-                out = self._new(ctx, Q.shape, torch.bfloat16)
-            o = self._packed(out, Q.shape[0], rows, "out")
-            queries = (Q.shape[0], Q.data_ptr(), q[0], q[1], out.data_ptr(), o[0], o[1])
+                out, o = self._new(ctx, (heads, rows, self.d), torch.bfloat16), (rows * self.d, self.d)
+            else:
+                o = self._packed(out, heads, rows, "out")
+            queries = (heads, Q.data_ptr(), q[0], q[1], out.data_ptr(), o[0], o[1])
         st = self._write_norm_rope(self.handle, self._seqs(seqs), how._ref, None if coord is None else coord.data_ptr(), rows,
                                    *queries, K.data_ptr(), k[0], k[1], V.data_ptr(), v[0], v[1], s)
         if st != DKV_OK:
