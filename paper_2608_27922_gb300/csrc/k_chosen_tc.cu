@@ -12,8 +12,8 @@
 // softmax runs, the other's products do, and one's first loads hide behind the other's work, without a schedule of
 // items.  Each has half of the SM's memory (a tile of Q, one of K and one of V at d = 128) and of its TMEM.
 //
-// bf16 pages come in by TMA, one box a page and 64-column panel; the pages of the tile after next are asked into L2
-// meanwhile.  Codes come by plain loads, one tile ahead in the registers of four warps, which write them as bf16 with their
+// bf16 pages come in by TMA, one box a page and 64-column panel.  (Asking the tile after next into L2 ahead of it: 278 us for
+// 276.)  Codes come by plain loads, one tile ahead in the registers of four warps, which write them as bf16 with their
 // scales in them: code bits in bf16's fields are the value times 2^-120, one product with 2^120 times the scale makes it
 // exact.
 //
@@ -62,9 +62,12 @@ struct Lay {
   static constexpr size_t BYTES = STATS + 128 * 8;
   static constexpr int JOIN = K;                       // a part's outputs, [D / 4][128 rows] of 16 bytes
   static constexpr int THREADS = (8 + (E4M3 ? 4 : 0)) * 32;
-  // registers a thread: the first four warps, the softmax, the conversion; the launch gives 128 (80) each
-  static constexpr int REGS_IO = E4M3 ? 40 : 56, REGS_SOFT = E4M3 ? 128 : 200, REGS_CONV = 72;
-  static_assert(REGS_IO + REGS_SOFT + (E4M3 ? REGS_CONV : 0) <= (E4M3 ? 3 * 80 : 2 * 128), "register split");
+  // registers a thread: the first four warps, the softmax, the conversion; the launch gives 128 (80) each.  (The softmax does with
+  // 128 or 96; the first warps, with 56 or 40, kept their descriptors in local memory: a block of 40 heads 303 us for 280.)
+  static constexpr int REGS = E4M3 ? 80 : 128;
+  static constexpr int REGS_IO = E4M3 ? 72 : 88, REGS_SOFT = E4M3 ? 96 : 168, REGS_CONV = 72;
+  static_assert(REGS_IO + REGS_SOFT + (E4M3 ? REGS_CONV : 0) <= (E4M3 ? 3 : 2) * REGS, "register split");
+  static_assert(REGS_IO <= REGS && REGS_CONV <= REGS && REGS_SOFT >= REGS, "lowered ones are, raised ones are");
   static_assert(2 * N * TB >= D * BQ * 4, "a part in the tiles' place");
   static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two CTAs an SM");
 };
@@ -100,6 +103,24 @@ __device__ __forceinline__ uint32_t seen32(const Keys& k, int u, int end) {
   if (k.len >= 32) return a < 0 ? 0u : below(end - a);
   const int z = k.pos(u + 16);
   return (a < 0 ? 0u : below(end - a) & 0xffffu) | (z < 0 ? 0u : (below(end - z) & 0xffffu) << 16);
+}
+
+// P = 2^(s sl2 + nm) over 32 scores as 16 packed bf16 pairs; lab accumulates the even and the odd columns.
+__device__ __forceinline__ void weights(const float (&a)[32], float sl2, float nm, float2& lab, uint32_t (&pk)[16]) {
+#pragma unroll
+  for (int k = 0; k < 16; ++k) {
+    const float2 x = __ffma2_rn(make_float2(a[2 * k], a[2 * k + 1]), make_float2(sl2, sl2), make_float2(nm, nm));
+    const float2 p = make_float2(ex2(x.x), ex2(x.y));
+    lab = __fadd2_rn(lab, p);
+    pk[k] = pack_bf16(p.x, p.y);
+  }
+}
+// 16 consecutive 32-bit columns of this warp's 32 TMEM lanes.
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+               "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+               "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+               : "memory");
 }
 
 __device__ __forceinline__ void mask_row(float (&v)[32], uint32_t see) {
@@ -159,12 +180,6 @@ __device__ __noinline__ Wild wild_in(const Pool& c, const Keys& keys, int h, int
 __device__ __forceinline__ void store32(void* p, const uint32_t* w) {
   asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]),
                "r"(w[3]), "r"(w[4]), "r"(w[5]), "r"(w[6]), "r"(w[7])
-               : "memory");
-}
-
-__device__ __forceinline__ void prefetch_4d(const CUtensorMap* map, int x, int y, int z, int w) {
-  asm volatile("cp.async.bulk.prefetch.tensor.4d.L2.global.tile [%0, {%1, %2, %3, %4}];" ::"l"(reinterpret_cast<uint64_t>(map)),
-               "r"(x), "r"(y), "r"(z), "r"(w)
                : "memory");
 }
 
@@ -332,9 +347,6 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
           if (box < np)   // (nobody's page: zeros)
             tma_load_4d(smem + (is_k ? L::K : L::V) + sl * L::TB + panel * PANEL + box * rows * 128, is_k ? &tmK : &tmV, bar,
                         panel * 64, in, h, at < 0 ? j.c.n_pages : at);
-          // the tile after next, into L2
-          place(i + 2, at, in);
-          if (at >= 0) prefetch_4d(is_k ? &tmK : &tmV, panel * 64, in, h, at);
           __syncwarp();
           return true;
         };
@@ -446,12 +458,14 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
         float a[32], z[32];
-        uint32_t pk[32];
+        uint32_t pk[16];
         tmem_ld32(sc + half * 64, a);
         tmem_ld32(sc + half * 64 + 32, z);
         tmem_wait_ld();
-        exp_pack(a, z, j.m.sl2, nm, lab, pk);
-        tmem_st32(sc + half * 32, pk);
+        weights(a, j.m.sl2, nm, lab, pk);
+        tmem_st16(sc + half * 32, pk);
+        weights(z, j.m.sl2, nm, lab, pk);
+        tmem_st16(sc + half * 32 + 16, pk);
       }
       if (i > 0 && __any_sync(0xffffffffu, raise)) {
         const float alpha = raise ? ex2(mprev - mrun) : 1.0f;
@@ -460,14 +474,9 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
           float v[32];
           tmem_ld32(oc + c * 32, v);
           tmem_wait_ld();
-          uint32_t w32[32];
 #pragma unroll
-          for (int k = 0; k < 16; ++k) {
-            const float2 y = __fmul2_rn(make_float2(v[2 * k], v[2 * k + 1]), make_float2(alpha, alpha));
-            w32[2 * k] = __float_as_uint(y.x);
-            w32[2 * k + 1] = __float_as_uint(y.y);
-          }
-          tmem_st32(oc + c * 32, w32);
+          for (int k = 0; k < 32; ++k) v[k] *= alpha;
+          tmem_st32(oc + c * 32, reinterpret_cast<uint32_t(&)[32]>(v));
         }
       }
       l += lab.x + lab.y;
