@@ -244,9 +244,9 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   uint64_t* v_full = bars + 5;      // [N]
   uint64_t* v_empty = bars + 7;     // [N]
   uint64_t* s_full = bars + 9;
-  uint64_t* p_full = bars + 10;
-  uint64_t* o_full = bars + 11;
-  uint64_t* over = bars + 12;       // every role but the producer has ended
+  uint64_t* p_full = bars + 10;     // [2] weights of a tile's first and last 64 keys
+  uint64_t* o_full = bars + 12;
+  uint64_t* over = bars + 13;       // every role but the producer has ended
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bars + 14);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 15);
   volatile int* wild = abort_flag + 1;
@@ -262,7 +262,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
       mbar_init(v_empty + i, 1);
     }
     mbar_init(s_full, 1);
-    mbar_init(p_full, 4);
+    mbar_init(p_full + 0, 4);
+    mbar_init(p_full + 1, 4);
     mbar_init(o_full, 1);
     mbar_init(over, 1 + 4 + (E4M3 ? 4 : 0));
     *abort_flag = 0;
@@ -387,17 +388,23 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
         }
         __syncwarp();
         if (!(ok = mbar_wait_warp_short(v_full + sl, (i / L::N) & 1, abort_flag))) break;
-        if (!(ok = mbar_wait_warp_short(p_full, i & 1, abort_flag))) break;
-        fence_after_sync();
         const uint64_t vd = desc_add(vd0, sl * L::TB);
-        if (elect_one()) {
+        // (the first half's product runs while the last half's weights are worked out)
 #pragma unroll
-          for (int kk = 0; kk < 8; ++kk)
-            mma_bf16_ts(tmem + 128, tmem + kk * 8, desc_add(vd, kk * 2048), id_o, i > 0 || kk > 0 ? 1u : 0u);
-          mma_commit(v_empty + sl);
-          if (i + 1 == n) mma_commit(o_full);
+        for (int half = 0; half < 2; ++half) {
+          if (!(ok = mbar_wait_warp_short(p_full + half, i & 1, abort_flag))) break;
+          fence_after_sync();
+          if (elect_one()) {
+#pragma unroll
+            for (int kk = half * 4; kk < half * 4 + 4; ++kk)
+              mma_bf16_ts(tmem + 128, tmem + kk * 8, desc_add(vd, kk * 2048), id_o, i > 0 || kk > 0 ? 1u : 0u);
+            if (half) {
+              mma_commit(v_empty + sl);
+              if (i + 1 == n) mma_commit(o_full);
+            }
+          }
+          __syncwarp();
         }
-        __syncwarp();
       }
       if (!ok && lane == 0) give_up(1);
       if (!ok) {   // every product complete before TMEM is freed
@@ -453,6 +460,18 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
         l *= i > 0 ? ex2(mrun - tmax) : 0.f;
         mrun = tmax;
       }
+      if (i > 0 && __any_sync(0xffffffffu, raise)) {
+        const float alpha = raise ? ex2(mprev - mrun) : 1.0f;
+#pragma unroll 1
+        for (int c = 0; c < D / 32; ++c) {
+          float v[32];
+          tmem_ld32(oc + c * 32, v);
+          tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 32; ++k) v[k] *= alpha;
+          tmem_st32(oc + c * 32, reinterpret_cast<uint32_t(&)[32]>(v));
+        }
+      }
       const float nm = mrun == -INFINITY ? 0.f : -mrun;   // (a row that has seen nothing yet: all weights 0)
       float2 lab = make_float2(0.f, 0.f);
 #pragma unroll 1
@@ -466,24 +485,12 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
         tmem_st16(sc + half * 32, pk);
         weights(z, j.m.sl2, nm, lab, pk);
         tmem_st16(sc + half * 32 + 16, pk);
-      }
-      if (i > 0 && __any_sync(0xffffffffu, raise)) {
-        const float alpha = raise ? ex2(mprev - mrun) : 1.0f;
-#pragma unroll 1
-        for (int c = 0; c < D / 32; ++c) {
-          float v[32];
-          tmem_ld32(oc + c * 32, v);
-          tmem_wait_ld();
-#pragma unroll
-          for (int k = 0; k < 32; ++k) v[k] *= alpha;
-          tmem_st32(oc + c * 32, reinterpret_cast<uint32_t(&)[32]>(v));
-        }
+        tmem_wait_st();
+        fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + half);
       }
       l += lab.x + lab.y;
-      tmem_wait_st();
-      fence_before_sync();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(p_full);
     }
     if (ok && n > 0) ok = mbar_wait_warp_short(o_full, 0, abort_flag);
     fence_after_sync();

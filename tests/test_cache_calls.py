@@ -144,9 +144,9 @@ def _walk(n, N, seed):
     turns at random, copies and products ending late: nobody is stuck, and nothing is read or overwritten too soon."""
     r = random.Random(seed)
     kf, ke, vf, ve = ([_Bar(1) for _ in range(N)] for _ in range(4))
-    sf, pf, of = _Bar(1), _Bar(4), _Bar(1)
+    sf, pf, of = _Bar(1), [_Bar(4), _Bar(4)], _Bar(1)
     pipe, copies, arriving = [], [], []
-    s_done, o_done, landed = [False] * n, [False] * n, {}
+    s_done, o_half, o_done, landed = [False] * n, [False] * n, [False] * n, {}
 
     def produce():
         order = [("k", 0)] if n else []
@@ -167,22 +167,24 @@ def _walk(n, N, seed):
             pipe.append((s_done, i, [sf, ke[i % N]]))
             while not vf[i % N].passed((i // N) & 1):
                 yield
-            while not pf.passed(i & 1):
-                yield
-            assert landed["v", i % N] == i
-            pipe.append((o_done, i, [ve[i % N]] + ([of] if i + 1 == n else [])))
+            for half in (0, 1):
+                while not pf[half].passed(i & 1):
+                    yield
+                assert landed["v", i % N] == i
+                pipe.append((o_done if half else o_half, i, [ve[i % N]] + ([of] if i + 1 == n else []) if half else []))
 
     def soft():
         for i in range(n):
             while not sf.passed(i & 1):
                 yield
-            assert s_done[i] and (i == 0 or o_done[i - 1]) and not o_done[i]
+            assert s_done[i] and (i == 0 or o_done[i - 1]) and not o_half[i]
             if r.random() < 0.3:                       # a tile that some row does not see whole
                 while not vf[i % N].passed((i // N) & 1):
                     yield
                 assert landed["v", i % N] == i and not o_done[i]
-            pf.arrive()
-            yield
+            for half in (0, 1):
+                pf[half].arrive()
+                yield
         while n and not of.passed(0):
             yield
         assert all(o_done)
@@ -201,7 +203,8 @@ def _walk(n, N, seed):
             done, i, bars = pipe.pop(0)
             done[i] = True
             r.shuffle(bars)
-            arriving.append(bars)
+            if bars:
+                arriving.append(bars)
         elif k == len(roles) + 1 and arriving:
             arriving[0].pop(0).arrive()
             if not arriving[0]:
