@@ -13,7 +13,7 @@
 // items.  Each has half of the SM's memory (a tile of Q, one of K and one of V at d = 128) and of its TMEM.
 //
 // bf16 pages come in by TMA, one box a page and 64-column panel.  (Asking the tile after next into L2 ahead of it: 278 us for
-// 276.)  Codes come by plain loads, one tile ahead in the registers of four warps, which write them as bf16 with their
+// 276.)  Codes come by plain loads, one tile ahead in the registers of warps of their own, which write them as bf16 with their
 // scales in them: code bits in bf16's fields are the value times 2^-120, one product with 2^120 times the scale makes it
 // exact.
 //
@@ -61,13 +61,16 @@ struct Lay {
   static constexpr int STATS = CTRL + 256;             // [128] maximum, sum (a cluster's join)
   static constexpr size_t BYTES = STATS + 128 * 8;
   static constexpr int JOIN = K;                       // a part's outputs, [D / 4][128 rows] of 16 bytes
-  static constexpr int THREADS = (8 + (E4M3 ? 4 : 0)) * 32;
-  // registers a thread: the first four warps, the softmax, the conversion; the launch gives 128 (80) each.  (The softmax does with
+  // converting warps (a block of 40 heads: 8 warps 526 us, 4 569; at d = 64 358 and 321)
+  static constexpr int CONV = !E4M3 ? 0 : D == 128 ? 8 : 4;
+  static constexpr int THREADS = (8 + CONV) * 32;
+  // registers a thread: the first four warps, the softmax, the conversion; the launch gives each
+  // thread REGS.  (The softmax does with
   // 128 or 96; the first warps, with 56 or 40, kept their descriptors in local memory: a block of 40 heads 303 us for 280.)
-  static constexpr int REGS = E4M3 ? 80 : 128;
-  static constexpr int REGS_IO = E4M3 ? 72 : 88, REGS_SOFT = E4M3 ? 96 : 168, REGS_CONV = 72;
-  static_assert(REGS_IO + REGS_SOFT + (E4M3 ? REGS_CONV : 0) <= (E4M3 ? 3 : 2) * REGS, "register split");
-  static_assert(REGS_IO <= REGS && REGS_CONV <= REGS && REGS_SOFT >= REGS, "lowered ones are, raised ones are");
+  static constexpr int REGS = CONV == 8 ? 64 : CONV == 4 ? 80 : 128;
+  static constexpr int REGS_IO = CONV == 8 ? 64 : CONV == 4 ? 72 : 88, REGS_SOFT = E4M3 ? 96 : 168, REGS_CONV = CONV == 8 ? 48 : 72;
+  static_assert(REGS_IO + REGS_SOFT + CONV / 4 * REGS_CONV <= (2 + CONV / 4) * REGS, "register split");
+  static_assert(REGS_IO <= REGS && (CONV == 0 || REGS_CONV <= REGS) && REGS_SOFT >= REGS, "lowered ones are, raised ones are");
   static_assert(2 * N * TB >= D * BQ * 4, "a part in the tiles' place");
   static_assert(2 * (BYTES + 1024) <= 228 * 1024, "two CTAs an SM");
 };
@@ -201,12 +204,12 @@ __device__ __forceinline__ uint32_t times(uint32_t x, __nv_bfloat162 f) {
   return *reinterpret_cast<const uint32_t*>(&y);
 }
 
-// Codes into bf16, 128 threads: eight neighbouring ones take four 16-byte parts (64 columns) of two neighbouring rows, so that
+// Codes into bf16, CONV warps: eight neighbouring threads take four 16-byte parts (64 columns) of two neighbouring rows, so that
 // their stores, swizzled by the row, touch every bank once.  A thread has N such parts, rows STEP apart; each is asked for
 // again, for the tile after, as soon as it has been used.  (Two sets of registers did not fit: a block of 40 heads took 2,005 us.)
-template <int D>
+template <int D, int CONV>
 struct Codes {
-  static constexpr int NP = D / 64, STEP = 32 / NP, N = 128 / STEP;
+  static constexpr int NP = D / 64, STEP = CONV * 8 / NP, N = 128 / STEP;
   static_assert(STEP % 8 == 0, "a thread's rows share their swizzle");
   uint4 x[N];
   uint32_t s[N];
@@ -256,16 +259,16 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   if (tid == 64) {
     mbar_init(q_full, 1);
     for (int i = 0; i < L::N; ++i) {
-      mbar_init(k_full + i, E4M3 ? 4 : 1);
+      mbar_init(k_full + i, E4M3 ? L::CONV : 1);
       mbar_init(k_empty + i, 1);
-      mbar_init(v_full + i, E4M3 ? 4 : 1);
+      mbar_init(v_full + i, E4M3 ? L::CONV : 1);
       mbar_init(v_empty + i, 1);
     }
     mbar_init(s_full, 1);
     mbar_init(p_full + 0, 4);
     mbar_init(p_full + 1, 4);
     mbar_init(o_full, 1);
-    mbar_init(over, 1 + 4 + (E4M3 ? 4 : 0));
+    mbar_init(over, 1 + 4 + L::CONV);
     *abort_flag = 0;
     *wild = 0;
     bounds[0] = bounds[1] = j.how.width;
@@ -544,7 +547,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   } else if constexpr (E4M3) {
     regs_lower<L::REGS_CONV>();
     // ---------------- codes into bf16: K(0), V(0), K(1), ..; the next tile's codes are on their way meanwhile
-    using W = Codes<D>;
+    using W = Codes<D, L::CONV>;
     const int ct = tid - 256, part = ct & 3, panel = (ct >> 3) % W::NP, r0 = (ct >> 3) / W::NP * 2 + ((ct >> 2) & 1);
     const uint32_t page_bytes = (uint32_t)D << j.c.page_log2;   // of a head
     const uint8_t* const kp = static_cast<const uint8_t*>(j.c.k) + panel * 64 + part * 16;
