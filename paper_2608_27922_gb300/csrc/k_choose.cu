@@ -3,7 +3,15 @@
 // A summary is the mean key of a page and head in 8 bits, so a page costs d + 1 bytes instead of its page_len rows.  The
 // score of a query row and a page is a product of whole numbers (magnitudes up to 127, sums of d of them below 2^21) times
 // a power of two: fp16 holds the numbers, the tensor cores' fp32 sums of them are exact in whatever order, and so
-// the choice does not depend on how the work is split.
+// the choice does not depend on how the work is split.  (In products of 8-bit whole numbers this GPU's tensor cores make 150 TOP/s,
+// mma.sync in fp16 594.)  The means' sums are kept as pairs of fp32 numbers, exact to some 45 bits, so that
+// their rounding to codes does not depend on the order either.
+//
+// Bound by latency: 32 tokens of 40 heads over up to 469 pages take 21 us in a graph (summaries 9, choice 16 by themselves), a chain of
+// reads (sequence, table, scale, codes), three rounds of counting and two launches.  A block of 4,680 tokens in
+// tiles of 64 over 732 pages, 12 heads: 57 us, 53 of them the choice: widening the codes for each tile of tokens 23 (shared memory is
+// 50% busy, 33 KB in and out a tile of 128 pages), the queries' codes 9, looking for the best 48 4, the start of 888 CTAs and the
+// summaries the rest.
 #include "attn_math.cuh"
 #include "cache_internal.h"
 #include "tc_ptx.cuh"
@@ -848,6 +856,8 @@ cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, cons
   if (n_sm <= 0) return cudaErrorInvalidDevice;
   const int slots = s.rows / how.tile + s.n, G = Hq / c.H;
   const int64_t lines = (int64_t)std::min(slots, s.rows) * c.H;   // (a tile has a row or more)
+  // few lists: a cluster each (one token over 2,047 pages, 8 heads: 8 CTAs a list 21 us, 1 29; 256 lists of 469 pages: 1 CTA 21,
+  // 2 29)
   int C = 1;
   while (C < 8 && lines * C <= n_sm && s.max_pages / C > 128 && 2 * C * how.top <= PLACES) C *= 2;
   auto four = [](int x) { return (x + 3) / 4 * 4; };
@@ -856,6 +866,7 @@ cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, cons
   z.cap = std::min(CAP, four((s.max_pages + C - 1) / C));
   z.places = std::max(z.cap + z.top, four(C * how.top));
   const Job job{c, s, code, scale, q, G, (uint32_t)((0x100000000ull + G - 1) / G), how, lists, z};
+  // (32 tokens of 5 or of 16 rows: the kernel for few rows 21 us, the other 26)
   const bool few = (int64_t)std::min(how.tile, s.rows) * G <= FEW;
   return c.d == 128 ? launch_choose_d<128>(job, slots, C, few, st) : launch_choose_d<64>(job, slots, C, few, st);
 }

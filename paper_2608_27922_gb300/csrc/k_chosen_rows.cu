@@ -5,13 +5,21 @@
 // shared out evenly to the warps of a cluster; each keeps a running maximum, sum and outputs in registers, and
 // the parts are joined in shared memory, over the cluster by reading the neighbours' (no scratch, no second launch).
 // HBM bounds it (4 d bytes a listed position in bf16, 2 d + 2 in e4m3), and for a single token the chain of dependent
-// reads before the first key: lengths, list, table.
+// reads before the first key: sequence, table, key.
 //
 // The products are turned round, as in the other few-row kernel: keys (columns of the values) are the 16 rows of mma.sync
 // m16n8k16, the query rows its 8 columns.  Keys go from memory to the product's registers by plain 16-byte loads, without
 // shared memory: the order in which d is summed is free, so lane (g, t) takes the 8 (16) numbers that its load brings as
 // its own share of the steps of 16, and the queries are laid out the same way.  The values' 8 x 8 blocks become operands by one
-// transposing move each; which d a column then stands for follows from the loads.
+// transposing move each; which d a column then stands for follows from the loads.  The next step's loads are issued as soon as
+// their registers are free.
+//
+// e4m3: the keys' codes become fp16, one conversion for two, and meet queries in fp16; their scales join the scores.  The values'
+// codes are transposed two at a time, a pair of columns in the place of one, and become bf16 with their scales in them.
+//
+// Measured: 32 tokens of 40 on 8 heads over 32 pages of 64 in e4m3 36 us (136 MB; 12 us of it with 3 pages: launch, chain, joining), in
+// bf16 49 (269 MB, 5.5 TB/s; 6.8 is a copy's); one token over as many pages of 131,001 positions, 8 heads, 12.5.  (By asynchronous copies
+// into shared memory, two or three steps ahead: 45.)
 #include "attn_math.cuh"
 #include "cache_internal.h"
 
@@ -30,7 +38,8 @@ namespace {
 using namespace tc;
 
 constexpr int MAX_WIDTH = 1024;
-// Warps of a CTA, CTAs of an SM (registers), times 16 positions of a warp's step.
+// Warps of a CTA, CTAs of an SM (registers), times 16 positions of a warp's step.  (32 tokens over 32 pages: e4m3 8 warps 39 us, 6
+// 43, 12 in one CTA 49; bf16 6 warps 50, 8 70; d = 64, e4m3: two times 16 positions 25, one 27; bf16 one 29, two 31.)
 template <int D, bool E4M3>
 struct Cfg {
   static constexpr int WARPS = !E4M3 && D == 128 ? 6 : 8, CTAS = 2, NH = E4M3 ? 128 / D : 1;
@@ -519,7 +528,8 @@ cudaError_t launch_chosen_rows(const Pool& c, const Seqs& s, const Packed& q, co
   const int n_sm = sm_count(), G = Hq / c.H;
   if (n_sm <= 0) return cudaErrorInvalidDevice;
   const int blocks = (how.tile * G + 7) / 8;
-  // a cluster for each unit, as large as leaves two CTAs an SM and a warp a step or more
+  // few units: a cluster for each, while its CTAs have 16 steps or more (8 units: 8 CTAs each 12.5 us, 4 14.4, 1 24.7; 64 units: 4 18.5 us, 8
+  // 27, 2 23; 256 units: 1 35, 2 45)
   int C = 1;
   const int64_t units = (int64_t)std::min(how.slots, s.rows) * blocks * c.H;   // (a tile has a row or more)
   while (C < 8 && units * C <= n_sm && how.width * (c.page_len / 16) >= 16 * C) C *= 2;

@@ -6,6 +6,10 @@
 // PLANNERS CTAs counts the free pages of its parts of refs, sums over the cluster say which free page goes to whom, and
 // only then is anything written: a call that finds a fault or too few pages leaves everything as it was.
 // A second kernel, launched beside the first, moves the rows: HBM bounds it (each byte read once and written once).
+//
+// Measured: 48 continuations forked (3.6 us) and grown (plan 8.5, copies 3.7) 14.5 us in a graph; three prompts on pages of
+// 256, 40 heads, into 64 continuations 50 us, of which the copies 33 (160 MB, read mostly from L2, where the 61 copies of three pages
+// find them); a window of 9,360 positions of two sequences, 40 heads, e4m3, moved together 64 us (look 5, plan 7, rows 49: 6.6 TB/s).
 #include "cache_internal.h"
 
 #include <cooperative_groups.h>
@@ -217,8 +221,9 @@ __device__ __forceinline__ bool give_pages(const Pool& c, int32_t* refs, int n_s
   return true;
 }
 
-// One CTA plans for small pools, a cluster for large ones (32,768 pages: 64 pages a thread).
-constexpr int ALONE_MOST = 32768;
+// One CTA plans for small pools, a cluster for large ones.  48 sequences grown on pools three quarters full, one CTA against a
+// cluster: 2,048 pages 4.2 us against 8.2, 8,192 10.3 against 8.2, 131,072 55 against 21; 2,000 sequences on 32,768 pages 64 against 23.
+constexpr int ALONE_MOST = 4096;
 int planners(const Pool& c) { return c.n_pages <= ALONE_MOST ? 1 : PLANNERS; }
 
 // What the second kernel moves for a sequence.

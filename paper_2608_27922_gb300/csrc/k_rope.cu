@@ -10,6 +10,10 @@
 // The angle c theta in turns, modulo 1: theta / 2 pi as a 64-bit fraction of a turn times the whole number c, modulo
 // 2^64, which is exact but for the fraction's own rounding; the upper 32 bits, as a number in [-1, 1) half turns, go to
 // sincospi.  The 64-bit fractions are a block's, made once (they need double precision).
+//
+// Measured: a block of 4,680 tokens, 40 heads of queries and of keys and values, into bf16 pages 55 us (47 us alone under the
+// counters: 6.2 TB/s of the 6.8 that a copy reaches), into e4m3 pages 58; a frame of 1,561 tokens, 24 + 8 heads of 64, dense 8.3 us; 32 tokens of
+// 40 + 8 heads 6.3 us, of which a launch is 4.
 #include "cache_internal.h"
 #include "cache_rows.cuh"
 
