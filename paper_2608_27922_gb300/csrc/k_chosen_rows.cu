@@ -27,6 +27,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <type_traits>
 
 namespace cg = cooperative_groups;
 
@@ -40,9 +41,11 @@ using namespace tc;
 constexpr int MAX_WIDTH = 1024;
 // Warps of a CTA, CTAs of an SM (registers), times 16 positions of a warp's step.  (32 tokens over 32 pages: e4m3 8 warps 39 us, 6
 // 43, 12 in one CTA 49; bf16 6 warps 50, 8 70; d = 64, e4m3: two times 16 positions 25, one 27; bf16 one 29, two 31.)
-template <int D, bool E4M3>
+// NARROW: two warps a CTA and as many warps an SM, where there are many units.
+template <int D, bool E4M3, bool NARROW>
 struct Cfg {
-  static constexpr int WARPS = !E4M3 && D == 128 ? 6 : 8, CTAS = 2, NH = E4M3 ? 128 / D : 1;
+  static constexpr int ALL = !E4M3 && D == 128 ? 12 : 16;   // warps of an SM
+  static constexpr int WARPS = NARROW ? 2 : ALL / 2, CTAS = ALL / WARPS, NH = E4M3 ? 128 / D : 1;
   static constexpr int THREADS = 32 * WARPS;
 };
 constexpr float RAISE_LOG2 = 8.0f;   // how far a score may pass the running maximum before that is raised
@@ -168,9 +171,10 @@ struct Smem {
   int count;
 };
 
-template <int D, bool E4M3>
-__global__ void __launch_bounds__(Cfg<D, E4M3>::THREADS, (Cfg<D, E4M3>::CTAS)) chosen_rows(Pool c, Seqs s, Packed qp, Packed op, int G, Mask m, Chosen how, int blocks) {
-  constexpr int WARPS = Cfg<D, E4M3>::WARPS, THREADS = Cfg<D, E4M3>::THREADS, NH = Cfg<D, E4M3>::NH;
+template <int D, bool E4M3, bool NARROW>
+__global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, NARROW>::CTAS)) chosen_rows(Pool c, Seqs s, Packed qp, Packed op, int G, Mask m, Chosen how, int blocks) {
+  using K = Cfg<D, E4M3, NARROW>;
+  constexpr int WARPS = K::WARPS, THREADS = K::THREADS, NH = K::NH;
   __shared__ Smem<D, WARPS> w;
   cg::cluster_group cluster = cg::this_cluster();
   const int C = cluster.num_blocks(), rank = cluster.block_rank();
@@ -535,11 +539,19 @@ cudaError_t launch_chosen_rows(const Pool& c, const Seqs& s, const Packed& q, co
   while (C < 8 && units * C <= n_sm && how.width * (c.page_len / 16) >= 16 * C) C *= 2;
   if ((int64_t)how.slots * blocks * C > 0x7fffffff) return cudaErrorInvalidValue;
   const dim3 grid(how.slots * blocks * C, c.H);
-  if (c.d == 128)
-    return c.e4m3 ? launch_kernel(chosen_rows<128, true>, grid, Cfg<128, true>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks)
-                  : launch_kernel(chosen_rows<128, false>, grid, Cfg<128, false>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks);
-  return c.e4m3 ? launch_kernel(chosen_rows<64, true>, grid, Cfg<64, true>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks)
-                : launch_kernel(chosen_rows<64, false>, grid, Cfg<64, false>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks);
+  // many short lists: two warps a CTA (8 pages of 64 in e4m3, 800 units 35 us, wide CTAs 43, 3,200 116 and 146; 29,384 lists of up to
+  // 4 pages in bf16 387 and 647; but 32 pages, 3,200 units 337 and 314)
+  const bool narrow = C == 1 && units > 4 * n_sm && how.width * (c.page_len / 16) <= 64;
+  auto launch = [&](auto d, auto e4m3) {
+    constexpr int D = decltype(d)::value;
+    constexpr bool E = decltype(e4m3)::value;
+    return narrow ? launch_kernel(chosen_rows<D, E, true>, grid, Cfg<D, E, true>::THREADS, 0, 1, false, st, c, s, q, o, G, m, how, blocks)
+                  : launch_kernel(chosen_rows<D, E, false>, grid, Cfg<D, E, false>::THREADS, 0, C, false, st, c, s, q, o, G, m, how, blocks);
+  };
+  using D128 = std::integral_constant<int, 128>;
+  using D64 = std::integral_constant<int, 64>;
+  if (c.d == 128) return c.e4m3 ? launch(D128(), std::true_type()) : launch(D128(), std::false_type());
+  return c.e4m3 ? launch(D64(), std::true_type()) : launch(D64(), std::false_type());
 }
 
 }  // namespace cache

@@ -123,17 +123,18 @@ def test_choose_large(dkv, H, Hq, seqs, page, top, tile):
     run_choose(dkv, case, Hq, top, tile, 1, 1, 2)
 
 
-def test_many_sequences(dkv):
-    """1,500 sequences of no, one or a few tokens: every tile is found, and nothing else is written."""
+@pytest.mark.parametrize("fmt,d,count", [("bf16", 64, 1500), ("e4m3", 128, 500), ("bf16", 128, 500), ("e4m3", 64, 500)])
+def test_many_sequences(dkv, fmt, d, count):
+    """Sequences of no, one or a few tokens: every tile is found, and nothing else is written."""
     g = np.random.default_rng(3)
     seqs = []
-    for _ in range(1500):
+    for _ in range(count):
         n = int(g.choice([0, 1, 1, 2, 5]))
-        seqs.append((n, n + int(g.integers(0, 50))))
-    case = cache_ref.Case(seqs, 1, 64, 16, "bf16", seed=7)
+        seqs.append((n, n + int(g.integers(0, 50 if count > 1000 else 14))))
+    case = cache_ref.Case(seqs, 1, d, 16, fmt, seed=7)
     c, s = case.cache(dkv), case.device_seqs(dkv)
     sums = dkv.Summaries(c)
-    c.summarise(s, sums, first=t32([0] * 1500))
+    c.summarise(s, sums, first=t32([0] * count))
     code, scale = ref.summaries(case)
     assert np.array_equal(sums.code.cpu().numpy(), code) and np.array_equal(sums.scale.cpu().numpy(), scale)
     for tile, Hq in ((1, 2), (2, 1), (3, 9)):
