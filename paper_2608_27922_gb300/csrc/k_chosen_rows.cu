@@ -169,6 +169,7 @@ struct Smem {
   float part[WARPS][8][D + 4];   // outputs, maximum, sum
   float joined[8][D + 4];
   int count;
+  int bad;   // least faulty entry: twice its place, odd: its page
 };
 
 template <int D, bool E4M3, bool NARROW>
@@ -197,7 +198,10 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
   };
   const int all_end = end_of(0), any_end = end_of(rows - 1);
   // the list: pages of the pool
-  if (tid == 0) w.count = how.width;
+  if (tid == 0) {
+    w.count = how.width;
+    w.bad = 0x7fffffff;
+  }
   __syncthreads();
   for (int k = tid; k < how.width; k += THREADS) {
     const int e = k == tid ? early : __ldg(line + k), before = k == tid ? early_before : __ldg(line + k - 1);
@@ -205,15 +209,17 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
     if (e < 0) {
       atomicMin(&w.count, k);
     } else if ((k && before >= 0 && e <= before) || e >= (q.len + c.page_len - 1) >> c.page_log2) {
-      fail(c.status, DEV_INCONSISTENT, SITE_LIST);
+      atomicMin(&w.bad, 2 * k);
     } else if ((e << c.page_log2) < any_end) {
-      const int64_t row = pool_row(c, s, b, h, e << c.page_log2);
-      if (row >= 0) page = (int)(row >> c.page_log2);   // page * H + h
+      const int at = s.table[(int64_t)b * s.max_pages + e];
+      if ((unsigned)at < (unsigned)c.n_pages) page = at * c.H + h;   // (memory holds fewer than 2^31)
+      else atomicMin(&w.bad, 2 * k + 1);
     }
     w.entry[k] = e;
     w.page[k] = page;
   }
   __syncthreads();
+  if (tid == 0 && w.bad >> 1 < w.count) fail(c.status, DEV_INCONSISTENT, w.bad & 1 ? SITE_PAGE : SITE_LIST);   // (what is behind the end is nothing)
   const int sub = c.page_log2 - 4, total = w.count << sub, warps = C * WARPS, gw = rank * WARPS + warp;
   const int first = (int)((int64_t)total * gw / warps), last = (int)((int64_t)total * (gw + 1) / warps);
   // queries: row g's numbers, laid out as the keys'

@@ -260,7 +260,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   uint32_t* tmem_holder = reinterpret_cast<uint32_t*>(bars + 14);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(bars + 15);
   volatile int* wild = abort_flag + 1;
-  int* bounds = reinterpret_cast<int*>(bars + 16);   // entries listed, leading ones that all rows see whole
+  // entries to be read, leading ones that all rows see whole, the list's end, its least faulty entry (twice its place, odd: its page)
+  int* bounds = reinterpret_cast<int*>(bars + 16);
   int* entry = reinterpret_cast<int*>(smem + L::LIST);
   int* page = entry + MAX_WIDTH;
   if (tid == 64) {
@@ -278,7 +279,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
     mbar_init(over, 1 + 4 + L::CONV);
     *abort_flag = 0;
     *wild = 0;
-    bounds[0] = bounds[1] = j.how.width;
+    bounds[0] = bounds[1] = bounds[2] = j.how.width;
+    bounds[3] = 0x7fffffff;
     fence_barrier_init();
     // Q is on its way while the list is looked through
     mbar_arrive_expect_tx(q_full, L::NP * j.TQ * j.G * 128);
@@ -297,14 +299,15 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
       int at = -1;
       if (e < 0) {
         atomicMin(bounds, k);
+        atomicMin(bounds + 2, k);
       } else if ((k && before >= 0 && e <= before) || e >= (q.len + j.c.page_len - 1) >> j.c.page_log2) {
-        fail(j.c.status, DEV_INCONSISTENT, SITE_LIST);
+        atomicMin(bounds + 3, 2 * k);
       } else if (((int64_t)e << j.c.page_log2) >= any_end) {
         atomicMin(bounds, k);   // (the rest of an ascending list lies behind it)
       } else {
         at = j.s.table[(int64_t)b * j.s.max_pages + e];
         if ((unsigned)at >= (unsigned)j.c.n_pages) {
-          fail(j.c.status, DEV_INCONSISTENT, SITE_PAGE);
+          atomicMin(bounds + 3, 2 * k + 1);
           at = -1;
         }
       }
@@ -317,6 +320,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
   __syncthreads();
   fence_after_sync();
   const uint32_t tmem = *tmem_holder;
+  if (tid == 64 && bounds[3] >> 1 < bounds[2])   // (what is behind the end is nothing)
+    fail(j.c.status, DEV_INCONSISTENT, bounds[3] & 1 ? SITE_PAGE : SITE_LIST);
   const Keys keys{entry, page, bounds[0], j.c.page_log2, j.c.page_len};
   const int whole_to = min(bounds[1], bounds[0]) << j.c.page_log2;   // places that every row sees
   const int NT = ((keys.count << j.c.page_log2) + BK - 1) / BK;

@@ -355,6 +355,26 @@ def test_faulty_lists_and_sequences(dkv, tile):
         c.sync()
 
 
+@pytest.mark.parametrize("tile", [1, 32])
+def test_behind_the_end_of_a_list(dkv, tile):
+    """What stands behind a list's first negative entry is nothing, whatever it is."""
+    case = cache_ref.Case([(33, 60), (2, 90)], 1, 128, 16, "bf16", seed=4, extra_cols=1)
+    c, s = case.cache(dkv), case.device_seqs(dkv)
+    s.block_table[1, 1] = -1                       # given back
+    Q = queries(case, 2)
+    lists = random_lists(case, tile, 6, most=3)
+    for b, i, m, slot in ref.tiles(case, tile):
+        lists[0, slot, 2:] = -1
+        if b == 1:
+            lists[0, slot, :2] = 0, 4
+    want = ref.attend(case, Q, lists, tile)
+    for rest in ([2, 1, 1], [10 ** 6, 3, 2 ** 31 - 1], [1, 5, -7]):
+        full = lists.copy()
+        full[:, :, 3:] = rest
+        cache_ref.check(c.attend_chosen(bf(Q), s, t32(full), tile=tile), want)
+        c.sync()
+
+
 def test_row_starts_that_go_back(dkv):
     """Arrays that contradict themselves: reported, and nothing outside the outputs is written."""
     case = cache_ref.Case([(8, 40), (8, 40), (8, 40)], 1, 64, 16, "bf16", seed=4)
