@@ -98,7 +98,7 @@ __device__ __forceinline__ Vals turned(const Vals& x, const float4* w, bool norm
     float s = squares(1.0f), r = rsqrtf(fmaf(s, 1.0f / D, eps));
     if (__any_sync(0xffffffffu, !(s < INFINITY))) {   // 128 squares of 2^58 stay below 2^124
       const float z = squares(0x1p-70f);
-      if (!(s < INFINITY)) r = z < INFINITY ? rsqrtf(z * (1.0f / D)) * 0x1p-70f : __int_as_float(0x7fffffff);
+      if (!(s < INFINITY)) r = z < INFINITY ? rsqrtf(fmaf(z, 1.0f / D, eps * 0x1p-70f * 0x1p-70f)) * 0x1p-70f : __int_as_float(0x7fffffff);
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {

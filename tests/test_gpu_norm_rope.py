@@ -77,6 +77,17 @@ def test_far_positions_and_no_weights(dkv):
     ref.check_rows(y, *ref.norm_rope(x, coord, theta, [64], False, True, float(np.float32(1e-6)), None))
 
 
+@pytest.mark.parametrize("d", [128, 64])
+def test_large_eps(dkv, d):
+    """An eps of the squares' own size, also where their sum passes fp32."""
+    g, theta, coord, w = inputs(9, d, [d // 2], 24)
+    eps = float(np.float32(1e37))
+    how = dkv.NormRope(d, f32(theta), eps=eps, k_weight=f32(w[1]))
+    x = cache_ref.bf16(g.standard_normal((3, 24, d)) * np.exp2(g.integers(54, 68, (3, 24, 1))))
+    for x0, y, wt in zip((x, x), dkv.norm_rope(bf(x), bf(x), how, t32(coord)), (None, w[1])):
+        ref.check_rows(y, *ref.norm_rope(x0, coord, theta, [d // 2], False, True, eps, wt))
+
+
 @pytest.mark.parametrize("half", [False, True])
 def test_extreme_rows(dkv, half):
     """Squares beyond fp32, zeros, tiny numbers, infinities and NaN, each row by itself."""
