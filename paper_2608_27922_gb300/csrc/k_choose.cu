@@ -259,7 +259,7 @@ __device__ __forceinline__ void biased4(uint32_t w, uint32_t& a, uint32_t& b) {
 // places t PER ..; counts of the keys in 256 even steps between the least and the largest, then in 256 steps of the one that the
 // top-th key lies in, and so on (two or three rounds as a rule), end at a bound with `top` keys above it, or at the top-th key
 // itself where others equal it.
-template <int PER>
+template <int THREADS, int PER>
 __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   uint32_t k[PER], least = 0xffffffffu, most = 0;
@@ -281,11 +281,11 @@ __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
     w.sums->hi[warp] = most;
     w.sums->total[warp] = valid;
   }
-  w.hist[tid] = 0;
+  for (int i = tid; i < 256; i += THREADS) w.hist[i] = 0;
   __syncthreads();
   valid = 0;
 #pragma unroll
-  for (int x = 0; x < CH_THREADS / 32; ++x) {
+  for (int x = 0; x < THREADS / 32; ++x) {
     least = min(least, w.sums->lo[x]);
     most = max(most, w.sums->hi[x]);
     valid += w.sums->total[x];
@@ -344,7 +344,7 @@ __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
       }
       span = (1u << shift) - 1;
       shift = max(0, shift - 8);
-      w.hist[tid] = 0;
+      for (int i = tid; i < 256; i += THREADS) w.hist[i] = 0;
       __syncthreads();
     }
   }
@@ -367,7 +367,7 @@ __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
   __syncthreads();
   int before = incl - mine, all = 0;
 #pragma unroll
-  for (int x = 0; x < CH_THREADS / 32; ++x) {
+  for (int x = 0; x < THREADS / 32; ++x) {
     if (x < warp) before += w.sums->total[x];
     all += w.sums->total[x];
   }
@@ -386,9 +386,10 @@ __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
   if (tid == 0) w.sums->kept = (all & 0xffff) + min(all >> 16, need);
   __syncthreads();
 }
+template <int THREADS>
 __device__ __forceinline__ void keep_best(const Work& w, int n, int top) {
-  if (n <= 4 * CH_THREADS) keep_best<4>(w, n, top);
-  else keep_best<PLACES / CH_THREADS>(w, n, top);
+  if (THREADS < CH_THREADS || n <= 4 * THREADS) keep_best<THREADS, 4>(w, n, top);
+  else keep_best<THREADS, PLACES / THREADS>(w, n, top);
 }
 
 // One list: its tile of tokens and the pages that are listed anyway.
@@ -418,9 +419,10 @@ __device__ __forceinline__ Line line_of(const Pool& c, const Seqs& s, const Choo
 }
 
 // Pages k0 .. k0 + n - 1 looked up, behind the `kept` ones.
+template <int THREADS>
 __device__ __forceinline__ void look_up(const Pool& c, const Seqs& s, const Work& w, const Line& l, const uint8_t* scale, int h,
                                         int k0, int n, int kept) {
-  for (int i = threadIdx.x; i < n; i += CH_THREADS) {
+  for (int i = threadIdx.x; i < n; i += THREADS) {
     const int k = k0 + i;
     int page = s.table[(int64_t)l.b * s.max_pages + k];   // (negative: given back)
     if (page >= c.n_pages) {
@@ -436,7 +438,7 @@ __device__ __forceinline__ void look_up(const Pool& c, const Seqs& s, const Work
     w.page[kept + i] = k;
     reinterpret_cast<float*>(w.key)[kept + i] = -INFINITY;
   }
-  for (int i = threadIdx.x; i < kept; i += CH_THREADS) {
+  for (int i = threadIdx.x; i < kept; i += THREADS) {
     w.key[i] = w.kept_key[i];
     w.page[i] = w.kept_page[i];
   }
@@ -493,6 +495,7 @@ __device__ __forceinline__ float row_codes(const Job& j, const Line& l, int h, i
 }
 
 // The cluster's shares joined, and the list written: sinks, then the chosen pages and the local ones as they ascend.
+template <int THREADS>
 __device__ __forceinline__ void finish(const Work& w, const Line& l, int kept, int top, int32_t* line, int width) {
   cg::cluster_group cluster = cg::this_cluster();
   const int C = cluster.num_blocks(), rank = cluster.block_rank(), tid = threadIdx.x;
@@ -505,14 +508,14 @@ __device__ __forceinline__ void finish(const Work& w, const Line& l, int kept, i
         const uint32_t* key = cluster.map_shared_rank(w.kept_key, r);
         const int* page = cluster.map_shared_rank(w.kept_page, r);
         const int m2 = cluster.map_shared_rank(w.sums, r)->kept;
-        for (int i = tid; i < m2; i += CH_THREADS) {
+        for (int i = tid; i < m2; i += THREADS) {
           w.key[n + i] = key[i];
           w.page[n + i] = page[i];
         }
         n += m2;
       }
       __syncthreads();
-      keep_best(w, n, top);
+      keep_best<THREADS>(w, n, top);
       kept = w.sums->kept;
     }
     cluster.sync();
@@ -525,18 +528,18 @@ __device__ __forceinline__ void finish(const Work& w, const Line& l, int kept, i
     if (w.kept_page[mid] < l0) before = mid + 1; else z = mid;
   }
   const int count = l.sinks + kept + locals;
-  for (int i = tid; i < l.sinks; i += CH_THREADS) line[i] = i;
-  for (int i = tid; i < locals; i += CH_THREADS) line[l.sinks + before + i] = l0 + i;
-  for (int i = tid; i < kept; i += CH_THREADS) line[l.sinks + i + (i < before ? 0 : locals)] = w.kept_page[i];
-  for (int i = count + tid; i < width; i += CH_THREADS) line[i] = -1;
+  for (int i = tid; i < l.sinks; i += THREADS) line[i] = i;
+  for (int i = tid; i < locals; i += THREADS) line[l.sinks + before + i] = l0 + i;
+  for (int i = tid; i < kept; i += THREADS) line[l.sinks + i + (i < before ? 0 : locals)] = w.kept_page[i];
+  for (int i = count + tid; i < width; i += THREADS) line[i] = -1;
 }
 
-// Cluster: one list (slot blockIdx.x / CTAs of the cluster, head blockIdx.y); its CTAs share the seen pages.  Few query
-// rows (a single token's group): mma.sync, the rows its 16, the pages its 8 columns.
+// Cluster: one list (slot blockIdx.x / CTAs of the cluster, head blockIdx.y); its CTAs share the seen pages.  (CTAs of fewer
+// threads hold up to 4 pages a thread, and come without a cluster.)  Few query rows (a single token's group): mma.sync, the rows its 16, the pages its 8 columns.
 constexpr int FEW = 16;
 
-template <int D>
-__global__ void __launch_bounds__(CH_THREADS, 3) choose(const __grid_constant__ Job j) {
+template <int D, int THREADS>
+__global__ void __launch_bounds__(THREADS, 3 * (CH_THREADS / THREADS)) choose(const __grid_constant__ Job j) {
   constexpr int STRIDE = D + 4;   // halves of a row: 8-byte reads of 4 lanes x 4 rows touch every bank once
   extern __shared__ __align__(16) uint8_t raw[];
   __half* qs = reinterpret_cast<__half*>(raw);                              // [FEW][STRIDE]
@@ -547,12 +550,12 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose(const __grid_constant__ 
   const int slot = blockIdx.x / C, h = blockIdx.y, slots = gridDim.x / C;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
   if (blockIdx.x == 0 && h == 0)
-    for (int b = tid; b < j.s.n; b += CH_THREADS) seq_at(c, j.s, b);
+    for (int b = tid; b < j.s.n; b += THREADS) seq_at(c, j.s, b);
   const Line l = line_of(c, j.s, j.how, slot);
   int32_t* line = j.lists + ((int64_t)h * slots + slot) * j.how.width;
   if (!l.any) {   // (the whole cluster)
     if (rank == 0)
-      for (int k = tid; k < j.how.width; k += CH_THREADS) line[k] = -1;
+      for (int k = tid; k < j.how.width; k += THREADS) line[k] = -1;
     return;
   }
   const int R = l.m * j.G;   // <= FEW
@@ -560,7 +563,7 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose(const __grid_constant__ 
   const int per = (l.whole + C - 1) / C, a = min(rank * per, l.whole), z = min(a + per, l.whole);
   int kept = 0;
   if (j.how.top > 0) {
-    for (int r = warp; r < FEW; r += CH_THREADS / 32) {
+    for (int r = warp; r < FEW; r += THREADS / 32) {
       float x[D / 32];
       const float u = row_codes<D>(j, l, h, r, R, x);
 #pragma unroll
@@ -570,7 +573,7 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose(const __grid_constant__ 
 #pragma unroll 1
     for (int k0 = a; k0 < z; k0 += j.z.cap) {
       const int n = min(j.z.cap, z - k0);
-      look_up(c, j.s, w, l, j.scale, h, k0, n, kept);
+      look_up<THREADS>(c, j.s, w, l, j.scale, h, k0, n, kept);
       __syncthreads();
       // eight pages a warp: page i + g's codes, 16 bytes at 16 t (and at 64 + 16 t), the next eight's on their way
       auto codes = [&](int i, uint4 (&v)[D / 64]) {
@@ -583,7 +586,7 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose(const __grid_constant__ 
       codes(warp * 8, v);
       const float u0 = unit[g], u1 = unit[g + 8];
 #pragma unroll 1
-      for (int i0 = warp * 8; i0 < n; i0 += CH_THREADS / 32 * 8) {
+      for (int i0 = warp * 8; i0 < n; i0 += THREADS / 32 * 8) {
         uint32_t B[D / 8];
 #pragma unroll
         for (int x = 0; x < D / 64; ++x) {
@@ -592,7 +595,7 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose(const __grid_constant__ 
           widen4(v[x].z, B[8 * x + 4], B[8 * x + 5]);
           widen4(v[x].w, B[8 * x + 6], B[8 * x + 7]);
         }
-        codes(i0 + CH_THREADS / 32 * 8, v);
+        codes(i0 + THREADS / 32 * 8, v);
         float acc[4] = {0.f, 0.f, 0.f, 0.f}, ac2[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < D / 16; ++i) {
@@ -619,11 +622,11 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose(const __grid_constant__ 
         }
       }
       __syncthreads();
-      keep_best(w, kept + n, j.how.top);
+      keep_best<THREADS>(w, kept + n, j.how.top);
       kept = w.sums->kept;
     }
   }
-  finish(w, l, kept, j.how.top, line, j.how.width);
+  finish<THREADS>(w, l, kept, j.how.top, line, j.how.width);
 }
 
 // The same for many query rows on the tensor cores, turned round: 128 pages are the rows of tcgen05.mma, 64 query rows its
@@ -690,7 +693,7 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant
 #pragma unroll 1
     for (int k0 = a; ok && k0 < z; k0 += j.z.cap) {
       const int n = min(j.z.cap, z - k0);
-      look_up(c, j.s, w, l, j.scale, h, k0, n, kept);
+      look_up<CH_THREADS>(c, j.s, w, l, j.scale, h, k0, n, kept);
       float* score = half ? w.other : reinterpret_cast<float*>(w.key) + kept;
 #pragma unroll 1
       for (int r0 = 0; ok && r0 < R; r0 += 64) {
@@ -795,7 +798,7 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant
         w.key[kept + i] = w.scale[i] != 0.f && x > -INFINITY ? key_of(x * w.scale[i]) : 0;
       }
       __syncthreads();
-      keep_best(w, kept + n, j.how.top);
+      keep_best<CH_THREADS>(w, kept + n, j.how.top);
       kept = w.sums->kept;
     }
   }
@@ -805,7 +808,7 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant
     fence_after_sync();
     tmem_dealloc(tmem, CH_TMEM);
   }
-  finish(w, l, kept, j.how.top, line, j.how.width);
+  finish<CH_THREADS>(w, l, kept, j.how.top, line, j.how.width);
 }
 
 }  // namespace
@@ -822,15 +825,17 @@ size_t tc_bytes(const Sizes& z) {
 template <int D>
 cudaError_t choose_limits() {
   const Sizes z{CAP, PLACES, MAX_TOP};
-  cudaError_t e = taken(cudaFuncSetAttribute(choose<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes<D>(z)));
+  cudaError_t e = taken(cudaFuncSetAttribute(choose<D, CH_THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes<D>(z)));
   if (e == cudaSuccess)
     e = taken(cudaFuncSetAttribute(choose_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_bytes<D>(z)));
   return e;
 }
 template <int D>
-cudaError_t launch_choose_d(const Job& job, int slots, int C, bool few, cudaStream_t st) {
+cudaError_t launch_choose_d(const Job& job, int slots, int C, bool few, int threads, cudaStream_t st) {
   const dim3 grid(slots * C, job.c.H);
-  if (few) return launch_kernel(choose<D>, grid, CH_THREADS, few_bytes<D>(job.z), C, false, st, job);
+  if (few && threads == 32) return launch_kernel(choose<D, 32>, grid, 32, few_bytes<D>(job.z), 1, false, st, job);
+  if (few && threads == 64) return launch_kernel(choose<D, 64>, grid, 64, few_bytes<D>(job.z), 1, false, st, job);
+  if (few) return launch_kernel(choose<D, CH_THREADS>, grid, CH_THREADS, few_bytes<D>(job.z), C, false, st, job);
   return launch_kernel(choose_tc<D>, grid, CH_THREADS, tc_bytes<D>(job.z), C, false, st, job);
 }
 }  // namespace
@@ -868,7 +873,11 @@ cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, cons
   const Job job{c, s, code, scale, q, G, (uint32_t)((0x100000000ull + G - 1) / G), how, lists, z};
   // (32 tokens of 5 or of 16 rows: the kernel for few rows 21 us, the other 26)
   const bool few = (int64_t)std::min(how.tile, s.rows) * G <= FEW;
-  return c.d == 128 ? launch_choose_d<128>(job, slots, C, few, st) : launch_choose_d<64>(job, slots, C, few, st);
+  // many short lists: a warp or two each, so that 24 or 12 run on an SM instead of 3 (47,888 lists of up to 94 pages 160 us with one warp, 221
+  // with two, 554 with eight; 3,200 of up to 146 62 with two, 91 with eight; 480 18.7 and 20.6, 256 18.5 and 16.5)
+  int threads = CH_THREADS;
+  if (C == 1 && lines > 3 * n_sm) threads = z.places <= 4 * 32 ? 32 : z.places <= 4 * 64 ? 64 : CH_THREADS;
+  return c.d == 128 ? launch_choose_d<128>(job, slots, C, few, threads, st) : launch_choose_d<64>(job, slots, C, few, threads, st);
 }
 
 }  // namespace cache

@@ -147,6 +147,23 @@ def test_many_sequences(dkv, fmt, d, count):
     c.sync()
 
 
+@pytest.mark.parametrize("pages,top", [(100, 28), (101, 28), (200, 56), (201, 56), (230, 1)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_lists(dkv, d, pages, top):
+    """480 lists of about as many pages as a CTA of a warp, of two or of eight looks at; many scores are equal."""
+    g = np.random.default_rng(pages)
+    seqs = [(1, int(g.integers(1, 16 * pages + 1))) for _ in range(119)] + [(1, 16 * pages)]
+    case = cache_ref.Case(seqs, 4, d, 16, "bf16", seed=6)
+    s, c = case.device_seqs(dkv), case.cache(dkv)
+    code = g.integers(-2, 3, (case.n_pages, 4, d)).astype(np.int8)
+    scale = g.integers(120, 123, (case.n_pages, 4)).astype(np.uint8)
+    sums = dkv.Summaries(c, torch.from_numpy(code).cuda(), torch.from_numpy(scale).cuda())
+    Q = np.round(queries(case, 12)) * 0.5
+    lists = c.choose(bf(Q), s, sums, top)
+    assert np.array_equal(lists.cpu().numpy(), ref.choose(case, Q, code, scale, top, 1, 1, 1, 2, lists.shape[-1]))
+    c.sync()
+
+
 def test_pages_given_back(dkv):
     """Pages that a window has left are neither summarised nor listed, and are no error."""
     case = cache_ref.Case([(2, 16 * 20)], 2, 64, 16, "bf16", seed=8)
