@@ -9,8 +9,8 @@
 //
 // Bound by latency: 32 tokens of 40 heads over up to 469 pages take 21 us in a graph (summaries 9, choice 16 by themselves), a chain of
 // reads (sequence, table, scale, codes), three rounds of counting and two launches.  A block of 4,680 tokens in
-// tiles of 64 over 732 pages, 12 heads: 57 us, 53 of them the choice: widening the codes for each tile of tokens 23 (shared memory is
-// 50% busy, 33 KB in and out a tile of 128 pages), the queries' codes 9, looking for the best 48 4, the start of 888 CTAs and the
+// tiles of 64 over 732 pages, 12 heads: 55.5 us, 52 of them the choice: widening the codes for each tile of tokens 23 (shared memory is
+// 50% busy, 33 KB in and out a tile of 128 pages), the queries' codes, looking for the best 48 4, the start of 888 CTAs and the
 // summaries the rest.
 #include "attn_math.cuh"
 #include "cache_internal.h"
@@ -457,34 +457,29 @@ struct Job {
   Sizes z;
 };
 
-// A warp's query row r of the tile (row = token * G + head): lane's D / 32 numbers as whole ones, its exponent's power of
-// two (0: no codes).
+// A warp's query row r of the tile (row = token * G + head), lane's D / 32 numbers of it; a row behind the last: infinities.
 template <int D>
-__device__ __forceinline__ float row_codes(const Job& j, const Line& l, int h, int r, int R, float (&x)[D / 32]) {
+__device__ __forceinline__ uint2 row_load(const Job& j, const Line& l, int h, int r, int R) {
   const int lane = threadIdx.x & 31;
   const Packed& qp = j.q;
-  uint32_t top = 0x7f800000u;   // (a row behind the last has none)
-  if (r < R) {
-    const int i = j.G == 1 ? r : (int)__umulhi((uint32_t)r, j.g_inverse), hq = h * j.G + r - i * j.G;
-    const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(qp.p) + hq * qp.head + (int64_t)(l.q.r0 + l.i0 + i) * qp.row + lane * (D / 32);
-    if (D == 128) {
-      const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
-      x[0] = __uint_as_float(v.x << 16);
-      x[1] = __uint_as_float(v.x & 0xffff0000u);
-      x[D / 32 - 2] = __uint_as_float(v.y << 16);
-      x[D / 32 - 1] = __uint_as_float(v.y & 0xffff0000u);
-    } else {
-      const uint32_t v = __ldg(reinterpret_cast<const uint32_t*>(p));
-      x[0] = __uint_as_float(v << 16);
-      x[1] = __uint_as_float(v & 0xffff0000u);
-    }
-    top = 0;   // (bits of magnitudes order like the magnitudes, NaN above infinity)
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
-  } else {
-#pragma unroll
-    for (int k = 0; k < D / 32; ++k) x[k] = 0.f;
+  if (r >= R) return make_uint2(0x7f807f80u, 0x7f807f80u);
+  const int i = j.G == 1 ? r : (int)__umulhi((uint32_t)r, j.g_inverse), hq = h * j.G + r - i * j.G;
+  const __nv_bfloat16* p = static_cast<const __nv_bfloat16*>(qp.p) + hq * qp.head + (int64_t)(l.q.r0 + l.i0 + i) * qp.row + lane * (D / 32);
+  if (D == 128) return __ldg(reinterpret_cast<const uint2*>(p));
+  return make_uint2(__ldg(reinterpret_cast<const uint32_t*>(p)), 0u);
+}
+// The numbers as whole ones, and the row's power of two (0: no codes).
+template <int D>
+__device__ __forceinline__ float row_codes(const uint2& v, float (&x)[D / 32]) {
+  x[0] = __uint_as_float(v.x << 16);
+  x[1] = __uint_as_float(v.x & 0xffff0000u);
+  if (D == 128) {
+    x[D / 32 - 2] = __uint_as_float(v.y << 16);
+    x[D / 32 - 1] = __uint_as_float(v.y & 0xffff0000u);
   }
+  uint32_t top = 0;   // (bits of magnitudes order like the magnitudes, NaN above infinity)
+#pragma unroll
+  for (int k = 0; k < D / 32; ++k) top = max(top, __float_as_uint(x[k]) & 0x7fffffffu);
   top = __reduce_max_sync(0xffffffffu, top);
   const bool fine = top < __float_as_uint(WILD);
   const int e = fine ? exponent_of(__uint_as_float(top)) : 0;
@@ -563,9 +558,9 @@ __global__ void __launch_bounds__(THREADS, 3 * (CH_THREADS / THREADS)) choose(co
   const int per = (l.whole + C - 1) / C, a = min(rank * per, l.whole), z = min(a + per, l.whole);
   int kept = 0;
   if (j.how.top > 0) {
-    for (int r = warp; r < FEW; r += THREADS / 32) {
+    for (int r = warp; r < FEW; r += THREADS / 32) {   // (their codes made after the pages are looked up: 47,888 lists 170 us, 160 so)
       float x[D / 32];
-      const float u = row_codes<D>(j, l, h, r, R, x);
+      const float u = row_codes<D>(row_load<D>(j, l, h, r, R), x);
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) qs[r * STRIDE + lane * (D / 32) + k] = __float2half_rn(x[k]);
       if (lane == 0) unit[r] = u;
@@ -629,25 +624,25 @@ __global__ void __launch_bounds__(THREADS, 3 * (CH_THREADS / THREADS)) choose(co
   finish<THREADS>(w, l, kept, j.how.top, line, j.how.width);
 }
 
-// The same for many query rows on the tensor cores, turned round: 128 pages are the rows of tcgen05.mma, 64 query rows its
+// The same for many query rows on the tensor cores, turned round: 128 pages are the rows of tcgen05.mma, 64 or 128 query rows its
 // columns, so that a thread's part of the result is one page, whose best score it finds by itself.  Two halves of the
 // threads take half of the query rows each.  Codes are widened to fp16 by all threads; a tile's product runs
 // while the last one's result is looked through.
-template <int D>
+template <int D, int ROWS>
 struct TcLay {
   static constexpr int NP = D / 64;
   static constexpr int A = 0;                            // [NP][128 pages][64] swizzled
-  static constexpr int B = NP * 128 * 128;               // [NP][64 rows][64]
-  static constexpr int UNIT = B + NP * 64 * 128;         // [64] 2^e, [64] 0 or -inf
-  static constexpr int CTRL = UNIT + 512;
+  static constexpr int B = NP * 128 * 128;               // [NP][ROWS][64]
+  static constexpr int UNIT = B + NP * ROWS * 128;             // [ROWS] 2^e, [ROWS] 0 or -inf
+  static constexpr int CTRL = UNIT + 8 * ROWS;
   static constexpr int WORK = CTRL + 32;
 };
-constexpr uint32_t CH_TMEM = 128;   // two results of 64 columns
 
-template <int D>
-__global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant__ Job j) {
+template <int D, int ROWS>
+__global__ void __launch_bounds__(CH_THREADS, ROWS == 64 ? 3 : 2) choose_tc(const __grid_constant__ Job j) {
   using namespace tc;
-  using L = TcLay<D>;
+  using L = TcLay<D, ROWS>;
+  constexpr uint32_t TMEM = 2 * ROWS;   // columns: two results
   extern __shared__ __align__(1024) uint8_t tile[];
   const Work w = work_in(tile + L::WORK, j.z);
   float* unit = reinterpret_cast<float*>(tile + L::UNIT);
@@ -674,12 +669,12 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant
     mbar_init(done, 1);
     fence_barrier_init();
   }
-  if (warp == 0) tmem_alloc(holder, CH_TMEM);
+  if (warp == 0) tmem_alloc(holder, TMEM);
   fence_before_sync();
   __syncthreads();
   fence_after_sync();
   const uint32_t tmem = *holder;
-  constexpr uint32_t idesc = idesc_bf16(128, 64) & ~((1u << 7) | (1u << 10));   // fp16
+  constexpr uint32_t idesc = idesc_bf16(128, ROWS) & ~((1u << 7) | (1u << 10));   // fp16
   const uint64_t ad = desc_sw128(smem_u32(tile + L::A)), bd = desc_sw128(smem_u32(tile + L::B));
   const int R = l.m * j.G;
   const int per = (l.whole + C - 1) / C, a = min(rank * per, l.whole), z = min(a + per, l.whole);
@@ -693,33 +688,18 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant
 #pragma unroll 1
     for (int k0 = a; ok && k0 < z; k0 += j.z.cap) {
       const int n = min(j.z.cap, z - k0);
-      look_up<CH_THREADS>(c, j.s, w, l, j.scale, h, k0, n, kept);
       float* score = half ? w.other : reinterpret_cast<float*>(w.key) + kept;
 #pragma unroll 1
-      for (int r0 = 0; ok && r0 < R; r0 += 64) {
-        // (the products that read the last rows are complete)
-#pragma unroll 4
-        for (int r = warp; r < 64; r += CH_THREADS / 32) {
-          float x[D / 32];
-          const float u = row_codes<D>(j, l, h, r0 + r, R, x);
-          const int col = lane * (D / 32), at = (col >> 6) * (64 * 128) + r * 128 + ((((col & 63) >> 3) ^ (r & 7)) << 4) + (col & 7) * 2;
-          const __half2 y = __floats2half2_rn(x[0], x[1]);
-          if (D == 128) {
-            const __half2 y2 = __floats2half2_rn(x[D / 32 - 2], x[D / 32 - 1]);
-            *reinterpret_cast<uint2*>(tile + L::B + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&y), *reinterpret_cast<const uint32_t*>(&y2));
-          } else {
-            *reinterpret_cast<uint32_t*>(tile + L::B + at) = *reinterpret_cast<const uint32_t*>(&y);
-          }
-          float sum = 0.f;   // (whole numbers)
+      for (int r0 = 0; ok && r0 < R; r0 += ROWS) {
+        // rows, then the pages, then their first codes are asked for before the rows' codes are made
+        constexpr int PER = 8;   // of a warp in one go
+        uint2 rows[PER];
 #pragma unroll
-          for (int k = 0; k < D / 32; ++k) sum += x[k];
-          sum = (float)__reduce_add_sync(0xffffffffu, (int)sum);
-          if (lane == 0) {
-            unit[r] = u * 0x1p24f;
-            unit[64 + r] = u != 0.f ? -128.f * sum * u : -INFINITY;
-          }
+        for (int k = 0; k < PER; ++k) rows[k] = row_load<D>(j, l, h, r0 + warp + k * (CH_THREADS / 32), R);
+        if (r0 == 0) {
+          look_up<CH_THREADS>(c, j.s, w, l, j.scale, h, k0, n, kept);
+          __syncthreads();
         }
-        __syncthreads();   // (the pages are looked up, too)
         // 16-byte parts of a tile's codes: eight threads take four parts (64 columns) of two neighbouring rows, so that their
         // stores, swizzled by the row, touch every bank once
         constexpr int V = 128 * (D / 16) / CH_THREADS, STEP = CH_THREADS / 4 / L::NP;
@@ -732,24 +712,55 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant
             v[k] = at >= 0 ? __ldg(reinterpret_cast<const uint4*>(from + (int64_t)at * (c.H * D))) : make_uint4(0, 0, 0, 0);
           }
         };
-        auto look = [&](int i0, uint32_t buf) {   // the best of the half's 32 rows for this thread's page
-          if (half * 32 >= R - r0) return;
-          float x[32];
-          tmem_ld32(tmem + lane_off + buf * 64 + half * 32, x);
-          tmem_wait_ld();
-          float best = -INFINITY;
+        uint4 v[V];
+        codes(0, v);
+        // (the products that read the last rows are complete, and nobody looks through their result any more)
+#pragma unroll 1
+        for (int k0 = 0;; k0 += PER) {
 #pragma unroll
-          for (int k = 0; k < 32; k += 4) {
-            const float4 u = *reinterpret_cast<const float4*>(unit + half * 32 + k), o = *reinterpret_cast<const float4*>(unit + 64 + half * 32 + k);
-            const float2 y = __ffma2_rn(make_float2(x[k], x[k + 1]), make_float2(u.x, u.y), make_float2(o.x, o.y));
-            const float2 y2 = __ffma2_rn(make_float2(x[k + 2], x[k + 3]), make_float2(u.z, u.w), make_float2(o.z, o.w));
-            best = max3(max3(best, y.x, y.y), y2.x, y2.y);
+          for (int k = 0; k < PER; ++k) {
+            const int r = warp + (k0 + k) * (CH_THREADS / 32);
+            float x[D / 32];
+            const float u = row_codes<D>(rows[k], x);
+            const int col = lane * (D / 32), at = (col >> 6) * (ROWS * 128) + r * 128 + ((((col & 63) >> 3) ^ (r & 7)) << 4) + (col & 7) * 2;
+            const __half2 y = __floats2half2_rn(x[0], x[1]);
+            if (D == 128) {
+              const __half2 y2 = __floats2half2_rn(x[D / 32 - 2], x[D / 32 - 1]);
+              *reinterpret_cast<uint2*>(tile + L::B + at) = make_uint2(*reinterpret_cast<const uint32_t*>(&y), *reinterpret_cast<const uint32_t*>(&y2));
+            } else {
+              *reinterpret_cast<uint32_t*>(tile + L::B + at) = *reinterpret_cast<const uint32_t*>(&y);
+            }
+            float sum = 0.f;   // (whole numbers)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) sum += x[i];
+            sum = (float)__reduce_add_sync(0xffffffffu, (int)sum);
+            if (lane == 0) {
+              unit[r] = u * 0x1p24f;
+              unit[ROWS + r] = u != 0.f ? -128.f * sum * u : -INFINITY;
+            }
+          }
+          if (k0 + PER >= ROWS / (CH_THREADS / 32)) break;
+#pragma unroll
+          for (int k = 0; k < PER; ++k) rows[k] = row_load<D>(j, l, h, r0 + warp + (k0 + PER + k) * (CH_THREADS / 32), R);
+        }
+        auto look = [&](int i0, uint32_t buf) {   // the best of the half's rows for this thread's page
+          float best = -INFINITY;
+#pragma unroll 1
+          for (int k0 = half * (ROWS / 2); k0 < (half + 1) * (ROWS / 2) && k0 < R - r0; k0 += 32) {
+            float x[32];
+            tmem_ld32(tmem + lane_off + buf * ROWS + k0, x);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < 32; k += 4) {
+              const float4 u = *reinterpret_cast<const float4*>(unit + k0 + k), o = *reinterpret_cast<const float4*>(unit + ROWS + k0 + k);
+              const float2 y = __ffma2_rn(make_float2(x[k], x[k + 1]), make_float2(u.x, u.y), make_float2(o.x, o.y));
+              const float2 y2 = __ffma2_rn(make_float2(x[k + 2], x[k + 3]), make_float2(u.z, u.w), make_float2(o.z, o.w));
+              best = max3(max3(best, y.x, y.y), y2.x, y2.y);
+            }
           }
           const int i = i0 + (warp & 3) * 32 + lane;
           if (i < n) score[i] = fmaxf(score[i], best);
         };
-        uint4 v[V];
-        codes(0, v);
         uint32_t buf = 0;
 #pragma unroll 1
         for (int i0 = 0; ok && i0 < n; i0 += 128, buf ^= 1) {
@@ -773,8 +784,8 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant
             if (elect_one()) {
 #pragma unroll
               for (int kk = 0; kk < D / 16; ++kk)
-                mma_bf16(tmem + buf * 64, desc_add(ad, (kk >> 2) * (128 * 128) + (kk & 3) * 32),
-                         desc_add(bd, (kk >> 2) * (64 * 128) + (kk & 3) * 32), idesc, kk > 0);
+                mma_bf16(tmem + buf * ROWS, desc_add(ad, (kk >> 2) * (128 * 128) + (kk & 3) * 32),
+                         desc_add(bd, (kk >> 2) * (ROWS * 128) + (kk & 3) * 32), idesc, kk > 0);
               mma_commit(done);
             }
             __syncwarp();
@@ -806,7 +817,7 @@ __global__ void __launch_bounds__(CH_THREADS, 3) choose_tc(const __grid_constant
   __syncthreads();
   if (warp == 0) {
     fence_after_sync();
-    tmem_dealloc(tmem, CH_TMEM);
+    tmem_dealloc(tmem, TMEM);
   }
   finish<CH_THREADS>(w, l, kept, j.how.top, line, j.how.width);
 }
@@ -818,16 +829,18 @@ template <int D>
 size_t few_bytes(const Sizes& z) {
   return FEW * (D + 4) * 2 + FEW * 4 + work_bytes(z);
 }
-template <int D>
+template <int D, int ROWS>
 size_t tc_bytes(const Sizes& z) {
-  return TcLay<D>::WORK + work_bytes(z);
+  return TcLay<D, ROWS>::WORK + work_bytes(z);
 }
 template <int D>
 cudaError_t choose_limits() {
   const Sizes z{CAP, PLACES, MAX_TOP};
   cudaError_t e = taken(cudaFuncSetAttribute(choose<D, CH_THREADS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)few_bytes<D>(z)));
   if (e == cudaSuccess)
-    e = taken(cudaFuncSetAttribute(choose_tc<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_bytes<D>(z)));
+    e = taken(cudaFuncSetAttribute(choose_tc<D, 64>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_bytes<D, 64>(z)));
+  if (e == cudaSuccess)
+    e = taken(cudaFuncSetAttribute(choose_tc<D, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)tc_bytes<D, 128>(z)));
   return e;
 }
 template <int D>
@@ -836,7 +849,11 @@ cudaError_t launch_choose_d(const Job& job, int slots, int C, bool few, int thre
   if (few && threads == 32) return launch_kernel(choose<D, 32>, grid, 32, few_bytes<D>(job.z), 1, false, st, job);
   if (few && threads == 64) return launch_kernel(choose<D, 64>, grid, 64, few_bytes<D>(job.z), 1, false, st, job);
   if (few) return launch_kernel(choose<D, CH_THREADS>, grid, CH_THREADS, few_bytes<D>(job.z), C, false, st, job);
-  return launch_kernel(choose_tc<D>, grid, CH_THREADS, tc_bytes<D>(job.z), C, false, st, job);
+  // More than 128 rows: 128 a product, so that the codes are widened half as often, but two CTAs an SM (4,680 tokens over 732 pages: 768
+  // rows 62 us, 101 by 64; 256 rows of d = 64 36 and 50; 320 rows 154 and 182; 128 rows 55 and 49).
+  if ((int64_t)std::min(job.how.tile, job.s.rows) * job.G > 128)
+    return launch_kernel(choose_tc<D, 128>, grid, CH_THREADS, tc_bytes<D, 128>(job.z), C, false, st, job);
+  return launch_kernel(choose_tc<D, 64>, grid, CH_THREADS, tc_bytes<D, 64>(job.z), C, false, st, job);
 }
 }  // namespace
 

@@ -123,6 +123,14 @@ def test_choose_large(dkv, H, Hq, seqs, page, top, tile):
     run_choose(dkv, case, Hq, top, tile, 1, 1, 2)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("H,Hq,tile", [(1, 3, 43), (2, 20, 128), (1, 9, 31), (3, 3, 128)])
+def test_choose_many_rows(dkv, d, H, Hq, tile):
+    """Tiles of 129, 1,280, 279 and 128 rows, and what is left of them at a sequence's end."""
+    case = cache_ref.Case([(130, 2300), (7, 3900), (0, 5), (50, 60)], H, d, 16, "bf16", seed=tile)
+    run_choose(dkv, case, Hq, 12, tile, 64, 1, 2)
+
+
 @pytest.mark.parametrize("fmt,d,count", [("bf16", 64, 1500), ("e4m3", 128, 500), ("bf16", 128, 500), ("e4m3", 64, 500)])
 def test_many_sequences(dkv, fmt, d, count):
     """Sequences of no, one or a few tokens: every tile is found, and nothing else is written."""
