@@ -633,11 +633,11 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
     if (t2 < j.TQ && t2 < tokens) {
       float M = -INFINITY, sum = 0.f;
       for (int x = 0; x < C; ++x) M = fmaxf(M, cluster.map_shared_rank(reinterpret_cast<float2*>(smem + L::STATS), x)[row].x);
-      float f[8];
+      float f[8];   // (0 times what is not finite is NaN, as it should be; a part that has seen nothing: -1)
       for (int x = 0; x < C; ++x) {
         const float2 y = cluster.map_shared_rank(reinterpret_cast<float2*>(smem + L::STATS), x)[row];
-        f[x] = y.x == -INFINITY && y.y == 0.f ? 0.f : y.x == M || y.x == -INFINITY ? 1.f : ex2(y.x - M);
-        sum = fmaf(f[x], y.y, sum);
+        f[x] = y.x == -INFINITY && y.y == 0.f ? -1.f : y.x == M || y.x == -INFINITY ? 1.f : ex2(y.x - M);
+        if (f[x] >= 0.f) sum = fmaf(f[x], y.y, sum);
       }
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
       __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + h2) * j.o.head +
@@ -645,7 +645,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
       for (int c = 0; c < cols; c += 8) {
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         for (int x = 0; x < C; ++x) {
-          if (f[x] == 0.f) continue;
+          if (f[x] < 0.f) continue;
           const float4* src = cluster.map_shared_rank(reinterpret_cast<float4*>(smem + L::JOIN), x) + ((g * cols + c) / 4) * BQ + row;
           const float4 a = src[0], z = src[BQ];
           v[0] = fmaf(f[x], a.x, v[0]); v[1] = fmaf(f[x], a.y, v[1]); v[2] = fmaf(f[x], a.z, v[2]); v[3] = fmaf(f[x], a.w, v[3]);

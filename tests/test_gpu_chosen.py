@@ -333,6 +333,30 @@ def test_scores_of_minus_infinity(dkv, tile):
     cache_ref.check(O, ref.attend(case, Q, lists, tile))
 
 
+@pytest.mark.parametrize("first", [640, 2560])
+@pytest.mark.parametrize("tile", [1, 33])
+def test_infinite_value_far_below_the_largest_score(dkv, tile, first):
+    """A weight too small for fp32 in front of a value that is not finite: the output is not finite there, and right elsewhere."""
+    case = cache_ref.Case([(33, 3300)], 1, 64, 16, "bf16", seed=3)
+    for pos in range(3300):
+        at = case.table[0, pos // 16], 0, pos % 16
+        case.k[at] = 0.0
+        case.k[at][0] = 8.0 if (pos < 640 if first == 640 else pos >= first) else -8.0
+    case.v[case.table[0, 125], 0, 3, 7] = -np.inf
+    case.v[case.table[0, 2], 0, 9, 20] = np.nan if first != 640 else 5.0
+    c, s = case.cache(dkv), case.device_seqs(dkv)
+    Q = np.zeros((1, 33, 64))
+    Q[..., 0] = 40.0
+    lists = np.full((1, 33 // tile + 1, 190), -1, np.int32)
+    lists[0, :, :] = np.arange(190)
+    O = c.attend_chosen(bf(Q), s, t32(lists), tile=tile, scale=1.0).double().cpu().numpy()
+    want = ref.attend(case, Q, lists, tile, scale=1.0)
+    for (h, row), (o, tol) in want.items():
+        fine = np.isfinite(o)
+        assert not fine.all() and not np.isfinite(O[h, row][~fine]).any()
+        assert (np.abs(O[h, row][fine] - o[fine]) <= tol[fine]).all()
+
+
 @pytest.mark.parametrize("tile", [1, 32])
 def test_scale_strides_and_rows_behind(dkv, tile):
     case = cache_ref.Case([(33, 60), (2, 90)], 2, 128, 16, "bf16", seed=4)
