@@ -587,7 +587,7 @@ size_t dkv_cache_attend_scratch_size(dkv_cache_t cache, int32_t n_seq, int32_t H
  * A token that sees no position (a negative position of its own, an empty sequence) gets
  * zeros, and so does one whose scores are all -infinity.  Rows from row_start[n_seq] on are left as they were.  What lies in places that a
  * token does not see, NaN and infinities too, does not reach its output; a value that is not
- * finite in a place that it does see makes its output infinite or NaN.  Scores, sums and
+ * finite in a place that it does see makes its output infinite or NaN (where its score is -infinity it may).  Scores, sums and
  * outputs are held in fp32; the weights are rounded to bf16 before they meet the values.  (Over an e4m3
  * cache a call of few rows meets its keys with queries in fp16, each row times a power of two: of a row's elements those
  * smaller than 2^-24 of its largest magnitude are rounded, to within 2^-32 of that.)
@@ -730,7 +730,8 @@ typedef struct {
 /* O[h][i] = sum_j softmax_j(scale Q[h][i] . K[j]) V[j] over the positions j < end(p) on the pages that lists[h / (H_q / H)]
  * names for the token's tile (a list ends at its first negative entry).  Arguments, numbers that are not
  * finite, rows that see nothing and rounding as in dkv_cache_attend, the few-row rounding of queries over an e4m3 cache among it
- * (where a tile's tokens and the group's heads make at most 16 rows); a place whose score is -infinity counts as not seen.  Entries that do not ascend or lie
+ * (where a tile's tokens and the group's heads make at most 16 rows).  A value that is not finite in a place that a token sees makes
+ * its output infinite or NaN whatever the score, -infinity too; a token whose scores are all -infinity gets zeros otherwise.  Entries that do not ascend or lie
  * behind the sequence's last page set the error word (DKV_ERR_DEVICE); what the tile's tokens get is then unspecified.  */
 dkv_status_t dkv_cache_attend_chosen(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const void* Q, int32_t H_q,
                                      int32_t rows, int64_t q_head_stride, int64_t q_row_stride, void* O,

@@ -480,7 +480,7 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
     }
   }
   __syncthreads();
-  // a part of weight: something was seen, or a NaN
+  // (a part that has seen nothing adds zeros; one whose scores are all -infinity the values that are not finite)
   auto join = [&](auto at, int n, float& M, float& L, float (&x)[D / 32]) {
     M = -INFINITY;
     L = 0.f;
@@ -490,7 +490,6 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
     for (int i = 0; i < n; ++i) {
       const float* y = at(i);
       const float mi = y[D], li = y[D + 1];
-      if (mi == -INFINITY && li == 0.f) continue;
       const float f = mi == M || mi == -INFINITY ? 1.f : ex2(mi - M);
       L = fmaf(f, li, L);
 #pragma unroll

@@ -512,8 +512,8 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
     if (!ok && lane == 0) give_up(2);
     // ---- outputs, or a part of them into the tiles' place
     if (ok) {
-      const bool fix = *wild != 0 && l != 0.f;
-      const float f = C > 1 ? 1.f : l == 0.f ? 0.f : 1.0f / l;         // (a NaN stays one)
+      const bool fix = *wild != 0;
+      const float f = C > 1 ? 1.f : l == 0.f ? 0.f : 1.0f / l;         // (a NaN stays one; what is not finite shows where all weights are 0 too)
 #pragma unroll 1
       for (int c = 0; c < D / 32; ++c) {
         float v[32];
@@ -522,7 +522,7 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
           tmem_wait_ld();
         }
 #pragma unroll
-        for (int k = 0; k < 32; ++k) v[k] = n > 0 && l != 0.f ? v[k] * f : 0.f;
+        for (int k = 0; k < 32; ++k) v[k] = n > 0 ? fmaf(v[k], f, 0.f) : 0.f;
         if (fix) {
           const Wild w = wild_in<D, E4M3>(j.c, keys, h, max(t0 * BK, whole_to / BK * BK), t1 * BK, end, c * 32);
 #pragma unroll
@@ -633,11 +633,12 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
     if (t2 < j.TQ && t2 < tokens) {
       float M = -INFINITY, sum = 0.f;
       for (int x = 0; x < C; ++x) M = fmaxf(M, cluster.map_shared_rank(reinterpret_cast<float2*>(smem + L::STATS), x)[row].x);
-      float f[8];   // (0 times what is not finite is NaN, as it should be; a part that has seen nothing: -1)
+      float f[8];   // (0 times what is not finite is NaN, as it should be; a part that has seen nothing adds zeros, one whose
+                    // scores are all -infinity the values that are not finite)
       for (int x = 0; x < C; ++x) {
         const float2 y = cluster.map_shared_rank(reinterpret_cast<float2*>(smem + L::STATS), x)[row];
-        f[x] = y.x == -INFINITY && y.y == 0.f ? -1.f : y.x == M || y.x == -INFINITY ? 1.f : ex2(y.x - M);
-        if (f[x] >= 0.f) sum = fmaf(f[x], y.y, sum);
+        f[x] = y.x == M || y.x == -INFINITY ? 1.f : ex2(y.x - M);
+        sum = fmaf(f[x], y.y, sum);
       }
       const float inv = sum == 0.f ? 0.f : 1.0f / sum;
       __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(j.o.p) + (int64_t)(h * j.G + h2) * j.o.head +
@@ -645,7 +646,6 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
       for (int c = 0; c < cols; c += 8) {
         float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         for (int x = 0; x < C; ++x) {
-          if (f[x] < 0.f) continue;
           const float4* src = cluster.map_shared_rank(reinterpret_cast<float4*>(smem + L::JOIN), x) + ((g * cols + c) / 4) * BQ + row;
           const float4 a = src[0], z = src[BQ];
           v[0] = fmaf(f[x], a.x, v[0]); v[1] = fmaf(f[x], a.y, v[1]); v[2] = fmaf(f[x], a.z, v[2]); v[3] = fmaf(f[x], a.w, v[3]);

@@ -194,8 +194,8 @@ def choose(case, Q, code, scale, top, tile, block, sinks, local, width):
     return out
 
 
-def attend(case, Q, lists, tile, block=1, scale=None):
-    """{(h, row): (O, tolerance)}, the tolerance as cache_ref.attend derives it."""
+def attend(case, Q, lists, tile, block=1, scale=None, hidden=()):
+    """{(h, row): (O, tolerance)}, the tolerance as cache_ref.attend derives it.  hidden: positions left out."""
     G, d = Q.shape[0] // case.H, case.d
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     out = {}
@@ -208,6 +208,7 @@ def attend(case, Q, lists, tile, block=1, scale=None):
             for row in range(int(case.row_start[b]) + i, int(case.row_start[b]) + i + m):
                 p = L - n + row - int(case.row_start[b])
                 j = pos[pos < (cache_ref.ends(p, L, block) if p >= 0 else 0)]
+                j = j[~np.isin(j, list(hidden))]
                 if not len(j):
                     out[h, row] = np.zeros(d), np.zeros(d)
                     continue

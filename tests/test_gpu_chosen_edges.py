@@ -1,0 +1,77 @@
+"""Attention over chosen pages at its borders: scores of -infinity before values that are not finite, large quantised keys, tiles
+larger than a call."""
+import numpy as np
+import pytest
+import torch
+
+import cache_more_ref as ref
+import cache_ref
+from test_gpu_chosen import bf, queries, random_lists, t32
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def dkv():
+    from paper_2608_27922_gb300 import dkv
+    return dkv
+
+
+# ---------------------------------------------------------------- scores of -infinity
+WILD = {"inf": np.inf, "-inf": -np.inf, "nan": np.nan}
+
+
+@pytest.mark.parametrize("wild", list(WILD))
+@pytest.mark.parametrize("page", [0, 2, 97, 188])              # the first, two in the middle, one that some rows see in part
+@pytest.mark.parametrize("tile", [1, 4, 33])
+@pytest.mark.parametrize("run", [0, 1, 24, 110])
+def test_value_behind_a_score_of_minus_infinity(dkv, wild, page, tile, run):
+    """It shows, wherever the work is split: in one place among finite scores, and in a run of pages all of whose scores are
+    -infinity (24: a warp's share of them, 110: a CTA's)."""
+    n, L, d, col = 33, 190 * 16 - 8, 64, 21
+    case = cache_ref.Case([(n, L)], 1, d, 16, "bf16", seed=3)
+    pos = page * 16 + 5
+    first = min(max(page - run // 2, 0), 189 - run)
+    hidden = set(range(first * 16, (first + run) * 16)) | {pos}
+    for p in hidden:
+        case.k[case.table[0, p // 16], 0, p % 16, 0] = -np.inf
+    case.v[case.table[0, page], 0, 5, col] = WILD[wild]
+    Q = cache_ref.bf16(np.abs(queries(case, 1)) + 1.0)
+    lists = np.full((1, n // tile + 1, 190), -1, np.int32)
+    lists[0, :] = np.arange(190)
+    O = case.cache(dkv).attend_chosen(bf(Q), case.device_seqs(dkv), t32(lists), tile=tile).double().cpu().numpy()
+    want = ref.attend(case, Q, lists, tile, hidden=hidden)
+    for (h, row), (o, tol) in want.items():
+        seen = pos <= L - n + row
+        assert np.isfinite(O[h, row, col]) == (not seen), (row, O[h, row, col])
+        rest = np.arange(d) != col if seen else np.ones(d, bool)
+        assert (np.abs(O[h, row] - o) <= tol)[rest].all(), row
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tile", [1, 40])
+@pytest.mark.parametrize("pages", [7, 190])
+def test_all_scores_minus_infinity(dkv, fmt, d, tile, pages):
+    """Zeros, but for a value that is not finite in a place that the row sees."""
+    n, L = 40, pages * 16 - 9
+    case = cache_ref.Case([(n, L)], 1, d, 16, fmt, seed=3)
+    Q = cache_ref.bf16(np.abs(queries(case, 1)) + 1.0)
+    pos, col = (pages - 2) * 16 + 3, 13                        # some rows end before it
+    at = case.table[0, pos // 16], 0, pos % 16
+    if fmt == "bf16":
+        case.k[..., 0] = -np.inf
+        case.v[at][col] = -np.inf
+        cols = [col]
+    else:
+        case.kc[..., 0], case.ks[:] = 0x38, 127                # ones
+        case.vc[at], case.vs[at] = 0x7F, 255
+        Q[..., 0] = -np.inf
+        cols = list(range(d))
+    lists = np.full((1, n // tile + 1, pages), -1, np.int32)
+    lists[0, :] = np.arange(pages)
+    O = case.cache(dkv).attend_chosen(bf(Q), case.device_seqs(dkv), t32(lists), tile=tile).double().cpu().numpy()
+    for row in range(n):
+        bad = cols if pos <= L - n + row else []
+        assert not np.isfinite(O[0, row, bad]).any(), row
+        assert (np.delete(O[0, row], bad) == 0).all(), row
