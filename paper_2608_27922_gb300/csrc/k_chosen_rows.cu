@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
   }
   // codes are met by queries in fp16, each row times a power of two that brings its largest magnitude to 2^14 .. 2^15: what is
   // 2^-28 of that or more stays exact, smaller numbers are off by 2^-39 of it at most
-  float mul[2] = {m.sl2, m.sl2};   // of the columns' scores, times log2(e)
+  float mul[2] = {m.sl2, m.sl2};   // of the columns' scores, into exponents of 2
   if constexpr (E4M3) {
     uint32_t top = 0;   // (bits of magnitudes order like the magnitudes)
 #pragma unroll
@@ -317,6 +317,8 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
       place(st + NH + n, next0[n], next[n]);
       partial = partial || pos0[n] + 16 > all_end;
     }
+    // scores in exponents of 2, rounded before the maximum goes off them: of large ones the rounding alone passes fp32 as an
+    // exponent.  (A scale is multiplied by its row's factor first: the sum of products times one of them may pass fp32 too.)
     float sc[NH][4];
 #pragma unroll
     for (int n = 0; n < NH; ++n) {
@@ -333,13 +335,13 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
         }
         const float f0 = scale_of(ks0[n]), f1 = scale_of(ks1[n]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[n][e] = (sc[n][e] + sd[e]) * (e < 2 ? f0 : f1);
+        for (int e = 0; e < 4; ++e) sc[n][e] = (sc[n][e] + sd[e]) * ((e < 2 ? f0 : f1) * mul[e & 1]);
       } else {
 #pragma unroll
         for (int i = 0; i < D / 16; ++i)
           mma(i & 1 ? sd : sc[n], word(k0[n], 2 * i), word(k1[n], 2 * i), word(k0[n], 2 * i + 1), word(k1[n], 2 * i + 1), Q.w[2 * i], Q.w[2 * i + 1]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sc[n][e] += sd[e];
+        for (int e = 0; e < 4; ++e) sc[n][e] = (sc[n][e] + sd[e]) * m.sl2;
       }
     }
     load_keys(next);
@@ -365,7 +367,6 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
     float alpha[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      mx[e] *= mul[e];
       raise[e] = mx[e] > mrun[e] + RAISE_LOG2 || (mrun[e] == -INFINITY && mx[e] > -INFINITY);
       alpha[e] = raise[e] ? (mrun[e] == -INFINITY ? 0.f : ex2(mrun[e] - mx[e])) : 1.f;
       if (raise[e]) mrun[e] = mx[e];
@@ -387,7 +388,7 @@ __global__ void __launch_bounds__(Cfg<D, E4M3, NARROW>::THREADS, (Cfg<D, E4M3, N
       float p[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        p[e] = ex2(fmaf(sc[n][e], mul[e & 1], mrun[e & 1] == -INFINITY ? 0.f : -mrun[e & 1]));
+        p[e] = ex2(sc[n][e] - (mrun[e & 1] == -INFINITY ? 0.f : mrun[e & 1]));
         l[e & 1] += p[e];
       }
       b0[n] = transpose(pack_bf16(p[0], p[1]));

@@ -488,6 +488,10 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
         }
       }
       const float nm = mrun == -INFINITY ? 0.f : -mrun;   // (a row that has seen nothing yet: all weights 0)
+      // large scores are rounded before the maximum goes off them: in one step the maximum's own rounding, 2^-24 of it, stays
+      // in the exponent
+      const bool large = __any_sync(0xffffffffu, fabsf(nm) > 0x1p24f);
+      const float sl2 = large ? 1.f : j.m.sl2;
       float2 lab = make_float2(0.f, 0.f);
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
@@ -496,9 +500,16 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
         tmem_ld32(sc + half * 64, a);
         tmem_ld32(sc + half * 64 + 32, z);
         tmem_wait_ld();
-        weights(a, j.m.sl2, nm, lab, pk);
+        if (large) {
+#pragma unroll
+          for (int k = 0; k < 32; ++k) {
+            a[k] *= j.m.sl2;
+            z[k] *= j.m.sl2;
+          }
+        }
+        weights(a, sl2, nm, lab, pk);
         tmem_st16(sc + half * 32, pk);
-        weights(z, j.m.sl2, nm, lab, pk);
+        weights(z, sl2, nm, lab, pk);
         tmem_st16(sc + half * 32 + 16, pk);
         tmem_wait_st();
         fence_before_sync();

@@ -1,4 +1,4 @@
-"""Attention over chosen pages at its borders: scores of -infinity before values that are not finite, large quantised keys, tiles
+"""Attention over chosen pages at its borders: scores of -infinity before values that are not finite, large and small scores, tiles
 larger than a call."""
 import numpy as np
 import pytest
@@ -75,3 +75,43 @@ def test_all_scores_minus_infinity(dkv, fmt, d, tile, pages):
         bad = cols if pos <= L - n + row else []
         assert not np.isfinite(O[0, row, bad]).any(), row
         assert (np.delete(O[0, row], bad) == 0).all(), row
+
+
+# ---------------------------------------------------------------- large and small scores
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tile", [1, 4, 33])
+@pytest.mark.parametrize("top", [111, 60, 22])
+def test_large_scores(dkv, fmt, d, tile, top):
+    """Keys of up to 2^120 whose scores fit 32 bits: the values of the two best come out, bit for bit."""
+    case = cache_ref.Case([(33, 300)], 1, d, 16, "e4m3", seed=3)
+    g = np.random.default_rng(0)
+    case.kc[:] = g.integers(0, 56, case.kc.shape)              # 0 .. 0.9
+    case.kc[..., 1:] &= 0x0F                                   # and the others below 2^-5
+    case.ks[:] = 127 + top - 1 + g.integers(0, 2, case.ks.shape)
+    best = 130, 200, 261
+    for i, p in enumerate(best):                               # 256 and 448 times the scale, far above the rest
+        case.kc[case.table[0, p // 16], 0, p % 16, 0], case.ks[case.table[0, p // 16], 0, p % 16] = (0x78, 0x7E, 0x7E)[i], 127 + top
+    case.k, case.fmt = cache_ref.decode(case.kc, case.ks), fmt
+    Q = np.zeros((2, 33, d))
+    Q[..., 0], Q[1, :, 1:] = 2.0, 2.0 ** -6
+    lists = np.full((1, 33 // tile + 1, 19), -1, np.int32)
+    lists[0, :] = np.arange(19)
+    v = cache_ref.bf16(sum(case.v[case.table[0, p // 16], 0, p % 16] for p in best[1:]) / 2)
+    for block in (0, 1):
+        O = case.cache(dkv).attend_chosen(bf(Q[:1]), case.device_seqs(dkv), t32(lists), tile=tile, block=block, scale=0.7)
+        assert np.array_equal(O[0].double().cpu().numpy(), np.broadcast_to(v, (33, d))), block
+    O = case.cache(dkv).attend_chosen(bf(Q[1:]), case.device_seqs(dkv), t32(lists), tile=tile)
+    assert bool(torch.isfinite(O).all())
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("tile", [1, 33])
+def test_small_scale(dkv, fmt, tile):
+    """Queries of zeros or far below one, a tiny scale: the mean of what a row sees."""
+    case = cache_ref.Case([(33, 300)], 1, 64, 16, fmt, seed=4)
+    Q = queries(case, 3)
+    Q[0], Q[1] = 0, cache_ref.bf16(Q[1] * 2.0 ** -110)
+    lists = random_lists(case, tile, 9)
+    O = case.cache(dkv).attend_chosen(bf(Q), case.device_seqs(dkv), t32(lists), tile=tile, scale=1e-12)
+    cache_ref.check(O, ref.attend(case, Q, lists, tile, scale=1e-12))
