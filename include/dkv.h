@@ -623,7 +623,8 @@ dkv_status_t dkv_cache_write_norm_rope(dkv_cache_t cache, const dkv_cache_seqs_t
  * What contradicts itself (a page outside the pool, a held page that refs calls free, a length outside the
  * table, a negative number of tokens) sets the sticky error word (DKV_ERR_DEVICE); too few free pages
  * set it to DKV_ERR_NOMEM.  extend and compact look first and then do nothing at all; fork and release leave out what
- * names no page.  Calls stay inside their buffers in every case.  refs, tables and
+ * names no page.  A page that the tables name more often than refs counts is found only where it is given up more often
+ * than that (its count then stays 0).  Calls stay inside their buffers in every case.  refs, tables and
  * lengths are changed by one call at a time (the caller orders the streams).              */
 typedef struct {
   int32_t* block_table;    /* device [n_seq][max_pages]                                    */

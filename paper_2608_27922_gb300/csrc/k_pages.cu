@@ -452,8 +452,12 @@ __global__ void __launch_bounds__(COPY_THREADS) compact_copy(Pool c, int32_t* re
     const int b = blockIdx.x - groups * c.H, stay = kept[b], n = keep_start[b + 1] - keep_start[b], all = pages_of(c, n);
     for (int k = threadIdx.x; k < max(from.max_pages, to.max_pages); k += COPY_THREADS) {
       const int page = k < from.max_pages ? from.table[(int64_t)b * from.max_pages + k] : -1;
-      if (k < stay) to.table[(int64_t)b * to.max_pages + k] = page;
-      else if (page >= 0) atomicSub(refs + page, 1);
+      if (k < stay) {
+        to.table[(int64_t)b * to.max_pages + k] = page;
+      } else if (page >= 0 && atomicSub(refs + page, 1) <= 0) {   // given up more often than counted
+        atomicAdd(refs + page, 1);
+        fail(c.status, DEV_INCONSISTENT, SITE_REFS);
+      }
       if (k >= all && k < to.max_pages) to.table[(int64_t)b * to.max_pages + k] = -1;
     }
     if (threadIdx.x == 0) to.len[b] = n;
