@@ -731,7 +731,7 @@ typedef struct {
 /* O[h][i] = sum_j softmax_j(scale Q[h][i] . K[j]) V[j] over the positions j < end(p) on the pages that lists[h / (H_q / H)]
  * names for the token's tile (a list ends at its first negative entry).  Arguments, numbers that are not
  * finite, rows that see nothing and rounding as in dkv_cache_attend, the few-row rounding of queries over an e4m3 cache among it
- * (where a tile's tokens and the group's heads make at most 16 rows).  A value that is not finite in a place that a token sees makes
+ * (where the tokens that a tile can have in the call, min(tile, rows), times the group's heads are at most 16).  A value that is not finite in a place that a token sees makes
  * its output infinite or NaN whatever the score, -infinity too; a token whose scores are all -infinity gets zeros otherwise.  Entries that do not ascend or lie
  * behind the sequence's last page set the error word (DKV_ERR_DEVICE); what the tile's tokens get is then unspecified.  */
 dkv_status_t dkv_cache_attend_chosen(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const void* Q, int32_t H_q,

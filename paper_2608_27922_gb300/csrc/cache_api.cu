@@ -63,8 +63,8 @@ bool few_rows(const cache::Pool& c, int Hq, int max_rows) { return (int64_t)max_
 // The same over chosen pages, where the few-row kernel takes 8 rows at a time: 32 tiles over 32 pages of 64 on 8 key heads, few
 // rows against tensor cores: 8 rows 50 us against 53 in bf16 and 36 against 80 in e4m3, 16 rows 93 against 54 and 63
 // against 81, 32 rows 145 against 55 and 116 against 82.  (Small tiles of 12 rows, d = 64, bf16: 181 against 158.)
-bool few_chosen_rows(const cache::Pool& c, int Hq, int tile) {
-  return (int64_t)tile * (Hq / c.H) <= (c.e4m3 ? 16 : 8);
+bool few_chosen_rows(const cache::Pool& c, int Hq, int tokens) {
+  return (int64_t)tokens * (Hq / c.H) <= (c.e4m3 ? 16 : 8);
 }
 
 size_t scratch_of(const cache::Pool& c, int Hq, int max_rows) {
@@ -434,11 +434,11 @@ dkv_status_t dkv_cache_attend_chosen(dkv_cache_t c, const dkv_cache_seqs_t* seqs
   if (st != DKV_OK) return st;
   const float scale = how->scale > 0.f ? how->scale : 1.0f / std::sqrt((float)c->pool.d);
   const cache::Mask m{scale * 1.4426950408889634f, 0, 0, how->block, cache::inverse_of(how->block)};
-  const cache::Chosen ch{lists, how->tile, how->width, rows / how->tile + s.n};
+  const cache::Chosen ch{lists, how->tile, how->width, rows / how->tile + s.n, how->tile < rows ? how->tile : rows};
   OnDevice on(c->device);
   if (!on.ok) return DKV_ERR_CUDA;
   c->last = (cudaStream_t)stream;
-  if (few_chosen_rows(c->pool, H_q, how->tile < rows ? how->tile : rows))
+  if (few_chosen_rows(c->pool, H_q, ch.tokens))
     return status_of(cache::launch_chosen_rows(c->pool, s, q, o, H_q, m, ch, (cudaStream_t)stream));
   return status_of(cache::launch_chosen_tc(c->pool, c->maps, s, q, o, H_q, m, ch, (cudaStream_t)stream));
 }

@@ -238,6 +238,7 @@ struct Choose {
 struct Chosen {
   const int32_t* lists;
   int tile, width, slots;
+  int tokens;   // most of a tile in the call
 };
 cudaError_t choose_set_smem_limits();   // on the current device
 cudaError_t launch_summarise(const Pool& c, const Seqs& s, const int32_t* first, int8_t* code, uint8_t* scale, cudaStream_t st);

@@ -537,7 +537,7 @@ cudaError_t launch_chosen_rows(const Pool& c, const Seqs& s, const Packed& q, co
                                const Chosen& how, cudaStream_t st) {
   const int n_sm = sm_count(), G = Hq / c.H;
   if (n_sm <= 0) return cudaErrorInvalidDevice;
-  const int blocks = (how.tile * G + 7) / 8;
+  const int blocks = (how.tokens * G + 7) / 8;
   // few units: a cluster for each, while its CTAs have 16 steps or more (8 units: 8 CTAs each 12.5 us, 4 14.4, 1 24.7; 64 units: 4 18.5 us, 8
   // 27, 2 23; 256 units: 1 35, 2 45)
   int C = 1;

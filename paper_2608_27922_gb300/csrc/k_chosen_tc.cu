@@ -693,7 +693,7 @@ cudaError_t chosen_tc_set_smem_limits() {
 
 cudaError_t launch_chosen_tc(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
                              const Mask& m, const Chosen& how, cudaStream_t st) {
-  const int G = Hq / c.H, TQ = BQ / G, n_sm = sm_count(), tiles = (how.tile + TQ - 1) / TQ;
+  const int G = Hq / c.H, TQ = BQ / G, n_sm = sm_count(), tiles = (how.tokens + TQ - 1) / TQ;
   if (n_sm <= 0) return cudaErrorInvalidDevice;
   CUtensorMap mq;
   const int64_t dim[4] = {c.d, G, s.rows, c.H};

@@ -1,5 +1,7 @@
 """Attention over chosen pages at its borders: scores of -infinity before values that are not finite, large and small scores, tiles
 larger than a call."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -115,3 +117,55 @@ def test_small_scale(dkv, fmt, tile):
     lists = random_lists(case, tile, 9)
     O = case.cache(dkv).attend_chosen(bf(Q), case.device_seqs(dkv), t32(lists), tile=tile, scale=1e-12)
     cache_ref.check(O, ref.attend(case, Q, lists, tile, scale=1e-12))
+
+
+# ---------------------------------------------------------------- tiles larger than the call
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,n", [(1, 1), (5, 1), (5, 2), (40, 1), (3, 5), (2, 33)])
+def test_tile_larger_than_the_call(dkv, fmt, Hq, n):
+    case = cache_ref.Case([(n, 700)], 1, 128, 16, fmt, seed=4)
+    c, s = case.cache(dkv), case.device_seqs(dkv)
+    sums = dkv.Summaries(c)
+    c.summarise(s, sums, first=t32([0]))
+    Q = queries(case, Hq)
+    code, scale = ref.summaries(case)
+    for tile in (n, n + 1, 64, 128):
+        lists = c.choose(bf(Q), s, sums, 9, tile=tile)
+        want = ref.choose(case, Q, code, scale, 9, tile, 1, 1, 2, lists.shape[-1])
+        assert np.array_equal(lists.cpu().numpy(), want)
+        cache_ref.check(c.attend_chosen(bf(Q), s, lists, tile=tile), ref.attend(case, Q, want, tile))
+    c.sync()
+
+
+class _Node(ctypes.Structure):
+    _fields_ = [("func", ctypes.c_void_p), ("grid", ctypes.c_uint * 3), ("block", ctypes.c_uint * 3), ("shared", ctypes.c_uint),
+                ("params", ctypes.c_void_p), ("extra", ctypes.c_void_p), ("kern", ctypes.c_void_p), ("ctx", ctypes.c_void_p)]
+
+
+def blocks_of(call):
+    """Blocks that a call's one kernel is launched with."""
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph(keep_graph=True)
+    with torch.cuda.graph(graph):
+        call()
+    cu, raw, n = ctypes.CDLL("libcuda.so.1"), ctypes.c_void_p(graph.raw_cuda_graph()), ctypes.c_size_t(0)
+    assert cu.cuGraphGetNodes(raw, None, ctypes.byref(n)) == 0 and n.value == 1
+    node, p = ctypes.c_void_p(), _Node()
+    assert cu.cuGraphGetNodes(raw, ctypes.byref(node), ctypes.byref(n)) == 0
+    assert cu.cuGraphKernelNodeGetParams_v2(node, ctypes.byref(p)) == 0
+    return p.grid[0] * p.grid[1] * p.grid[2]
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,n", [(5, 1), (40, 1), (2, 33)])
+def test_blocks_of_a_tile_larger_than_the_call(dkv, fmt, Hq, n):
+    """The launch goes by the tokens that a tile can have in the call."""
+    case = cache_ref.Case([(n, 700)], 1, 128, 16, fmt, seed=4)
+    c, s = case.cache(dkv), case.device_seqs(dkv)
+    Q = bf(queries(case, Hq))
+    count = []
+    for tile in (n + 1, 128):                                  # one slot either way
+        lists, out = t32(random_lists(case, tile, 9)), torch.empty_like(Q)
+        count.append(blocks_of(lambda: c.attend_chosen(Q, s, lists, tile=tile, out=out)))
+    assert count[0] == count[1], count
