@@ -104,43 +104,67 @@ __host__ __device__ __forceinline__ Seq seq_at(const Pool& c, const Seqs& s, int
 }
 
 // Tiles of new tokens: the slots of sequence b begin at row_start[b] / tile + b, which ascends by 1 or more.
-__host__ __device__ __forceinline__ int first_slot(const Seqs& s, int tile, int b) { return clamp(s.row_start[b], 0, s.rows) / tile + b; }
+__host__ __device__ __forceinline__ int slot_at(const Seqs& s, int tile, int b, int start) { return clamp(start, 0, s.rows) / tile + b; }
+inline int first_slot(const Seqs& s, int tile, int b) { return slot_at(s, tile, b, s.row_start[b]); }   // (host)
 
-// The sequence whose tiles a slot may be one of: the last b with first_slot(b) <= slot (row starts that do not ascend give
-// some sequence).
-__host__ __device__ __forceinline__ int seq_of_slot(const Seqs& s, int tile, int slot) {
-  int lo = 0, hi = s.n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first_slot(s, tile, mid) <= slot) lo = mid; else hi = mid;
+// The search for the sequence whose tiles a slot may be one of, the last b with first_slot(b) <= slot, by 32 lanes that look at
+// sequences evenly apart: it is among [lo, lo + n), and step() == 1 is the last round.  (Row starts that do not ascend give some
+// sequence.)
+struct SlotSearch {
+  int lo, n;
+  __host__ __device__ __forceinline__ int step() const { return (n + 31) / 32; }
+  __host__ __device__ __forceinline__ int at(int lane) const { return lane * step() < n ? lo + lane * step() : lo; }
+  __host__ __device__ __forceinline__ bool past(const Seqs& s, int tile, int slot, int lane, int start) const {
+    return lane * step() < n && slot_at(s, tile, at(lane), start) <= slot;
   }
-  return lo;
+  // mask: the lanes that are past; the one whose sequences are left.
+  __host__ __device__ __forceinline__ int narrow(uint32_t mask) {
+#ifdef __CUDA_ARCH__
+    const int ones = __popc(mask);
+#else
+    const int ones = __builtin_popcount(mask);
+#endif
+    const int k = ones > 0 ? ones - 1 : 0, every = step();   // (k * every < n, whatever the starts hold)
+    lo += k * every;
+    n = every < n - k * every ? every : n - k * every;
+    return k;
+  }
+};
+
+// The search lane by lane, on the host.
+inline int seq_of_slot(const Seqs& s, int tile, int slot) {
+  SlotSearch w{0, s.n};
+  for (;;) {
+    const bool last = w.step() == 1;
+    uint32_t mask = 0;
+    for (int lane = 0; lane < 32; ++lane) mask |= (uint32_t)w.past(s, tile, slot, lane, s.row_start[w.at(lane)]) << lane;
+    w.narrow(mask);
+    if (last) return w.lo;
+  }
 }
 
 #ifdef __CUDACC__
-// The same by a warp, and the sequence itself as the call may use it: the lanes look at 32 sequences at a time (one or two
-// dependent reads instead of one a halving, and the length comes with the last).
+// By a warp, and the sequence itself as the call may use it (one or two dependent reads instead of one a halving, and the length
+// comes with the last).
 __device__ __forceinline__ int seq_of_slot_warp(const Pool& c, const Seqs& s, int tile, int slot, Seq& q) {
   const int lane = threadIdx.x & 31;
-  int lo = 0, n = s.n, start = 0, end = 0, len = 0;
+  SlotSearch w{0, s.n};
+  int start = 0, end = 0, len = 0;
   for (;;) {
-    const int step = (n + 31) / 32, b = min(lo + lane * step, s.n - 1);
+    const bool last = w.step() == 1;
+    const int b = w.at(lane);
     start = __ldg(s.row_start + b);
-    if (step == 1) {
+    if (last) {
       end = __ldg(s.row_start + b + 1);
       len = __ldg(s.len + b);
     }
-    const bool past = lane * step < n && clamp(start, 0, s.rows) / tile + b <= slot;
-    const int k = max(__popc(__ballot_sync(0xffffffffu, past)) - 1, 0);   // (in range whatever the array holds)
-    if (step == 1) {
+    const int k = w.narrow(__ballot_sync(0xffffffffu, w.past(s, tile, slot, lane, start)));
+    if (last) {
       start = __shfl_sync(0xffffffffu, start, k);
       end = __shfl_sync(0xffffffffu, end, k);
       len = __shfl_sync(0xffffffffu, len, k);
-      lo = min(lo + k, s.n - 1);
       break;
     }
-    lo += k * step;
-    n = min(step, n - k * step);
   }
   const int64_t cap = (int64_t)s.max_pages << c.page_log2;
   q.r0 = clamp(start, 0, s.rows);
@@ -148,7 +172,7 @@ __device__ __forceinline__ int seq_of_slot_warp(const Pool& c, const Seqs& s, in
   q.len = clamp(len, 0, (int)cap);
   if (start < 0 || end < start || end > s.rows) fail(c.status, DEV_INCONSISTENT, SITE_ROWS);
   if (len < 0 || len > cap) fail(c.status, DEV_INCONSISTENT, SITE_LEN);
-  return lo;
+  return w.lo;
 }
 #endif
 
@@ -246,7 +270,6 @@ cudaError_t launch_choose(const Pool& c, const Seqs& s, const int8_t* code, cons
                           const Choose& how, int32_t* lists, cudaStream_t st);
 
 cudaError_t chosen_tc_set_smem_limits();   // on the current device
-struct Maps;
 cudaError_t launch_chosen_tc(const Pool& c, const Maps& maps, const Seqs& s, const Packed& q, const Packed& o, int Hq,
                              const Mask& m, const Chosen& how, cudaStream_t st);
 cudaError_t launch_chosen_rows(const Pool& c, const Seqs& s, const Packed& q, const Packed& o, int Hq, const Mask& m,

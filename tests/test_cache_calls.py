@@ -125,6 +125,65 @@ def test_slots_of_tiles(tmp_path):
     assert subprocess.run([str(exe)]).returncode == 0
 
 
+SEARCH = r"""
+#include "cache_internal.h"
+#include <vector>
+using namespace dkv::cache;
+int main() {
+  unsigned r = 3;
+  auto rnd = [&](int m) { r = r * 1664525u + 1013904223u; return (int)((r >> 8) % (unsigned)m); };
+  for (int n : {1, 2, 31, 32, 33, 63, 64, 65, 1000, 1023, 1024, 1025, 1056, 1057, 2049, 4095, 4096})
+    for (int kind = 0; kind < 6; ++kind) {
+      const int tile = kind == 0 ? 1 : 1 + rnd(kind < 3 ? 5 : 128);
+      std::vector<int32_t> start{rnd(2)};
+      for (int b = 0; b < n; ++b) start.push_back(start.back() + (kind == 5 ? 0 : rnd(3) ? rnd(kind == 1 ? 2 : 60) : 0));
+      const int rows = start.back() + rnd(9) + 1;
+      Seqs s{nullptr, nullptr, start.data(), n, 1, rows};
+      for (int slot = 0; slot < rows / tile + n; slot += n > 64 ? 1 + rnd(4) : 1) {
+        int want = 0;
+        for (int lo = 0, hi = n; lo < hi;) {   // the first sequence whose slots begin behind this one
+          const int mid = (lo + hi) / 2;
+          if (start[mid] / tile + mid <= slot) want = mid, lo = mid + 1; else hi = mid;
+        }
+        if (seq_of_slot(s, tile, slot) != want) return 1;
+      }
+      // starts that contradict themselves
+      const int edges[] = {-2147483647 - 1, -1, 0, 5, rows, 2147483647};
+      for (auto& x : start) if (rnd(3) == 0) x = edges[rnd(6)];
+      for (int i = 0; i < 200; ++i) {
+        SlotSearch w{0, n};
+        const int slot = rnd(3) ? rnd(rows / tile + n) : edges[rnd(6)];
+        for (bool last = false; !last;) {
+          last = w.step() == 1;
+          uint32_t mask = 0;
+          for (int lane = 0; lane < 32; ++lane) {
+            const int b = w.at(lane);
+            if (b < w.lo || b >= w.lo + w.n) return 2;
+            mask |= (uint32_t)w.past(s, tile, slot, lane, start[b]) << lane;
+          }
+          const int lo = w.lo, before = w.n, k = w.narrow(mask);
+          if (k < 0 || k > 31 || w.n < 1 || w.lo < lo || w.lo + w.n > lo + before || (last && w.n != 1)) return 3;
+        }
+        if (w.lo < 0 || w.lo >= n) return 4;
+      }
+    }
+  return 0;
+}
+"""
+
+
+def test_search_of_a_slot(tmp_path):
+    """The search that the kernels' warps make, lane by lane: the definition's sequence, or one inside for starts that do not ascend."""
+    try:
+        nvcc = B.nvcc()
+    except RuntimeError:
+        pytest.skip("no nvcc")
+    src, exe = tmp_path / "search.cu", tmp_path / "search"
+    src.write_text(SEARCH)
+    subprocess.check_call([nvcc, *B.ARCH, "-std=c++17", "-I", B.ROOT + "/include", "-I", B.CSRC, str(src), "-o", str(exe)])
+    assert subprocess.run([str(exe)], timeout=120).returncode == 0
+
+
 class _Bar:
     def __init__(self, n):
         self.n = self.c = n
