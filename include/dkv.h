@@ -437,15 +437,17 @@ dkv_status_t dkv_candidate_order_noalloc(const void* K_bank, const float* base, 
 /* ------------------------------------------------------------------------------------
  * Norm and rotation of queries and keys.
  *
- * The backbones norm the queries and keys of each head and rotate them to their token's
- * position before attention reads them and before the window keeps them (App. A,
- * "Attention-logit" setup: keys are post-RoPE).  Both in one pass, for a row x of d values
- * of one head at coordinates c:
+ * Queries and keys are normed and rotated to their token's position before attention reads
+ * them and before the window keeps them (App. A, "Attention-logit" setup: keys are post-RoPE).
+ * Both in one pass, for backbones that norm each head by itself with one weight of d numbers for
+ * all heads; one that norms a token's whole projected row (Wan2.1) does that before and calls
+ * with norm = 0.  For a row x of d values of one head at coordinates c:
  *     y = x w / sqrt(mean(x^2) + eps)                 (norm = 0: y = x)
  *     pair (y0, y1) -> (y0 cos a - y1 sin a, y0 sin a + y1 cos a),   a = c[axis] theta[pair]
  * in fp32, rounded once to bf16 (to nearest, ties to even).  Angles are reduced to one turn in 64-bit whole numbers
  * and off by no more than 2^-22 + |a| 2^-51 radians, at any coordinate.  The squares of a row whose sum passes fp32
- * are taken again at a smaller scale; a row that holds a NaN or an infinity gives NaN.  dkv_bank_admit_rope takes the
+ * are taken again at a smaller scale; a row that holds a NaN or an infinity gives NaN (norm = 0: its pair alone gives NaN or
+ * infinities).  dkv_bank_admit_rope takes the
  * temporal rotation off again.                                                            */
 typedef struct {
   const float* theta;      /* device [d / 2] angular frequency of each rotation pair, finite; 0: not
