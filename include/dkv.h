@@ -654,14 +654,15 @@ dkv_status_t dkv_cache_extend(dkv_cache_t cache, int32_t* refs, const dkv_cache_
 /* Gives back the pages of sequence b all of whose held positions lie in [first[b], last[b]) (device int32 [n_seq]): their
  * entries become -1.  Where last[b] >= seq_len[b] the sequence ends at first[b] (rejected tokens; first = 0: all of
  * it); else its length stays, and later calls must not touch the positions given back (those that a
- * window has left).                                                                       */
+ * window has left).  A sequence that ends inside a page leaves that page's summary (see below) as it was.  */
 dkv_status_t dkv_cache_release(dkv_cache_t cache, int32_t* refs, const dkv_cache_table_t* seqs, const int32_t* first,
                                const int32_t* last, void* stream);
 
 /* Position i of sequence b of `to` := position keep[keep_start[b] + i] of sequence b of `from`, for the positions kept (any
  * order, the same one more than once too); `from` is given up.  Leading pages whose positions all stay in place are
  * kept as they are, the others are fresh ones and their rows copied, so the pool has to hold both for
- * the time being.  Keys keep the rotation that they have.
+ * the time being.  Keys keep the rotation that they have.  Summaries (see below) are of pages, and do not move: the
+ * fresh pages' are those of whoever held them before, until they are made again.
  *   keep : device int32 [n_keep], keep_start : device int32 [n_seq + 1], ascending from 0 to at most n_keep;
  *   0 <= n_keep <= 2^26.  from->n_seq = to->n_seq; tables as for dkv_cache_fork.
  * A kept position outside [0, seq_len[b]) or on a page that was given back is an error (the call does nothing).
@@ -677,7 +678,9 @@ dkv_status_t dkv_cache_compact(dkv_cache_t cache, int32_t* refs, const dkv_cache
  * A long past need not be read whole: an 8-bit mean key of every page and head tells which pages a token's
  * queries point to, and attention reads those.
  *
- *   dkv_cache_summarise       summaries of pages, after their positions have been written
+ *   dkv_cache_summarise       summaries of pages, after their positions have been written, moved (dkv_cache_compact:
+ *                             first = 0) or given up in part (dkv_cache_release of a sequence's end: first = its
+ *                             new length - 1); a choice goes by what it finds there, however old
  *   dkv_cache_choose          for each tile of tokens and key head the pages with the best scores
  *   dkv_cache_attend_chosen   softmax attention over the listed pages
  *
@@ -717,7 +720,8 @@ typedef struct {
  *   - of the other seen pages the `top` with the best scores, equal ones in the order of their numbers.
  * score(page) = max over the tile's tokens and the head's group of queries of (c_q . c_page) 2^(e_q + e_page), with Q's rows in
  * codes of 8 bits like the summaries: whole numbers times powers of two, so every choice is exact.  Queries and pages
- * without codes count as -infinity, so do pages given back, and such a score is not listed.  A tile whose tokens all lie at negative positions has an empty list.
+ * without codes count as -infinity, so do pages given back, and such a score is not listed.  (Local pages and those below
+ * sink_pages are listed in any case: sink_pages is 0 where the first ones have been given back.)  A tile whose tokens all lie at negative positions has an empty list.
  *   Q : device [H_q][rows][d] bf16 as for dkv_cache_attend;  lists : device int32 [H][rows / tile + n_seq][width].  */
 dkv_status_t dkv_cache_choose(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, const dkv_cache_summaries_t* summaries,
                               const void* Q, int32_t H_q, int32_t rows, int64_t q_head_stride, int64_t q_row_stride,

@@ -921,7 +921,8 @@ class PagedCache:
             _check(st, "dkv_cache_extend")
 
     def release(self, refs: torch.Tensor, seqs: PageTable, first: torch.Tensor, last: torch.Tensor, stream=None) -> None:
-        """Gives back the pages whose positions all lie in [first[b], last[b]) (int32); last[b] >= seq_len[b] ends the sequence at first[b]."""
+        """Gives back the pages whose positions all lie in [first[b], last[b]) (int32); last[b] >= seq_len[b] ends the sequence
+        at first[b] (inside a page: its summary is made again by summarise from the new length - 1 on)."""
         _check_i32(first, (seqs.n_seq,), "first", self.device)
         _check_i32(last, (seqs.n_seq,), "last", self.device)
         s, _ = self._on(stream)
@@ -931,7 +932,8 @@ class PagedCache:
 
     def compact(self, refs: torch.Tensor, src: PageTable, keep: torch.Tensor, keep_start: torch.Tensor, dst: PageTable,
                 stream=None) -> None:
-        """Position i of sequence b of dst := position keep[keep_start[b] + i] of sequence b of src (int32); src is given up."""
+        """Position i of sequence b of dst := position keep[keep_start[b] + i] of sequence b of src (int32); src is given up.
+        Summaries of moved pages are made again by summarise(first=0)."""
         _check_i32(keep, (keep.numel(),), "keep", self.device)
         _check_i32(keep_start, (src.n_seq + 1,), "keep_start", self.device)
         s, ctx = self._on(stream)

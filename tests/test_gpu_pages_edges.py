@@ -33,3 +33,48 @@ def test_compact_of_a_page_named_more_often_than_counted(dkv, held):
     x.cache.release(x.refs, to, t32([0] * 3), t32([9] * 3))
     x.cache.sync()
     assert int(x.refs.min()) == 0
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+def test_choice_after_a_move(dkv, fmt):
+    """Compacted sequences, whose moved pages are summarised anew, and one that ends earlier, whose last page is: choices and
+    attention as of the positions that they hold now."""
+    H, d, page = 2, 64, 16
+    x = Both(dkv, 90, H, d, page, "bf16")
+    c = x.cache
+    if fmt == "e4m3":
+        c = x.cache = dkv.PagedCache(H, d, page, 90, "e4m3")
+        x.refs = c.new_refs()
+        x.book = ref.Book(90, page, [p.cpu().numpy() for p in x.pools()])
+    x.start([300, 211], cols=24)
+    seqs = dkv.CacheSeqs(x.table.block_table, x.table.seq_len, t32([0, 300, 511]))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    K, V = (torch.randn(H, 511, d, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    c.write(K, V, seqs)
+    x.book.rows = [p.cpu().numpy() for p in x.pools()]
+    sums = dkv.Summaries(c)
+    c.summarise(seqs, sums)
+    n = [3, 2]
+
+    def look(first):
+        case = cache_ref.Case([(a, L) for a, L in zip(n, x.book.length)], H, d, page, "bf16")
+        case.table, case.n_pages = x.table.block_table.cpu().numpy(), 90
+        k, v = (p.cpu().numpy() for p in x.pools()[:2])
+        if fmt == "e4m3":
+            case.k, case.v = (cache_ref.decode(a, s.cpu().numpy()) for a, s in zip((k, v), x.pools()[2:]))
+        else:
+            case.k, case.v = c.k.double().cpu().numpy(), c.v.double().cpu().numpy()
+        s = dkv.CacheSeqs(x.table.block_table, x.table.seq_len, t32(case.row_start))
+        c.summarise(s, sums, first=t32(first))
+        Q = queries(case, 4)
+        lists = c.choose(bf(Q), s, sums, 4, tile=2)
+        want = ref.choose(case, Q, *ref.summaries(case), 4, 2, 1, 1, 2, lists.shape[-1])
+        assert np.array_equal(lists.cpu().numpy(), want)
+        cache_ref.check(c.attend_chosen(bf(Q), s, lists, tile=2), ref.attend(case, Q, want, 2))
+        c.sync()
+    look([0, 0])
+    x.compact([[j for j in range(300) if j < 40 or j % 3], list(range(30, 211))])
+    look([0, 0])
+    x.release([203, 100], [2 ** 31 - 1] * 2)
+    look([length - 1 for length in x.book.length])
