@@ -119,6 +119,17 @@ def test_small_scale(dkv, fmt, tile):
     cache_ref.check(O, ref.attend(case, Q, lists, tile, scale=1e-12))
 
 
+# ---------------------------------------------------------------- repetition
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,seqs,tile", [(1, [(1, 6000)], 1), (3, [(40, 900), (3, 77)], 16), (4, [(300, 3000)], 128)])
+def test_same_bits_again(dkv, fmt, Hq, seqs, tile):
+    case = cache_ref.Case(seqs, 1, 64, 16, fmt, seed=4)
+    c, s = case.cache(dkv), case.device_seqs(dkv)
+    lists, Q = t32(random_lists(case, tile, 180)), bf(queries(case, Hq))
+    want = c.attend_chosen(Q, s, lists, tile=tile)
+    assert all(torch.equal(want, c.attend_chosen(Q, s, lists, tile=tile)) for _ in range(30))
+
+
 # ---------------------------------------------------------------- tiles larger than the call
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 @pytest.mark.parametrize("Hq,n", [(1, 1), (5, 1), (5, 2), (40, 1), (3, 5), (2, 33)])

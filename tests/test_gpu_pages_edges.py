@@ -35,6 +35,37 @@ def test_compact_of_a_page_named_more_often_than_counted(dkv, held):
     assert int(x.refs.min()) == 0
 
 
+def test_streams_other_than_the_current_one(dkv):
+    """Each call's work and scratch belong to the stream that it is given, a torch stream or a raw handle."""
+    x = Both(dkv, 60, fmt="e4m3")
+    x.start([5, 20, 33], cols=6)
+    side = torch.cuda.Stream()
+    for handle in (side, side.cuda_stream):
+        n = len(x.book.length)
+        add, parents = t32([3] * n), [1, 1, 0, 2][:n + 1]
+        keep = [list(range(0, m + 3, 2)) for m in (x.book.length[p] for p in parents)]
+        start = np.concatenate([[0], np.cumsum([len(k) for k in keep])])
+        args = t32(parents), t32(np.concatenate(keep)), t32(start), t32([10] * len(parents)), t32([2 ** 31 - 1] * len(parents))
+        forked, kept = x.other(len(parents), 6), x.other(len(parents), 6)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        x.cache.extend(x.refs, x.table, add, stream=handle)
+        x.cache.fork(x.refs, x.table, args[0], forked, stream=handle)
+        x.cache.compact(x.refs, forked, args[1], args[2], kept, stream=handle)
+        x.cache.release(x.refs, kept, args[3], args[4], stream=handle)
+        junk = [torch.full((1 << 16,), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(8)]    # (not the calls' scratch)
+        x.book.extend([3] * n)
+        x.book.fork(parents)
+        x.book.compact(keep)
+        x.book.release([10] * len(parents), [2 ** 31 - 1] * len(parents))
+        x.table = kept
+        side.synchronize()
+        x.check()
+        assert all(bool((j == 0x7F).all()) for j in junk)
+    x.cache.sync()
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 def test_choice_after_a_move(dkv, fmt):
     """Compacted sequences, whose moved pages are summarised anew, and one that ends earlier, whose last page is: choices and
