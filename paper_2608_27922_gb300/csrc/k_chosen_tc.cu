@@ -492,6 +492,18 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
       // in the exponent
       const bool large = __any_sync(0xffffffffu, fabsf(nm) > 0x1p24f);
       const float sl2 = large ? 1.f : j.m.sl2;
+      if (large) {
+#pragma unroll 1
+        for (int k0 = 0; k0 < BK; k0 += 32) {
+          float a[32];
+          tmem_ld32(sc + k0, a);
+          tmem_wait_ld();
+#pragma unroll
+          for (int k = 0; k < 32; ++k) a[k] *= j.m.sl2;
+          tmem_st32(sc + k0, reinterpret_cast<uint32_t(&)[32]>(a));
+        }
+        tmem_wait_st();
+      }
       float2 lab = make_float2(0.f, 0.f);
 #pragma unroll 1
       for (int half = 0; half < 2; ++half) {
@@ -500,13 +512,6 @@ __global__ void __launch_bounds__(Lay<D, E4M3>::THREADS, 2)
         tmem_ld32(sc + half * 64, a);
         tmem_ld32(sc + half * 64 + 32, z);
         tmem_wait_ld();
-        if (large) {
-#pragma unroll
-          for (int k = 0; k < 32; ++k) {
-            a[k] *= j.m.sl2;
-            z[k] *= j.m.sl2;
-          }
-        }
         weights(a, sl2, nm, lab, pk);
         tmem_st16(sc + half * 32, pk);
         weights(z, sl2, nm, lab, pk);
