@@ -17,8 +17,11 @@
 // e4m3: the keys' codes become fp16, one conversion for two, and meet queries in fp16; their scales join the scores.  The values'
 // codes are transposed two at a time, a pair of columns in the place of one, and become bf16 with their scales in them.
 //
+// Weights are rounded to bf16 where they meet the values (mma.sync's other operand would have to be fp32 too, at a fraction of the rate);
+// their sum takes them unrounded.
+//
 // Measured: 32 tokens of 40 on 8 heads over 32 pages of 64 in e4m3 36 us (136 MB; 12 us of it with 3 pages: launch, chain, joining), in
-// bf16 49 (269 MB, 5.5 TB/s; 6.8 is a copy's); one token over as many pages of 131,001 positions, 8 heads, 12.5.  (By asynchronous copies
+// bf16 49 (269 MB, 5.5 TB/s; 6.8 is a copy's); one token over as many pages of 131,001 positions, 8 heads, 10 to 12.  (By asynchronous copies
 // into shared memory, two or three steps ahead: 45.)
 #include "attn_math.cuh"
 #include "cache_internal.h"

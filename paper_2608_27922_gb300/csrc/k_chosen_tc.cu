@@ -17,6 +17,10 @@
 // scales in them: code bits in bf16's fields are the value times 2^-120, one product with 2^120 times the scale makes it
 // exact.
 //
+// Weights are rounded to bf16 for the second product, whose values are bf16 and whose rate fp32 weights would cut to a part; their sum takes
+// them unrounded.  A weight is off by 2^-8 of it at most: over a case outputs are 0.0023 from float64, where 32 bits throughout and
+// the outputs' own rounding make 0.0017.
+//
 // Values in places that a row does not see meet its weight 0, and 0 times a NaN or an infinity is NaN: in the tiles that some
 // row does not see whole, the softmax threads clear what is not finite in V's tile, and rows that do see such a value get
 // it back at the end (wild_in).
@@ -24,8 +28,8 @@
 // Measured: 4,680 tokens of 40 heads in tiles of 128, 28 pages of 128 each, in bf16 276 us, 1.24 PFLOP/s of 1.89.  Every tile of
 // tokens reads its own keys, so a key tile serves 128 rows instead of 256 or more: 2.7 GB come through L2 (at 9.7 TB/s; 1.0 GB of
 // it from HBM), and shared memory moves 1,280 cycles' worth of operands and copies a tile and CTA, 2,560 of the 3,200 that two CTAs' tiles
-// take.  A CTA's start and end are 8 of its 50 us.  In e4m3 523 us: the conversion (5,200 of 8,000 instructions a tile).  d = 64: 226 and
-// 322.  Chunks of 333 to 700 tokens of a small model in tiles of 16 (48 of 128 rows used) 47 us: three rounds of CTAs of 11 us.
+// take.  A CTA's start and end are 8 of its 50 us.  In e4m3 436 us: the conversion (5,200 of 8,000 instructions a tile).  d = 64: 224 and
+// 300.  Chunks of 333 to 700 tokens of a small model in tiles of 16 (48 of 128 rows used) 47 us, in e4m3 57.5: three rounds of CTAs of 11 us.
 // (Tiles of 64 keys, two of them in TMEM, so that a tile's softmax overlaps the next one's scores: 290 at d = 128, 212 at 64.)
 #include "attn_math.cuh"
 #include "cache_internal.h"

@@ -9,7 +9,8 @@
 //
 // Measured: 48 continuations forked (3.6 us) and grown (plan 8.5, copies 3.7) 14.5 us in a graph; three prompts on pages of
 // 256, 40 heads, into 64 continuations 50 us, of which the copies 33 (160 MB, read mostly from L2, where the 61 copies of three pages
-// find them); a window of 9,360 positions of two sequences, 40 heads, e4m3, moved together 64 us (look 5, plan 7, rows 49: 6.6 TB/s).
+// find them); a window of 9,360 positions of two sequences, 40 heads, e4m3, moved together 64 us (look 5, plan 7, rows 49: 6.6 TB/s); half of the
+// pages of 48 sequences given back 1.6 us among other launches, of 4,096 sequences of 64 pages 3.6.
 #include "cache_internal.h"
 
 #include <cooperative_groups.h>
