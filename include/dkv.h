@@ -729,7 +729,8 @@ dkv_status_t dkv_cache_choose(dkv_cache_t cache, const dkv_cache_seqs_t* seqs, c
 
 typedef struct {
   float scale;           /* of q.k; <= 0 selects 1 / sqrt(d)                               */
-  int32_t tile;          /* of the lists                                                   */
+  int32_t tile;          /* of the lists; the choice of kernel goes by min(tile, rows) (1 where every
+                            sequence brings one token)                                     */
   int32_t block;         /* as in dkv_cache_attend_t                                       */
   int32_t width;         /* of the lists, 1 .. 1024                                        */
 } dkv_cache_chosen_t;
