@@ -68,7 +68,7 @@ typedef enum {
   DKV_ERR_SHAPE = 2,        /* size outside what the handle / library supports           */
   DKV_ERR_STATE = 3,        /* call out of order (admit twice, compress without admit)   */
   DKV_ERR_CUDA = 4,         /* a CUDA runtime call or launch failed                      */
-  DKV_ERR_NOMEM = 5,        /* workspace smaller than dkv_bank_workspace_size_ex(); pages  */
+  DKV_ERR_NOMEM = 5,        /* workspace smaller than its size call says; too few free pages */
   DKV_ERR_TIMEOUT = 6,      /* a bounded device-side wait gave up (sticky, see sync)     */
   DKV_ERR_UNSUPPORTED = 7,  /* feature not available for this dtype / d / device         */
   DKV_ERR_DEVICE = 8        /* device-side consistency check failed (sticky, see sync)   */
